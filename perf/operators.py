@@ -13,6 +13,7 @@ bits.  ``exact`` restates the definitions in 64 bits.  Matrices of one shape are
 one stack, so that outputs are a handful of tensors however many matrices a list has.
 """
 import math
+import random
 
 import torch
 
@@ -34,7 +35,7 @@ def listed():
         dict(name="orth_adapter_layer", op="orth", kind="adapters", layers=1, hidden=2048, rank=16,
              dtype="f32"),
         # Matrices of odd sizes from a single element to a thousand rows.
-        dict(name="orth_odd", op="orth", kind="odd", sizes=7, count=6, largest=1500, dtype="bf16"),
+        dict(name="orth_odd", op="orth", kind="odd", sizes=7, count=8, largest=1500, dtype="bf16"),
         # The projections of one layer of the 3B-class model, bf16 momentum.
         dict(name="orth_layer_3b", op="orth", kind="decoder", hidden=2048, ffn=11008, kv=256,
              dtype="bf16"),
@@ -79,7 +80,7 @@ def draw(rng):
             c.update(layers=rng.randint(1, 40), hidden=64 * rng.randint(8, 80),
                      rank=rng.choice([4, 8, 16, 32, 64]))
         elif kind == "odd":
-            c.update(sizes=rng.randrange(1 << 20), count=rng.randint(2, 12),
+            c.update(sizes=rng.randrange(1 << 20), count=rng.randint(2, 14),
                      largest=_log_int(rng, 40, 4000))
         elif kind == "decoder":
             hidden = 64 * _log_int(rng, 4, 64)
@@ -105,11 +106,10 @@ def _groups(case):
         n = 4 * case["layers"]
         return [(n, case["rank"], case["hidden"]), (n, case["hidden"], case["rank"])]
     if case["kind"] == "odd":
-        import random
         r = random.Random(case["sizes"])
         return [(1, 1, 1), (1, 1, case["largest"])] + \
-            [(r.randint(1, 3), _log_int(r, 1, case["largest"]), _log_int(r, 1, case["largest"]))
-             for _ in range(case["count"])]
+            [(1, _log_int(r, 1, case["largest"]), _log_int(r, 1, case["largest"]))
+             for _ in range(case["count"])]    # odd sizes: every matrix its own allocation
     if case["kind"] == "one":
         return [(1, case["rows"], case["cols"])]
     h, f, kv = case["hidden"], case["ffn"], case["kv"]
