@@ -21,7 +21,9 @@
  *   f1  fp32-state AdamW for tensors outside the 8-bit slice, and the slice;
  *   f2  the dynamic (non-linear) 8-bit code map;
  *   f3  the bf16 copy of the updated weights;
- *   f4  the gradient norm accumulated as gradients arrive.
+ *   f4  the gradient norm accumulated as gradients arrive;
+ *   f5  orthogonalising matrices by Newton-Schulz products;
+ *   f6  the Muon step with 8-bit momentum.
  *
  * Conventions for every entry point:
  *  - Tensor data, workspace and scalar outputs are DEVICE pointers on the
@@ -472,6 +474,57 @@ lt_err lt_adamw_fp32_step(float* const* params, const void* const* grads, int gr
  */
 lt_err lt_select_8bit_slice(const int64_t* numels, int n_tensors, double fraction,
                             uint8_t* is_8bit, int64_t* n_8bit_params);
+
+/* Bytes of device workspace lt_orthogonalize needs for these matrices; never 0 for a valid
+ * list.  Returns 0 if n_matrices < 0, a list is NULL for n_matrices > 0, or a size is not in
+ * [0, 2^23). */
+size_t lt_orthogonalize_workspace_bytes(const int64_t* rows, const int64_t* cols, int n_matrices);
+
+/*
+ * f5: orthogonalises a list of matrices by Newton-Schulz products, as the Muon optimizer
+ * does with its updates.  For U = matrices[k], dense and row-major with rows[k] x cols[k]
+ * elements of in_dtype: X = U / ||U||_F, then ns_steps (1..64; customarily 5) times
+ *   A = X X^T,  B = -4.7750 A + 2.0315 A A,  X = 3.4445 X + B X
+ * (on the side of the smaller dimension: the same polynomial of the singular values, which
+ * end between about 0.7 and 1.2).  out[k]: device, same shape, out_dtype (LT_DTYPE_F32 or
+ * LT_DTYPE_BF16, as in_dtype), overlapping no other array of the call.
+ * Products take fp16 operands scaled by powers of two and sum in fp32, X is carried with
+ * twice fp16's bits in the linear term: results are 1e-3 to 2e-3 of their 2-norm from the
+ * exact polynomial (bf16 output rounds by as much again).  The norm is a sum in fp64.
+ * A zero matrix gives zeros; one with a NaN or an infinity gives NaN throughout, and leaves
+ * the other matrices of the list alone.
+ * Matrices of one call are worked on together: pass lists, not matrices one by one.
+ */
+lt_err lt_orthogonalize(const void* const* matrices, int in_dtype, void* const* out, int out_dtype,
+                        const int64_t* rows, const int64_t* cols, int n_matrices, int ns_steps,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of device workspace lt_muon_step needs (see lt_orthogonalize_workspace_bytes); 0 also
+ * if block_size is not one the steps take. */
+size_t lt_muon_workspace_bytes(const int64_t* rows, const int64_t* cols, int n_matrices,
+                               int block_size);
+
+/*
+ * f6: one Muon step over a list of matrices with 8-bit block-wise momentum.  params[k]: device
+ * float, rows[k] x cols[k], row-major; grads[k] alike in grad_dtype; m_codes[k] and m_absmax[k]:
+ * the momentum, blocks, maps and codes exactly as lt_hybrid8bit_adamw_step's first moment;
+ * params_bf16, coef, status, step_state and the no-overlap rule as there (of the step state
+ * only whether it lets a step apply is used).  In fp32, products and sums rounded each:
+ *   g = grad * coef,  m1 = beta * m0 + rest * g,  u = beta * m1 + rest * g (nesterov) or m1,
+ * with beta = fp32(momentum), rest = fp32(1 - momentum); m1 is requantized per block; and
+ *   w1 = fma(-rate, O, w * decay),  O = lt_orthogonalize's result for u (in fp32),
+ *   rate = fp32(lr * update_rms * sqrt(max(rows, cols))),  decay = fp32(1 - lr * weight_decay).
+ * O's elements have a root mean square of about 1 / sqrt(max(rows, cols)), so update_rms is
+ * the update's, in units of lr (0.2 is about AdamW's).
+ * lr, weight_decay >= 0, 0 <= momentum < 1, update_rms > 0, all finite; ns_steps in [1, 64].
+ * A skipped step writes nothing but the bf16 copy, which then holds the unchanged weights.
+ */
+lt_err lt_muon_step(float* const* params, const void* const* grads, int grad_dtype,
+                    int8_t* const* m_codes, float* const* m_absmax, uint16_t* const* params_bf16,
+                    const int64_t* rows, const int64_t* cols, int n_matrices, int block_size,
+                    int code_map, double lr, double momentum, int nesterov, double weight_decay,
+                    double update_rms, int ns_steps, const float* coef, const int32_t* status,
+                    const void* step_state, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Copies the device status word to *out and synchronizes `stream` (the only
  * entry point that blocks the host).  An asynchronous device fault from

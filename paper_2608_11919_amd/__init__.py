@@ -17,3 +17,5 @@ from .lazytrain import (  # noqa: F401
     lt_step_state_bytes, lt_step_table, lt_step_state_init, lt_step_state_advance,
     GradNormAccumulator,
     StreamedHybrid8bitAdamW)
+from .muon import (  # noqa: F401
+    lt_muon_step, lt_muon_workspace_bytes, lt_orthogonalize, lt_orthogonalize_workspace_bytes)

@@ -130,6 +130,16 @@ def lib() -> ctypes.CDLL:
     L.lt_select_8bit_slice.argtypes = [i64p, ctypes.c_int, ctypes.c_double,
                                        ctypes.POINTER(ctypes.c_uint8),
                                        ctypes.POINTER(ctypes.c_int64)]
+    L.lt_orthogonalize_workspace_bytes.argtypes = [i64p, i64p, ctypes.c_int]
+    L.lt_orthogonalize_workspace_bytes.restype = ctypes.c_size_t
+    L.lt_orthogonalize.argtypes = [vpp, ctypes.c_int, vpp, ctypes.c_int, i64p, i64p, ctypes.c_int,
+                                   ctypes.c_int, vp, ctypes.c_size_t, vp]
+    L.lt_muon_workspace_bytes.argtypes = [i64p, i64p, ctypes.c_int, ctypes.c_int]
+    L.lt_muon_workspace_bytes.restype = ctypes.c_size_t
+    L.lt_muon_step.argtypes = [vpp, vpp, ctypes.c_int, vpp, vpp, vpp, i64p, i64p, ctypes.c_int,
+                               ctypes.c_int, ctypes.c_int, ctypes.c_double, ctypes.c_double,
+                               ctypes.c_int, ctypes.c_double, ctypes.c_double, ctypes.c_int, vp,
+                               vp, vp, vp, ctypes.c_size_t, vp]
     L.lt_read_status.argtypes = [vp, vp, ctypes.POINTER(ctypes.c_int32)]
     L.lt_set_max_workgroups.argtypes = [ctypes.c_int]
     L.lt_workspace_release.argtypes = [vp]
@@ -140,7 +150,7 @@ def lib() -> ctypes.CDLL:
                  "lt_set_max_workgroups", "lt_streamed_hybrid8bit_adamw_step",
                  "lt_adamw_fp32_step", "lt_select_8bit_slice", "lt_workspace_release",
                  "lt_grad_sqnorm_noalloc", "lt_step_table", "lt_step_state_init",
-                 "lt_step_state_advance"):
+                 "lt_step_state_advance", "lt_orthogonalize", "lt_muon_step"):
         getattr(L, name).restype = ctypes.c_int
     _lib = L
     return L
