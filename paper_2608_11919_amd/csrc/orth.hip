@@ -1,18 +1,33 @@
 // orth.hip -- Newton-Schulz orthogonalisation of a list of matrices, and the Muon step.
 //
-// X_0 = U / ||U||_F; five times (ns_steps) A = X X^T, B = b A + c A A, X = a X + B X, on the
-// side of the smaller dimension (A = X^T X and X B where there are more rows than columns).
-// The singular values of X_0 lie in [0, 1], those of every later X in [0, 1.203]: the
-// polynomial's largest value on [0, 1.203] is f(0.5545) = 1.2024.  Hence |A| <= 1.446 and
-// |B| <= 2.81, and powers of two place every operand in fp16's range: X times 2^15, A and B
-// times 2^14.
+// X_0 = U / ||U||_F; ns_steps times A = X X^T, B = b A + c A A, X = a X + B X, on the side of
+// the smaller dimension (A = X^T X and X B where there are more rows than columns).
 //
-// Products take fp16 operands and sum in fp32.  fp16 has three bits more than bf16 at the
-// same rate.  The linear term a X reads X as a sum of two fp16 numbers: directions whose
-// singular values are far below the largest grow by a factor of a in every step, and one
-// fp16 number loses them against the large ones.  Simulated for Gaussian matrices of 64 to
-// 1024 rows: 1.2e-3 to 2.0e-3 off in 2-norm (bf16 operands: 1.1e-2 to 1.6e-2); for eight strong
-// directions over noise 1.3e-4 (one fp16 X: 1.4e-2, bf16: 0.12).
+// Long matrices take their steps in pairs.  With n the smaller side and m the larger, A and
+// every polynomial of it are n x n and commute, so the second step of a pair needs no new X:
+// with P = a I + B, A' = P A P, and X'' = P' P X.  A pair takes 3 n^2 m + 5 n^3 multiply-adds
+// where two single steps take 6 n^2 m + 2 n^3 (products of symmetric matrices compute half
+// their tiles), and X is written once.  Rounding errors of a pair grow by a^2 in directions of
+// small singular values.  Simulated with the roundings below, single steps and pairs: Gaussian
+// matrices of 64 x 64 1.0e-3 and 1.8e-3 off, 256 x 1024 with strong directions 5.6e-4 and
+// 4.0e-4, eight directions over noise 1.5e-3 and 2.7e-3, a spectrum over three decades 1.9e-3
+// and 3.9e-3 (bf16 operands: 1e-2 to 0.12), rows of scales from 1 to 0.01 at 64 x 64 9e-4 and
+// 5e-3.  So pairs are for matrices that gain by them.  Three steps and more are cheaper still
+// but 7e-3 off and more on such spectra; five diverge.
+//
+// The singular values of X_0 lie in [0, 1], those of every later X in [0, 1.203]: the
+// polynomial's largest value on [0, 1.203] is f(0.5545) = 1.2024.  So the eigenvalues of A lie
+// in [0, 1.446], of B in [-2.81, 0], of P in [0.63, 3.45]; powers of two place every operand in
+// fp16's range: X times 2^15, n x n matrices times 2^14, P' P times 2^12.
+//
+// Products take fp16 operands and sum in fp32: fp16 has three bits more than bf16 at the same
+// rate.  Two things keep what is rounded small.  X enters the linear term as a sum of two fp16
+// numbers: directions whose singular values are far below the largest grow by a factor of a in
+// every step, and one fp16 number loses them against the large ones.  And every n x n matrix is
+// kept without the part that is a multiple of I: S = A - d I with d the eigenvalue that A would
+// have if all were equal (1/n at first, then d' = (a + b d + c d^2)^2 d), and so on for what
+// is made of it.  What is left is small wherever singular values are alike, as they mostly are
+// after a step or two; it halves the error for Gaussian matrices.
 //
 // X is kept three times: its leading half row-major (H) and transposed (T), and the rest
 // row-major (L).  Every product then has its summed index contiguous in both operands.
@@ -34,18 +49,17 @@ using host::round_up;
 using namespace tiles;
 
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
-constexpr float kScaleX = 32768.0f;               // X is stored times 2^15
-constexpr float kGramOut = 1.0f / 65536.0f;       // (2^15)^2 -> 2^14
-constexpr float kSquareOut = kC / 16384.0f;       // (2^14)^2 -> 2^14
-constexpr float kUpdateOut = 1.0f / 16384.0f;     // 2^14 * 2^15 -> 2^15
-constexpr int kTile = 128;                        // output tile, and what sizes are padded to
+constexpr float kScaleX = 32768.0f;  // X is stored times 2^15
+constexpr float kScaleS = 16384.0f;  // n x n matrices times 2^14
+constexpr float kScaleR = 4096.0f;   // products of a pair's two P times 2^12
+constexpr int kTile = 128;           // what sizes are padded to
 constexpr int kThreads = 256;
 constexpr int kPrep = 64;                         // tile of the transposing pass
 
 struct Matrix {
     const void* src;           // the matrix, or the Muon step's update in fp32
     _Float16 *h[2], *t[2], *l[2];
-    _Float16 *a, *b;
+    _Float16* sym[3];          // n x n matrices
     double *partial, *square;  // sums of squares of its units; their sum
     void* out;                 // orthogonalise: the result
     float* w;                  // Muon: weights and their bf16 copy (or null)
@@ -198,108 +212,118 @@ __global__ __launch_bounds__(kThreads) void k_orth_prepare(Gate gate,
 
 // ------------------------------------------------------------- products
 
-// One 128 x 128 output tile by four waves of 64 x 64; a lane ends with
-// acc[i][j][r] = C[64 * (wave / 2) + 16 i + lane % 16][64 * (wave % 2) + 16 j + 4 (lane / 16) + r]
-// (the operands are swapped in the instruction, so that a lane holds consecutive columns).
-struct TileAcc {
-    f32x4 v[4][4];
+typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+
+// The multiples of I at step `step`: of A, of P = a I + B and of P A.
+struct Shift {
+    float d, p;
 };
 
-__device__ inline void tile_step(const uint8_t* p, const uint8_t* q, int wave, int lane,
-                                 TileAcc& acc)
+__device__ inline Shift shift_at(const Matrix& m, int step)
 {
-    i32x4 a[4][2], b[4][2];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        read_chunks(p, 64 * (wave >> 1) + 16 * i, lane, a[i]);
-        read_chunks(q, 64 * (wave & 1) + 16 * i, lane, b[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            acc.v[i][j] = Half::mul<0>(b[j], a[i], acc.v[i][j]);
-}
-
-// P and Q: the tiles' first rows; steps >= 1 of 128 bytes.
-__device__ inline void tile_product(const _Float16* P, int64_t pitch_p, const _Float16* Q,
-                                    int64_t pitch_q, int steps, uint8_t* lds, TileAcc& acc)
-{
-    constexpr int kHalf = 2 * kTile * kStepBytes;
-    const int lane = int(threadIdx.x) & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
-    TileLoad<kTile, kThreads> load_p, load_q;
-    load_p.init(pitch_p * 2, kTile);
-    load_q.init(pitch_q * 2, kTile);
-    const auto* p = reinterpret_cast<const uint8_t*>(P);
-    const auto* q = reinterpret_cast<const uint8_t*>(Q);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            acc.v[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    load_p.issue(p, lds);
-    load_q.issue(q, lds + kTile * kStepBytes);
-    for (int s = 0; s < steps; ++s) {
-        uint8_t* now = lds + (s & 1) * kHalf;
-        uint8_t* next = lds + (~s & 1) * kHalf;
-        wait_loads();
-        __syncthreads();  // the step's tiles are in place, and no wave reads the other buffer
-        if (s + 1 < steps) {
-            load_p.issue(p + int64_t(s + 1) * kStepBytes, next);
-            load_q.issue(q + int64_t(s + 1) * kStepBytes, next + kTile * kStepBytes);
-        }
-        tile_step(now, now + kTile * kStepBytes, wave, lane, acc);
+    Shift s;
+    s.d = 1.0f / float(m.rows < m.cols ? m.rows : m.cols);
+    for (int i = 0;; ++i) {
+        s.p = kA + s.d * (kB + kC * s.d);
+        if (i == step)
+            return s;
+        s.d = s.p * s.p * s.d;
     }
 }
 
-// A = X X^T (or X^T X), or B = b A + c A A: symmetric, tiles on and above the diagonal, each
-// stored on both sides.
-template <bool SQUARE>
-__global__ __launch_bounds__(kThreads) void k_orth_gram(Gate gate,
-                                                        const int64_t* __restrict__ prefix,
-                                                        const Matrix* __restrict__ mats, int first,
-                                                        int n, int from)
+// Products of n x n matrices, all symmetric: tiles on and above the diagonal, each stored on
+// both sides of it.  With S = A - d I, P^ = P - p I, W^ = P A - p d I, R^ = P' P - p' p I:
+enum Sym {
+    kGram,    // S = X X^T - d I (or X^T X)
+    kStep,    // P^ = c S S + (b + 2 c d) S
+    kHalf,    // W^ = P^ S + p S + d P^
+    kNext,    // S' = P^ W^ + p W^ + p d P^
+    kPair,    // R^ = P'^ P^ + p' P^ + p P'^
+};
+
+struct SymArgs {
+    int step;      // the number of Newton-Schulz steps before this one
+    int from;      // which X
+    int m, n, out; // operands and result among sym[]
+};
+
+template <typename Tile, int OP>
+__global__ __launch_bounds__(Tile::kThreads) void k_orth_sym(Gate gate,
+                                                             const int64_t* __restrict__ prefix,
+                                                             const Matrix* __restrict__ mats,
+                                                             int first, int n, SymArgs args)
 {
-    __shared__ __align__(1024) uint8_t lds[4 * kTile * kStepBytes];
+    __shared__ __align__(1024) uint8_t lds[Tile::kLdsBytes];
     if (!descriptors_ok(gate) || !step_applies(gate))
         return;
     const int64_t unit = prefix[first] + blockIdx.x;
     const int k = find_matrix(prefix, first, n, unit);
     const Matrix& m = mats[k];
     const bool wide = m.rows <= m.cols;
-    const int side = wide ? m.rp : m.cp, inner = SQUARE ? side : (wide ? m.cp : m.rp);
+    const int side = wide ? m.rp : m.cp, real = wide ? m.rows : m.cols;
+    const int inner = OP == kGram ? (wide ? m.cp : m.rp) : side;
     // the tile's place in the upper triangle, row by row
-    const int count = side / kTile;
+    const int count = (side + Tile::kRows - 1) / Tile::kRows;
     int left = int(unit - prefix[k]), ti = 0;
     while (left >= count - ti) {
         left -= count - ti;
         ++ti;
     }
-    const int tj = ti + left;
-    const _Float16* x = SQUARE ? m.a : (wide ? m.h[from] : m.t[from]);
-    TileAcc acc;
-    tile_product(x + int64_t(ti) * kTile * inner, inner, x + int64_t(tj) * kTile * inner, inner,
-                 inner / 64, lds, acc);
-    const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
-    _Float16* out = SQUARE ? m.b : m.a;
+    const int r0 = ti * Tile::kRows, c0 = (ti + left) * Tile::kRows;
+    const _Float16* M = OP == kGram ? (wide ? m.h[args.from] : m.t[args.from]) : m.sym[args.m];
+    const _Float16* N = OP == kGram ? M : m.sym[args.n];
+    Tile tile;
+    product_half(tile, M + int64_t(r0) * inner, int64_t(inner) * 2, side - r0,
+                 N + int64_t(c0) * inner, int64_t(inner) * 2, side - c0, inner / 64, lds);
+
+    const Shift s = shift_at(m, args.step);
+    // out = by * sum + at_m * M + at_n * N, in the scales of what is stored
+    float by = 1.0f / kScaleS, at_m = 0.0f, at_n = 0.0f;
+    if constexpr (OP == kGram) {
+        by = kScaleS / (kScaleX * kScaleX);
+    } else if constexpr (OP == kStep) {
+        by = kC / kScaleS;
+        at_m = kB + 2.0f * kC * s.d;
+    } else if constexpr (OP == kHalf) {
+        at_m = s.d;
+        at_n = s.p;
+    } else if constexpr (OP == kNext) {
+        at_m = s.p * s.d;
+        at_n = s.p;
+    } else {
+        by = kScaleR / (kScaleS * kScaleS);
+        const Shift before = shift_at(m, args.step - 1);
+        at_m = before.p * (kScaleR / kScaleS);
+        at_n = s.p * (kScaleR / kScaleS);
+    }
+    _Float16* out = m.sym[args.out];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int row = ti * kTile + 64 * (wave >> 1) + 16 * i + (lane & 15);
+    for (int i = 0; i < Tile::I; ++i) {
+        const int row = r0 + tile.row(i);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int col = tj * kTile + 64 * (wave & 1) + 16 * j + 4 * (lane >> 4);
+        for (int j = 0; j < Tile::J; ++j) {
+            const int col = c0 + tile.col(j);
+            if (row >= side || col >= side)
+                continue;
             const int64_t at = int64_t(row) * side + col;
-            typedef _Float16 half4 __attribute__((ext_vector_type(4)));
-            half4 v, old = {};
-            if constexpr (SQUARE)
-                old = *reinterpret_cast<const half4*>(m.a + at);
+            half4 v, x = {}, y = {};
+            if constexpr (OP != kGram)
+                x = *reinterpret_cast<const half4*>(M + at);
+            if constexpr (OP != kGram && OP != kStep)
+                y = *reinterpret_cast<const half4*>(N + at);
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                v[r] = _Float16(SQUARE ? kSquareOut * acc.v[i][j][r] + kB * float(old[r])
-                                       : kGramOut * acc.v[i][j][r]);
+            for (int r = 0; r < 4; ++r) {
+                float z = by * tile.acc[i][j][r];
+                if constexpr (OP == kGram)
+                    z -= row == col + r && row < real ? s.d * kScaleS : 0.0f;
+                else if constexpr (OP == kStep)
+                    z += at_m * float(x[r]);
+                else
+                    z += at_m * float(x[r]) + at_n * float(y[r]);
+                v[r] = _Float16(z);
+            }
             *reinterpret_cast<half4*>(out + at) = v;
-            if (ti != tj) {
+            if (r0 != c0) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
                     out[int64_t(col + r) * side + row] = v[r];
@@ -308,16 +332,23 @@ __global__ __launch_bounds__(kThreads) void k_orth_gram(Gate gate,
     }
 }
 
-enum Final { kNext, kOutF32, kOutBf16, kWeights };
+enum Final { kAgain, kOutF32, kOutBf16, kWeights };
 
-// X' = a X + B X (or a X + X B): the next X, or where it goes.
-template <int FINAL>
-__global__ __launch_bounds__(kThreads) void k_orth_update(Gate gate,
-                                                          const int64_t* __restrict__ prefix,
-                                                          const Matrix* __restrict__ mats,
-                                                          int first, int n, int from, float decay)
+struct UpdateArgs {
+    int step, steps;  // steps before, and steps applied now: 1 (P) or 2 (P' P)
+    int from, sym;    // which X, and where P^ or R^ is
+    float decay;
+};
+
+// X' = p X + P^ X (or p X + X P^), P standing for P' P after a pair: the next X, or where it
+// goes.
+template <typename Tile, int FINAL>
+__global__ __launch_bounds__(Tile::kThreads) void k_orth_update(Gate gate,
+                                                                const int64_t* __restrict__ prefix,
+                                                                const Matrix* __restrict__ mats,
+                                                                int first, int n, UpdateArgs args)
 {
-    __shared__ __align__(1024) uint8_t lds[4 * kTile * kStepBytes];
+    __shared__ __align__(1024) uint8_t lds[Tile::kLdsBytes];
     if (!descriptors_ok(gate))
         return;
     const bool applies = step_applies(gate);
@@ -327,35 +358,42 @@ __global__ __launch_bounds__(kThreads) void k_orth_update(Gate gate,
     const int k = find_matrix(prefix, first, n, unit);
     const Matrix& m = mats[k];
     const bool wide = m.rows <= m.cols;
-    const int across = m.cp / kTile, tile = int(unit - prefix[k]);
-    const int r0 = tile / across * kTile, c0 = tile % across * kTile;
-    const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
-    TileAcc acc;
+    const int across = (m.cp + Tile::kCols - 1) / Tile::kCols, at_tile = int(unit - prefix[k]);
+    const int r0 = at_tile / across * Tile::kRows, c0 = at_tile % across * Tile::kCols;
+    const int from = args.from;
+    Tile tile;
+    float by = 0.0f, linear = 0.0f;
     if (applies) {
         const int inner = wide ? m.rp : m.cp;
-        const _Float16* P = (wide ? m.b : m.h[from]) + int64_t(r0) * inner;
-        const _Float16* Q = (wide ? m.t[from] : m.b) + int64_t(c0) * inner;
-        tile_product(P, inner, Q, inner, inner / 64, lds, acc);
+        const _Float16* P = (wide ? m.sym[args.sym] : m.h[from]) + int64_t(r0) * inner;
+        const _Float16* Q = (wide ? m.t[from] : m.sym[args.sym]) + int64_t(c0) * inner;
+        product_half(tile, P, int64_t(inner) * 2, m.rp - r0, Q, int64_t(inner) * 2, m.cp - c0,
+                     inner / 64, lds);
+        by = 1.0f / (args.steps == 2 ? kScaleR : kScaleS);
+        linear = shift_at(m, args.step).p;
+        if (args.steps == 2)
+            linear *= shift_at(m, args.step + 1).p;
     } else if (!m.wb) {
         return;
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int row = r0 + 64 * (wave >> 1) + 16 * i + (lane & 15);
+    for (int i = 0; i < Tile::I; ++i) {
+        const int row = r0 + tile.row(i);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int col = c0 + 64 * (wave & 1) + 16 * j + 4 * (lane >> 4);
+        for (int j = 0; j < Tile::J; ++j) {
+            const int col = c0 + tile.col(j);
+            if (row >= m.rp || col >= m.cp)
+                continue;
             const int64_t at = int64_t(row) * m.cp + col;
-            typedef _Float16 half4 __attribute__((ext_vector_type(4)));
             float v[4] = {};
             if (applies) {
                 const half4 h = *reinterpret_cast<const half4*>(m.h[from] + at);
                 const half4 l = *reinterpret_cast<const half4*>(m.l[from] + at);
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    v[r] = kUpdateOut * acc.v[i][j][r] + kA * (float(h[r]) + float(l[r]));
+                    v[r] = by * tile.acc[i][j][r] + linear * (float(h[r]) + float(l[r]));
             }
-            if constexpr (FINAL == kNext) {
+            if constexpr (FINAL == kAgain) {
                 half4 h, l;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
@@ -381,7 +419,7 @@ __global__ __launch_bounds__(kThreads) void k_orth_update(Gate gate,
                     } else {
                         float w = m.w[to];
                         if (applies) {
-                            w = __builtin_fmaf(-m.rate, o, w * decay);
+                            w = __builtin_fmaf(-m.rate, o, w * args.decay);
                             m.w[to] = w;
                         }
                         if (m.wb)
@@ -397,22 +435,34 @@ __global__ __launch_bounds__(kThreads) void k_orth_update(Gate gate,
 
 // The workspace: [tag][prefixes][momentum descriptors][matrices][square sums][partials] and
 // the region that the batches share.
+constexpr int64_t kLargeTiles = 256;  // tiles of 256 x 256 that a launch takes them for
 constexpr int64_t kBatchElems = int64_t(1) << 27;  // padded elements of a batch of several
 
-enum { kPreUnits, kPrePrep, kPreGram, kPreTile, kPrefixes };
+enum { kPreUnits, kPrePrep, kPreSym, kPreTile, kPreSymLarge, kPreTileLarge, kPrefixes };
 
 struct Plan {
     size_t prefix[kPrefixes], momentum, mats, header, squares, partials, region, total;
-    std::vector<int> batch;  // first matrix of each batch, and the list's length
+    std::vector<int> order;    // the list's matrices in the order in which they are worked on
+    std::vector<int> batch;    // first place of each batch, and the list's length
+    std::vector<bool> pairs;   // of each batch: steps are taken in pairs
 };
+
+// Whether a matrix takes its steps in pairs: long ones, for which that saves a sixth of the
+// multiply-adds or more; 128 rows or columns are the least that a tile computes anyway.
+bool in_pairs(int64_t rows, int64_t cols)
+{
+    const int64_t n = std::min(rows, cols), m = std::max(rows, cols);
+    return n >= kTile && m >= 2 * n;
+}
 
 int64_t padded(int64_t x) { return int64_t(round_up(size_t(x), kTile)); }
 
 int64_t units_of(int64_t numel, int64_t span) { return (numel + span - 1) / span; }
 
-// Bytes of a matrix in the region: X in three layouts twice, A and B, the Muon step's update.
+// Bytes of a matrix in the region: X in three layouts twice, three n x n matrices, the Muon
+// step's update.
 struct Place {
-    size_t h[2], t[2], l[2], a, b, u, bytes;
+    size_t h[2], t[2], l[2], sym[3], u, bytes;
 };
 
 Place place(int64_t rows, int64_t cols, bool muon)
@@ -431,8 +481,8 @@ Place place(int64_t rows, int64_t cols, bool muon)
         p.t[i] = take(x);
         p.l[i] = take(x);
     }
-    p.a = take(side * side * 2);
-    p.b = take(side * side * 2);
+    for (int i = 0; i < 3; ++i)
+        p.sym[i] = take(side * side * 2);
     p.u = take(muon ? size_t(rows) * size_t(cols) * 4 : 0);
     p.bytes = at;
     return p;
@@ -454,21 +504,25 @@ Plan make_plan(const int64_t* rows, const int64_t* cols, int K, bool muon, int64
     p.header = at;
     p.squares = round_up(at, 256);
     p.partials = p.squares + round_up(sizeof(double) * size_t(K), 256);
+    for (int pass = 0; pass < 2; ++pass)
+        for (int k = 0; k < K; ++k)
+            if (in_pairs(rows[k], cols[k]) == (pass == 1))
+                p.order.push_back(k);
     int64_t units = 0, elems = 0;
     size_t region = 0, bytes = 0;
-    for (int k = 0; k < K; ++k) {
-        if (rows[k] == 0 || cols[k] == 0) {
-            if (p.batch.empty())
-                p.batch.push_back(k);
-            continue;
-        }
-        units += units_of(rows[k] * cols[k], span);
+    for (int i = 0; i < K; ++i) {
+        const int k = p.order[i];
+        const bool pairs = in_pairs(rows[k], cols[k]);
         const int64_t n = padded(rows[k]) * padded(cols[k]);
-        if (p.batch.empty() || (elems > 0 && elems + n > kBatchElems)) {
-            p.batch.push_back(k);
+        if (p.batch.empty() || pairs != p.pairs.back() || (elems > 0 && elems + n > kBatchElems)) {
+            p.batch.push_back(i);
+            p.pairs.push_back(pairs);
             elems = 0;
             bytes = 0;
         }
+        if (rows[k] == 0 || cols[k] == 0)
+            continue;
+        units += units_of(rows[k] * cols[k], span);
         elems += n;
         bytes += place(rows[k], cols[k], muon).bytes;
         region = std::max(region, bytes);
@@ -505,6 +559,41 @@ struct Call {
     hipStream_t st;
 };
 
+// The product launches of one batch.
+struct Launch {
+    const Gate& gate;
+    const Matrix* mats;
+    int first, n;
+    hipStream_t st;
+    const int64_t* const* dev;  // prefixes on the device and on the host
+    int64_t* const* pre;
+
+    int64_t blocks(int i) const { return pre[i][first + n] - pre[i][first]; }
+
+    template <int OP>
+    void sym(const SymArgs& a) const
+    {
+        if (large(kPreSymLarge))
+            k_orth_sym<Large, OP><<<dim3(uint32_t(blocks(kPreSymLarge))), Large::kThreads, 0, st>>>(
+                gate, dev[kPreSymLarge], mats, first, n, a);
+        else
+            k_orth_sym<Small, OP><<<dim3(uint32_t(blocks(kPreSym))), Small::kThreads, 0, st>>>(
+                gate, dev[kPreSym], mats, first, n, a);
+    }
+    template <int FINAL>
+    void update(const UpdateArgs& a) const
+    {
+        if (large(kPreTileLarge))
+            k_orth_update<Large, FINAL>
+                <<<dim3(uint32_t(blocks(kPreTileLarge))), Large::kThreads, 0, st>>>(
+                    gate, dev[kPreTileLarge], mats, first, n, a);
+        else
+            k_orth_update<Small, FINAL><<<dim3(uint32_t(blocks(kPreTile))), Small::kThreads, 0, st>>>(
+                gate, dev[kPreTile], mats, first, n, a);
+    }
+    bool large(int i) const { return blocks(i) >= kLargeTiles; }
+};
+
 // Descriptors in place, then every batch in turn: `begin` enqueues what leaves the sources
 // and their sums of squares, `fill` completes a matrix's descriptor.
 template <typename Fill, typename Begin>
@@ -525,38 +614,47 @@ lt_err run_batches(const Call& c, float decay, Fill fill, Begin begin)
     auto* partial = reinterpret_cast<double*>(ws + p.partials);
     for (size_t b = 0; b + 1 < p.batch.size(); ++b) {
         uint8_t* at = ws + p.region;
-        for (int k = p.batch[b]; k < p.batch[b + 1]; ++k) {
+        for (int i = p.batch[b]; i < p.batch[b + 1]; ++i) {
+            const int k = p.order[i];  // the i-th matrix of the descriptors
             const int64_t numel = c.rows[k] * c.cols[k];
-            Matrix& m = mats[k];
-            int64_t prep = 0, gram = 0, tile = 0;
+            Matrix& m = mats[i];
+            int64_t grid[kPrefixes] = {};
             if (numel > 0) {
                 const Place x = place(c.rows[k], c.cols[k], c.muon);
-                for (int i = 0; i < 2; ++i) {
-                    m.h[i] = reinterpret_cast<_Float16*>(at + x.h[i]);
-                    m.t[i] = reinterpret_cast<_Float16*>(at + x.t[i]);
-                    m.l[i] = reinterpret_cast<_Float16*>(at + x.l[i]);
+                for (int j = 0; j < 2; ++j) {
+                    m.h[j] = reinterpret_cast<_Float16*>(at + x.h[j]);
+                    m.t[j] = reinterpret_cast<_Float16*>(at + x.t[j]);
+                    m.l[j] = reinterpret_cast<_Float16*>(at + x.l[j]);
                 }
-                m.a = reinterpret_cast<_Float16*>(at + x.a);
-                m.b = reinterpret_cast<_Float16*>(at + x.b);
+                for (int j = 0; j < 3; ++j)
+                    m.sym[j] = reinterpret_cast<_Float16*>(at + x.sym[j]);
                 m.partial = partial;
-                m.square = reinterpret_cast<double*>(ws + p.squares) + k;
+                m.square = reinterpret_cast<double*>(ws + p.squares) + i;
                 m.rows = int32_t(c.rows[k]);
                 m.cols = int32_t(c.cols[k]);
                 m.rp = int32_t(padded(c.rows[k]));
                 m.cp = int32_t(padded(c.cols[k]));
                 m.units = int32_t(units_of(numel, c.span));
-                fill(k, m, momentum[c.muon ? k : 0], reinterpret_cast<float*>(at + x.u));
+                fill(k, m, momentum[c.muon ? i : 0], reinterpret_cast<float*>(at + x.u));
                 partial += m.units;
                 at += x.bytes;
-                const int64_t side = std::min(m.rp, m.cp) / kTile;
-                prep = int64_t(m.rp / kPrep) * (m.cp / kPrep);
-                gram = side * (side + 1) / 2;
-                tile = int64_t(m.rp / kTile) * (m.cp / kTile);
+                const int64_t side = std::min(m.rp, m.cp);
+                const auto triangle = [&](int64_t t) {
+                    const int64_t n = host::ceil_div(side, t);
+                    return n * (n + 1) / 2;
+                };
+                const auto rectangle = [&](int64_t t) {
+                    return host::ceil_div(m.rp, t) * host::ceil_div(m.cp, t);
+                };
+                grid[kPreUnits] = m.units;
+                grid[kPrePrep] = rectangle(kPrep);
+                grid[kPreSym] = triangle(Small::kRows);
+                grid[kPreTile] = rectangle(Small::kRows);
+                grid[kPreSymLarge] = triangle(Large::kRows);
+                grid[kPreTileLarge] = rectangle(Large::kRows);
             }
-            pre[kPreUnits][k + 1] = pre[kPreUnits][k] + m.units;
-            pre[kPrePrep][k + 1] = pre[kPrePrep][k] + prep;
-            pre[kPreGram][k + 1] = pre[kPreGram][k] + gram;
-            pre[kPreTile][k + 1] = pre[kPreTile][k] + tile;
+            for (int j = 0; j < kPrefixes; ++j)
+                pre[j][i + 1] = pre[j][i] + grid[j];
         }
     }
     if (K == 0 || pre[kPreTile][K] == 0)
@@ -577,7 +675,6 @@ lt_err run_batches(const Call& c, float decay, Fill fill, Begin begin)
         const auto blocks = [&](int i) { return pre[i][first + n] - pre[i][first]; };
         if (n == 0 || blocks(kPreTile) == 0)
             continue;
-        const dim3 tiles_(uint32_t(blocks(kPreTile))), grams(uint32_t(blocks(kPreGram)));
         if (lt_err e = begin(gate, dev[kPreUnits], d_momentum, d_mats, first, n,
                              pre[kPreUnits][first], blocks(kPreUnits)))
             return e;
@@ -586,18 +683,28 @@ lt_err run_batches(const Call& c, float decay, Fill fill, Begin begin)
         auto* prep = wide_src ? k_orth_prepare<float> : k_orth_prepare<uint16_t>;
         prep<<<dim3(uint32_t(blocks(kPrePrep))), kThreads, 0, st>>>(gate, dev[kPrePrep], d_mats,
                                                                     first, n);
-        auto* last = c.muon ? k_orth_update<kWeights>
-                            : (c.out_dtype == LT_DTYPE_F32 ? k_orth_update<kOutF32>
-                                                           : k_orth_update<kOutBf16>);
-        for (int s = 0; s < c.ns_steps; ++s) {
-            const int from = s & 1;
-            k_orth_gram<false><<<grams, kThreads, 0, st>>>(gate, dev[kPreGram], d_mats, first, n,
-                                                           from);
-            k_orth_gram<true><<<grams, kThreads, 0, st>>>(gate, dev[kPreGram], d_mats, first, n,
-                                                          from);
-            auto* update = s + 1 < c.ns_steps ? k_orth_update<kNext> : last;
-            update<<<tiles_, kThreads, 0, st>>>(gate, dev[kPreTile], d_mats, first, n, from,
-                                                decay);
+        const Launch launch{gate, d_mats, first, n, st, dev, pre};
+        int from = 0;
+        for (int step = 0; step < c.ns_steps; from ^= 1) {
+            launch.sym<kGram>({step, from, 0, 0, 0});
+            launch.sym<kStep>({step, from, 0, 0, 1});
+            const int now = p.pairs[b] && step + 1 < c.ns_steps ? 2 : 1;
+            if (now == 2) {
+                launch.sym<kHalf>({step, from, 1, 0, 2});
+                launch.sym<kNext>({step, from, 1, 2, 0});
+                launch.sym<kStep>({step + 1, from, 0, 0, 2});
+                launch.sym<kPair>({step + 1, from, 2, 1, 0});
+            }
+            const UpdateArgs args{step, now, from, now == 2 ? 0 : 1, decay};
+            step += now;
+            if (step < c.ns_steps)
+                launch.update<kAgain>(args);
+            else if (c.muon)
+                launch.update<kWeights>(args);
+            else if (c.out_dtype == LT_DTYPE_F32)
+                launch.update<kOutF32>(args);
+            else
+                launch.update<kOutBf16>(args);
         }
         LT_TRY_HIP(hipGetLastError());
     }

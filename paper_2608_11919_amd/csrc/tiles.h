@@ -68,17 +68,85 @@ __device__ inline void read_chunks(const uint8_t* tile, int row16, int lane, i32
 
 // Products of 16-bit floating point; the lane's chunks hold k = 8 * (lane / 16) + 0..7 of the
 // step's first and second 32 values, alike for both operands.
-struct Half {
-    struct Scales {};
-    template <int I>
-    __device__ static inline f32x4 mul(const i32x4 (&a)[2], const i32x4 (&b)[2], f32x4 c)
+__device__ inline f32x4 mul_half(const i32x4 (&a)[2], const i32x4 (&b)[2], f32x4 c)
+{
+    c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a[0]),
+                                               __builtin_bit_cast(half8, b[0]), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a[1]),
+                                                  __builtin_bit_cast(half8, b[1]), c, 0, 0, 0);
+}
+
+// One BM x BN output tile by waves of WM x WN each; lane l of the wave at (wm, wn) ends with
+// acc[i][j][r] = C[wm + 16 i + l % 16][wn + 16 j + 4 (l / 16) + r]
+// (the operands are swapped in the instruction, so that a lane holds consecutive columns).
+template <int BM, int BN, int WM, int WN>
+struct Shape {
+    static constexpr int kRows = BM, kCols = BN, I = WM / 16, J = WN / 16;
+    static constexpr int kWavesAcross = BN / WN, kWaves = BM / WM * kWavesAcross;
+    static constexpr int kThreads = 64 * kWaves;
+    static constexpr int kBufferBytes = (BM + BN) * kStepBytes;
+    static constexpr int kLdsBytes = 2 * kBufferBytes;
+    f32x4 acc[I][J];
+
+    __device__ static inline int wave() { return __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6); }
+    __device__ static inline int lane() { return int(threadIdx.x) & 63; }
+    // this lane's row of block i and first column of block j within the tile
+    __device__ static inline int row(int i) { return wave() / kWavesAcross * WM + 16 * i + (lane() & 15); }
+    __device__ static inline int col(int j)
     {
-        c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a[0]),
-                                                   __builtin_bit_cast(half8, b[0]), c, 0, 0, 0);
-        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a[1]),
-                                                      __builtin_bit_cast(half8, b[1]), c, 0, 0, 0);
+        return wave() % kWavesAcross * WN + 16 * j + 4 * (lane() >> 4);
     }
 };
+
+typedef Shape<128, 128, 64, 64> Small;
+typedef Shape<256, 256, 128, 64> Large;
+
+// The main loop over `steps` >= 1 steps.  P, Q: first rows of the tile's operands, pitches in
+// bytes, of which limit_p and limit_q rows exist.
+template <typename S>
+__device__ inline void product_half(S& c, const void* P, int64_t pitch_p, int64_t limit_p,
+                                    const void* Q, int64_t pitch_q, int64_t limit_q, int steps,
+                                    uint8_t* lds)
+{
+    const int lane = S::lane(), wm = S::wave() / S::kWavesAcross * (16 * S::I),
+              wn = S::wave() % S::kWavesAcross * (16 * S::J);
+    TileLoad<S::kRows, S::kThreads> load_p;
+    TileLoad<S::kCols, S::kThreads> load_q;
+    load_p.init(pitch_p, limit_p);
+    load_q.init(pitch_q, limit_q);
+    const auto* p = static_cast<const uint8_t*>(P);
+    const auto* q = static_cast<const uint8_t*>(Q);
+#pragma unroll
+    for (int i = 0; i < S::I; ++i)
+#pragma unroll
+        for (int j = 0; j < S::J; ++j)
+            c.acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    load_p.issue(p, lds);
+    load_q.issue(q, lds + S::kRows * kStepBytes);
+#pragma unroll 1
+    for (int s = 0; s < steps; ++s) {
+        uint8_t* now = lds + (s & 1) * S::kBufferBytes;
+        uint8_t* next = lds + (~s & 1) * S::kBufferBytes;
+        wait_loads();
+        __syncthreads();  // the step's tiles are in place, and no wave reads the other buffer
+        if (s + 1 < steps) {
+            load_p.issue(p + int64_t(s + 1) * kStepBytes, next);
+            load_q.issue(q + int64_t(s + 1) * kStepBytes, next + S::kRows * kStepBytes);
+        }
+        i32x4 b[S::J][2];
+#pragma unroll
+        for (int j = 0; j < S::J; ++j)
+            read_chunks(now + S::kRows * kStepBytes, wn + 16 * j, lane, b[j]);
+#pragma unroll
+        for (int i = 0; i < S::I; ++i) {
+            i32x4 a[2];
+            read_chunks(now, wm + 16 * i, lane, a);
+#pragma unroll
+            for (int j = 0; j < S::J; ++j)
+                c.acc[i][j] = mul_half(b[j], a, c.acc[i][j]);
+        }
+    }
+}
 
 }  // namespace tiles
 
