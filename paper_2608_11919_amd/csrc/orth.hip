@@ -212,7 +212,6 @@ __global__ __launch_bounds__(kThreads) void k_orth_prepare(Gate gate,
 
 // ------------------------------------------------------------- products
 
-typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 
 // The multiples of I at step `step`: of A, of P = a I + B and of P A.
 struct Shift {
@@ -247,8 +246,56 @@ struct SymArgs {
     int m, n, out; // operands and result among sym[]
 };
 
+// out = by * sum + at_m * M + at_n * N, in the scales of what is stored.
+template <int OP>
+struct SymWriter {
+    static constexpr bool kTurned = true;
+    static constexpr int kSlots = 8;
+    float by, at_m, at_n, diagonal;
+    int64_t pitch;
+    const _Float16 *m, *n;  // at the tile's origin, like the result and its transpose
+    _Float16 *to, *turned;
+    int below, real;        // of the diagonal: the tile's column minus its row, rows that exist
+    bool mirror;
+    half8 x[OP == kGram ? 1 : kSlots], y[OP == kGram || OP == kStep ? 1 : kSlots];
+
+    __device__ inline void fetch(int row, int col, int p)
+    {
+        if constexpr (OP != kGram)
+            x[p] = *reinterpret_cast<const half8*>(m + row * pitch + col);
+        if constexpr (OP != kGram && OP != kStep)
+            y[p] = *reinterpret_cast<const half8*>(n + row * pitch + col);
+    }
+    __device__ inline void store(int row, int col, float (&v)[8], int p)
+    {
+        half8 h;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            v[e] *= by;
+            if constexpr (OP == kGram)
+                v[e] -= row == col + e + below && row < real ? diagonal : 0.0f;
+            else
+                v[e] += at_m * float(x[p][e]);
+            if constexpr (OP != kGram && OP != kStep)
+                v[e] += at_n * float(y[p][e]);
+            h[e] = _Float16(v[e]);
+        }
+        *reinterpret_cast<half8*>(to + row * pitch + col) = h;
+    }
+    __device__ inline void turn(int col, int row, const float (&v)[8]) const
+    {
+        if (!mirror)
+            return;
+        half8 h;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            h[e] = _Float16(v[e]);
+        *reinterpret_cast<half8*>(turned + col * pitch + row) = h;
+    }
+};
+
 template <typename Tile, int OP>
-__global__ __launch_bounds__(Tile::kThreads) void k_orth_sym(Gate gate,
+__global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_orth_sym(Gate gate,
                                                              const int64_t* __restrict__ prefix,
                                                              const Matrix* __restrict__ mats,
                                                              int first, int n, SymArgs args)
@@ -256,80 +303,53 @@ __global__ __launch_bounds__(Tile::kThreads) void k_orth_sym(Gate gate,
     __shared__ __align__(1024) uint8_t lds[Tile::kLdsBytes];
     if (!descriptors_ok(gate) || !step_applies(gate))
         return;
-    const int64_t unit = prefix[first] + blockIdx.x;
+    const int64_t unit = prefix[first] + unit_of_workgroup(Tile::kRun);
     const int k = find_matrix(prefix, first, n, unit);
     const Matrix& m = mats[k];
     const bool wide = m.rows <= m.cols;
     const int side = wide ? m.rp : m.cp, real = wide ? m.rows : m.cols;
     const int inner = OP == kGram ? (wide ? m.cp : m.rp) : side;
-    // the tile's place in the upper triangle, row by row
-    const int count = (side + Tile::kRows - 1) / Tile::kRows;
-    int left = int(unit - prefix[k]), ti = 0;
-    while (left >= count - ti) {
-        left -= count - ti;
-        ++ti;
-    }
-    const int r0 = ti * Tile::kRows, c0 = (ti + left) * Tile::kRows;
+    const TilePlace at_tile =
+        triangle_place(int(unit - prefix[k]), (side + Tile::kRows - 1) / Tile::kRows);
+    const int r0 = at_tile.row * Tile::kRows, c0 = at_tile.col * Tile::kCols;
     const _Float16* M = OP == kGram ? (wide ? m.h[args.from] : m.t[args.from]) : m.sym[args.m];
     const _Float16* N = OP == kGram ? M : m.sym[args.n];
     Tile tile;
-    product_half(tile, M + int64_t(r0) * inner, int64_t(inner) * 2, side - r0,
+    product<Half>(tile, M + int64_t(r0) * inner, int64_t(inner) * 2, side - r0,
                  N + int64_t(c0) * inner, int64_t(inner) * 2, side - c0, inner / 64, lds);
 
     const Shift s = shift_at(m, args.step);
-    // out = by * sum + at_m * M + at_n * N, in the scales of what is stored
-    float by = 1.0f / kScaleS, at_m = 0.0f, at_n = 0.0f;
+    SymWriter<OP> out = {};
+    out.by = 1.0f / kScaleS;
     if constexpr (OP == kGram) {
-        by = kScaleS / (kScaleX * kScaleX);
+        out.by = kScaleS / (kScaleX * kScaleX);
     } else if constexpr (OP == kStep) {
-        by = kC / kScaleS;
-        at_m = kB + 2.0f * kC * s.d;
+        out.by = kC / kScaleS;
+        out.at_m = kB + 2.0f * kC * s.d;
     } else if constexpr (OP == kHalf) {
-        at_m = s.d;
-        at_n = s.p;
+        out.at_m = s.d;
+        out.at_n = s.p;
     } else if constexpr (OP == kNext) {
-        at_m = s.p * s.d;
-        at_n = s.p;
+        out.at_m = s.p * s.d;
+        out.at_n = s.p;
     } else {
-        by = kScaleR / (kScaleS * kScaleS);
+        out.by = kScaleR / (kScaleS * kScaleS);
         const Shift before = shift_at(m, args.step - 1);
-        at_m = before.p * (kScaleR / kScaleS);
-        at_n = s.p * (kScaleR / kScaleS);
+        out.at_m = before.p * (kScaleR / kScaleS);
+        out.at_n = s.p * (kScaleR / kScaleS);
     }
-    _Float16* out = m.sym[args.out];
-#pragma unroll
-    for (int i = 0; i < Tile::I; ++i) {
-        const int row = r0 + tile.row(i);
-#pragma unroll
-        for (int j = 0; j < Tile::J; ++j) {
-            const int col = c0 + tile.col(j);
-            if (row >= side || col >= side)
-                continue;
-            const int64_t at = int64_t(row) * side + col;
-            half4 v, x = {}, y = {};
-            if constexpr (OP != kGram)
-                x = *reinterpret_cast<const half4*>(M + at);
-            if constexpr (OP != kGram && OP != kStep)
-                y = *reinterpret_cast<const half4*>(N + at);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                float z = by * tile.acc[i][j][r];
-                if constexpr (OP == kGram)
-                    z -= row == col + r && row < real ? s.d * kScaleS : 0.0f;
-                else if constexpr (OP == kStep)
-                    z += at_m * float(x[r]);
-                else
-                    z += at_m * float(x[r]) + at_n * float(y[r]);
-                v[r] = _Float16(z);
-            }
-            *reinterpret_cast<half4*>(out + at) = v;
-            if (r0 != c0) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    out[int64_t(col + r) * side + row] = v[r];
-            }
-        }
-    }
+    if (r0 + Tile::wave_row() >= side || c0 + Tile::wave_col() >= side)
+        return;  // sizes are multiples of 128: a wave's block lies inside or outside
+    out.pitch = side;
+    out.m = M + int64_t(r0) * side + c0;
+    out.n = N + int64_t(r0) * side + c0;
+    out.to = m.sym[args.out] + int64_t(r0) * side + c0;
+    out.turned = m.sym[args.out] + int64_t(c0) * side + r0;
+    out.diagonal = s.d * kScaleS;
+    out.below = c0 - r0;
+    out.real = real - r0;
+    out.mirror = r0 != c0;
+    finish(tile, lds, out);
 }
 
 enum Final { kAgain, kOutF32, kOutBf16, kWeights };
@@ -340,10 +360,114 @@ struct UpdateArgs {
     float decay;
 };
 
+typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+
+// The rest of k_orth_update: X' = by * sum + linear * X and where it goes.
+template <int FINAL>
+struct UpdateWriter {
+    static constexpr bool kTurned = FINAL == kAgain;
+    static constexpr int kSlots = 8;
+    float by, linear, rate, decay;
+    bool applies, whole;      // whole: eight results are in one aligned piece of the caller's rows
+    const _Float16 *h, *l;    // X at the tile's origin, and X'
+    _Float16 *next_h, *next_l, *next_t;
+    int64_t pitch, pitch_t;
+    int rows, cols, width;    // results that exist from the tile's origin on; the caller's pitch
+    float* out;               // the result in fp32 or the weights, at the tile's origin
+    uint16_t* out16;          // in bf16, or null
+    half8 x[kSlots], y[kSlots];
+    float w[FINAL == kWeights ? kSlots : 1][8];
+
+    __device__ inline void fetch(int row, int col, int p)
+    {
+        if (applies) {
+            x[p] = *reinterpret_cast<const half8*>(h + row * pitch + col);
+            y[p] = *reinterpret_cast<const half8*>(l + row * pitch + col);
+        }
+        if constexpr (FINAL == kWeights) {
+            const float* from = out + int64_t(row) * width + col;
+            if (whole) {
+                if (row < rows && col < cols) {
+                    const f32x4 a = *reinterpret_cast<const f32x4*>(from);
+                    const f32x4 b = *reinterpret_cast<const f32x4*>(from + 4);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        w[p][e] = a[e], w[p][4 + e] = b[e];
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    w[p][e] = row < rows && col + e < cols ? from[e] : 0.0f;
+            }
+        }
+    }
+    __device__ inline void store(int row, int col, float (&v)[8], int p)
+    {
+        if (applies) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                v[e] = by * v[e] + linear * (float(x[p][e]) + float(y[p][e]));
+        }
+        if constexpr (FINAL == kAgain) {
+            half8 hi, lo;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                hi[e] = _Float16(v[e]);
+                lo[e] = _Float16(v[e] - float(hi[e]));
+            }
+            *reinterpret_cast<half8*>(next_h + row * pitch + col) = hi;
+            *reinterpret_cast<half8*>(next_l + row * pitch + col) = lo;
+            return;
+        }
+        if (row >= rows || col >= cols)
+            return;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            v[e] *= 1.0f / kScaleX;
+            if constexpr (FINAL == kWeights)
+                v[e] = applies ? __builtin_fmaf(-rate, v[e], w[p][e] * decay) : w[p][e];
+        }
+        const int64_t to = int64_t(row) * width + col;
+        const bool wide = FINAL == kOutF32 || (FINAL == kWeights && applies);
+        const bool narrow = FINAL == kOutBf16 || (FINAL == kWeights && out16);
+        if (whole) {
+            if (wide) {
+                *reinterpret_cast<f32x4*>(out + to) = f32x4{v[0], v[1], v[2], v[3]};
+                *reinterpret_cast<f32x4*>(out + to + 4) = f32x4{v[4], v[5], v[6], v[7]};
+            }
+            if (narrow) {
+                u16x8 b;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    b[e] = bf16_bits(v[e]);
+                *reinterpret_cast<u16x8*>(out16 + to) = b;
+            }
+            return;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (col + e >= cols)
+                break;
+            if (wide)
+                out[to + e] = v[e];
+            if (narrow)
+                out16[to + e] = bf16_bits(v[e]);
+        }
+    }
+    __device__ inline void turn(int col, int row, const float (&v)[8]) const
+    {
+        half8 hi;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            hi[e] = _Float16(v[e]);
+        *reinterpret_cast<half8*>(next_t + col * pitch_t + row) = hi;
+    }
+};
+
 // X' = p X + P^ X (or p X + X P^), P standing for P' P after a pair: the next X, or where it
 // goes.
 template <typename Tile, int FINAL>
-__global__ __launch_bounds__(Tile::kThreads) void k_orth_update(Gate gate,
+__global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_orth_update(Gate gate,
                                                                 const int64_t* __restrict__ prefix,
                                                                 const Matrix* __restrict__ mats,
                                                                 int first, int n, UpdateArgs args)
@@ -354,12 +478,14 @@ __global__ __launch_bounds__(Tile::kThreads) void k_orth_update(Gate gate,
     const bool applies = step_applies(gate);
     if (!applies && FINAL != kWeights)
         return;
-    const int64_t unit = prefix[first] + blockIdx.x;
+    const int64_t unit = prefix[first] + unit_of_workgroup(Tile::kRun);
     const int k = find_matrix(prefix, first, n, unit);
     const Matrix& m = mats[k];
     const bool wide = m.rows <= m.cols;
-    const int across = (m.cp + Tile::kCols - 1) / Tile::kCols, at_tile = int(unit - prefix[k]);
-    const int r0 = at_tile / across * Tile::kRows, c0 = at_tile % across * Tile::kCols;
+    const TilePlace at_tile =
+        tile_place(int(unit - prefix[k]), (m.rp + Tile::kRows - 1) / Tile::kRows,
+                   (m.cp + Tile::kCols - 1) / Tile::kCols);
+    const int r0 = at_tile.row * Tile::kRows, c0 = at_tile.col * Tile::kCols;
     const int from = args.from;
     Tile tile;
     float by = 0.0f, linear = 0.0f;
@@ -367,7 +493,7 @@ __global__ __launch_bounds__(Tile::kThreads) void k_orth_update(Gate gate,
         const int inner = wide ? m.rp : m.cp;
         const _Float16* P = (wide ? m.sym[args.sym] : m.h[from]) + int64_t(r0) * inner;
         const _Float16* Q = (wide ? m.t[from] : m.sym[args.sym]) + int64_t(c0) * inner;
-        product_half(tile, P, int64_t(inner) * 2, m.rp - r0, Q, int64_t(inner) * 2, m.cp - c0,
+        product<Half>(tile, P, int64_t(inner) * 2, m.rp - r0, Q, int64_t(inner) * 2, m.cp - c0,
                      inner / 64, lds);
         by = 1.0f / (args.steps == 2 ? kScaleR : kScaleS);
         linear = shift_at(m, args.step).p;
@@ -376,59 +502,35 @@ __global__ __launch_bounds__(Tile::kThreads) void k_orth_update(Gate gate,
     } else if (!m.wb) {
         return;
     }
-#pragma unroll
-    for (int i = 0; i < Tile::I; ++i) {
-        const int row = r0 + tile.row(i);
-#pragma unroll
-        for (int j = 0; j < Tile::J; ++j) {
-            const int col = c0 + tile.col(j);
-            if (row >= m.rp || col >= m.cp)
-                continue;
-            const int64_t at = int64_t(row) * m.cp + col;
-            float v[4] = {};
-            if (applies) {
-                const half4 h = *reinterpret_cast<const half4*>(m.h[from] + at);
-                const half4 l = *reinterpret_cast<const half4*>(m.l[from] + at);
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    v[r] = by * tile.acc[i][j][r] + linear * (float(h[r]) + float(l[r]));
-            }
-            if constexpr (FINAL == kAgain) {
-                half4 h, l;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    h[r] = _Float16(v[r]);
-                    l[r] = _Float16(v[r] - float(h[r]));
-                    m.t[from ^ 1][int64_t(col + r) * m.rp + row] = h[r];
-                }
-                *reinterpret_cast<half4*>(m.h[from ^ 1] + at) = h;
-                *reinterpret_cast<half4*>(m.l[from ^ 1] + at) = l;
-            } else {
-                if (row >= m.rows)
-                    continue;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    if (col + r >= m.cols)
-                        continue;
-                    const int64_t to = int64_t(row) * m.cols + col + r;
-                    const float o = v[r] * (1.0f / kScaleX);
-                    if constexpr (FINAL == kOutF32) {
-                        static_cast<float*>(m.out)[to] = o;
-                    } else if constexpr (FINAL == kOutBf16) {
-                        static_cast<uint16_t*>(m.out)[to] = bf16_bits(o);
-                    } else {
-                        float w = m.w[to];
-                        if (applies) {
-                            w = __builtin_fmaf(-m.rate, o, w * args.decay);
-                            m.w[to] = w;
-                        }
-                        if (m.wb)
-                            m.wb[to] = bf16_bits(w);
-                    }
-                }
-            }
-        }
+    if (r0 + Tile::wave_row() >= m.rp || c0 + Tile::wave_col() >= m.cp)
+        return;  // sizes are multiples of 128: a wave's block lies inside or outside
+    UpdateWriter<FINAL> out = {};
+    out.by = by;
+    out.linear = linear;
+    out.rate = m.rate;
+    out.decay = args.decay;
+    out.applies = applies;
+    out.whole = m.cols % 8 == 0;
+    const int64_t at = int64_t(r0) * m.cp + c0, to = int64_t(r0) * m.cols + c0;
+    out.h = m.h[from] + at;
+    out.l = m.l[from] + at;
+    out.next_h = m.h[from ^ 1] + at;
+    out.next_l = m.l[from ^ 1] + at;
+    out.next_t = m.t[from ^ 1] + int64_t(c0) * m.rp + r0;
+    out.pitch = m.cp;
+    out.pitch_t = m.rp;
+    out.rows = m.rows - r0;
+    out.cols = m.cols - c0;
+    out.width = m.cols;
+    if constexpr (FINAL == kWeights) {
+        out.out = m.w + to;
+        out.out16 = m.wb ? m.wb + to : nullptr;
+    } else if constexpr (FINAL == kOutF32) {
+        out.out = static_cast<float*>(m.out) + to;
+    } else if constexpr (FINAL == kOutBf16) {
+        out.out16 = static_cast<uint16_t*>(m.out) + to;
     }
+    finish(tile, lds, out);
 }
 
 // ---------------------------------------------------------------- host side

@@ -4,8 +4,10 @@
 // Operands move in bytes: a step of the loop takes 128 bytes of every row (64 fp16 or 128
 // fp8 values), from HBM straight into LDS (16 bytes a lane, no registers in between), into
 // one of two buffers while the other is multiplied.  Row r keeps its 16-byte chunk c at
-// position c ^ (r & 7): the eight rows that one LDS cycle serves then fall on different
-// banks, and the load writes LDS in lane order by permuting what each lane fetches.
+// position c ^ (r / 2 & 7): LDS serves 256 bytes a cycle, two rows wide, so the sixteen rows that
+// one cycle reads at 16 bytes each must differ in position from one pair of rows to the next
+// (by r & 7 every read took twice its cycles).  The load writes LDS in lane order, by permuting
+// what each lane fetches.
 #ifndef LAZYTRAIN_TILES_H
 #define LAZYTRAIN_TILES_H
 
@@ -39,111 +41,276 @@ struct TileLoad {
         for (int i = 0; i < N; ++i) {
             const int q = i * THREADS + int(threadIdx.x);
             int64_t r = q >> 3;
-            const int chunk = (q & 7) ^ int(r & 7);
+            const int chunk = (q & 7) ^ int(r >> 1 & 7);
             r = r < limit ? r : limit - 1;
             offset[i] = uint32_t(r * pitch) + uint32_t(chunk * 16);
         }
     }
-    __device__ inline void issue(const uint8_t* src, uint8_t* lds) const
+    // the i-th of the N copies of this lane
+    __device__ inline void issue(int i, const uint8_t* src, uint8_t* lds) const
     {
         const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            __builtin_amdgcn_global_load_lds(
-                (const LT_GLOBAL void*)(src + offset[i]),
-                (LT_LDS void*)(lds + (i * THREADS + wave * 64) * 16), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((const LT_GLOBAL void*)(src + offset[i]),
+                                         (LT_LDS void*)(lds + (i * THREADS + wave * 64) * 16), 16,
+                                         0, 0);
     }
 };
 
+// Every LDS read and every copy into LDS that the wave has under way is complete.
+__device__ inline void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 __device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
-// A lane's two 16-byte chunks of row `row16 + lane % 16`: chunks lane / 16 and lane / 16 + 4.
-__device__ inline void read_chunks(const uint8_t* tile, int row16, int lane, i32x4 (&c)[2])
+// The 32 x 32 instructions: a lane holds 32 bytes of row `l % 32` of a block of 32 rows for
+// each 64 bytes of the summed index, of which it takes 16-byte chunks l / 32 and l / 32 + 2 of
+// four (any assignment does that is the same for both operands).
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+struct Chunks {
+    i32x4 c[2];
+};
+
+__device__ inline i32x4 read_chunk(const uint8_t* tile, int row32, int half, int c, int lane)
 {
-    const uint8_t* row = tile + (row16 + (lane & 15)) * kStepBytes;
-    const int at = ((lane >> 4) ^ (lane & 7)) << 4;
-    c[0] = *reinterpret_cast<const i32x4*>(row + at);
-    c[1] = *reinterpret_cast<const i32x4*>(row + (at ^ 64));
+    const uint8_t* row = tile + (row32 + (lane & 31)) * kStepBytes;
+    const int at = ((4 * half + 2 * c + (lane >> 5)) ^ (lane >> 1 & 7)) << 4;
+    return *reinterpret_cast<const i32x4*>(row + at);
 }
 
-// Products of 16-bit floating point; the lane's chunks hold k = 8 * (lane / 16) + 0..7 of the
-// step's first and second 32 values, alike for both operands.
-__device__ inline f32x4 mul_half(const i32x4 (&a)[2], const i32x4 (&b)[2], f32x4 c)
-{
-    c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a[0]),
-                                               __builtin_bit_cast(half8, b[0]), c, 0, 0, 0);
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a[1]),
-                                                  __builtin_bit_cast(half8, b[1]), c, 0, 0, 0);
-}
+// Products of fp16: 32 values a half step, in two instructions.
+struct Half {
+    static constexpr int kInstructions = 2;
+    __device__ static inline f32x16 mul(int t, const Chunks& a, const Chunks& b, f32x16 c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, a.c[t]),
+                                                      __builtin_bit_cast(half8, b.c[t]), c, 0, 0,
+                                                      0);
+    }
+};
 
 // One BM x BN output tile by waves of WM x WN each; lane l of the wave at (wm, wn) ends with
-// acc[i][j][r] = C[wm + 16 i + l % 16][wn + 16 j + 4 (l / 16) + r]
+// acc[i][j][4 g + r] = C[wm + 32 i + l % 32][wn + 32 j + 8 g + 4 (l / 32) + r]
 // (the operands are swapped in the instruction, so that a lane holds consecutive columns).
 template <int BM, int BN, int WM, int WN>
 struct Shape {
-    static constexpr int kRows = BM, kCols = BN, I = WM / 16, J = WN / 16;
+    static constexpr int kRows = BM, kCols = BN, I = WM / 32, J = WN / 32;
     static constexpr int kWavesAcross = BN / WN, kWaves = BM / WM * kWavesAcross;
     static constexpr int kThreads = 64 * kWaves;
+    static constexpr int kWavesPerSimd = WM * WN > 64 * 128 ? 1 : 2;  // at this many registers
     static constexpr int kBufferBytes = (BM + BN) * kStepBytes;
     static constexpr int kLdsBytes = 2 * kBufferBytes;
-    f32x4 acc[I][J];
+    static constexpr int kRun = 32 * (kWavesPerSimd == 2 ? 2 : 1);  // tiles an XCD's 32 CUs hold
+    f32x16 acc[I][J];
 
     __device__ static inline int wave() { return __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6); }
     __device__ static inline int lane() { return int(threadIdx.x) & 63; }
-    // this lane's row of block i and first column of block j within the tile
-    __device__ static inline int row(int i) { return wave() / kWavesAcross * WM + 16 * i + (lane() & 15); }
-    __device__ static inline int col(int j)
-    {
-        return wave() % kWavesAcross * WN + 16 * j + 4 * (lane() >> 4);
-    }
+    __device__ static inline int wave_row() { return wave() / kWavesAcross * WM; }
+    __device__ static inline int wave_col() { return wave() % kWavesAcross * WN; }
+    // this lane's row of block i, and the first of its four columns g of block j, in the tile
+    __device__ static inline int row(int i) { return wave_row() + 32 * i + (lane() & 31); }
+    __device__ static inline int col(int j, int g) { return wave_col() + 32 * j + 8 * g + 4 * (lane() >> 5); }
 };
 
+// The work unit of this workgroup.  Workgroups go to the eight XCDs in turn, each with an L2 of
+// its own; units are dealt out so that an XCD works on `run` consecutive units at a time (as
+// many as it holds workgroups), which tile_place makes neighbours that share operands.
+__device__ inline int64_t unit_of_workgroup(int run)
+{
+    const uint32_t n = gridDim.x, b = blockIdx.x, round = 8u * uint32_t(run);
+    const uint32_t base = b / round * round, here = min(round, n - base);
+    const uint32_t x = b % 8u, i = (b - base) / 8u;
+    return int64_t(base + x * (here / 8u) + min(x, here % 8u) + i);
+}
+
+// Row and column of the t-th tile of `down` x `across`: strips of eight rows, column by column.
+struct TilePlace {
+    int row, col;
+};
+
+constexpr int kStrip = 8;
+
+__device__ inline TilePlace tile_place(int t, int down, int across)
+{
+    const int strip = t / (kStrip * across), first = strip * kStrip;
+    const int high = min(kStrip, down - first), left = t - first * across;
+    return {first + left % high, left / high};
+}
+
+// The same for the tiles on and above the diagonal of side x side.
+__device__ inline TilePlace triangle_place(int t, int side)
+{
+    int first = 0;
+    for (;; first += kStrip) {
+        const int high = min(kStrip, side - first);
+        const int corner = high * (high + 1) / 2, all = corner + (side - first - high) * high;
+        if (t >= all) {
+            t -= all;
+            continue;
+        }
+        if (t >= corner)
+            return {first + (t - corner) % high, first + high + (t - corner) / high};
+        int col = 0;
+        while (t > col)
+            t -= ++col;
+        return {first + t, first + col};
+    }
+}
+
 typedef Shape<128, 128, 64, 64> Small;
-typedef Shape<256, 256, 128, 64> Large;
+typedef Shape<256, 256, 128, 128> Large;
 
 // The main loop over `steps` >= 1 steps.  P, Q: first rows of the tile's operands, pitches in
 // bytes, of which limit_p and limit_q rows exist.
-template <typename S>
-__device__ inline void product_half(S& c, const void* P, int64_t pitch_p, int64_t limit_p,
-                                    const void* Q, int64_t pitch_q, int64_t limit_q, int steps,
-                                    uint8_t* lds)
+//
+// A step runs in two halves, and the operands of one half come out of LDS while the other is
+// multiplied.  Between them every wave has all of the step in registers: one barrier there
+// frees the buffer, and the copy of the step after next starts, a whole step before it is read.
+// The loop has no branches: past the end it copies and reads the last step again, unused.
+template <typename Mul, typename S>
+__device__ inline void product(S& c, const void* P, int64_t pitch_p, int64_t limit_p,
+                               const void* Q, int64_t pitch_q, int64_t limit_q, int steps,
+                               uint8_t* lds)
 {
-    const int lane = S::lane(), wm = S::wave() / S::kWavesAcross * (16 * S::I),
-              wn = S::wave() % S::kWavesAcross * (16 * S::J);
+    constexpr int I = S::I, J = S::J;
+    const int lane = S::lane(), wm = S::wave_row(), wn = S::wave_col();
     TileLoad<S::kRows, S::kThreads> load_p;
     TileLoad<S::kCols, S::kThreads> load_q;
     load_p.init(pitch_p, limit_p);
     load_q.init(pitch_q, limit_q);
     const auto* p = static_cast<const uint8_t*>(P);
     const auto* q = static_cast<const uint8_t*>(Q);
+    constexpr int kLoads = load_p.N + load_q.N, kReads = 2 * (I + J);
+    constexpr int kMuls = I * J * Mul::kInstructions, kPaced = kMuls * 3 / 4;
+    // the k-th share of n things spread over the first three quarters of the products: the last
+    // quarter covers the latency of the reads
+    const auto share = [](int n, int k) { return k < kPaced ? n * k / kPaced : n; };
+    const auto load = [&](int s, int k) {
+        uint8_t* to = lds + (s & 1) * S::kBufferBytes;
+        const int64_t at = int64_t(s < steps ? s : steps - 1) * kStepBytes;
+        if (k < load_p.N)
+            load_p.issue(k, p + at, to);
+        else
+            load_q.issue(k - load_p.N, q + at, to + S::kRows * kStepBytes);
+    };
+    struct Operands {
+        Chunks a[I], b[J];
+    } x0, x1;
+    const auto read = [&](int s, int half, int k, Operands& x) {
+        const uint8_t* from = lds + (s & 1) * S::kBufferBytes;
+        const int c = k / (I + J), n = k % (I + J);
+        if (n < J)
+            x.b[n].c[c] = read_chunk(from + S::kRows * kStepBytes, wn + 32 * n, half, c, lane);
+        else
+            x.a[n - J].c[c] = read_chunk(from, wm + 32 * (n - J), half, c, lane);
+    };
+    // The products of one half step, with what the next one needs issued evenly between them.
+    // Every border keeps its place: left to itself the compiler issues reads right before the
+    // products that wait for them, and products of the second half ahead of the barrier.
+    const auto multiply = [&](const Operands& x, auto between) {
 #pragma unroll
-    for (int i = 0; i < S::I; ++i)
+        for (int k = 0; k < kMuls; ++k) {
+            between(k);
+            const int t = k / (I * J), i = k / J % I, j = k % J;
+            c.acc[i][j] = Mul::mul(t, x.b[j], x.a[i], c.acc[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
 #pragma unroll
-        for (int j = 0; j < S::J; ++j)
-            c.acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    load_p.issue(p, lds);
-    load_q.issue(q, lds + S::kRows * kStepBytes);
+    for (int i = 0; i < I; ++i)
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                c.acc[i][j][r] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 2 * kLoads; ++k)
+        load(k / kLoads, k % kLoads);
+    wait_loads();
+    __builtin_amdgcn_s_barrier();
+#pragma unroll
+    for (int k = 0; k < kReads; ++k)
+        read(0, 0, k, x0);
 #pragma unroll 1
     for (int s = 0; s < steps; ++s) {
-        uint8_t* now = lds + (s & 1) * S::kBufferBytes;
-        uint8_t* next = lds + (~s & 1) * S::kBufferBytes;
+        multiply(x0, [&](int k) {
+#pragma unroll
+            for (int r = share(kReads, k); r < share(kReads, k + 1); ++r)
+                read(s, 1, r, x1);
+        });
+        wait_reads();
         wait_loads();
-        __syncthreads();  // the step's tiles are in place, and no wave reads the other buffer
-        if (s + 1 < steps) {
-            load_p.issue(p + int64_t(s + 1) * kStepBytes, next);
-            load_q.issue(q + int64_t(s + 1) * kStepBytes, next + S::kRows * kStepBytes);
+        __builtin_amdgcn_s_barrier();  // the next step is in place, this one's buffer is free
+        multiply(x1, [&](int k) {
+#pragma unroll
+            for (int r = share(kLoads, k); r < share(kLoads, k + 1); ++r)
+                load(s + 2, r);
+#pragma unroll
+            for (int r = share(kReads, k); r < share(kReads, k + 1); ++r)
+                read(s + 1, 0, r, x0);
+        });
+    }
+    wait_loads();
+    __builtin_amdgcn_s_barrier();  // nothing is on its way into LDS any more
+}
+
+// What follows the main loop, for one wave's block, 32 rows at a time through LDS (the loop is
+// done with it): a lane then has eight consecutive columns of a row, so that a wave reads and
+// writes whole lines, and the code is a few short loops.  From the registers as they come a lane
+// has four columns of 32 rows: accesses of 16 bytes a row, unrolled to 36 to 118 KB of code.
+// Writer w:
+//   w.fetch(row, col, p)     requests what results [row][col .. col + 8) need, into slot p;
+//   w.store(row, col, v, p)  takes the sums v, leaves the results there and stores them;
+//   w.turn(col, row, v)      with kTurned: stores results [row .. row + 8)[col] of the transpose.
+// Rows and columns count from the tile's origin.
+template <typename S, typename Writer>
+__device__ inline void finish(const S& c, uint8_t* lds, Writer& w)
+{
+    constexpr int W = 32 * S::J, kAcross = W / 8, kDown = 64 / kAcross, kPasses = 32 / kDown;
+    constexpr int kPitch = W + 4;
+    static_assert(S::kWaves * 32 * kPitch * 4 <= S::kLdsBytes, "every wave's rows fit");
+    static_assert(kPasses <= Writer::kSlots, "a slot for every pass");
+    float* mine = reinterpret_cast<float*>(lds) + S::wave() * 32 * kPitch;
+    const int lane = S::lane(), down = lane / kAcross, across = lane % kAcross * 8;
+    const int r0 = S::wave_row(), c0 = S::wave_col();
+#pragma unroll
+    for (int i = 0; i < S::I; ++i) {
+#pragma unroll
+        for (int p = 0; p < kPasses; ++p)
+            w.fetch(r0 + 32 * i + p * kDown + down, c0 + across, p);
+#pragma unroll
+        for (int jg = 0; jg < 4 * S::J; ++jg) {
+            const int j = jg / 4, g = jg % 4;
+            *reinterpret_cast<f32x4*>(mine + (lane & 31) * kPitch + 32 * j + 8 * g +
+                                      4 * (lane >> 5)) =
+                f32x4{c.acc[i][j][4 * g], c.acc[i][j][4 * g + 1], c.acc[i][j][4 * g + 2],
+                      c.acc[i][j][4 * g + 3]};
         }
-        i32x4 b[S::J][2];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-        for (int j = 0; j < S::J; ++j)
-            read_chunks(now + S::kRows * kStepBytes, wn + 16 * j, lane, b[j]);
+        for (int p = 0; p < kPasses; ++p) {
+            float* at = mine + (p * kDown + down) * kPitch + across;
+            float v[8];
 #pragma unroll
-        for (int i = 0; i < S::I; ++i) {
-            i32x4 a[2];
-            read_chunks(now, wm + 16 * i, lane, a);
+            for (int e = 0; e < 8; ++e)
+                v[e] = at[e];
+            w.store(r0 + 32 * i + p * kDown + down, c0 + across, v, p);
+            if constexpr (Writer::kTurned) {
 #pragma unroll
-            for (int j = 0; j < S::J; ++j)
-                c.acc[i][j] = mul_half(b[j], a, c.acc[i][j]);
+                for (int e = 0; e < 8; ++e)
+                    at[e] = v[e];
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if constexpr (Writer::kTurned) {
+#pragma unroll
+            for (int q = 0; q < W / 16; ++q) {
+                const int col = q * 16 + lane / 4, row = lane % 4 * 8;
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    v[e] = mine[(row + e) * kPitch + col];
+                w.turn(c0 + col, r0 + 32 * i + row, v);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
     }
 }
