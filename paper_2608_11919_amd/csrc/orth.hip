@@ -533,6 +533,245 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_orth_up
     finish(tile, lds, out);
 }
 
+// ---------------------------------------------------------------- thin matrices
+//
+// A matrix with n <= 32 rows (or columns) and at most 2^17 elements, by one workgroup in one
+// launch: with G = X X^T, every step stays n x n (P = a I + b G + c G G, G' = P G P, R' = P R),
+// and the result is R X.  Adapters, small layers and odd leftovers come in hundreds, and the
+// general path would pad each to 128 and take 18 launches.  Its arithmetic is small (17
+// products of n x n); what it waits for is one workgroup's reads, twice over X, and the steps
+// one after the other.  An error of G grows by a^2 with every step in directions of small
+// singular values, 2e5 in five: G and the steps are in 64 bits (in 32 a 64 x 64 matrix with a
+// few strong directions ends 5e-3 off), R X in 32.
+
+constexpr int kThinThreads = 512;
+constexpr int kThinSide = 32;
+constexpr int64_t kThinElems = int64_t(1) << 17;
+
+typedef double f64x4 __attribute__((ext_vector_type(4)));
+
+template <int NP>
+struct Thin {
+    static constexpr int kWidth = NP == 16 ? 1024 : 256;  // columns of X at a time
+    static constexpr int kPitch = kWidth + 4, kSidePitch = NP + 2, kBlocks = NP / 16;
+    typedef double Sym[NP][kSidePitch];
+    float x[NP][kPitch];
+    Sym sym[4];
+    double red[kThinThreads / 64];
+};
+
+// dst = alpha * M N + beta * N + gamma * I, all symmetric; every wave takes some blocks of 16.
+// The 64-bit instruction leaves row 4 t + lane / 16 and column lane % 16 in a lane's t-th result.
+template <int NP>
+__device__ inline void thin_product(typename Thin<NP>::Sym& dst, const typename Thin<NP>::Sym& M,
+                                    const typename Thin<NP>::Sym& N, double alpha, double beta,
+                                    double gamma)
+{
+    constexpr int kBlocks = NP / 16;
+    const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
+    const int r = lane & 15, q = lane >> 4;
+    for (int b = wave; b < kBlocks * kBlocks; b += kThinThreads / 64) {
+        const int bi = b / kBlocks * 16, bj = b % kBlocks * 16;
+        f64x4 acc = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+        for (int k = 0; k < NP; k += 4)
+            acc = __builtin_amdgcn_mfma_f64_16x16x4f64(M[bi + r][k + q], N[bj + r][k + q], acc, 0,
+                                                       0, 0);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int i = bi + 4 * t + q, j = bj + r;
+            dst[i][j] = alpha * acc[t] + beta * N[i][j] + (i == j ? gamma : 0.0);
+        }
+    }
+    __syncthreads();
+}
+
+// Columns [k0, k0 + kWidth) of X (zeros outside it) into LDS.
+template <int NP, typename T>
+__device__ inline void thin_load(Thin<NP>& t, const Matrix& m, bool wide, int k0, double by)
+{
+    constexpr int W = Thin<NP>::kWidth;
+    const int n = wide ? m.rows : m.cols, len = wide ? m.cols : m.rows;
+    const T* src = static_cast<const T*>(m.src);
+#pragma unroll 8
+    for (int e = threadIdx.x; e < NP * W; e += kThinThreads) {
+        const int i = wide ? e / W : e % NP, k = wide ? e % W : e / NP;
+        const int at = k0 + k;
+        float v = 0.0f;
+        if (i < n && at < len)
+            v = float(double(load_value(src + (wide ? i * len + at : at * n + i))) * by);
+        t.x[i][k] = v;
+    }
+    __syncthreads();
+}
+
+template <int NP, typename T, int FINAL>
+__global__ __launch_bounds__(kThinThreads) void k_orth_thin(Gate gate,
+                                                            const Matrix* __restrict__ mats,
+                                                            int first, int steps, int summed,
+                                                            float decay)
+{
+    constexpr int W = Thin<NP>::kWidth, kBlocks = Thin<NP>::kBlocks, kWaves = kThinThreads / 64;
+    __shared__ __align__(16) Thin<NP> t;
+    if (!descriptors_ok(gate))
+        return;
+    const bool applies = step_applies(gate);
+    const Matrix& m = mats[first + blockIdx.x];
+    const bool wide = m.rows <= m.cols;
+    const int n = wide ? m.rows : m.cols, len = wide ? m.cols : m.rows, numel = n * len;
+    if (numel == 0)
+        return;
+    if (!applies) {
+        if (FINAL == kWeights && m.wb)
+            for (int e = threadIdx.x; e < numel; e += kThinThreads)
+                m.wb[e] = bf16_bits(m.w[e]);
+        return;
+    }
+    const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
+    const int r = lane & 15, q = lane >> 4;
+
+    // the norm: from the momentum pass's sums, or from X itself
+    double sq = 0.0;
+    if (summed) {
+        for (int i = threadIdx.x; i < m.units; i += kThinThreads)
+            sq += m.partial[i];
+    } else {
+        const T* src = static_cast<const T*>(m.src);
+#pragma unroll 8
+        for (int e = threadIdx.x; e < numel; e += kThinThreads) {
+            const double x = load_value(src + e);
+            sq += x * x;
+        }
+    }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1)
+        sq += __shfl_xor(sq, o, 64);
+    if (lane == 0)
+        t.red[wave] = sq;
+    __syncthreads();
+    sq = 0.0;
+    for (int i = 0; i < kWaves; ++i)
+        sq += t.red[i];
+    const double by = isfinite(sq) ? (sq == 0.0 ? 0.0 : 1.0 / sqrt(sq)) : __builtin_nan("");
+
+    // G, each wave over its columns of every piece
+    f64x4 g[kBlocks][kBlocks] = {};
+    for (int k0 = 0; k0 < len; k0 += W) {
+        thin_load<NP, T>(t, m, wide, k0, by);
+        for (int k = wave * (W / kWaves); k < (wave + 1) * (W / kWaves); k += 16) {
+            f32x4 x[kBlocks];
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+                x[b] = *reinterpret_cast<const f32x4*>(&t.x[16 * b + r][k + 4 * q]);
+#pragma unroll
+            for (int a = 0; a < kBlocks; ++a)
+#pragma unroll
+                for (int b = a; b < kBlocks; ++b)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        g[a][b] = __builtin_amdgcn_mfma_f64_16x16x4f64(
+                            double(x[a][e]), double(x[b][e]), g[a][b], 0, 0, 0);
+        }
+        __syncthreads();
+    }
+    for (int w = 0; w < kWaves; ++w) {  // one after the other: the sum has a fixed order
+        if (wave == w) {
+#pragma unroll
+            for (int a = 0; a < kBlocks; ++a)
+#pragma unroll
+                for (int b = a; b < kBlocks; ++b)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        double* to = &t.sym[0][16 * a + 4 * e + q][16 * b + r];
+                        *to = w > 0 ? *to + g[a][b][e] : g[a][b][e];
+                    }
+        }
+        __syncthreads();
+    }
+    for (int e = threadIdx.x; e < NP * NP; e += kThinThreads)
+        if (e / NP / 16 > e % NP / 16)
+            t.sym[0][e / NP][e % NP] = t.sym[0][e % NP][e / NP];
+    __syncthreads();
+
+    int G = 0, P = 1, R = 2, S = 3;
+    for (int step = 0; step < steps; ++step) {
+        thin_product<NP>(t.sym[P], t.sym[G], t.sym[G], 2.0315, -4.7750, 3.4445);
+        if (step > 0) {
+            thin_product<NP>(t.sym[S], t.sym[P], t.sym[R], 1.0, 0.0, 0.0);
+            const int old = R;
+            R = S;
+            S = old;
+        }
+        if (step + 1 < steps) {
+            thin_product<NP>(t.sym[S], t.sym[P], t.sym[G], 1.0, 0.0, 0.0);
+            thin_product<NP>(t.sym[G], t.sym[S], t.sym[P], 1.0, 0.0, 0.0);
+        }
+        if (step == 0) {
+            const int old = R;
+            R = P;
+            P = old;
+        }
+    }
+
+    // R X, blocks of 16 columns in turn
+    f32x4 a[kBlocks][kBlocks];
+#pragma unroll
+    for (int bi = 0; bi < kBlocks; ++bi)
+#pragma unroll
+        for (int bk = 0; bk < kBlocks; ++bk)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                a[bi][bk][e] = float(t.sym[R][16 * bi + r][16 * bk + 4 * q + e]);
+    for (int k0 = 0; k0 < len; k0 += W) {
+        if (len > W)
+            thin_load<NP, T>(t, m, wide, k0, by);
+        for (int k = 16 * wave; k < W && k0 + k < len; k += 16 * kWaves) {
+            f32x4 acc[kBlocks] = {};
+#pragma unroll
+            for (int bk = 0; bk < kBlocks; ++bk)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float x = t.x[16 * bk + 4 * q + e][k + r];
+#pragma unroll
+                    for (int bi = 0; bi < kBlocks; ++bi)
+                        acc[bi] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[bi][bk][e], x, acc[bi], 0,
+                                                                       0, 0);
+                }
+            const int col = k0 + k + r;
+            float w[kBlocks][4] = {};
+#pragma unroll
+            for (int bi = 0; bi < kBlocks; ++bi)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int i = 16 * bi + 4 * q + e;
+                    if (FINAL == kWeights && i < n && col < len)
+                        w[bi][e] = m.w[wide ? i * len + col : col * n + i];
+                }
+#pragma unroll
+            for (int bi = 0; bi < kBlocks; ++bi)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int i = 16 * bi + 4 * q + e;
+                    if (i >= n || col >= len)
+                        continue;
+                    const int to = wide ? i * len + col : col * n + i;
+                    const float o = acc[bi][e];
+                    if constexpr (FINAL == kOutF32) {
+                        static_cast<float*>(m.out)[to] = o;
+                    } else if constexpr (FINAL == kOutBf16) {
+                        static_cast<uint16_t*>(m.out)[to] = bf16_bits(o);
+                    } else {
+                        const float v = __builtin_fmaf(-m.rate, o, w[bi][e] * decay);
+                        m.w[to] = v;
+                        if (m.wb)
+                            m.wb[to] = bf16_bits(v);
+                    }
+                }
+        }
+        __syncthreads();
+    }
+}
+
 // ---------------------------------------------------------------- host side
 
 // The workspace: [tag][prefixes][momentum descriptors][matrices][square sums][partials] and
@@ -546,15 +785,20 @@ struct Plan {
     size_t prefix[kPrefixes], momentum, mats, header, squares, partials, region, total;
     std::vector<int> order;    // the list's matrices in the order in which they are worked on
     std::vector<int> batch;    // first place of each batch, and the list's length
-    std::vector<bool> pairs;   // of each batch: steps are taken in pairs
+    std::vector<int> way;      // of each batch: how its matrices are worked on
 };
 
-// Whether a matrix takes its steps in pairs: long ones, for which that saves a sixth of the
-// multiply-adds or more; 128 rows or columns are the least that a tile computes anyway.
-bool in_pairs(int64_t rows, int64_t cols)
+// How a matrix is worked on.  Thin ones by one workgroup each, by the smaller side up to 16 or
+// 32.  Long ones take their steps in pairs, which saves a sixth of the multiply-adds or
+// more; 128 rows or columns are the least that a tile computes anyway.
+enum { kThin16, kThin32, kSingle, kPairs, kWays };
+
+int way_of(int64_t rows, int64_t cols)
 {
     const int64_t n = std::min(rows, cols), m = std::max(rows, cols);
-    return n >= kTile && m >= 2 * n;
+    if (n <= kThinSide && n * m <= kThinElems)
+        return n <= 16 ? kThin16 : kThin32;
+    return n >= kTile && m >= 2 * n ? kPairs : kSingle;
 }
 
 int64_t padded(int64_t x) { return int64_t(round_up(size_t(x), kTile)); }
@@ -570,8 +814,9 @@ struct Place {
 Place place(int64_t rows, int64_t cols, bool muon)
 {
     Place p;
-    const size_t x = round_up(size_t(padded(rows)) * size_t(padded(cols)) * 2, 256);
-    const size_t side = size_t(std::min(padded(rows), padded(cols)));
+    const bool thin = way_of(rows, cols) <= kThin32;  // X and the rest are in LDS
+    const size_t x = thin ? 0 : size_t(padded(rows)) * size_t(padded(cols)) * 2;
+    const size_t side = thin ? 0 : size_t(std::min(padded(rows), padded(cols)));
     size_t at = 0;
     const auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -606,19 +851,19 @@ Plan make_plan(const int64_t* rows, const int64_t* cols, int K, bool muon, int64
     p.header = at;
     p.squares = round_up(at, 256);
     p.partials = p.squares + round_up(sizeof(double) * size_t(K), 256);
-    for (int pass = 0; pass < 2; ++pass)
+    for (int way = 0; way < kWays; ++way)
         for (int k = 0; k < K; ++k)
-            if (in_pairs(rows[k], cols[k]) == (pass == 1))
+            if (way_of(rows[k], cols[k]) == way)
                 p.order.push_back(k);
     int64_t units = 0, elems = 0;
     size_t region = 0, bytes = 0;
     for (int i = 0; i < K; ++i) {
         const int k = p.order[i];
-        const bool pairs = in_pairs(rows[k], cols[k]);
-        const int64_t n = padded(rows[k]) * padded(cols[k]);
-        if (p.batch.empty() || pairs != p.pairs.back() || (elems > 0 && elems + n > kBatchElems)) {
+        const int way = way_of(rows[k], cols[k]);
+        const int64_t n = way <= kThin32 ? rows[k] * cols[k] : padded(rows[k]) * padded(cols[k]);
+        if (p.batch.empty() || way != p.way.back() || (elems > 0 && elems + n > kBatchElems)) {
             p.batch.push_back(i);
-            p.pairs.push_back(pairs);
+            p.way.push_back(way);
             elems = 0;
             bytes = 0;
         }
@@ -695,6 +940,30 @@ struct Launch {
     }
     bool large(int i) const { return blocks(i) >= kLargeTiles; }
 };
+
+template <int NP>
+void launch_thin_side(const Gate& gate, const Matrix* mats, int first, int n, const Call& c,
+                      float decay)
+{
+    const bool wide_src = c.muon || c.in_dtype == LT_DTYPE_F32;
+    auto* kernel = c.muon ? k_orth_thin<NP, float, kWeights>
+                   : c.out_dtype == LT_DTYPE_F32
+                       ? (wide_src ? k_orth_thin<NP, float, kOutF32>
+                                   : k_orth_thin<NP, uint16_t, kOutF32>)
+                       : (wide_src ? k_orth_thin<NP, float, kOutBf16>
+                                   : k_orth_thin<NP, uint16_t, kOutBf16>);
+    kernel<<<dim3(uint32_t(n)), kThinThreads, 0, c.st>>>(gate, mats, first, c.ns_steps, c.muon,
+                                                         decay);
+}
+
+void launch_thin(int way, const Gate& gate, const Matrix* mats, int first, int n, const Call& c,
+                 float decay)
+{
+    if (way == kThin16)
+        launch_thin_side<16>(gate, mats, first, n, c, decay);
+    else
+        launch_thin_side<32>(gate, mats, first, n, c, decay);
+}
 
 // Descriptors in place, then every batch in turn: `begin` enqueues what leaves the sources
 // and their sums of squares, `fill` completes a matrix's descriptor.
@@ -777,9 +1046,16 @@ lt_err run_batches(const Call& c, float decay, Fill fill, Begin begin)
         const auto blocks = [&](int i) { return pre[i][first + n] - pre[i][first]; };
         if (n == 0 || blocks(kPreTile) == 0)
             continue;
-        if (lt_err e = begin(gate, dev[kPreUnits], d_momentum, d_mats, first, n,
-                             pre[kPreUnits][first], blocks(kPreUnits)))
-            return e;
+        const bool thin = p.way[b] <= kThin32;
+        if (c.muon || !thin)
+            if (lt_err e = begin(gate, dev[kPreUnits], d_momentum, d_mats, first, n,
+                                 pre[kPreUnits][first], blocks(kPreUnits)))
+                return e;
+        if (thin) {
+            launch_thin(p.way[b], gate, d_mats, first, n, c, decay);
+            LT_TRY_HIP(hipGetLastError());
+            continue;
+        }
         k_orth_norm<<<dim3(uint32_t(n)), kThreads, 0, st>>>(gate, d_mats, first);
         const bool wide_src = c.muon || c.in_dtype == LT_DTYPE_F32;
         auto* prep = wide_src ? k_orth_prepare<float> : k_orth_prepare<uint16_t>;
@@ -790,7 +1066,7 @@ lt_err run_batches(const Call& c, float decay, Fill fill, Begin begin)
         for (int step = 0; step < c.ns_steps; from ^= 1) {
             launch.sym<kGram>({step, from, 0, 0, 0});
             launch.sym<kStep>({step, from, 0, 0, 1});
-            const int now = p.pairs[b] && step + 1 < c.ns_steps ? 2 : 1;
+            const int now = p.way[b] == kPairs && step + 1 < c.ns_steps ? 2 : 1;
             if (now == 2) {
                 launch.sym<kHalf>({step, from, 1, 0, 2});
                 launch.sym<kNext>({step, from, 1, 2, 0});
