@@ -23,7 +23,9 @@
  *   f3  the bf16 copy of the updated weights;
  *   f4  the gradient norm accumulated as gradients arrive;
  *   f5  orthogonalising matrices by Newton-Schulz products;
- *   f6  the Muon step with 8-bit momentum.
+ *   f6  the Muon step with 8-bit momentum;
+ *   f7  quantizing matrices to 8-bit floating point, a scale for each block of 128;
+ *   f8  their products.
  *
  * Conventions for every entry point:
  *  - Tensor data, workspace and scalar outputs are DEVICE pointers on the
@@ -525,6 +527,49 @@ lt_err lt_muon_step(float* const* params, const void* const* grads, int grad_dty
                     int code_map, double lr, double momentum, int nesterov, double weight_decay,
                     double update_rms, int ns_steps, const float* coef, const int32_t* status,
                     const void* step_state, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Layout of a matrix in 8-bit floating point (f7): bytes of a row of codes (its columns rounded
+ * up to 128) and of a row of scales (one for each 128 columns, rounded up to 4).  0 if cols < 0. */
+int64_t lt_fp8_code_pitch(int64_t cols);
+int64_t lt_fp8_scale_pitch(int64_t cols);
+
+/*
+ * f7: quantizes a matrix x, rows x cols elements of dtype with row_stride elements from row to
+ * row (>= cols), to 8-bit floating point with a power-of-two scale for each block of 128.
+ *   codes[rows][code_pitch(cols)]    e4m3 codes (bias 7, no infinities); columns past cols are 0;
+ *   scales[rows][scale_pitch(cols)]  a byte for each 128 columns, e + 127: value = code * 2^e,
+ *                                    e the least with max |x| <= 448 * 2^e over the group, at
+ *                                    least -126, and 0 for a group of zeros; unused bytes 127.
+ *   codes_t, scales_t                the same for the transpose, cols x rows: its groups are
+ *                                    128 rows of a column of x.
+ * Either layout may be NULL (both pointers of it).  square = 0: a scale for each group of 128
+ * as stated; square != 0: one for each 128 x 128 block (every row of the block, in either
+ * layout, holds that scale), so that codes_t is the transpose of codes: for weights, which a
+ * forward and a backward product read.  Codes are x * 2^-e rounded to nearest even.  A group with
+ * a NaN or an infinity has scale 255 and NaN codes, and makes the results that read it NaN.
+ * x and codes 16-byte aligned, scales 4-byte.
+ */
+lt_err lt_fp8_quantize(const void* x, int dtype, int64_t rows, int64_t cols, int64_t row_stride,
+                       int square, uint8_t* codes, uint8_t* scales, uint8_t* codes_t,
+                       uint8_t* scales_t, void* stream);
+
+/* Bytes of device workspace lt_fp8_matmul needs (partial sums where few results share a long
+ * sum); 0 if an argument is invalid. */
+size_t lt_fp8_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k);
+
+/*
+ * f8: out[i][j] = sum over k of A[i][k] * B[j][k], for A (m x k) and B (n x k) as lt_fp8_quantize
+ * stores them, summed in fp32 in a fixed order, rounded once to out_dtype (LT_DTYPE_F32 or
+ * LT_DTYPE_BF16); out has out_stride elements (>= n) from row to row.  k = 0 gives zeros.
+ * A linear layer's three products, with x (tokens x in), weight (out x in) and dy:
+ *   y  = matmul(x, weight),  dx = matmul(dy, weight's transpose),
+ *   dw = matmul(dy's transpose, x's transpose).
+ * m, n < 2^31, k < 2^23.
+ */
+lt_err lt_fp8_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes,
+                     const uint8_t* b_scales, int64_t m, int64_t n, int64_t k, void* out,
+                     int out_dtype, int64_t out_stride, void* workspace, size_t workspace_bytes,
+                     void* stream);
 
 /* Copies the device status word to *out and synchronizes `stream` (the only
  * entry point that blocks the host).  An asynchronous device fault from

@@ -1,0 +1,540 @@
+// fp8.hip -- matrix products in 8-bit floating point (e4m3) with a power-of-two scale for each
+// block of 128 values, and the quantizer that makes their operands.
+//
+// A matrix is stored as codes, row by row, and for each row and each 128 columns the exponent e
+// of a scale 2^e: value = code * 2^e, e the least with max |x| <= 448 * 2^e.  Powers of two
+// are what the matrix instruction applies by itself, exactly and at no cost: sums stay in its
+// accumulators from the first value to the last, where any other scale would need every 128
+// products' sums multiplied and added apart.  Scaling by them is exact, so a value is rounded
+// once, to four significant bits.
+//
+// Both operands of a product have the summed index contiguous, so a training step needs each of
+// its matrices in the layouts of its products: x and dy by rows (forward, input gradient) and
+// transposed, quantized along the tokens (weight gradient); the weight with one scale for each
+// 128 x 128 block, whose codes are then the same in both layouts.  The quantizer writes both
+// from one read.
+
+#include "host.h"
+#include "tiles.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace {
+
+using host::fail;
+using namespace tiles;
+
+constexpr int kGroup = 128;
+
+int64_t code_pitch(int64_t cols) { return host::ceil_div(cols, kGroup) * kGroup; }
+int64_t scale_pitch(int64_t cols) { return host::ceil_div(host::ceil_div(cols, kGroup), 4) * 4; }
+
+__device__ inline float load_value(const float* p) { return *p; }
+__device__ inline float load_value(const uint16_t* p) { return __uint_as_float(uint32_t(*p) << 16); }
+
+__device__ inline uint16_t bf16_bits(float x)
+{
+    return __builtin_bit_cast(uint16_t, (__bf16)x);  // to nearest even; a NaN becomes quiet
+}
+
+// ------------------------------------------------------------- quantizer
+
+// Biased exponent of the scale for a group whose largest |x| has these bits, and its inverse.
+// A group with an infinity or a NaN has the NaN scale (255), and NaN codes.
+struct Scale {
+    uint32_t biased;
+    float inverse;
+};
+
+__device__ inline Scale scale_of(uint32_t top)
+{
+    Scale s;
+    if (top >= 0x7F800000u)
+        return {255u, __builtin_nanf("")};
+    // 448 = 1.75 * 2^8; subnormals and what is below 2^-118 take the least exponent, -126
+    int e = int(top >> 23) - 127 - 8 + ((top & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    e = max(e, -126);
+    e = top == 0u ? 0 : e;
+    s.biased = uint32_t(e + 127);
+    s.inverse = __uint_as_float(uint32_t(127 - e) << 23);
+    return s;
+}
+
+__device__ inline uint32_t pack_codes(float a, float b, float c, float d)
+{
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true));
+}
+
+struct QuantizeArgs {
+    const void* x;
+    int64_t rows, cols, stride;  // elements; stride of x's rows
+    uint8_t *codes, *scales;     // by rows, or null
+    uint8_t *codes_t, *scales_t; // of the transpose, or null
+    int64_t pitch, scale_pitch, pitch_t, scale_pitch_t;
+    int across;                  // blocks of 128 columns
+};
+
+constexpr int kQuantizeThreads = 256;
+
+// One block of 128 x 128 by a workgroup: thread t holds rows 4 (t / 16) + 64 h + r (h < 2,
+// r < 4) and columns 8 (t % 16) .. + 7, so that a row's 128 columns are 16 neighbouring lanes,
+// and four rows of a column are one word of the transpose.  Bound by HBM: x is read once, each
+// layout of the codes written once, in whole lines.
+template <typename T, bool SQUARE>
+__global__ __launch_bounds__(kQuantizeThreads) void k_fp8_quantize(QuantizeArgs a)
+{
+    constexpr int kTurnPitch = kGroup + 4;
+    __shared__ __align__(16) uint8_t turned[kGroup * kTurnPitch];
+    __shared__ uint32_t top_of[16][kGroup];  // of 8 rows of each column; [0] of all rows at last
+    const int t = threadIdx.x, q = t >> 4, l = t & 15;
+    const int64_t r0 = int64_t(blockIdx.x / a.across) * kGroup;
+    const int64_t c0 = int64_t(blockIdx.x % a.across) * kGroup;
+    const T* x = static_cast<const T*>(a.x);
+    const bool whole = c0 + kGroup <= a.cols &&
+                       (a.stride * int64_t(sizeof(T))) % 16 == 0;  // rows start 16-byte aligned
+    float v[2][4][8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int64_t row = r0 + 4 * q + 64 * h + r, col = c0 + 8 * l;
+            const T* p = x + row * a.stride + col;
+            if (row >= a.rows) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    v[h][r][e] = 0.0f;
+            } else if (whole) {
+                if constexpr (sizeof(T) == 2) {
+                    const i32x4 w = *reinterpret_cast<const i32x4*>(p);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        v[h][r][2 * e] = __uint_as_float(uint32_t(w[e]) << 16);
+                        v[h][r][2 * e + 1] = __uint_as_float(uint32_t(w[e]) & 0xFFFF0000u);
+                    }
+                } else {
+                    const f32x4 w0 = *reinterpret_cast<const f32x4*>(p);
+                    const f32x4 w1 = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        v[h][r][e] = w0[e];
+                        v[h][r][4 + e] = w1[e];
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    v[h][r][e] = col + e < a.cols ? load_value(p + e) : 0.0f;
+            }
+        }
+
+    const auto magnitude = [](float f) { return __float_as_uint(f) & 0x7FFFFFFFu; };
+    uint32_t block_top = 0;
+    if constexpr (SQUARE) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    block_top = max(block_top, magnitude(v[h][r][e]));
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1)
+            block_top = max(block_top, uint32_t(__shfl_xor(int(block_top), o, 64)));
+        if ((t & 63) == 0)
+            top_of[0][t >> 6] = block_top;
+        __syncthreads();
+        block_top = max(max(top_of[0][0], top_of[0][1]), max(top_of[0][2], top_of[0][3]));
+    }
+
+    // by rows
+    if (a.codes) {
+        const int group = int(c0 / kGroup);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                uint32_t top = block_top;
+                if constexpr (!SQUARE) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        top = max(top, magnitude(v[h][r][e]));
+#pragma unroll
+                    for (int o = 8; o >= 1; o >>= 1)
+                        top = max(top, uint32_t(__shfl_xor(int(top), o, 64)));
+                }
+                const Scale s = scale_of(top);
+                const int64_t row = r0 + 4 * q + 64 * h + r;
+                if (row >= a.rows)
+                    continue;
+                const float(&w)[8] = v[h][r];
+                uint32_t lo = pack_codes(w[0] * s.inverse, w[1] * s.inverse, w[2] * s.inverse,
+                                         w[3] * s.inverse);
+                uint32_t hi = pack_codes(w[4] * s.inverse, w[5] * s.inverse, w[6] * s.inverse,
+                                         w[7] * s.inverse);
+                *reinterpret_cast<uint2*>(a.codes + row * a.pitch + c0 + 8 * l) =
+                    make_uint2(lo, hi);
+                uint8_t* to = a.scales + row * a.scale_pitch + group;
+                if (l == 0)
+                    *to = uint8_t(s.biased);
+                else if (group + 1 == a.across && group + l < a.scale_pitch)
+                    to[l] = 127;  // the last word's unused bytes
+            }
+    }
+
+    // the transpose
+    if (a.codes_t) {
+        Scale s[8];
+        if constexpr (SQUARE) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                s[e] = scale_of(block_top);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                uint32_t top = 0;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        top = max(top, magnitude(v[h][r][e]));
+                top_of[q][8 * l + e] = top;
+            }
+            __syncthreads();
+            if (t < kGroup) {
+                uint32_t top = 0;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    top = max(top, top_of[i][t]);
+                top_of[0][t] = top;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                s[e] = scale_of(top_of[0][8 * l + e]);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                *reinterpret_cast<uint32_t*>(turned + (8 * l + e) * kTurnPitch + 64 * h + 4 * q) =
+                    pack_codes(v[h][0][e] * s[e].inverse, v[h][1][e] * s[e].inverse,
+                               v[h][2][e] * s[e].inverse, v[h][3][e] * s[e].inverse);
+        __syncthreads();
+        for (int i = t; i < kGroup * 8; i += kQuantizeThreads) {
+            const int64_t col = c0 + i / 8;
+            if (col >= a.cols)
+                continue;
+            const auto* from =
+                reinterpret_cast<const uint32_t*>(turned + i / 8 * kTurnPitch + i % 8 * 16);
+            *reinterpret_cast<uint4*>(a.codes_t + col * a.pitch_t + r0 + i % 8 * 16) =
+                make_uint4(from[0], from[1], from[2], from[3]);
+        }
+        const int group = int(r0 / kGroup), groups = int((a.rows + kGroup - 1) / kGroup);
+        if (t < kGroup && c0 + t < a.cols) {
+            const Scale st = scale_of(SQUARE ? block_top : top_of[0][t]);
+            uint8_t* to = a.scales_t + (c0 + t) * a.scale_pitch_t + group;
+            *to = uint8_t(st.biased);
+            if (group + 1 == groups)
+                for (int i = 1; group + i < a.scale_pitch_t; ++i)
+                    to[i] = 127;
+        }
+    }
+}
+
+// ------------------------------------------------------------- products
+
+struct ProductArgs {
+    const uint8_t *a, *a_scales, *b, *b_scales;
+    int64_t m, n;              // rows of a and of b
+    int64_t pitch, scale_pitch;
+    int steps;                 // of 128 summed values
+    int slice;                 // steps of one slice of the sum (gridDim.y slices), whole words
+    void* out;
+    int64_t stride;            // of out's rows, elements
+    float* partial;            // several slices: [slice][m][n]
+};
+
+// Results to out, or one slice's sums to the workspace.
+template <bool F32>
+struct ProductWriter {
+    static constexpr bool kTurned = false;
+    static constexpr int kSlots = 8;
+    void* out;
+    int64_t stride, rows, cols;  // from the tile's origin on
+    bool whole;
+    __device__ inline void fetch(int, int, int) {}
+    __device__ inline void turn(int, int, const float (&)[8]) {}
+    __device__ inline void store(int row, int col, float (&v)[8], int)
+    {
+        typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+        if (row >= rows || col >= cols)
+            return;
+        const int64_t at = row * stride + col;
+        if constexpr (F32) {
+            float* p = static_cast<float*>(out) + at;
+            if (whole && col + 8 <= cols) {
+                *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+                *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+                return;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (col + e < cols)
+                    p[e] = v[e];
+        } else {
+            uint16_t* p = static_cast<uint16_t*>(out) + at;
+            if (whole && col + 8 <= cols) {
+                u16x8 b;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    b[e] = bf16_bits(v[e]);
+                *reinterpret_cast<u16x8*>(p) = b;
+                return;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (col + e < cols)
+                    p[e] = bf16_bits(v[e]);
+        }
+    }
+};
+
+template <typename Tile, bool F32>
+__global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_fp8_product(ProductArgs g)
+{
+    __shared__ __align__(1024) uint8_t lds[Tile::kLdsBytes + Fp8<Tile>::kLdsBytes];
+    const int64_t unit = unit_of_workgroup(Tile::kRun);
+    const TilePlace at = tile_place(int(unit), int((g.m + Tile::kRows - 1) / Tile::kRows),
+                                    int((g.n + Tile::kCols - 1) / Tile::kCols));
+    const int64_t r0 = int64_t(at.row) * Tile::kRows, c0 = int64_t(at.col) * Tile::kCols;
+    const int first = int(blockIdx.y) * g.slice, steps = min(g.slice, g.steps - first);
+    Tile tile;
+    Fp8<Tile> mul;
+    mul.scales_p = g.a_scales + r0 * g.scale_pitch + first;
+    mul.scales_q = g.b_scales + c0 * g.scale_pitch + first;
+    mul.pitch = g.scale_pitch;
+    mul.limit_p = g.m - r0;
+    mul.limit_q = g.n - c0;
+    mul.words = (steps + 3) / 4;
+    mul.lds = lds + Tile::kLdsBytes;
+    product(mul, tile, g.a + r0 * g.pitch + int64_t(first) * kStepBytes, g.pitch, g.m - r0,
+            g.b + c0 * g.pitch + int64_t(first) * kStepBytes, g.pitch, g.n - c0, steps, lds);
+    ProductWriter<F32> w;
+    w.rows = g.m - r0;
+    w.cols = g.n - c0;
+    if (g.partial) {
+        ProductWriter<true> p;
+        p.rows = w.rows;
+        p.cols = w.cols;
+        p.stride = g.n;
+        p.whole = g.n % 4 == 0;
+        p.out = g.partial + (int64_t(blockIdx.y) * g.m + r0) * g.n + c0;
+        finish(tile, lds, p);
+        return;
+    }
+    w.stride = g.stride;
+    w.whole = g.stride % (F32 ? 4 : 8) == 0;
+    w.out = F32 ? static_cast<void*>(static_cast<float*>(g.out) + r0 * g.stride + c0)
+                : static_cast<void*>(static_cast<uint16_t*>(g.out) + r0 * g.stride + c0);
+    finish(tile, lds, w);
+}
+
+// out = the slices' sums, added in their order.
+template <bool F32>
+__global__ __launch_bounds__(256) void k_fp8_join(const float* __restrict__ partial, int slices,
+                                                  int64_t m, int64_t n, void* out, int64_t stride)
+{
+    const int64_t all = m * n;
+    for (int64_t e = int64_t(blockIdx.x) * 256 + threadIdx.x; e < all;
+         e += int64_t(gridDim.x) * 256) {
+        float s = partial[e];
+        for (int i = 1; i < slices; ++i)
+            s += partial[i * all + e];
+        const int64_t to = e / n * stride + e % n;
+        if constexpr (F32)
+            static_cast<float*>(out)[to] = s;
+        else
+            static_cast<uint16_t*>(out)[to] = bf16_bits(s);
+    }
+}
+
+template <bool F32>
+__global__ __launch_bounds__(256) void k_fp8_zero(int64_t m, int64_t n, void* out, int64_t stride)
+{
+    const int64_t all = m * n;
+    for (int64_t e = int64_t(blockIdx.x) * 256 + threadIdx.x; e < all;
+         e += int64_t(gridDim.x) * 256) {
+        const int64_t to = e / n * stride + e % n;
+        if constexpr (F32)
+            static_cast<float*>(out)[to] = 0.0f;
+        else
+            static_cast<uint16_t*>(out)[to] = 0;
+    }
+}
+
+// ---------------------------------------------------------------- host side
+
+// Rows of codes stay within the 32-bit offsets of a tile's loads.
+constexpr int64_t kMostSummed = int64_t(1) << 23;
+
+struct Way {
+    int tile;    // 256, 128 or 64
+    int slices;  // of the sum
+    int slice;   // steps of each
+};
+
+// The largest tile that still leaves every CU a workgroup; where even the smallest does not, the
+// sum is cut as well, into slices of 512 values or more.
+Way way_of(int64_t m, int64_t n, int64_t k)
+{
+    const int steps = int(host::ceil_div(k, kGroup));
+    Way w{64, 1, steps};
+    int64_t tiles = 0;
+    for (const int t : {256, 128, 64}) {
+        w.tile = t;
+        tiles = host::ceil_div(m, t) * host::ceil_div(n, t);
+        if (tiles >= 256)
+            return w;
+    }
+    const int words = int(host::ceil_div(steps, 4));
+    const int want = int(std::min<int64_t>(words, host::ceil_div(512, std::max<int64_t>(tiles, 1))));
+    const int per = int(host::ceil_div(words, std::max(want, 1)));
+    w.slice = std::max(per, 1) * 4;
+    w.slices = std::max(1, int(host::ceil_div(steps, w.slice)));
+    if (w.slices == 1)
+        w.slice = steps;
+    return w;
+}
+
+bool valid_sizes(int64_t m, int64_t n, int64_t k)
+{
+    const int64_t most = int64_t(1) << 31;
+    return m >= 0 && n >= 0 && k >= 0 && m < most && n < most && k < kMostSummed &&
+           host::ceil_div(m, 64) * host::ceil_div(n, 64) < most;
+}
+
+template <typename Tile>
+void launch_product(const ProductArgs& g, const Way& w, bool f32, hipStream_t st)
+{
+    const dim3 grid(uint32_t(host::ceil_div(g.m, Tile::kRows) * host::ceil_div(g.n, Tile::kCols)),
+                    uint32_t(w.slices));
+    if (f32)
+        k_fp8_product<Tile, true><<<grid, Tile::kThreads, 0, st>>>(g);
+    else
+        k_fp8_product<Tile, false><<<grid, Tile::kThreads, 0, st>>>(g);
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t lt_fp8_code_pitch(int64_t cols) { return cols < 0 ? 0 : code_pitch(cols); }
+
+int64_t lt_fp8_scale_pitch(int64_t cols) { return cols < 0 ? 0 : scale_pitch(cols); }
+
+lt_err lt_fp8_quantize(const void* x, int dtype, int64_t rows, int64_t cols, int64_t row_stride,
+                       int square, uint8_t* codes, uint8_t* scales, uint8_t* codes_t,
+                       uint8_t* scales_t, void* stream)
+{
+    host::clear_error();
+    if (dtype != LT_DTYPE_F32 && dtype != LT_DTYPE_BF16)
+        return fail(LT_ERR_INVALID_ARG, "dtype must be LT_DTYPE_F32 or LT_DTYPE_BF16");
+    const int64_t most = int64_t(1) << 31;
+    if (rows < 0 || cols < 0 || rows >= most || cols >= most || row_stride < cols ||
+        host::ceil_div(rows, kGroup) * host::ceil_div(cols, kGroup) >= most)
+        return fail(LT_ERR_INVALID_ARG, "need 0 <= rows, cols < 2^31 and row_stride >= cols");
+    if ((codes != nullptr) != (scales != nullptr) || (codes_t != nullptr) != (scales_t != nullptr))
+        return fail(LT_ERR_INVALID_ARG, "codes come with their scales");
+    if (rows == 0 || cols == 0)
+        return LT_OK;
+    if (!x || (!codes && !codes_t))
+        return fail(LT_ERR_INVALID_ARG, "x and at least one layout of codes must be given");
+    if (!host::aligned(x, 16) || !host::aligned(codes, 16) || !host::aligned(codes_t, 16) ||
+        !host::aligned(scales, 4) || !host::aligned(scales_t, 4))
+        return fail(LT_ERR_ALIGNMENT, "x and codes must be 16-byte aligned, scales 4-byte");
+    QuantizeArgs a{x,
+                   rows,
+                   cols,
+                   row_stride,
+                   codes,
+                   scales,
+                   codes_t,
+                   scales_t,
+                   code_pitch(cols),
+                   scale_pitch(cols),
+                   code_pitch(rows),
+                   scale_pitch(rows),
+                   int(host::ceil_div(cols, kGroup))};
+    const dim3 grid(uint32_t(host::ceil_div(rows, kGroup) * a.across));
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    auto* kernel = dtype == LT_DTYPE_BF16
+                       ? (square ? k_fp8_quantize<uint16_t, true> : k_fp8_quantize<uint16_t, false>)
+                       : (square ? k_fp8_quantize<float, true> : k_fp8_quantize<float, false>);
+    kernel<<<grid, kQuantizeThreads, 0, st>>>(a);
+    LT_TRY_HIP(hipGetLastError());
+    return LT_OK;
+}
+
+size_t lt_fp8_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k)
+{
+    if (!valid_sizes(m, n, k))
+        return 0;
+    const Way w = way_of(m, n, k);
+    return std::max(size_t(256),
+                    w.slices > 1 ? size_t(w.slices) * size_t(m) * size_t(n) * 4 : size_t(0));
+}
+
+lt_err lt_fp8_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes,
+                     const uint8_t* b_scales, int64_t m, int64_t n, int64_t k, void* out,
+                     int out_dtype, int64_t out_stride, void* workspace, size_t workspace_bytes,
+                     void* stream)
+{
+    host::clear_error();
+    if (!valid_sizes(m, n, k) || out_stride < n)
+        return fail(LT_ERR_INVALID_ARG, "need 0 <= m, n < 2^31, 0 <= k < 2^23 and out_stride >= n");
+    if (out_dtype != LT_DTYPE_F32 && out_dtype != LT_DTYPE_BF16)
+        return fail(LT_ERR_INVALID_ARG, "out_dtype must be LT_DTYPE_F32 or LT_DTYPE_BF16");
+    if (m == 0 || n == 0)
+        return LT_OK;
+    if (!out || (k > 0 && (!a_codes || !a_scales || !b_codes || !b_scales)))
+        return fail(LT_ERR_INVALID_ARG, "operands and out must not be NULL");
+    if (!host::aligned(a_codes, 16) || !host::aligned(b_codes, 16) || !host::aligned(out, 16) ||
+        !host::aligned(a_scales, 4) || !host::aligned(b_scales, 4))
+        return fail(LT_ERR_ALIGNMENT, "codes and out must be 16-byte aligned, scales 4-byte");
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    const bool f32 = out_dtype == LT_DTYPE_F32;
+    const Way w = way_of(m, n, k);
+    if (k == 0) {  // an empty sum
+        auto* join = f32 ? k_fp8_zero<true> : k_fp8_zero<false>;
+        join<<<dim3(uint32_t(std::min<int64_t>(4096, host::ceil_div(m * n, 256)))), 256, 0, st>>>(
+            m, n, out, out_stride);
+        LT_TRY_HIP(hipGetLastError());
+        return LT_OK;
+    }
+    ProductArgs g{a_codes, a_scales,   b_codes, b_scales,   m,      n, code_pitch(k),
+                  scale_pitch(k), int(host::ceil_div(k, kGroup)), w.slice, out, out_stride, nullptr};
+    if (w.slices > 1) {
+        const size_t need = lt_fp8_matmul_workspace_bytes(m, n, k);
+        if (!workspace || !host::aligned(workspace, 256) || workspace_bytes < need)
+            return fail(LT_ERR_WORKSPACE, "workspace must be 256-byte aligned and hold " +
+                                              std::to_string(need) + " bytes");
+        g.partial = static_cast<float*>(workspace);
+    }
+    if (w.tile == 256)
+        launch_product<Large>(g, w, f32, st);
+    else if (w.tile == 128)
+        launch_product<Small>(g, w, f32, st);
+    else
+        launch_product<Tiny>(g, w, f32, st);
+    if (g.partial) {
+        auto* join = f32 ? k_fp8_join<true> : k_fp8_join<false>;
+        join<<<dim3(uint32_t(std::min<int64_t>(4096, host::ceil_div(m * n, 256)))), 256, 0, st>>>(
+            g.partial, w.slices, m, n, out, out_stride);
+    }
+    LT_TRY_HIP(hipGetLastError());
+    return LT_OK;
+}
+
+}  // extern "C"

@@ -315,7 +315,8 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_orth_sy
     const _Float16* M = OP == kGram ? (wide ? m.h[args.from] : m.t[args.from]) : m.sym[args.m];
     const _Float16* N = OP == kGram ? M : m.sym[args.n];
     Tile tile;
-    product<Half>(tile, M + int64_t(r0) * inner, int64_t(inner) * 2, side - r0,
+    Half mul;
+    product(mul, tile, M + int64_t(r0) * inner, int64_t(inner) * 2, side - r0,
                  N + int64_t(c0) * inner, int64_t(inner) * 2, side - c0, inner / 64, lds);
 
     const Shift s = shift_at(m, args.step);
@@ -493,7 +494,8 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_orth_up
         const int inner = wide ? m.rp : m.cp;
         const _Float16* P = (wide ? m.sym[args.sym] : m.h[from]) + int64_t(r0) * inner;
         const _Float16* Q = (wide ? m.t[from] : m.sym[args.sym]) + int64_t(c0) * inner;
-        product<Half>(tile, P, int64_t(inner) * 2, m.rp - r0, Q, int64_t(inner) * 2, m.cp - c0,
+        Half mul;
+        product(mul, tile, P, int64_t(inner) * 2, m.rp - r0, Q, int64_t(inner) * 2, m.cp - c0,
                      inner / 64, lds);
         by = 1.0f / (args.steps == 2 ? kScaleR : kScaleS);
         linear = shift_at(m, args.step).p;

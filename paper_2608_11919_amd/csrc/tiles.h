@@ -79,7 +79,11 @@ __device__ inline i32x4 read_chunk(const uint8_t* tile, int row32, int half, int
 // Products of fp16: 32 values a half step, in two instructions.
 struct Half {
     static constexpr int kInstructions = 2;
-    __device__ static inline f32x16 mul(int t, const Chunks& a, const Chunks& b, f32x16 c)
+    __device__ inline void begin() {}
+    __device__ inline void copy(int) {}
+    __device__ inline void read(int) {}
+    __device__ inline void next() {}
+    __device__ inline f32x16 mul(int t, int, int, const Chunks& a, const Chunks& b, f32x16 c) const
     {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, a.c[t]),
                                                       __builtin_bit_cast(half8, b.c[t]), c, 0, 0,
@@ -157,6 +161,78 @@ __device__ inline TilePlace triangle_place(int t, int side)
 
 typedef Shape<128, 128, 64, 64> Small;
 typedef Shape<256, 256, 128, 128> Large;
+typedef Shape<64, 64, 32, 32> Tiny;
+
+// Products of fp8 (e4m3) with a power-of-two scale for each row and each 128 values: 64 values a
+// half step, in one instruction, which applies the scales itself.  A scale is a byte, the
+// exponent biased by 127; four steps' worth are a word, copied into LDS four steps at a time.
+template <typename S>
+struct Fp8 {
+    static constexpr int kInstructions = 1;
+    static constexpr int kRowsAll = S::kRows + S::kCols, kLdsBytes = 2 * kRowsAll * 4;
+    const uint8_t *scales_p, *scales_q;  // of the tile's first rows, at the first step
+    int64_t pitch, limit_p, limit_q;     // bytes of a row's scales; rows that exist
+    int words;                           // of four steps
+    uint8_t* lds;                        // kLdsBytes
+    uint32_t now_p[S::I], now_q[S::J], then_p[S::I], then_q[S::J];
+
+    // words w of all rows of the tile into their buffer
+    __device__ inline void copy_word(int w)
+    {
+        const int64_t at = int64_t(w < words ? w : words - 1) * 4;
+        uint8_t* to = lds + (w & 1) * kRowsAll * 4;
+#pragma unroll
+        for (int first = 0; first < kRowsAll; first += S::kThreads) {
+            const int base = first + S::wave() * 64;
+            if (base >= kRowsAll)
+                break;
+            const bool is_p = base < S::kRows;
+            int64_t r = (is_p ? base : base - S::kRows) + S::lane();
+            const int64_t limit = is_p ? limit_p : limit_q;
+            r = r < limit ? r : limit - 1;
+            __builtin_amdgcn_global_load_lds(
+                (const LT_GLOBAL void*)((is_p ? scales_p : scales_q) + r * pitch + at),
+                (LT_LDS void*)(to + base * 4), 4, 0, 0);
+        }
+    }
+    __device__ inline void begin() { copy_word(0); }
+    // after the barrier of step s: the buffer of the word before last is free
+    __device__ inline void copy(int s)
+    {
+        if ((s & 3) == 0)
+            copy_word((s >> 2) + 1);
+    }
+    // the scales of step s
+    __device__ inline void read(int s)
+    {
+        const auto* from = reinterpret_cast<const uint32_t*>(lds + (s >> 2 & 1) * kRowsAll * 4);
+        const int shift = 8 * (s & 3);
+#pragma unroll
+        for (int i = 0; i < S::I; ++i)
+            then_p[i] = from[S::row(i)] >> shift;
+#pragma unroll
+        for (int j = 0; j < S::J; ++j)
+            then_q[j] = from[S::kRows + S::wave_col() + 32 * j + (S::lane() & 31)] >> shift;
+    }
+    __device__ inline void next()
+    {
+#pragma unroll
+        for (int i = 0; i < S::I; ++i)
+            now_p[i] = then_p[i];
+#pragma unroll
+        for (int j = 0; j < S::J; ++j)
+            now_q[j] = then_q[j];
+    }
+    __device__ inline f32x16 mul(int, int i, int j, const Chunks& a, const Chunks& b, f32x16 c) const
+    {
+        const auto join = [](const Chunks& x) {
+            return i32x8{x.c[0][0], x.c[0][1], x.c[0][2], x.c[0][3],
+                         x.c[1][0], x.c[1][1], x.c[1][2], x.c[1][3]};
+        };
+        return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(join(a), join(b), c, 0, 0, 0,
+                                                               int(now_q[j]), 0, int(now_p[i]));
+    }
+};
 
 // The main loop over `steps` >= 1 steps.  P, Q: first rows of the tile's operands, pitches in
 // bytes, of which limit_p and limit_q rows exist.
@@ -166,7 +242,7 @@ typedef Shape<256, 256, 128, 128> Large;
 // frees the buffer, and the copy of the step after next starts, a whole step before it is read.
 // The loop has no branches: past the end it copies and reads the last step again, unused.
 template <typename Mul, typename S>
-__device__ inline void product(S& c, const void* P, int64_t pitch_p, int64_t limit_p,
+__device__ inline void product(Mul& mul, S& c, const void* P, int64_t pitch_p, int64_t limit_p,
                                const void* Q, int64_t pitch_q, int64_t limit_q, int steps,
                                uint8_t* lds)
 {
@@ -179,7 +255,7 @@ __device__ inline void product(S& c, const void* P, int64_t pitch_p, int64_t lim
     const auto* p = static_cast<const uint8_t*>(P);
     const auto* q = static_cast<const uint8_t*>(Q);
     constexpr int kLoads = load_p.N + load_q.N, kReads = 2 * (I + J);
-    constexpr int kMuls = I * J * Mul::kInstructions, kPaced = kMuls * 3 / 4;
+    constexpr int kMuls = I * J * Mul::kInstructions, kPaced = kMuls < 2 ? 1 : kMuls * 3 / 4;
     // the k-th share of n things spread over the first three quarters of the products: the last
     // quarter covers the latency of the reads
     const auto share = [](int n, int k) { return k < kPaced ? n * k / kPaced : n; };
@@ -210,7 +286,7 @@ __device__ inline void product(S& c, const void* P, int64_t pitch_p, int64_t lim
         for (int k = 0; k < kMuls; ++k) {
             between(k);
             const int t = k / (I * J), i = k / J % I, j = k % J;
-            c.acc[i][j] = Mul::mul(t, x.b[j], x.a[i], c.acc[i][j]);
+            c.acc[i][j] = mul.mul(t, i, j, x.b[j], x.a[i], c.acc[i][j]);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -224,13 +300,16 @@ __device__ inline void product(S& c, const void* P, int64_t pitch_p, int64_t lim
 #pragma unroll
     for (int k = 0; k < 2 * kLoads; ++k)
         load(k / kLoads, k % kLoads);
+    mul.begin();
     wait_loads();
     __builtin_amdgcn_s_barrier();
+    mul.read(0);
 #pragma unroll
     for (int k = 0; k < kReads; ++k)
         read(0, 0, k, x0);
 #pragma unroll 1
     for (int s = 0; s < steps; ++s) {
+        mul.next();
         multiply(x0, [&](int k) {
 #pragma unroll
             for (int r = share(kReads, k); r < share(kReads, k + 1); ++r)
@@ -239,6 +318,8 @@ __device__ inline void product(S& c, const void* P, int64_t pitch_p, int64_t lim
         wait_reads();
         wait_loads();
         __builtin_amdgcn_s_barrier();  // the next step is in place, this one's buffer is free
+        mul.copy(s);
+        mul.read(s + 1);
         multiply(x1, [&](int k) {
 #pragma unroll
             for (int r = share(kLoads, k); r < share(kLoads, k + 1); ++r)

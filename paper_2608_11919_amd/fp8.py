@@ -1,0 +1,212 @@
+"""Matrix products in 8-bit floating point (f7, f8; see include/lazytrain.h) and the linear layer
+made of them: weights that the optimizer has just updated are quantized once, read by the
+forward and the input-gradient product, and the weight gradient comes back in bfloat16 (or
+float32) for the next step.
+"""
+from __future__ import annotations
+
+from typing import Optional, Tuple
+
+import torch
+
+from .lazytrain import (LT_DTYPE_BF16, LT_DTYPE_F32, _check, _current, _stream_handle, _workspace,
+                        lib)
+
+_DTYPES = {torch.float32: LT_DTYPE_F32, torch.bfloat16: LT_DTYPE_BF16}
+_BYTES = (torch.uint8, torch.float8_e4m3fn)
+
+
+def lt_fp8_code_pitch(cols: int) -> int:
+    """Bytes of a row of codes of a matrix with `cols` columns."""
+    return -(-cols // 128) * 128
+
+
+def lt_fp8_scale_pitch(cols: int) -> int:
+    """Bytes of a row of its scales."""
+    return -(-cols // 512) * 4
+
+
+def _dtype_code(t: torch.Tensor, what: str) -> int:
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{what} must be float32 or bfloat16, got {t.dtype}")
+    return code
+
+
+def _rows(t: torch.Tensor, what: str) -> int:
+    """The row stride of a matrix whose rows are contiguous."""
+    if t.dim() != 2:
+        raise ValueError(f"{what} must be a matrix (two dimensions, got {t.dim()})")
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{what} must have contiguous rows")
+    stride = t.stride(0) if rows > 1 else cols
+    if stride < cols:
+        raise ValueError(f"{what}: rows must not overlap")
+    return stride
+
+
+def _layout(codes, scales, rows: int, cols: int, device, what: str) -> Tuple[int, int]:
+    """Addresses of a layout's codes and scales (0, 0 for none)."""
+    if codes is None and scales is None:
+        return 0, 0
+    if codes is None or scales is None:
+        raise ValueError(f"{what} come with their scales")
+    for t, pitch, name in ((codes, lt_fp8_code_pitch(cols), what),
+                           (scales, lt_fp8_scale_pitch(cols), what + " scales")):
+        if t.device != device or t.dtype not in _BYTES or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous bytes on {device}")
+        if t.numel() != rows * pitch:
+            raise ValueError(f"{name} must have {rows} rows of {pitch} bytes")
+    return codes.data_ptr(), scales.data_ptr()
+
+
+def lt_fp8_quantize(x: torch.Tensor, codes: Optional[torch.Tensor] = None,
+                    scales: Optional[torch.Tensor] = None,
+                    codes_t: Optional[torch.Tensor] = None,
+                    scales_t: Optional[torch.Tensor] = None, square: bool = False,
+                    stream=None) -> None:
+    """f7: quantizes x (rows, cols; float32 or bfloat16, contiguous rows) into codes and scales
+    by rows, and into those of its transpose; either may be left out.  With `square` a scale
+    holds for a 128 x 128 block, else for 128 columns of a row."""
+    stride = _rows(x, "x")
+    rows, cols = x.shape
+    code = _dtype_code(x, "x")
+    device = x.device
+    c, s = _layout(codes, scales, rows, cols, device, "codes")
+    ct, st = _layout(codes_t, scales_t, cols, rows, device, "codes_t")
+    with _current(device):
+        _check(lib().lt_fp8_quantize(x.data_ptr(), code, rows, cols, stride, int(bool(square)), c,
+                                     s, ct, st, _stream_handle(stream, device)))
+
+
+def lt_fp8_matmul(a_codes: torch.Tensor, a_scales: torch.Tensor, b_codes: torch.Tensor,
+                  b_scales: torch.Tensor, k: int, out: torch.Tensor,
+                  workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """f8: out[i, j] = sum over k of A[i, k] * B[j, k] for operands that lt_fp8_quantize made;
+    out is (m, n), float32 or bfloat16, with contiguous rows."""
+    stride = _rows(out, "out")
+    m, n = out.shape
+    code = _dtype_code(out, "out")
+    device = out.device
+    a, sa = _layout(a_codes, a_scales, m, k, device, "a_codes")
+    b, sb = _layout(b_codes, b_scales, n, k, device, "b_codes")
+    ws, nbytes = 0, int(lib().lt_fp8_matmul_workspace_bytes(m, n, k))
+    if nbytes > 256 or workspace is not None:
+        held = _workspace(device, nbytes, workspace, stream, "fp8")
+        ws, nbytes = held.data_ptr(), held.numel() * held.element_size()
+    with _current(device):
+        _check(lib().lt_fp8_matmul(a, sa, b, sb, m, n, k, out.data_ptr(), code, stride, ws,
+                                   nbytes, _stream_handle(stream, device)))
+
+
+class Fp8Weight:
+    """A linear layer's weight (out_features x in_features) in 8-bit floating point, a scale for
+    each 128 x 128 block: codes and scales by rows, which the forward product reads, and of
+    the transpose, which the input-gradient product reads (None where only answers are
+    computed).  ``update`` quantizes the master weights into it again after a step."""
+
+    __slots__ = ("rows", "cols", "codes", "scales", "codes_t", "scales_t")
+
+    def __init__(self, rows: int, cols: int, codes: torch.Tensor, scales: torch.Tensor,
+                 codes_t: Optional[torch.Tensor] = None, scales_t: Optional[torch.Tensor] = None):
+        self.rows, self.cols = int(rows), int(cols)
+        _layout(codes, scales, self.rows, self.cols, codes.device, "codes")
+        _layout(codes_t, scales_t, self.cols, self.rows, codes.device, "codes_t")
+        self.codes, self.scales, self.codes_t, self.scales_t = codes, scales, codes_t, scales_t
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, device, transposed: bool = True) -> "Fp8Weight":
+        codes, scales = _empty(rows, cols, device)
+        codes_t, scales_t = _empty(cols, rows, device) if transposed else (None, None)
+        return cls(rows, cols, codes, scales, codes_t, scales_t)
+
+    @classmethod
+    def from_master(cls, w: torch.Tensor, transposed: bool = True, stream=None) -> "Fp8Weight":
+        """Quantizes a weight matrix (float32 or bfloat16)."""
+        _rows(w, "w")
+        weight = cls.empty(w.shape[0], w.shape[1], w.device, transposed)
+        weight.update(w, stream=stream)
+        return weight
+
+    def update(self, w: torch.Tensor, stream=None) -> None:
+        if tuple(w.shape) != (self.rows, self.cols):
+            raise ValueError(f"w must have shape {(self.rows, self.cols)}")
+        lt_fp8_quantize(w, self.codes, self.scales, self.codes_t, self.scales_t, square=True,
+                        stream=stream)
+
+
+def _empty(rows: int, cols: int, device):
+    return (torch.empty(rows, lt_fp8_code_pitch(cols), dtype=torch.uint8, device=device),
+            torch.empty(rows, lt_fp8_scale_pitch(cols), dtype=torch.uint8, device=device))
+
+
+def _tokens(x: torch.Tensor, features: int, what: str) -> torch.Tensor:
+    if x.dim() < 1 or x.shape[-1] != features:
+        raise ValueError(f"{what} must have {features} features, got shape {tuple(x.shape)}")
+    return x if x.dim() == 2 else x.reshape(-1, features)
+
+
+def fp8_linear(x: torch.Tensor, weight: Fp8Weight,
+               out_dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+    """x weight^T for x (..., in_features), quantized on the way; for answering: nothing is
+    kept for a backward pass.  Works on the current stream."""
+    t = _tokens(x, weight.cols, "x")
+    codes, scales = _empty(t.shape[0], weight.cols, x.device)
+    lt_fp8_quantize(t, codes, scales)
+    y = torch.empty(t.shape[0], weight.rows, dtype=out_dtype, device=x.device)
+    lt_fp8_matmul(codes, scales, weight.codes, weight.scales, weight.cols, y)
+    return y.view(*x.shape[:-1], weight.rows)
+
+
+def fp8_linear_forward(x: torch.Tensor, weight: Fp8Weight,
+                       out_dtype: torch.dtype = torch.bfloat16):
+    """As fp8_linear, and what the backward pass needs of x: its transpose, quantized along the
+    tokens (one byte a value)."""
+    t = _tokens(x, weight.cols, "x")
+    codes, scales = _empty(t.shape[0], weight.cols, x.device)
+    saved = _empty(weight.cols, t.shape[0], x.device)
+    lt_fp8_quantize(t, codes, scales, *saved)
+    y = torch.empty(t.shape[0], weight.rows, dtype=out_dtype, device=x.device)
+    lt_fp8_matmul(codes, scales, weight.codes, weight.scales, weight.cols, y)
+    return y.view(*x.shape[:-1], weight.rows), saved
+
+
+def fp8_linear_backward(dy: torch.Tensor, saved, weight: Fp8Weight,
+                        out_dtype: torch.dtype = torch.bfloat16,
+                        grad_dtype: torch.dtype = torch.bfloat16):
+    """(dx, dw) of fp8_linear_forward: dx in out_dtype with dy's leading shape, dw (out_features
+    x in_features) in grad_dtype."""
+    if weight.codes_t is None:
+        raise ValueError("the weight has no transposed codes: the backward pass needs them")
+    t = _tokens(dy, weight.rows, "dy")
+    tokens, device = t.shape[0], dy.device
+    codes, scales = _empty(tokens, weight.rows, device)
+    codes_t, scales_t = _empty(weight.rows, tokens, device)
+    lt_fp8_quantize(t, codes, scales, codes_t, scales_t)
+    dx = torch.empty(tokens, weight.cols, dtype=out_dtype, device=device)
+    lt_fp8_matmul(codes, scales, weight.codes_t, weight.scales_t, weight.rows, dx)
+    dw = torch.empty(weight.rows, weight.cols, dtype=grad_dtype, device=device)
+    lt_fp8_matmul(codes_t, scales_t, saved[0], saved[1], tokens, dw)
+    return dx.view(*dy.shape[:-1], weight.cols), dw
+
+
+class Fp8Linear(torch.autograd.Function):
+    """``Fp8Linear.apply(x, w, weight)``: x weight^T with gradients for x and for w, the tensor
+    (float32 or bfloat16, for instance the optimizer's bf16 copy) that stands for the weight in
+    the graph and whose values ``weight`` was quantized from."""
+
+    @staticmethod
+    def forward(ctx, x, w, weight):
+        if tuple(w.shape) != (weight.rows, weight.cols):
+            raise ValueError(f"w must have shape {(weight.rows, weight.cols)}")
+        y, (codes_t, scales_t) = fp8_linear_forward(x, weight, out_dtype=x.dtype)
+        ctx.save_for_backward(codes_t, scales_t)
+        ctx.weight, ctx.w_dtype = weight, w.dtype
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        dx, dw = fp8_linear_backward(dy.contiguous(), ctx.saved_tensors, ctx.weight,
+                                     out_dtype=dy.dtype, grad_dtype=ctx.w_dtype)
+        return dx, dw, None

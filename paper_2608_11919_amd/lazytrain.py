@@ -140,6 +140,17 @@ def lib() -> ctypes.CDLL:
                                ctypes.c_int, ctypes.c_int, ctypes.c_double, ctypes.c_double,
                                ctypes.c_int, ctypes.c_double, ctypes.c_double, ctypes.c_int, vp,
                                vp, vp, vp, ctypes.c_size_t, vp]
+    i64 = ctypes.c_int64
+    L.lt_fp8_code_pitch.argtypes = [i64]
+    L.lt_fp8_code_pitch.restype = i64
+    L.lt_fp8_scale_pitch.argtypes = [i64]
+    L.lt_fp8_scale_pitch.restype = i64
+    L.lt_fp8_quantize.argtypes = [vp, ctypes.c_int, i64, i64, i64, ctypes.c_int, vp, vp, vp, vp,
+                                  vp]
+    L.lt_fp8_matmul_workspace_bytes.argtypes = [i64, i64, i64]
+    L.lt_fp8_matmul_workspace_bytes.restype = ctypes.c_size_t
+    L.lt_fp8_matmul.argtypes = [vp, vp, vp, vp, i64, i64, i64, vp, ctypes.c_int, i64, vp,
+                                ctypes.c_size_t, vp]
     L.lt_read_status.argtypes = [vp, vp, ctypes.POINTER(ctypes.c_int32)]
     L.lt_set_max_workgroups.argtypes = [ctypes.c_int]
     L.lt_workspace_release.argtypes = [vp]
@@ -150,7 +161,8 @@ def lib() -> ctypes.CDLL:
                  "lt_set_max_workgroups", "lt_streamed_hybrid8bit_adamw_step",
                  "lt_adamw_fp32_step", "lt_select_8bit_slice", "lt_workspace_release",
                  "lt_grad_sqnorm_noalloc", "lt_step_table", "lt_step_state_init",
-                 "lt_step_state_advance", "lt_orthogonalize", "lt_muon_step"):
+                 "lt_step_state_advance", "lt_orthogonalize", "lt_muon_step",
+                 "lt_fp8_quantize", "lt_fp8_matmul"):
         getattr(L, name).restype = ctypes.c_int
     _lib = L
     return L

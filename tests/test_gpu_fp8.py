@@ -1,0 +1,345 @@
+"""8-bit floating-point quantizer, products and linear layer on the GPU.
+
+The quantizer is bitwise: its scales come from exponents and its codes from one rounding, which
+numpy and the definition in 64 bits give alike.  A product of two codes is exact in fp32, and so is its scaling.  The matrix instruction
+cuts the products of eight neighbours off at 2^-13 of the largest one's power of two, toward
+zero, before it adds them (seen with powers of two in every pair of places): at most
+7 * 2^-13 of the largest product of the eight, which is at most the product of the largest
+values of each side.  Sums of eight are added in fp32: (K / 8 + 2) * 2^-24 of the sum of
+magnitudes at most.  bf16 results, seven fraction bits, round by 2^-8 of themselves."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2608_11919_amd as lt
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def decode(codes):
+    """Values of e4m3 bytes, in 64 bits."""
+    c = codes.astype(np.int64)
+    e, f = (c >> 3) & 15, (c & 7).astype(np.float64)
+    v = np.where(e > 0, (1 + f / 8) * 2.0 ** (e - 7), f / 8 * 2.0 ** -6)
+    return np.where((c & 127) == 127, np.nan, np.where(c >= 128, -v, v))
+
+
+def grid():
+    """The non-negative values of the format, rising."""
+    return decode(np.arange(127))
+
+
+def round_to_grid(v):
+    """Nearest value of the format, ties to the even code, of |v| <= 448."""
+    g = grid()
+    hi = np.searchsorted(g, np.abs(v)).clip(0, 126)
+    lo = (hi - 1).clip(0)
+    d_hi, d_lo = g[hi] - np.abs(v), np.abs(v) - g[lo]
+    take_lo = (d_lo < d_hi) | ((d_lo == d_hi) & (lo % 2 == 0))
+    return np.where(take_lo, g[lo], g[hi]) * np.sign(v)
+
+
+def expected(x, square):
+    """(values, biased exponents by row and group) of x in 64 bits."""
+    rows, cols = x.shape
+    br = 128 if square else 1
+    g = np.zeros((-(-rows // br) * br, -(-cols // 128) * 128))
+    g[:rows, :cols] = x
+    g = g.reshape(g.shape[0] // br, br, -1, 128)
+    top = np.abs(g).max((1, 3), keepdims=True)
+    with np.errstate(divide="ignore"):
+        e = np.ceil(np.log2(top / 448.0))
+    for _ in range(2):
+        e = np.where(top > 448.0 * 2.0 ** e, e + 1, e)
+        e = np.where(top <= 448.0 * 2.0 ** (e - 1), e - 1, e)
+    e = np.where(top > 0, np.maximum(e, -126), 0)
+    v = (round_to_grid(g / 2.0 ** e) * 2.0 ** e).reshape(-1, g.shape[2] * 128)[:rows, :cols]
+    return v, np.broadcast_to(e + 127, g.shape[:3] + (1,))[..., 0].reshape(-1, g.shape[2])[:rows]
+
+
+def values(codes, scales, cols):
+    """What codes and scales stand for, in 64 bits, and the scales' bytes."""
+    c, s = codes.cpu().numpy(), scales.cpu().numpy()
+    p = 2.0 ** (s.astype(np.float64) - 127)
+    p = np.repeat(p, 128, 1)[:, :c.shape[1]]
+    return (decode(c) * p)[:, :cols], s
+
+
+def quantize(x, square=False, both=True):
+    rows, cols = x.shape
+    mk = lambda r, c: torch.full((r, c), 99, dtype=torch.uint8, device=DEV)
+    codes, scales = mk(rows, lt.lt_fp8_code_pitch(cols)), mk(rows, lt.lt_fp8_scale_pitch(cols))
+    codes_t, scales_t = mk(cols, lt.lt_fp8_code_pitch(rows)), mk(cols, lt.lt_fp8_scale_pitch(rows))
+    if both:
+        lt.lt_fp8_quantize(x, codes, scales, codes_t, scales_t, square=square)
+    else:
+        lt.lt_fp8_quantize(x, codes, scales, square=square)
+        lt.lt_fp8_quantize(x, codes_t=codes_t, scales_t=scales_t, square=square)
+    return codes, scales, codes_t, scales_t
+
+
+def matrix(rows, cols, seed, dtype, spread=True):
+    gen = torch.Generator(DEV).manual_seed(seed)
+    x = torch.randn(rows, cols, device=DEV, generator=gen)
+    if spread:  # magnitudes over several decades, so that codes and scales of every kind occur
+        x = x * torch.exp(3 * torch.randn(rows, 1, device=DEV, generator=gen)) * \
+            torch.exp(2 * torch.randn(1, cols, device=DEV, generator=gen))
+    return x.to(dtype)
+
+
+QSHAPES = [(1, 1), (1, 129), (5, 128), (128, 128), (129, 127), (300, 257), (64, 700), (257, 1030)]
+
+
+@pytest.mark.parametrize("shape", QSHAPES)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("square", [False, True])
+def test_quantizer(shape, dtype, square):
+    x = matrix(*shape, 3, dtype)
+    if shape[0] > 4:
+        x[3] = 0.0                       # a row of zeros
+        x[2, :1] = 1e-38                 # a group of tiny values
+    rows, cols = shape
+    host = x.double().cpu().numpy()
+    for both in (True, False):
+        codes, scales, codes_t, scales_t = quantize(x, square, both)
+        for c, s, h in ((codes, scales, host), (codes_t, scales_t, host.T)):
+            got, bytes_ = values(c, s, h.shape[1])
+            want, e = expected(h, square)
+            assert np.array_equal(bytes_[:, :e.shape[1]], e)
+            assert (bytes_[:, e.shape[1]:] == 127).all()
+            assert np.array_equal(got, want)
+            assert not c.cpu().numpy()[:, h.shape[1]:].any()
+    if square:
+        a, _ = values(codes, scales, cols)
+        b, _ = values(codes_t, scales_t, rows)
+        assert np.array_equal(a, b.T)
+
+
+def test_quantizer_edges():
+    """Exact bounds of a scale, ties, subnormal codes, largest and smallest numbers."""
+    x = torch.zeros(6, 128, device=DEV)
+    x[0, :3] = torch.tensor([448.0, -448.0, 1.0])
+    x[1, 0] = 448.00003                               # just past: twice the scale
+    x[2, :4] = torch.tensor([448.0, 17.0, 19.0, 2.0 ** -10])   # ties; half the least code
+    x[3, 0] = torch.finfo(torch.float32).max
+    x[4, 0] = 2.0 ** -149
+    x[5, :2] = torch.tensor([448.0, 3 * 2.0 ** -10])  # a tie between codes 1 and 2
+    codes, scales, _, _ = quantize(x)
+    got, s = values(codes, scales, 128)
+    want, e = expected(x.double().cpu().numpy(), False)
+    assert np.array_equal(got, want) and np.array_equal(s[:, :1], e)
+    assert list(s[:3, 0]) == [127, 128, 127] and s[4, 0] == 1
+    assert list(got[2, :4]) == [448.0, 16.0, 20.0, 0.0]
+    assert got[5, 1] == 4 * 2.0 ** -10
+
+
+@pytest.mark.parametrize("square", [False, True])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_values_that_are_not_finite(square, bad):
+    x = matrix(200, 300, 5, torch.float32, spread=False)
+    x[150, 140] = bad
+    codes, scales, codes_t, scales_t = quantize(x, square)
+    got, _ = values(codes, scales, 300)
+    hit = np.zeros((200, 300), bool)
+    hit[128:200 if square else 150 + 1, 128:256] = True
+    if not square:
+        hit[:150] = False
+    assert np.isnan(got[hit]).all() and np.isfinite(got[~hit]).all()
+    out = torch.empty(200, 64, device=DEV)
+    w = lt.Fp8Weight.from_master(matrix(64, 300, 6, torch.float32, spread=False))
+    lt.lt_fp8_matmul(codes, scales, w.codes, w.scales, 300, out)
+    rows = hit.any(1)
+    o = out.cpu().numpy()
+    assert np.isnan(o[rows]).all() and np.isfinite(o[~rows]).all()
+
+
+def test_strided_rows():
+    base = matrix(130, 700, 7, torch.bfloat16)
+    for view in (base[:, :300], base[:, 8:309], base[::3, :256], base[:, :1]):
+        want = quantize(view.contiguous())
+        got = quantize(view) if view.data_ptr() % 16 == 0 else None
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+
+
+def check(out, a, b):
+    """out against A B^T in 64 bits (a, b: values)."""
+    a, b = torch.from_numpy(a).to(DEV), torch.from_numpy(b).to(DEV)
+    want, size = a @ b.t(), a.abs() @ b.abs().t()
+    k = a.shape[1]
+    eight = lambda x: torch.nn.functional.pad(x.abs(), (0, -k % 8)).unflatten(1, (-1, 8)).amax(2)
+    bound = 7 * 2.0 ** -13 * (eight(a) @ eight(b).t()) + (k / 8 + 2) * 2.0 ** -24 * size
+    if out.dtype == torch.bfloat16:
+        bound = bound + 2.0 ** -8 * (want.abs() + bound) + 2.0 ** -133
+    off = (out.double() - want).abs()
+    assert (off <= bound).all(), (tuple(out.shape), k, (off / bound.clamp_min(1e-300)).max().item())
+
+
+SHAPES = [(1, 1, 1), (1, 64, 128), (3, 100, 130), (16, 300, 2048), (17, 256, 129), (33, 70, 5000),
+          (64, 1000, 700), (65, 65, 65), (128, 128, 512), (200, 333, 1030), (513, 257, 640),
+          (1000, 2100, 300), (4096, 4224, 256), (4100, 4200, 129)]
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_products(shape, dtype):
+    m, n, k = shape
+    a = quantize(matrix(m, k, 11, torch.float32, spread=m < 600))
+    b = quantize(matrix(n, k, 12, torch.float32, spread=m < 600), square=True)
+    out = torch.full((m, n), float("nan"), device=DEV, dtype=dtype)
+    lt.lt_fp8_matmul(a[0], a[1], b[0], b[1], k, out)
+    check(out, values(a[0], a[1], k)[0], values(b[0], b[1], k)[0])
+    again = torch.empty_like(out)
+    lt.lt_fp8_matmul(a[0], a[1], b[0], b[1], k, again)
+    assert torch.equal(out, again)
+
+
+@pytest.mark.parametrize("shape", [(5, 40, 300), (130, 140, 513), (300, 2500, 1000)])
+def test_results_into_rows_of_a_wider_matrix(shape):
+    m, n, k = shape
+    a = quantize(matrix(m, k, 13, torch.bfloat16))
+    b = quantize(matrix(n, k, 14, torch.bfloat16))
+    for dtype in (torch.float32, torch.bfloat16):
+        whole = torch.full((m, n + 13), 5.0, device=DEV, dtype=dtype)
+        lt.lt_fp8_matmul(a[0], a[1], b[0], b[1], k, whole[:, :n])
+        check(whole[:, :n], values(a[0], a[1], k)[0], values(b[0], b[1], k)[0])
+        assert (whole[:, n:] == 5.0).all()
+
+
+def test_exact_small_integers():
+    """Sums of small integers are exact in any order, at every size of tile."""
+    for m, n, k in ((7, 50, 640), (100, 300, 1000), (1030, 2050, 384), (4097, 4097, 128)):
+        gen = torch.Generator(DEV).manual_seed(1)
+        x = torch.randint(-8, 9, (m, k), device=DEV, generator=gen).float()
+        w = torch.randint(-8, 9, (n, k), device=DEV, generator=gen).float()
+        a, b = quantize(x), quantize(w, square=True)
+        out = torch.empty(m, n, device=DEV)
+        lt.lt_fp8_matmul(a[0], a[1], b[0], b[1], k, out)
+        assert torch.equal(out, x @ w.t())
+
+
+def test_empty_sizes():
+    out = torch.full((3, 5), 7.0, device=DEV)
+    e = lambda r, c: torch.empty(r, c, dtype=torch.uint8, device=DEV)
+    lt.lt_fp8_matmul(e(3, 0), e(3, 0), e(5, 0), e(5, 0), 0, out)
+    assert not out.any()
+    w = lt.Fp8Weight.from_master(matrix(40, 70, 1, torch.float32))
+    assert lt.fp8_linear(torch.empty(0, 70, device=DEV), w).shape == (0, 40)
+    y, saved = lt.fp8_linear_forward(torch.empty(0, 70, device=DEV, dtype=torch.bfloat16), w)
+    dx, dw = lt.fp8_linear_backward(torch.empty(0, 40, device=DEV), saved, w)
+    assert dx.shape == (0, 70) and dw.shape == (40, 70) and not dw.any()
+
+
+LAYERS = [(1, 64, 64), (7, 130, 300), (64, 512, 256), (300, 257, 1000), (1024, 700, 1300)]
+
+
+@pytest.mark.parametrize("layer", LAYERS)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_linear_layer(layer, dtype):
+    t, k, n = layer
+    x, w = matrix(t, k, 21, dtype, False), matrix(n, k, 22, torch.float32, False)
+    dy = matrix(t, n, 23, dtype, False)
+    weight = lt.Fp8Weight.from_master(w)
+    y, saved = lt.fp8_linear_forward(x, weight)
+    assert torch.equal(y, lt.fp8_linear(x, weight)) and y.dtype == torch.bfloat16
+    dx, dw = lt.fp8_linear_backward(dy, saved, weight, out_dtype=torch.float32,
+                                    grad_dtype=torch.float32)
+    h = lambda v: v.double().cpu().numpy()
+    xv, wv = expected(h(x), False)[0], expected(h(w), True)[0]
+    check(y, xv, wv)
+    check(dx, expected(h(dy), False)[0], wv.T.copy())
+    check(dw, expected(h(dy).T, False)[0], expected(h(x).T, False)[0])
+
+
+def test_gradients_against_differences():
+    """Through autograd, against differences of the layer without rounding: quantization is off
+    by at most 2^-4 of a value, so gradients by 2^-3 of the sum of magnitudes, and far less
+    on average."""
+    t, k, n = 40, 96, 72
+    x = matrix(t, k, 31, torch.float32, False).requires_grad_()
+    w = matrix(n, k, 32, torch.float32, False).requires_grad_()
+    c = matrix(t, n, 33, torch.float32, False)
+    y = lt.Fp8Linear.apply(x, w, lt.Fp8Weight.from_master(w.detach()))
+    (y * c).sum().backward()
+    f = lambda a, b: ((a.double() @ b.double().t()) * c.double()).sum()
+    for p, grad, other in ((x, x.grad, w), (w, w.grad, x)):
+        size = (c.abs().double() @ w.abs().double() if p is x else
+                c.t().abs().double() @ x.abs().double())
+        for i, j in ((0, 0), (5, 17), (39, 95), (20, 50)):
+            d = torch.zeros_like(p, dtype=torch.float64)
+            d[i, j] = 1.0
+            up = f(x + d, w) - f(x - d, w) if p is x else f(x, w + d) - f(x, w - d)
+            assert abs(grad[i, j].item() - up.item() / 2) <= 2.0 ** -3 * size[i, j].item()
+    wide = torch.linalg.vector_norm(x.grad.double() - c.double() @ w.double())
+    assert wide <= 0.06 * torch.linalg.vector_norm(c.double() @ w.double())
+
+
+def test_leading_dimensions_and_other_streams():
+    w = lt.Fp8Weight.from_master(matrix(200, 300, 41, torch.float32, False))
+    x = matrix(60, 300, 42, torch.bfloat16, False)
+    want = lt.fp8_linear(x, w)
+    assert torch.equal(lt.fp8_linear(x.view(3, 20, 300), w), want.view(3, 20, 200))
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        got = lt.fp8_linear(x, w)
+    s.synchronize()
+    assert torch.equal(got, want)
+
+
+def test_in_a_graph():
+    w = lt.Fp8Weight.from_master(matrix(300, 4000, 51, torch.float32, False))
+    x = matrix(9, 4000, 52, torch.bfloat16, False)
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        lt.fp8_linear(x, w)
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        y = lt.fp8_linear(x, w)
+    for seed in (61, 62, 63):
+        x.copy_(matrix(9, 4000, seed, torch.bfloat16, False))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, lt.fp8_linear(x, w))
+        torch.cuda.synchronize()
+
+
+def test_refusals():
+    x = matrix(16, 256, 1, torch.float32)
+    codes, scales, codes_t, scales_t = quantize(x)
+    w = lt.Fp8Weight.from_master(x, transposed=False)
+    out = torch.empty(16, 16, device=DEV)
+    with pytest.raises(TypeError):
+        lt.lt_fp8_quantize(x.half(), codes, scales)
+    with pytest.raises(ValueError):
+        lt.lt_fp8_quantize(x.t(), codes, scales)          # rows are not contiguous
+    with pytest.raises(ValueError):
+        lt.lt_fp8_quantize(x, codes)                      # codes without scales
+    with pytest.raises(ValueError):
+        lt.lt_fp8_quantize(x, codes[:8], scales)
+    with pytest.raises(ValueError):
+        lt.lt_fp8_quantize(x, codes.float(), scales)
+    with pytest.raises(lt.LazyTrainError):
+        lt.lt_fp8_quantize(x)                             # no layout
+    with pytest.raises(lt.LazyTrainError):
+        lt.lt_fp8_quantize(x.view(-1)[1:257].view(1, 256), codes[:1], scales[:1])  # unaligned
+    with pytest.raises(ValueError):
+        lt.lt_fp8_matmul(codes, scales, codes[:8], scales[:8], 256, out)
+    with pytest.raises(ValueError):
+        lt.lt_fp8_matmul(codes, scales, codes, scales, 300, out)
+    with pytest.raises(TypeError):
+        lt.lt_fp8_matmul(codes, scales, codes, scales, 256, out.half())
+    with pytest.raises(ValueError):
+        lt.lt_fp8_matmul(codes, scales, codes, scales, 256, out.t())
+    with pytest.raises(ValueError):
+        lt.fp8_linear(x[:, :255], w)
+    with pytest.raises(ValueError):
+        w.update(x[:8])
+    y, saved = lt.fp8_linear_forward(x, w)
+    with pytest.raises(ValueError):
+        lt.fp8_linear_backward(y, saved, w)               # no transposed codes
+    L = lt.lib()
+    assert L.lt_fp8_matmul_workspace_bytes(-1, 4, 4) == 0
+    assert L.lt_fp8_matmul_workspace_bytes(4, 4, 1 << 23) == 0
