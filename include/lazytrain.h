@@ -25,7 +25,8 @@
  *   f5  orthogonalising matrices by Newton-Schulz products;
  *   f6  the Muon step with 8-bit momentum;
  *   f7  quantizing matrices to 8-bit floating point, a scale for each block of 128;
- *   f8  their products.
+ *   f8  their products;
+ *   f9  a linear layer's answer in one call.
  *
  * Conventions for every entry point:
  *  - Tensor data, workspace and scalar outputs are DEVICE pointers on the
@@ -568,6 +569,20 @@ size_t lt_fp8_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k);
  */
 lt_err lt_fp8_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes,
                      const uint8_t* b_scales, int64_t m, int64_t n, int64_t k, void* out,
+                     int out_dtype, int64_t out_stride, void* workspace, size_t workspace_bytes,
+                     void* stream);
+
+/* Bytes of device workspace lt_fp8_linear needs; 0 if an argument is invalid. */
+size_t lt_fp8_linear_workspace_bytes(int64_t m, int64_t n, int64_t k);
+
+/*
+ * f9: a linear layer's answer, out = x W^T: x (m x k, dtype, x_stride elements from row to row)
+ * is quantized on the way, W (n x k) is as lt_fp8_quantize stores it.  The same values as
+ * lt_fp8_quantize and lt_fp8_matmul, but where a sum is cut into other pieces; up to 16 rows
+ * of x take one launch.
+ */
+lt_err lt_fp8_linear(const void* x, int dtype, int64_t x_stride, const uint8_t* w_codes,
+                     const uint8_t* w_scales, int64_t m, int64_t n, int64_t k, void* out,
                      int out_dtype, int64_t out_stride, void* workspace, size_t workspace_bytes,
                      void* stream);
 

@@ -40,11 +40,11 @@ __device__ inline uint16_t bf16_bits(float x)
 
 // ------------------------------------------------------------- quantizer
 
-// Biased exponent of the scale for a group whose largest |x| has these bits, and its inverse.
+// Biased exponent of the scale for a group whose largest |x| has these bits, and the scale.
 // A group with an infinity or a NaN has the NaN scale (255), and NaN codes.
 struct Scale {
     uint32_t biased;
-    float inverse;
+    float power;  // 2^e, or NaN
 };
 
 __device__ inline Scale scale_of(uint32_t top)
@@ -57,14 +57,28 @@ __device__ inline Scale scale_of(uint32_t top)
     e = max(e, -126);
     e = top == 0u ? 0 : e;
     s.biased = uint32_t(e + 127);
-    s.inverse = __uint_as_float(uint32_t(127 - e) << 23);
+    s.power = __uint_as_float(uint32_t(127 + e) << 23);
     return s;
 }
 
-__device__ inline uint32_t pack_codes(float a, float b, float c, float d)
+// Four codes of values divided by a power of two, in the conversion itself.
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+__device__ inline uint32_t pack_codes(float a, float b, float c, float d, float power)
 {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-    return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true));
+    s16x2 w = {0, 0};
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, a, b, power, false);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, c, d, power, true);
+    return __builtin_bit_cast(uint32_t, w);
+}
+
+__device__ inline uint32_t pack_codes(uint32_t ab, uint32_t cd, float power)
+{
+    s16x2 w = {0, 0};
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, ab), power, false);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, cd), power, true);
+    return __builtin_bit_cast(uint32_t, w);
 }
 
 struct QuantizeArgs {
@@ -169,12 +183,9 @@ __global__ __launch_bounds__(kQuantizeThreads) void k_fp8_quantize(QuantizeArgs 
                 if (row >= a.rows)
                     continue;
                 const float(&w)[8] = v[h][r];
-                uint32_t lo = pack_codes(w[0] * s.inverse, w[1] * s.inverse, w[2] * s.inverse,
-                                         w[3] * s.inverse);
-                uint32_t hi = pack_codes(w[4] * s.inverse, w[5] * s.inverse, w[6] * s.inverse,
-                                         w[7] * s.inverse);
                 *reinterpret_cast<uint2*>(a.codes + row * a.pitch + c0 + 8 * l) =
-                    make_uint2(lo, hi);
+                    make_uint2(pack_codes(w[0], w[1], w[2], w[3], s.power),
+                               pack_codes(w[4], w[5], w[6], w[7], s.power));
                 uint8_t* to = a.scales + row * a.scale_pitch + group;
                 if (l == 0)
                     *to = uint8_t(s.biased);
@@ -219,8 +230,7 @@ __global__ __launch_bounds__(kQuantizeThreads) void k_fp8_quantize(QuantizeArgs 
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 *reinterpret_cast<uint32_t*>(turned + (8 * l + e) * kTurnPitch + 64 * h + 4 * q) =
-                    pack_codes(v[h][0][e] * s[e].inverse, v[h][1][e] * s[e].inverse,
-                               v[h][2][e] * s[e].inverse, v[h][3][e] * s[e].inverse);
+                    pack_codes(v[h][0][e], v[h][1][e], v[h][2][e], v[h][3][e], s[e].power);
         __syncthreads();
         for (int i = t; i < kGroup * 8; i += kQuantizeThreads) {
             const int64_t col = c0 + i / 8;
@@ -360,6 +370,225 @@ __global__ __launch_bounds__(256) void k_fp8_join(const float* __restrict__ part
     }
 }
 
+// ------------------------------------------------------------- few tokens
+
+// y for up to 16 T tokens, bound by reading the weight once: no LDS tiles, every lane loads its
+// 32 bytes of the instruction's 16 weight rows straight from HBM.  The waves of a workgroup
+// share R blocks of 16 rows and cut the sum.  x comes as
+// codes, or (T = 1) as it is: a lane then quantizes the 32 values of its token that it
+// multiplies, with the group's maximum from the other three lanes that hold the group, so that a
+// single token is one launch and x never waits for a pass of its own.
+struct FewArgs {
+    const uint8_t *w, *w_scales;
+    const void* x;               // codes, or values
+    const uint8_t* x_scales;
+    int64_t m, n, k;
+    int64_t pitch, scale_pitch;  // of the weight's rows, and of x's codes
+    int64_t x_stride;            // of x's values
+    int steps;
+    void* out;
+    int64_t stride;
+};
+
+enum { kCodes, kF32, kBf16 };
+
+struct FewToken {
+    i32x8 codes;
+    uint32_t scale;
+};
+
+// What a lane has of its token and one step, as loaded: 32 codes and their scale, or 32 values.
+template <int X>
+struct FewInput {
+    static constexpr int kWords = X == kCodes ? 2 : (X == kBf16 ? 4 : 8);
+    i32x4 w[kWords];
+    uint32_t scale;
+};
+
+template <typename T>
+__device__ inline void few_load(const T* row, int64_t k, int s, int q, bool aligned, i32x4* w)
+{
+    const int64_t at = int64_t(s) * kGroup + 32 * q;
+    const T* p = row + at;
+    constexpr int kWords = int(32 * sizeof(T) / 16);
+    if (aligned && at + 32 <= k) {
+#pragma unroll
+        for (int c = 0; c < kWords; ++c)
+            w[c] = reinterpret_cast<const i32x4*>(p)[c];
+        return;
+    }
+#pragma unroll
+    for (int c = 0; c < kWords; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (sizeof(T) == 2) {
+                const int i = 8 * c + 2 * e;
+                const uint32_t lo = at + i < k ? p[i] : 0u, hi = at + i + 1 < k ? p[i + 1] : 0u;
+                w[c][e] = int(lo | hi << 16);
+            } else {
+                w[c][e] = at + 4 * c + e < k ? __float_as_int(p[4 * c + e]) : 0;
+            }
+        }
+}
+
+template <int X>
+__device__ inline FewToken few_quantize(const FewInput<X>& in)
+{
+    FewToken f;
+    if constexpr (X == kCodes) {
+        f.codes = i32x8{in.w[0][0], in.w[0][1], in.w[0][2], in.w[0][3],
+                        in.w[1][0], in.w[1][1], in.w[1][2], in.w[1][3]};
+        f.scale = in.scale;
+        return f;
+    }
+    constexpr int kWords = FewInput<X>::kWords;
+    uint32_t top = 0;
+    if constexpr (X == kBf16) {
+        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+        u16x2 most = {0, 0};  // a bf16's magnitude is its pattern without the sign
+#pragma unroll
+        for (int c = 0; c < kWords; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                most = __builtin_elementwise_max(
+                    most, __builtin_bit_cast(u16x2, uint32_t(in.w[c][e]) & 0x7FFF7FFFu));
+        top = uint32_t(max(most[0], most[1])) << 16;
+    } else {
+#pragma unroll
+        for (int c = 0; c < kWords; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                top = max(top, uint32_t(in.w[c][e]) & 0x7FFFFFFFu);
+    }
+    top = max(top, uint32_t(__shfl_xor(int(top), 16, 64)));
+    top = max(top, uint32_t(__shfl_xor(int(top), 32, 64)));
+    const Scale scale = scale_of(top);
+    f.scale = scale.biased;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if constexpr (X == kBf16) {
+            f.codes[e] = int(pack_codes(uint32_t(in.w[e / 2][e % 2 * 2]),
+                                        uint32_t(in.w[e / 2][e % 2 * 2 + 1]), scale.power));
+        } else {
+            const i32x4 v = in.w[e];
+            f.codes[e] = int(pack_codes(__int_as_float(v[0]), __int_as_float(v[1]),
+                                        __int_as_float(v[2]), __int_as_float(v[3]), scale.power));
+        }
+    }
+    return f;
+}
+
+__device__ inline i32x8 load_codes(const uint8_t* p)
+{
+    const i32x4 a = reinterpret_cast<const i32x4*>(p)[0], b = reinterpret_cast<const i32x4*>(p)[1];
+    return i32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+}
+
+template <int T, int R, int X, bool F32>
+__global__ __launch_bounds__(512) void k_fp8_few(FewArgs g)
+{
+    extern __shared__ float sums[];  // [wave][R][T][lane][4]
+    const int lane = int(threadIdx.x) & 63, r = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+    const int waves = int(blockDim.x) >> 6;
+    const int64_t n0 = int64_t(blockIdx.x) * 16 * R;
+    const uint8_t *w[R], *ws[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        int64_t row = n0 + 16 * i + r;
+        row = row < g.n ? row : g.n - 1;
+        w[i] = g.w + row * g.pitch + 32 * q;
+        ws[i] = g.w_scales + row * g.scale_pitch;
+    }
+    int64_t token[T];
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+        token[t] = 16 * t + r;
+        token[t] = token[t] < g.m ? token[t] : g.m - 1;
+    }
+    const bool aligned = (g.x_stride * (X == kF32 ? 4 : 2)) % 16 == 0;
+    f32x4 acc[R][T] = {};
+    // one step is under way while the one before is multiplied
+    struct Loaded {
+        i32x8 a[R];
+        uint32_t as[R];
+        FewInput<X> x[T];
+    };
+    const auto load = [&](int s, Loaded& in) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            in.a[i] = load_codes(w[i] + int64_t(s) * kGroup);
+            in.as[i] = ws[i][s];
+        }
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            if constexpr (X == kCodes) {
+                const auto* p = reinterpret_cast<const i32x4*>(
+                    static_cast<const uint8_t*>(g.x) + token[t] * g.pitch + int64_t(s) * kGroup +
+                    32 * q);
+                in.x[t].w[0] = p[0];
+                in.x[t].w[1] = p[1];
+                in.x[t].scale = g.x_scales[token[t] * g.scale_pitch + s];
+            } else if constexpr (X == kF32) {
+                few_load(static_cast<const float*>(g.x) + token[t] * g.x_stride, g.k, s, q, aligned,
+                         in.x[t].w);
+            } else {
+                few_load(static_cast<const uint16_t*>(g.x) + token[t] * g.x_stride, g.k, s, q,
+                         aligned, in.x[t].w);
+            }
+        }
+    };
+    const auto multiply = [&](const Loaded& in) {
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            const FewToken f = few_quantize<X>(in.x[t]);
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+                acc[i][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                    in.a[i], f.codes, acc[i][t], 0, 0, 0, int(in.as[i]), 0, int(f.scale));
+        }
+    };
+    // each wave has a run of neighbouring steps: its rows are read in long pieces
+    const int first = g.steps * wave / waves, last = g.steps * (wave + 1) / waves;
+    if (first < last) {
+        Loaded even, odd;
+        load(first, even);
+        int s = first;
+        for (; s + 1 < last; s += 2) {
+            load(s + 1, odd);
+            multiply(even);
+            if (s + 2 < last)
+                load(s + 2, even);
+            multiply(odd);
+        }
+        if (s < last)
+            multiply(even);
+    }
+    // the waves' sums, added in their order: acc[i][t][e] is row 16 i + 4 q + e, token 16 t + r
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int t = 0; t < T; ++t)
+            *reinterpret_cast<f32x4*>(sums + (((wave * R + i) * T + t) * 64 + lane) * 4) =
+                acc[i][t];
+    __syncthreads();
+    for (int e = threadIdx.x; e < R * T * 256; e += int(blockDim.x)) {
+        float v = sums[e];
+        for (int i = 1; i < waves; ++i)
+            v += sums[i * R * T * 256 + e];
+        const int l = e / 4 % 64, block = e / 256;
+        const int64_t row = n0 + 16 * (block / T) + 4 * (l >> 4) + e % 4;
+        const int64_t tok = 16 * (block % T) + (l & 15);
+        if (row >= g.n || tok >= g.m)
+            continue;
+        const int64_t to = tok * g.stride + row;
+        if constexpr (F32)
+            static_cast<float*>(g.out)[to] = v;
+        else
+            static_cast<uint16_t*>(g.out)[to] = bf16_bits(v);
+    }
+}
+
 template <bool F32>
 __global__ __launch_bounds__(256) void k_fp8_zero(int64_t m, int64_t n, void* out, int64_t stride)
 {
@@ -426,6 +655,58 @@ void launch_product(const ProductArgs& g, const Way& w, bool f32, hipStream_t st
         k_fp8_product<Tile, false><<<grid, Tile::kThreads, 0, st>>>(g);
 }
 
+// Tokens that the kernel for few takes, and up to which it takes them unquantized.  At 64 the
+// tiles are faster: 2048 x 11008 21 us against 31, 5120 x 17408 45 against 70; at 32 19 against
+// 21 and 47 against 45.
+constexpr int64_t kFewTokens = 32;
+constexpr int64_t kFewValues = 16;
+
+template <int T, int R, int X>
+void launch_few_rows(const FewArgs& g, bool f32, hipStream_t st)
+{
+    // eight waves where four would not give every CU sixteen and the sum is long enough to cut
+    const int64_t groups = host::ceil_div(g.n, 16 * R);
+    const int waves = groups * 4 < 4096 && g.steps >= 8 ? 8 : 4;
+    const size_t lds = size_t(waves) * R * T * 1024;
+    auto* kernel = f32 ? k_fp8_few<T, R, X, true> : k_fp8_few<T, R, X, false>;
+    kernel<<<dim3(uint32_t(groups)), 64 * waves, lds, st>>>(g);
+}
+
+// Two blocks of 16 rows share a token's codes where that leaves every CU two workgroups (a token
+// through 2048 x 151936: 64 us, with one block 79; through 2048 x 2048 4.8, with two 5.8).
+template <int T, int X>
+void launch_few(const FewArgs& g, bool f32, hipStream_t st)
+{
+    if (g.n >= 32 * 512)
+        launch_few_rows<T, 2, X>(g, f32, st);
+    else
+        launch_few_rows<T, 1, X>(g, f32, st);
+}
+
+void launch_few_codes(const FewArgs& g, bool f32, hipStream_t st)
+{
+    if (g.m <= 16)
+        launch_few<1, kCodes>(g, f32, st);
+    else
+        launch_few<2, kCodes>(g, f32, st);
+}
+
+// Workspace of lt_fp8_linear where x is quantized apart: [codes][scales][matmul's].
+struct LinearLayout {
+    size_t scales, matmul, total;
+};
+
+LinearLayout linear_layout(int64_t m, int64_t n, int64_t k)
+{
+    LinearLayout l{0, 0, 256};
+    if (m <= kFewValues)
+        return l;
+    l.scales = host::round_up(size_t(m) * size_t(code_pitch(k)), 256);
+    l.matmul = l.scales + host::round_up(size_t(m) * size_t(scale_pitch(k)), 256);
+    l.total = l.matmul + lt_fp8_matmul_workspace_bytes(m, n, k);
+    return l;
+}
+
 }  // namespace
 
 extern "C" {
@@ -481,6 +762,8 @@ size_t lt_fp8_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k)
 {
     if (!valid_sizes(m, n, k))
         return 0;
+    if (m <= kFewTokens)
+        return 256;
     const Way w = way_of(m, n, k);
     return std::max(size_t(256),
                     w.slices > 1 ? size_t(w.slices) * size_t(m) * size_t(n) * 4 : size_t(0));
@@ -513,6 +796,13 @@ lt_err lt_fp8_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const uint
         LT_TRY_HIP(hipGetLastError());
         return LT_OK;
     }
+    if (m <= kFewTokens) {
+        const FewArgs f{b_codes, b_scales, a_codes, a_scales, m, n, k, code_pitch(k),
+                        scale_pitch(k), 0, int(host::ceil_div(k, kGroup)), out, out_stride};
+        launch_few_codes(f, f32, st);
+        LT_TRY_HIP(hipGetLastError());
+        return LT_OK;
+    }
     ProductArgs g{a_codes, a_scales,   b_codes, b_scales,   m,      n, code_pitch(k),
                   scale_pitch(k), int(host::ceil_div(k, kGroup)), w.slice, out, out_stride, nullptr};
     if (w.slices > 1) {
@@ -535,6 +825,57 @@ lt_err lt_fp8_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const uint
     }
     LT_TRY_HIP(hipGetLastError());
     return LT_OK;
+}
+
+size_t lt_fp8_linear_workspace_bytes(int64_t m, int64_t n, int64_t k)
+{
+    return valid_sizes(m, n, k) ? linear_layout(m, n, k).total : 0;
+}
+
+lt_err lt_fp8_linear(const void* x, int dtype, int64_t x_stride, const uint8_t* w_codes,
+                     const uint8_t* w_scales, int64_t m, int64_t n, int64_t k, void* out,
+                     int out_dtype, int64_t out_stride, void* workspace, size_t workspace_bytes,
+                     void* stream)
+{
+    host::clear_error();
+    if (!valid_sizes(m, n, k) || out_stride < n || x_stride < k)
+        return fail(LT_ERR_INVALID_ARG, "need 0 <= m, n < 2^31, 0 <= k < 2^23, x_stride >= k and "
+                                        "out_stride >= n");
+    if ((dtype != LT_DTYPE_F32 && dtype != LT_DTYPE_BF16) ||
+        (out_dtype != LT_DTYPE_F32 && out_dtype != LT_DTYPE_BF16))
+        return fail(LT_ERR_INVALID_ARG, "dtypes must be LT_DTYPE_F32 or LT_DTYPE_BF16");
+    if (m == 0 || n == 0)
+        return LT_OK;
+    if (!out || (k > 0 && (!x || !w_codes || !w_scales)))
+        return fail(LT_ERR_INVALID_ARG, "x, the weight and out must not be NULL");
+    if (!host::aligned(x, 16) || !host::aligned(w_codes, 16) || !host::aligned(out, 16) ||
+        !host::aligned(w_scales, 4))
+        return fail(LT_ERR_ALIGNMENT, "x, codes and out must be 16-byte aligned, scales 4-byte");
+    if (k == 0)
+        return lt_fp8_matmul(nullptr, nullptr, nullptr, nullptr, m, n, k, out, out_dtype,
+                             out_stride, nullptr, 0, stream);
+    if (m <= kFewValues) {
+        const FewArgs f{w_codes, w_scales, x, nullptr, m, n, k, code_pitch(k), scale_pitch(k),
+                        x_stride, int(host::ceil_div(k, kGroup)), out, out_stride};
+        const bool f32 = out_dtype == LT_DTYPE_F32;
+        const hipStream_t st = static_cast<hipStream_t>(stream);
+        if (dtype == LT_DTYPE_F32)
+            launch_few<1, kF32>(f, f32, st);
+        else
+            launch_few<1, kBf16>(f, f32, st);
+        LT_TRY_HIP(hipGetLastError());
+        return LT_OK;
+    }
+    const LinearLayout l = linear_layout(m, n, k);
+    if (!workspace || !host::aligned(workspace, 256) || workspace_bytes < l.total)
+        return fail(LT_ERR_WORKSPACE, "workspace must be 256-byte aligned and hold " +
+                                          std::to_string(l.total) + " bytes");
+    auto* ws = static_cast<uint8_t*>(workspace);
+    if (lt_err e = lt_fp8_quantize(x, dtype, m, k, x_stride, 0, ws, ws + l.scales, nullptr,
+                                   nullptr, stream))
+        return e;
+    return lt_fp8_matmul(ws, ws + l.scales, w_codes, w_scales, m, n, k, out, out_dtype, out_stride,
+                         ws + l.matmul, l.total - l.matmul, stream);
 }
 
 }  // extern "C"

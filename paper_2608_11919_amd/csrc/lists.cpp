@@ -118,11 +118,58 @@ PyObject* covers(PyObject*, PyObject* const* args, Py_ssize_t n_args)
     Py_RETURN_TRUE;
 }
 
+// sides(tensors) -> (rows, cols) or None: bytes objects of one 64-bit word per tensor; None
+// unless it is a list or tuple of plain tensors of two dimensions.
+PyObject* sides(PyObject*, PyObject* const* args, Py_ssize_t n_args)
+{
+    if (n_args != 1) {
+        PyErr_SetString(PyExc_TypeError, "sides(tensors)");
+        return nullptr;
+    }
+    PyObject* list = args[0];
+    const bool is_list = PyList_CheckExact(list);
+    if (!(is_list || PyTuple_CheckExact(list)) || at::impl::torch_function_mode_enabled())
+        Py_RETURN_NONE;
+    const Py_ssize_t n = is_list ? PyList_GET_SIZE(list) : PyTuple_GET_SIZE(list);
+    PyObject* side[2] = {PyBytes_FromStringAndSize(nullptr, 8 * n),
+                         PyBytes_FromStringAndSize(nullptr, 8 * n)};
+    bool in_order = side[0] && side[1];
+    const bool memory = in_order;
+    try {
+        for (Py_ssize_t i = 0; i < n && in_order; ++i) {
+            PyObject* o = is_list ? PyList_GET_ITEM(list, i) : PyTuple_GET_ITEM(list, i);
+            if (!THPVariable_CheckExact(o) || THPVariable_Unpack(o).dim() != 2) {
+                in_order = false;
+                break;
+            }
+            for (int d = 0; d < 2; ++d) {
+                const int64_t size = THPVariable_Unpack(o).size(d);
+                std::memcpy(PyBytes_AS_STRING(side[d]) + 8 * i, &size, 8);
+            }
+        }
+    } catch (const std::exception&) {
+        in_order = false;
+    }
+    PyObject* out = nullptr;
+    if (in_order) {
+        out = PyTuple_Pack(2, side[0], side[1]);
+    } else if (memory) {
+        PyErr_Clear();
+        out = Py_None;
+        Py_INCREF(out);
+    }
+    Py_XDECREF(side[0]);
+    Py_XDECREF(side[1]);
+    return out;
+}
+
 PyMethodDef methods[] = {
     {"take", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(take)), METH_FASTCALL,
      "Addresses, sizes and dtype of a list of contiguous tensors on one device, or None."},
     {"covers", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(covers)), METH_FASTCALL,
      "Whether every have[i] holds ceil(sizes[i] / block) entries."},
+    {"sides", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(sides)), METH_FASTCALL,
+     "Rows and columns of a list of matrices, or None."},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lists", nullptr, -1, methods,

@@ -537,16 +537,17 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_orth_up
 
 // ---------------------------------------------------------------- thin matrices
 //
-// A matrix with n <= 32 rows (or columns) and at most 2^17 elements, by one workgroup in one
-// launch: with G = X X^T, every step stays n x n (P = a I + b G + c G G, G' = P G P, R' = P R),
-// and the result is R X.  Adapters, small layers and odd leftovers come in hundreds, and the
-// general path would pad each to 128 and take 18 launches.  Its arithmetic is small (17
-// products of n x n); what it waits for is one workgroup's reads, twice over X, and the steps
-// one after the other.  An error of G grows by a^2 with every step in directions of small
-// singular values, 2e5 in five: G and the steps are in 64 bits (in 32 a 64 x 64 matrix with a
-// few strong directions ends 5e-3 off), R X in 32.
+// A matrix with n <= 32 rows (or columns), padded to 16 or 32 of at most 2^17 elements, by one
+// workgroup in one launch: with G = X X^T, every step stays n x n (P = a I + b G + c G G,
+// G' = P G P, R' = P R), and the result is R X.  Adapters, small layers and odd leftovers come
+// in hundreds, and the general path would pad each to 128 and take 18 launches.  An error of G
+// grows by a^2 with every step in directions of small singular values, 2e5 in five: G and the
+// steps are in 64 bits (in 32 a 64 x 64 matrix with a few strong directions ends 5e-3 off), R X
+// in 32.  The norm is G's trace, so X is read once, into LDS, where it fits, and else twice.
+// What bounds it is latency: one workgroup's reads, 16 n^2 products of m values at the 64-bit
+// rate, and the steps one after the other.
 
-constexpr int kThinThreads = 512;
+constexpr int kThinThreads = 512, kThinWaves = kThinThreads / 64;
 constexpr int kThinSide = 32;
 constexpr int64_t kThinElems = int64_t(1) << 17;
 
@@ -554,29 +555,58 @@ typedef double f64x4 __attribute__((ext_vector_type(4)));
 
 template <int NP>
 struct Thin {
-    static constexpr int kWidth = NP == 16 ? 1024 : 256;  // columns of X at a time
-    static constexpr int kPitch = kWidth + 4, kSidePitch = NP + 2, kBlocks = NP / 16;
-    typedef double Sym[NP][kSidePitch];
+    static constexpr int kBlocks = NP / 16, kUpper = kBlocks * (kBlocks + 1) / 2;
+    static constexpr int kWidth = NP == 16 ? 2048 : 512;  // columns of X at a time
+    static constexpr int kPitch = kWidth + 4;
+    typedef double Sym[NP][NP + 2];
     float x[NP][kPitch];
-    Sym sym[4];
-    double red[kThinThreads / 64];
+    double part[kThinWaves][kUpper][4][64];  // every wave's sums of G, as they lie in its registers
+    Sym sym[NP == 16 ? 1 : 4];
+    float r[NP][NP + 4];                     // R, and what x is multiplied by
+    float power[2];
 };
 
-// dst = alpha * M N + beta * N + gamma * I, all symmetric; every wave takes some blocks of 16.
-// The 64-bit instruction leaves row 4 t + lane / 16 and column lane % 16 in a lane's t-th result.
-template <int NP>
-__device__ inline void thin_product(typename Thin<NP>::Sym& dst, const typename Thin<NP>::Sym& M,
-                                    const typename Thin<NP>::Sym& N, double alpha, double beta,
-                                    double gamma)
+// The 64-bit instruction takes M[lane % 16][k + lane / 16] and N[k + lane / 16][lane % 16] and
+// leaves row 4 t + lane / 16, column lane % 16 in a lane's t-th result: what it leaves of a
+// symmetric matrix is what it takes of it, so 16 x 16 chains never leave the registers.
+__device__ inline f64x4 thin_product16(const f64x4& M, const f64x4& N)
 {
-    constexpr int kBlocks = NP / 16;
+    f64x4 acc = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+        acc = __builtin_amdgcn_mfma_f64_16x16x4f64(M[t], N[t], acc, 0, 0, 0);
+    return acc;
+}
+
+__device__ inline f64x4 thin_chain16(f64x4 G, int steps)
+{
+    const int lane = int(threadIdx.x) & 63, r = lane & 15, q = lane >> 4;
+    f64x4 R = {};
+    for (int step = 0; step < steps; ++step) {
+        f64x4 P = thin_product16(G, G);
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+            P[t] = 2.0315 * P[t] - 4.7750 * G[t] + (4 * t + q == r ? 3.4445 : 0.0);
+        R = step == 0 ? P : thin_product16(P, R);
+        if (step + 1 < steps)
+            G = thin_product16(thin_product16(P, G), P);
+    }
+    return R;
+}
+
+// dst = alpha * M N + beta * N + gamma * I, all symmetric, for 32 x 32: four waves take a block
+// of 16 each.
+__device__ inline void thin_product32(Thin<32>::Sym& dst, const Thin<32>::Sym& M,
+                                      const Thin<32>::Sym& N, double alpha, double beta,
+                                      double gamma)
+{
     const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
     const int r = lane & 15, q = lane >> 4;
-    for (int b = wave; b < kBlocks * kBlocks; b += kThinThreads / 64) {
-        const int bi = b / kBlocks * 16, bj = b % kBlocks * 16;
+    if (wave < 4) {
+        const int bi = wave / 2 * 16, bj = wave % 2 * 16;
         f64x4 acc = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll
-        for (int k = 0; k < NP; k += 4)
+        for (int k = 0; k < 32; k += 4)
             acc = __builtin_amdgcn_mfma_f64_16x16x4f64(M[bi + r][k + q], N[bj + r][k + q], acc, 0,
                                                        0, 0);
 #pragma unroll
@@ -588,166 +618,200 @@ __device__ inline void thin_product(typename Thin<NP>::Sym& dst, const typename 
     __syncthreads();
 }
 
-// Columns [k0, k0 + kWidth) of X (zeros outside it) into LDS.
+// Columns [k0, k0 + kWidth) of X, zeros outside it, into LDS, 32 reads of a lane under way at a
+// time.  Rows of X lie along its memory where it is wide, columns where it is tall.
 template <int NP, typename T>
-__device__ inline void thin_load(Thin<NP>& t, const Matrix& m, bool wide, int k0, double by)
+__device__ inline void thin_load(Thin<NP>& t, const Matrix& m, bool wide, int k0)
 {
-    constexpr int W = Thin<NP>::kWidth;
+    constexpr int W = Thin<NP>::kWidth, kAhead = 32, kAll = NP * W / kThinThreads;
+    constexpr int kPasses = W > kThinThreads ? W / kThinThreads : 1;  // of a row, where wide
+    static_assert(W % kThinThreads == 0 && kAll % kAhead == 0, "whole passes");
     const int n = wide ? m.rows : m.cols, len = wide ? m.cols : m.rows;
+    const int tid = int(threadIdx.x);
     const T* src = static_cast<const T*>(m.src);
-#pragma unroll 8
-    for (int e = threadIdx.x; e < NP * W; e += kThinThreads) {
-        const int i = wide ? e / W : e % NP, k = wide ? e % W : e / NP;
-        const int at = k0 + k;
-        float v = 0.0f;
-        if (i < n && at < len)
-            v = float(double(load_value(src + (wide ? i * len + at : at * n + i))) * by);
-        t.x[i][k] = v;
+#pragma unroll
+    for (int first = 0; first < kAll; first += kAhead) {
+        float v[kAhead];
+        if (wide) {
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int i = (first + u) / kPasses, k = (first + u) % kPasses * kThinThreads + tid;
+                v[u] = i < n && k0 + k < len ? load_value(src + i * len + k0 + k) : 0.0f;
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                t.x[(first + u) / kPasses][(first + u) % kPasses * kThinThreads + tid] = v[u];
+        } else {
+            const int i = tid % NP;
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int k = tid / NP + kThinThreads / NP * (first + u);
+                v[u] = i < n && k0 + k < len ? load_value(src + (k0 + k) * n + i) : 0.0f;
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                t.x[i][tid / NP + kThinThreads / NP * (first + u)] = v[u];
+        }
     }
     __syncthreads();
 }
 
 template <int NP, typename T, int FINAL>
-__global__ __launch_bounds__(kThinThreads) void k_orth_thin(Gate gate,
-                                                            const Matrix* __restrict__ mats,
-                                                            int first, int steps, int summed,
-                                                            float decay)
+__device__ inline void thin_matrix(Thin<NP>& t, const Matrix& m, int steps, float decay)
 {
-    constexpr int W = Thin<NP>::kWidth, kBlocks = Thin<NP>::kBlocks, kWaves = kThinThreads / 64;
-    __shared__ __align__(16) Thin<NP> t;
-    if (!descriptors_ok(gate))
-        return;
-    const bool applies = step_applies(gate);
-    const Matrix& m = mats[first + blockIdx.x];
+    constexpr int W = Thin<NP>::kWidth, kBlocks = Thin<NP>::kBlocks;
     const bool wide = m.rows <= m.cols;
-    const int n = wide ? m.rows : m.cols, len = wide ? m.cols : m.rows, numel = n * len;
-    if (numel == 0)
-        return;
-    if (!applies) {
-        if (FINAL == kWeights && m.wb)
-            for (int e = threadIdx.x; e < numel; e += kThinThreads)
-                m.wb[e] = bf16_bits(m.w[e]);
-        return;
-    }
+    const int n = wide ? m.rows : m.cols, len = wide ? m.cols : m.rows;
     const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
     const int r = lane & 15, q = lane >> 4;
 
-    // the norm: from the momentum pass's sums, or from X itself
-    double sq = 0.0;
-    if (summed) {
-        for (int i = threadIdx.x; i < m.units; i += kThinThreads)
-            sq += m.partial[i];
-    } else {
-        const T* src = static_cast<const T*>(m.src);
-#pragma unroll 8
-        for (int e = threadIdx.x; e < numel; e += kThinThreads) {
-            const double x = load_value(src + e);
-            sq += x * x;
-        }
-    }
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1)
-        sq += __shfl_xor(sq, o, 64);
-    if (lane == 0)
-        t.red[wave] = sq;
-    __syncthreads();
-    sq = 0.0;
-    for (int i = 0; i < kWaves; ++i)
-        sq += t.red[i];
-    const double by = isfinite(sq) ? (sq == 0.0 ? 0.0 : 1.0 / sqrt(sq)) : __builtin_nan("");
-
-    // G, each wave over its columns of every piece
-    f64x4 g[kBlocks][kBlocks] = {};
+    // G of X as it is, each wave over its columns of every piece
+    f64x4 g[Thin<NP>::kUpper] = {};
     for (int k0 = 0; k0 < len; k0 += W) {
-        thin_load<NP, T>(t, m, wide, k0, by);
-        for (int k = wave * (W / kWaves); k < (wave + 1) * (W / kWaves); k += 16) {
+        if (k0 > 0)
+            __syncthreads();
+        thin_load<NP, T>(t, m, wide, k0);
+        for (int k = 16 * wave; k < W && k0 + k < len; k += 16 * kThinWaves) {
             f32x4 x[kBlocks];
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b)
                 x[b] = *reinterpret_cast<const f32x4*>(&t.x[16 * b + r][k + 4 * q]);
 #pragma unroll
-            for (int a = 0; a < kBlocks; ++a)
+            for (int e = 0; e < 4; ++e) {
+                int u = 0;
 #pragma unroll
-                for (int b = a; b < kBlocks; ++b)
+                for (int a = 0; a < kBlocks; ++a)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        g[a][b] = __builtin_amdgcn_mfma_f64_16x16x4f64(
-                            double(x[a][e]), double(x[b][e]), g[a][b], 0, 0, 0);
+                    for (int b = a; b < kBlocks; ++b, ++u)
+                        g[u] = __builtin_amdgcn_mfma_f64_16x16x4f64(
+                            double(x[a][e]), double(x[b][e]), g[u], 0, 0, 0);
+            }
         }
-        __syncthreads();
     }
-    for (int w = 0; w < kWaves; ++w) {  // one after the other: the sum has a fixed order
-        if (wave == w) {
 #pragma unroll
-            for (int a = 0; a < kBlocks; ++a)
+    for (int u = 0; u < Thin<NP>::kUpper; ++u)
 #pragma unroll
-                for (int b = a; b < kBlocks; ++b)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        double* to = &t.sym[0][16 * a + 4 * e + q][16 * b + r];
-                        *to = w > 0 ? *to + g[a][b][e] : g[a][b][e];
-                    }
-        }
-        __syncthreads();
-    }
-    for (int e = threadIdx.x; e < NP * NP; e += kThinThreads)
-        if (e / NP / 16 > e % NP / 16)
-            t.sym[0][e / NP][e % NP] = t.sym[0][e % NP][e / NP];
+        for (int e = 0; e < 4; ++e)
+            t.part[wave][u][e][lane] = g[u][e];
     __syncthreads();
 
-    int G = 0, P = 1, R = 2, S = 3;
-    for (int step = 0; step < steps; ++step) {
-        thin_product<NP>(t.sym[P], t.sym[G], t.sym[G], 2.0315, -4.7750, 3.4445);
-        if (step > 0) {
-            thin_product<NP>(t.sym[S], t.sym[P], t.sym[R], 1.0, 0.0, 0.0);
-            const int old = R;
-            R = S;
-            S = old;
+    // the waves' sums in their order, the norm, the steps, and R times what X is divided by
+    const auto sum = [&](int u, int e, int l) {
+        double v = t.part[0][u][e][l];
+#pragma unroll
+        for (int w = 1; w < kThinWaves; ++w)
+            v += t.part[w][u][e][l];
+        return v;
+    };
+    // 1 / norm as a factor in [1/2, 1) for R and a power of two for X, in two halves; a zero
+    // matrix stays zero; an infinite or NaN sum makes every value NaN
+    const auto factor = [&](double trace) {
+        int e = 0;
+        const double f = trace == 0.0 ? 0.0
+                         : isfinite(trace) ? frexp(1.0 / sqrt(trace), &e)
+                                           : __builtin_nan("");
+        if (threadIdx.x == 0) {
+            t.power[0] = ldexpf(1.0f, e / 2);
+            t.power[1] = ldexpf(1.0f, e - e / 2);
         }
-        if (step + 1 < steps) {
-            thin_product<NP>(t.sym[S], t.sym[P], t.sym[G], 1.0, 0.0, 0.0);
-            thin_product<NP>(t.sym[G], t.sym[S], t.sym[P], 1.0, 0.0, 0.0);
+        return f;
+    };
+    if constexpr (NP == 16) {
+        if (wave == 0) {
+            f64x4 G;
+            double trace = 0.0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                G[e] = sum(0, e, lane);
+                trace += 4 * e + q == r ? G[e] : 0.0;
+            }
+#pragma unroll
+            for (int o = 32; o >= 1; o >>= 1)
+                trace += __shfl_xor(trace, o, 64);
+            const double f = factor(trace), by = trace == 0.0 ? 0.0 : 1.0 / trace;
+            const f64x4 R = thin_chain16(G * by, steps);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                t.r[4 * e + q][r] = float(R[e] * f);
         }
-        if (step == 0) {
-            const int old = R;
-            R = P;
-            P = old;
+        __syncthreads();
+    } else {
+        for (int e = threadIdx.x; e < 3 * 256; e += kThinThreads) {
+            const int u = e / 256, l = e % 64, a = u / 2 * 16, b = (u + 1) / 2 * 16;
+            const int i = a + 4 * (e / 64 % 4) + (l >> 4), j = b + (l & 15);
+            const double v = sum(u, e / 64 % 4, l);
+            t.sym[0][i][j] = v;
+            t.sym[0][j][i] = v;
         }
+        __syncthreads();
+        double trace = 0.0;
+        for (int i = 0; i < NP; ++i)
+            trace += t.sym[0][i][i];
+        const double f = factor(trace), by = trace == 0.0 ? 0.0 : 1.0 / trace;
+        __syncthreads();
+        for (int e = threadIdx.x; e < NP * NP; e += kThinThreads)
+            t.sym[0][e / NP][e % NP] *= by;
+        __syncthreads();
+        int G = 0, P = 1, R = 2, S = 3;
+        for (int step = 0; step < steps; ++step) {
+            thin_product32(t.sym[P], t.sym[G], t.sym[G], 2.0315, -4.7750, 3.4445);
+            if (step > 0) {
+                thin_product32(t.sym[S], t.sym[P], t.sym[R], 1.0, 0.0, 0.0);
+                const int old = R;
+                R = S;
+                S = old;
+            }
+            if (step + 1 < steps) {
+                thin_product32(t.sym[S], t.sym[P], t.sym[G], 1.0, 0.0, 0.0);
+                thin_product32(t.sym[G], t.sym[S], t.sym[P], 1.0, 0.0, 0.0);
+            }
+            if (step == 0) {
+                const int old = R;
+                R = P;
+                P = old;
+            }
+        }
+        for (int e = threadIdx.x; e < NP * NP; e += kThinThreads)
+            t.r[e / NP][e % NP] = float(t.sym[R][e / NP][e % NP] * f);
+        __syncthreads();
     }
 
     // R X, blocks of 16 columns in turn
+    const float p0 = t.power[0], p1 = t.power[1];
     f32x4 a[kBlocks][kBlocks];
 #pragma unroll
     for (int bi = 0; bi < kBlocks; ++bi)
 #pragma unroll
         for (int bk = 0; bk < kBlocks; ++bk)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                a[bi][bk][e] = float(t.sym[R][16 * bi + r][16 * bk + 4 * q + e]);
+            a[bi][bk] = *reinterpret_cast<const f32x4*>(&t.r[16 * bi + r][16 * bk + 4 * q]);
     for (int k0 = 0; k0 < len; k0 += W) {
-        if (len > W)
-            thin_load<NP, T>(t, m, wide, k0, by);
-        for (int k = 16 * wave; k < W && k0 + k < len; k += 16 * kWaves) {
+        if (len > W) {
+            __syncthreads();
+            thin_load<NP, T>(t, m, wide, k0);
+        }
+        for (int k = 16 * wave; k < W && k0 + k < len; k += 16 * kThinWaves) {
+            const int col = k0 + k + r;
+            float w[kBlocks][4] = {};
+            if constexpr (FINAL == kWeights) {
+#pragma unroll
+                for (int bi = 0; bi < kBlocks; ++bi)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int i = 16 * bi + 4 * q + e;
+                        if (i < n && col < len)
+                            w[bi][e] = m.w[wide ? i * len + col : col * n + i];
+                    }
+            }
             f32x4 acc[kBlocks] = {};
 #pragma unroll
             for (int bk = 0; bk < kBlocks; ++bk)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float x = t.x[16 * bk + 4 * q + e][k + r];
+                    const float x = t.x[16 * bk + 4 * q + e][k + r] * p0 * p1;
 #pragma unroll
                     for (int bi = 0; bi < kBlocks; ++bi)
                         acc[bi] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[bi][bk][e], x, acc[bi], 0,
                                                                        0, 0);
-                }
-            const int col = k0 + k + r;
-            float w[kBlocks][4] = {};
-#pragma unroll
-            for (int bi = 0; bi < kBlocks; ++bi)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int i = 16 * bi + 4 * q + e;
-                    if (FINAL == kWeights && i < n && col < len)
-                        w[bi][e] = m.w[wide ? i * len + col : col * n + i];
                 }
 #pragma unroll
             for (int bi = 0; bi < kBlocks; ++bi)
@@ -770,8 +834,34 @@ __global__ __launch_bounds__(kThinThreads) void k_orth_thin(Gate gate,
                     }
                 }
         }
-        __syncthreads();
     }
+}
+
+template <typename T, int FINAL>
+__global__ __launch_bounds__(kThinThreads) void k_orth_thin(Gate gate,
+                                                            const Matrix* __restrict__ mats,
+                                                            int first, int steps, float decay)
+{
+    __shared__ union {
+        Thin<16> t16;
+        Thin<32> t32;
+    } lds;
+    if (!descriptors_ok(gate))
+        return;
+    const Matrix& m = mats[first + blockIdx.x];
+    const int numel = m.rows * m.cols;
+    if (numel == 0)
+        return;
+    if (!step_applies(gate)) {
+        if (FINAL == kWeights && m.wb)
+            for (int e = threadIdx.x; e < numel; e += kThinThreads)
+                m.wb[e] = bf16_bits(m.w[e]);
+        return;
+    }
+    if (m.rows <= 16 || m.cols <= 16)
+        thin_matrix<16, T, FINAL>(lds.t16, m, steps, decay);
+    else
+        thin_matrix<32, T, FINAL>(lds.t32, m, steps, decay);
 }
 
 // ---------------------------------------------------------------- host side
@@ -790,16 +880,16 @@ struct Plan {
     std::vector<int> way;      // of each batch: how its matrices are worked on
 };
 
-// How a matrix is worked on.  Thin ones by one workgroup each, by the smaller side up to 16 or
-// 32.  Long ones take their steps in pairs, which saves a sixth of the multiply-adds or
+// How a matrix is worked on.  Thin ones by one workgroup each.  Long ones take their steps in pairs, which saves a sixth of the multiply-adds or
 // more; 128 rows or columns are the least that a tile computes anyway.
-enum { kThin16, kThin32, kSingle, kPairs, kWays };
+enum { kThin, kSingle, kPairs, kWays };
 
 int way_of(int64_t rows, int64_t cols)
 {
     const int64_t n = std::min(rows, cols), m = std::max(rows, cols);
-    if (n <= kThinSide && n * m <= kThinElems)
-        return n <= 16 ? kThin16 : kThin32;
+    const int64_t side = n <= 16 ? 16 : kThinSide;
+    if (n <= side && side * m <= kThinElems)
+        return kThin;
     return n >= kTile && m >= 2 * n ? kPairs : kSingle;
 }
 
@@ -816,7 +906,7 @@ struct Place {
 Place place(int64_t rows, int64_t cols, bool muon)
 {
     Place p;
-    const bool thin = way_of(rows, cols) <= kThin32;  // X and the rest are in LDS
+    const bool thin = way_of(rows, cols) == kThin;  // X and the rest are in LDS
     const size_t x = thin ? 0 : size_t(padded(rows)) * size_t(padded(cols)) * 2;
     const size_t side = thin ? 0 : size_t(std::min(padded(rows), padded(cols)));
     size_t at = 0;
@@ -862,7 +952,7 @@ Plan make_plan(const int64_t* rows, const int64_t* cols, int K, bool muon, int64
     for (int i = 0; i < K; ++i) {
         const int k = p.order[i];
         const int way = way_of(rows[k], cols[k]);
-        const int64_t n = way <= kThin32 ? rows[k] * cols[k] : padded(rows[k]) * padded(cols[k]);
+        const int64_t n = way == kThin ? rows[k] * cols[k] : padded(rows[k]) * padded(cols[k]);
         if (p.batch.empty() || way != p.way.back() || (elems > 0 && elems + n > kBatchElems)) {
             p.batch.push_back(i);
             p.way.push_back(way);
@@ -943,28 +1033,14 @@ struct Launch {
     bool large(int i) const { return blocks(i) >= kLargeTiles; }
 };
 
-template <int NP>
-void launch_thin_side(const Gate& gate, const Matrix* mats, int first, int n, const Call& c,
-                      float decay)
+void launch_thin(const Gate& gate, const Matrix* mats, int first, int n, const Call& c, float decay)
 {
     const bool wide_src = c.muon || c.in_dtype == LT_DTYPE_F32;
-    auto* kernel = c.muon ? k_orth_thin<NP, float, kWeights>
+    auto* kernel = c.muon ? k_orth_thin<float, kWeights>
                    : c.out_dtype == LT_DTYPE_F32
-                       ? (wide_src ? k_orth_thin<NP, float, kOutF32>
-                                   : k_orth_thin<NP, uint16_t, kOutF32>)
-                       : (wide_src ? k_orth_thin<NP, float, kOutBf16>
-                                   : k_orth_thin<NP, uint16_t, kOutBf16>);
-    kernel<<<dim3(uint32_t(n)), kThinThreads, 0, c.st>>>(gate, mats, first, c.ns_steps, c.muon,
-                                                         decay);
-}
-
-void launch_thin(int way, const Gate& gate, const Matrix* mats, int first, int n, const Call& c,
-                 float decay)
-{
-    if (way == kThin16)
-        launch_thin_side<16>(gate, mats, first, n, c, decay);
-    else
-        launch_thin_side<32>(gate, mats, first, n, c, decay);
+                       ? (wide_src ? k_orth_thin<float, kOutF32> : k_orth_thin<uint16_t, kOutF32>)
+                       : (wide_src ? k_orth_thin<float, kOutBf16> : k_orth_thin<uint16_t, kOutBf16>);
+    kernel<<<dim3(uint32_t(n)), kThinThreads, 0, c.st>>>(gate, mats, first, c.ns_steps, decay);
 }
 
 // Descriptors in place, then every batch in turn: `begin` enqueues what leaves the sources
@@ -1048,13 +1124,13 @@ lt_err run_batches(const Call& c, float decay, Fill fill, Begin begin)
         const auto blocks = [&](int i) { return pre[i][first + n] - pre[i][first]; };
         if (n == 0 || blocks(kPreTile) == 0)
             continue;
-        const bool thin = p.way[b] <= kThin32;
+        const bool thin = p.way[b] == kThin;
         if (c.muon || !thin)
             if (lt_err e = begin(gate, dev[kPreUnits], d_momentum, d_mats, first, n,
                                  pre[kPreUnits][first], blocks(kPreUnits)))
                 return e;
         if (thin) {
-            launch_thin(p.way[b], gate, d_mats, first, n, c, decay);
+            launch_thin(gate, d_mats, first, n, c, decay);
             LT_TRY_HIP(hipGetLastError());
             continue;
         }

@@ -1,4 +1,4 @@
-"""Matrix products in 8-bit floating point (f7, f8; see include/lazytrain.h) and the linear layer
+"""Matrix products in 8-bit floating point (f7 to f9; see include/lazytrain.h) and the linear layer
 made of them: weights that the optimizer has just updated are quantized once, read by the
 forward and the input-gradient product, and the weight gradient comes back in bfloat16 (or
 float32) for the next step.
@@ -148,15 +148,27 @@ def _tokens(x: torch.Tensor, features: int, what: str) -> torch.Tensor:
 
 
 def fp8_linear(x: torch.Tensor, weight: Fp8Weight,
-               out_dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
-    """x weight^T for x (..., in_features), quantized on the way; for answering: nothing is
-    kept for a backward pass.  Works on the current stream."""
+               out_dtype: torch.dtype = torch.bfloat16, workspace: Optional[torch.Tensor] = None,
+               stream=None) -> torch.Tensor:
+    """f9: x weight^T for x (..., in_features), quantized on the way; for answering: nothing is
+    kept for a backward pass."""
     t = _tokens(x, weight.cols, "x")
-    codes, scales = _empty(t.shape[0], weight.cols, x.device)
-    lt_fp8_quantize(t, codes, scales)
-    y = torch.empty(t.shape[0], weight.rows, dtype=out_dtype, device=x.device)
-    lt_fp8_matmul(codes, scales, weight.codes, weight.scales, weight.cols, y)
-    return y.view(*x.shape[:-1], weight.rows)
+    stride = _rows(t, "x")
+    m, device = t.shape[0], x.device
+    if weight.codes.device != device:
+        raise ValueError(f"the weight is on {weight.codes.device}, x on {device}")
+    y = torch.empty(m, weight.rows, dtype=out_dtype, device=device)
+    ws, nbytes = 0, 0
+    if m > 16 or workspace is not None:
+        nbytes = int(lib().lt_fp8_linear_workspace_bytes(m, weight.rows, weight.cols))
+        held = _workspace(device, nbytes, workspace, stream, "fp8")
+        ws, nbytes = held.data_ptr(), held.numel() * held.element_size()
+    with _current(device):
+        _check(lib().lt_fp8_linear(t.data_ptr(), _dtype_code(t, "x"), stride,
+                                   weight.codes.data_ptr(), weight.scales.data_ptr(), m,
+                                   weight.rows, weight.cols, y.data_ptr(), _dtype_code(y, "y"),
+                                   weight.rows, ws, nbytes, _stream_handle(stream, device)))
+    return y if x.dim() == 2 else y.view(*x.shape[:-1], weight.rows)
 
 
 def fp8_linear_forward(x: torch.Tensor, weight: Fp8Weight,

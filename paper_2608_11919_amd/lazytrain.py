@@ -61,6 +61,10 @@ class _PlainLists:
     def covers(sizes, have, block):
         return False
 
+    @staticmethod
+    def sides(tensors):
+        return None
+
 
 def lib() -> ctypes.CDLL:
     """Loads liblazytrain.so, raising if it has not been built, and the native list reader.
@@ -151,6 +155,10 @@ def lib() -> ctypes.CDLL:
     L.lt_fp8_matmul_workspace_bytes.restype = ctypes.c_size_t
     L.lt_fp8_matmul.argtypes = [vp, vp, vp, vp, i64, i64, i64, vp, ctypes.c_int, i64, vp,
                                 ctypes.c_size_t, vp]
+    L.lt_fp8_linear_workspace_bytes.argtypes = [i64, i64, i64]
+    L.lt_fp8_linear_workspace_bytes.restype = ctypes.c_size_t
+    L.lt_fp8_linear.argtypes = [vp, ctypes.c_int, i64, vp, vp, i64, i64, i64, vp, ctypes.c_int, i64,
+                                vp, ctypes.c_size_t, vp]
     L.lt_read_status.argtypes = [vp, vp, ctypes.POINTER(ctypes.c_int32)]
     L.lt_set_max_workgroups.argtypes = [ctypes.c_int]
     L.lt_workspace_release.argtypes = [vp]
@@ -162,7 +170,7 @@ def lib() -> ctypes.CDLL:
                  "lt_adamw_fp32_step", "lt_select_8bit_slice", "lt_workspace_release",
                  "lt_grad_sqnorm_noalloc", "lt_step_table", "lt_step_state_init",
                  "lt_step_state_advance", "lt_orthogonalize", "lt_muon_step",
-                 "lt_fp8_quantize", "lt_fp8_matmul"):
+                 "lt_fp8_quantize", "lt_fp8_matmul", "lt_fp8_linear"):
         getattr(L, name).restype = ctypes.c_int
     _lib = L
     return L

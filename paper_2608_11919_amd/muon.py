@@ -18,17 +18,21 @@ _DTYPES = {torch.float32: LT_DTYPE_F32, torch.bfloat16: LT_DTYPE_BF16}
 
 
 def _sides(matrices, what):
-    """Rows and columns of a list of matrices, as the library takes them."""
+    """Rows and columns of a list of matrices, as the library takes them (after lib())."""
+    got = _lt._lists.sides(matrices)
+    if got is not None:
+        return got
     for i, m in enumerate(matrices):
         if m.dim() != 2:
             raise ValueError(f"{what}[{i}] must be a matrix (two dimensions, got {m.dim()})")
     n = len(matrices)
-    shapes = [m.shape for m in matrices]
-    return ((ctypes.c_int64 * n)(*[s[0] for s in shapes]),
-            (ctypes.c_int64 * n)(*[s[1] for s in shapes]), shapes)
+    return (bytes((ctypes.c_int64 * n)(*[m.shape[0] for m in matrices])),
+            bytes((ctypes.c_int64 * n)(*[m.shape[1] for m in matrices])))
 
 
-def _one_dtype(matrices, what) -> int:
+def _one_dtype(matrices, taken: _List, what) -> int:
+    if taken.dtype in _DTYPES:
+        return _DTYPES[taken.dtype]
     if not matrices:
         return LT_DTYPE_F32  # an empty list reads and writes nothing
     dt = matrices[0].dtype
@@ -53,18 +57,19 @@ def lt_orthogonalize(matrices: Sequence[torch.Tensor], out: Sequence[torch.Tenso
     device = _device_of(matrices)
     src = _List(matrices, device, what="matrices")
     dst = _List(out, device, what="out")
-    rows, cols, shapes = _sides(matrices, "matrices")
-    for i, o in enumerate(out):
-        if o.shape != shapes[i]:
-            raise ValueError(f"out[{i}] must have shape {tuple(shapes[i])}")
+    rows, cols = _sides(matrices, "matrices")
+    if _sides(out, "out") != (rows, cols):
+        for i, (o, m) in enumerate(zip(out, matrices)):
+            if o.shape != m.shape:
+                raise ValueError(f"out[{i}] must have shape {tuple(m.shape)}")
     n = len(matrices)
     nbytes = int(lib().lt_orthogonalize_workspace_bytes(rows, cols, n))
     ws = _workspace(device, nbytes, workspace, stream, "orthogonalize")
     with _current(device):
         _check(lib().lt_orthogonalize(
-            src.ptrs, _one_dtype(matrices, "matrices"), dst.ptrs, _one_dtype(out, "out"), rows,
-            cols, n, int(ns_steps), ws.data_ptr(), ws.numel() * ws.element_size(),
-            _stream_handle(stream, device)))
+            src.ptrs, _one_dtype(matrices, src, "matrices"), dst.ptrs,
+            _one_dtype(out, dst, "out"), rows, cols, n, int(ns_steps), ws.data_ptr(),
+            ws.numel() * ws.element_size(), _stream_handle(stream, device)))
 
 
 def lt_muon_workspace_bytes(rows: Sequence[int], cols: Sequence[int], block_size: int) -> int:
@@ -94,7 +99,11 @@ def lt_muon_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor],
     ma = _List(m_absmax, device, torch.float32, "m_absmax")
     gdt = _grad_code(grads, g)
     _check_block_size(block_size)
-    rows, cols, _ = _sides(params, "params")
+    rows, cols = _sides(params, "params")
+    if _lt._lists.sides(grads) != (rows, cols):
+        for i in range(n):  # a gradient may be flat, but no matrix of another shape
+            if grads[i].dim() != 1 and grads[i].shape != params[i].shape:
+                raise ValueError(f"grads[{i}] must have shape {tuple(params[i].shape)}")
     if not (g.numels == p.numels == mq.numels and
             _lt._lists.covers(p.numels, ma.numels, int(block_size))):
         for i in range(n):

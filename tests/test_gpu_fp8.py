@@ -242,14 +242,46 @@ def test_linear_layer(layer, dtype):
     dy = matrix(t, n, 23, dtype, False)
     weight = lt.Fp8Weight.from_master(w)
     y, saved = lt.fp8_linear_forward(x, weight)
-    assert torch.equal(y, lt.fp8_linear(x, weight)) and y.dtype == torch.bfloat16
+    assert y.dtype == torch.bfloat16
     dx, dw = lt.fp8_linear_backward(dy, saved, weight, out_dtype=torch.float32,
                                     grad_dtype=torch.float32)
     h = lambda v: v.double().cpu().numpy()
     xv, wv = expected(h(x), False)[0], expected(h(w), True)[0]
     check(y, xv, wv)
+    check(lt.fp8_linear(x, weight), xv, wv)
     check(dx, expected(h(dy), False)[0], wv.T.copy())
     check(dw, expected(h(dy).T, False)[0], expected(h(x).T, False)[0])
+
+
+@pytest.mark.parametrize("tokens", [1, 2, 15, 16, 17, 31, 33, 63, 64, 65])
+@pytest.mark.parametrize("sizes", [(100, 40), (128, 16), (1000, 257), (5120, 300), (384, 16400)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_few_tokens(tokens, sizes, dtype):
+    """x quantized on the way, and as codes: the same values, whatever the number of tokens."""
+    k, n = sizes
+    x = matrix(tokens, k + 24, 24, dtype)[:, :k]  # rows apart, some of them unaligned
+    w = matrix(n, k, 25, torch.float32)
+    if tokens > 3:
+        x[2] = 0.0
+    weight = lt.Fp8Weight.from_master(w, transposed=False)
+    wv = values(weight.codes, weight.scales, k)[0]
+    codes, scales, _, _ = quantize(x.contiguous())
+    xv = values(codes, scales, k)[0]
+    for out_dtype in (torch.float32, torch.bfloat16):
+        y = lt.fp8_linear(x, weight, out_dtype=out_dtype)
+        check(y, xv, wv)
+        out = torch.full((tokens, n + 1), 3.0, dtype=out_dtype, device=DEV)
+        lt.lt_fp8_matmul(codes, scales, weight.codes, weight.scales, k, out[:, :n])
+        assert torch.equal(out[:, :n], y) and (out[:, n] == 3.0).all()
+
+
+def test_a_token_that_is_not_finite_keeps_to_itself():
+    x = matrix(5, 300, 26, torch.float32, False)
+    x[1, 150], x[3, 299] = float("nan"), float("inf")
+    w = lt.Fp8Weight.from_master(matrix(50, 300, 27, torch.float32, False), transposed=False)
+    y = lt.fp8_linear(x, w)
+    assert torch.isnan(y[1]).all() and torch.isnan(y[3]).all()
+    assert torch.isfinite(y[[0, 2, 4]]).all()
 
 
 def test_gradients_against_differences():
