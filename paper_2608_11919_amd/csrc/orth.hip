@@ -40,6 +40,8 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <mutex>
+#include <unordered_map>
 
 namespace {
 
@@ -868,13 +870,16 @@ __global__ __launch_bounds__(kThinThreads) void k_orth_thin(Gate gate,
 
 // The workspace: [tag][prefixes][momentum descriptors][matrices][square sums][partials] and
 // the region that the batches share.
-constexpr int64_t kLargeTiles = 256;  // tiles of 256 x 256 that a launch takes them for
-constexpr int64_t kBatchElems = int64_t(1) << 27;  // padded elements of a batch of several
+//
+// A batch is what one sequence of launches works on.  Large ones fill the last rounds of their
+// launches: the three feed-forward matrices of a 27B-class layer (2.7e8 elements) one by one
+// leave a fifth of the CUs idle in every product.  16 bytes of workspace go with an element.
+constexpr int64_t kBatchElems = int64_t(3) << 27;  // padded elements of a batch of several
 
 enum { kPreUnits, kPrePrep, kPreSym, kPreTile, kPreSymLarge, kPreTileLarge, kPrefixes };
 
 struct Plan {
-    size_t prefix[kPrefixes], momentum, mats, header, squares, partials, region, total;
+    size_t prefix[kPrefixes], momentum, mats, header, squares, partials, region[2], total;
     std::vector<int> order;    // the list's matrices in the order in which they are worked on
     std::vector<int> batch;    // first place of each batch, and the list's length
     std::vector<int> way;      // of each batch: how its matrices are worked on
@@ -948,7 +953,7 @@ Plan make_plan(const int64_t* rows, const int64_t* cols, int K, bool muon, int64
             if (way_of(rows[k], cols[k]) == way)
                 p.order.push_back(k);
     int64_t units = 0, elems = 0;
-    size_t region = 0, bytes = 0;
+    size_t region[2] = {0, 0}, bytes = 0;  // of single steps, and of everything else
     for (int i = 0; i < K; ++i) {
         const int k = p.order[i];
         const int way = way_of(rows[k], cols[k]);
@@ -964,11 +969,12 @@ Plan make_plan(const int64_t* rows, const int64_t* cols, int K, bool muon, int64
         units += units_of(rows[k] * cols[k], span);
         elems += n;
         bytes += place(rows[k], cols[k], muon).bytes;
-        region = std::max(region, bytes);
+        region[way == kSingle ? 0 : 1] = std::max(region[way == kSingle ? 0 : 1], bytes);
     }
     p.batch.push_back(K);
-    p.region = p.partials + round_up(sizeof(double) * size_t(units), 256);
-    p.total = round_up(p.region + region, 256);
+    p.region[0] = p.partials + round_up(sizeof(double) * size_t(units), 256);
+    p.region[1] = p.region[0] + round_up(region[0], 256);
+    p.total = p.region[1] + round_up(region[1], 256);
     return p;
 }
 
@@ -1002,7 +1008,7 @@ struct Call {
 struct Launch {
     const Gate& gate;
     const Matrix* mats;
-    int first, n;
+    int first, n, cus;
     hipStream_t st;
     const int64_t* const* dev;  // prefixes on the device and on the host
     int64_t* const* pre;
@@ -1012,7 +1018,7 @@ struct Launch {
     template <int OP>
     void sym(const SymArgs& a) const
     {
-        if (large(kPreSymLarge))
+        if (large(kPreSymLarge, kPreSym))
             k_orth_sym<Large, OP><<<dim3(uint32_t(blocks(kPreSymLarge))), Large::kThreads, 0, st>>>(
                 gate, dev[kPreSymLarge], mats, first, n, a);
         else
@@ -1022,7 +1028,7 @@ struct Launch {
     template <int FINAL>
     void update(const UpdateArgs& a) const
     {
-        if (large(kPreTileLarge))
+        if (large(kPreTileLarge, kPreTile))
             k_orth_update<Large, FINAL>
                 <<<dim3(uint32_t(blocks(kPreTileLarge))), Large::kThreads, 0, st>>>(
                     gate, dev[kPreTileLarge], mats, first, n, a);
@@ -1030,7 +1036,12 @@ struct Launch {
             k_orth_update<Small, FINAL><<<dim3(uint32_t(blocks(kPreTile))), Small::kThreads, 0, st>>>(
                 gate, dev[kPreTile], mats, first, n, a);
     }
-    bool large(int i) const { return blocks(i) >= kLargeTiles; }
+    // 256 x 256 tiles, one to a CU, where their rounds are cheaper than those of 128 x 128, two
+    // to a CU: a step of 64 summed values takes 1.85 us and 1.12 us a round.
+    bool large(int i, int small) const
+    {
+        return host::ceil_div(blocks(i), cus) * 185 < host::ceil_div(blocks(small), 2 * cus) * 112;
+    }
 };
 
 void launch_thin(const Gate& gate, const Matrix* mats, int first, int n, const Call& c, float decay)
@@ -1042,6 +1053,58 @@ void launch_thin(const Gate& gate, const Matrix* mats, int first, int n, const C
                        : (wide_src ? k_orth_thin<float, kOutBf16> : k_orth_thin<uint16_t, kOutBf16>);
     kernel<<<dim3(uint32_t(n)), kThinThreads, 0, c.st>>>(gate, mats, first, c.ns_steps, decay);
 }
+
+// A second stream of the library's own, for the batches of single steps beside those of pairs:
+// the launches of a few square matrices fill half the CUs (two of 2048 x 2048: 272 tiles of
+// 128 x 128).  It starts after what the caller's stream holds and the caller's stream goes on
+// after it.  Calls enqueue on it one at a time; under capture there is none, and everything goes
+// into the caller's stream.
+class Fork {
+public:
+    lt_err begin(hipStream_t st)
+    {
+        hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+        LT_TRY_HIP(hipStreamIsCapturing(st, &capture));
+        if (capture != hipStreamCaptureStatusNone)
+            return LT_OK;
+        int dev;
+        LT_TRY_HIP(hipGetDevice(&dev));
+        static std::mutex mu;
+        static std::unordered_map<int, Lane> lanes;
+        lock_ = std::unique_lock<std::mutex>(mu);
+        Lane& l = lanes[dev];
+        if (!l.stream) {
+            Lane made;
+            LT_TRY_HIP(hipEventCreateWithFlags(&made.forked, hipEventDisableTiming));
+            LT_TRY_HIP(hipEventCreateWithFlags(&made.joined, hipEventDisableTiming));
+            LT_TRY_HIP(hipStreamCreateWithFlags(&made.stream, hipStreamNonBlocking));
+            l = made;
+        }
+        LT_TRY_HIP(hipEventRecord(l.forked, st));
+        LT_TRY_HIP(hipStreamWaitEvent(l.stream, l.forked, 0));
+        lane_ = &l;
+        return LT_OK;
+    }
+    hipStream_t side(hipStream_t st) const { return lane_ ? lane_->stream : st; }
+    lt_err end(hipStream_t st)
+    {
+        if (!lane_)
+            return LT_OK;
+        Lane& l = *lane_;
+        lane_ = nullptr;
+        LT_TRY_HIP(hipEventRecord(l.joined, l.stream));
+        LT_TRY_HIP(hipStreamWaitEvent(st, l.joined, 0));
+        return LT_OK;
+    }
+
+private:
+    struct Lane {
+        hipStream_t stream = nullptr;
+        hipEvent_t forked = nullptr, joined = nullptr;
+    };
+    Lane* lane_ = nullptr;
+    std::unique_lock<std::mutex> lock_;
+};
 
 // Descriptors in place, then every batch in turn: `begin` enqueues what leaves the sources
 // and their sums of squares, `fill` completes a matrix's descriptor.
@@ -1062,7 +1125,7 @@ lt_err run_batches(const Call& c, float decay, Fill fill, Begin begin)
     auto* mats = reinterpret_cast<Matrix*>(image.data() + p.mats);
     auto* partial = reinterpret_cast<double*>(ws + p.partials);
     for (size_t b = 0; b + 1 < p.batch.size(); ++b) {
-        uint8_t* at = ws + p.region;
+        uint8_t* at = ws + p.region[p.way[b] == kSingle ? 0 : 1];
         for (int i = p.batch[b]; i < p.batch[b + 1]; ++i) {
             const int k = p.order[i];  // the i-th matrix of the descriptors
             const int64_t numel = c.rows[k] * c.cols[k];
@@ -1118,8 +1181,18 @@ lt_err run_batches(const Call& c, float decay, Fill fill, Begin begin)
         dev[i] = reinterpret_cast<const int64_t*>(ws + p.prefix[i]);
     const auto* d_mats = reinterpret_cast<const Matrix*>(ws + p.mats);
     const auto* d_momentum = reinterpret_cast<const host::MomentumTensor*>(ws + p.momentum);
-    const hipStream_t st = c.st;
+    int cus;
+    if (lt_err e = host::compute_units(&cus))
+        return e;
+    Fork fork;
+    const auto has = [&](int way) {
+        return std::find(p.way.begin(), p.way.end(), way) != p.way.end();
+    };
+    if (has(kSingle) && has(kPairs))
+        if (lt_err e = fork.begin(c.st))
+            return e;
     for (size_t b = 0; b + 1 < p.batch.size(); ++b) {
+        const hipStream_t st = p.way[b] == kSingle ? fork.side(c.st) : c.st;
         const int first = p.batch[b], n = p.batch[b + 1] - first;
         const auto blocks = [&](int i) { return pre[i][first + n] - pre[i][first]; };
         if (n == 0 || blocks(kPreTile) == 0)
@@ -1127,7 +1200,7 @@ lt_err run_batches(const Call& c, float decay, Fill fill, Begin begin)
         const bool thin = p.way[b] == kThin;
         if (c.muon || !thin)
             if (lt_err e = begin(gate, dev[kPreUnits], d_momentum, d_mats, first, n,
-                                 pre[kPreUnits][first], blocks(kPreUnits)))
+                                 pre[kPreUnits][first], blocks(kPreUnits), st))
                 return e;
         if (thin) {
             launch_thin(gate, d_mats, first, n, c, decay);
@@ -1139,7 +1212,7 @@ lt_err run_batches(const Call& c, float decay, Fill fill, Begin begin)
         auto* prep = wide_src ? k_orth_prepare<float> : k_orth_prepare<uint16_t>;
         prep<<<dim3(uint32_t(blocks(kPrePrep))), kThreads, 0, st>>>(gate, dev[kPrePrep], d_mats,
                                                                     first, n);
-        const Launch launch{gate, d_mats, first, n, st, dev, pre};
+        const Launch launch{gate, d_mats, first, n, cus, st, dev, pre};
         int from = 0;
         for (int step = 0; step < c.ns_steps; from ^= 1) {
             launch.sym<kGram>({step, from, 0, 0, 0});
@@ -1164,7 +1237,7 @@ lt_err run_batches(const Call& c, float decay, Fill fill, Begin begin)
         }
         LT_TRY_HIP(hipGetLastError());
     }
-    return LT_OK;
+    return fork.end(c.st);
 }
 
 void add_range(std::vector<host::Range>& r, const void* p, size_t bytes, bool written)
@@ -1227,10 +1300,10 @@ lt_err lt_orthogonalize(const void* const* matrices, int in_dtype, void* const* 
             m.out = out[k];
         },
         [&](const Gate& gate, const int64_t* prefix, const host::MomentumTensor*,
-            const Matrix* mats, int first, int n, int64_t, int64_t units) {
+            const Matrix* mats, int first, int n, int64_t, int64_t units, hipStream_t st) {
             auto* squares = in_dtype == LT_DTYPE_F32 ? k_orth_squares<float>
                                                      : k_orth_squares<uint16_t>;
-            squares<<<dim3(uint32_t(units)), kThreads, 0, c.st>>>(gate, prefix, mats, first, n);
+            squares<<<dim3(uint32_t(units)), kThreads, 0, st>>>(gate, prefix, mats, first, n);
             LT_TRY_HIP(hipGetLastError());
             return LT_OK;
         });
@@ -1314,10 +1387,10 @@ lt_err lt_muon_step(float* const* params, const void* const* grads, int grad_dty
                                      rows[k] * cols[k]};
         },
         [&](const Gate& gate, const int64_t* prefix, const host::MomentumTensor* momenta,
-            const Matrix*, int first, int n, int64_t first_unit, int64_t units) {
+            const Matrix*, int first, int n, int64_t first_unit, int64_t units, hipStream_t st) {
             return host::launch_momentum(gate.guard, prefix, momenta, first, n, first_unit, units,
                                          grad_dtype, block_size, code_map, s, coef, status,
-                                         step_state, c.st);
+                                         step_state, st);
         });
 }
 
