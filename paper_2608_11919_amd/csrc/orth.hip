@@ -110,6 +110,24 @@ __device__ inline int find_matrix(const int64_t* __restrict__ prefix, int first,
 __device__ inline float load_value(const float* p) { return *p; }
 __device__ inline float load_value(const uint16_t* p) { return __uint_as_float(uint32_t(*p) << 16); }
 
+// The 16 bytes at p.
+__device__ inline void load_line(const float* p, float (&x)[4])
+{
+    const f32x4 w = *reinterpret_cast<const f32x4*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        x[i] = w[i];
+}
+__device__ inline void load_line(const uint16_t* p, float (&x)[8])
+{
+    const i32x4 w = *reinterpret_cast<const i32x4*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(uint32_t(w[i]) << 16);
+        x[2 * i + 1] = __uint_as_float(uint32_t(w[i]) & 0xFFFF0000u);
+    }
+}
+
 __device__ inline uint16_t bf16_bits(float x)
 {
     return __builtin_bit_cast(uint16_t, (__bf16)x);  // to nearest even; a NaN becomes quiet
@@ -148,7 +166,17 @@ __global__ __launch_bounds__(kThreads) void k_orth_squares(Gate gate,
     const int64_t e1 = e0 + kSquareUnit < numel ? e0 + kSquareUnit : numel;
     const T* src = static_cast<const T*>(m.src);
     double sq = 0.0;
-    for (int64_t e = e0 + threadIdx.x; e < e1; e += kThreads) {
+    constexpr int kLine = 16 / sizeof(T);  // values of a 16-byte load; units start aligned
+    int64_t e = e0 + int64_t(threadIdx.x) * kLine;
+#pragma unroll 8
+    for (; e + kLine <= e1; e += kThreads * kLine) {
+        float x[kLine];
+        load_line(src + e, x);
+#pragma unroll
+        for (int i = 0; i < kLine; ++i)
+            sq += double(x[i]) * double(x[i]);
+    }
+    for (; e < e1; ++e) {  // the lane that the matrix ends in
         const double x = load_value(src + e);
         sq += x * x;
     }
@@ -182,7 +210,7 @@ __global__ __launch_bounds__(kThreads) void k_orth_prepare(Gate gate,
                                                            const Matrix* __restrict__ mats,
                                                            int first, int n)
 {
-    __shared__ _Float16 turned[kPrep][kPrep + 2];
+    __shared__ __align__(16) _Float16 turned[kPrep][kPrep + 8];
     if (!descriptors_ok(gate) || !step_applies(gate))
         return;
     const int64_t unit = prefix[first] + blockIdx.x;
@@ -195,21 +223,44 @@ __global__ __launch_bounds__(kThreads) void k_orth_prepare(Gate gate,
     const double scale = sq == 0.0 ? 0.0 : double(kScaleX) / sqrt(sq);
     const double by = isfinite(sq) ? scale : __builtin_nan("");
     const T* src = static_cast<const T*>(m.src);
-    const int c = int(threadIdx.x) & 63;
-    for (int r = int(threadIdx.x) >> 6; r < kPrep; r += kThreads / 64) {
+    // a lane has eight values of a row, a wave eight rows
+    constexpr int kLine = 16 / sizeof(T);
+    const int t = int(threadIdx.x), c = t % 8 * 8;
+    const bool whole = m.cols % kLine == 0;  // rows keep 16-byte pieces aligned
+    for (int r = t / 8; r < kPrep; r += kThreads / 8) {
         const int row = r0 + r, col = c0 + c;
-        float x = 0.0f;
-        if (row < m.rows && col < m.cols)
-            x = float(double(load_value(src + int64_t(row) * m.cols + col)) * by);
-        const _Float16 hi = _Float16(x);
+        const T* p = src + int64_t(row) * m.cols + col;
+        float x[8];
+        if (whole && row < m.rows && col + 8 <= m.cols) {
+#pragma unroll
+            for (int e = 0; e < 8; e += kLine) {
+                float w[kLine];
+                load_line(p + e, w);
+#pragma unroll
+                for (int i = 0; i < kLine; ++i)
+                    x[e + i] = w[i];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                x[e] = row < m.rows && col + e < m.cols ? load_value(p + e) : 0.0f;
+        }
+        half8 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float v = float(double(x[e]) * by);
+            hi[e] = _Float16(v);
+            lo[e] = _Float16(v - float(hi[e]));
+            turned[c + e][r] = hi[e];
+        }
         const int64_t at = int64_t(row) * m.cp + col;
-        m.h[0][at] = hi;
-        m.l[0][at] = _Float16(x - float(hi));
-        turned[c][r] = hi;
+        *reinterpret_cast<half8*>(m.h[0] + at) = hi;
+        *reinterpret_cast<half8*>(m.l[0] + at) = lo;
     }
     __syncthreads();
-    for (int q = int(threadIdx.x) >> 6; q < kPrep; q += kThreads / 64)
-        m.t[0][int64_t(c0 + q) * m.rp + r0 + c] = turned[q][c];
+    for (int q = t / 8; q < kPrep; q += kThreads / 8)
+        *reinterpret_cast<half8*>(m.t[0] + int64_t(c0 + q) * m.rp + r0 + c) =
+            *reinterpret_cast<const half8*>(&turned[q][c]);
 }
 
 // ------------------------------------------------------------- products
