@@ -253,6 +253,57 @@ __global__ __launch_bounds__(kQuantizeThreads) void k_fp8_quantize(QuantizeArgs 
     }
 }
 
+// By rows only: a group is 16 lanes, a wave four groups of one row.  A block of 128 x 128 to a
+// workgroup would leave most CUs idle for a prompt (1237 x 2011: 160 blocks).
+template <typename T>
+__global__ __launch_bounds__(kQuantizeThreads) void k_fp8_quantize_rows(QuantizeArgs a)
+{
+    const int l = int(threadIdx.x) & 15;
+    const int64_t words = a.scale_pitch / 4;  // of four groups
+    const int64_t unit = int64_t(blockIdx.x) * (kQuantizeThreads / 64) + (threadIdx.x >> 6);
+    const int64_t row = unit / words;
+    if (row >= a.rows)
+        return;
+    const int64_t group = unit % words * 4 + (threadIdx.x >> 4 & 3);
+    const int64_t col = group * kGroup + 8 * l;
+    const T* p = static_cast<const T*>(a.x) + row * a.stride + col;
+    float v[8];
+    if (a.stride % int64_t(16 / sizeof(T)) == 0 && col + 8 <= a.cols) {
+        constexpr int kLine = 16 / sizeof(T);
+#pragma unroll
+        for (int c = 0; c < 8; c += kLine) {
+            const i32x4 w = *reinterpret_cast<const i32x4*>(p + c);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if constexpr (sizeof(T) == 2) {
+                    v[2 * e] = __uint_as_float(uint32_t(w[e]) << 16);
+                    v[2 * e + 1] = __uint_as_float(uint32_t(w[e]) & 0xFFFF0000u);
+                } else {
+                    v[c + e] = __int_as_float(w[e]);
+                }
+            }
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            v[e] = col + e < a.cols ? load_value(p + e) : 0.0f;
+    }
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        top = max(top, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+#pragma unroll
+    for (int o = 8; o >= 1; o >>= 1)
+        top = max(top, uint32_t(__shfl_xor(int(top), o, 64)));
+    const Scale s = scale_of(top);  // a group past the last column is zeros: 127
+    if (l == 0)
+        a.scales[row * a.scale_pitch + group] = uint8_t(s.biased);
+    if (group * kGroup < a.cols)
+        *reinterpret_cast<uint2*>(a.codes + row * a.pitch + col) =
+            make_uint2(pack_codes(v[0], v[1], v[2], v[3], s.power),
+                       pack_codes(v[4], v[5], v[6], v[7], s.power));
+}
+
 // ------------------------------------------------------------- products
 
 struct ProductArgs {
@@ -273,40 +324,41 @@ struct ProductWriter {
     static constexpr int kSlots = 8;
     void* out;
     int64_t stride, rows, cols;  // from the tile's origin on
-    bool whole;
+    bool narrow;
     __device__ inline void fetch(int, int, int) {}
     __device__ inline void turn(int, int, const float (&)[8]) {}
-    __device__ inline void store(int row, int col, float (&v)[8], int)
+    __device__ inline void store_one(int row, int col, float v)
     {
-        typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
         if (row >= rows || col >= cols)
             return;
         const int64_t at = row * stride + col;
+        if constexpr (F32)
+            static_cast<float*>(out)[at] = v;
+        else
+            static_cast<uint16_t*>(out)[at] = bf16_bits(v);
+    }
+    __device__ inline void store(int row, int col, float (&v)[8], int)
+    {
+        typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+        if (row >= rows)
+            return;
+        if (col + 8 > cols) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                store_one(row, col + e, v[e]);
+            return;
+        }
+        const int64_t at = row * stride + col;
         if constexpr (F32) {
             float* p = static_cast<float*>(out) + at;
-            if (whole && col + 8 <= cols) {
-                *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
-                *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
-                return;
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (col + e < cols)
-                    p[e] = v[e];
+            *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+            *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
         } else {
-            uint16_t* p = static_cast<uint16_t*>(out) + at;
-            if (whole && col + 8 <= cols) {
-                u16x8 b;
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    b[e] = bf16_bits(v[e]);
-                *reinterpret_cast<u16x8*>(p) = b;
-                return;
-            }
+            u16x8 b;
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                if (col + e < cols)
-                    p[e] = bf16_bits(v[e]);
+                b[e] = bf16_bits(v[e]);
+            *reinterpret_cast<u16x8*>(static_cast<uint16_t*>(out) + at) = b;
         }
     }
 };
@@ -339,13 +391,13 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_fp8_pro
         p.rows = w.rows;
         p.cols = w.cols;
         p.stride = g.n;
-        p.whole = g.n % 4 == 0;
+        p.narrow = g.n % 4 != 0;
         p.out = g.partial + (int64_t(blockIdx.y) * g.m + r0) * g.n + c0;
         finish(tile, lds, p);
         return;
     }
     w.stride = g.stride;
-    w.whole = g.stride % (F32 ? 4 : 8) == 0;
+    w.narrow = g.stride % (F32 ? 4 : 8) != 0;
     w.out = F32 ? static_cast<void*>(static_cast<float*>(g.out) + r0 * g.stride + c0)
                 : static_cast<void*>(static_cast<uint16_t*>(g.out) + r0 * g.stride + c0);
     finish(tile, lds, w);
@@ -478,6 +530,26 @@ __device__ inline FewToken few_quantize(const FewInput<X>& in)
     return f;
 }
 
+// Step s of one token, as a lane needs it.
+template <int X>
+__device__ inline void few_input(const FewArgs& g, int64_t token, int s, int q, FewInput<X>& in)
+{
+    if constexpr (X == kCodes) {
+        const auto* p = reinterpret_cast<const i32x4*>(static_cast<const uint8_t*>(g.x) +
+                                                       token * g.pitch + int64_t(s) * kGroup +
+                                                       32 * q);
+        in.w[0] = p[0];
+        in.w[1] = p[1];
+        in.scale = g.x_scales[token * g.scale_pitch + s];
+    } else if constexpr (X == kF32) {
+        few_load(static_cast<const float*>(g.x) + token * g.x_stride, g.k, s, q,
+                 g.x_stride % 4 == 0, in.w);
+    } else {
+        few_load(static_cast<const uint16_t*>(g.x) + token * g.x_stride, g.k, s, q,
+                 g.x_stride % 8 == 0, in.w);
+    }
+}
+
 __device__ inline i32x8 load_codes(const uint8_t* p)
 {
     const i32x4 a = reinterpret_cast<const i32x4*>(p)[0], b = reinterpret_cast<const i32x4*>(p)[1];
@@ -506,7 +578,6 @@ __global__ __launch_bounds__(512) void k_fp8_few(FewArgs g)
         token[t] = 16 * t + r;
         token[t] = token[t] < g.m ? token[t] : g.m - 1;
     }
-    const bool aligned = (g.x_stride * (X == kF32 ? 4 : 2)) % 16 == 0;
     f32x4 acc[R][T] = {};
     // one step is under way while the one before is multiplied
     struct Loaded {
@@ -521,22 +592,8 @@ __global__ __launch_bounds__(512) void k_fp8_few(FewArgs g)
             in.as[i] = ws[i][s];
         }
 #pragma unroll
-        for (int t = 0; t < T; ++t) {
-            if constexpr (X == kCodes) {
-                const auto* p = reinterpret_cast<const i32x4*>(
-                    static_cast<const uint8_t*>(g.x) + token[t] * g.pitch + int64_t(s) * kGroup +
-                    32 * q);
-                in.x[t].w[0] = p[0];
-                in.x[t].w[1] = p[1];
-                in.x[t].scale = g.x_scales[token[t] * g.scale_pitch + s];
-            } else if constexpr (X == kF32) {
-                few_load(static_cast<const float*>(g.x) + token[t] * g.x_stride, g.k, s, q, aligned,
-                         in.x[t].w);
-            } else {
-                few_load(static_cast<const uint16_t*>(g.x) + token[t] * g.x_stride, g.k, s, q,
-                         aligned, in.x[t].w);
-            }
-        }
+        for (int t = 0; t < T; ++t)
+            few_input(g, token[t], s, q, in.x[t]);
     };
     const auto multiply = [&](const Loaded& in) {
 #pragma unroll
@@ -586,6 +643,98 @@ __global__ __launch_bounds__(512) void k_fp8_few(FewArgs g)
             static_cast<float*>(g.out)[to] = v;
         else
             static_cast<uint16_t*>(g.out)[to] = bf16_bits(v);
+    }
+}
+
+// The same where a wave can hold its share of x: eight waves cut the sum, each with up to STEPS
+// steps of 16 T tokens in its registers, and go through blocks of 16 rows together, the next
+// block's codes under way while one is multiplied.  x is read (and quantized) once for a
+// workgroup and not once for every 16 or 32 rows: 16 tokens through 5120 x 17408 28 us (3.2 TB/s
+// of the weight), without 41; a token through 2048 x 11008 8.3 and 10.3.
+constexpr int kHeldWaves = 8;
+
+template <int STEPS, int T, int X, bool F32>
+__global__ __launch_bounds__(64 * kHeldWaves) void k_fp8_few_held(FewArgs g)
+{
+    __shared__ float sums[2][kHeldWaves][T][256];
+    const int lane = int(threadIdx.x) & 63, r = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+    const int first = g.steps * wave / kHeldWaves;
+    const int count = g.steps * (wave + 1) / kHeldWaves - first;
+    const int64_t blocks = (g.n + 15) / 16;
+
+    struct Rows {
+        i32x8 codes[STEPS];
+        uint32_t scale[STEPS];
+    } even, odd;
+    const auto load = [&](int64_t block, Rows& w) {
+        int64_t row = block * 16 + r;
+        row = row < g.n ? row : g.n - 1;
+        const uint8_t* p = g.w + row * g.pitch + int64_t(first) * kGroup + 32 * q;
+        const uint8_t* s = g.w_scales + row * g.scale_pitch + first;
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i)
+            if (i < count) {
+                w.codes[i] = load_codes(p + i * kGroup);
+                w.scale[i] = s[i];
+            }
+    };
+    load(blockIdx.x, even);
+
+    FewToken x[T][STEPS];
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+        const int64_t token = 16 * t + r < g.m ? 16 * t + r : g.m - 1;
+        FewInput<X> in[STEPS];
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i)
+            if (i < count)
+                few_input(g, token, first + i, q, in[i]);
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i)
+            if (i < count)
+                x[t][i] = few_quantize<X>(in[i]);
+    }
+    const auto multiply = [&](int64_t block, const Rows& w, int turn) {
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i)
+                if (i < count)
+                    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                        w.codes[i], x[t][i].codes, acc, 0, 0, 0, int(w.scale[i]), 0,
+                        int(x[t][i].scale));
+            // acc[e] is row 4 q + e, token 16 t + r
+            *reinterpret_cast<f32x4*>(&sums[turn][wave][t][lane * 4]) = acc;
+        }
+        __syncthreads();  // and the other buffer's sums have been read
+        const int e = threadIdx.x % 256, t = threadIdx.x / 256;
+        if (t >= T)
+            return;
+        float v = sums[turn][0][t][e];
+#pragma unroll
+        for (int i = 1; i < kHeldWaves; ++i)
+            v += sums[turn][i][t][e];
+        const int64_t row = block * 16 + 4 * (e >> 6) + e % 4, tok = 16 * t + e / 4 % 16;
+        if (row >= g.n || tok >= g.m)
+            return;
+        const int64_t to = tok * g.stride + row;
+        if constexpr (F32)
+            static_cast<float*>(g.out)[to] = v;
+        else
+            static_cast<uint16_t*>(g.out)[to] = bf16_bits(v);
+    };
+    for (int64_t b = blockIdx.x; b < blocks; b += 2 * int64_t(gridDim.x)) {
+        const int64_t next = b + gridDim.x;
+        if (next < blocks)
+            load(next, odd);
+        multiply(b, even, 0);
+        if (next >= blocks)
+            break;
+        if (next + gridDim.x < blocks)
+            load(next + gridDim.x, even);
+        multiply(next, odd, 1);
     }
 }
 
@@ -683,12 +832,44 @@ void launch_few(const FewArgs& g, bool f32, hipStream_t st)
         launch_few_rows<T, 1, X>(g, f32, st);
 }
 
-void launch_few_codes(const FewArgs& g, bool f32, hipStream_t st)
+template <int STEPS, int T, int X>
+void launch_held(const FewArgs& g, bool f32, int cus, hipStream_t st)
 {
-    if (g.m <= 16)
-        launch_few<1, kCodes>(g, f32, st);
-    else
-        launch_few<2, kCodes>(g, f32, st);
+    // two workgroups to a CU where they are small (16 tokens through 2048 x 151936 69 us, with one
+    // 81), else one (5120 x 17408: 28 us, with two 34)
+    const int64_t groups = std::min<int64_t>(host::ceil_div(g.n, 16), STEPS <= 2 ? 2 * cus : cus);
+    auto* kernel = f32 ? k_fp8_few_held<STEPS, T, X, true> : k_fp8_few_held<STEPS, T, X, false>;
+    kernel<<<dim3(uint32_t(groups)), 64 * kHeldWaves, 0, st>>>(g);
+}
+
+// x is held where its share fits a wave's registers: up to 8192 values of 16 tokens (5120 in
+// fp32 on the way), 5120 of 32.
+template <int X>
+void launch_few_tokens(const FewArgs& g, bool f32, int cus, hipStream_t st)
+{
+    const int each = int(host::ceil_div(g.steps, kHeldWaves));
+    if constexpr (X == kCodes)
+        if (g.m > 16) {
+            if (each <= 2)
+                launch_held<2, 2, X>(g, f32, cus, st);
+            else if (each <= 5)
+                launch_held<5, 2, X>(g, f32, cus, st);
+            else
+                launch_few<2, X>(g, f32, st);
+            return;
+        }
+    if (each <= 2) {
+        launch_held<2, 1, X>(g, f32, cus, st);
+    } else if (each <= 5) {
+        launch_held<5, 1, X>(g, f32, cus, st);
+    } else {
+        if constexpr (X != kF32)
+            if (each <= 8) {
+                launch_held<8, 1, X>(g, f32, cus, st);
+                return;
+            }
+        launch_few<1, X>(g, f32, st);
+    }
 }
 
 // Workspace of lt_fp8_linear where x is quantized apart: [codes][scales][matmul's].
@@ -750,6 +931,14 @@ lt_err lt_fp8_quantize(const void* x, int dtype, int64_t rows, int64_t cols, int
                    int(host::ceil_div(cols, kGroup))};
     const dim3 grid(uint32_t(host::ceil_div(rows, kGroup) * a.across));
     const hipStream_t st = static_cast<hipStream_t>(stream);
+    const int64_t by_rows = host::ceil_div(rows * (a.scale_pitch / 4), kQuantizeThreads / 64);
+    if (!codes_t && !square && by_rows < most) {
+        auto* kernel = dtype == LT_DTYPE_BF16 ? k_fp8_quantize_rows<uint16_t>
+                                              : k_fp8_quantize_rows<float>;
+        kernel<<<dim3(uint32_t(by_rows)), kQuantizeThreads, 0, st>>>(a);
+        LT_TRY_HIP(hipGetLastError());
+        return LT_OK;
+    }
     auto* kernel = dtype == LT_DTYPE_BF16
                        ? (square ? k_fp8_quantize<uint16_t, true> : k_fp8_quantize<uint16_t, false>)
                        : (square ? k_fp8_quantize<float, true> : k_fp8_quantize<float, false>);
@@ -799,7 +988,10 @@ lt_err lt_fp8_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const uint
     if (m <= kFewTokens) {
         const FewArgs f{b_codes, b_scales, a_codes, a_scales, m, n, k, code_pitch(k),
                         scale_pitch(k), 0, int(host::ceil_div(k, kGroup)), out, out_stride};
-        launch_few_codes(f, f32, st);
+        int cus;
+        if (lt_err e = host::compute_units(&cus))
+            return e;
+        launch_few_tokens<kCodes>(f, f32, cus, st);
         LT_TRY_HIP(hipGetLastError());
         return LT_OK;
     }
@@ -859,10 +1051,13 @@ lt_err lt_fp8_linear(const void* x, int dtype, int64_t x_stride, const uint8_t* 
                         x_stride, int(host::ceil_div(k, kGroup)), out, out_stride};
         const bool f32 = out_dtype == LT_DTYPE_F32;
         const hipStream_t st = static_cast<hipStream_t>(stream);
+        int cus;
+        if (lt_err e = host::compute_units(&cus))
+            return e;
         if (dtype == LT_DTYPE_F32)
-            launch_few<1, kF32>(f, f32, st);
+            launch_few_tokens<kF32>(f, f32, cus, st);
         else
-            launch_few<1, kBf16>(f, f32, st);
+            launch_few_tokens<kBf16>(f, f32, cus, st);
         LT_TRY_HIP(hipGetLastError());
         return LT_OK;
     }

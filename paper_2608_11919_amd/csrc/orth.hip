@@ -302,7 +302,7 @@ struct SymArgs {
 // out = by * sum + at_m * M + at_n * N, in the scales of what is stored.
 template <int OP>
 struct SymWriter {
-    static constexpr bool kTurned = true;
+    static constexpr bool kTurned = true, narrow = false;
     static constexpr int kSlots = 8;
     float by, at_m, at_n, diagonal;
     int64_t pitch;
@@ -312,6 +312,7 @@ struct SymWriter {
     bool mirror;
     half8 x[OP == kGram ? 1 : kSlots], y[OP == kGram || OP == kStep ? 1 : kSlots];
 
+    __device__ inline void store_one(int, int, float) {}
     __device__ inline void fetch(int row, int col, int p)
     {
         if constexpr (OP != kGram)
@@ -422,7 +423,7 @@ struct UpdateWriter {
     static constexpr bool kTurned = FINAL == kAgain;
     static constexpr int kSlots = 8;
     float by, linear, rate, decay;
-    bool applies, whole;      // whole: eight results are in one aligned piece of the caller's rows
+    bool applies, narrow;     // narrow: the caller's rows do not keep eight results aligned
     const _Float16 *h, *l;    // X at the tile's origin, and X'
     _Float16 *next_h, *next_l, *next_t;
     int64_t pitch, pitch_t;
@@ -439,21 +440,32 @@ struct UpdateWriter {
             y[p] = *reinterpret_cast<const half8*>(l + row * pitch + col);
         }
         if constexpr (FINAL == kWeights) {
-            const float* from = out + int64_t(row) * width + col;
-            if (whole) {
-                if (row < rows && col < cols) {
-                    const f32x4 a = *reinterpret_cast<const f32x4*>(from);
-                    const f32x4 b = *reinterpret_cast<const f32x4*>(from + 4);
+            if (row < rows && col < cols) {
+                const float* from = out + int64_t(row) * width + col;
+                const f32x4 a = *reinterpret_cast<const f32x4*>(from);
+                const f32x4 b = *reinterpret_cast<const f32x4*>(from + 4);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        w[p][e] = a[e], w[p][4 + e] = b[e];
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    w[p][e] = row < rows && col + e < cols ? from[e] : 0.0f;
+                for (int e = 0; e < 4; ++e)
+                    w[p][e] = a[e], w[p][4 + e] = b[e];
             }
         }
+    }
+    __device__ inline void store_one(int row, int col, float v)
+    {
+        if (row >= rows || col >= cols)
+            return;
+        const int64_t at = row * pitch + col, to = int64_t(row) * width + col;
+        if (applies)
+            v = by * v + linear * (float(h[at]) + float(l[at]));
+        v *= 1.0f / kScaleX;
+        if constexpr (FINAL == kWeights) {
+            const float old = out[to];
+            v = applies ? __builtin_fmaf(-rate, v, old * decay) : old;
+        }
+        if (FINAL == kOutF32 || (FINAL == kWeights && applies))
+            out[to] = v;
+        if (FINAL == kOutBf16 || (FINAL == kWeights && out16))
+            out16[to] = bf16_bits(v);
     }
     __device__ inline void store(int row, int col, float (&v)[8], int p)
     {
@@ -482,30 +494,16 @@ struct UpdateWriter {
                 v[e] = applies ? __builtin_fmaf(-rate, v[e], w[p][e] * decay) : w[p][e];
         }
         const int64_t to = int64_t(row) * width + col;
-        const bool wide = FINAL == kOutF32 || (FINAL == kWeights && applies);
-        const bool narrow = FINAL == kOutBf16 || (FINAL == kWeights && out16);
-        if (whole) {
-            if (wide) {
-                *reinterpret_cast<f32x4*>(out + to) = f32x4{v[0], v[1], v[2], v[3]};
-                *reinterpret_cast<f32x4*>(out + to + 4) = f32x4{v[4], v[5], v[6], v[7]};
-            }
-            if (narrow) {
-                u16x8 b;
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    b[e] = bf16_bits(v[e]);
-                *reinterpret_cast<u16x8*>(out16 + to) = b;
-            }
-            return;
+        if (FINAL == kOutF32 || (FINAL == kWeights && applies)) {
+            *reinterpret_cast<f32x4*>(out + to) = f32x4{v[0], v[1], v[2], v[3]};
+            *reinterpret_cast<f32x4*>(out + to + 4) = f32x4{v[4], v[5], v[6], v[7]};
         }
+        if (FINAL == kOutBf16 || (FINAL == kWeights && out16)) {
+            u16x8 b;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if (col + e >= cols)
-                break;
-            if (wide)
-                out[to + e] = v[e];
-            if (narrow)
-                out16[to + e] = bf16_bits(v[e]);
+            for (int e = 0; e < 8; ++e)
+                b[e] = bf16_bits(v[e]);
+            *reinterpret_cast<u16x8*>(out16 + to) = b;
         }
     }
     __device__ inline void turn(int col, int row, const float (&v)[8]) const
@@ -565,7 +563,7 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_orth_up
     out.rate = m.rate;
     out.decay = args.decay;
     out.applies = applies;
-    out.whole = m.cols % 8 == 0;
+    out.narrow = FINAL != kAgain && m.cols % 8 != 0;
     const int64_t at = int64_t(r0) * m.cp + c0, to = int64_t(r0) * m.cols + c0;
     out.h = m.h[from] + at;
     out.l = m.l[from] + at;

@@ -340,7 +340,9 @@ __device__ inline void product(Mul& mul, S& c, const void* P, int64_t pitch_p, i
 // Writer w:
 //   w.fetch(row, col, p)     requests what results [row][col .. col + 8) need, into slot p;
 //   w.store(row, col, v, p)  takes the sums v, leaves the results there and stores them;
-//   w.turn(col, row, v)      with kTurned: stores results [row .. row + 8)[col] of the transpose.
+//   w.turn(col, row, v)      with kTurned: stores results [row .. row + 8)[col] of the transpose;
+//   w.narrow                 true: results go one by one, w.store_one(row, col, sum), a wave's
+//                            lanes side by side (rows that do not keep eight results aligned).
 // Rows and columns count from the tile's origin.
 template <typename S, typename Writer>
 __device__ inline void finish(const S& c, uint8_t* lds, Writer& w)
@@ -354,9 +356,11 @@ __device__ inline void finish(const S& c, uint8_t* lds, Writer& w)
     const int r0 = S::wave_row(), c0 = S::wave_col();
 #pragma unroll
     for (int i = 0; i < S::I; ++i) {
+        if (!w.narrow) {
 #pragma unroll
-        for (int p = 0; p < kPasses; ++p)
-            w.fetch(r0 + 32 * i + p * kDown + down, c0 + across, p);
+            for (int p = 0; p < kPasses; ++p)
+                w.fetch(r0 + 32 * i + p * kDown + down, c0 + across, p);
+        }
 #pragma unroll
         for (int jg = 0; jg < 4 * S::J; ++jg) {
             const int j = jg / 4, g = jg % 4;
@@ -366,6 +370,13 @@ __device__ inline void finish(const S& c, uint8_t* lds, Writer& w)
                       c.acc[i][j][4 * g + 3]};
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (w.narrow) {
+#pragma unroll 8
+            for (int e = lane; e < 32 * W; e += 64)
+                w.store_one(r0 + 32 * i + e / W, c0 + e % W, mine[e / W * kPitch + e % W]);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            continue;
+        }
 #pragma unroll
         for (int p = 0; p < kPasses; ++p) {
             float* at = mine + (p * kDown + down) * kPitch + across;

@@ -254,7 +254,8 @@ def test_linear_layer(layer, dtype):
 
 
 @pytest.mark.parametrize("tokens", [1, 2, 15, 16, 17, 31, 33, 63, 64, 65])
-@pytest.mark.parametrize("sizes", [(100, 40), (128, 16), (1000, 257), (5120, 300), (384, 16400)])
+@pytest.mark.parametrize("sizes", [(100, 40), (128, 16), (1000, 257), (5120, 300), (384, 16400),
+                                   (7000, 90), (9000, 70)])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_few_tokens(tokens, sizes, dtype):
     """x quantized on the way, and as codes: the same values, whatever the number of tokens."""
