@@ -18,7 +18,8 @@ from .lazytrain import (  # noqa: F401
     GradNormAccumulator,
     StreamedHybrid8bitAdamW)
 from .muon import (  # noqa: F401
-    lt_muon_step, lt_muon_workspace_bytes, lt_orthogonalize, lt_orthogonalize_workspace_bytes)
+    HybridMuon, lt_muon_step, lt_muon_workspace_bytes, lt_orthogonalize,
+    lt_orthogonalize_workspace_bytes)
 from .fp8 import (  # noqa: F401
     Fp8Linear, Fp8Weight, fp8_linear, fp8_linear_backward, fp8_linear_forward, lt_fp8_code_pitch,
     lt_fp8_matmul, lt_fp8_quantize, lt_fp8_scale_pitch)

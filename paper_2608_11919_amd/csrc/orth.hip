@@ -1110,6 +1110,8 @@ void launch_thin(const Gate& gate, const Matrix* mats, int first, int n, const C
 // into the caller's stream.
 class Fork {
 public:
+    Fork() = default;
+    Fork(const Fork&) = delete;
     lt_err begin(hipStream_t st)
     {
         hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
@@ -1132,17 +1134,19 @@ public:
         LT_TRY_HIP(hipEventRecord(l.forked, st));
         LT_TRY_HIP(hipStreamWaitEvent(l.stream, l.forked, 0));
         lane_ = &l;
+        st_ = st;
         return LT_OK;
     }
+    ~Fork() { (void)end(); }  // a call that fails half way is joined too
     hipStream_t side(hipStream_t st) const { return lane_ ? lane_->stream : st; }
-    lt_err end(hipStream_t st)
+    lt_err end()
     {
         if (!lane_)
             return LT_OK;
         Lane& l = *lane_;
         lane_ = nullptr;
         LT_TRY_HIP(hipEventRecord(l.joined, l.stream));
-        LT_TRY_HIP(hipStreamWaitEvent(st, l.joined, 0));
+        LT_TRY_HIP(hipStreamWaitEvent(st_, l.joined, 0));
         return LT_OK;
     }
 
@@ -1152,6 +1156,7 @@ private:
         hipEvent_t forked = nullptr, joined = nullptr;
     };
     Lane* lane_ = nullptr;
+    hipStream_t st_ = nullptr;
     std::unique_lock<std::mutex> lock_;
 };
 
@@ -1286,7 +1291,7 @@ lt_err run_batches(const Call& c, float decay, Fill fill, Begin begin)
         }
         LT_TRY_HIP(hipGetLastError());
     }
-    return fork.end(c.st);
+    return fork.end();
 }
 
 void add_range(std::vector<host::Range>& r, const void* p, size_t bytes, bool written)

@@ -122,11 +122,11 @@ class Fp8Weight:
         return cls(rows, cols, codes, scales, codes_t, scales_t)
 
     @classmethod
-    def from_master(cls, w: torch.Tensor, transposed: bool = True, stream=None) -> "Fp8Weight":
-        """Quantizes a weight matrix (float32 or bfloat16)."""
+    def from_master(cls, w: torch.Tensor, transposed: bool = True) -> "Fp8Weight":
+        """Quantizes a weight matrix (float32 or bfloat16) on the current stream."""
         _rows(w, "w")
         weight = cls.empty(w.shape[0], w.shape[1], w.device, transposed)
-        weight.update(w, stream=stream)
+        weight.update(w)
         return weight
 
     def update(self, w: torch.Tensor, stream=None) -> None:
@@ -148,10 +148,11 @@ def _tokens(x: torch.Tensor, features: int, what: str) -> torch.Tensor:
 
 
 def fp8_linear(x: torch.Tensor, weight: Fp8Weight,
-               out_dtype: torch.dtype = torch.bfloat16, workspace: Optional[torch.Tensor] = None,
-               stream=None) -> torch.Tensor:
+               out_dtype: torch.dtype = torch.bfloat16,
+               workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """f9: x weight^T for x (..., in_features), quantized on the way; for answering: nothing is
-    kept for a backward pass."""
+    kept for a backward pass.  This and the functions below allocate and work on the current
+    stream."""
     t = _tokens(x, weight.cols, "x")
     stride = _rows(t, "x")
     m, device = t.shape[0], x.device
@@ -161,13 +162,13 @@ def fp8_linear(x: torch.Tensor, weight: Fp8Weight,
     ws, nbytes = 0, 0
     if m > 16 or workspace is not None:
         nbytes = int(lib().lt_fp8_linear_workspace_bytes(m, weight.rows, weight.cols))
-        held = _workspace(device, nbytes, workspace, stream, "fp8")
+        held = _workspace(device, nbytes, workspace, None, "fp8")
         ws, nbytes = held.data_ptr(), held.numel() * held.element_size()
     with _current(device):
         _check(lib().lt_fp8_linear(t.data_ptr(), _dtype_code(t, "x"), stride,
                                    weight.codes.data_ptr(), weight.scales.data_ptr(), m,
                                    weight.rows, weight.cols, y.data_ptr(), _dtype_code(y, "y"),
-                                   weight.rows, ws, nbytes, _stream_handle(stream, device)))
+                                   weight.rows, ws, nbytes, _stream_handle(None, device)))
     return y if x.dim() == 2 else y.view(*x.shape[:-1], weight.rows)
 
 

@@ -792,13 +792,15 @@ class Hybrid8bitAdamW:
         self.device = dev
         self.lr, self.betas, self.eps, self.weight_decay = lr, betas, eps, weight_decay
         self.max_norm, self.block_size, self.code_map = max_norm, block_size, code_map
+        elsewhere = self._elsewhere()
         if slice_fraction is None:
             self.is_8bit = [True] * len(self.params)
         else:
-            self.is_8bit, _ = lt_select_8bit_slice([p.numel() for p in self.params],
-                                                   slice_fraction)
-        self.idx8 = [i for i, b in enumerate(self.is_8bit) if b]
-        self.idx32 = [i for i, b in enumerate(self.is_8bit) if not b]
+            self.is_8bit, _ = lt_select_8bit_slice(
+                [0 if i in elsewhere else p.numel() for i, p in enumerate(self.params)],
+                slice_fraction)
+        self.idx8 = [i for i, b in enumerate(self.is_8bit) if b and i not in elsewhere]
+        self.idx32 = [i for i, b in enumerate(self.is_8bit) if not b and i not in elsewhere]
         p8 = [self.params[i] for i in self.idx8]
         self.m_codes = [torch.zeros(p.numel(), dtype=torch.int8, device=dev) for p in p8]
         self.v_codes = [torch.zeros(p.numel(), dtype=torch.uint8, device=dev) for p in p8]
@@ -823,6 +825,14 @@ class Hybrid8bitAdamW:
         # the zeroed states and the step state were written on the current stream; steps
         # may come on any stream
         torch.cuda.synchronize(dev)
+
+    # ------------------------------------------- parameters another step updates
+    def _elsewhere(self) -> frozenset:
+        """Indices of the parameters that AdamW leaves to _step_elsewhere (a subclass's)."""
+        return frozenset()
+
+    def _step_elsewhere(self, grads, stream) -> None:
+        pass
 
     # ------------------------------------------------------------ step state
     def _reset_state(self, applied: int, skips: int, stream=None) -> None:
@@ -940,6 +950,7 @@ class Hybrid8bitAdamW:
                                [grads[i] for i in self.idx32], self.exp_avg, self.exp_avg_sq,
                                params_bf16=None if wb is None else [wb[i] for i in self.idx32],
                                **hyper)
+        self._step_elsewhere(grads, stream)
         lt_step_state_advance(self._state, self.status, stream=stream)
         self._bound += 1
         # a snapshot of the count and the status, read later without waiting

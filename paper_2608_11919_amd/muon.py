@@ -10,9 +10,9 @@ from typing import Optional, Sequence
 import torch
 
 from . import lazytrain as _lt
-from .lazytrain import (LT_DTYPE_BF16, LT_DTYPE_F32, LT_MAP_LINEAR, _List, _bf16_list, _check,
-                        _check_block_size, _current, _device_of, _grad_code, _scalar, _state_ptr,
-                        _stream_handle, _workspace, lib)
+from .lazytrain import (LT_DTYPE_BF16, LT_DTYPE_F32, LT_MAP_LINEAR, Hybrid8bitAdamW, _List,
+                        _bf16_list, _check, _check_block_size, _current, _device_of, _grad_code,
+                        _scalar, _state_ptr, _stream_handle, _workspace, lib)
 
 _DTYPES = {torch.float32: LT_DTYPE_F32, torch.bfloat16: LT_DTYPE_BF16}
 
@@ -123,3 +123,85 @@ def lt_muon_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor],
             float(update_rms), int(ns_steps), _scalar(coef, device, torch.float32, "coef"),
             _scalar(status, device, torch.int32, "status"), _state_ptr(step_state, device),
             ws.data_ptr(), ws.numel() * ws.element_size(), _stream_handle(stream, device)))
+
+
+# ------------------------------------------------------------- optimizer object
+
+class HybridMuon(Hybrid8bitAdamW):
+    """Muon for matrices, 8-bit AdamW for the rest, under one global norm: a step is
+    lt_grad_sqnorm -> lt_clip_coef -> the AdamW steps -> lt_muon_step, on one stream without a
+    host synchronization, with the step count, the skips and the checkpoints of
+    Hybrid8bitAdamW.
+
+    ``matrices`` says which parameters Muon updates, one truth value each; by default every
+    parameter of two dimensions with two rows and two columns or more.  Embeddings and output
+    heads are commonly left to AdamW.  A Muon update has a root mean square of about
+    ``update_rms`` times lr, 0.2 being about AdamW's, so that one learning rate serves both.
+    Its momentum is held in 8 bits in blocks of ``block_size`` with ``muon_code_map``'s codes
+    (linear: nothing divides by it, so small values may round to 0)."""
+
+    def __init__(self, params: Sequence[torch.Tensor], lr: float = 1e-5, momentum: float = 0.95,
+                 nesterov: bool = True, ns_steps: int = 5, update_rms: float = 0.2,
+                 matrices: Optional[Sequence[bool]] = None, muon_code_map: int = LT_MAP_LINEAR,
+                 **adamw):
+        params = list(params)
+        if matrices is None:
+            matrices = [p.dim() == 2 and min(p.shape) > 1 for p in params]
+        matrices = [bool(m) for m in matrices]
+        if len(matrices) != len(params):
+            raise ValueError("matrices needs one truth value per parameter")
+        for i, (m, p) in enumerate(zip(matrices, params)):
+            if m and (p.dim() != 2 or not p.is_contiguous()):
+                raise ValueError(f"parameter {i} must be a contiguous matrix")
+        self.is_matrix = matrices
+        self.idx_muon = [i for i, m in enumerate(matrices) if m]
+        self.momentum, self.nesterov, self.ns_steps = momentum, nesterov, ns_steps
+        self.update_rms, self.muon_code_map = update_rms, muon_code_map
+        super().__init__(params, lr=lr, **adamw)
+        dev = self.device
+        mine = [self.params[i] for i in self.idx_muon]
+        self.muon_codes = [torch.zeros(p.numel(), dtype=torch.int8, device=dev) for p in mine]
+        self.muon_absmax = [torch.zeros(-(-p.numel() // self.block_size), dtype=torch.float32,
+                                        device=dev) for p in mine]
+        torch.cuda.synchronize(dev)  # steps may come on any stream
+
+    def _elsewhere(self) -> frozenset:
+        return frozenset(self.idx_muon)
+
+    def _step_elsewhere(self, grads, stream) -> None:
+        if not self.idx_muon:
+            return
+        wb = self.params_bf16
+        lt_muon_step([self.params[i] for i in self.idx_muon], [grads[i] for i in self.idx_muon],
+                     self.muon_codes, self.muon_absmax, self.block_size, lr=self.lr,
+                     momentum=self.momentum, weight_decay=self.weight_decay,
+                     ns_steps=self.ns_steps, nesterov=self.nesterov, update_rms=self.update_rms,
+                     coef=self.coef, status=self.status, stream=stream,
+                     params_bf16=None if wb is None else [wb[i] for i in self.idx_muon],
+                     code_map=self.muon_code_map, step_state=self._state)
+
+    def state_dict(self, stream=None) -> dict:
+        state = super().state_dict(stream)
+        host = lambda ts: [t.detach().cpu().clone() for t in ts]
+        state["muon"] = {"is_matrix": list(self.is_matrix), "momentum": self.momentum,
+                         "nesterov": self.nesterov, "ns_steps": self.ns_steps,
+                         "update_rms": self.update_rms, "code_map": self.muon_code_map,
+                         "codes": host(self.muon_codes), "absmax": host(self.muon_absmax)}
+        return state
+
+    def load_state_dict(self, state: dict) -> None:
+        mine = state.get("muon")
+        if mine is None or list(mine["is_matrix"]) != list(self.is_matrix):
+            raise ValueError("the checkpoint's Muon matrices differ from this optimizer's")
+        if mine["code_map"] != self.muon_code_map:
+            raise ValueError("the checkpoint's code map of the momentum differs")
+        for name, tensors in (("codes", self.muon_codes), ("absmax", self.muon_absmax)):
+            if [t.shape for t in mine[name]] != [t.shape for t in tensors]:
+                raise ValueError(f"muon {name}: shapes differ from the checkpoint")
+        super().load_state_dict(state)
+        self.momentum, self.nesterov = mine["momentum"], mine["nesterov"]
+        self.ns_steps, self.update_rms = mine["ns_steps"], mine["update_rms"]
+        for name, tensors in (("codes", self.muon_codes), ("absmax", self.muon_absmax)):
+            for a, b in zip(tensors, mine[name]):
+                a.copy_(b)
+        torch.cuda.synchronize(self.device)
