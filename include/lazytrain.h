@@ -85,7 +85,8 @@ typedef enum lt_err {
     LT_ERR_INVALID_ARG = 1, /* NULL pointer, negative size, unsupported block size or dtype, bad hyperparameter */
     LT_ERR_ALIGNMENT = 2,   /* a base pointer is not aligned as stated above */
     LT_ERR_HIP = 3,         /* a HIP runtime call failed (device query, copy, launch, sync) */
-    LT_ERR_WORKSPACE = 4    /* workspace NULL, misaligned or smaller than the size query returns */
+    LT_ERR_WORKSPACE = 4,   /* workspace NULL, misaligned or smaller than the size query returns */
+    LT_ERR_HOST = 5         /* host memory ran out (f5 to f9; their size queries return 0 then) */
 } lt_err;
 
 /* The status word written on the device by the norm (and lt_clip_coef).  The
@@ -548,7 +549,8 @@ int64_t lt_fp8_scale_pitch(int64_t cols);
  * layout, holds that scale), so that codes_t is the transpose of codes: for weights, which a
  * forward and a backward product read.  Codes are x * 2^-e rounded to nearest even.  A group with
  * a NaN or an infinity has scale 255 and NaN codes, and makes the results that read it NaN.
- * x and codes 16-byte aligned, scales 4-byte.
+ * rows, cols < 2^31, fewer than 2^24 blocks of 128 x 128; x and codes 16-byte aligned, scales
+ * 4-byte; no array overlaps another.
  */
 lt_err lt_fp8_quantize(const void* x, int dtype, int64_t rows, int64_t cols, int64_t row_stride,
                        int square, uint8_t* codes, uint8_t* scales, uint8_t* codes_t,
@@ -565,7 +567,7 @@ size_t lt_fp8_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k);
  * A linear layer's three products, with x (tokens x in), weight (out x in) and dy:
  *   y  = matmul(x, weight),  dx = matmul(dy, weight's transpose),
  *   dw = matmul(dy's transpose, x's transpose).
- * m, n < 2^31, k < 2^23.
+ * m, n < 2^28, k < 2^23; out overlaps no operand.
  */
 lt_err lt_fp8_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes,
                      const uint8_t* b_scales, int64_t m, int64_t n, int64_t k, void* out,

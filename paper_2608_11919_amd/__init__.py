@@ -6,7 +6,7 @@ binding.  Importing it does not load the library; the first call does, and
 raises if the library has not been built.
 """
 from .lazytrain import (  # noqa: F401
-    LT_OK, LT_ERR_INVALID_ARG, LT_ERR_ALIGNMENT, LT_ERR_HIP, LT_ERR_WORKSPACE,
+    LT_OK, LT_ERR_INVALID_ARG, LT_ERR_ALIGNMENT, LT_ERR_HIP, LT_ERR_WORKSPACE, LT_ERR_HOST,
     LT_DTYPE_BF16, LT_DTYPE_F32, LT_MAP_DYNAMIC, LT_MAP_LINEAR, LT_STATUS_BAD_WORKSPACE,
     LT_STATUS_NONFINITE, LT_STATUS_OK, Hybrid8bitAdamW, LazyTrainError, NonFiniteAbort, lib,
     lt_clip_coef, lt_grad_sqnorm, lt_grad_sqnorm_workspace_bytes, lt_hybrid8bit_adamw_step,

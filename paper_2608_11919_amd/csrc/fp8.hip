@@ -18,7 +18,8 @@
 #include "tiles.h"
 
 #include <algorithm>
-#include <cmath>
+#include <string>
+#include <vector>
 
 namespace {
 
@@ -756,6 +757,8 @@ __global__ __launch_bounds__(256) void k_fp8_zero(int64_t m, int64_t n, void* ou
 
 // Rows of codes stay within the 32-bit offsets of a tile's loads.
 constexpr int64_t kMostSummed = int64_t(1) << 23;
+// Workgroups of 256 threads in a launch: the grid counts threads in 32 bits.
+constexpr int64_t kMostGroups = int64_t(1) << 24;
 
 struct Way {
     int tile;    // 256, 128 or 64
@@ -788,9 +791,23 @@ Way way_of(int64_t m, int64_t n, int64_t k)
 
 bool valid_sizes(int64_t m, int64_t n, int64_t k)
 {
-    const int64_t most = int64_t(1) << 31;
+    const int64_t most = int64_t(1) << 28;
     return m >= 0 && n >= 0 && k >= 0 && m < most && n < most && k < kMostSummed &&
-           host::ceil_div(m, 64) * host::ceil_div(n, 64) < most;
+           host::ceil_div(m, 256) * host::ceil_div(n, 256) < kMostGroups;
+}
+
+// The last element of a matrix has an address, with room to spare in 64 bits.
+bool valid_stride(int64_t rows, int64_t cols, int64_t stride)
+{
+    return stride >= cols && stride <= (int64_t(1) << 46) / std::max<int64_t>(rows, 1);
+}
+
+// Bytes from the first to the last element of rows x cols, `stride` elements from row to row.
+size_t span_bytes(int64_t rows, int64_t cols, int64_t stride, int dtype)
+{
+    if (rows == 0 || cols == 0)
+        return 0;
+    return size_t((rows - 1) * stride + cols) * (dtype == LT_DTYPE_BF16 ? 2 : 4);
 }
 
 template <typename Tile>
@@ -899,14 +916,16 @@ int64_t lt_fp8_scale_pitch(int64_t cols) { return cols < 0 ? 0 : scale_pitch(col
 lt_err lt_fp8_quantize(const void* x, int dtype, int64_t rows, int64_t cols, int64_t row_stride,
                        int square, uint8_t* codes, uint8_t* scales, uint8_t* codes_t,
                        uint8_t* scales_t, void* stream)
-{
+try {
     host::clear_error();
     if (dtype != LT_DTYPE_F32 && dtype != LT_DTYPE_BF16)
         return fail(LT_ERR_INVALID_ARG, "dtype must be LT_DTYPE_F32 or LT_DTYPE_BF16");
     const int64_t most = int64_t(1) << 31;
-    if (rows < 0 || cols < 0 || rows >= most || cols >= most || row_stride < cols ||
-        host::ceil_div(rows, kGroup) * host::ceil_div(cols, kGroup) >= most)
-        return fail(LT_ERR_INVALID_ARG, "need 0 <= rows, cols < 2^31 and row_stride >= cols");
+    if (rows < 0 || cols < 0 || rows >= most || cols >= most ||
+        !valid_stride(rows, cols, row_stride) ||
+        host::ceil_div(rows, kGroup) * host::ceil_div(cols, kGroup) >= kMostGroups)
+        return fail(LT_ERR_INVALID_ARG, "need 0 <= rows, cols < 2^31, blocks of 128 x 128 < 2^24 "
+                                        "and row_stride >= cols");
     if ((codes != nullptr) != (scales != nullptr) || (codes_t != nullptr) != (scales_t != nullptr))
         return fail(LT_ERR_INVALID_ARG, "codes come with their scales");
     if (rows == 0 || cols == 0)
@@ -916,6 +935,20 @@ lt_err lt_fp8_quantize(const void* x, int dtype, int64_t rows, int64_t cols, int
     if (!host::aligned(x, 16) || !host::aligned(codes, 16) || !host::aligned(codes_t, 16) ||
         !host::aligned(scales, 4) || !host::aligned(scales_t, 4))
         return fail(LT_ERR_ALIGNMENT, "x and codes must be 16-byte aligned, scales 4-byte");
+    std::vector<host::Range> ranges;
+    const auto range = [&](const void* p, size_t bytes, bool written) {
+        const auto lo = reinterpret_cast<uintptr_t>(p);
+        if (p)
+            ranges.push_back({lo, lo + bytes, written});
+    };
+    range(x, span_bytes(rows, cols, row_stride, dtype), false);
+    range(codes, size_t(rows) * size_t(code_pitch(cols)), true);
+    range(scales, size_t(rows) * size_t(scale_pitch(cols)), true);
+    range(codes_t, size_t(cols) * size_t(code_pitch(rows)), true);
+    range(scales_t, size_t(cols) * size_t(scale_pitch(rows)), true);
+    const std::string overlap = host::overlap(ranges);
+    if (!overlap.empty())
+        return fail(LT_ERR_INVALID_ARG, overlap);
     QuantizeArgs a{x,
                    rows,
                    cols,
@@ -932,7 +965,7 @@ lt_err lt_fp8_quantize(const void* x, int dtype, int64_t rows, int64_t cols, int
     const dim3 grid(uint32_t(host::ceil_div(rows, kGroup) * a.across));
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const int64_t by_rows = host::ceil_div(rows * (a.scale_pitch / 4), kQuantizeThreads / 64);
-    if (!codes_t && !square && by_rows < most) {
+    if (!codes_t && !square && by_rows < kMostGroups) {
         auto* kernel = dtype == LT_DTYPE_BF16 ? k_fp8_quantize_rows<uint16_t>
                                               : k_fp8_quantize_rows<float>;
         kernel<<<dim3(uint32_t(by_rows)), kQuantizeThreads, 0, st>>>(a);
@@ -945,6 +978,8 @@ lt_err lt_fp8_quantize(const void* x, int dtype, int64_t rows, int64_t cols, int
     kernel<<<grid, kQuantizeThreads, 0, st>>>(a);
     LT_TRY_HIP(hipGetLastError());
     return LT_OK;
+} catch (...) {
+    return host::caught();
 }
 
 size_t lt_fp8_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k)
@@ -962,10 +997,10 @@ lt_err lt_fp8_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const uint
                      const uint8_t* b_scales, int64_t m, int64_t n, int64_t k, void* out,
                      int out_dtype, int64_t out_stride, void* workspace, size_t workspace_bytes,
                      void* stream)
-{
+try {
     host::clear_error();
-    if (!valid_sizes(m, n, k) || out_stride < n)
-        return fail(LT_ERR_INVALID_ARG, "need 0 <= m, n < 2^31, 0 <= k < 2^23 and out_stride >= n");
+    if (!valid_sizes(m, n, k) || !valid_stride(m, n, out_stride))
+        return fail(LT_ERR_INVALID_ARG, "need 0 <= m, n < 2^28, 0 <= k < 2^23 and out_stride >= n");
     if (out_dtype != LT_DTYPE_F32 && out_dtype != LT_DTYPE_BF16)
         return fail(LT_ERR_INVALID_ARG, "out_dtype must be LT_DTYPE_F32 or LT_DTYPE_BF16");
     if (m == 0 || n == 0)
@@ -978,6 +1013,20 @@ lt_err lt_fp8_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const uint
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const bool f32 = out_dtype == LT_DTYPE_F32;
     const Way w = way_of(m, n, k);
+    const bool few = m <= kFewTokens, cut = k > 0 && !few && w.slices > 1;
+    if (cut) {
+        const size_t need = lt_fp8_matmul_workspace_bytes(m, n, k);
+        if (!workspace || !host::aligned(workspace, 256) || workspace_bytes < need)
+            return fail(LT_ERR_WORKSPACE, "workspace must be 256-byte aligned and hold " +
+                                              std::to_string(need) + " bytes");
+    }
+    const size_t out_bytes = span_bytes(m, n, out_stride, out_dtype);
+    const size_t a_pitch = size_t(code_pitch(k)), a_scale_pitch = size_t(scale_pitch(k));
+    if (host::overlaps(out, out_bytes, a_codes, size_t(m) * a_pitch) ||
+        host::overlaps(out, out_bytes, b_codes, size_t(n) * a_pitch) ||
+        host::overlaps(out, out_bytes, a_scales, size_t(m) * a_scale_pitch) ||
+        host::overlaps(out, out_bytes, b_scales, size_t(n) * a_scale_pitch))
+        return fail(LT_ERR_INVALID_ARG, "out overlaps an operand");
     if (k == 0) {  // an empty sum
         auto* join = f32 ? k_fp8_zero<true> : k_fp8_zero<false>;
         join<<<dim3(uint32_t(std::min<int64_t>(4096, host::ceil_div(m * n, 256)))), 256, 0, st>>>(
@@ -985,7 +1034,7 @@ lt_err lt_fp8_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const uint
         LT_TRY_HIP(hipGetLastError());
         return LT_OK;
     }
-    if (m <= kFewTokens) {
+    if (few) {
         const FewArgs f{b_codes, b_scales, a_codes, a_scales, m, n, k, code_pitch(k),
                         scale_pitch(k), 0, int(host::ceil_div(k, kGroup)), out, out_stride};
         int cus;
@@ -997,13 +1046,8 @@ lt_err lt_fp8_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const uint
     }
     ProductArgs g{a_codes, a_scales,   b_codes, b_scales,   m,      n, code_pitch(k),
                   scale_pitch(k), int(host::ceil_div(k, kGroup)), w.slice, out, out_stride, nullptr};
-    if (w.slices > 1) {
-        const size_t need = lt_fp8_matmul_workspace_bytes(m, n, k);
-        if (!workspace || !host::aligned(workspace, 256) || workspace_bytes < need)
-            return fail(LT_ERR_WORKSPACE, "workspace must be 256-byte aligned and hold " +
-                                              std::to_string(need) + " bytes");
+    if (cut)
         g.partial = static_cast<float*>(workspace);
-    }
     if (w.tile == 256)
         launch_product<Large>(g, w, f32, st);
     else if (w.tile == 128)
@@ -1017,6 +1061,8 @@ lt_err lt_fp8_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const uint
     }
     LT_TRY_HIP(hipGetLastError());
     return LT_OK;
+} catch (...) {
+    return host::caught();
 }
 
 size_t lt_fp8_linear_workspace_bytes(int64_t m, int64_t n, int64_t k)
@@ -1028,10 +1074,10 @@ lt_err lt_fp8_linear(const void* x, int dtype, int64_t x_stride, const uint8_t* 
                      const uint8_t* w_scales, int64_t m, int64_t n, int64_t k, void* out,
                      int out_dtype, int64_t out_stride, void* workspace, size_t workspace_bytes,
                      void* stream)
-{
+try {
     host::clear_error();
-    if (!valid_sizes(m, n, k) || out_stride < n || x_stride < k)
-        return fail(LT_ERR_INVALID_ARG, "need 0 <= m, n < 2^31, 0 <= k < 2^23, x_stride >= k and "
+    if (!valid_sizes(m, n, k) || !valid_stride(m, n, out_stride) || !valid_stride(m, k, x_stride))
+        return fail(LT_ERR_INVALID_ARG, "need 0 <= m, n < 2^28, 0 <= k < 2^23, x_stride >= k and "
                                         "out_stride >= n");
     if ((dtype != LT_DTYPE_F32 && dtype != LT_DTYPE_BF16) ||
         (out_dtype != LT_DTYPE_F32 && out_dtype != LT_DTYPE_BF16))
@@ -1046,6 +1092,15 @@ lt_err lt_fp8_linear(const void* x, int dtype, int64_t x_stride, const uint8_t* 
     if (k == 0)
         return lt_fp8_matmul(nullptr, nullptr, nullptr, nullptr, m, n, k, out, out_dtype,
                              out_stride, nullptr, 0, stream);
+    const LinearLayout l = linear_layout(m, n, k);
+    if (m > kFewValues && (!workspace || !host::aligned(workspace, 256) || workspace_bytes < l.total))
+        return fail(LT_ERR_WORKSPACE, "workspace must be 256-byte aligned and hold " +
+                                          std::to_string(l.total) + " bytes");
+    const size_t out_bytes = span_bytes(m, n, out_stride, out_dtype);
+    if (host::overlaps(out, out_bytes, x, span_bytes(m, k, x_stride, dtype)) ||
+        host::overlaps(out, out_bytes, w_codes, size_t(n) * size_t(code_pitch(k))) ||
+        host::overlaps(out, out_bytes, w_scales, size_t(n) * size_t(scale_pitch(k))))
+        return fail(LT_ERR_INVALID_ARG, "out overlaps x or the weight");
     if (m <= kFewValues) {
         const FewArgs f{w_codes, w_scales, x, nullptr, m, n, k, code_pitch(k), scale_pitch(k),
                         x_stride, int(host::ceil_div(k, kGroup)), out, out_stride};
@@ -1061,16 +1116,14 @@ lt_err lt_fp8_linear(const void* x, int dtype, int64_t x_stride, const uint8_t* 
         LT_TRY_HIP(hipGetLastError());
         return LT_OK;
     }
-    const LinearLayout l = linear_layout(m, n, k);
-    if (!workspace || !host::aligned(workspace, 256) || workspace_bytes < l.total)
-        return fail(LT_ERR_WORKSPACE, "workspace must be 256-byte aligned and hold " +
-                                          std::to_string(l.total) + " bytes");
     auto* ws = static_cast<uint8_t*>(workspace);
     if (lt_err e = lt_fp8_quantize(x, dtype, m, k, x_stride, 0, ws, ws + l.scales, nullptr,
                                    nullptr, stream))
         return e;
     return lt_fp8_matmul(ws, ws + l.scales, w_codes, w_scales, m, n, k, out, out_dtype, out_stride,
                          ws + l.matmul, l.total - l.matmul, stream);
+} catch (...) {
+    return host::caught();
 }
 
 }  // extern "C"

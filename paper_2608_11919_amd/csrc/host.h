@@ -37,6 +37,10 @@ lt_err put_descriptors(std::vector<uint8_t>& image, void* ws, hipStream_t st, Gu
 
 lt_err compute_units(int* cus);
 
+// For an entry point's handler of all exceptions, none of which leaves it: a list that does not
+// fit host memory is an error like any other.
+lt_err caught() noexcept;
+
 bool aligned(const void* p, size_t a);
 bool valid_block_size(int block);
 
@@ -47,6 +51,12 @@ struct Range {
 };
 // Empty when nothing overlaps, else a message.
 std::string overlap(std::vector<Range>& ranges);
+
+inline bool overlaps(const void* a, size_t a_bytes, const void* b, size_t b_bytes)
+{
+    const auto x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return a && b && a_bytes && b_bytes && x < y + b_bytes && y < x + a_bytes;
+}
 
 // ------------------------------------------------------- 8-bit momentum (momentum.hip)
 

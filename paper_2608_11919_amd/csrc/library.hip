@@ -10,6 +10,15 @@ namespace host {
 
 lt_err fail(lt_err code, const std::string& msg) { return ::fail(code, msg); }
 
+lt_err caught() noexcept
+{
+    try {
+        return ::fail(LT_ERR_HOST, "host memory ran out");
+    } catch (...) {
+        return LT_ERR_HOST;
+    }
+}
+
 void clear_error() { g_last_error.clear(); }
 
 lt_err put_descriptors(std::vector<uint8_t>& image, void* ws, hipStream_t st, Guard* guard)

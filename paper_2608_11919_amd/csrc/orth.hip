@@ -923,7 +923,8 @@ __global__ __launch_bounds__(kThinThreads) void k_orth_thin(Gate gate,
 // A batch is what one sequence of launches works on.  Large ones fill the last rounds of their
 // launches: the three feed-forward matrices of a 27B-class layer (2.7e8 elements) one by one
 // leave a fifth of the CUs idle in every product.  16 bytes of workspace go with an element.
-constexpr int64_t kBatchElems = int64_t(3) << 27;  // padded elements of a batch of several
+constexpr int64_t kBatchElems = int64_t(1) << 27;  // padded elements of a batch of several,
+constexpr int64_t kBatchLargest = 4;               // or this many of the list's largest matrix
 
 enum { kPreUnits, kPrePrep, kPreSym, kPreTile, kPreSymLarge, kPreTileLarge, kPrefixes };
 
@@ -934,8 +935,9 @@ struct Plan {
     std::vector<int> way;      // of each batch: how its matrices are worked on
 };
 
-// How a matrix is worked on.  Thin ones by one workgroup each.  Long ones take their steps in pairs, which saves a sixth of the multiply-adds or
-// more; 128 rows or columns are the least that a tile computes anyway.
+// How a matrix is worked on.  Thin ones by one workgroup each.  Long ones take their steps in
+// pairs, which saves a sixth of the multiply-adds or more; 128 rows or columns are the least
+// that a tile computes anyway.
 enum { kThin, kSingle, kPairs, kWays };
 
 int way_of(int64_t rows, int64_t cols)
@@ -1001,13 +1003,16 @@ Plan make_plan(const int64_t* rows, const int64_t* cols, int K, bool muon, int64
         for (int k = 0; k < K; ++k)
             if (way_of(rows[k], cols[k]) == way)
                 p.order.push_back(k);
+    int64_t most = kBatchElems;
+    for (int k = 0; k < K; ++k)
+        most = std::max(most, kBatchLargest * padded(rows[k]) * padded(cols[k]));
     int64_t units = 0, elems = 0;
     size_t region[2] = {0, 0}, bytes = 0;  // of single steps, and of everything else
     for (int i = 0; i < K; ++i) {
         const int k = p.order[i];
         const int way = way_of(rows[k], cols[k]);
         const int64_t n = way == kThin ? rows[k] * cols[k] : padded(rows[k]) * padded(cols[k]);
-        if (p.batch.empty() || way != p.way.back() || (elems > 0 && elems + n > kBatchElems)) {
+        if (p.batch.empty() || way != p.way.back() || (elems > 0 && elems + n > most)) {
             p.batch.push_back(i);
             p.way.push_back(way);
             elems = 0;
@@ -1308,16 +1313,18 @@ constexpr int kMaxNsSteps = 64;
 extern "C" {
 
 size_t lt_orthogonalize_workspace_bytes(const int64_t* rows, const int64_t* cols, int n_matrices)
-{
+try {
     return valid_sizes(rows, cols, n_matrices)
                ? make_plan(rows, cols, n_matrices, false, kSquareUnit).total
                : 0;
+} catch (...) {
+    return 0;
 }
 
 lt_err lt_orthogonalize(const void* const* matrices, int in_dtype, void* const* out, int out_dtype,
                         const int64_t* rows, const int64_t* cols, int n_matrices, int ns_steps,
                         void* workspace, size_t workspace_bytes, void* stream)
-{
+try {
     host::clear_error();
     const int K = n_matrices;
     if (!valid_sizes(rows, cols, K) || (K > 0 && (!matrices || !out)))
@@ -1361,14 +1368,18 @@ lt_err lt_orthogonalize(const void* const* matrices, int in_dtype, void* const* 
             LT_TRY_HIP(hipGetLastError());
             return LT_OK;
         });
+} catch (...) {
+    return host::caught();
 }
 
 size_t lt_muon_workspace_bytes(const int64_t* rows, const int64_t* cols, int n_matrices,
                                int block_size)
-{
+try {
     return valid_sizes(rows, cols, n_matrices) && host::valid_block_size(block_size)
                ? make_plan(rows, cols, n_matrices, true, host::momentum_unit(block_size)).total
                : 0;
+} catch (...) {
+    return 0;
 }
 
 lt_err lt_muon_step(float* const* params, const void* const* grads, int grad_dtype,
@@ -1377,7 +1388,7 @@ lt_err lt_muon_step(float* const* params, const void* const* grads, int grad_dty
                     int code_map, double lr, double momentum, int nesterov, double weight_decay,
                     double update_rms, int ns_steps, const float* coef, const int32_t* status,
                     const void* step_state, void* workspace, size_t workspace_bytes, void* stream)
-{
+try {
     host::clear_error();
     const int K = n_matrices;
     if (!valid_sizes(rows, cols, K) ||
@@ -1446,6 +1457,8 @@ lt_err lt_muon_step(float* const* params, const void* const* grads, int grad_dty
                                          grad_dtype, block_size, code_map, s, coef, status,
                                          step_state, st);
         });
+} catch (...) {
+    return host::caught();
 }
 
 }  // extern "C"

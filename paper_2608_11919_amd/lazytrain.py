@@ -22,12 +22,13 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liblazytrain.so")
 
-LT_OK, LT_ERR_INVALID_ARG, LT_ERR_ALIGNMENT, LT_ERR_HIP, LT_ERR_WORKSPACE = range(5)
+(LT_OK, LT_ERR_INVALID_ARG, LT_ERR_ALIGNMENT, LT_ERR_HIP, LT_ERR_WORKSPACE,
+ LT_ERR_HOST) = range(6)
 LT_STATUS_OK, LT_STATUS_NONFINITE, LT_STATUS_BAD_WORKSPACE = 0, 1, 2
 LT_DTYPE_F32, LT_DTYPE_BF16 = 0, 1
 LT_MAP_LINEAR, LT_MAP_DYNAMIC = 0, 1
 ERROR_NAMES = {1: "LT_ERR_INVALID_ARG", 2: "LT_ERR_ALIGNMENT", 3: "LT_ERR_HIP",
-               4: "LT_ERR_WORKSPACE"}
+               4: "LT_ERR_WORKSPACE", 5: "LT_ERR_HOST"}
 
 _lib = None
 _lists = None  # the module paper_2608_11919_amd._lists or _PlainLists, set by lib()
