@@ -2,18 +2,18 @@
 // C[m][n] += sum_k P[m][k] * Q[n][k] over one output tile, both operands with k contiguous.
 //
 // Operands move in bytes: a step of the loop takes 128 bytes of every row (64 fp16 or 128
-// fp8 values), from HBM straight into LDS (16 bytes a lane, no registers in between), into
-// one of two buffers while the other is multiplied.  Row r keeps its 16-byte chunk c at
-// position c ^ (r / 2 & 7): LDS serves 256 bytes a cycle, two rows wide, so the sixteen rows that
-// one cycle reads at 16 bytes each must differ in position from one pair of rows to the next
-// (by r & 7 every read took twice its cycles).  The load writes LDS in lane order, by permuting
-// what each lane fetches.
+// fp8 values), whole lines, from HBM straight into LDS (16 bytes a lane, no registers in
+// between), into one of two buffers.  Row r keeps its 16-byte chunk c at position c ^ (r / 2 & 7):
+// LDS serves 256 bytes a cycle, two rows wide, so the sixteen rows that one cycle reads at 16
+// bytes each must differ in position from one pair of rows to the next (by r & 7 every read took
+// twice its cycles).  The load writes LDS in lane order, by permuting what each lane fetches.
 #ifndef LAZYTRAIN_TILES_H
 #define LAZYTRAIN_TILES_H
 
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 namespace tiles {
 
@@ -32,7 +32,7 @@ constexpr int kStepBytes = 128;  // of every row, per step of the main loop
 template <int ROWS, int THREADS>
 struct TileLoad {
     static constexpr int N = ROWS * 8 / THREADS;
-    static_assert(ROWS * 8 % THREADS == 0, "whole chunks per lane");
+    static_assert(N * 32 == ROWS, "a copy is a block of 32 rows");
     uint32_t offset[N];
 
     __device__ inline void init(int64_t pitch, int64_t limit)
@@ -56,33 +56,44 @@ struct TileLoad {
     }
 };
 
-// Every LDS read and every copy into LDS that the wave has under way is complete.
-__device__ inline void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
-__device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// Every LDS read that the wave has under way is complete: lgkmcnt(0), in the form that the
+// compiler sees, which then waits for no read of its own again.
+__device__ inline void wait_reads()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    asm volatile("" ::: "memory");
+}
+// Every copy into LDS but the wave's latest LEFT.
+template <int LEFT>
+__device__ inline void wait_loads()
+{
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
+}
 
-// The 32 x 32 instructions: a lane holds 32 bytes of row `l % 32` of a block of 32 rows for
-// each 64 bytes of the summed index, of which it takes 16-byte chunks l / 32 and l / 32 + 2 of
-// four (any assignment does that is the same for both operands).
+// The 32 x 32 instructions: of a step's 128 bytes of row `l % 32` of a block of 32 rows a lane
+// holds 16-byte chunks l / 32, + 2, + 4 and + 6 (any assignment does that is the same for both
+// operands).
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 struct Chunks {
-    i32x4 c[2];
+    i32x4 c[4];
 };
 
-__device__ inline i32x4 read_chunk(const uint8_t* tile, int row32, int half, int c, int lane)
+__device__ inline i32x4 read_chunk(const uint8_t* tile, int row32, int c, int lane)
 {
     const uint8_t* row = tile + (row32 + (lane & 31)) * kStepBytes;
-    const int at = ((4 * half + 2 * c + (lane >> 5)) ^ (lane >> 1 & 7)) << 4;
+    const int at = ((2 * c + (lane >> 5)) ^ (lane >> 1 & 7)) << 4;
     return *reinterpret_cast<const i32x4*>(row + at);
 }
 
-// Products of fp16: 32 values a half step, in two instructions.
+// Products of fp16: 64 values a step, in four instructions.
 struct Half {
-    static constexpr int kInstructions = 2;
+    static constexpr int kInstructions = 4;
     __device__ inline void begin() {}
     __device__ inline void copy(int) {}
     __device__ inline void read(int) {}
-    __device__ inline void next() {}
+    __device__ inline void next(int) {}
     __device__ inline f32x16 mul(int t, int, int, const Chunks& a, const Chunks& b, f32x16 c) const
     {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, a.c[t]),
@@ -163,12 +174,12 @@ typedef Shape<128, 128, 64, 64> Small;
 typedef Shape<256, 256, 128, 128> Large;
 typedef Shape<64, 64, 32, 32> Tiny;
 
-// Products of fp8 (e4m3) with a power-of-two scale for each row and each 128 values: 64 values a
-// half step, in one instruction, which applies the scales itself.  A scale is a byte, the
+// Products of fp8 (e4m3) with a power-of-two scale for each row and each 128 values: a step's in
+// two instructions of 64, which apply the scales themselves.  A scale is a byte, the
 // exponent biased by 127; four steps' worth are a word, copied into LDS four steps at a time.
 template <typename S>
 struct Fp8 {
-    static constexpr int kInstructions = 1;
+    static constexpr int kInstructions = 2;
     static constexpr int kRowsAll = S::kRows + S::kCols, kLdsBytes = 2 * kRowsAll * 4;
     const uint8_t *scales_p, *scales_q;  // of the tile's first rows, at the first step
     int64_t pitch, limit_p, limit_q;     // bytes of a row's scales; rows that exist
@@ -196,38 +207,40 @@ struct Fp8 {
         }
     }
     __device__ inline void begin() { copy_word(0); }
-    // after the barrier of step s: the buffer of the word before last is free
+    // before step s: the buffer of the word before last is free
     __device__ inline void copy(int s)
     {
         if ((s & 3) == 0)
             copy_word((s >> 2) + 1);
     }
-    // the scales of step s
+    // the word that holds the scales of step s
     __device__ inline void read(int s)
     {
         const auto* from = reinterpret_cast<const uint32_t*>(lds + (s >> 2 & 1) * kRowsAll * 4);
+#pragma unroll
+        for (int i = 0; i < S::I; ++i)
+            then_p[i] = from[S::row(i)];
+#pragma unroll
+        for (int j = 0; j < S::J; ++j)
+            then_q[j] = from[S::kRows + S::wave_col() + 32 * j + (S::lane() & 31)];
+    }
+    // its byte, where the multiplies look for it
+    __device__ inline void next(int s)
+    {
         const int shift = 8 * (s & 3);
 #pragma unroll
         for (int i = 0; i < S::I; ++i)
-            then_p[i] = from[S::row(i)] >> shift;
+            now_p[i] = then_p[i] >> shift;
 #pragma unroll
         for (int j = 0; j < S::J; ++j)
-            then_q[j] = from[S::kRows + S::wave_col() + 32 * j + (S::lane() & 31)] >> shift;
+            now_q[j] = then_q[j] >> shift;
     }
-    __device__ inline void next()
+    __device__ inline f32x16 mul(int t, int i, int j, const Chunks& a, const Chunks& b,
+                                 f32x16 c) const
     {
-#pragma unroll
-        for (int i = 0; i < S::I; ++i)
-            now_p[i] = then_p[i];
-#pragma unroll
-        for (int j = 0; j < S::J; ++j)
-            now_q[j] = then_q[j];
-    }
-    __device__ inline f32x16 mul(int, int i, int j, const Chunks& a, const Chunks& b, f32x16 c) const
-    {
-        const auto join = [](const Chunks& x) {
-            return i32x8{x.c[0][0], x.c[0][1], x.c[0][2], x.c[0][3],
-                         x.c[1][0], x.c[1][1], x.c[1][2], x.c[1][3]};
+        const auto join = [t](const Chunks& x) {
+            const i32x4 u = x.c[2 * t], v = x.c[2 * t + 1];
+            return i32x8{u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
         };
         return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(join(a), join(b), c, 0, 0, 0,
                                                                int(now_q[j]), 0, int(now_p[i]));
@@ -237,10 +250,21 @@ struct Fp8 {
 // The main loop over `steps` >= 1 steps.  P, Q: first rows of the tile's operands, pitches in
 // bytes, of which limit_p and limit_q rows exist.
 //
-// A step runs in two halves, and the operands of one half come out of LDS while the other is
-// multiplied.  Between them every wave has all of the step in registers: one barrier there
-// frees the buffer, and the copy of the step after next starts, a whole step before it is read.
-// The loop has no branches: past the end it copies and reads the last step again, unused.
+// A wave's block is multiplied in four quarters: the rows' blocks of 32 in two groups a0 and a1,
+// the columns' in b0 and b1, in an order in which neighbours share a group:
+//   even steps  a0 b0, a0 b1, a1 b1, a1 b0;   odd steps  a0 b1, a0 b0, a1 b0, a1 b1.
+// A group's registers are free once its last quarter is multiplied, and take the next step's
+// operands out of LDS during the quarters after: b1, a1, then the next step's a0 and b1 (odd
+// steps: b0, a1, a0, b0).  A step's first two reads are its late rows, the others early rows of
+// the next; each half of a step ends with a barrier, after which all waves have the rows read in
+// it in registers, and during the next half the copy of the step after next goes into their
+// place.  A copy has three halves' products' time to land, counted by the wave's own copies, and
+// copies come evenly, eight to a half: L2 feeds a CU some 26 bytes a cycle (15 TB/s in all),
+// and products of fp8 in tiles of 256 take 32.  In stages of 64 bytes of every row, half lines,
+// the copies alone took a fifth longer.
+// A body of two steps has no branches but one at its top: past the end it copies and reads the
+// last step again, unused, and a branch inside made the compiler move all products before it
+// behind it, away from the loads that they cover.
 template <typename Mul, typename S>
 __device__ inline void product(Mul& mul, S& c, const void* P, int64_t pitch_p, int64_t limit_p,
                                const void* Q, int64_t pitch_q, int64_t limit_q, int steps,
@@ -254,41 +278,94 @@ __device__ inline void product(Mul& mul, S& c, const void* P, int64_t pitch_p, i
     load_q.init(pitch_q, limit_q);
     const auto* p = static_cast<const uint8_t*>(P);
     const auto* q = static_cast<const uint8_t*>(Q);
-    constexpr int kLoads = load_p.N + load_q.N, kReads = 2 * (I + J);
-    constexpr int kMuls = I * J * Mul::kInstructions, kPaced = kMuls < 2 ? 1 : kMuls * 3 / 4;
-    // the k-th share of n things spread over the first three quarters of the products: the last
-    // quarter covers the latency of the reads
-    const auto share = [](int n, int k) { return k < kPaced ? n * k / kPaced : n; };
-    const auto load = [&](int s, int k) {
-        uint8_t* to = lds + (s & 1) * S::kBufferBytes;
+    constexpr int kLoads = load_p.N + load_q.N;
+    struct Groups {
+        // the blocks [first, first + n) of group g of `all`
+        static constexpr int n(int all, int g) { return g == 0 ? (all + 1) / 2 : all / 2; }
+        static constexpr int first(int all, int g) { return g == 0 ? 0 : (all + 1) / 2; }
+        // copies of the early or late rows of an even (0) or odd (1) step
+        static constexpr int loads(int odd, int late)
+        {
+            return S::kRows / 32 / I * n(I, late) + S::kCols / 32 / J * n(J, odd ^ late);
+        }
+    };
+    Chunks a[I], b[J];
+    // the k-th copy of step s's early or late rows
+    const auto load = [&](int s, int odd, int late, int k) {
+        uint8_t* to = lds + odd * S::kBufferBytes;
         const int64_t at = int64_t(s < steps ? s : steps - 1) * kStepBytes;
-        if (k < load_p.N)
-            load_p.issue(k, p + at, to);
-        else
-            load_q.issue(k - load_p.N, q + at, to + S::kRows * kStepBytes);
+        const int np = Groups::n(I, late), nq = Groups::n(J, odd ^ late);
+        const int all_p = S::kRows / 32 / I * np;
+        if (k < all_p) {
+            load_p.issue(k / np * I + Groups::first(I, late) + k % np, p + at, to);
+        } else {
+            const int l = k - all_p;
+            load_q.issue(l / nq * J + Groups::first(J, odd ^ late) + l % nq, q + at,
+                         to + S::kRows * kStepBytes);
+        }
     };
-    struct Operands {
-        Chunks a[I], b[J];
-    } x0, x1;
-    const auto read = [&](int s, int half, int k, Operands& x) {
-        const uint8_t* from = lds + (s & 1) * S::kBufferBytes;
-        const int c = k / (I + J), n = k % (I + J);
-        if (n < J)
-            x.b[n].c[c] = read_chunk(from + S::kRows * kStepBytes, wn + 32 * n, half, c, lane);
-        else
-            x.a[n - J].c[c] = read_chunk(from, wm + 32 * (n - J), half, c, lane);
+    const auto read_a = [&](int odd, int g, int k) {
+        const int i = Groups::first(I, g) + k / 4;
+        a[i].c[k % 4] = read_chunk(lds + odd * S::kBufferBytes, wm + 32 * i, k % 4, lane);
     };
-    // The products of one half step, with what the next one needs issued evenly between them.
-    // Every border keeps its place: left to itself the compiler issues reads right before the
-    // products that wait for them, and products of the second half ahead of the barrier.
-    const auto multiply = [&](const Operands& x, auto between) {
+    const auto read_b = [&](int odd, int g, int k) {
+        const int j = Groups::first(J, g) + k / 4;
+        b[j].c[k % 4] = read_chunk(lds + odd * S::kBufferBytes + S::kRows * kStepBytes,
+                                   wn + 32 * j, k % 4, lane);
+    };
+    // the products of groups ga and gb, with reads and copies issued evenly between them: reads
+    // within the first three quarters, so that the last covers their latency.  Every border
+    // keeps its place: left to itself the compiler issues reads right before the products that
+    // wait for them, and products ahead of the barrier.
+    const auto multiply = [&](int ga, int gb, int reads, auto read, int loads, auto copy) {
+        const int ni = Groups::n(I, ga), nj = Groups::n(J, gb);
+        const int muls = ni * nj * Mul::kInstructions, paced = muls * 3 / 4;
+        const auto share = [](int n, int of, int k) { return k < of ? n * k / of : n; };
+        if (muls == 0) {
 #pragma unroll
-        for (int k = 0; k < kMuls; ++k) {
-            between(k);
-            const int t = k / (I * J), i = k / J % I, j = k % J;
-            c.acc[i][j] = mul.mul(t, i, j, x.b[j], x.a[i], c.acc[i][j]);
+            for (int r = 0; r < loads; ++r)
+                copy(r);
+#pragma unroll
+            for (int r = 0; r < reads; ++r)
+                read(r);
+            return;
+        }
+#pragma unroll
+        for (int k = 0; k < muls; ++k) {
+#pragma unroll
+            for (int r = share(loads, muls, k); r < share(loads, muls, k + 1); ++r)
+                copy(r);
+#pragma unroll
+            for (int r = share(reads, paced, k); r < share(reads, paced, k + 1); ++r)
+                read(r);
+            const int t = k / (ni * nj), i = Groups::first(I, ga) + k / nj % ni,
+                      j = Groups::first(J, gb) + k % nj;
+            c.acc[i][j] = mul.mul(t, i, j, b[j], a[i], c.acc[i][j]);
             __builtin_amdgcn_sched_barrier(0);
         }
+    };
+    // step s, odd or even
+    const auto step = [&](int s, auto parity) {
+        constexpr int odd = decltype(parity)::value;
+        constexpr int early = Groups::loads(odd, 0), late = Groups::loads(odd, 1);
+        constexpr int b_first = odd, b_second = 1 - odd;
+        mul.next(s);
+        multiply(0, b_first, 4 * Groups::n(J, b_second), [&](int k) { read_b(odd, b_second, k); },
+                 early / 2, [&](int k) { load(s + 2, odd, 0, k); });
+        multiply(0, b_second, 4 * Groups::n(I, 1), [&](int k) { read_a(odd, 1, k); },
+                 early - early / 2, [&](int k) { load(s + 2, odd, 0, early / 2 + k); });
+        wait_reads();
+        wait_loads<early + Groups::loads(1 - odd, 1)>();  // the next step's early rows are there
+        __builtin_amdgcn_s_barrier();
+        mul.read(s + 1);
+        multiply(1, b_second, 4 * Groups::n(I, 0), [&](int k) { read_a(1 - odd, 0, k); },
+                 late / 2, [&](int k) { load(s + 2, odd, 1, k); });
+        multiply(1, b_first, 4 * Groups::n(J, b_second),
+                 [&](int k) { read_b(1 - odd, b_second, k); }, late - late / 2,
+                 [&](int k) { load(s + 2, odd, 1, late / 2 + k); });
+        wait_reads();
+        wait_loads<kLoads>();  // and its late rows
+        __builtin_amdgcn_s_barrier();
     };
 #pragma unroll
     for (int i = 0; i < I; ++i)
@@ -297,39 +374,35 @@ __device__ inline void product(Mul& mul, S& c, const void* P, int64_t pitch_p, i
 #pragma unroll
             for (int r = 0; r < 16; ++r)
                 c.acc[i][j][r] = 0.0f;
-#pragma unroll
-    for (int k = 0; k < 2 * kLoads; ++k)
-        load(k / kLoads, k % kLoads);
     mul.begin();
-    wait_loads();
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) {
+            const int early = Groups::loads(s, 0);
+            load(s, s, k >= early, k < early ? k : k - early);
+        }
+    wait_loads<kLoads>();
     __builtin_amdgcn_s_barrier();
     mul.read(0);
 #pragma unroll
-    for (int k = 0; k < kReads; ++k)
-        read(0, 0, k, x0);
+    for (int k = 0; k < 4 * Groups::n(I, 0); ++k)
+        read_a(0, 0, k);
+#pragma unroll
+    for (int k = 0; k < 4 * Groups::n(J, 0); ++k)
+        read_b(0, 0, k);
+    wait_reads();
+    __builtin_amdgcn_s_barrier();
+    int s = 0;
 #pragma unroll 1
-    for (int s = 0; s < steps; ++s) {
-        mul.next();
-        multiply(x0, [&](int k) {
-#pragma unroll
-            for (int r = share(kReads, k); r < share(kReads, k + 1); ++r)
-                read(s, 1, r, x1);
-        });
-        wait_reads();
-        wait_loads();
-        __builtin_amdgcn_s_barrier();  // the next step is in place, this one's buffer is free
+    for (; s + 2 <= steps; s += 2) {
         mul.copy(s);
-        mul.read(s + 1);
-        multiply(x1, [&](int k) {
-#pragma unroll
-            for (int r = share(kLoads, k); r < share(kLoads, k + 1); ++r)
-                load(s + 2, r);
-#pragma unroll
-            for (int r = share(kReads, k); r < share(kReads, k + 1); ++r)
-                read(s + 1, 0, r, x0);
-        });
+        step(s, std::integral_constant<int, 0>());
+        step(s + 1, std::integral_constant<int, 1>());
     }
-    wait_loads();
+    if (s < steps)
+        step(s, std::integral_constant<int, 0>());
+    wait_loads<0>();
     __builtin_amdgcn_s_barrier();  // nothing is on its way into LDS any more
 }
 
