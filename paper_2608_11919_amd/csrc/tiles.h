@@ -87,9 +87,10 @@ __device__ inline i32x4 read_chunk(const uint8_t* tile, int row32, int c, int la
     return *reinterpret_cast<const i32x4*>(row + at);
 }
 
-// Products of fp16: 64 values a step, in four instructions.
+// Products of fp16: 64 values a step, in four instructions; sums over multiples of 128.
 struct Half {
     static constexpr int kInstructions = 4;
+    static constexpr bool kOddSteps = false;
     __device__ inline void begin() {}
     __device__ inline void copy(int) {}
     __device__ inline void read(int) {}
@@ -180,6 +181,7 @@ typedef Shape<64, 64, 32, 32> Tiny;
 template <typename S>
 struct Fp8 {
     static constexpr int kInstructions = 2;
+    static constexpr bool kOddSteps = true;
     static constexpr int kRowsAll = S::kRows + S::kCols, kLdsBytes = 2 * kRowsAll * 4;
     const uint8_t *scales_p, *scales_q;  // of the tile's first rows, at the first step
     int64_t pitch, limit_p, limit_q;     // bytes of a row's scales; rows that exist
@@ -400,8 +402,9 @@ __device__ inline void product(Mul& mul, S& c, const void* P, int64_t pitch_p, i
         step(s, std::integral_constant<int, 0>());
         step(s + 1, std::integral_constant<int, 1>());
     }
-    if (s < steps)
-        step(s, std::integral_constant<int, 0>());
+    if constexpr (Mul::kOddSteps)
+        if (s < steps)
+            step(s, std::integral_constant<int, 0>());
     wait_loads<0>();
     __builtin_amdgcn_s_barrier();  // nothing is on its way into LDS any more
 }
