@@ -766,8 +766,14 @@ struct Way {
     int slice;   // steps of each
 };
 
-// The largest tile that still leaves every CU a workgroup; where even the smallest does not, the
-// sum is cut as well, into slices of 512 values or more.
+// The largest tile that still leaves every CU a workgroup (2048 x 4096 x 4096: tiles of 128 38 us,
+// of 256 50; 4096 x 4096 x 4096: 76 and 61; 128 x 4096 x 4096: of 64 14, of 128 18).  Where even
+// the smallest does not, a long sum is cut as well, into slices of 512 values or more: with the
+// pass that joins them 64 x 4096 x 4096 takes 18 us, in one piece 13; 64 x 4096 x 8192 17 and 25,
+// 256 x 256 x 16384 21 and 36.
+constexpr int kLongSum = 48;        // steps
+constexpr int64_t kUncutSum = 512;  // values: up to here no workspace is looked at
+
 Way way_of(int64_t m, int64_t n, int64_t k)
 {
     const int steps = int(host::ceil_div(k, kGroup));
@@ -779,6 +785,8 @@ Way way_of(int64_t m, int64_t n, int64_t k)
         if (tiles >= 256)
             return w;
     }
+    if (steps < kLongSum)
+        return w;
     const int words = int(host::ceil_div(steps, 4));
     const int want = int(std::min<int64_t>(words, host::ceil_div(512, std::max<int64_t>(tiles, 1))));
     const int per = int(host::ceil_div(words, std::max(want, 1)));
@@ -1013,8 +1021,8 @@ try {
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const bool f32 = out_dtype == LT_DTYPE_F32;
     const Way w = way_of(m, n, k);
-    const bool few = m <= kFewTokens, cut = k > 0 && !few && w.slices > 1;
-    if (cut) {
+    const bool few = m <= kFewTokens;
+    if (k > kUncutSum && !few) {
         const size_t need = lt_fp8_matmul_workspace_bytes(m, n, k);
         if (!workspace || !host::aligned(workspace, 256) || workspace_bytes < need)
             return fail(LT_ERR_WORKSPACE, "workspace must be 256-byte aligned and hold " +
@@ -1046,7 +1054,7 @@ try {
     }
     ProductArgs g{a_codes, a_scales,   b_codes, b_scales,   m,      n, code_pitch(k),
                   scale_pitch(k), int(host::ceil_div(k, kGroup)), w.slice, out, out_stride, nullptr};
-    if (cut)
+    if (w.slices > 1)
         g.partial = static_cast<float*>(workspace);
     if (w.tile == 256)
         launch_product<Large>(g, w, f32, st);

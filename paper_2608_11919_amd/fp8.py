@@ -91,8 +91,9 @@ def lt_fp8_matmul(a_codes: torch.Tensor, a_scales: torch.Tensor, b_codes: torch.
     device = out.device
     a, sa = _layout(a_codes, a_scales, m, k, device, "a_codes")
     b, sb = _layout(b_codes, b_scales, n, k, device, "b_codes")
-    ws, nbytes = 0, int(lib().lt_fp8_matmul_workspace_bytes(m, n, k))
-    if nbytes > 256 or workspace is not None:
+    ws, nbytes = 0, 0
+    if (m > 32 and k > 512) or workspace is not None:
+        nbytes = int(lib().lt_fp8_matmul_workspace_bytes(m, n, k))
         held = _workspace(device, nbytes, workspace, stream, "fp8")
         ws, nbytes = held.data_ptr(), held.numel() * held.element_size()
     with _current(device):
