@@ -107,8 +107,7 @@ __global__ __launch_bounds__(kQuantizeThreads) void k_fp8_quantize(QuantizeArgs 
     const int64_t r0 = int64_t(blockIdx.x / a.across) * kGroup;
     const int64_t c0 = int64_t(blockIdx.x % a.across) * kGroup;
     const T* x = static_cast<const T*>(a.x);
-    const bool whole = c0 + kGroup <= a.cols &&
-                       (a.stride * int64_t(sizeof(T))) % 16 == 0;  // rows start 16-byte aligned
+    const bool whole = c0 + kGroup <= a.cols;
     float v[2][4][8];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -122,15 +121,15 @@ __global__ __launch_bounds__(kQuantizeThreads) void k_fp8_quantize(QuantizeArgs 
                     v[h][r][e] = 0.0f;
             } else if (whole) {
                 if constexpr (sizeof(T) == 2) {
-                    const i32x4 w = *reinterpret_cast<const i32x4*>(p);
+                    const i32x4 w = load_any(p);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         v[h][r][2 * e] = __uint_as_float(uint32_t(w[e]) << 16);
                         v[h][r][2 * e + 1] = __uint_as_float(uint32_t(w[e]) & 0xFFFF0000u);
                     }
                 } else {
-                    const f32x4 w0 = *reinterpret_cast<const f32x4*>(p);
-                    const f32x4 w1 = *reinterpret_cast<const f32x4*>(p + 4);
+                    const f32x4 w0 = __builtin_bit_cast(f32x4, load_any(p));
+                    const f32x4 w1 = __builtin_bit_cast(f32x4, load_any(p + 4));
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         v[h][r][e] = w0[e];
@@ -269,11 +268,11 @@ __global__ __launch_bounds__(kQuantizeThreads) void k_fp8_quantize_rows(Quantize
     const int64_t col = group * kGroup + 8 * l;
     const T* p = static_cast<const T*>(a.x) + row * a.stride + col;
     float v[8];
-    if (a.stride % int64_t(16 / sizeof(T)) == 0 && col + 8 <= a.cols) {
+    if (col + 8 <= a.cols) {
         constexpr int kLine = 16 / sizeof(T);
 #pragma unroll
         for (int c = 0; c < 8; c += kLine) {
-            const i32x4 w = *reinterpret_cast<const i32x4*>(p + c);
+            const i32x4 w = load_any(p + c);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 if constexpr (sizeof(T) == 2) {
@@ -325,7 +324,6 @@ struct ProductWriter {
     static constexpr int kSlots = 8;
     void* out;
     int64_t stride, rows, cols;  // from the tile's origin on
-    bool narrow;
     __device__ inline void fetch(int, int, int) {}
     __device__ inline void turn(int, int, const float (&)[8]) {}
     __device__ inline void store_one(int row, int col, float v)
@@ -352,14 +350,14 @@ struct ProductWriter {
         const int64_t at = row * stride + col;
         if constexpr (F32) {
             float* p = static_cast<float*>(out) + at;
-            *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
-            *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+            store_any(p, f32x4{v[0], v[1], v[2], v[3]});
+            store_any(p + 4, f32x4{v[4], v[5], v[6], v[7]});
         } else {
             u16x8 b;
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 b[e] = bf16_bits(v[e]);
-            *reinterpret_cast<u16x8*>(static_cast<uint16_t*>(out) + at) = b;
+            store_any(static_cast<uint16_t*>(out) + at, b);
         }
     }
 };
@@ -392,13 +390,11 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_fp8_pro
         p.rows = w.rows;
         p.cols = w.cols;
         p.stride = g.n;
-        p.narrow = g.n % 4 != 0;
         p.out = g.partial + (int64_t(blockIdx.y) * g.m + r0) * g.n + c0;
         finish(tile, lds, p);
         return;
     }
     w.stride = g.stride;
-    w.narrow = g.stride % (F32 ? 4 : 8) != 0;
     w.out = F32 ? static_cast<void*>(static_cast<float*>(g.out) + r0 * g.stride + c0)
                 : static_cast<void*>(static_cast<uint16_t*>(g.out) + r0 * g.stride + c0);
     finish(tile, lds, w);
@@ -459,15 +455,15 @@ struct FewInput {
 };
 
 template <typename T>
-__device__ inline void few_load(const T* row, int64_t k, int s, int q, bool aligned, i32x4* w)
+__device__ inline void few_load(const T* row, int64_t k, int s, int q, i32x4* w)
 {
     const int64_t at = int64_t(s) * kGroup + 32 * q;
     const T* p = row + at;
     constexpr int kWords = int(32 * sizeof(T) / 16);
-    if (aligned && at + 32 <= k) {
+    if (at + 32 <= k) {
 #pragma unroll
         for (int c = 0; c < kWords; ++c)
-            w[c] = reinterpret_cast<const i32x4*>(p)[c];
+            w[c] = load_any(p + c * int(16 / sizeof(T)));
         return;
     }
 #pragma unroll
@@ -544,10 +540,10 @@ __device__ inline void few_input(const FewArgs& g, int64_t token, int s, int q, 
         in.scale = g.x_scales[token * g.scale_pitch + s];
     } else if constexpr (X == kF32) {
         few_load(static_cast<const float*>(g.x) + token * g.x_stride, g.k, s, q,
-                 g.x_stride % 4 == 0, in.w);
+                 in.w);
     } else {
         few_load(static_cast<const uint16_t*>(g.x) + token * g.x_stride, g.k, s, q,
-                 g.x_stride % 8 == 0, in.w);
+                 in.w);
     }
 }
 

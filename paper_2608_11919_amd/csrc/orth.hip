@@ -110,17 +110,17 @@ __device__ inline int find_matrix(const int64_t* __restrict__ prefix, int first,
 __device__ inline float load_value(const float* p) { return *p; }
 __device__ inline float load_value(const uint16_t* p) { return __uint_as_float(uint32_t(*p) << 16); }
 
-// The 16 bytes at p.
+// The values in the 16 bytes at p.
 __device__ inline void load_line(const float* p, float (&x)[4])
 {
-    const f32x4 w = *reinterpret_cast<const f32x4*>(p);
+    const f32x4 w = __builtin_bit_cast(f32x4, load_any(p));
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         x[i] = w[i];
 }
 __device__ inline void load_line(const uint16_t* p, float (&x)[8])
 {
-    const i32x4 w = *reinterpret_cast<const i32x4*>(p);
+    const i32x4 w = load_any(p);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         x[2 * i] = __uint_as_float(uint32_t(w[i]) << 16);
@@ -226,12 +226,11 @@ __global__ __launch_bounds__(kThreads) void k_orth_prepare(Gate gate,
     // a lane has eight values of a row, a wave eight rows
     constexpr int kLine = 16 / sizeof(T);
     const int t = int(threadIdx.x), c = t % 8 * 8;
-    const bool whole = m.cols % kLine == 0;  // rows keep 16-byte pieces aligned
     for (int r = t / 8; r < kPrep; r += kThreads / 8) {
         const int row = r0 + r, col = c0 + c;
         const T* p = src + int64_t(row) * m.cols + col;
         float x[8];
-        if (whole && row < m.rows && col + 8 <= m.cols) {
+        if (row < m.rows && col + 8 <= m.cols) {
 #pragma unroll
             for (int e = 0; e < 8; e += kLine) {
                 float w[kLine];
@@ -302,7 +301,7 @@ struct SymArgs {
 // out = by * sum + at_m * M + at_n * N, in the scales of what is stored.
 template <int OP>
 struct SymWriter {
-    static constexpr bool kTurned = true, narrow = false;
+    static constexpr bool kTurned = true;
     static constexpr int kSlots = 8;
     float by, at_m, at_n, diagonal;
     int64_t pitch;
@@ -312,7 +311,6 @@ struct SymWriter {
     bool mirror;
     half8 x[OP == kGram ? 1 : kSlots], y[OP == kGram || OP == kStep ? 1 : kSlots];
 
-    __device__ inline void store_one(int, int, float) {}
     __device__ inline void fetch(int row, int col, int p)
     {
         if constexpr (OP != kGram)
@@ -423,7 +421,7 @@ struct UpdateWriter {
     static constexpr bool kTurned = FINAL == kAgain;
     static constexpr int kSlots = 8;
     float by, linear, rate, decay;
-    bool applies, narrow;     // narrow: the caller's rows do not keep eight results aligned
+    bool applies;
     const _Float16 *h, *l;    // X at the tile's origin, and X'
     _Float16 *next_h, *next_l, *next_t;
     int64_t pitch, pitch_t;
@@ -442,30 +440,19 @@ struct UpdateWriter {
         if constexpr (FINAL == kWeights) {
             if (row < rows && col < cols) {
                 const float* from = out + int64_t(row) * width + col;
-                const f32x4 a = *reinterpret_cast<const f32x4*>(from);
-                const f32x4 b = *reinterpret_cast<const f32x4*>(from + 4);
+                if (col + 8 <= cols) {
+                    const f32x4 a = __builtin_bit_cast(f32x4, load_any(from));
+                    const f32x4 b = __builtin_bit_cast(f32x4, load_any(from + 4));
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    w[p][e] = a[e], w[p][4 + e] = b[e];
+                    for (int e = 0; e < 4; ++e)
+                        w[p][e] = a[e], w[p][4 + e] = b[e];
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        w[p][e] = col + e < cols ? from[e] : 0.0f;
+                }
             }
         }
-    }
-    __device__ inline void store_one(int row, int col, float v)
-    {
-        if (row >= rows || col >= cols)
-            return;
-        const int64_t at = row * pitch + col, to = int64_t(row) * width + col;
-        if (applies)
-            v = by * v + linear * (float(h[at]) + float(l[at]));
-        v *= 1.0f / kScaleX;
-        if constexpr (FINAL == kWeights) {
-            const float old = out[to];
-            v = applies ? __builtin_fmaf(-rate, v, old * decay) : old;
-        }
-        if (FINAL == kOutF32 || (FINAL == kWeights && applies))
-            out[to] = v;
-        if (FINAL == kOutBf16 || (FINAL == kWeights && out16))
-            out16[to] = bf16_bits(v);
     }
     __device__ inline void store(int row, int col, float (&v)[8], int p)
     {
@@ -494,16 +481,31 @@ struct UpdateWriter {
                 v[e] = applies ? __builtin_fmaf(-rate, v[e], w[p][e] * decay) : w[p][e];
         }
         const int64_t to = int64_t(row) * width + col;
+        const bool whole = col + 8 <= cols;
         if (FINAL == kOutF32 || (FINAL == kWeights && applies)) {
-            *reinterpret_cast<f32x4*>(out + to) = f32x4{v[0], v[1], v[2], v[3]};
-            *reinterpret_cast<f32x4*>(out + to + 4) = f32x4{v[4], v[5], v[6], v[7]};
+            if (whole) {
+                store_any(out + to, f32x4{v[0], v[1], v[2], v[3]});
+                store_any(out + to + 4, f32x4{v[4], v[5], v[6], v[7]});
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (col + e < cols)
+                        out[to + e] = v[e];
+            }
         }
         if (FINAL == kOutBf16 || (FINAL == kWeights && out16)) {
             u16x8 b;
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 b[e] = bf16_bits(v[e]);
-            *reinterpret_cast<u16x8*>(out16 + to) = b;
+            if (whole) {
+                store_any(out16 + to, b);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (col + e < cols)
+                        out16[to + e] = b[e];
+            }
         }
     }
     __device__ inline void turn(int col, int row, const float (&v)[8]) const
@@ -563,7 +565,6 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_orth_up
     out.rate = m.rate;
     out.decay = args.decay;
     out.applies = applies;
-    out.narrow = FINAL != kAgain && m.cols % 8 != 0;
     const int64_t at = int64_t(r0) * m.cp + c0, to = int64_t(r0) * m.cols + c0;
     out.h = m.h[from] + at;
     out.l = m.l[from] + at;

@@ -22,6 +22,18 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
+// 16 bytes wherever an element may begin: rows of any length are read and written in them (the
+// hardware takes global accesses at any address).
+typedef int i32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+
+__device__ inline i32x4 load_any(const void* p) { return *static_cast<const i32x4_any*>(p); }
+
+template <typename V>
+__device__ inline void store_any(void* p, const V& v)
+{
+    *static_cast<i32x4_any*>(p) = __builtin_bit_cast(i32x4, v);
+}
+
 constexpr int kStepBytes = 128;  // of every row, per step of the main loop
 
 #define LT_GLOBAL __attribute__((address_space(1)))
@@ -417,8 +429,6 @@ __device__ inline void product(Mul& mul, S& c, const void* P, int64_t pitch_p, i
 //   w.fetch(row, col, p)     requests what results [row][col .. col + 8) need, into slot p;
 //   w.store(row, col, v, p)  takes the sums v, leaves the results there and stores them;
 //   w.turn(col, row, v)      with kTurned: stores results [row .. row + 8)[col] of the transpose;
-//   w.narrow                 true: results go one by one, w.store_one(row, col, sum), a wave's
-//                            lanes side by side (rows that do not keep eight results aligned).
 // Rows and columns count from the tile's origin.
 template <typename S, typename Writer>
 __device__ inline void finish(const S& c, uint8_t* lds, Writer& w)
@@ -432,11 +442,9 @@ __device__ inline void finish(const S& c, uint8_t* lds, Writer& w)
     const int r0 = S::wave_row(), c0 = S::wave_col();
 #pragma unroll
     for (int i = 0; i < S::I; ++i) {
-        if (!w.narrow) {
 #pragma unroll
-            for (int p = 0; p < kPasses; ++p)
-                w.fetch(r0 + 32 * i + p * kDown + down, c0 + across, p);
-        }
+        for (int p = 0; p < kPasses; ++p)
+            w.fetch(r0 + 32 * i + p * kDown + down, c0 + across, p);
 #pragma unroll
         for (int jg = 0; jg < 4 * S::J; ++jg) {
             const int j = jg / 4, g = jg % 4;
@@ -446,13 +454,6 @@ __device__ inline void finish(const S& c, uint8_t* lds, Writer& w)
                       c.acc[i][j][4 * g + 3]};
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (w.narrow) {
-#pragma unroll 8
-            for (int e = lane; e < 32 * W; e += 64)
-                w.store_one(r0 + 32 * i + e / W, c0 + e % W, mine[e / W * kPitch + e % W]);
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            continue;
-        }
 #pragma unroll
         for (int p = 0; p < kPasses; ++p) {
             float* at = mine + (p * kDown + down) * kPitch + across;
