@@ -600,6 +600,7 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_orth_up
 // rate, and the steps one after the other.
 
 constexpr int kThinThreads = 512, kThinWaves = kThinThreads / 64;
+constexpr int kThinSpan = 16 * kThinWaves;  // columns that a workgroup's waves multiply at a time
 constexpr int kThinSide = 32;
 constexpr int64_t kThinElems = int64_t(1) << 17;
 
@@ -670,10 +671,11 @@ __device__ inline void thin_product32(Thin<32>::Sym& dst, const Thin<32>::Sym& M
     __syncthreads();
 }
 
-// Columns [k0, k0 + kWidth) of X, zeros outside it, into LDS, 32 reads of a lane under way at a
+// Columns [k0, k0 + kWidth) of X, zeros from column `end` on, into LDS, 32 reads of a lane under way at a
 // time.  Rows of X lie along its memory where it is wide, columns where it is tall.
 template <int NP, typename T>
-__device__ inline void thin_load(Thin<NP>& t, const Matrix& m, bool wide, int k0)
+__device__ inline void thin_load(Thin<NP>& t, const Matrix& m, bool wide, int k0,
+                                 int end)
 {
     constexpr int W = Thin<NP>::kWidth, kAhead = 32, kAll = NP * W / kThinThreads;
     constexpr int kPasses = W > kThinThreads ? W / kThinThreads : 1;  // of a row, where wide
@@ -688,7 +690,7 @@ __device__ inline void thin_load(Thin<NP>& t, const Matrix& m, bool wide, int k0
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 const int i = (first + u) / kPasses, k = (first + u) % kPasses * kThinThreads + tid;
-                v[u] = i < n && k0 + k < len ? load_value(src + i * len + k0 + k) : 0.0f;
+                v[u] = i < n && k0 + k < end ? load_value(src + i * len + k0 + k) : 0.0f;
             }
 #pragma unroll
             for (int u = 0; u < kAhead; ++u)
@@ -698,7 +700,7 @@ __device__ inline void thin_load(Thin<NP>& t, const Matrix& m, bool wide, int k0
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 const int k = tid / NP + kThinThreads / NP * (first + u);
-                v[u] = i < n && k0 + k < len ? load_value(src + (k0 + k) * n + i) : 0.0f;
+                v[u] = i < n && k0 + k < end ? load_value(src + (k0 + k) * n + i) : 0.0f;
             }
 #pragma unroll
             for (int u = 0; u < kAhead; ++u)
@@ -708,8 +710,49 @@ __device__ inline void thin_load(Thin<NP>& t, const Matrix& m, bool wide, int k0
     __syncthreads();
 }
 
+// Element `to` of the result, or of the weights.
+template <int FINAL>
+__device__ inline void thin_store(const Matrix& m, int to, float o, float decay)
+{
+    if constexpr (FINAL == kOutF32) {
+        static_cast<float*>(m.out)[to] = o;
+    } else if constexpr (FINAL == kOutBf16) {
+        static_cast<uint16_t*>(m.out)[to] = bf16_bits(o);
+    } else {
+        const float v = __builtin_fmaf(-m.rate, o, m.w[to] * decay);
+        m.w[to] = v;
+        if (m.wb)
+            m.wb[to] = bf16_bits(v);
+    }
+}
+
+// The same for elements to .. to + 3.
+template <int FINAL>
+__device__ inline void thin_store4(const Matrix& m, int to, f32x4 o, float decay)
+{
+    typedef uint16_t u16x4_any __attribute__((ext_vector_type(4), aligned(2)));
+    const auto narrow = [](const f32x4& v) {
+        return u16x4_any{bf16_bits(v[0]), bf16_bits(v[1]), bf16_bits(v[2]), bf16_bits(v[3])};
+    };
+    if constexpr (FINAL == kOutF32) {
+        store_any(static_cast<float*>(m.out) + to, o);
+    } else if constexpr (FINAL == kOutBf16) {
+        *reinterpret_cast<u16x4_any*>(static_cast<uint16_t*>(m.out) + to) = narrow(o);
+    } else {
+        const f32x4 w = __builtin_bit_cast(f32x4, load_any(m.w + to));
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            o[e] = __builtin_fmaf(-m.rate, o[e], w[e] * decay);
+        store_any(m.w + to, o);
+        if (m.wb)
+            *reinterpret_cast<u16x4_any*>(m.wb + to) = narrow(o);
+    }
+}
+
+// Columns [begin, end) of the result, by one workgroup.
 template <int NP, typename T, int FINAL>
-__device__ inline void thin_matrix(Thin<NP>& t, const Matrix& m, int steps, float decay)
+__device__ inline void thin_matrix(Thin<NP>& t, const Matrix& m, int steps, float decay, int begin,
+                                   int end)
 {
     constexpr int W = Thin<NP>::kWidth, kBlocks = Thin<NP>::kBlocks;
     const bool wide = m.rows <= m.cols;
@@ -722,7 +765,7 @@ __device__ inline void thin_matrix(Thin<NP>& t, const Matrix& m, int steps, floa
     for (int k0 = 0; k0 < len; k0 += W) {
         if (k0 > 0)
             __syncthreads();
-        thin_load<NP, T>(t, m, wide, k0);
+        thin_load<NP, T>(t, m, wide, k0, len);
         for (int k = 16 * wave; k < W && k0 + k < len; k += 16 * kThinWaves) {
             f32x4 x[kBlocks];
 #pragma unroll
@@ -828,7 +871,7 @@ __device__ inline void thin_matrix(Thin<NP>& t, const Matrix& m, int steps, floa
         __syncthreads();
     }
 
-    // R X, blocks of 16 columns in turn
+    // R X over the workgroup's columns, blocks of 16 in turn
     const float p0 = t.power[0], p1 = t.power[1];
     f32x4 a[kBlocks][kBlocks];
 #pragma unroll
@@ -836,55 +879,41 @@ __device__ inline void thin_matrix(Thin<NP>& t, const Matrix& m, int steps, floa
 #pragma unroll
         for (int bk = 0; bk < kBlocks; ++bk)
             a[bi][bk] = *reinterpret_cast<const f32x4*>(&t.r[16 * bi + r][16 * bk + 4 * q]);
-    for (int k0 = 0; k0 < len; k0 += W) {
+    for (int k0 = begin; k0 < end; k0 += W) {
+        const int base = len <= W ? 0 : k0;  // column of X at the head of what LDS holds
         if (len > W) {
             __syncthreads();
-            thin_load<NP, T>(t, m, wide, k0);
+            thin_load<NP, T>(t, m, wide, k0, end);
         }
-        for (int k = 16 * wave; k < W && k0 + k < len; k += 16 * kThinWaves) {
-            const int col = k0 + k + r;
-            float w[kBlocks][4] = {};
-            if constexpr (FINAL == kWeights) {
-#pragma unroll
-                for (int bi = 0; bi < kBlocks; ++bi)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int i = 16 * bi + 4 * q + e;
-                        if (i < n && col < len)
-                            w[bi][e] = m.w[wide ? i * len + col : col * n + i];
-                    }
-            }
+        const int stop = min(end, k0 + W);
+        for (int k = k0 + 16 * wave; k < stop; k += 16 * kThinWaves) {
+            const int col = k + r;
             f32x4 acc[kBlocks] = {};
 #pragma unroll
             for (int bk = 0; bk < kBlocks; ++bk)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float x = t.x[16 * bk + 4 * q + e][k + r] * p0 * p1;
+                    const float x = t.x[16 * bk + 4 * q + e][k - base + r] * p0 * p1;
 #pragma unroll
                     for (int bi = 0; bi < kBlocks; ++bi)
                         acc[bi] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[bi][bk][e], x, acc[bi], 0,
                                                                        0, 0);
                 }
+            if (col >= len)
+                continue;
 #pragma unroll
-            for (int bi = 0; bi < kBlocks; ++bi)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int i = 16 * bi + 4 * q + e;
-                    if (i >= n || col >= len)
-                        continue;
-                    const int to = wide ? i * len + col : col * n + i;
-                    const float o = acc[bi][e];
-                    if constexpr (FINAL == kOutF32) {
-                        static_cast<float*>(m.out)[to] = o;
-                    } else if constexpr (FINAL == kOutBf16) {
-                        static_cast<uint16_t*>(m.out)[to] = bf16_bits(o);
-                    } else {
-                        const float v = __builtin_fmaf(-m.rate, o, w[bi][e] * decay);
-                        m.w[to] = v;
-                        if (m.wb)
-                            m.wb[to] = bf16_bits(v);
-                    }
+            for (int bi = 0; bi < kBlocks; ++bi) {
+                const int i = 16 * bi + 4 * q;
+                if (!wide && i + 4 <= n) {  // four neighbours in memory
+                    thin_store4<FINAL>(m, col * n + i, acc[bi], decay);
+                    continue;
                 }
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (i + e < n)
+                        thin_store<FINAL>(m, wide ? (i + e) * len + col : col * n + i + e,
+                                          acc[bi][e], decay);
+            }
         }
     }
 }
@@ -892,7 +921,8 @@ __device__ inline void thin_matrix(Thin<NP>& t, const Matrix& m, int steps, floa
 template <typename T, int FINAL>
 __global__ __launch_bounds__(kThinThreads) void k_orth_thin(Gate gate,
                                                             const Matrix* __restrict__ mats,
-                                                            int first, int steps, float decay)
+                                                            int first, int n, int parts, int steps,
+                                                            float decay)
 {
     __shared__ union {
         Thin<16> t16;
@@ -900,20 +930,25 @@ __global__ __launch_bounds__(kThinThreads) void k_orth_thin(Gate gate,
     } lds;
     if (!descriptors_ok(gate))
         return;
-    const Matrix& m = mats[first + blockIdx.x];
-    const int numel = m.rows * m.cols;
+    const Matrix& m = mats[first + blockIdx.x % uint32_t(n)];
+    const int part = int(blockIdx.x / uint32_t(n));
+    const int numel = m.rows * m.cols, len = max(m.rows, m.cols);
     if (numel == 0)
         return;
     if (!step_applies(gate)) {
-        if (FINAL == kWeights && m.wb)
+        if (FINAL == kWeights && m.wb && part == 0)
             for (int e = threadIdx.x; e < numel; e += kThinThreads)
                 m.wb[e] = bf16_bits(m.w[e]);
         return;
     }
+    const int span = ((len + parts - 1) / parts + kThinSpan - 1) / kThinSpan * kThinSpan;
+    const int begin = part * span, end = min(len, begin + span);
+    if (begin >= len)
+        return;
     if (m.rows <= 16 || m.cols <= 16)
-        thin_matrix<16, T, FINAL>(lds.t16, m, steps, decay);
+        thin_matrix<16, T, FINAL>(lds.t16, m, steps, decay, begin, end);
     else
-        thin_matrix<32, T, FINAL>(lds.t32, m, steps, decay);
+        thin_matrix<32, T, FINAL>(lds.t32, m, steps, decay, begin, end);
 }
 
 // ---------------------------------------------------------------- host side
@@ -1099,14 +1134,22 @@ struct Launch {
     }
 };
 
-void launch_thin(const Gate& gate, const Matrix* mats, int first, int n, const Call& c, float decay)
+// A few thin matrices leave CUs idle: several workgroups take one, all of them its Gram matrix and
+// steps, each its columns of the result.  Eight of 16 x 2048 take 14 us so, 19 by one workgroup
+// each (of 2048 x 16 15 and 27, of 32 x 2048 36 and 50); 256 of them 26 either way.
+constexpr int kThinParts = 16;
+
+void launch_thin(const Gate& gate, const Matrix* mats, int first, int n, const Call& c, int cus,
+                 float decay)
 {
+    const int parts = std::min(std::max(cus / n, 1), kThinParts);
     const bool wide_src = c.muon || c.in_dtype == LT_DTYPE_F32;
     auto* kernel = c.muon ? k_orth_thin<float, kWeights>
                    : c.out_dtype == LT_DTYPE_F32
                        ? (wide_src ? k_orth_thin<float, kOutF32> : k_orth_thin<uint16_t, kOutF32>)
                        : (wide_src ? k_orth_thin<float, kOutBf16> : k_orth_thin<uint16_t, kOutBf16>);
-    kernel<<<dim3(uint32_t(n)), kThinThreads, 0, c.st>>>(gate, mats, first, c.ns_steps, decay);
+    kernel<<<dim3(uint32_t(n * parts)), kThinThreads, 0, c.st>>>(gate, mats, first, n, parts,
+                                                                 c.ns_steps, decay);
 }
 
 // A second stream of the library's own, for the batches of single steps beside those of pairs:
@@ -1263,7 +1306,7 @@ lt_err run_batches(const Call& c, float decay, Fill fill, Begin begin)
                                  pre[kPreUnits][first], blocks(kPreUnits), st))
                 return e;
         if (thin) {
-            launch_thin(gate, d_mats, first, n, c, decay);
+            launch_thin(gate, d_mats, first, n, c, cus, decay);
             LT_TRY_HIP(hipGetLastError());
             continue;
         }
