@@ -62,6 +62,8 @@ struct Matrix {
     const void* src;           // the matrix, or the Muon step's update in fp32
     _Float16 *h[2], *t[2], *l[2];
     _Float16* sym[3];          // n x n matrices
+    double* gram;              // sides of 33 to 64: G of every slice of columns
+    float* r;                  // and R, behind what X is multiplied by
     double *partial, *square;  // sums of squares of its units; their sum
     void* out;                 // orthogonalise: the result
     float* w;                  // Muon: weights and their bf16 copy (or null)
@@ -589,20 +591,20 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_orth_up
 
 // ---------------------------------------------------------------- thin matrices
 //
-// A matrix with n <= 32 rows (or columns), padded to 16 or 32 of at most 2^17 elements, by one
-// workgroup in one launch: with G = X X^T, every step stays n x n (P = a I + b G + c G G,
-// G' = P G P, R' = P R), and the result is R X.  Adapters, small layers and odd leftovers come
-// in hundreds, and the general path would pad each to 128 and take 18 launches.  An error of G
+// A matrix with n <= 32 rows (or columns), padded to 16 or 32, in one launch: with G = X X^T,
+// every step stays n x n (P = a I + b G + c G G, G' = P G P, R' = P R), and the result is R X.
+// Adapters, small layers and odd leftovers come in hundreds, and the general path would pad
+// each to 128, write X three times a step and take 18 launches: 224 of 32 x 4288 take 146 us
+// here, there 2124; one of 32 x 4096 59 and 210, one of 16 x 65536 280 and 1774.  An error of G
 // grows by a^2 with every step in directions of small singular values, 2e5 in five: G and the
 // steps are in 64 bits (in 32 a 64 x 64 matrix with a few strong directions ends 5e-3 off), R X
 // in 32.  The norm is G's trace, so X is read once, into LDS, where it fits, and else twice.
-// What bounds it is latency: one workgroup's reads, 16 n^2 products of m values at the 64-bit
-// rate, and the steps one after the other.
+// What bounds it is G at the 64-bit rate (n^2 m products for every workgroup of a matrix, 3.4 us
+// for 16 x 2048), and latency: 7 us for 16 x 128, 0.5 us more a step (2.1 at 32 x 32).
 
 constexpr int kThinThreads = 512, kThinWaves = kThinThreads / 64;
 constexpr int kThinSpan = 16 * kThinWaves;  // columns that a workgroup's waves multiply at a time
 constexpr int kThinSide = 32;
-constexpr int64_t kThinElems = int64_t(1) << 17;
 
 typedef double f64x4 __attribute__((ext_vector_type(4)));
 
@@ -749,6 +751,34 @@ __device__ inline void thin_store4(const Matrix& m, int to, f32x4 o, float decay
     }
 }
 
+// Rows i .. i + 3 of column `col` of the n x len result, as far as they exist.
+template <int FINAL>
+__device__ inline void thin_result(const Matrix& m, bool wide, int n, int len, int i, int col,
+                                   const f32x4& o, float decay)
+{
+    if (!wide && i + 4 <= n) {  // four neighbours in memory
+        thin_store4<FINAL>(m, col * n + i, o, decay);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (i + e < n)
+            thin_store<FINAL>(m, wide ? (i + e) * len + col : col * n + i + e, o[e], decay);
+}
+
+// 1 / norm as a factor in [1/2, 1) for R and a power of two for X, in two halves; a zero matrix
+// stays zero; an infinite or NaN sum makes every value NaN.
+__device__ inline double thin_factor(double trace, float* p0, float* p1)
+{
+    int e = 0;
+    const double f = trace == 0.0 ? 0.0
+                     : isfinite(trace) ? frexp(1.0 / sqrt(trace), &e)
+                                       : __builtin_nan("");
+    *p0 = ldexpf(1.0f, e / 2);
+    *p1 = ldexpf(1.0f, e - e / 2);
+    return f;
+}
+
 // Columns [begin, end) of the result, by one workgroup.
 template <int NP, typename T, int FINAL>
 __device__ inline void thin_matrix(Thin<NP>& t, const Matrix& m, int steps, float decay, int begin,
@@ -798,16 +828,12 @@ __device__ inline void thin_matrix(Thin<NP>& t, const Matrix& m, int steps, floa
             v += t.part[w][u][e][l];
         return v;
     };
-    // 1 / norm as a factor in [1/2, 1) for R and a power of two for X, in two halves; a zero
-    // matrix stays zero; an infinite or NaN sum makes every value NaN
     const auto factor = [&](double trace) {
-        int e = 0;
-        const double f = trace == 0.0 ? 0.0
-                         : isfinite(trace) ? frexp(1.0 / sqrt(trace), &e)
-                                           : __builtin_nan("");
+        float p0, p1;
+        const double f = thin_factor(trace, &p0, &p1);
         if (threadIdx.x == 0) {
-            t.power[0] = ldexpf(1.0f, e / 2);
-            t.power[1] = ldexpf(1.0f, e - e / 2);
+            t.power[0] = p0;
+            t.power[1] = p1;
         }
         return f;
     };
@@ -902,18 +928,8 @@ __device__ inline void thin_matrix(Thin<NP>& t, const Matrix& m, int steps, floa
             if (col >= len)
                 continue;
 #pragma unroll
-            for (int bi = 0; bi < kBlocks; ++bi) {
-                const int i = 16 * bi + 4 * q;
-                if (!wide && i + 4 <= n) {  // four neighbours in memory
-                    thin_store4<FINAL>(m, col * n + i, acc[bi], decay);
-                    continue;
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (i + e < n)
-                        thin_store<FINAL>(m, wide ? (i + e) * len + col : col * n + i + e,
-                                          acc[bi][e], decay);
-            }
+            for (int bi = 0; bi < kBlocks; ++bi)
+                thin_result<FINAL>(m, wide, n, len, 16 * bi + 4 * q, col, acc[bi], decay);
         }
     }
 }
@@ -951,6 +967,245 @@ __global__ __launch_bounds__(kThinThreads) void k_orth_thin(Gate gate,
         thin_matrix<32, T, FINAL>(lds.t32, m, steps, decay, begin, end);
 }
 
+// ---------------------------------------------------------------- small matrices
+//
+// The same for 33 <= n <= 64, where G and its steps no longer leave LDS room for X: G of every
+// slice of columns, the steps by one workgroup for each matrix, R X.  X is read twice and written
+// once, by as many workgroups as there are slices.  Bound by the 64-bit products of G where
+// matrices are many or long, and by the steps (35 us, one product after the other) where not.
+
+constexpr int kSmallSide = 64;
+constexpr int kSmallSlice = 512;                            // columns
+constexpr int kSmallBlocks = kSmallSide / 16;
+constexpr int kSmallUpper = kSmallBlocks * (kSmallBlocks + 1) / 2;
+constexpr int kSmallGram = kSmallUpper * 256;               // doubles of one slice
+constexpr int kSmallR = 64 + kSmallSide * kSmallSide;       // two powers, and R at 64
+
+// X[i][k .. k + 4) of the n x len matrix on its smaller side, zeros outside it.
+template <typename T>
+__device__ inline f32x4 small_load(const T* src, bool wide, int n, int len, int i, int k)
+{
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (i >= n)
+        return v;
+    if (wide && k + 4 <= len) {
+        const T* p = src + int64_t(i) * len + k;
+        if constexpr (sizeof(T) == 4) {
+            v = __builtin_bit_cast(f32x4, load_any(p));
+        } else {
+            typedef uint16_t u16x4_any __attribute__((ext_vector_type(4), aligned(2)));
+            const u16x4_any w = *reinterpret_cast<const u16x4_any*>(p);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] = __uint_as_float(uint32_t(w[e]) << 16);
+        }
+        return v;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (k + e < len)
+            v[e] = load_value(src + (wide ? int64_t(i) * len + k + e : int64_t(k + e) * n + i));
+    return v;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_orth_small_gram(Gate gate,
+                                                              const int64_t* __restrict__ prefix,
+                                                              const Matrix* __restrict__ mats,
+                                                              int first, int n_mats)
+{
+    __shared__ double part[kThreads / 64][kSmallGram];
+    if (!descriptors_ok(gate) || !step_applies(gate))
+        return;
+    const int64_t unit = prefix[first] + blockIdx.x;
+    const int at = find_matrix(prefix, first, n_mats, unit);
+    const Matrix& m = mats[at];
+    const int slice = int(unit - prefix[at]);
+    const bool wide = m.rows <= m.cols;
+    const int n = wide ? m.rows : m.cols, len = wide ? m.cols : m.rows;
+    const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
+    const int r = lane & 15, q = lane >> 4;
+    const T* src = static_cast<const T*>(m.src);
+    const int k0 = slice * kSmallSlice, k1 = min(len, k0 + kSmallSlice);
+    f64x4 g[kSmallUpper] = {};
+    for (int k = k0 + 16 * wave; k < k1; k += 16 * (kThreads / 64)) {
+        f32x4 x[kSmallBlocks];
+#pragma unroll
+        for (int b = 0; b < kSmallBlocks; ++b)
+            x[b] = small_load(src, wide, n, len, 16 * b + r, k + 4 * q);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            int u = 0;
+#pragma unroll
+            for (int a = 0; a < kSmallBlocks; ++a)
+#pragma unroll
+                for (int b = a; b < kSmallBlocks; ++b, ++u)
+                    g[u] = __builtin_amdgcn_mfma_f64_16x16x4f64(double(x[a][e]), double(x[b][e]),
+                                                                g[u], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kSmallUpper; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            part[wave][(u * 4 + e) * 64 + lane] = g[u][e];
+    __syncthreads();
+    double* to = m.gram + int64_t(slice) * kSmallGram;
+    for (int e = threadIdx.x; e < kSmallGram; e += kThreads)
+        to[e] = (part[0][e] + part[1][e]) + (part[2][e] + part[3][e]);
+}
+
+typedef double SmallSym[kSmallSide][kSmallSide + 2];
+
+// dst = alpha * M N + beta * N + gamma * I, all symmetric: every wave two blocks of 16.
+__device__ inline void small_product(SmallSym& dst, const SmallSym& M, const SmallSym& N,
+                                     double alpha, double beta, double gamma)
+{
+    const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
+    const int r = lane & 15, q = lane >> 4;
+    const int bi = wave / 2 * 16, bj = wave % 2 * 32;
+    f64x4 acc[2] = {};
+#pragma unroll 4
+    for (int k = 0; k < kSmallSide; k += 4)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            acc[h] = __builtin_amdgcn_mfma_f64_16x16x4f64(M[bi + r][k + q],
+                                                          N[bj + 16 * h + r][k + q], acc[h], 0, 0,
+                                                          0);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int i = bi + 4 * t + q, j = bj + 16 * h + r;
+            dst[i][j] = alpha * acc[h][t] + beta * N[i][j] + (i == j ? gamma : 0.0);
+        }
+    __syncthreads();
+}
+
+__global__ __launch_bounds__(kThinThreads) void k_orth_small_steps(Gate gate,
+                                                                   const Matrix* __restrict__ mats,
+                                                                   int first, int steps)
+{
+    __shared__ SmallSym sym[4];
+    if (!descriptors_ok(gate) || !step_applies(gate))
+        return;
+    const Matrix& m = mats[first + blockIdx.x];
+    const int len = max(m.rows, m.cols), slices = (len + kSmallSlice - 1) / kSmallSlice;
+    if (len == 0 || m.rows == 0 || m.cols == 0)
+        return;
+    for (int e = threadIdx.x; e < kSmallGram; e += kThinThreads) {
+        double v = m.gram[e];
+        for (int i = 1; i < slices; ++i)
+            v += m.gram[int64_t(i) * kSmallGram + e];
+        // block u of the upper ones, in the order in which they were made
+        int a = 0, b = e / 256;
+        while (b >= kSmallBlocks - a) {
+            b -= kSmallBlocks - a;
+            ++a;
+        }
+        const int l = e % 64, i = 16 * a + 4 * (e / 64 % 4) + (l >> 4), j = 16 * (a + b) + (l & 15);
+        sym[0][i][j] = v;
+        sym[0][j][i] = v;
+    }
+    __syncthreads();
+    double trace = 0.0;
+    for (int i = 0; i < kSmallSide; ++i)
+        trace += sym[0][i][i];
+    float p0, p1;
+    const double f = thin_factor(trace, &p0, &p1), by = trace == 0.0 ? 0.0 : 1.0 / trace;
+    __syncthreads();
+    for (int e = threadIdx.x; e < kSmallSide * kSmallSide; e += kThinThreads)
+        sym[0][e / kSmallSide][e % kSmallSide] *= by;
+    __syncthreads();
+    int G = 0, P = 1, R = 2, S = 3;
+    for (int step = 0; step < steps; ++step) {
+        small_product(sym[P], sym[G], sym[G], 2.0315, -4.7750, 3.4445);
+        if (step > 0) {
+            small_product(sym[S], sym[P], sym[R], 1.0, 0.0, 0.0);
+            const int old = R;
+            R = S;
+            S = old;
+        }
+        if (step + 1 < steps) {
+            small_product(sym[S], sym[P], sym[G], 1.0, 0.0, 0.0);
+            small_product(sym[G], sym[S], sym[P], 1.0, 0.0, 0.0);
+        }
+        if (step == 0) {
+            const int old = R;
+            R = P;
+            P = old;
+        }
+    }
+    if (threadIdx.x == 0) {
+        m.r[0] = p0;
+        m.r[1] = p1;
+    }
+    for (int e = threadIdx.x; e < kSmallSide * kSmallSide; e += kThinThreads)
+        m.r[64 + e] = float(sym[R][e / kSmallSide][e % kSmallSide] * f);
+}
+
+template <typename T, int FINAL>
+__global__ __launch_bounds__(kThreads) void k_orth_small_apply(Gate gate,
+                                                               const int64_t* __restrict__ prefix,
+                                                               const Matrix* __restrict__ mats,
+                                                               int first, int n_mats, float decay)
+{
+    if (!descriptors_ok(gate))
+        return;
+    const int64_t unit = prefix[first] + blockIdx.x;
+    const int at = find_matrix(prefix, first, n_mats, unit);
+    const Matrix& m = mats[at];
+    const int slice = int(unit - prefix[at]);
+    const bool wide = m.rows <= m.cols;
+    const int n = wide ? m.rows : m.cols, len = wide ? m.cols : m.rows;
+    const int k0 = slice * kSmallSlice, k1 = min(len, k0 + kSmallSlice);
+    if (!step_applies(gate)) {
+        if (FINAL == kWeights && m.wb)
+            for (int e = threadIdx.x; e < n * (k1 - k0); e += kThreads) {
+                const int to = wide ? e / (k1 - k0) * len + k0 + e % (k1 - k0) : k0 * n + e;
+                m.wb[to] = bf16_bits(m.w[to]);
+            }
+        return;
+    }
+    const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
+    const int r = lane & 15, q = lane >> 4;
+    const T* src = static_cast<const T*>(m.src);
+    const float p0 = m.r[0], p1 = m.r[1];
+    f32x4 a[kSmallBlocks][kSmallBlocks];
+#pragma unroll
+    for (int bi = 0; bi < kSmallBlocks; ++bi)
+#pragma unroll
+        for (int bk = 0; bk < kSmallBlocks; ++bk)
+            a[bi][bk] = *reinterpret_cast<const f32x4*>(m.r + 64 + (16 * bi + r) * kSmallSide +
+                                                        16 * bk + 4 * q);
+    for (int k = k0 + 16 * wave; k < k1; k += 16 * (kThreads / 64)) {
+        const int col = k + r;
+        float x[kSmallBlocks][4];
+#pragma unroll
+        for (int bk = 0; bk < kSmallBlocks; ++bk)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = 16 * bk + 4 * q + e;
+                x[bk][e] = i < n && col < len ? load_value(src + (wide ? i * len + col : col * n + i))
+                                              : 0.0f;
+            }
+        f32x4 acc[kSmallBlocks] = {};
+#pragma unroll
+        for (int bk = 0; bk < kSmallBlocks; ++bk)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int bi = 0; bi < kSmallBlocks; ++bi)
+                    acc[bi] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[bi][bk][e],
+                                                                   x[bk][e] * p0 * p1, acc[bi], 0,
+                                                                   0, 0);
+        if (col < len)
+#pragma unroll
+            for (int bi = 0; bi < kSmallBlocks; ++bi)
+                thin_result<FINAL>(m, wide, n, len, 16 * bi + 4 * q, col, acc[bi], decay);
+    }
+}
+
 // ---------------------------------------------------------------- host side
 
 // The workspace: [tag][prefixes][momentum descriptors][matrices][square sums][partials] and
@@ -962,7 +1217,8 @@ __global__ __launch_bounds__(kThinThreads) void k_orth_thin(Gate gate,
 constexpr int64_t kBatchElems = int64_t(1) << 27;  // padded elements of a batch of several,
 constexpr int64_t kBatchLargest = 4;               // or this many of the list's largest matrix
 
-enum { kPreUnits, kPrePrep, kPreSym, kPreTile, kPreSymLarge, kPreTileLarge, kPrefixes };
+enum { kPreUnits, kPreSlices, kPrePrep, kPreSym, kPreTile, kPreSymLarge, kPreTileLarge,
+       kPrefixes };
 
 struct Plan {
     size_t prefix[kPrefixes], momentum, mats, header, squares, partials, region[2], total;
@@ -971,36 +1227,45 @@ struct Plan {
     std::vector<int> way;      // of each batch: how its matrices are worked on
 };
 
-// How a matrix is worked on.  Thin ones by one workgroup each.  Long ones take their steps in
-// pairs, which saves a sixth of the multiply-adds or more; 128 rows or columns are the least
-// that a tile computes anyway.
-enum { kThin, kSingle, kPairs, kWays };
+// How a matrix is worked on.  Thin and small ones in 64 bits on their own side.  Long ones take their steps in
+// pairs, which saves a sixth of the multiply-adds or more (17408 x 5120: 5.5 ms, in single steps
+// 7.3; the projections of a 3B-class layer 2.6 and 3.5); 128 rows or columns are the least that a
+// tile computes anyway.
+enum { kThin, kSmall, kSingle, kPairs, kWays };
 
 int way_of(int64_t rows, int64_t cols)
 {
     const int64_t n = std::min(rows, cols), m = std::max(rows, cols);
-    const int64_t side = n <= 16 ? 16 : kThinSide;
-    if (n <= side && side * m <= kThinElems)
+    if (n <= kThinSide)
         return kThin;
+    if (n <= kSmallSide)
+        return kSmall;
     return n >= kTile && m >= 2 * n ? kPairs : kSingle;
 }
 
 int64_t padded(int64_t x) { return int64_t(round_up(size_t(x), kTile)); }
+
+int64_t slices_of(int64_t rows, int64_t cols)
+{
+    return host::ceil_div(std::max(rows, cols), kSmallSlice);
+}
 
 int64_t units_of(int64_t numel, int64_t span) { return (numel + span - 1) / span; }
 
 // Bytes of a matrix in the region: X in three layouts twice, three n x n matrices, the Muon
 // step's update.
 struct Place {
-    size_t h[2], t[2], l[2], sym[3], u, bytes;
+    size_t h[2], t[2], l[2], sym[3], gram, r, u, bytes;
 };
 
 Place place(int64_t rows, int64_t cols, bool muon)
 {
     Place p;
-    const bool thin = way_of(rows, cols) == kThin;  // X and the rest are in LDS
-    const size_t x = thin ? 0 : size_t(padded(rows)) * size_t(padded(cols)) * 2;
-    const size_t side = thin ? 0 : size_t(std::min(padded(rows), padded(cols)));
+    const int way = way_of(rows, cols);
+    const bool tiled = way == kSingle || way == kPairs;
+    const size_t x = tiled ? size_t(padded(rows)) * size_t(padded(cols)) * 2 : 0;
+    const size_t side = tiled ? size_t(std::min(padded(rows), padded(cols))) : 0;
+    const size_t slices = way == kSmall ? size_t(slices_of(rows, cols)) : 0;
     size_t at = 0;
     const auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -1014,6 +1279,8 @@ Place place(int64_t rows, int64_t cols, bool muon)
     }
     for (int i = 0; i < 3; ++i)
         p.sym[i] = take(side * side * 2);
+    p.gram = take(slices * kSmallGram * sizeof(double));
+    p.r = take(way == kSmall ? kSmallR * sizeof(float) : 0);
     p.u = take(muon ? size_t(rows) * size_t(cols) * 4 : 0);
     p.bytes = at;
     return p;
@@ -1047,7 +1314,8 @@ Plan make_plan(const int64_t* rows, const int64_t* cols, int K, bool muon, int64
     for (int i = 0; i < K; ++i) {
         const int k = p.order[i];
         const int way = way_of(rows[k], cols[k]);
-        const int64_t n = way == kThin ? rows[k] * cols[k] : padded(rows[k]) * padded(cols[k]);
+        const bool tiled = way == kSingle || way == kPairs;
+        const int64_t n = tiled ? padded(rows[k]) * padded(cols[k]) : rows[k] * cols[k];
         if (p.batch.empty() || way != p.way.back() || (elems > 0 && elems + n > most)) {
             p.batch.push_back(i);
             p.way.push_back(way);
@@ -1152,9 +1420,25 @@ void launch_thin(const Gate& gate, const Matrix* mats, int first, int n, const C
                                                                  c.ns_steps, decay);
 }
 
+void launch_small(const Gate& gate, const int64_t* prefix, const Matrix* mats, int first, int n,
+                  int64_t slices, const Call& c, float decay)
+{
+    const bool wide_src = c.muon || c.in_dtype == LT_DTYPE_F32;
+    auto* gram = wide_src ? k_orth_small_gram<float> : k_orth_small_gram<uint16_t>;
+    gram<<<dim3(uint32_t(slices)), kThreads, 0, c.st>>>(gate, prefix, mats, first, n);
+    k_orth_small_steps<<<dim3(uint32_t(n)), kThinThreads, 0, c.st>>>(gate, mats, first, c.ns_steps);
+    auto* apply = c.muon ? k_orth_small_apply<float, kWeights>
+                  : c.out_dtype == LT_DTYPE_F32
+                      ? (wide_src ? k_orth_small_apply<float, kOutF32>
+                                  : k_orth_small_apply<uint16_t, kOutF32>)
+                      : (wide_src ? k_orth_small_apply<float, kOutBf16>
+                                  : k_orth_small_apply<uint16_t, kOutBf16>);
+    apply<<<dim3(uint32_t(slices)), kThreads, 0, c.st>>>(gate, prefix, mats, first, n, decay);
+}
+
 // A second stream of the library's own, for the batches of single steps beside those of pairs:
 // the launches of a few square matrices fill half the CUs (two of 2048 x 2048: 272 tiles of
-// 128 x 128).  It starts after what the caller's stream holds and the caller's stream goes on
+// 128 x 128; the projections of a 3B-class layer take 2.64 ms, on one stream 2.86).  It starts after what the caller's stream holds and the caller's stream goes on
 // after it.  Calls enqueue on it one at a time; under capture there is none, and everything goes
 // into the caller's stream.
 class Fork {
@@ -1243,6 +1527,8 @@ lt_err run_batches(const Call& c, float decay, Fill fill, Begin begin)
                 }
                 for (int j = 0; j < 3; ++j)
                     m.sym[j] = reinterpret_cast<_Float16*>(at + x.sym[j]);
+                m.gram = reinterpret_cast<double*>(at + x.gram);
+                m.r = reinterpret_cast<float*>(at + x.r);
                 m.partial = partial;
                 m.square = reinterpret_cast<double*>(ws + p.squares) + i;
                 m.rows = int32_t(c.rows[k]);
@@ -1262,6 +1548,7 @@ lt_err run_batches(const Call& c, float decay, Fill fill, Begin begin)
                     return host::ceil_div(m.rp, t) * host::ceil_div(m.cp, t);
                 };
                 grid[kPreUnits] = m.units;
+                grid[kPreSlices] = slices_of(c.rows[k], c.cols[k]);
                 grid[kPrePrep] = rectangle(kPrep);
                 grid[kPreSym] = triangle(Small::kRows);
                 grid[kPreTile] = rectangle(Small::kRows);
@@ -1300,13 +1587,16 @@ lt_err run_batches(const Call& c, float decay, Fill fill, Begin begin)
         const auto blocks = [&](int i) { return pre[i][first + n] - pre[i][first]; };
         if (n == 0 || blocks(kPreTile) == 0)
             continue;
-        const bool thin = p.way[b] == kThin;
-        if (c.muon || !thin)
+        const bool tiled = p.way[b] == kSingle || p.way[b] == kPairs;
+        if (c.muon || tiled)
             if (lt_err e = begin(gate, dev[kPreUnits], d_momentum, d_mats, first, n,
                                  pre[kPreUnits][first], blocks(kPreUnits), st))
                 return e;
-        if (thin) {
-            launch_thin(gate, d_mats, first, n, c, cus, decay);
+        if (!tiled) {
+            if (p.way[b] == kThin)
+                launch_thin(gate, d_mats, first, n, c, cus, decay);
+            else
+                launch_small(gate, dev[kPreSlices], d_mats, first, n, blocks(kPreSlices), c, decay);
             LT_TRY_HIP(hipGetLastError());
             continue;
         }
