@@ -56,6 +56,9 @@ constexpr float kScaleS = 16384.0f;  // n x n matrices times 2^14
 constexpr float kScaleR = 4096.0f;   // products of a pair's two P times 2^12
 constexpr int kTile = 128;           // what sizes are padded to
 constexpr int kThreads = 256;
+static_assert(Tiny::kThreads == kThreads && Small::kThreads == kThreads &&
+              Large::kThreads == kThreads && Small::kRows == 2 * Tiny::kRows &&
+              Large::kRows == 4 * Tiny::kRows, "tiles of one kind by workgroups of one size");
 constexpr int kPrep = 64;                         // tile of the transposing pass
 
 struct Matrix {
@@ -1217,8 +1220,7 @@ __global__ __launch_bounds__(kThreads) void k_orth_small_apply(Gate gate,
 constexpr int64_t kBatchElems = int64_t(1) << 27;  // padded elements of a batch of several,
 constexpr int64_t kBatchLargest = 4;               // or this many of the list's largest matrix
 
-enum { kPreUnits, kPreSlices, kPrePrep, kPreSym, kPreTile, kPreSymLarge, kPreTileLarge,
-       kPrefixes };
+enum { kPreUnits, kPreSlices, kPrePrep, kPreSym, kPreTile = kPreSym + 3, kPrefixes = kPreTile + 3 };
 
 struct Plan {
     size_t prefix[kPrefixes], momentum, mats, header, squares, partials, region[2], total;
@@ -1376,29 +1378,29 @@ struct Launch {
     template <int OP>
     void sym(const SymArgs& a) const
     {
-        if (large(kPreSymLarge, kPreSym))
-            k_orth_sym<Large, OP><<<dim3(uint32_t(blocks(kPreSymLarge))), Large::kThreads, 0, st>>>(
-                gate, dev[kPreSymLarge], mats, first, n, a);
-        else
-            k_orth_sym<Small, OP><<<dim3(uint32_t(blocks(kPreSym))), Small::kThreads, 0, st>>>(
-                gate, dev[kPreSym], mats, first, n, a);
+        const int size = tile_size(kPreSym), i = kPreSym + size;
+        auto* kernel = size == 0 ? k_orth_sym<Tiny, OP>
+                       : size == 1 ? k_orth_sym<Small, OP> : k_orth_sym<Large, OP>;
+        kernel<<<dim3(uint32_t(blocks(i))), kThreads, 0, st>>>(gate, dev[i], mats, first, n, a);
     }
     template <int FINAL>
     void update(const UpdateArgs& a) const
     {
-        if (large(kPreTileLarge, kPreTile))
-            k_orth_update<Large, FINAL>
-                <<<dim3(uint32_t(blocks(kPreTileLarge))), Large::kThreads, 0, st>>>(
-                    gate, dev[kPreTileLarge], mats, first, n, a);
-        else
-            k_orth_update<Small, FINAL><<<dim3(uint32_t(blocks(kPreTile))), Small::kThreads, 0, st>>>(
-                gate, dev[kPreTile], mats, first, n, a);
+        const int size = tile_size(kPreTile), i = kPreTile + size;
+        auto* kernel = size == 0 ? k_orth_update<Tiny, FINAL>
+                       : size == 1 ? k_orth_update<Small, FINAL> : k_orth_update<Large, FINAL>;
+        kernel<<<dim3(uint32_t(blocks(i))), kThreads, 0, st>>>(gate, dev[i], mats, first, n, a);
     }
-    // 256 x 256 tiles, one to a CU, where their rounds are cheaper than those of 128 x 128, two
-    // to a CU: a step of 64 summed values takes 1.85 us and 1.12 us a round.
-    bool large(int i, int small) const
+    // Tiles of 64, 128 or 256 on a side, whose rounds are cheapest.  A step of 64 summed values takes
+    // 1.85 us a round of one tile of 256 a CU, 1.12 us a round of two of 128 (0.6 where a CU has
+    // one), 0.48 us of two of 64 (four: 1.15).  1024 x 1024 by tiles of 64 161 us, of 128 212, of
+    // 256 524; 2048 x 2048 423, 365 and 776; 17408 x 5120 by tiles of 256 5.5 ms, of 128 6.3.
+    int tile_size(int i) const
     {
-        return host::ceil_div(blocks(i), cus) * 185 < host::ceil_div(blocks(small), 2 * cus) * 112;
+        if (blocks(i) <= 2 * cus)
+            return 0;
+        return host::ceil_div(blocks(i + 2), cus) * 185 < host::ceil_div(blocks(i + 1), 2 * cus) * 112
+                   ? 2 : 1;
     }
 };
 
@@ -1550,10 +1552,10 @@ lt_err run_batches(const Call& c, float decay, Fill fill, Begin begin)
                 grid[kPreUnits] = m.units;
                 grid[kPreSlices] = slices_of(c.rows[k], c.cols[k]);
                 grid[kPrePrep] = rectangle(kPrep);
-                grid[kPreSym] = triangle(Small::kRows);
-                grid[kPreTile] = rectangle(Small::kRows);
-                grid[kPreSymLarge] = triangle(Large::kRows);
-                grid[kPreTileLarge] = rectangle(Large::kRows);
+                for (int size = 0; size < 3; ++size) {
+                    grid[kPreSym + size] = triangle(Tiny::kRows << size);
+                    grid[kPreTile + size] = rectangle(Tiny::kRows << size);
+                }
             }
             for (int j = 0; j < kPrefixes; ++j)
                 pre[j][i + 1] = pre[j][i] + grid[j];
