@@ -1394,7 +1394,7 @@ struct Launch {
     // Tiles of 64, 128 or 256 on a side, whose rounds are cheapest.  A step of 64 summed values takes
     // 1.85 us a round of one tile of 256 a CU, 1.12 us a round of two of 128 (0.6 where a CU has
     // one), 0.48 us of two of 64 (four: 1.15).  1024 x 1024 by tiles of 64 161 us, of 128 212, of
-    // 256 524; 2048 x 2048 423, 365 and 776; 17408 x 5120 by tiles of 256 5.5 ms, of 128 6.3.
+    // 256 524; 2048 x 2048 423, 365 and 776; 17408 x 5120 by tiles of 256 5.5 ms, of 128 6.5.
     int tile_size(int i) const
     {
         if (blocks(i) <= 2 * cus)
