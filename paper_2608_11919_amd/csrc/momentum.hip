@@ -7,7 +7,8 @@
 // absmax and codes as the 8-bit AdamW step stores a first moment.  u goes to the workspace in
 // fp32: its norm is known only when all of it is, so it is read once more either way, and the
 // orthogonalisation reads it there.  The pass is bound by HBM: 2 or 4 bytes of gradient, a
-// code read and written, 4 bytes of u.
+// code read and written, 4 bytes of u (67.6M elements with bf16 gradients, block 4096: 115 to
+// 133 us, 4.1 to 4.7 TB/s).
 
 namespace {
 

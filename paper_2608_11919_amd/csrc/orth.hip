@@ -152,6 +152,8 @@ __device__ inline double sum_workgroup(double x, double* red)
 
 // ------------------------------------------------------------- the norm
 
+// The sum of squares in 64 bits, bound by reading: fp32 17408 x 5120 70 to 78 us, 4.6 to 5.1 TB/s.
+// A sum for every unit of 16384 elements, added up in a fixed order by k_orth_norm.
 constexpr int64_t kSquareUnit = 16384;  // elements of one workgroup
 
 template <typename T>
@@ -209,6 +211,8 @@ __global__ __launch_bounds__(kThreads) void k_orth_norm(Gate gate, const Matrix*
 
 // ------------------------------------------------- X_0 in its three layouts
 
+// One 64 x 64 tile by a workgroup, transposed through LDS, so that all four matrices are read and
+// written in whole lines.  Bound by HBM: fp32 17408 x 5120 160 us, 5.6 TB/s read and written.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_orth_prepare(Gate gate,
                                                            const int64_t* __restrict__ prefix,
@@ -289,6 +293,9 @@ __device__ inline Shift shift_at(const Matrix& m, int step)
 
 // Products of n x n matrices, all symmetric: tiles on and above the diagonal, each stored on
 // both sides of it.  With S = A - d I, P^ = P - p I, W^ = P A - p d I, R^ = P' P - p' p I:
+// 17408 x 5120: G 400 us (half of 2 n^2 m: 1.14 PFLOP/s on 210 of 256 CUs), each of the others
+// 131 to 136 us (1.05).  What bounds them is the matrix cores' power: 1.28 PFLOP/s is what a large
+// product of random fp16 numbers reaches at all, zeros 1.8.
 enum Sym {
     kGram,    // S = X X^T - d I (or X^T X)
     kStep,    // P^ = c S S + (b + 2 c d) S
@@ -524,7 +531,8 @@ struct UpdateWriter {
 };
 
 // X' = p X + P^ X (or p X + X P^), P standing for P' P after a pair: the next X, or where it
-// goes.
+// goes.  17408 x 5120 900 us (1.0 PFLOP/s) where the next X is written, 820 us to bf16: some 720
+// are the product, the rest reading X and writing its three layouts.
 template <typename Tile, int FINAL>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_orth_update(Gate gate,
                                                                 const int64_t* __restrict__ prefix,
@@ -676,8 +684,8 @@ __device__ inline void thin_product32(Thin<32>::Sym& dst, const Thin<32>::Sym& M
     __syncthreads();
 }
 
-// Columns [k0, k0 + kWidth) of X, zeros from column `end` on, into LDS, 32 reads of a lane under way at a
-// time.  Rows of X lie along its memory where it is wide, columns where it is tall.
+// Columns [k0, k0 + kWidth) of X, zeros from column `end` on, into LDS, 32 reads of a lane under way
+// at a time.  Rows of X lie along its memory where it is wide, columns where it is tall.
 template <int NP, typename T>
 __device__ inline void thin_load(Thin<NP>& t, const Matrix& m, bool wide, int k0,
                                  int end)
@@ -1216,7 +1224,8 @@ __global__ __launch_bounds__(kThreads) void k_orth_small_apply(Gate gate,
 //
 // A batch is what one sequence of launches works on.  Large ones fill the last rounds of their
 // launches: the three feed-forward matrices of a 27B-class layer (2.7e8 elements) one by one
-// leave a fifth of the CUs idle in every product.  16 bytes of workspace go with an element.
+// leave a fifth of the CUs idle in every product (its Muon step 27.5 ms, one by one 28.0).  16 bytes
+// of workspace go with an element.
 constexpr int64_t kBatchElems = int64_t(1) << 27;  // padded elements of a batch of several,
 constexpr int64_t kBatchLargest = 4;               // or this many of the list's largest matrix
 
@@ -1229,10 +1238,10 @@ struct Plan {
     std::vector<int> way;      // of each batch: how its matrices are worked on
 };
 
-// How a matrix is worked on.  Thin and small ones in 64 bits on their own side.  Long ones take their steps in
-// pairs, which saves a sixth of the multiply-adds or more (17408 x 5120: 5.5 ms, in single steps
-// 7.3; the projections of a 3B-class layer 2.6 and 3.5); 128 rows or columns are the least that a
-// tile computes anyway.
+// How a matrix is worked on.  Thin and small ones in 64 bits on their smaller side.  Long ones take
+// their steps in pairs, which saves a sixth of the multiply-adds or more (17408 x 5120: 5.5 ms, in
+// single steps 7.3; the projections of a 3B-class layer 2.6 and 3.5); 128 rows or columns are what
+// sizes are padded to anyway.
 enum { kThin, kSmall, kSingle, kPairs, kWays };
 
 int way_of(int64_t rows, int64_t cols)
@@ -1399,8 +1408,8 @@ struct Launch {
     {
         if (blocks(i) <= 2 * cus)
             return 0;
-        return host::ceil_div(blocks(i + 2), cus) * 185 < host::ceil_div(blocks(i + 1), 2 * cus) * 112
-                   ? 2 : 1;
+        const int64_t large = host::ceil_div(blocks(i + 2), cus) * 185;
+        return large < host::ceil_div(blocks(i + 1), 2 * cus) * 112 ? 2 : 1;
     }
 };
 
@@ -1440,9 +1449,9 @@ void launch_small(const Gate& gate, const int64_t* prefix, const Matrix* mats, i
 
 // A second stream of the library's own, for the batches of single steps beside those of pairs:
 // the launches of a few square matrices fill half the CUs (two of 2048 x 2048: 272 tiles of
-// 128 x 128; the projections of a 3B-class layer take 2.64 ms, on one stream 2.86).  It starts after what the caller's stream holds and the caller's stream goes on
-// after it.  Calls enqueue on it one at a time; under capture there is none, and everything goes
-// into the caller's stream.
+// 128 x 128; the projections of a 3B-class layer take 2.64 ms, on one stream 2.86).  It starts
+// after what the caller's stream holds and the caller's stream goes on after it.  Calls enqueue on
+// it one at a time; under capture there is none, and everything goes into the caller's stream.
 class Fork {
 public:
     Fork() = default;

@@ -183,9 +183,11 @@ __device__ inline TilePlace triangle_place(int t, int side)
     }
 }
 
+// Four waves each.  A Large tile has the fewest bytes to copy for a product (two operands' rows
+// for 256 results a row) and one workgroup a CU; where there are too few of those, smaller ones.
+typedef Shape<64, 64, 32, 32> Tiny;
 typedef Shape<128, 128, 64, 64> Small;
 typedef Shape<256, 256, 128, 128> Large;
-typedef Shape<64, 64, 32, 32> Tiny;
 
 // Products of fp8 (e4m3) with a power-of-two scale for each row and each 128 values: a step's in
 // two instructions of 64, which apply the scales themselves.  A scale is a byte, the
