@@ -61,6 +61,17 @@ def _layout(codes, scales, rows: int, cols: int, device, what: str) -> Tuple[int
     return codes.data_ptr(), scales.data_ptr()
 
 
+def _scratch(device, nbytes: int, workspace, stream) -> Tuple[torch.Tensor, int, int]:
+    """(tensor, address, bytes) of the caller's workspace, or of the cached one.  A call that is
+    being captured gets memory from the graph's pool: a larger call may replace the cached one
+    while the graph lives."""
+    if workspace is None and torch.cuda.is_current_stream_capturing():
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    else:
+        ws = _workspace(device, nbytes, workspace, stream, "fp8")
+    return ws, ws.data_ptr(), ws.numel() * ws.element_size()
+
+
 def lt_fp8_quantize(x: torch.Tensor, codes: Optional[torch.Tensor] = None,
                     scales: Optional[torch.Tensor] = None,
                     codes_t: Optional[torch.Tensor] = None,
@@ -94,8 +105,7 @@ def lt_fp8_matmul(a_codes: torch.Tensor, a_scales: torch.Tensor, b_codes: torch.
     ws, nbytes = 0, 0
     if (m > 32 and k > 512) or workspace is not None:
         nbytes = int(lib().lt_fp8_matmul_workspace_bytes(m, n, k))
-        held = _workspace(device, nbytes, workspace, stream, "fp8")
-        ws, nbytes = held.data_ptr(), held.numel() * held.element_size()
+        held, ws, nbytes = _scratch(device, nbytes, workspace, stream)
     with _current(device):
         _check(lib().lt_fp8_matmul(a, sa, b, sb, m, n, k, out.data_ptr(), code, stride, ws,
                                    nbytes, _stream_handle(stream, device)))
@@ -163,8 +173,7 @@ def fp8_linear(x: torch.Tensor, weight: Fp8Weight,
     ws, nbytes = 0, 0
     if m > 16 or workspace is not None:
         nbytes = int(lib().lt_fp8_linear_workspace_bytes(m, weight.rows, weight.cols))
-        held = _workspace(device, nbytes, workspace, None, "fp8")
-        ws, nbytes = held.data_ptr(), held.numel() * held.element_size()
+        held, ws, nbytes = _scratch(device, nbytes, workspace, None)
     with _current(device):
         _check(lib().lt_fp8_linear(t.data_ptr(), _dtype_code(t, "x"), stride,
                                    weight.codes.data_ptr(), weight.scales.data_ptr(), m,
