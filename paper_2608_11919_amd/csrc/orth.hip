@@ -65,6 +65,7 @@ struct Matrix {
     const void* src;           // the matrix, or the Muon step's update in fp32
     _Float16 *h[2], *t[2], *l[2];
     _Float16* sym[3];          // n x n matrices
+    float* sums;               // G's sums by slices of the summed index
     double* gram;              // sides of 33 to 64: G of every slice of columns
     float* r;                  // and R, behind what X is multiplied by
     double *partial, *square;  // sums of squares of its units; their sum
@@ -415,6 +416,112 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_orth_sy
     out.real = real - r0;
     out.mirror = r0 != c0;
     finish(tile, lds, out);
+}
+
+// G of a few long matrices has few tiles of long sums: the sums are cut into slices of a whole
+// number of pairs of steps, and added up in order by the pass that stores G.
+__device__ inline int slice_steps(int inner, int slices)
+{
+    return (inner / 64 + 2 * slices - 1) / (2 * slices) * 2;
+}
+
+struct SumWriter {
+    static constexpr bool kTurned = false;
+    static constexpr int kSlots = 8;
+    float* to;  // at the tile's origin
+    int64_t pitch;
+    __device__ inline void fetch(int, int, int) {}
+    __device__ inline void turn(int, int, const float (&)[8]) {}
+    __device__ inline void store(int row, int col, float (&v)[8], int)
+    {
+        float* p = to + row * pitch + col;
+        *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+        *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+    }
+};
+
+template <typename Tile>
+__global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_orth_gram(Gate gate,
+                                                             const int64_t* __restrict__ prefix,
+                                                             const Matrix* __restrict__ mats,
+                                                             int first, int n, int from)
+{
+    __shared__ __align__(1024) uint8_t lds[Tile::kLdsBytes];
+    if (!descriptors_ok(gate) || !step_applies(gate))
+        return;
+    const int64_t unit = prefix[first] + unit_of_workgroup(Tile::kRun);
+    const int k = find_matrix(prefix, first, n, unit);
+    const Matrix& m = mats[k];
+    const bool wide = m.rows <= m.cols;
+    const int side = wide ? m.rp : m.cp, inner = wide ? m.cp : m.rp;
+    const int per = slice_steps(inner, int(gridDim.y)), begin = int(blockIdx.y) * per;
+    const int steps = min(per, inner / 64 - begin);
+    if (steps <= 0)
+        return;
+    const TilePlace at_tile =
+        triangle_place(int(unit - prefix[k]), (side + Tile::kRows - 1) / Tile::kRows);
+    const int r0 = at_tile.row * Tile::kRows, c0 = at_tile.col * Tile::kCols;
+    const _Float16* X = (wide ? m.h[from] : m.t[from]) + int64_t(begin) * 64;
+    Tile tile;
+    Half mul;
+    product(mul, tile, X + int64_t(r0) * inner, int64_t(inner) * 2, side - r0,
+            X + int64_t(c0) * inner, int64_t(inner) * 2, side - c0, steps, lds);
+    if (r0 + Tile::wave_row() >= side || c0 + Tile::wave_col() >= side)
+        return;  // sizes are multiples of 128: a wave's block lies inside or outside
+    SumWriter out;
+    out.pitch = side;
+    out.to = m.sums + (int64_t(blockIdx.y) * side + r0) * side + c0;
+    finish(tile, lds, out);
+}
+
+// G = the slices' sums: a block of 64 x 64 on or above the diagonal and its mirror image by a
+// workgroup.
+__global__ __launch_bounds__(kThreads) void k_orth_gram_join(Gate gate,
+                                                             const int64_t* __restrict__ prefix,
+                                                             const Matrix* __restrict__ mats,
+                                                             int first, int n, int slices,
+                                                             SymArgs args)
+{
+    __shared__ __align__(16) _Float16 turned[64][64 + 8];
+    if (!descriptors_ok(gate) || !step_applies(gate))
+        return;
+    const int64_t unit = prefix[first] + blockIdx.x;
+    const int k = find_matrix(prefix, first, n, unit);
+    const Matrix& m = mats[k];
+    const bool wide = m.rows <= m.cols;
+    const int side = wide ? m.rp : m.cp, inner = wide ? m.cp : m.rp;
+    const int real = wide ? m.rows : m.cols;
+    const int per = slice_steps(inner, slices), used = (inner / 64 + per - 1) / per;
+    const TilePlace at = triangle_place(int(unit - prefix[k]), side / 64);
+    const int r0 = at.row * 64, c0 = at.col * 64;
+    const int row = int(threadIdx.x) / 4, col = int(threadIdx.x) % 4 * 16;
+    const float* from = m.sums + int64_t(r0 + row) * side + c0 + col;
+    f32x4 v[4] = {};
+    for (int i = 0; i < used; ++i, from += int64_t(side) * side)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            v[c] += *reinterpret_cast<const f32x4*>(from + 4 * c);
+    const float by = kScaleS / (kScaleX * kScaleX);
+    const float diagonal = shift_at(m, args.step).d * kScaleS;
+    half8 h[2];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const int r = r0 + row;
+        const float x = v[e / 4][e % 4] * by - (r == c0 + col + e && r < real ? diagonal : 0.0f);
+        h[e / 8][e % 8] = _Float16(x);
+        turned[col + e][row] = _Float16(x);
+    }
+    _Float16* to = m.sym[args.out];
+    half8* p = reinterpret_cast<half8*>(to + int64_t(r0 + row) * side + c0 + col);
+    p[0] = h[0];
+    p[1] = h[1];
+    if (r0 == c0)
+        return;
+    __syncthreads();
+    half8* q = reinterpret_cast<half8*>(to + int64_t(c0 + row) * side + r0 + col);
+    const half8* w = reinterpret_cast<const half8*>(&turned[row][col]);
+    q[0] = w[0];
+    q[1] = w[1];
 }
 
 enum Final { kAgain, kOutF32, kOutBf16, kWeights };
@@ -1231,11 +1338,18 @@ constexpr int64_t kBatchLargest = 4;               // or this many of the list's
 
 enum { kPreUnits, kPreSlices, kPrePrep, kPreSym, kPreTile = kPreSym + 3, kPrefixes = kPreTile + 3 };
 
+// Tile size and slices of the sums of a batch's G.
+struct GramWay {
+    int size, slices;
+};
+
 struct Plan {
     size_t prefix[kPrefixes], momentum, mats, header, squares, partials, region[2], total;
     std::vector<int> order;    // the list's matrices in the order in which they are worked on
     std::vector<int> batch;    // first place of each batch, and the list's length
     std::vector<int> way;      // of each batch: how its matrices are worked on
+    std::vector<size_t> sums;  // where in its region its sums of G's slices lie
+    std::vector<GramWay> gram;
 };
 
 // How a matrix is worked on.  Thin and small ones in 64 bits on their smaller side.  Long ones take
@@ -1263,6 +1377,50 @@ int64_t slices_of(int64_t rows, int64_t cols)
 
 int64_t units_of(int64_t numel, int64_t span) { return (numel + span - 1) / span; }
 
+bool tiled(int way) { return way == kSingle || way == kPairs; }
+
+// Tiles of `tile` on and above the diagonal of side x side.
+int64_t triangle(int64_t side, int64_t tile)
+{
+    const int64_t n = host::ceil_div(side, tile);
+    return n * (n + 1) / 2;
+}
+
+// The cheapest tiles and slices, for sums of up to `steps` steps and `bytes` of one slice's sums.  A
+// round's step takes 0.48 us by two tiles of 64 a CU (0.39 by one), 1.12 by two of 128 (0.6) and 1.5
+// by one of 256, the rest of a round 3, 5 and 9; joining slices takes 12 us beside their bytes'
+// way to memory and back.  In slices only where that saves a fifth by this account: 128 x 17408 takes
+// 151 us and in one piece 336, 1024 x 17408 502 and 641, eight of 256 x 8192 328 and 387; without the
+// sums' bytes in the account 4096 x 4096 was cut as well and took 2253 instead of 1671.
+GramWay gram_way(const int64_t (&tiles)[3], int64_t steps, size_t bytes)
+{
+    constexpr int64_t kCus = 256;
+    constexpr double kAlone[3] = {0.39, 0.6, 1.5}, kFull[3] = {0.48, 1.12, 1.5}, kRest[3] = {3, 5, 9};
+    GramWay best{-1, 1};  // tiles as for the other products
+    double whole = 0.0, least = 0.0;
+    for (const int slices : {1, 2, 4, 8, 16}) {
+        const int64_t per = host::ceil_div(steps, 2 * slices) * 2;
+        if (slices > 1 && per < 8)
+            break;
+        for (int size = 0; size < 3; ++size) {
+            const int64_t all = tiles[size] * slices, places = size == 2 ? kCus : 2 * kCus;
+            const double step = all <= kCus ? kAlone[size] : kFull[size];
+            double cost = double(host::ceil_div(all, places)) * (double(per) * step + kRest[size]);
+            if (slices == 1) {
+                whole = size == 0 ? cost : std::min(whole, cost);
+                least = 0.8 * whole;
+                continue;
+            }
+            cost += 12.0 + double(bytes) * slices / 4.0e6;
+            if (cost < least) {
+                least = cost;
+                best = GramWay{size, slices};
+            }
+        }
+    }
+    return best;
+}
+
 // Bytes of a matrix in the region: X in three layouts twice, three n x n matrices, the Muon
 // step's update.
 struct Place {
@@ -1273,9 +1431,8 @@ Place place(int64_t rows, int64_t cols, bool muon)
 {
     Place p;
     const int way = way_of(rows, cols);
-    const bool tiled = way == kSingle || way == kPairs;
-    const size_t x = tiled ? size_t(padded(rows)) * size_t(padded(cols)) * 2 : 0;
-    const size_t side = tiled ? size_t(std::min(padded(rows), padded(cols))) : 0;
+    const size_t x = tiled(way) ? size_t(padded(rows)) * size_t(padded(cols)) * 2 : 0;
+    const size_t side = tiled(way) ? size_t(std::min(padded(rows), padded(cols))) : 0;
     const size_t slices = way == kSmall ? size_t(slices_of(rows, cols)) : 0;
     size_t at = 0;
     const auto take = [&](size_t bytes) {
@@ -1321,24 +1478,42 @@ Plan make_plan(const int64_t* rows, const int64_t* cols, int K, bool muon, int64
     for (int k = 0; k < K; ++k)
         most = std::max(most, kBatchLargest * padded(rows[k]) * padded(cols[k]));
     int64_t units = 0, elems = 0;
-    size_t region[2] = {0, 0}, bytes = 0;  // of single steps, and of everything else
     for (int i = 0; i < K; ++i) {
         const int k = p.order[i];
         const int way = way_of(rows[k], cols[k]);
-        const bool tiled = way == kSingle || way == kPairs;
-        const int64_t n = tiled ? padded(rows[k]) * padded(cols[k]) : rows[k] * cols[k];
+        const int64_t n = tiled(way) ? padded(rows[k]) * padded(cols[k]) : rows[k] * cols[k];
         if (p.batch.empty() || way != p.way.back() || (elems > 0 && elems + n > most)) {
             p.batch.push_back(i);
             p.way.push_back(way);
             elems = 0;
-            bytes = 0;
         }
-        if (rows[k] == 0 || cols[k] == 0)
-            continue;
         units += units_of(rows[k] * cols[k], span);
         elems += n;
-        bytes += place(rows[k], cols[k], muon).bytes;
-        region[way == kSingle ? 0 : 1] = std::max(region[way == kSingle ? 0 : 1], bytes);
+    }
+    size_t region[2] = {0, 0};  // of single steps, and of everything else
+    for (size_t b = 0; b < p.way.size(); ++b) {
+        const int end = b + 1 < p.way.size() ? p.batch[b + 1] : K;
+        int64_t tiles[3] = {}, steps = 0;
+        size_t bytes = 0, squares = 0;
+        for (int i = p.batch[b]; i < end; ++i) {
+            const int k = p.order[i];
+            if (rows[k] == 0 || cols[k] == 0)
+                continue;
+            bytes += place(rows[k], cols[k], muon).bytes;
+            if (!tiled(p.way[b]))
+                continue;
+            const int64_t side = std::min(padded(rows[k]), padded(cols[k]));
+            for (int size = 0; size < 3; ++size)
+                tiles[size] += triangle(side, Tiny::kRows << size);
+            steps = std::max(steps, std::max(padded(rows[k]), padded(cols[k])) / 64);
+            squares += size_t(side) * size_t(side) * sizeof(float);
+        }
+        p.gram.push_back(gram_way(tiles, steps, squares));
+        p.sums.push_back(bytes);
+        if (p.gram[b].slices > 1)
+            bytes += squares * size_t(p.gram[b].slices);
+        size_t& most_bytes = region[p.way[b] == kSingle ? 0 : 1];
+        most_bytes = std::max(most_bytes, bytes);
     }
     p.batch.push_back(K);
     p.region[0] = p.partials + round_up(sizeof(double) * size_t(units), 256);
@@ -1391,6 +1566,20 @@ struct Launch {
         auto* kernel = size == 0 ? k_orth_sym<Tiny, OP>
                        : size == 1 ? k_orth_sym<Small, OP> : k_orth_sym<Large, OP>;
         kernel<<<dim3(uint32_t(blocks(i))), kThreads, 0, st>>>(gate, dev[i], mats, first, n, a);
+    }
+    void gram(const SymArgs& a, const GramWay& way) const
+    {
+        if (way.slices == 1) {
+            sym<kGram>(a);
+            return;
+        }
+        const int i = kPreSym + way.size;
+        auto* kernel = way.size == 0 ? k_orth_gram<Tiny>
+                       : way.size == 1 ? k_orth_gram<Small> : k_orth_gram<Large>;
+        kernel<<<dim3(uint32_t(blocks(i)), uint32_t(way.slices)), kThreads, 0, st>>>(
+            gate, dev[i], mats, first, n, a.from);
+        k_orth_gram_join<<<dim3(uint32_t(blocks(kPreSym))), kThreads, 0, st>>>(
+            gate, dev[kPreSym], mats, first, n, way.slices, a);
     }
     template <int FINAL>
     void update(const UpdateArgs& a) const
@@ -1524,6 +1713,7 @@ lt_err run_batches(const Call& c, float decay, Fill fill, Begin begin)
     auto* partial = reinterpret_cast<double*>(ws + p.partials);
     for (size_t b = 0; b + 1 < p.batch.size(); ++b) {
         uint8_t* at = ws + p.region[p.way[b] == kSingle ? 0 : 1];
+        auto* sums = reinterpret_cast<float*>(at + p.sums[b]);
         for (int i = p.batch[b]; i < p.batch[b + 1]; ++i) {
             const int k = p.order[i];  // the i-th matrix of the descriptors
             const int64_t numel = c.rows[k] * c.cols[k];
@@ -1551,10 +1741,10 @@ lt_err run_batches(const Call& c, float decay, Fill fill, Begin begin)
                 partial += m.units;
                 at += x.bytes;
                 const int64_t side = std::min(m.rp, m.cp);
-                const auto triangle = [&](int64_t t) {
-                    const int64_t n = host::ceil_div(side, t);
-                    return n * (n + 1) / 2;
-                };
+                if (tiled(p.way[b]) && p.gram[b].slices > 1) {
+                    m.sums = sums;
+                    sums += side * side * p.gram[b].slices;
+                }
                 const auto rectangle = [&](int64_t t) {
                     return host::ceil_div(m.rp, t) * host::ceil_div(m.cp, t);
                 };
@@ -1562,7 +1752,7 @@ lt_err run_batches(const Call& c, float decay, Fill fill, Begin begin)
                 grid[kPreSlices] = slices_of(c.rows[k], c.cols[k]);
                 grid[kPrePrep] = rectangle(kPrep);
                 for (int size = 0; size < 3; ++size) {
-                    grid[kPreSym + size] = triangle(Tiny::kRows << size);
+                    grid[kPreSym + size] = triangle(side, Tiny::kRows << size);
                     grid[kPreTile + size] = rectangle(Tiny::kRows << size);
                 }
             }
@@ -1598,12 +1788,11 @@ lt_err run_batches(const Call& c, float decay, Fill fill, Begin begin)
         const auto blocks = [&](int i) { return pre[i][first + n] - pre[i][first]; };
         if (n == 0 || blocks(kPreTile) == 0)
             continue;
-        const bool tiled = p.way[b] == kSingle || p.way[b] == kPairs;
-        if (c.muon || tiled)
+        if (c.muon || tiled(p.way[b]))
             if (lt_err e = begin(gate, dev[kPreUnits], d_momentum, d_mats, first, n,
                                  pre[kPreUnits][first], blocks(kPreUnits), st))
                 return e;
-        if (!tiled) {
+        if (!tiled(p.way[b])) {
             if (p.way[b] == kThin)
                 launch_thin(gate, d_mats, first, n, c, cus, decay);
             else
@@ -1619,7 +1808,7 @@ lt_err run_batches(const Call& c, float decay, Fill fill, Begin begin)
         const Launch launch{gate, d_mats, first, n, cus, st, dev, pre};
         int from = 0;
         for (int step = 0; step < c.ns_steps; from ^= 1) {
-            launch.sym<kGram>({step, from, 0, 0, 0});
+            launch.gram({step, from, 0, 0, 0}, p.gram[b]);
             launch.sym<kStep>({step, from, 0, 0, 1});
             const int now = p.way[b] == kPairs && step + 1 < c.ns_steps ? 2 : 1;
             if (now == 2) {
