@@ -61,14 +61,14 @@ def _layout(codes, scales, rows: int, cols: int, device, what: str) -> Tuple[int
     return codes.data_ptr(), scales.data_ptr()
 
 
-def _scratch(device, nbytes: int, workspace, stream) -> Tuple[torch.Tensor, int, int]:
+def _scratch(device, nbytes: int, workspace, stream, handle: int) -> Tuple[torch.Tensor, int, int]:
     """(tensor, address, bytes) of the caller's workspace, or of the cached one.  A call that is
     being captured gets memory from the graph's pool: a larger call may replace the cached one
     while the graph lives."""
     if workspace is None and torch.cuda.is_current_stream_capturing():
         ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
     else:
-        ws = _workspace(device, nbytes, workspace, stream, "fp8")
+        ws = _workspace(device, nbytes, workspace, stream, "fp8", handle)
     return ws, ws.data_ptr(), ws.numel() * ws.element_size()
 
 
@@ -102,13 +102,13 @@ def lt_fp8_matmul(a_codes: torch.Tensor, a_scales: torch.Tensor, b_codes: torch.
     device = out.device
     a, sa = _layout(a_codes, a_scales, m, k, device, "a_codes")
     b, sb = _layout(b_codes, b_scales, n, k, device, "b_codes")
-    ws, nbytes = 0, 0
+    ws, nbytes, handle = 0, 0, _stream_handle(stream, device)
     if (m > 32 and k > 512) or workspace is not None:
         nbytes = int(lib().lt_fp8_matmul_workspace_bytes(m, n, k))
-        held, ws, nbytes = _scratch(device, nbytes, workspace, stream)
+        held, ws, nbytes = _scratch(device, nbytes, workspace, stream, handle)
     with _current(device):
         _check(lib().lt_fp8_matmul(a, sa, b, sb, m, n, k, out.data_ptr(), code, stride, ws,
-                                   nbytes, _stream_handle(stream, device)))
+                                   nbytes, handle))
 
 
 class Fp8Weight:
@@ -170,15 +170,15 @@ def fp8_linear(x: torch.Tensor, weight: Fp8Weight,
     if weight.codes.device != device:
         raise ValueError(f"the weight is on {weight.codes.device}, x on {device}")
     y = torch.empty(m, weight.rows, dtype=out_dtype, device=device)
-    ws, nbytes = 0, 0
+    ws, nbytes, handle = 0, 0, _stream_handle(None, device)
     if m > 16 or workspace is not None:
         nbytes = int(lib().lt_fp8_linear_workspace_bytes(m, weight.rows, weight.cols))
-        held, ws, nbytes = _scratch(device, nbytes, workspace, None)
+        held, ws, nbytes = _scratch(device, nbytes, workspace, None, handle)
     with _current(device):
         _check(lib().lt_fp8_linear(t.data_ptr(), _dtype_code(t, "x"), stride,
                                    weight.codes.data_ptr(), weight.scales.data_ptr(), m,
                                    weight.rows, weight.cols, y.data_ptr(), _dtype_code(y, "y"),
-                                   weight.rows, ws, nbytes, _stream_handle(None, device)))
+                                   weight.rows, ws, nbytes, handle))
     return y if x.dim() == 2 else y.view(*x.shape[:-1], weight.rows)
 
 

@@ -342,19 +342,20 @@ def _track(ws: torch.Tensor) -> None:
 
 
 def _workspace(device, nbytes: int, workspace: Optional[torch.Tensor], stream,
-               kind: str) -> torch.Tensor:
+               kind: str, handle: Optional[int] = None) -> torch.Tensor:
     """The caller's workspace, or one cached per (device, stream, kind of call), so
     that a call repeated over the same tensors finds its descriptors in place (the
     library then copies nothing; see include/lazytrain.h).  A cached workspace is
     allocated on the stream that uses it, so that when a larger one replaces it the
     caching allocator hands its memory out again only in that stream's order; the
-    library is told to forget the old one first."""
+    library is told to forget the old one first.  `handle` is the stream's, where the
+    caller has it already."""
     if workspace is not None:
         if workspace.device != device or workspace.numel() * workspace.element_size() < nbytes:
             raise ValueError(f"workspace must hold {nbytes} bytes on {device}")
         _track(workspace)
         return workspace
-    key = (device, _stream_handle(stream, device), kind)
+    key = (device, _stream_handle(stream, device) if handle is None else handle, kind)
     ws = _workspaces.get(key)
     if ws is None or ws.numel() < nbytes:
         if ws is not None:

@@ -64,12 +64,13 @@ def lt_orthogonalize(matrices: Sequence[torch.Tensor], out: Sequence[torch.Tenso
                 raise ValueError(f"out[{i}] must have shape {tuple(m.shape)}")
     n = len(matrices)
     nbytes = int(lib().lt_orthogonalize_workspace_bytes(rows, cols, n))
-    ws = _workspace(device, nbytes, workspace, stream, "orthogonalize")
+    handle = _stream_handle(stream, device)
+    ws = _workspace(device, nbytes, workspace, stream, "orthogonalize", handle)
     with _current(device):
         _check(lib().lt_orthogonalize(
             src.ptrs, _one_dtype(matrices, src, "matrices"), dst.ptrs,
             _one_dtype(out, dst, "out"), rows, cols, n, int(ns_steps), ws.data_ptr(),
-            ws.numel() * ws.element_size(), _stream_handle(stream, device)))
+            ws.numel() * ws.element_size(), handle))
 
 
 def lt_muon_workspace_bytes(rows: Sequence[int], cols: Sequence[int], block_size: int) -> int:
@@ -115,14 +116,15 @@ def lt_muon_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor],
                 raise ValueError(f"tensor {i}: m_absmax needs {nb} entries")
     wb = _bf16_list(params_bf16, params, device, p.numels)
     nbytes = int(lib().lt_muon_workspace_bytes(rows, cols, n, int(block_size)))
-    ws = _workspace(device, nbytes, workspace, stream, "muon")
+    handle = _stream_handle(stream, device)
+    ws = _workspace(device, nbytes, workspace, stream, "muon", handle)
     with _current(device):
         _check(lib().lt_muon_step(
             p.ptrs, g.ptrs, gdt, mq.ptrs, ma.ptrs, wb, rows, cols, n, int(block_size),
             int(code_map), float(lr), float(momentum), int(bool(nesterov)), float(weight_decay),
             float(update_rms), int(ns_steps), _scalar(coef, device, torch.float32, "coef"),
             _scalar(status, device, torch.int32, "status"), _state_ptr(step_state, device),
-            ws.data_ptr(), ws.numel() * ws.element_size(), _stream_handle(stream, device)))
+            ws.data_ptr(), ws.numel() * ws.element_size(), handle))
 
 
 # ------------------------------------------------------------- optimizer object
