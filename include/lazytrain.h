@@ -66,7 +66,12 @@
  *    one uncaptured call with the same workspace and tensor list whose work has
  *    completed; a captured call that would have to copy descriptors returns
  *    LT_ERR_INVALID_ARG.  lt_clip_coef copies nothing and may always be
- *    captured.  The streamed step (host copies) is not capturable.
+ *    captured, and so may f5 and f6: kernels of the graph write descriptors
+ *    that are not in place at capture, at every replay.  The memory of such a
+ *    workspace belongs to the graph for as long as that may be replayed; a
+ *    workspace whose descriptors were in place must not be given to a call
+ *    with another list meanwhile (replays would find these and return).
+ *    The streamed step (host copies) is not capturable.
  *  - Results are bitwise reproducible: they do not depend on the grid size,
  *    the device occupancy or the stream.
  */

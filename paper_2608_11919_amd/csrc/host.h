@@ -32,7 +32,8 @@ lt_err fail(lt_err code, const std::string& msg);
 void clear_error();
 
 // Makes the workspace hold `image` (its first kTagBytes are the tag slot) before the work
-// enqueued next on the stream reads it; nothing is copied when it already does.
+// enqueued next on the stream reads it; nothing is copied when it already does.  Under capture
+// the graph writes it, at every replay.
 lt_err put_descriptors(std::vector<uint8_t>& image, void* ws, hipStream_t st, Guard* guard);
 
 lt_err compute_units(int* cus);

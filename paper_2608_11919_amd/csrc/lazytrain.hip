@@ -144,6 +144,11 @@ StepLayout step_layout(int K)
 // Images are staged in pinned host slots.  A slot is reused once the copy out of
 // it has run (checked without waiting); when the next slot is still in use, the
 // ring grows by one slot rather than wait, so no call waits on the host.
+//
+// A captured call may have its descriptors written by kernels of the graph (`in_graph`), at
+// every replay.  What such a workspace holds between replays is then unknown on the host: it
+// is marked, and every later call on it writes its descriptors again until
+// lt_workspace_release.
 
 struct WsGuard {
     const uint64_t* at;  // the workspace's tag word
@@ -164,6 +169,7 @@ struct CachedImage {
     uint64_t tag = 0;
     hipEvent_t copied = nullptr;
     hipStream_t stream = nullptr;
+    bool by_graph = false;  // a graph writes other descriptors here when it is replayed
 };
 
 constexpr int kMaxDevices = 64;
@@ -287,10 +293,12 @@ lt_err put_words(const PutWords& a, void* ws, hipStream_t st)
 // Makes the workspace `ws` hold `image` (the bytes of its head; the first
 // kTagBytes are the tag slot, filled here) before the work enqueued next on `st`
 // reads it, and returns the guard that work's kernels check.  `write(words)`
-// enqueues the writing of an image that fits a launch's arguments.
+// enqueues the writing of an image that fits a launch's arguments.  Under capture a
+// call whose descriptors are not in place is refused, or (in_graph; images of whole words)
+// has them written by the graph, 3.5 KB a launch.
 template <typename Write>
 lt_err put_descriptors(std::vector<uint8_t>& image, void* ws, hipStream_t st, WsGuard* guard,
-                       Write write)
+                       Write write, bool in_graph = false)
 {
     int dev;
     if (lt_err e = current_device(&dev))
@@ -303,7 +311,7 @@ lt_err put_descriptors(std::vector<uint8_t>& image, void* ws, hipStream_t st, Ws
     CachedImage& c = ds.cache[ws];
     guard->at = static_cast<const uint64_t*>(ws);
     const size_t n = image.size();
-    if (c.tag != 0 && c.image.size() == n &&
+    if (c.tag != 0 && !c.by_graph && c.image.size() == n &&
         std::memcmp(c.image.data() + kTagBytes, image.data() + kTagBytes, n - kTagBytes) == 0) {
         // Already in place.  Work on another stream waits for the copy; under
         // capture the copy must have completed before capture began (the header
@@ -313,13 +321,27 @@ lt_err put_descriptors(std::vector<uint8_t>& image, void* ws, hipStream_t st, Ws
         guard->tag = c.tag;
         return LT_OK;
     }
-    if (capturing)
+    if (capturing && !in_graph)
         return fail(LT_ERR_INVALID_ARG,
                     "the descriptors of this tensor list are not in the workspace: make one "
                     "uncaptured call with this workspace and list, and let it complete, before "
                     "capturing");
     const uint64_t tag = fresh_tag();
     std::memcpy(image.data(), &tag, sizeof(tag));
+    if (capturing) {
+        PutWords a;
+        for (size_t at = 0; at < n; at += 8 * size_t(kPutWords)) {
+            const size_t bytes = std::min(n - at, 8 * size_t(kPutWords));
+            a.offset = at;
+            a.n = uint32_t(bytes / 8);
+            std::memcpy(a.w, image.data() + at, bytes);
+            if (lt_err e = put_words(a, ws, st))
+                return e;
+        }
+        c.by_graph = true;
+        guard->tag = tag;
+        return LT_OK;
+    }
     if (n <= 8 * size_t(kPutWords) && n % 8 == 0) {
         // The image travels in a launch's arguments: no staging buffer, no event behind
         // the copy and no copy command between two kernels of one stream.  Twelve norm

@@ -25,7 +25,8 @@ lt_err put_descriptors(std::vector<uint8_t>& image, void* ws, hipStream_t st, Gu
 {
     static_assert(kTagBytes == ::kTagBytes, "one tag slot");
     WsGuard g;
-    if (lt_err e = ::put_descriptors(image, ws, st, &g))
+    if (lt_err e = ::put_descriptors(
+            image, ws, st, &g, [&](const PutWords& a) { return put_words(a, ws, st); }, true))
         return e;
     *guard = Guard{g.at, g.tag};
     return LT_OK;

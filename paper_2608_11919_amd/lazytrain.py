@@ -318,6 +318,7 @@ def _scalar(t: Optional[torch.Tensor], device, dtype, what) -> int:
 
 
 _workspaces = {}
+_captured = []  # cached workspaces that captured calls use: a graph may be replayed at any time
 _finalizers = {}
 
 
@@ -341,6 +342,32 @@ def _track(ws: torch.Tensor) -> None:
     _finalizers[key] = weakref.finalize(ws, _forget, ws.data_ptr(), key)
 
 
+def _as_stream(stream, device):
+    """torch's stream object for what a caller may pass as a stream."""
+    if stream is None:
+        return torch.cuda.current_stream(device)
+    if hasattr(stream, "cuda_stream"):
+        return stream
+    return torch.cuda.ExternalStream(int(stream), device=device)
+
+
+def _capturing(stream, device) -> bool:
+    """Whether the stream a call works on is being captured into a graph."""
+    if stream is None and _current(device) is _NO_SWITCH:
+        return torch.cuda.is_current_stream_capturing()
+    with torch.cuda.stream(_as_stream(stream, device)):
+        return torch.cuda.is_current_stream_capturing()
+
+
+def _own(device, nbytes: int, stream) -> torch.Tensor:
+    """Device memory for one call alone, allocated on the stream that uses it, so that nothing
+    else gets it before that call's work has run; under capture it is the graph's."""
+    if stream is None:
+        return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+    with torch.cuda.stream(_as_stream(stream, device)):
+        return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+
+
 def _workspace(device, nbytes: int, workspace: Optional[torch.Tensor], stream,
                kind: str, handle: Optional[int] = None) -> torch.Tensor:
     """The caller's workspace, or one cached per (device, stream, kind of call), so
@@ -348,8 +375,9 @@ def _workspace(device, nbytes: int, workspace: Optional[torch.Tensor], stream,
     library then copies nothing; see include/lazytrain.h).  A cached workspace is
     allocated on the stream that uses it, so that when a larger one replaces it the
     caching allocator hands its memory out again only in that stream's order; the
-    library is told to forget the old one first.  `handle` is the stream's, where the
-    caller has it already."""
+    library is told to forget the old one first.  One that a captured call uses is kept
+    for good: a graph reads and writes it whenever it is replayed.  `handle` is the
+    stream's, where the caller has it already."""
     if workspace is not None:
         if workspace.device != device or workspace.numel() * workspace.element_size() < nbytes:
             raise ValueError(f"workspace must hold {nbytes} bytes on {device}")
@@ -360,17 +388,25 @@ def _workspace(device, nbytes: int, workspace: Optional[torch.Tensor], stream,
     if ws is None or ws.numel() < nbytes:
         if ws is not None:
             lt_workspace_release(ws)
-        if stream is None:
-            s = torch.cuda.current_stream(device)
-        elif hasattr(stream, "cuda_stream"):
-            s = stream
-        else:
-            s = torch.cuda.ExternalStream(int(stream), device=device)
-        with torch.cuda.stream(s):
+        with torch.cuda.stream(_as_stream(stream, device)):
             ws = torch.empty(max(nbytes, 4096), dtype=torch.uint8, device=device)
         _workspaces[key] = ws
         _track(ws)
+    if _capturing(stream, device) and not any(ws is c for c in _captured):
+        _captured.append(ws)
     return ws
+
+
+def _list_workspace(device, nbytes: int, workspace: Optional[torch.Tensor], stream, kind: str,
+                    handle: int) -> torch.Tensor:
+    """The same for calls that a graph can write the descriptors of: a captured one takes memory
+    of the graph's, which lives as long as the graph and which no later call can reach.  To be
+    held until the call is enqueued."""
+    if workspace is None and _capturing(stream, device):
+        ws = _own(device, nbytes, stream)
+        _track(ws)
+        return ws
+    return _workspace(device, nbytes, workspace, stream, kind, handle)
 
 
 # ------------------------------------------------------------------ entry points

@@ -12,7 +12,7 @@ import torch
 from . import lazytrain as _lt
 from .lazytrain import (LT_DTYPE_BF16, LT_DTYPE_F32, LT_MAP_LINEAR, Hybrid8bitAdamW, _List,
                         _bf16_list, _check, _check_block_size, _current, _device_of, _grad_code,
-                        _scalar, _state_ptr, _stream_handle, _workspace, lib)
+                        _list_workspace, _scalar, _state_ptr, _stream_handle, lib)
 
 _DTYPES = {torch.float32: LT_DTYPE_F32, torch.bfloat16: LT_DTYPE_BF16}
 
@@ -65,7 +65,7 @@ def lt_orthogonalize(matrices: Sequence[torch.Tensor], out: Sequence[torch.Tenso
     n = len(matrices)
     nbytes = int(lib().lt_orthogonalize_workspace_bytes(rows, cols, n))
     handle = _stream_handle(stream, device)
-    ws = _workspace(device, nbytes, workspace, stream, "orthogonalize", handle)
+    ws = _list_workspace(device, nbytes, workspace, stream, "orthogonalize", handle)
     with _current(device):
         _check(lib().lt_orthogonalize(
             src.ptrs, _one_dtype(matrices, src, "matrices"), dst.ptrs,
@@ -117,7 +117,7 @@ def lt_muon_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor],
     wb = _bf16_list(params_bf16, params, device, p.numels)
     nbytes = int(lib().lt_muon_workspace_bytes(rows, cols, n, int(block_size)))
     handle = _stream_handle(stream, device)
-    ws = _workspace(device, nbytes, workspace, stream, "muon", handle)
+    ws = _list_workspace(device, nbytes, workspace, stream, "muon", handle)
     with _current(device):
         _check(lib().lt_muon_step(
             p.ptrs, g.ptrs, gdt, mq.ptrs, ma.ptrs, wb, rows, cols, n, int(block_size),
