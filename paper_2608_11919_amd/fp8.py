@@ -9,8 +9,8 @@ from typing import Optional, Tuple
 
 import torch
 
-from .lazytrain import (LT_DTYPE_BF16, LT_DTYPE_F32, _check, _current, _stream_handle, _workspace,
-                        lib)
+from .lazytrain import (LT_DTYPE_BF16, LT_DTYPE_F32, _check, _current, _own, _stream_handle,
+                        _workspace, lib)
 
 _DTYPES = {torch.float32: LT_DTYPE_F32, torch.bfloat16: LT_DTYPE_BF16}
 _BYTES = (torch.uint8, torch.float8_e4m3fn)
@@ -61,14 +61,12 @@ def _layout(codes, scales, rows: int, cols: int, device, what: str) -> Tuple[int
     return codes.data_ptr(), scales.data_ptr()
 
 
-def _scratch(device, nbytes: int, workspace, stream, handle: int) -> Tuple[torch.Tensor, int, int]:
-    """(tensor, address, bytes) of the caller's workspace, or of the cached one.  A call that is
-    being captured gets memory from the graph's pool: a larger call may replace the cached one
-    while the graph lives."""
-    if workspace is None and torch.cuda.is_current_stream_capturing():
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    else:
-        ws = _workspace(device, nbytes, workspace, stream, "fp8", handle)
+def _scratch(device, nbytes: int, workspace, stream) -> Tuple[torch.Tensor, int, int]:
+    """(tensor, address, bytes) of the caller's workspace, or of memory of this call's own: what
+    a call keeps there between its launches is not for another call on the stream to overwrite,
+    from another thread or in a graph's replays."""
+    ws = (_own(device, nbytes, stream) if workspace is None
+          else _workspace(device, nbytes, workspace, stream, "fp8"))
     return ws, ws.data_ptr(), ws.numel() * ws.element_size()
 
 
@@ -105,7 +103,7 @@ def lt_fp8_matmul(a_codes: torch.Tensor, a_scales: torch.Tensor, b_codes: torch.
     ws, nbytes, handle = 0, 0, _stream_handle(stream, device)
     if (m > 32 and k > 512) or workspace is not None:
         nbytes = int(lib().lt_fp8_matmul_workspace_bytes(m, n, k))
-        held, ws, nbytes = _scratch(device, nbytes, workspace, stream, handle)
+        held, ws, nbytes = _scratch(device, nbytes, workspace, stream)
     with _current(device):
         _check(lib().lt_fp8_matmul(a, sa, b, sb, m, n, k, out.data_ptr(), code, stride, ws,
                                    nbytes, handle))
@@ -173,7 +171,7 @@ def fp8_linear(x: torch.Tensor, weight: Fp8Weight,
     ws, nbytes, handle = 0, 0, _stream_handle(None, device)
     if m > 16 or workspace is not None:
         nbytes = int(lib().lt_fp8_linear_workspace_bytes(m, weight.rows, weight.cols))
-        held, ws, nbytes = _scratch(device, nbytes, workspace, None, handle)
+        held, ws, nbytes = _scratch(device, nbytes, workspace, None)
     with _current(device):
         _check(lib().lt_fp8_linear(t.data_ptr(), _dtype_code(t, "x"), stride,
                                    weight.codes.data_ptr(), weight.scales.data_ptr(), m,

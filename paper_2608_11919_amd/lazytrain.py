@@ -13,6 +13,7 @@ import contextlib
 import ctypes
 import math
 import os
+import threading
 import warnings
 import weakref
 from typing import Optional, Sequence
@@ -317,7 +318,16 @@ def _scalar(t: Optional[torch.Tensor], device, dtype, what) -> int:
     return t.data_ptr()
 
 
-_workspaces = {}
+class _Workspaces(threading.local):
+    """Cached workspaces, each host thread's own: what one call enqueues between writing its
+    workspace and reading it again is not one step to another thread on the same stream.  A
+    thread's are freed with it."""
+
+    def __init__(self):
+        self.held = {}
+
+
+_workspaces = _Workspaces()
 _captured = []  # cached workspaces that captured calls use: a graph may be replayed at any time
 _finalizers = {}
 
@@ -370,7 +380,7 @@ def _own(device, nbytes: int, stream) -> torch.Tensor:
 
 def _workspace(device, nbytes: int, workspace: Optional[torch.Tensor], stream,
                kind: str, handle: Optional[int] = None) -> torch.Tensor:
-    """The caller's workspace, or one cached per (device, stream, kind of call), so
+    """The caller's workspace, or one cached per (thread, device, stream, kind of call), so
     that a call repeated over the same tensors finds its descriptors in place (the
     library then copies nothing; see include/lazytrain.h).  A cached workspace is
     allocated on the stream that uses it, so that when a larger one replaces it the
@@ -384,13 +394,14 @@ def _workspace(device, nbytes: int, workspace: Optional[torch.Tensor], stream,
         _track(workspace)
         return workspace
     key = (device, _stream_handle(stream, device) if handle is None else handle, kind)
-    ws = _workspaces.get(key)
+    held = _workspaces.held
+    ws = held.get(key)
     if ws is None or ws.numel() < nbytes:
         if ws is not None:
             lt_workspace_release(ws)
         with torch.cuda.stream(_as_stream(stream, device)):
             ws = torch.empty(max(nbytes, 4096), dtype=torch.uint8, device=device)
-        _workspaces[key] = ws
+        held[key] = ws
         _track(ws)
     if _capturing(stream, device) and not any(ws is c for c in _captured):
         _captured.append(ws)
