@@ -55,7 +55,9 @@
  *    pinned staging buffer (the ring of buffers grows rather than wait for a
  *    copy still in flight).  Between calls the
  *    caller therefore must not write into a workspace; before freeing it or
- *    using its memory for anything else, call lt_workspace_release.  A kernel
+ *    using its memory for anything else, call lt_workspace_release.  (Calls in
+ *    stream order may be given one workspace: f8 and f9, which keep no
+ *    descriptors there, make the library forget what they overwrite.)  A kernel
  *    whose workspace no longer holds the descriptors it was launched for
  *    (checked through a per-copy tag in the workspace's first word) returns
  *    without reading or writing any tensor; lt_grad_sqnorm and

@@ -1057,8 +1057,12 @@ try {
     }
     ProductArgs g{a_codes, a_scales,   b_codes, b_scales,   m,      n, code_pitch(k),
                   scale_pitch(k), int(host::ceil_div(k, kGroup)), w.slice, out, out_stride, nullptr};
-    if (w.slices > 1)
+    if (w.slices > 1) {
         g.partial = static_cast<float*>(workspace);
+        if (lt_err e = host::workspace_written(
+                workspace, size_t(w.slices) * size_t(m) * size_t(n) * 4, st))
+            return e;
+    }
     if (w.tile == 256)
         launch_product<Large>(g, w, f32, st);
     else if (w.tile == 128)
@@ -1128,6 +1132,8 @@ try {
         return LT_OK;
     }
     auto* ws = static_cast<uint8_t*>(workspace);
+    if (lt_err e = host::workspace_written(ws, l.total, static_cast<hipStream_t>(stream)))
+        return e;
     if (lt_err e = lt_fp8_quantize(x, dtype, m, k, x_stride, 0, ws, ws + l.scales, nullptr,
                                    nullptr, stream))
         return e;

@@ -36,6 +36,10 @@ void clear_error();
 // the graph writes it, at every replay.
 lt_err put_descriptors(std::vector<uint8_t>& image, void* ws, hipStream_t st, Guard* guard);
 
+// Before work on the stream writes [ws, ws + bytes) as anything but descriptors: a list call that
+// finds its workspace there writes its descriptors again.
+lt_err workspace_written(const void* ws, size_t bytes, hipStream_t st);
+
 lt_err compute_units(int* cus);
 
 // For an entry point's handler of all exceptions, none of which leaves it: a list that does not

@@ -379,6 +379,31 @@ lt_err put_descriptors(std::vector<uint8_t>& image, void* ws, hipStream_t st, Ws
                            [&](const PutWords& a) { return put_words(a, ws, st); });
 }
 
+// To be called before work on `st` writes [ws, ws + bytes) as anything but descriptors:
+// what the library put there is no longer in place, under capture at no time again.
+lt_err workspace_written(const void* ws, size_t bytes, hipStream_t st)
+{
+    int dev;
+    if (lt_err e = current_device(&dev))
+        return e;
+    bool capturing;
+    if (lt_err e = stream_capturing(st, &capturing))
+        return e;
+    DeviceState& ds = g_dev[dev];
+    std::lock_guard<std::mutex> lock(ds.mu);
+    if (capturing)
+        ds.cache[ws].by_graph = true;
+    const auto lo = reinterpret_cast<uintptr_t>(ws);
+    for (auto& [at, c] : ds.cache) {
+        const auto p = reinterpret_cast<uintptr_t>(at);
+        if (p >= lo + bytes || lo >= p + std::max(c.image.size(), kTagBytes))
+            continue;
+        c.tag = 0;
+        c.by_graph = c.by_graph || capturing;
+    }
+    return LT_OK;
+}
+
 lt_err compute_units(int* cus)
 {
     int dev;

@@ -32,6 +32,11 @@ lt_err put_descriptors(std::vector<uint8_t>& image, void* ws, hipStream_t st, Gu
     return LT_OK;
 }
 
+lt_err workspace_written(const void* ws, size_t bytes, hipStream_t st)
+{
+    return ::workspace_written(ws, bytes, st);
+}
+
 lt_err compute_units(int* cus) { return ::compute_units(cus); }
 
 bool aligned(const void* p, size_t a) { return ::aligned(p, a); }

@@ -9,8 +9,8 @@ from typing import Optional, Tuple
 
 import torch
 
-from .lazytrain import (LT_DTYPE_BF16, LT_DTYPE_F32, _check, _current, _own, _stream_handle,
-                        _workspace, lib)
+from .lazytrain import (LT_DTYPE_BF16, LT_DTYPE_F32, _capturing, _check, _current, _own,
+                        _stream_handle, _track, _workspace, lib)
 
 _DTYPES = {torch.float32: LT_DTYPE_F32, torch.bfloat16: LT_DTYPE_BF16}
 _BYTES = (torch.uint8, torch.float8_e4m3fn)
@@ -65,8 +65,12 @@ def _scratch(device, nbytes: int, workspace, stream) -> Tuple[torch.Tensor, int,
     """(tensor, address, bytes) of the caller's workspace, or of memory of this call's own: what
     a call keeps there between its launches is not for another call on the stream to overwrite,
     from another thread or in a graph's replays."""
-    ws = (_own(device, nbytes, stream) if workspace is None
-          else _workspace(device, nbytes, workspace, stream, "fp8"))
+    if workspace is not None:
+        ws = _workspace(device, nbytes, workspace, stream, "fp8")
+    else:
+        ws = _own(device, nbytes, stream)
+        if _capturing(stream, device):
+            _track(ws)  # the library notes that a graph writes there
     return ws, ws.data_ptr(), ws.numel() * ws.element_size()
 
 
