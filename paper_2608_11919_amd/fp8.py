@@ -219,7 +219,9 @@ def fp8_linear_backward(dy: torch.Tensor, saved, weight: Fp8Weight,
 class Fp8Linear(torch.autograd.Function):
     """``Fp8Linear.apply(x, w, weight)``: x weight^T with gradients for x and for w, the tensor
     (float32 or bfloat16, for instance the optimizer's bf16 copy) that stands for the weight in
-    the graph and whose values ``weight`` was quantized from."""
+    the graph and whose values ``weight`` was quantized from.  First derivatives only: a
+    backward pass that is itself to be differentiated raises, where its gradients depend on
+    what needs one."""
 
     @staticmethod
     def forward(ctx, x, w, weight):
@@ -232,6 +234,10 @@ class Fp8Linear(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dy):
+        # dx depends on dy and w, dw on dy and x, and the products leave no graph
+        if torch.is_grad_enabled() and (dy.requires_grad or all(ctx.needs_input_grad[:2])):
+            raise RuntimeError("Fp8Linear has first derivatives only: its backward pass cannot be "
+                               "part of a graph (create_graph=True)")
         dx, dw = fp8_linear_backward(dy.contiguous(), ctx.saved_tensors, ctx.weight,
                                      out_dtype=dy.dtype, grad_dtype=ctx.w_dtype)
         return dx, dw, None
