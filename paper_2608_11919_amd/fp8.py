@@ -8,6 +8,7 @@ from __future__ import annotations
 from typing import Optional, Tuple
 
 import torch
+from torch.autograd.graph import increment_version
 
 from .lazytrain import (LT_DTYPE_BF16, LT_DTYPE_F32, _capturing, _check, _current, _own,
                         _stream_handle, _track, _workspace, lib)
@@ -91,6 +92,8 @@ def lt_fp8_quantize(x: torch.Tensor, codes: Optional[torch.Tensor] = None,
     with _current(device):
         _check(lib().lt_fp8_quantize(x.data_ptr(), code, rows, cols, stride, int(bool(square)), c,
                                      s, ct, st, _stream_handle(stream, device)))
+    # autograd's in-place rule: a graph that saved one of these has lost its values
+    increment_version([t for t in (codes, scales, codes_t, scales_t) if t is not None])
 
 
 def lt_fp8_matmul(a_codes: torch.Tensor, a_scales: torch.Tensor, b_codes: torch.Tensor,
@@ -204,32 +207,40 @@ def fp8_linear_backward(dy: torch.Tensor, saved, weight: Fp8Weight,
     x in_features) in grad_dtype."""
     if weight.codes_t is None:
         raise ValueError("the weight has no transposed codes: the backward pass needs them")
-    t = _tokens(dy, weight.rows, "dy")
+    return _gradients(dy, saved, (weight.codes_t, weight.scales_t), weight.rows, weight.cols,
+                      out_dtype, grad_dtype)
+
+
+def _gradients(dy, saved, transposed, rows: int, cols: int, out_dtype, grad_dtype):
+    """dx and dw from dy, the transpose of x and that of the weight, as codes and scales."""
+    t = _tokens(dy, rows, "dy")
     tokens, device = t.shape[0], dy.device
-    codes, scales = _empty(tokens, weight.rows, device)
-    codes_t, scales_t = _empty(weight.rows, tokens, device)
+    codes, scales = _empty(tokens, rows, device)
+    codes_t, scales_t = _empty(rows, tokens, device)
     lt_fp8_quantize(t, codes, scales, codes_t, scales_t)
-    dx = torch.empty(tokens, weight.cols, dtype=out_dtype, device=device)
-    lt_fp8_matmul(codes, scales, weight.codes_t, weight.scales_t, weight.rows, dx)
-    dw = torch.empty(weight.rows, weight.cols, dtype=grad_dtype, device=device)
-    lt_fp8_matmul(codes_t, scales_t, saved[0], saved[1], tokens, dw)
-    return dx.view(*dy.shape[:-1], weight.cols), dw
+    dx = torch.empty(tokens, cols, dtype=out_dtype, device=device)
+    lt_fp8_matmul(codes, scales, *transposed, rows, dx)
+    dw = torch.empty(rows, cols, dtype=grad_dtype, device=device)
+    lt_fp8_matmul(codes_t, scales_t, *saved, tokens, dw)
+    return dx.view(*dy.shape[:-1], cols), dw
 
 
 class Fp8Linear(torch.autograd.Function):
     """``Fp8Linear.apply(x, w, weight)``: x weight^T with gradients for x and for w, the tensor
     (float32 or bfloat16, for instance the optimizer's bf16 copy) that stands for the weight in
-    the graph and whose values ``weight`` was quantized from.  First derivatives only: a
-    backward pass that is itself to be differentiated raises, where its gradients depend on
-    what needs one."""
+    the graph and whose values ``weight`` was quantized from.  The gradient for x reads the
+    weight's codes again: once ``weight`` is updated, a backward pass of a forward pass before
+    raises, like autograd's own after a change in place.  First derivatives only: a backward
+    pass that is itself to be differentiated raises, where its gradients depend on what needs
+    one."""
 
     @staticmethod
     def forward(ctx, x, w, weight):
         if tuple(w.shape) != (weight.rows, weight.cols):
             raise ValueError(f"w must have shape {(weight.rows, weight.cols)}")
-        y, (codes_t, scales_t) = fp8_linear_forward(x, weight, out_dtype=x.dtype)
-        ctx.save_for_backward(codes_t, scales_t)
-        ctx.weight, ctx.w_dtype = weight, w.dtype
+        y, saved = fp8_linear_forward(x, weight, out_dtype=x.dtype)
+        ctx.save_for_backward(*saved, weight.codes_t, weight.scales_t)
+        ctx.sizes, ctx.w_dtype = (weight.rows, weight.cols), w.dtype
         return y
 
     @staticmethod
@@ -238,6 +249,9 @@ class Fp8Linear(torch.autograd.Function):
         if torch.is_grad_enabled() and (dy.requires_grad or all(ctx.needs_input_grad[:2])):
             raise RuntimeError("Fp8Linear has first derivatives only: its backward pass cannot be "
                                "part of a graph (create_graph=True)")
-        dx, dw = fp8_linear_backward(dy.contiguous(), ctx.saved_tensors, ctx.weight,
-                                     out_dtype=dy.dtype, grad_dtype=ctx.w_dtype)
+        x_t, x_scales_t, w_t, w_scales_t = ctx.saved_tensors
+        if w_t is None:
+            raise ValueError("the weight has no transposed codes: the backward pass needs them")
+        dx, dw = _gradients(dy.contiguous(), (x_t, x_scales_t), (w_t, w_scales_t), *ctx.sizes,
+                            dy.dtype, ctx.w_dtype)
         return dx, dw, None

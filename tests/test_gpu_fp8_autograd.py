@@ -46,3 +46,50 @@ def test_gradients_that_are_constant_may_be_part_of_a_graph():
     assert torch.equal(g.detach(), want + 3 * x.detach().square())
     second, = torch.autograd.grad(g.sum(), x)
     assert torch.allclose(second, 6 * x.detach())
+
+
+# ------------------------------------------------------- a weight that changed since
+
+def updated(weight, w):
+    weight.update(w.detach() * 2)
+
+
+def requantized(weight, w):
+    lt.lt_fp8_quantize(w.detach() * 2, codes_t=weight.codes_t, scales_t=weight.scales_t,
+                       square=True)
+
+
+def written(weight, w):
+    weight.codes_t.zero_()
+
+
+@pytest.mark.parametrize("change", [updated, requantized, written])
+def test_a_weight_that_changed_since_the_forward_pass(change):
+    x, w, weight = layer()
+    y = lt.Fp8Linear.apply(x, w, weight)
+    y.sum().backward(retain_graph=True)
+    change(weight, w)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+
+
+def test_a_weight_updated_between_steps():
+    """Forward, backward, update, and again: as with weights of their own."""
+    x, w, weight = layer(33, 200, 130, torch.bfloat16)
+    for turn in range(3):
+        master = draw(w.shape, 50 + turn)
+        weight.update(master)
+        got = torch.autograd.grad(lt.Fp8Linear.apply(x, w, weight).square().sum(), (x, w))
+        fresh = lt.Fp8Weight.from_master(master)
+        want = torch.autograd.grad(lt.Fp8Linear.apply(x, w, fresh).square().sum(), (x, w))
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_weights_are_updated_in_inference_mode_too():
+    x, w, weight = layer()
+    with torch.inference_mode():
+        weight.update(w)
+        other = lt.Fp8Weight.from_master(w)
+        other.update(w)
+        assert torch.equal(lt.fp8_linear(x, weight), lt.fp8_linear(x, other))
+    lt.Fp8Linear.apply(x, w, weight).sum().backward()
