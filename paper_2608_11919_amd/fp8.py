@@ -212,17 +212,21 @@ def fp8_linear_backward(dy: torch.Tensor, saved, weight: Fp8Weight,
 
 
 def _gradients(dy, saved, transposed, rows: int, cols: int, out_dtype, grad_dtype):
-    """dx and dw from dy, the transpose of x and that of the weight, as codes and scales."""
+    """dx (None without the weight's) and dw from dy, the transpose of x and that of the weight,
+    as codes and scales."""
     t = _tokens(dy, rows, "dy")
     tokens, device = t.shape[0], dy.device
     codes, scales = _empty(tokens, rows, device)
     codes_t, scales_t = _empty(rows, tokens, device)
     lt_fp8_quantize(t, codes, scales, codes_t, scales_t)
-    dx = torch.empty(tokens, cols, dtype=out_dtype, device=device)
-    lt_fp8_matmul(codes, scales, *transposed, rows, dx)
+    dx = None
+    if transposed is not None:
+        dx = torch.empty(tokens, cols, dtype=out_dtype, device=device)
+        lt_fp8_matmul(codes, scales, *transposed, rows, dx)
+        dx = dx.view(*dy.shape[:-1], cols)
     dw = torch.empty(rows, cols, dtype=grad_dtype, device=device)
     lt_fp8_matmul(codes_t, scales_t, *saved, tokens, dw)
-    return dx.view(*dy.shape[:-1], cols), dw
+    return dx, dw
 
 
 class Fp8Linear(torch.autograd.Function):
@@ -238,6 +242,10 @@ class Fp8Linear(torch.autograd.Function):
     def forward(ctx, x, w, weight):
         if tuple(w.shape) != (weight.rows, weight.cols):
             raise ValueError(f"w must have shape {(weight.rows, weight.cols)}")
+        if ctx.needs_input_grad[0] and weight.codes_t is None:
+            raise ValueError("the weight has no transposed codes: the gradient for x needs them")
+        if ctx.needs_input_grad[1]:
+            _dtype_code(w, "w")  # its gradient's
         y, saved = fp8_linear_forward(x, weight, out_dtype=x.dtype)
         ctx.save_for_backward(*saved, weight.codes_t, weight.scales_t)
         ctx.sizes, ctx.w_dtype = (weight.rows, weight.cols), w.dtype
@@ -250,8 +258,7 @@ class Fp8Linear(torch.autograd.Function):
             raise RuntimeError("Fp8Linear has first derivatives only: its backward pass cannot be "
                                "part of a graph (create_graph=True)")
         x_t, x_scales_t, w_t, w_scales_t = ctx.saved_tensors
-        if w_t is None:
-            raise ValueError("the weight has no transposed codes: the backward pass needs them")
-        dx, dw = _gradients(dy.contiguous(), (x_t, x_scales_t), (w_t, w_scales_t), *ctx.sizes,
-                            dy.dtype, ctx.w_dtype)
+        transposed = (w_t, w_scales_t) if ctx.needs_input_grad[0] else None
+        dx, dw = _gradients(dy.contiguous(), (x_t, x_scales_t), transposed, *ctx.sizes, dy.dtype,
+                            ctx.w_dtype)
         return dx, dw, None

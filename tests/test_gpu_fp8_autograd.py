@@ -93,3 +93,24 @@ def test_weights_are_updated_in_inference_mode_too():
         other.update(w)
         assert torch.equal(lt.fp8_linear(x, weight), lt.fp8_linear(x, other))
     lt.Fp8Linear.apply(x, w, weight).sum().backward()
+
+
+# ------------------------------------------------------------------ refusals
+
+def test_a_weight_without_transposed_codes_is_refused_at_once():
+    x, w, weight = layer()
+    bare = lt.Fp8Weight.from_master(w.detach(), transposed=False)
+    with pytest.raises(ValueError, match="transposed"):
+        lt.Fp8Linear.apply(x, w, bare)
+    # the gradient for w does not read them
+    got, = torch.autograd.grad(lt.Fp8Linear.apply(x.detach(), w, bare).square().sum(), w)
+    want, = torch.autograd.grad(lt.Fp8Linear.apply(x.detach(), w, weight).square().sum(), w)
+    assert torch.equal(got, want)
+
+
+def test_a_weight_whose_gradient_has_no_type_is_refused_at_once():
+    x, w, weight = layer()
+    with pytest.raises(TypeError):
+        lt.Fp8Linear.apply(x, w.detach().half().requires_grad_(), weight)
+    with pytest.raises(ValueError):
+        lt.Fp8Linear.apply(x, w.detach()[:8], weight)
