@@ -191,9 +191,14 @@ def fp8_linear_forward(x: torch.Tensor, weight: Fp8Weight,
                        out_dtype: torch.dtype = torch.bfloat16):
     """As fp8_linear, and what the backward pass needs of x: its transpose, quantized along the
     tokens (one byte a value)."""
+    return _answer(x, weight, out_dtype, True)
+
+
+def _answer(x, weight: Fp8Weight, out_dtype, keep: bool):
+    """y, and x's transpose (codes and scales) where it is to be kept."""
     t = _tokens(x, weight.cols, "x")
     codes, scales = _empty(t.shape[0], weight.cols, x.device)
-    saved = _empty(weight.cols, t.shape[0], x.device)
+    saved = _empty(weight.cols, t.shape[0], x.device) if keep else (None, None)
     lt_fp8_quantize(t, codes, scales, *saved)
     y = torch.empty(t.shape[0], weight.rows, dtype=out_dtype, device=x.device)
     lt_fp8_matmul(codes, scales, weight.codes, weight.scales, weight.cols, y)
@@ -212,20 +217,22 @@ def fp8_linear_backward(dy: torch.Tensor, saved, weight: Fp8Weight,
 
 
 def _gradients(dy, saved, transposed, rows: int, cols: int, out_dtype, grad_dtype):
-    """dx (None without the weight's) and dw from dy, the transpose of x and that of the weight,
-    as codes and scales."""
+    """dx (None without the weight's transpose) and dw (None without x's) from dy, the operands
+    as codes and scales; dy is laid out for what is asked for."""
     t = _tokens(dy, rows, "dy")
     tokens, device = t.shape[0], dy.device
-    codes, scales = _empty(tokens, rows, device)
-    codes_t, scales_t = _empty(rows, tokens, device)
-    lt_fp8_quantize(t, codes, scales, codes_t, scales_t)
-    dx = None
+    dx = dw = None
+    by_rows = _empty(tokens, rows, device) if transposed is not None else (None, None)
+    turned = _empty(rows, tokens, device) if saved is not None else (None, None)
+    if transposed is not None or saved is not None:
+        lt_fp8_quantize(t, *by_rows, *turned)
     if transposed is not None:
         dx = torch.empty(tokens, cols, dtype=out_dtype, device=device)
-        lt_fp8_matmul(codes, scales, *transposed, rows, dx)
+        lt_fp8_matmul(*by_rows, *transposed, rows, dx)
         dx = dx.view(*dy.shape[:-1], cols)
-    dw = torch.empty(rows, cols, dtype=grad_dtype, device=device)
-    lt_fp8_matmul(codes_t, scales_t, *saved, tokens, dw)
+    if saved is not None:
+        dw = torch.empty(rows, cols, dtype=grad_dtype, device=device)
+        lt_fp8_matmul(*turned, *saved, tokens, dw)
     return dx, dw
 
 
@@ -246,8 +253,10 @@ class Fp8Linear(torch.autograd.Function):
             raise ValueError("the weight has no transposed codes: the gradient for x needs them")
         if ctx.needs_input_grad[1]:
             _dtype_code(w, "w")  # its gradient's
-        y, saved = fp8_linear_forward(x, weight, out_dtype=x.dtype)
-        ctx.save_for_backward(*saved, weight.codes_t, weight.scales_t)
+        y, saved = _answer(x, weight, x.dtype, ctx.needs_input_grad[1])
+        transposed = ((weight.codes_t, weight.scales_t) if ctx.needs_input_grad[0]
+                      else (None, None))
+        ctx.save_for_backward(*saved, *transposed)
         ctx.sizes, ctx.w_dtype = (weight.rows, weight.cols), w.dtype
         return y
 
@@ -258,7 +267,7 @@ class Fp8Linear(torch.autograd.Function):
             raise RuntimeError("Fp8Linear has first derivatives only: its backward pass cannot be "
                                "part of a graph (create_graph=True)")
         x_t, x_scales_t, w_t, w_scales_t = ctx.saved_tensors
+        saved = (x_t, x_scales_t) if ctx.needs_input_grad[1] else None
         transposed = (w_t, w_scales_t) if ctx.needs_input_grad[0] else None
-        dx, dw = _gradients(dy.contiguous(), (x_t, x_scales_t), transposed, *ctx.sizes, dy.dtype,
-                            ctx.w_dtype)
+        dx, dw = _gradients(dy.contiguous(), saved, transposed, *ctx.sizes, dy.dtype, ctx.w_dtype)
         return dx, dw, None

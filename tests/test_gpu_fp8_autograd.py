@@ -114,3 +114,44 @@ def test_a_weight_whose_gradient_has_no_type_is_refused_at_once():
         lt.Fp8Linear.apply(x, w.detach().half().requires_grad_(), weight)
     with pytest.raises(ValueError):
         lt.Fp8Linear.apply(x, w.detach()[:8], weight)
+
+
+# ---------------------------------------------------------- only what is asked for
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("asked", [(True, False), (False, True), (False, False), (True, True)])
+def test_only_the_layouts_and_products_that_are_asked_for(asked, dtype, monkeypatch):
+    from paper_2608_11919_amd import fp8
+    x, w, weight = layer(40, 300, 130, dtype)
+    want = torch.autograd.grad(lt.Fp8Linear.apply(x, w, weight).square().sum(), (x, w))
+    layouts, products = [], []
+    quantize, matmul = fp8.lt_fp8_quantize, fp8.lt_fp8_matmul
+
+    def count_layouts(t, codes=None, scales=None, codes_t=None, scales_t=None, **kw):
+        layouts.append((codes is not None, codes_t is not None))
+        quantize(t, codes, scales, codes_t, scales_t, **kw)
+
+    def count_products(*args, **kw):
+        products.append(args[5].shape)
+        matmul(*args, **kw)
+
+    monkeypatch.setattr(fp8, "lt_fp8_quantize", count_layouts)
+    monkeypatch.setattr(fp8, "lt_fp8_matmul", count_products)
+    x2, w2 = x.detach().requires_grad_(asked[0]), w.detach().requires_grad_(asked[1])
+    y = lt.Fp8Linear.apply(x2, w2, weight)
+    assert layouts == [(True, asked[1])] and products == [(40, 130)]
+    if any(asked):
+        y.square().sum().backward()
+        assert layouts[1:] == [asked]
+        assert products[1:] == [s for s, a in (((40, 300), asked[0]), ((130, 300), asked[1])) if a]
+    for t, g, a in ((x2, want[0], asked[0]), (w2, want[1], asked[1])):
+        assert (t.grad is None) if not a else torch.equal(t.grad, g)
+
+
+def test_a_gradient_that_does_not_read_the_weight_survives_its_update():
+    x, w, weight = layer()
+    want, = torch.autograd.grad(lt.Fp8Linear.apply(x.detach(), w, weight).sum(), w)
+    y = lt.Fp8Linear.apply(x.detach(), w, weight)
+    updated(weight, w)
+    got, = torch.autograd.grad(y.sum(), w)
+    assert torch.equal(got, want)
