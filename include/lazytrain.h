@@ -585,8 +585,8 @@ lt_err lt_fp8_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const uint
 size_t lt_fp8_linear_workspace_bytes(int64_t m, int64_t n, int64_t k);
 
 /*
- * f9: a linear layer's answer, out = x W^T: x (m x k, dtype, x_stride elements from row to row)
- * is quantized on the way, W (n x k) is as lt_fp8_quantize stores it.  The same values as
+ * f9: a linear layer's answer, out = x W^T: x (m x k, dtype, x_stride elements from row to row,
+ * beginning at any element's address) is quantized on the way, W (n x k) is as lt_fp8_quantize stores it.  The same values as
  * lt_fp8_quantize and lt_fp8_matmul, but where a sum is cut into other pieces; up to 16 rows
  * of x take one launch.
  */

@@ -900,6 +900,41 @@ void launch_few_tokens(const FewArgs& g, bool f32, int cus, hipStream_t st)
     }
 }
 
+// The quantizer's launch, its arguments checked; x at any element's address.
+lt_err launch_quantize(const void* x, int dtype, int64_t rows, int64_t cols, int64_t row_stride,
+                       bool square, uint8_t* codes, uint8_t* scales, uint8_t* codes_t,
+                       uint8_t* scales_t, hipStream_t st)
+{
+    QuantizeArgs a{x,
+                   rows,
+                   cols,
+                   row_stride,
+                   codes,
+                   scales,
+                   codes_t,
+                   scales_t,
+                   code_pitch(cols),
+                   scale_pitch(cols),
+                   code_pitch(rows),
+                   scale_pitch(rows),
+                   int(host::ceil_div(cols, kGroup))};
+    const dim3 grid(uint32_t(host::ceil_div(rows, kGroup) * a.across));
+    const int64_t by_rows = host::ceil_div(rows * (a.scale_pitch / 4), kQuantizeThreads / 64);
+    if (!codes_t && !square && by_rows < kMostGroups) {
+        auto* kernel = dtype == LT_DTYPE_BF16 ? k_fp8_quantize_rows<uint16_t>
+                                              : k_fp8_quantize_rows<float>;
+        kernel<<<dim3(uint32_t(by_rows)), kQuantizeThreads, 0, st>>>(a);
+        LT_TRY_HIP(hipGetLastError());
+        return LT_OK;
+    }
+    auto* kernel = dtype == LT_DTYPE_BF16
+                       ? (square ? k_fp8_quantize<uint16_t, true> : k_fp8_quantize<uint16_t, false>)
+                       : (square ? k_fp8_quantize<float, true> : k_fp8_quantize<float, false>);
+    kernel<<<grid, kQuantizeThreads, 0, st>>>(a);
+    LT_TRY_HIP(hipGetLastError());
+    return LT_OK;
+}
+
 // Workspace of lt_fp8_linear where x is quantized apart: [codes][scales][matmul's].
 struct LinearLayout {
     size_t scales, matmul, total;
@@ -960,35 +995,8 @@ try {
     const std::string overlap = host::overlap(ranges);
     if (!overlap.empty())
         return fail(LT_ERR_INVALID_ARG, overlap);
-    QuantizeArgs a{x,
-                   rows,
-                   cols,
-                   row_stride,
-                   codes,
-                   scales,
-                   codes_t,
-                   scales_t,
-                   code_pitch(cols),
-                   scale_pitch(cols),
-                   code_pitch(rows),
-                   scale_pitch(rows),
-                   int(host::ceil_div(cols, kGroup))};
-    const dim3 grid(uint32_t(host::ceil_div(rows, kGroup) * a.across));
-    const hipStream_t st = static_cast<hipStream_t>(stream);
-    const int64_t by_rows = host::ceil_div(rows * (a.scale_pitch / 4), kQuantizeThreads / 64);
-    if (!codes_t && !square && by_rows < kMostGroups) {
-        auto* kernel = dtype == LT_DTYPE_BF16 ? k_fp8_quantize_rows<uint16_t>
-                                              : k_fp8_quantize_rows<float>;
-        kernel<<<dim3(uint32_t(by_rows)), kQuantizeThreads, 0, st>>>(a);
-        LT_TRY_HIP(hipGetLastError());
-        return LT_OK;
-    }
-    auto* kernel = dtype == LT_DTYPE_BF16
-                       ? (square ? k_fp8_quantize<uint16_t, true> : k_fp8_quantize<uint16_t, false>)
-                       : (square ? k_fp8_quantize<float, true> : k_fp8_quantize<float, false>);
-    kernel<<<grid, kQuantizeThreads, 0, st>>>(a);
-    LT_TRY_HIP(hipGetLastError());
-    return LT_OK;
+    return launch_quantize(x, dtype, rows, cols, row_stride, square != 0, codes, scales, codes_t,
+                           scales_t, static_cast<hipStream_t>(stream));
 } catch (...) {
     return host::caught();
 }
@@ -1101,9 +1109,10 @@ try {
         return LT_OK;
     if (!out || (k > 0 && (!x || !w_codes || !w_scales)))
         return fail(LT_ERR_INVALID_ARG, "x, the weight and out must not be NULL");
-    if (!host::aligned(x, 16) || !host::aligned(w_codes, 16) || !host::aligned(out, 16) ||
-        !host::aligned(w_scales, 4))
-        return fail(LT_ERR_ALIGNMENT, "x, codes and out must be 16-byte aligned, scales 4-byte");
+    if (!host::aligned(x, dtype == LT_DTYPE_BF16 ? 2 : 4) || !host::aligned(w_codes, 16) ||
+        !host::aligned(out, 16) || !host::aligned(w_scales, 4))
+        return fail(LT_ERR_ALIGNMENT, "x must be aligned to its elements, codes and out to 16 "
+                                      "bytes, scales to 4");
     if (k == 0)
         return lt_fp8_matmul(nullptr, nullptr, nullptr, nullptr, m, n, k, out, out_dtype,
                              out_stride, nullptr, 0, stream);
@@ -1134,8 +1143,8 @@ try {
     auto* ws = static_cast<uint8_t*>(workspace);
     if (lt_err e = host::workspace_written(ws, l.total, static_cast<hipStream_t>(stream)))
         return e;
-    if (lt_err e = lt_fp8_quantize(x, dtype, m, k, x_stride, 0, ws, ws + l.scales, nullptr,
-                                   nullptr, stream))
+    if (lt_err e = launch_quantize(x, dtype, m, k, x_stride, false, ws, ws + l.scales, nullptr,
+                                   nullptr, static_cast<hipStream_t>(stream)))
         return e;
     return lt_fp8_matmul(ws, ws + l.scales, w_codes, w_scales, m, n, k, out, out_dtype, out_stride,
                          ws + l.matmul, l.total - l.matmul, stream);

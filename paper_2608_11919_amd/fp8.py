@@ -10,7 +10,7 @@ from typing import Optional, Tuple
 import torch
 from torch.autograd.graph import increment_version
 
-from .lazytrain import (LT_DTYPE_BF16, LT_DTYPE_F32, _capturing, _check, _current, _own,
+from .lazytrain import (LT_DTYPE_BF16, LT_DTYPE_F32, _capturing, _check, _current, _on, _own,
                         _stream_handle, _track, _workspace, lib)
 
 _DTYPES = {torch.float32: LT_DTYPE_F32, torch.bfloat16: LT_DTYPE_BF16}
@@ -140,7 +140,8 @@ class Fp8Weight:
     @classmethod
     def from_master(cls, w: torch.Tensor, transposed: bool = True) -> "Fp8Weight":
         """Quantizes a weight matrix (float32 or bfloat16) on the current stream."""
-        _rows(w, "w")
+        if w.dim() != 2:
+            raise ValueError(f"w must be a matrix (two dimensions, got {w.dim()})")
         weight = cls.empty(w.shape[0], w.shape[1], w.device, transposed)
         weight.update(w)
         return weight
@@ -148,8 +149,9 @@ class Fp8Weight:
     def update(self, w: torch.Tensor, stream=None) -> None:
         if tuple(w.shape) != (self.rows, self.cols):
             raise ValueError(f"w must have shape {(self.rows, self.cols)}")
-        lt_fp8_quantize(w, self.codes, self.scales, self.codes_t, self.scales_t, square=True,
-                        stream=stream)
+        with _on(stream, w.device):  # a copy of w belongs to the stream that reads it
+            w = _laid_out(w)
+            lt_fp8_quantize(w, self.codes, self.scales, self.codes_t, self.scales_t, square=True)
 
 
 def _empty(rows: int, cols: int, device):
@@ -157,10 +159,20 @@ def _empty(rows: int, cols: int, device):
             torch.empty(rows, lt_fp8_scale_pitch(cols), dtype=torch.uint8, device=device))
 
 
-def _tokens(x: torch.Tensor, features: int, what: str) -> torch.Tensor:
+def _laid_out(t: torch.Tensor, aligned: bool = True) -> torch.Tensor:
+    """A matrix as the library takes it: rows contiguous and apart, beginning on 16 bytes (not
+    `aligned`: anywhere).  Any other is copied: transposed or broadcast tokens, part of a packed
+    batch at an odd width."""
+    if ((t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]) or
+            (aligned and t.data_ptr() % 16)):
+        return t.clone(memory_format=torch.contiguous_format)
+    return t
+
+
+def _tokens(x: torch.Tensor, features: int, what: str, aligned: bool = True) -> torch.Tensor:
     if x.dim() < 1 or x.shape[-1] != features:
         raise ValueError(f"{what} must have {features} features, got shape {tuple(x.shape)}")
-    return x if x.dim() == 2 else x.reshape(-1, features)
+    return _laid_out(x if x.dim() == 2 else x.reshape(-1, features), aligned)
 
 
 def fp8_linear(x: torch.Tensor, weight: Fp8Weight,
@@ -169,7 +181,7 @@ def fp8_linear(x: torch.Tensor, weight: Fp8Weight,
     """f9: x weight^T for x (..., in_features), quantized on the way; for answering: nothing is
     kept for a backward pass.  This and the functions below allocate and work on the current
     stream."""
-    t = _tokens(x, weight.cols, "x")
+    t = _tokens(x, weight.cols, "x", aligned=False)
     stride = _rows(t, "x")
     m, device = t.shape[0], x.device
     if weight.codes.device != device:
@@ -269,5 +281,5 @@ class Fp8Linear(torch.autograd.Function):
         x_t, x_scales_t, w_t, w_scales_t = ctx.saved_tensors
         saved = (x_t, x_scales_t) if ctx.needs_input_grad[1] else None
         transposed = (w_t, w_scales_t) if ctx.needs_input_grad[0] else None
-        dx, dw = _gradients(dy.contiguous(), saved, transposed, *ctx.sizes, dy.dtype, ctx.w_dtype)
+        dx, dw = _gradients(dy, saved, transposed, *ctx.sizes, dy.dtype, ctx.w_dtype)
         return dx, dw, None

@@ -361,20 +361,21 @@ def _as_stream(stream, device):
     return torch.cuda.ExternalStream(int(stream), device=device)
 
 
+def _on(stream, device):
+    """Makes the stream a call works on the current one, and `device` the current device."""
+    return _current(device) if stream is None else torch.cuda.stream(_as_stream(stream, device))
+
+
 def _capturing(stream, device) -> bool:
     """Whether the stream a call works on is being captured into a graph."""
-    if stream is None and _current(device) is _NO_SWITCH:
-        return torch.cuda.is_current_stream_capturing()
-    with torch.cuda.stream(_as_stream(stream, device)):
+    with _on(stream, device):
         return torch.cuda.is_current_stream_capturing()
 
 
 def _own(device, nbytes: int, stream) -> torch.Tensor:
     """Device memory for one call alone, allocated on the stream that uses it, so that nothing
     else gets it before that call's work has run; under capture it is the graph's."""
-    if stream is None:
-        return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
-    with torch.cuda.stream(_as_stream(stream, device)):
+    with _on(stream, device):
         return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
 
 
@@ -399,7 +400,7 @@ def _workspace(device, nbytes: int, workspace: Optional[torch.Tensor], stream,
     if ws is None or ws.numel() < nbytes:
         if ws is not None:
             lt_workspace_release(ws)
-        with torch.cuda.stream(_as_stream(stream, device)):
+        with _on(stream, device):
             ws = torch.empty(max(nbytes, 4096), dtype=torch.uint8, device=device)
         held[key] = ws
         _track(ws)
