@@ -529,6 +529,8 @@ size_t lt_muon_workspace_bytes(const int64_t* rows, const int64_t* cols, int n_m
  * the update's, in units of lr (0.2 is about AdamW's).
  * lr, weight_decay >= 0, 0 <= momentum < 1, update_rms > 0, all finite; ns_steps in [1, 64].
  * A skipped step writes nothing but the bf16 copy, which then holds the unchanged weights.
+ * The workspace is looked at last: a call without one enqueues nothing and returns
+ * LT_ERR_WORKSPACE if nothing else is to be refused.
  */
 lt_err lt_muon_step(float* const* params, const void* const* grads, int grad_dtype,
                     int8_t* const* m_codes, float* const* m_absmax, uint16_t* const* params_bf16,

@@ -881,8 +881,13 @@ class Hybrid8bitAdamW:
         """Indices of the parameters that AdamW leaves to _step_elsewhere (a subclass's)."""
         return frozenset()
 
-    def _step_elsewhere(self, grads, stream) -> None:
-        pass
+    def _prepare_elsewhere(self, grads, stream):
+        """That step with everything checked and its memory in hand, before AdamW's are enqueued:
+        a step that is refused changes no parameter."""
+        return None
+
+    def _step_elsewhere(self, prepared) -> None:
+        """Enqueues it."""
 
     # ------------------------------------------------------------ step state
     def _reset_state(self, applied: int, skips: int, stream=None) -> None:
@@ -982,6 +987,7 @@ class Hybrid8bitAdamW:
         self._raise_if_stopped()
         if self._bound + 1 > self._table_len:
             self._grow_state(stream)
+        prepared = self._prepare_elsewhere(grads, stream)
         lt_grad_sqnorm(grads, self.sq_total, self.status, stream=stream)
         clip = self.max_norm if self.max_norm is not None else math.inf
         lt_clip_coef(self.sq_total, clip, self.coef, self.total_norm, stream=stream)
@@ -1000,7 +1006,7 @@ class Hybrid8bitAdamW:
                                [grads[i] for i in self.idx32], self.exp_avg, self.exp_avg_sq,
                                params_bf16=None if wb is None else [wb[i] for i in self.idx32],
                                **hyper)
-        self._step_elsewhere(grads, stream)
+        self._step_elsewhere(prepared)
         lt_step_state_advance(self._state, self.status, stream=stream)
         self._bound += 1
         # a snapshot of the count and the status, read later without waiting

@@ -10,9 +10,10 @@ from typing import Optional, Sequence
 import torch
 
 from . import lazytrain as _lt
-from .lazytrain import (LT_DTYPE_BF16, LT_DTYPE_F32, LT_MAP_LINEAR, Hybrid8bitAdamW, _List,
-                        _bf16_list, _check, _check_block_size, _current, _device_of, _grad_code,
-                        _list_workspace, _scalar, _state_ptr, _stream_handle, lib)
+from .lazytrain import (LT_DTYPE_BF16, LT_DTYPE_F32, LT_ERR_WORKSPACE, LT_MAP_LINEAR,
+                        Hybrid8bitAdamW, _List, _bf16_list, _check, _check_block_size, _current,
+                        _device_of, _grad_code, _list_workspace, _scalar, _state_ptr,
+                        _stream_handle, lib)
 
 _DTYPES = {torch.float32: LT_DTYPE_F32, torch.bfloat16: LT_DTYPE_BF16}
 
@@ -79,6 +80,66 @@ def lt_muon_workspace_bytes(rows: Sequence[int], cols: Sequence[int], block_size
                                              (ctypes.c_int64 * n)(*cols), n, int(block_size)))
 
 
+class _MuonCall:
+    """A Muon step's arguments, checked as far as the binding does, with its workspace: run()
+    enqueues it, check() has the library refuse what it would, and enqueues nothing."""
+
+    __slots__ = ("device", "args", "workspace", "handle", "held")
+
+    def __init__(self, params, grads, m_codes, m_absmax, block_size, lr, momentum=0.95,
+                 weight_decay=0.0, ns_steps=5, nesterov=True, update_rms=0.2, coef=None,
+                 status=None, workspace=None, stream=None, params_bf16=None,
+                 code_map=LT_MAP_LINEAR, step_state=None):
+        n = len(params)
+        if not (len(grads) == len(m_codes) == len(m_absmax) == n):
+            raise ValueError("tensor lists must be of equal length")
+        device = _device_of(params, coef, status)
+        p = _List(params, device, torch.float32, "params")
+        g = _List(grads, device, what="grads")
+        mq = _List(m_codes, device, torch.int8, "m_codes")
+        ma = _List(m_absmax, device, torch.float32, "m_absmax")
+        gdt = _grad_code(grads, g)
+        _check_block_size(block_size)
+        rows, cols = _sides(params, "params")
+        if _lt._lists.sides(grads) != (rows, cols):
+            for i in range(n):  # a gradient may be flat, but no matrix of another shape
+                if grads[i].dim() != 1 and grads[i].shape != params[i].shape:
+                    raise ValueError(f"grads[{i}] must have shape {tuple(params[i].shape)}")
+        if not (g.numels == p.numels == mq.numels and
+                _lt._lists.covers(p.numels, ma.numels, int(block_size))):
+            for i in range(n):
+                size = params[i].numel()
+                nb = -(-size // int(block_size))
+                if grads[i].numel() != size or m_codes[i].numel() != size:
+                    raise ValueError(f"tensor {i}: params, grads and codes must have {size} "
+                                     "elements")
+                if m_absmax[i].numel() < nb:
+                    raise ValueError(f"tensor {i}: m_absmax needs {nb} entries")
+        wb = _bf16_list(params_bf16, params, device, p.numels)
+        nbytes = int(lib().lt_muon_workspace_bytes(rows, cols, n, int(block_size)))
+        self.device, self.handle = device, _stream_handle(stream, device)
+        self.workspace = _list_workspace(device, nbytes, workspace, stream, "muon", self.handle)
+        self.args = (p.ptrs, g.ptrs, gdt, mq.ptrs, ma.ptrs, wb, rows, cols, n, int(block_size),
+                     int(code_map), float(lr), float(momentum), int(bool(nesterov)),
+                     float(weight_decay), float(update_rms), int(ns_steps),
+                     _scalar(coef, device, torch.float32, "coef"),
+                     _scalar(status, device, torch.int32, "status"),
+                     _state_ptr(step_state, device))
+        self.held = (params, grads, m_codes, m_absmax, params_bf16, coef, status, step_state)
+
+    def check(self) -> None:
+        with _current(self.device):
+            rc = lib().lt_muon_step(*self.args, 0, 0, self.handle)
+        if rc != LT_ERR_WORKSPACE:  # what it looks at last
+            _check(rc)
+
+    def run(self) -> None:
+        ws = self.workspace
+        with _current(self.device):
+            _check(lib().lt_muon_step(*self.args, ws.data_ptr(), ws.numel() * ws.element_size(),
+                                      self.handle))
+
+
 def lt_muon_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor],
                  m_codes: Sequence[torch.Tensor], m_absmax: Sequence[torch.Tensor],
                  block_size: int, lr: float, momentum: float = 0.95, weight_decay: float = 0.0,
@@ -90,41 +151,9 @@ def lt_muon_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor],
     """f6: one Muon step in place on params (float32 matrices), codes and absmax (see
     include/lazytrain.h); grads have the parameters' sizes, in float32 or bfloat16;
     params_bf16, coef, status and step_state as in lt_hybrid8bit_adamw_step."""
-    n = len(params)
-    if not (len(grads) == len(m_codes) == len(m_absmax) == n):
-        raise ValueError("tensor lists must be of equal length")
-    device = _device_of(params, coef, status)
-    p = _List(params, device, torch.float32, "params")
-    g = _List(grads, device, what="grads")
-    mq = _List(m_codes, device, torch.int8, "m_codes")
-    ma = _List(m_absmax, device, torch.float32, "m_absmax")
-    gdt = _grad_code(grads, g)
-    _check_block_size(block_size)
-    rows, cols = _sides(params, "params")
-    if _lt._lists.sides(grads) != (rows, cols):
-        for i in range(n):  # a gradient may be flat, but no matrix of another shape
-            if grads[i].dim() != 1 and grads[i].shape != params[i].shape:
-                raise ValueError(f"grads[{i}] must have shape {tuple(params[i].shape)}")
-    if not (g.numels == p.numels == mq.numels and
-            _lt._lists.covers(p.numels, ma.numels, int(block_size))):
-        for i in range(n):
-            size = params[i].numel()
-            nb = -(-size // int(block_size))
-            if grads[i].numel() != size or m_codes[i].numel() != size:
-                raise ValueError(f"tensor {i}: params, grads and codes must have {size} elements")
-            if m_absmax[i].numel() < nb:
-                raise ValueError(f"tensor {i}: m_absmax needs {nb} entries")
-    wb = _bf16_list(params_bf16, params, device, p.numels)
-    nbytes = int(lib().lt_muon_workspace_bytes(rows, cols, n, int(block_size)))
-    handle = _stream_handle(stream, device)
-    ws = _list_workspace(device, nbytes, workspace, stream, "muon", handle)
-    with _current(device):
-        _check(lib().lt_muon_step(
-            p.ptrs, g.ptrs, gdt, mq.ptrs, ma.ptrs, wb, rows, cols, n, int(block_size),
-            int(code_map), float(lr), float(momentum), int(bool(nesterov)), float(weight_decay),
-            float(update_rms), int(ns_steps), _scalar(coef, device, torch.float32, "coef"),
-            _scalar(status, device, torch.int32, "status"), _state_ptr(step_state, device),
-            ws.data_ptr(), ws.numel() * ws.element_size(), handle))
+    _MuonCall(params, grads, m_codes, m_absmax, block_size, lr, momentum, weight_decay, ns_steps,
+              nesterov, update_rms, coef, status, workspace, stream, params_bf16, code_map,
+              step_state).run()
 
 
 # ------------------------------------------------------------- optimizer object
@@ -170,17 +199,24 @@ class HybridMuon(Hybrid8bitAdamW):
     def _elsewhere(self) -> frozenset:
         return frozenset(self.idx_muon)
 
-    def _step_elsewhere(self, grads, stream) -> None:
+    def _prepare_elsewhere(self, grads, stream):
         if not self.idx_muon:
-            return
+            return None
         wb = self.params_bf16
-        lt_muon_step([self.params[i] for i in self.idx_muon], [grads[i] for i in self.idx_muon],
-                     self.muon_codes, self.muon_absmax, self.block_size, lr=self.lr,
-                     momentum=self.momentum, weight_decay=self.weight_decay,
-                     ns_steps=self.ns_steps, nesterov=self.nesterov, update_rms=self.update_rms,
-                     coef=self.coef, status=self.status, stream=stream,
-                     params_bf16=None if wb is None else [wb[i] for i in self.idx_muon],
-                     code_map=self.muon_code_map, step_state=self._state)
+        call = _MuonCall(
+            [self.params[i] for i in self.idx_muon], [grads[i] for i in self.idx_muon],
+            self.muon_codes, self.muon_absmax, self.block_size, lr=self.lr,
+            momentum=self.momentum, weight_decay=self.weight_decay, ns_steps=self.ns_steps,
+            nesterov=self.nesterov, update_rms=self.update_rms, coef=self.coef,
+            status=self.status, stream=stream,
+            params_bf16=None if wb is None else [wb[i] for i in self.idx_muon],
+            code_map=self.muon_code_map, step_state=self._state)
+        call.check()
+        return call
+
+    def _step_elsewhere(self, prepared) -> None:
+        if prepared is not None:
+            prepared.run()
 
     def state_dict(self, stream=None) -> dict:
         state = super().state_dict(stream)
