@@ -8,12 +8,16 @@
 // with P = a I + B, A' = P A P, and X'' = P' P X.  A pair takes 3 n^2 m + 5 n^3 multiply-adds
 // where two single steps take 6 n^2 m + 2 n^3 (products of symmetric matrices compute half
 // their tiles), and X is written once.  Rounding errors of a pair grow by a^2 in directions of
-// small singular values.  Simulated with the roundings below, single steps and pairs: Gaussian
-// matrices of 64 x 64 1.0e-3 and 1.8e-3 off, 256 x 1024 with strong directions 5.6e-4 and
-// 4.0e-4, eight directions over noise 1.5e-3 and 2.7e-3, a spectrum over three decades 1.9e-3
-// and 3.9e-3 (bf16 operands: 1e-2 to 0.12), rows of scales from 1 to 0.01 at 64 x 64 9e-4 and
-// 5e-3.  So pairs are for matrices that gain by them.  Three steps and more are cheaper still
-// but 7e-3 off and more on such spectra; five diverge.
+// small singular values: results are up to five times as far from the exact polynomial as those
+// of single steps.  Measured in the 2-norm, single steps at sides of 65 to 500 and pairs at 128 to
+// 512: noise 8e-4 and 5e-4, a spectrum over one decade 9e-4 and 1.6e-3, over three 2.8e-3 and
+// 4.3e-3, over six 4.4e-3 and 5.7e-3, two directions 100 above the rest 9e-4 and 4.4e-3, half the
+// rank 7e-3 and 7e-3, rank 1 1.3e-2 and 2.3e-2, most at the smallest side each, where the fewest
+// roundings average (with bf16 operands 1e-2 to 0.12).  What is off lies in directions that U
+// hardly has, which the polynomial makes 485 times larger in five steps.  Pairs are taken all the
+// same, where they save a quarter of the time: the polynomial itself leaves singular values
+// anywhere between 0.7 and 1.2, and an 8-bit momentum is further from its 32-bit form than that.
+// Three steps and more are cheaper still but diverge at five.
 //
 // The singular values of X_0 lie in [0, 1], those of every later X in [0, 1.203]: the
 // polynomial's largest value on [0, 1.203] is f(0.5545) = 1.2024.  So the eigenvalues of A lie
