@@ -368,6 +368,8 @@ def _on(stream, device):
 
 def _capturing(stream, device) -> bool:
     """Whether the stream a call works on is being captured into a graph."""
+    if stream is None and device.index == torch.cuda.current_device():
+        return torch.cuda.is_current_stream_capturing()
     with _on(stream, device):
         return torch.cuda.is_current_stream_capturing()
 
@@ -379,8 +381,8 @@ def _own(device, nbytes: int, stream) -> torch.Tensor:
         return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
 
 
-def _workspace(device, nbytes: int, workspace: Optional[torch.Tensor], stream,
-               kind: str, handle: Optional[int] = None) -> torch.Tensor:
+def _workspace(device, nbytes: int, workspace: Optional[torch.Tensor], stream, kind: str,
+               handle: Optional[int] = None, captured: Optional[bool] = None) -> torch.Tensor:
     """The caller's workspace, or one cached per (thread, device, stream, kind of call), so
     that a call repeated over the same tensors finds its descriptors in place (the
     library then copies nothing; see include/lazytrain.h).  A cached workspace is
@@ -388,7 +390,7 @@ def _workspace(device, nbytes: int, workspace: Optional[torch.Tensor], stream,
     caching allocator hands its memory out again only in that stream's order; the
     library is told to forget the old one first.  One that a captured call uses is kept
     for good: a graph reads and writes it whenever it is replayed.  `handle` is the
-    stream's, where the caller has it already."""
+    stream's and `captured` whether it is being captured, where the caller knows."""
     if workspace is not None:
         if workspace.device != device or workspace.numel() * workspace.element_size() < nbytes:
             raise ValueError(f"workspace must hold {nbytes} bytes on {device}")
@@ -404,7 +406,9 @@ def _workspace(device, nbytes: int, workspace: Optional[torch.Tensor], stream,
             ws = torch.empty(max(nbytes, 4096), dtype=torch.uint8, device=device)
         held[key] = ws
         _track(ws)
-    if _capturing(stream, device) and not any(ws is c for c in _captured):
+    if captured is None:
+        captured = _capturing(stream, device)
+    if captured and not any(ws is c for c in _captured):
         _captured.append(ws)
     return ws
 
@@ -418,7 +422,7 @@ def _list_workspace(device, nbytes: int, workspace: Optional[torch.Tensor], stre
         ws = _own(device, nbytes, stream)
         _track(ws)
         return ws
-    return _workspace(device, nbytes, workspace, stream, kind, handle)
+    return _workspace(device, nbytes, workspace, stream, kind, handle, False)
 
 
 # ------------------------------------------------------------------ entry points
