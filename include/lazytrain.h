@@ -75,7 +75,8 @@
  *    with another list meanwhile (replays would find these and return).
  *    The streamed step (host copies) is not capturable.
  *  - Results are bitwise reproducible: they do not depend on the grid size,
- *    the device occupancy or the stream.
+ *    the device occupancy or the stream (nor, but for f5 and f6, on what else
+ *    is in the list).
  */
 #ifndef LAZYTRAIN_H
 #define LAZYTRAIN_H
@@ -510,7 +511,9 @@ size_t lt_orthogonalize_workspace_bytes(const int64_t* rows, const int64_t* cols
  * about half of the last two.  bf16 results round by up to 2^-9 of an element more.
  * A zero matrix gives zeros; one with a NaN or an infinity gives NaN throughout, and leaves
  * the other matrices of the list alone.
- * Matrices of one call are worked on together: pass lists, not matrices one by one.
+ * Matrices of one call are worked on together: pass lists, not matrices one by one.  The same list
+ * gives the same bits every time; in another list a matrix's sums may be cut and its tiles taken
+ * otherwise, and its result differ by the roundings of the paragraph above.
  */
 lt_err lt_orthogonalize(const void* const* matrices, int in_dtype, void* const* out, int out_dtype,
                         const int64_t* rows, const int64_t* cols, int n_matrices, int ns_steps,
