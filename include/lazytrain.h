@@ -507,8 +507,8 @@ size_t lt_orthogonalize_workspace_bytes(const int64_t* rows, const int64_t* cols
  * singular values (measured at n from 65 to 512): 1e-4 to 3e-3 where they lie within a factor of
  * ten; up to 8e-3 where they spread over decades, a few directions stand far above the rest or
  * half of them are missing; up to 2.5e-2 where one direction is nearly all of U, falling as n
- * grows (1.3e-2 at 512).  Matrices with n < 128 or m < 2 n, whose steps are single, are within
- * about half of the last two.  bf16 results round by up to 2^-9 of an element more.
+ * grows (1.3e-2 at 512).  Matrices with n < 128 or m < 2 n, whose steps are single, are within 7e-3
+ * and 1.4e-2 of the last two.  bf16 results round by up to 2^-9 of an element more.
  * A zero matrix gives zeros; one with a NaN or an infinity gives NaN throughout, and leaves
  * the other matrices of the list alone.
  * Matrices of one call are worked on together: pass lists, not matrices one by one.  The same list

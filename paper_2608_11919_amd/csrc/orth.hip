@@ -716,13 +716,15 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_orth_up
 // A matrix with n <= 32 rows (or columns), padded to 16 or 32, in one launch: with G = X X^T,
 // every step stays n x n (P = a I + b G + c G G, G' = P G P, R' = P R), and the result is R X.
 // Adapters, small layers and odd leftovers come in hundreds, and the general path would pad
-// each to 128, write X three times a step and take 18 launches: 224 of 32 x 4288 take 146 us
+// each to 128, write X three times a step and take 18 launches: 224 of 32 x 4288 take 141 us
 // here, there 2124; one of 32 x 4096 59 and 210, one of 16 x 65536 280 and 1774.  An error of G
 // grows by a^2 with every step in directions of small singular values, 2e5 in five: G and the
 // steps are in 64 bits (in 32 a 64 x 64 matrix with a few strong directions ends 5e-3 off), R X
 // in 32.  The norm is G's trace, so X is read once, into LDS, where it fits, and else twice.
-// What bounds it is G at the 64-bit rate (n^2 m products for every workgroup of a matrix, 3.4 us
-// for 16 x 2048), and latency: 7 us for 16 x 128, 0.5 us more a step (2.1 at 32 x 32).
+// Where matrices are few, what bounds it is latency (7 us for 16 x 128, 0.5 us more a step; 2.1 at
+// 32 x 32) beside G at the 64-bit rate (n^2 m products for every workgroup of a matrix, 3.4 us for
+// 16 x 2048); where they are many, that a CU holds one workgroup, which loads, waits and multiplies
+// in turn: 224 of 32 x 4288 take 138 us, their bytes 41, their 64-bit products 21.
 
 constexpr int kThinThreads = 512, kThinWaves = kThinThreads / 64;
 constexpr int kThinSpan = 16 * kThinWaves;  // columns that a workgroup's waves multiply at a time
@@ -1093,8 +1095,11 @@ __global__ __launch_bounds__(kThinThreads) void k_orth_thin(Gate gate,
 //
 // The same for 33 <= n <= 64, where G and its steps no longer leave LDS room for X: G of every
 // slice of columns, the steps by one workgroup for each matrix, R X.  X is read twice and written
-// once, by as many workgroups as there are slices.  Bound by the 64-bit products of G where
-// matrices are many or long, and by the steps (35 us, one product after the other) where not.
+// once, by as many workgroups as there are slices.  224 of 64 x 4288 in fp32 take 377 us: 155 the
+// Gram matrices (246 MB, 42 us at the rate of reading; 64-bit products, 63 us at theirs), 62 the
+// steps (35 for a single matrix, one product after the other; a workgroup a CU), 155 R X.  What
+// bounds the two passes is how X is read: a wave asks for 64 bytes of each of 16 rows (single
+// elements where X is tall: 381 us in all), then multiplies, with nothing else under way.
 
 constexpr int kSmallSide = 64;
 constexpr int kSmallSlice = 512;                            // columns
@@ -1526,8 +1531,8 @@ Plan make_plan(const int64_t* rows, const int64_t* cols, int K, bool muon, int64
     return p;
 }
 
-// Sizes a call can take: rows and columns in [0, 2^23), so that 128 rows of the widest matrix
-// stay within the 32-bit offsets of a tile's loads.
+// Sizes a call can take: rows and columns in [0, 2^23), so that 256 rows of the widest matrix, the
+// largest tile's, stay within the 32-bit offsets of a tile's loads: the last is 255 * 2^24 on.
 bool valid_sizes(const int64_t* rows, const int64_t* cols, int K)
 {
     if (K < 0 || (K > 0 && (!rows || !cols)))
