@@ -871,7 +871,8 @@ void launch_held(const FewArgs& g, bool f32, int cus, hipStream_t st)
 }
 
 // x is held where its share fits a wave's registers: up to 8192 values of 16 tokens (5120 in
-// fp32 on the way), 5120 of 32.
+// fp32 on the way), 5120 of 32.  Kernels are for 2, 5 and 8 steps a wave: between, a length takes
+// the next larger one's registers, and above 2048 values its one workgroup a CU.
 template <int X>
 void launch_few_tokens(const FewArgs& g, bool f32, int cus, hipStream_t st)
 {

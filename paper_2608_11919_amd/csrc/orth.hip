@@ -1095,11 +1095,11 @@ __global__ __launch_bounds__(kThinThreads) void k_orth_thin(Gate gate,
 //
 // The same for 33 <= n <= 64, where G and its steps no longer leave LDS room for X: G of every
 // slice of columns, the steps by one workgroup for each matrix, R X.  X is read twice and written
-// once, by as many workgroups as there are slices.  224 of 64 x 4288 in fp32 take 377 us: 155 the
-// Gram matrices (246 MB, 42 us at the rate of reading; 64-bit products, 63 us at theirs), 62 the
-// steps (35 for a single matrix, one product after the other; a workgroup a CU), 155 R X.  What
-// bounds the two passes is how X is read: a wave asks for 64 bytes of each of 16 rows (single
-// elements where X is tall: 381 us in all), then multiplies, with nothing else under way.
+// once, by as many workgroups as there are slices.  224 of 64 x 4288 in fp32 take 377 us: 166 the
+// Gram matrices (246 MB, 42 us at the rate of reading; 64-bit products, 63 us at theirs), 61 the
+// steps (35 for a single matrix, one product after the other; a workgroup a CU), 143 R X; of 4288 x
+// 64 143, 63 and 168.  What bounds the two passes is waiting: a wave asks for 64 bytes of each of
+// 16 rows (single elements where X is tall), then multiplies, with no other read under way.
 
 constexpr int kSmallSide = 64;
 constexpr int kSmallSlice = 512;                            // columns
