@@ -5,6 +5,7 @@ float32) for the next step.
 """
 from __future__ import annotations
 
+import math
 from typing import Optional, Tuple
 
 import torch
@@ -172,7 +173,8 @@ def _laid_out(t: torch.Tensor, aligned: bool = True) -> torch.Tensor:
 def _tokens(x: torch.Tensor, features: int, what: str, aligned: bool = True) -> torch.Tensor:
     if x.dim() < 1 or x.shape[-1] != features:
         raise ValueError(f"{what} must have {features} features, got shape {tuple(x.shape)}")
-    return _laid_out(x if x.dim() == 2 else x.reshape(-1, features), aligned)
+    t = x if x.dim() == 2 else x.reshape(math.prod(x.shape[:-1]), features)
+    return _laid_out(t, aligned)
 
 
 def fp8_linear(x: torch.Tensor, weight: Fp8Weight,

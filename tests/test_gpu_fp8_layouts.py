@@ -84,3 +84,27 @@ def test_weights(layout):
     for name in ("codes", "scales", "codes_t", "scales_t"):
         assert torch.equal(getattr(weight, name), getattr(want, name))
         assert torch.equal(getattr(other, name), getattr(want, name))
+
+
+@pytest.mark.parametrize("shape", [(2, 3, 0), (0, 3, 0), (0, 3, 7), (40, 1, 0), (0,), (7,), (1, 1, 1)])
+@pytest.mark.parametrize("rows", [0, 5])
+def test_dimensions_of_zero_and_more_than_two(shape, rows):
+    cols = shape[-1]
+    x, dy = draw(shape, 1), draw(shape[:-1] + (rows,), 2)
+    weight = lt.Fp8Weight.from_master(draw((rows, cols), 3))
+    tokens = 1
+    for n in shape[:-1]:
+        tokens *= n
+    x2, dy2 = x.reshape(tokens, cols), dy.reshape(tokens, rows)
+    y, saved = lt.fp8_linear_forward(x, weight, out_dtype=torch.float32)
+    y2, saved2 = lt.fp8_linear_forward(x2, weight, out_dtype=torch.float32)
+    assert y.shape == shape[:-1] + (rows,) and torch.equal(y.reshape(tokens, rows), y2)
+    assert torch.equal(lt.fp8_linear(x, weight, out_dtype=torch.float32), y)
+    dx, dw = lt.fp8_linear_backward(dy, saved, weight)
+    dx2, dw2 = lt.fp8_linear_backward(dy2, saved2, weight)
+    assert dx.shape == shape and torch.equal(dx.reshape(tokens, cols), dx2)
+    assert torch.equal(dw, dw2) and dw.shape == (rows, cols)
+    if cols == 0:
+        assert not y.any()
+    if tokens == 0:
+        assert not dw.any()
