@@ -56,8 +56,8 @@
  *    copy still in flight).  Between calls the
  *    caller therefore must not write into a workspace; before freeing it or
  *    using its memory for anything else, call lt_workspace_release.  (Calls in
- *    stream order may be given one workspace: f8 and f9, which keep no
- *    descriptors there, make the library forget what they overwrite.)  A kernel
+ *    stream order may be given one workspace: f8, f9 and f11 to f14, which
+ *    keep no descriptors there, make the library forget what they overwrite.)  A kernel
  *    whose workspace no longer holds the descriptors it was launched for
  *    (checked through a per-copy tag in the workspace's first word) returns
  *    without reading or writing any tensor; lt_grad_sqnorm and
@@ -610,6 +610,117 @@ lt_err lt_fp8_linear(const void* x, int dtype, int64_t x_stride, const uint8_t* 
                      const uint8_t* w_scales, int64_t m, int64_t n, int64_t k, void* out,
                      int out_dtype, int64_t out_stride, void* workspace, size_t workspace_bytes,
                      void* stream);
+
+/* Bytes of a row of 8-bit integer codes (f10): its columns rounded up to 128.  0 if cols < 0. */
+int64_t lt_int8_code_pitch(int64_t cols);
+
+/*
+ * f10: quantizes a matrix x, rows x cols elements of dtype with row_stride elements from row to
+ * row (>= cols, beginning at any element's address), to 8-bit integers with a scale for each row.
+ *   codes[rows][lt_int8_code_pitch(cols)]  with most the row's largest |x|, at least 2^-100: the
+ *                  integer nearest to x * fp32(127 / most), ties to even (the product exact,
+ *                  rounded once); in [-127, 127], and 0 in columns past cols;
+ *   scales[rows]   fp32(most / 127): value = code * scale.
+ * A row with a NaN or an infinity has codes 0 and the scale NaN, and makes the results that read it
+ * NaN.  rows, cols < 2^31; codes 16-byte aligned; no array overlaps another.  Nothing is written
+ * where rows or cols is 0.
+ */
+lt_err lt_int8_quantize(const void* x, int dtype, int64_t rows, int64_t cols, int64_t row_stride,
+                        int8_t* codes, float* scales, void* stream);
+
+/* Bytes of device workspace lt_int8_matmul needs (partial sums where few results share a long
+ * sum, else 256, which it does not look at); 0 if an argument is invalid. */
+size_t lt_int8_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k);
+
+/*
+ * f11: out[i][j] = (sum over k of a_codes[i][k] * b_codes[j][k]) * a_scales[i] * b_scales[j], for
+ * operands as lt_int8_quantize stores them (m x k and n x k; any int8 codes, but 0 past k).  The
+ * sum is exact; it is rounded to fp32, multiplied by either scale in that order in fp32, and
+ * rounded to out_dtype (LT_DTYPE_F32 or LT_DTYPE_BF16).  out has out_stride elements (>= n) from row
+ * to row; k = 0 gives zeros.  m, n < 2^26, fewer than 2^24 tiles of 64 x 64, k <= 2^17 (codes of
+ * -128 in both operands: k < 2^17).
+ * out overlaps no operand.
+ */
+lt_err lt_int8_matmul(const int8_t* a_codes, const float* a_scales, const int8_t* b_codes,
+                      const float* b_scales, int64_t m, int64_t n, int64_t k, void* out,
+                      int out_dtype, int64_t out_stride, void* workspace, size_t workspace_bytes,
+                      void* stream);
+
+/* Bytes of device workspace lt_int8_linear needs; 0 if an argument is invalid. */
+size_t lt_int8_linear_workspace_bytes(int64_t m, int64_t n, int64_t k);
+
+/*
+ * f11: a linear layer's answer, out = x W^T: x (m x k, dtype, x_stride elements from row to row,
+ * beginning at any element's address) is quantized on the way, a scale for each token; W (n x k)
+ * is as lt_int8_quantize stores it.  The same bits as lt_int8_quantize and lt_int8_matmul.
+ */
+lt_err lt_int8_linear(const void* x, int dtype, int64_t x_stride, const int8_t* w_codes,
+                      const float* w_scales, int64_t m, int64_t n, int64_t k, void* out,
+                      int out_dtype, int64_t out_stride, void* workspace, size_t workspace_bytes,
+                      void* stream);
+
+/* The activations of a gated block: g / (1 + e^-g); g Phi(g), Phi the normal distribution's
+ * function; 0.5 g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))); max(g, 0). */
+enum { LT_ACT_SILU = 0, LT_ACT_GELU = 1, LT_ACT_GELU_TANH = 2, LT_ACT_RELU = 3 };
+
+/* Bytes of device workspace lt_int8_gated needs; 0 if an argument is invalid. */
+size_t lt_int8_gated_workspace_bytes(int64_t m, int64_t n, int64_t k);
+
+/*
+ * f12: the gated projections of a feed-forward block in 8-bit integers, for answering:
+ *   out = act(x Wg^T) * (x Wu^T),  activation one of LT_ACT_*,
+ * both products as lt_int8_linear's in fp32, the rest in fp32, rounded once to out_dtype.  Arguments as
+ * there; gate and up are both n x k.
+ */
+lt_err lt_int8_gated(const void* x, int dtype, int64_t x_stride, const int8_t* gate_codes,
+                     const float* gate_scales, const int8_t* up_codes, const float* up_scales,
+                     int activation, int64_t m, int64_t n, int64_t k, void* out, int out_dtype,
+                     int64_t out_stride, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes that lt_gated_forward keeps for the backward pass; 0 if an argument is invalid. */
+size_t lt_gated_saved_bytes(int64_t m, int64_t n);
+
+/* Bytes of device workspace lt_gated_forward needs: copies of operands whose rows are not whole
+ * steps of 64 values, or not multiples of 8 apart, else 256, which it does not look at (nor where
+ * m <= 32 and nothing is saved).  0 if an argument is invalid. */
+size_t lt_gated_forward_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t x_stride,
+                                        int64_t gate_stride, int64_t up_stride);
+
+/*
+ * f13: the gated projections of a feed-forward block in bf16,
+ *   g = x gate^T,  u = x up^T,  out = act(g) * u,  activation one of LT_ACT_*,
+ * for x (m x k) and two weights (n x k) of bf16, strides in elements from row to row.  Sums and the
+ * activation are fp32, out is rounded once to out_dtype.
+ *   saved   NULL, or lt_gated_saved_bytes(m, n) bytes for lt_gated_backward: u act'(g) and act(g),
+ *           24 bits each (a relative 2^-17).
+ * k = 0 gives zeros.  m, n, k < 2^21, fewer than 2^23 tiles of 64 x 64 in each matrix.  x, the
+ * weights, out and saved 16-byte aligned; what is written overlaps nothing else.
+ */
+lt_err lt_gated_forward(const void* x, int64_t x_stride, const void* gate, int64_t gate_stride,
+                        const void* up, int64_t up_stride, int activation, int64_t m, int64_t n,
+                        int64_t k, void* out, int out_dtype, int64_t out_stride, void* saved,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of device workspace lt_gated_backward needs for the gradients that are asked for; 0 if an
+ * argument is invalid. */
+size_t lt_gated_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int dx, int dw);
+
+/*
+ * f14: the gradients of f13 from dh, out's (m x n, dh_dtype):
+ *   dg = dh * u act'(g),  du = dh * act(g),
+ *   dx = dg gate + du up,  dgate = dg^T x,  dup = du^T x.
+ * dg and du are rounded to bf16 for the products, whose sums are fp32's; dx is rounded to dx_dtype,
+ * the weights' gradients to grad_dtype.  dx may be NULL, and so may dgate and dup together: what only
+ * they need (the weights; x) is not looked at then.  saved is lt_gated_forward's.  Empty sums give
+ * zeros.  saved and the gradients 16-byte aligned, the rest to its elements; what is written overlaps
+ * nothing else.
+ */
+lt_err lt_gated_backward(const void* dh, int dh_dtype, int64_t dh_stride, const void* saved,
+                         const void* x, int64_t x_stride, const void* gate, int64_t gate_stride,
+                         const void* up, int64_t up_stride, int64_t m, int64_t n, int64_t k,
+                         void* dx, int dx_dtype, int64_t dx_stride, void* dgate,
+                         int64_t dgate_stride, void* dup, int64_t dup_stride, int grad_dtype,
+                         void* workspace, size_t workspace_bytes, void* stream);
 
 /* Copies the device status word to *out and synchronizes `stream` (the only
  * entry point that blocks the host).  An asynchronous device fault from

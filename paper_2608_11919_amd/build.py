@@ -12,7 +12,8 @@ import sysconfig
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "liblazytrain.so")
-SOURCES = [os.path.join(HERE, "csrc", f) for f in ("library.hip", "orth.hip", "fp8.hip")]
+SOURCES = [os.path.join(HERE, "csrc", f) for f in ("library.hip", "orth.hip", "fp8.hip", "int8.hip",
+                                               "gated.hip")]
 ARCH = os.environ.get("LT_OFFLOAD_ARCH", "gfx950")
 
 HIPCC_FLAGS = [

@@ -1,0 +1,878 @@
+// gated.hip -- the gated projections of a feed-forward block in bf16, forward and backward:
+//
+//   g = x Wg^T,  u = x Wu^T,  h = act(g) * u
+//   a = u act'(g),  b = act(g)                       (kept by the forward pass, 24 bits each)
+//   dg = dh * a,  du = dh * b                        (rounded to bf16 for the products)
+//   dx = dg Wg + du Wu,  dWg = dg^T x,  dWu = du^T x
+//
+// Sums are fp32's.  The forward pass takes both products in one tile, the weights' rows in turns
+// of 32, so that a lane ends with g and u of the same places and no product is stored.
+
+#include "gated.h"
+#include "host.h"
+
+#include <algorithm>
+#include <string>
+#include <vector>
+
+namespace {
+
+using host::fail;
+using namespace tiles;
+using gated::store_row;
+using gated::u16x8;
+
+constexpr int kStep = 64;  // values of every row, per step of the main loop
+
+int64_t padded(int64_t values) { return host::ceil_div(values, kStep) * kStep; }
+
+// ------------------------------------------------------------- layouts
+
+// A matrix of bf16 with rows of whole steps, zeros behind their ends: what the products read
+// where a row as it is has another length or place.
+struct PackArgs {
+    const uint16_t* x;
+    int64_t rows, cols, stride;
+    uint16_t* out;
+    int64_t pitch;
+};
+
+__global__ __launch_bounds__(256) void k_gated_pack(PackArgs a)
+{
+    const int64_t lines = a.pitch / 8, all = a.rows * lines;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < all;
+         i += int64_t(gridDim.x) * 256) {
+        const int64_t row = i / lines, col = i % lines * 8;
+        const uint16_t* p = a.x + row * a.stride + col;
+        i32x4 v;
+        if (col + 8 <= a.cols) {
+            v = load_any(p);
+        } else {
+            u16x8 b;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                b[e] = col + e < a.cols ? p[e] : uint16_t(0);
+            v = __builtin_bit_cast(i32x4, b);
+        }
+        *reinterpret_cast<i32x4*>(a.out + row * a.pitch + col) = v;
+    }
+}
+
+// The transpose: out[c][r] = x[r][c], zeros for r from rows up to whole steps.  64 x 64 a
+// workgroup, through LDS.
+__global__ __launch_bounds__(256) void k_gated_turn(PackArgs a)
+{
+    constexpr int kTurnPitch = 64 + 2;
+    __shared__ uint16_t block[64 * kTurnPitch];
+    const int64_t down = (a.rows + 63) / 64;
+    const int64_t r0 = int64_t(blockIdx.x) % down * 64, c0 = int64_t(blockIdx.x) / down * 64;
+    const int line = int(threadIdx.x) / 8, at = int(threadIdx.x) % 8 * 8;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int64_t row = r0 + line + 32 * h, col = c0 + at;
+        const uint16_t* p = a.x + row * a.stride + col;
+        u16x8 v = {};
+        if (row < a.rows && col + 8 <= a.cols) {
+            v = __builtin_bit_cast(u16x8, load_any(p));
+        } else if (row < a.rows) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                v[e] = col + e < a.cols ? p[e] : uint16_t(0);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            block[(at + e) * kTurnPitch + line + 32 * h] = v[e];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int64_t col = c0 + line + 32 * h;
+        if (col >= a.cols)
+            continue;
+        u16x8 v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            v[e] = block[(line + 32 * h) * kTurnPitch + at + e];
+        *reinterpret_cast<i32x4*>(a.out + col * a.pitch + r0 + at) = __builtin_bit_cast(i32x4, v);
+    }
+}
+
+struct ZeroArgs {
+    void* out;
+    int64_t m, n, stride;
+};
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_zero_rows(ZeroArgs a)
+{
+    const int64_t all = a.m * a.n;
+    for (int64_t e = int64_t(blockIdx.x) * 256 + threadIdx.x; e < all;
+         e += int64_t(gridDim.x) * 256)
+        static_cast<T*>(a.out)[e / a.n * a.stride + e % a.n] = 0;
+}
+
+// ------------------------------------------------------------- the forward pass
+
+// What the backward pass needs of every result, a and b, in 24 bits each: their upper halves as
+// bf16 and a byte more.  In bf16 alone either rounding would add as much to the gradients as
+// theirs; in fp32 they take a third more memory.
+struct Saved {
+    uint16_t *a_high, *b_high;
+    uint8_t *a_low, *b_low;
+    int64_t pitch;  // values of a row, a multiple of 8
+};
+
+Saved saved_layout(void* saved, int64_t m, int64_t n)
+{
+    Saved s;
+    s.pitch = host::ceil_div(n, 8) * 8;
+    s.a_high = static_cast<uint16_t*>(saved);
+    s.b_high = s.a_high + m * s.pitch;
+    s.a_low = reinterpret_cast<uint8_t*>(s.b_high + m * s.pitch);
+    s.b_low = s.a_low + m * s.pitch;
+    return s;
+}
+
+__device__ inline uint32_t round_24(float x)
+{
+    const uint32_t b = __float_as_uint(x);
+    // to nearest; an infinity or a NaN keeps its bits (a NaN that has its all in the last byte
+    // becomes one that has not)
+    return (b & 0x7F800000u) == 0x7F800000u ? b | ((b & 0xFFu) != 0u ? 0x400000u : 0u) : b + 0x80u;
+}
+
+__device__ inline void save_eight(uint16_t* high, uint8_t* low, int64_t at, const float (&v)[8])
+{
+    uint32_t h[4], l[2] = {0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        const uint32_t x = round_24(v[e]), y = round_24(v[e + 1]);
+        h[e / 2] = x >> 16 | (y & 0xFFFF0000u);
+        l[e / 4] |= (x >> 8 & 0xFFu) << (8 * (e % 4)) | (y >> 8 & 0xFFu) << (8 * (e % 4) + 8);
+    }
+    *reinterpret_cast<uint4*>(high + at) = make_uint4(h[0], h[1], h[2], h[3]);
+    *reinterpret_cast<uint2*>(low + at) = make_uint2(l[0], l[1]);
+}
+
+__device__ inline void load_eight(const uint16_t* high, const uint8_t* low, int64_t at,
+                                  float (&v)[8])
+{
+    const uint4 h = *reinterpret_cast<const uint4*>(high + at);
+    const uint2 l = *reinterpret_cast<const uint2*>(low + at);
+    const uint32_t hs[4] = {h.x, h.y, h.z, h.w}, ls[2] = {l.x, l.y};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const uint32_t top = e % 2 == 0 ? hs[e / 2] << 16 : hs[e / 2] & 0xFFFF0000u;
+        v[e] = __uint_as_float(top | (ls[e / 4] >> (8 * (e % 4)) & 0xFFu) << 8);
+    }
+}
+
+struct ForwardArgs {
+    const uint8_t *x, *gate, *up;
+    int64_t x_pitch, gate_pitch, up_pitch;  // bytes
+    int64_t m, n;
+    int steps;
+    int activation;
+    void* out;
+    int64_t stride;
+    Saved saved;
+};
+
+template <bool F32, bool SAVE>
+struct ForwardWriter {
+    const ForwardArgs& g;
+    int64_t r0, c0;
+    __device__ inline void store(int row_, int col_, float (&u)[8], float (&v)[8])
+    {
+        const int64_t row = r0 + row_, col = c0 + col_;
+        if (row >= g.m || col >= g.n)
+            return;
+        float h[8];
+        if constexpr (SAVE) {
+            float a[8], b[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float slope;
+                b[e] = gated::activate(g.activation, u[e], &slope);
+                a[e] = v[e] * slope;
+                h[e] = b[e] * v[e];
+            }
+            const int64_t at = row * g.saved.pitch + col;
+            save_eight(g.saved.a_high, g.saved.a_low, at, a);
+            save_eight(g.saved.b_high, g.saved.b_low, at, b);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                h[e] = gated::activate(g.activation, u[e]) * v[e];
+        }
+        store_row<F32>(g.out, row * g.stride + col, h, g.n - col);
+    }
+};
+
+template <typename Tile, bool F32, bool SAVE>
+__global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_gated_forward(ForwardArgs g)
+{
+    __shared__ __align__(1024) uint8_t lds[Tile::kLdsBytes];
+    constexpr int kCols = Tile::kCols / 2;
+    const TilePlace at = tile_place(int(unit_of_workgroup(Tile::kRun)),
+                                    int((g.m + Tile::kRows - 1) / Tile::kRows),
+                                    int((g.n + kCols - 1) / kCols));
+    const int64_t r0 = int64_t(at.row) * Tile::kRows, c0 = int64_t(at.col) * kCols;
+    Tile tile;
+    Bf16 mul;
+    product_pairs(mul, tile, g.x + r0 * g.x_pitch, g.x_pitch, g.m - r0, g.gate + c0 * g.gate_pitch,
+                  g.gate_pitch, g.up + c0 * g.up_pitch, g.up_pitch, g.n - c0, g.steps, lds);
+    ForwardWriter<F32, SAVE> w{g, r0, c0};
+    finish_pairs(tile, lds, w);
+}
+
+// ------------------------------------------------------------- the backward pass
+
+// dg and du as the products read them: by rows next to each other, dg in the first
+// padded(n) columns (their sum with both weights is one product), and of the transpose, dg's n
+// rows before du's.
+struct SlopeArgs {
+    const void* dh;
+    int64_t stride;
+    Saved saved;
+    int64_t m, n;
+    uint16_t* by_rows;  // [m][2 * half], or null
+    int64_t half;
+    uint16_t* turned;   // [2 n][turned_pitch], or null
+    int64_t turned_pitch;
+};
+
+// 64 tokens x 64 channels to a workgroup.  Bound by HBM: 8 bytes read and 4 to 8 written a value.
+template <bool F32>
+__global__ __launch_bounds__(256) void k_gated_slopes(SlopeArgs g)
+{
+    constexpr int kTurnPitch = 64 + 2;
+    __shared__ uint16_t block[2][64 * kTurnPitch];
+    const int64_t across = g.half / 64;
+    const int64_t r0 = int64_t(blockIdx.x) / across * 64, c0 = int64_t(blockIdx.x) % across * 64;
+    const int line = int(threadIdx.x) / 8, at = int(threadIdx.x) % 8 * 8;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int64_t row = r0 + line + 32 * h, col = c0 + at;
+        u16x8 dg = {}, du = {};
+        if (row < g.m && col < g.n) {
+            float a[8], b[8], d[8];
+            load_eight(g.saved.a_high, g.saved.a_low, row * g.saved.pitch + col, a);
+            load_eight(g.saved.b_high, g.saved.b_low, row * g.saved.pitch + col, b);
+            const int64_t from = row * g.stride + col;
+            if (col + 8 <= g.n) {
+                if constexpr (F32) {
+                    const auto* p = static_cast<const float*>(g.dh) + from;
+                    const f32x4 lo = __builtin_bit_cast(f32x4, load_any(p));
+                    const f32x4 hi = __builtin_bit_cast(f32x4, load_any(p + 4));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        d[e] = lo[e];
+                        d[4 + e] = hi[e];
+                    }
+                } else {
+                    const i32x4 w = load_any(static_cast<const uint16_t*>(g.dh) + from);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        d[2 * e] = __uint_as_float(uint32_t(w[e]) << 16);
+                        d[2 * e + 1] = __uint_as_float(uint32_t(w[e]) & 0xFFFF0000u);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    d[e] = 0.0f;
+                    if (col + e < g.n) {
+                        if constexpr (F32)
+                            d[e] = static_cast<const float*>(g.dh)[from + e];
+                        else
+                            d[e] = __uint_as_float(
+                                uint32_t(static_cast<const uint16_t*>(g.dh)[from + e]) << 16);
+                    }
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (col + e < g.n) {  // what is kept behind a row's end is anything
+                    dg[e] = gated::bf16_bits(d[e] * a[e]);
+                    du[e] = gated::bf16_bits(d[e] * b[e]);
+                }
+        }
+        if (g.by_rows && row < g.m) {
+            uint16_t* to = g.by_rows + row * 2 * g.half + col;
+            *reinterpret_cast<i32x4*>(to) = __builtin_bit_cast(i32x4, dg);
+            *reinterpret_cast<i32x4*>(to + g.half) = __builtin_bit_cast(i32x4, du);
+        }
+        if (g.turned) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                block[0][(at + e) * kTurnPitch + line + 32 * h] = dg[e];
+                block[1][(at + e) * kTurnPitch + line + 32 * h] = du[e];
+            }
+        }
+    }
+    if (!g.turned)
+        return;
+    __syncthreads();
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t col = c0 + line + 32 * h;
+            if (col >= g.n)
+                continue;
+            u16x8 v;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                v[e] = block[b][(line + 32 * h) * kTurnPitch + at + e];
+            *reinterpret_cast<i32x4*>(g.turned + (b * g.n + col) * g.turned_pitch + r0 + at) =
+                __builtin_bit_cast(i32x4, v);
+        }
+}
+
+// out[i] = A_i B^T for one or two matrices A_i of m rows each, one behind the other.
+struct ProductArgs {
+    const uint8_t *a, *b;
+    int64_t a_pitch, b_pitch;  // bytes
+    int64_t m, n;
+    int count;
+    int steps, slice;
+    void* out[2];
+    int64_t stride[2];
+    float* partial;  // several slices: [slice][count][m][n]
+};
+
+template <bool F32>
+struct ProductWriter {
+    static constexpr bool kTurned = false;
+    static constexpr int kSlots = 8;
+    void* out;
+    int64_t stride, rows, cols;  // from the tile's origin on
+    __device__ inline void fetch(int, int, int) {}
+    __device__ inline void turn(int, int, const float (&)[8]) {}
+    __device__ inline void store(int row, int col, float (&v)[8], int)
+    {
+        if (row < rows && col < cols)
+            store_row<F32>(out, row * stride + col, v, cols - col);
+    }
+};
+
+template <typename Tile, bool F32>
+__global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_gated_product(ProductArgs g)
+{
+    __shared__ __align__(1024) uint8_t lds[Tile::kLdsBytes];
+    const int down = int((g.m + Tile::kRows - 1) / Tile::kRows);
+    const int across = int((g.n + Tile::kCols - 1) / Tile::kCols);
+    const int64_t unit = unit_of_workgroup(Tile::kRun);
+    const int which = unit >= int64_t(down) * across ? 1 : 0;
+    const TilePlace at = tile_place(int(unit - int64_t(which) * down * across), down, across);
+    const int64_t r0 = int64_t(at.row) * Tile::kRows, c0 = int64_t(at.col) * Tile::kCols;
+    const int first = int(blockIdx.y) * g.slice, steps = min(g.slice, g.steps - first);
+    const int64_t k0 = int64_t(first) * kStepBytes;
+    Tile tile;
+    Bf16 mul;
+    product(mul, tile, g.a + (which * g.m + r0) * g.a_pitch + k0, g.a_pitch, g.m - r0,
+            g.b + c0 * g.b_pitch + k0, g.b_pitch, g.n - c0, steps, lds);
+    if (g.partial) {
+        ProductWriter<true> p;
+        p.rows = g.m - r0;
+        p.cols = g.n - c0;
+        p.stride = g.n;
+        p.out = g.partial + ((int64_t(blockIdx.y) * g.count + which) * g.m + r0) * g.n + c0;
+        finish(tile, lds, p);
+        return;
+    }
+    ProductWriter<F32> w;
+    w.rows = g.m - r0;
+    w.cols = g.n - c0;
+    w.stride = which ? g.stride[1] : g.stride[0];
+    void* out = which ? g.out[1] : g.out[0];
+    w.out = F32 ? static_cast<void*>(static_cast<float*>(out) + r0 * w.stride + c0)
+                : static_cast<void*>(static_cast<uint16_t*>(out) + r0 * w.stride + c0);
+    finish(tile, lds, w);
+}
+
+// out = the slices' sums, added in their order.
+template <bool F32>
+__global__ __launch_bounds__(256) void k_gated_join(ProductArgs g, int slices)
+{
+    const int64_t one = g.m * g.n, all = one * g.count;
+    for (int64_t e = int64_t(blockIdx.x) * 256 + threadIdx.x; e < all;
+         e += int64_t(gridDim.x) * 256) {
+        float s = g.partial[e];
+        for (int i = 1; i < slices; ++i)
+            s += g.partial[i * all + e];
+        const int which = e >= one ? 1 : 0;
+        const int64_t i = e - which * one;
+        const int64_t to = i / g.n * (which ? g.stride[1] : g.stride[0]) + i % g.n;
+        void* out = which ? g.out[1] : g.out[0];
+        if constexpr (F32)
+            static_cast<float*>(out)[to] = s;
+        else
+            static_cast<uint16_t*>(out)[to] = gated::bf16_bits(s);
+    }
+}
+
+// ---------------------------------------------------------------- host side
+
+// Dimensions and strides stay within the 32-bit offsets of a tile's loads: 256 rows of 2^23 bytes.
+constexpr int64_t kMost = int64_t(1) << 21;
+constexpr int64_t kMostGroups = int64_t(1) << 24;  // a grid counts threads in 32 bits
+constexpr int kLongSum = 96;  // steps: shorter sums are not cut
+
+struct Way {
+    int tile;    // 256, 128 or 64
+    int slices;  // of the sum
+    int slice;   // steps of each
+};
+
+// The largest tile that gives every CU a workgroup; few results of a long sum are cut into
+// slices.  `pair`: a tile's columns are two weights'.
+Way way_of(int64_t m, int64_t n, int count, int steps, bool pair)
+{
+    Way w{64, 1, steps};
+    int64_t tiles = 0;
+    for (const int t : {256, 128, 64}) {
+        w.tile = t;
+        const int64_t wide = pair && t > 64 ? t / 2 : t;
+        tiles = host::ceil_div(m, t) * host::ceil_div(n, wide) * count;
+        if (tiles >= 256)
+            return w;
+    }
+    if (pair || steps < kLongSum)
+        return w;
+    const int want = int(std::min<int64_t>(steps / 8, host::ceil_div(512, std::max<int64_t>(tiles, 1))));
+    w.slice = int(host::ceil_div(steps, std::max(want, 1)));
+    w.slices = int(host::ceil_div(steps, w.slice));
+    return w;
+}
+
+bool valid_sizes(int64_t m, int64_t n, int64_t k)
+{
+    const auto tiles = [](int64_t a, int64_t b) {
+        return host::ceil_div(a, 64) * host::ceil_div(b, 64) * 2 < kMostGroups;
+    };
+    return m >= 0 && n >= 0 && k >= 0 && m < kMost && n < kMost && k < kMost && tiles(m, n) &&
+           tiles(m, k) && tiles(n, k);
+}
+
+bool valid_stride(int64_t rows, int64_t cols, int64_t stride)
+{
+    return stride >= cols && stride <= (int64_t(1) << 46) / std::max<int64_t>(rows, 1);
+}
+
+bool valid_dtype(int dtype) { return dtype == LT_DTYPE_F32 || dtype == LT_DTYPE_BF16; }
+
+size_t span_bytes(int64_t rows, int64_t cols, int64_t stride, int dtype)
+{
+    if (rows == 0 || cols == 0)
+        return 0;
+    return size_t((rows - 1) * stride + cols) * (dtype == LT_DTYPE_BF16 ? 2 : 4);
+}
+
+// Whether the tiles can read rows of k values, `stride` apart, as they are.
+bool readable(int64_t k, int64_t stride) { return k % kStep == 0 && stride % 8 == 0 && stride < 2 * kMost; }
+
+int64_t take(int64_t& at, int64_t bytes)
+{
+    const int64_t from = at;
+    at += int64_t(host::round_up(size_t(bytes), 256));
+    return from;
+}
+
+struct ForwardLayout {
+    int64_t x = -1, gate = -1, up = -1;  // of packed copies
+    int64_t total = 0;
+};
+
+ForwardLayout forward_layout(int64_t m, int64_t n, int64_t k, int64_t x_stride,
+                             int64_t gate_stride, int64_t up_stride)
+{
+    ForwardLayout l;
+    const int64_t pitch = padded(k) * 2;
+    if (!readable(k, x_stride))
+        l.x = take(l.total, m * pitch);
+    if (!readable(k, gate_stride))
+        l.gate = take(l.total, n * pitch);
+    if (!readable(k, up_stride))
+        l.up = take(l.total, n * pitch);
+    l.total = std::max<int64_t>(l.total, 256);
+    return l;
+}
+
+struct BackwardLayout {
+    int64_t by_rows = -1, turned = -1, w = -1, x = -1, partial = -1;
+    int64_t total = 0;
+};
+
+BackwardLayout backward_layout(int64_t m, int64_t n, int64_t k, bool dx, bool dw)
+{
+    BackwardLayout l;
+    if (dx) {
+        l.by_rows = take(l.total, m * 2 * padded(n) * 2);
+        l.w = take(l.total, k * 2 * padded(n) * 2);
+    }
+    if (dw) {
+        l.turned = take(l.total, 2 * n * padded(m) * 2);
+        l.x = take(l.total, k * padded(m) * 2);
+    }
+    int64_t partial = 0;
+    if (dx) {
+        const Way w = way_of(m, k, 1, int(2 * padded(n) / kStep), false);
+        if (w.slices > 1)
+            partial = w.slices * m * k * 4;
+    }
+    if (dw) {
+        const Way w = way_of(n, k, 2, int(padded(m) / kStep), false);
+        if (w.slices > 1)
+            partial = std::max(partial, w.slices * 2 * n * k * 4);
+    }
+    if (partial)
+        l.partial = take(l.total, partial);
+    l.total = std::max<int64_t>(l.total, 256);
+    return l;
+}
+
+uint32_t groups_for(int64_t work) { return uint32_t(std::min<int64_t>(host::ceil_div(work, 256), 8192)); }
+
+void launch_pack(const void* x, int64_t rows, int64_t cols, int64_t stride, uint8_t* out,
+                 hipStream_t st)
+{
+    const PackArgs a{static_cast<const uint16_t*>(x), rows, cols, stride,
+                     reinterpret_cast<uint16_t*>(out), padded(cols)};
+    k_gated_pack<<<dim3(groups_for(rows * a.pitch / 8)), 256, 0, st>>>(a);
+}
+
+void launch_turn(const void* x, int64_t rows, int64_t cols, int64_t stride, uint8_t* out,
+                 int64_t pitch, hipStream_t st)
+{
+    const PackArgs a{static_cast<const uint16_t*>(x), rows, cols, stride,
+                     reinterpret_cast<uint16_t*>(out), pitch};
+    k_gated_turn<<<dim3(uint32_t(host::ceil_div(rows, 64) * host::ceil_div(cols, 64))), 256, 0,
+                   st>>>(a);
+}
+
+template <typename Tile>
+void launch_forward(const ForwardArgs& g, bool f32, bool save, hipStream_t st)
+{
+    auto* kernel = save ? (f32 ? k_gated_forward<Tile, true, true>
+                               : k_gated_forward<Tile, false, true>)
+                        : (f32 ? k_gated_forward<Tile, true, false>
+                               : k_gated_forward<Tile, false, false>);
+    kernel<<<dim3(uint32_t(host::ceil_div(g.m, Tile::kRows) *
+                           host::ceil_div(g.n, Tile::kCols / 2))),
+             Tile::kThreads, 0, st>>>(g);
+}
+
+template <typename Tile>
+void launch_product(const ProductArgs& g, const Way& w, bool f32, hipStream_t st)
+{
+    const dim3 grid(uint32_t(host::ceil_div(g.m, Tile::kRows) * host::ceil_div(g.n, Tile::kCols) *
+                             g.count),
+                    uint32_t(w.slices));
+    if (f32)
+        k_gated_product<Tile, true><<<grid, Tile::kThreads, 0, st>>>(g);
+    else
+        k_gated_product<Tile, false><<<grid, Tile::kThreads, 0, st>>>(g);
+}
+
+void run_product(ProductArgs g, bool f32, uint8_t* partial, hipStream_t st)
+{
+    const Way w = way_of(g.m, g.n, g.count, g.steps, false);
+    g.slice = w.slice;
+    g.partial = w.slices > 1 ? reinterpret_cast<float*>(partial) : nullptr;
+    if (w.tile == 256)
+        launch_product<Large>(g, w, f32, st);
+    else if (w.tile == 128)
+        launch_product<Small>(g, w, f32, st);
+    else
+        launch_product<Tiny>(g, w, f32, st);
+    if (g.partial) {
+        auto* join = f32 ? k_gated_join<true> : k_gated_join<false>;
+        join<<<dim3(groups_for(g.m * g.n * g.count)), 256, 0, st>>>(g, w.slices);
+    }
+}
+
+struct Read {
+    const void* p;
+    size_t bytes;
+};
+
+}  // namespace
+
+namespace host {
+
+lt_err launch_zero(void* out, int item, int64_t m, int64_t n, int64_t stride, hipStream_t st)
+{
+    const ZeroArgs a{out, m, n, stride};
+    if (item == 1)
+        k_zero_rows<uint8_t><<<dim3(groups_for(m * n)), 256, 0, st>>>(a);
+    else if (item == 2)
+        k_zero_rows<uint16_t><<<dim3(groups_for(m * n)), 256, 0, st>>>(a);
+    else
+        k_zero_rows<uint32_t><<<dim3(groups_for(m * n)), 256, 0, st>>>(a);
+    LT_TRY_HIP(hipGetLastError());
+    return LT_OK;
+}
+
+}  // namespace host
+
+extern "C" {
+
+size_t lt_gated_saved_bytes(int64_t m, int64_t n)
+{
+    if (m < 0 || n < 0 || m >= kMost || n >= kMost)
+        return 0;
+    return size_t(m) * size_t(host::ceil_div(n, 8) * 8) * 6;
+}
+
+size_t lt_gated_forward_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t x_stride,
+                                        int64_t gate_stride, int64_t up_stride)
+{
+    if (!valid_sizes(m, n, k))
+        return 0;
+    return size_t(forward_layout(m, n, k, x_stride, gate_stride, up_stride).total);
+}
+
+lt_err lt_gated_forward(const void* x, int64_t x_stride, const void* gate, int64_t gate_stride,
+                        const void* up, int64_t up_stride, int activation, int64_t m, int64_t n,
+                        int64_t k, void* out, int out_dtype, int64_t out_stride, void* saved,
+                        void* workspace, size_t workspace_bytes, void* stream)
+try {
+    host::clear_error();
+    if (!valid_sizes(m, n, k) || !valid_stride(m, n, out_stride) || !valid_stride(m, k, x_stride) ||
+        !valid_stride(n, k, gate_stride) || !valid_stride(n, k, up_stride))
+        return fail(LT_ERR_INVALID_ARG, "need 0 <= m, n, k < 2^21, fewer than 2^23 tiles of 64 x 64 "
+                                        "in each matrix, and strides of a row's length or more");
+    if (!valid_dtype(out_dtype))
+        return fail(LT_ERR_INVALID_ARG, "out_dtype must be LT_DTYPE_F32 or LT_DTYPE_BF16");
+    if (activation < LT_ACT_SILU || activation > LT_ACT_RELU)
+        return fail(LT_ERR_INVALID_ARG, "unknown activation");
+    if (m == 0 || n == 0)
+        return LT_OK;
+    if (!out || (k > 0 && (!x || !gate || !up)))
+        return fail(LT_ERR_INVALID_ARG, "x, the weights and out must not be NULL");
+    if (!host::aligned(x, 16) || !host::aligned(gate, 16) || !host::aligned(up, 16) ||
+        !host::aligned(out, 16) || !host::aligned(saved, 16))
+        return fail(LT_ERR_ALIGNMENT, "x, the weights, out and saved must be 16-byte aligned");
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    const size_t out_bytes = span_bytes(m, n, out_stride, out_dtype);
+    const size_t saved_bytes = saved ? lt_gated_saved_bytes(m, n) : 0;
+    const bool few = m <= gated::kFewTokens && !saved;
+    const ForwardLayout l = forward_layout(m, n, k, x_stride, gate_stride, up_stride);
+    const bool works = !few && k > 0 && (l.x >= 0 || l.gate >= 0 || l.up >= 0);
+    if (works && (!workspace || !host::aligned(workspace, 256) || workspace_bytes < size_t(l.total)))
+        return fail(LT_ERR_WORKSPACE, "workspace must be 256-byte aligned and hold " +
+                                          std::to_string(l.total) + " bytes");
+    const size_t ws_bytes = works ? size_t(l.total) : 0;
+    const Read read[] = {{x, span_bytes(m, k, x_stride, LT_DTYPE_BF16)},
+                         {gate, span_bytes(n, k, gate_stride, LT_DTYPE_BF16)},
+                         {up, span_bytes(n, k, up_stride, LT_DTYPE_BF16)}};
+    for (const Read& r : read)
+        if (host::overlaps(out, out_bytes, r.p, r.bytes) ||
+            host::overlaps(saved, saved_bytes, r.p, r.bytes) ||
+            host::overlaps(workspace, ws_bytes, r.p, r.bytes))
+            return fail(LT_ERR_INVALID_ARG, "an array that is written overlaps x or a weight");
+    if (host::overlaps(out, out_bytes, saved, saved_bytes) ||
+        host::overlaps(out, out_bytes, workspace, ws_bytes) ||
+        host::overlaps(saved, saved_bytes, workspace, ws_bytes))
+        return fail(LT_ERR_INVALID_ARG, "out, saved and the workspace overlap");
+    if (k == 0) {  // empty sums: act(0) * 0, and a = b = 0
+        if (saved)
+            if (lt_err e = host::launch_zero(saved, 1, 1, int64_t(saved_bytes), int64_t(saved_bytes),
+                                             st))
+                return e;
+        return host::launch_zero(out, out_dtype == LT_DTYPE_F32 ? 4 : 2, m, n, out_stride, st);
+    }
+    const bool f32 = out_dtype == LT_DTYPE_F32;
+    if (few) {
+        gated::FewArgs f{};
+        f.w[0] = static_cast<const uint8_t*>(gate);
+        f.w[1] = static_cast<const uint8_t*>(up);
+        f.w_pitch[0] = gate_stride * 2;
+        f.w_pitch[1] = up_stride * 2;
+        f.x = static_cast<const uint8_t*>(x);
+        f.x_pitch = x_stride * 2;
+        f.m = m;
+        f.n = n;
+        f.bytes = k * 2;
+        f.activation = activation;
+        f.out = out;
+        f.stride = out_stride;
+        gated::launch_few<gated::FewBf16, 2>(f, f32, st);
+        LT_TRY_HIP(hipGetLastError());
+        return LT_OK;
+    }
+    auto* ws = static_cast<uint8_t*>(workspace);
+    if (works)
+        if (lt_err e = host::workspace_written(ws, ws_bytes, st))
+            return e;
+    ForwardArgs g{};
+    g.steps = int(padded(k) / kStep);
+    g.m = m;
+    g.n = n;
+    g.activation = activation;
+    g.out = out;
+    g.stride = out_stride;
+    if (saved)
+        g.saved = saved_layout(saved, m, n);
+    const auto operand = [&](const void* p, int64_t rows, int64_t stride, int64_t at,
+                             const uint8_t** from, int64_t* pitch) {
+        *from = static_cast<const uint8_t*>(p);
+        *pitch = stride * 2;
+        if (at < 0)
+            return;
+        launch_pack(p, rows, k, stride, ws + at, st);
+        *from = ws + at;
+        *pitch = padded(k) * 2;
+    };
+    operand(x, m, x_stride, l.x, &g.x, &g.x_pitch);
+    operand(gate, n, gate_stride, l.gate, &g.gate, &g.gate_pitch);
+    operand(up, n, up_stride, l.up, &g.up, &g.up_pitch);
+    const Way w = way_of(m, n, 1, g.steps, true);
+    if (w.tile == 256)
+        launch_forward<Large>(g, f32, saved != nullptr, st);
+    else if (w.tile == 128)
+        launch_forward<Small>(g, f32, saved != nullptr, st);
+    else
+        launch_forward<Pair>(g, f32, saved != nullptr, st);
+    LT_TRY_HIP(hipGetLastError());
+    return LT_OK;
+} catch (...) {
+    return host::caught();
+}
+
+size_t lt_gated_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int dx, int dw)
+{
+    if (!valid_sizes(m, n, k))
+        return 0;
+    return size_t(backward_layout(m, n, k, dx != 0, dw != 0).total);
+}
+
+lt_err lt_gated_backward(const void* dh, int dh_dtype, int64_t dh_stride, const void* saved,
+                         const void* x, int64_t x_stride, const void* gate, int64_t gate_stride,
+                         const void* up, int64_t up_stride, int64_t m, int64_t n, int64_t k,
+                         void* dx, int dx_dtype, int64_t dx_stride, void* dgate,
+                         int64_t dgate_stride, void* dup, int64_t dup_stride, int grad_dtype,
+                         void* workspace, size_t workspace_bytes, void* stream)
+try {
+    host::clear_error();
+    const bool want_dw = dgate || dup;
+    if (!valid_sizes(m, n, k) || !valid_stride(m, n, dh_stride) ||
+        (want_dw && (!valid_stride(m, k, x_stride) || !valid_stride(n, k, dgate_stride) ||
+                     !valid_stride(n, k, dup_stride))) ||
+        (dx && (!valid_stride(n, k, gate_stride) || !valid_stride(n, k, up_stride) ||
+                !valid_stride(m, k, dx_stride))))
+        return fail(LT_ERR_INVALID_ARG, "need 0 <= m, n, k < 2^21, fewer than 2^23 tiles of 64 x 64 "
+                                        "in each matrix, and strides of a row's length or more");
+    if (!valid_dtype(dh_dtype) || !valid_dtype(dx_dtype) || !valid_dtype(grad_dtype))
+        return fail(LT_ERR_INVALID_ARG, "dtypes must be LT_DTYPE_F32 or LT_DTYPE_BF16");
+    if ((dgate != nullptr) != (dup != nullptr))
+        return fail(LT_ERR_INVALID_ARG, "the weights' gradients come together");
+    if (k == 0 || (!dx && !want_dw))
+        return LT_OK;
+    const bool empty = m == 0 || n == 0;
+    if (!empty && (!dh || !saved || (dx && (!gate || !up)) || (want_dw && !x)))
+        return fail(LT_ERR_INVALID_ARG, "dh, saved and the operands must not be NULL");
+    if (!host::aligned(dh, dh_dtype == LT_DTYPE_BF16 ? 2 : 4) || !host::aligned(saved, 16) ||
+        !host::aligned(x, 2) || !host::aligned(gate, 2) || !host::aligned(up, 2) ||
+        !host::aligned(dx, 16) || !host::aligned(dgate, 16) || !host::aligned(dup, 16))
+        return fail(LT_ERR_ALIGNMENT, "operands must be aligned to their elements, saved and the "
+                                      "gradients to 16 bytes");
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    const size_t need = lt_gated_backward_workspace_bytes(m, n, k, dx != nullptr, want_dw);
+    if (!empty && (!workspace || !host::aligned(workspace, 256) || workspace_bytes < need))
+        return fail(LT_ERR_WORKSPACE, "workspace must be 256-byte aligned and hold " +
+                                          std::to_string(need) + " bytes");
+    std::vector<host::Range> ranges;
+    const auto range = [&](const void* p, size_t bytes, bool written) {
+        const auto lo = reinterpret_cast<uintptr_t>(p);
+        if (p && bytes)
+            ranges.push_back({lo, lo + bytes, written});
+    };
+    range(dx, span_bytes(m, k, dx_stride, dx_dtype), true);
+    range(dgate, span_bytes(n, k, dgate_stride, grad_dtype), true);
+    range(dup, span_bytes(n, k, dup_stride, grad_dtype), true);
+    if (!empty) {
+        range(dh, span_bytes(m, n, dh_stride, dh_dtype), false);
+        range(saved, lt_gated_saved_bytes(m, n), false);
+        range(workspace, need, true);
+        if (want_dw)
+            range(x, span_bytes(m, k, x_stride, LT_DTYPE_BF16), false);
+        if (dx) {
+            range(gate, span_bytes(n, k, gate_stride, LT_DTYPE_BF16), false);
+            range(up, span_bytes(n, k, up_stride, LT_DTYPE_BF16), false);
+        }
+    }
+    const std::string overlap = host::overlap(ranges);
+    if (!overlap.empty())
+        return fail(LT_ERR_INVALID_ARG, overlap);
+    if (empty) {  // empty sums
+        if (dx && m > 0)
+            return host::launch_zero(dx, dx_dtype == LT_DTYPE_F32 ? 4 : 2, m, k, dx_stride, st);
+        if (want_dw && n > 0) {
+            const int item = grad_dtype == LT_DTYPE_F32 ? 4 : 2;
+            if (lt_err e = host::launch_zero(dgate, item, n, k, dgate_stride, st))
+                return e;
+            return host::launch_zero(dup, item, n, k, dup_stride, st);
+        }
+        return LT_OK;
+    }
+    auto* ws = static_cast<uint8_t*>(workspace);
+    if (lt_err e = host::workspace_written(ws, need, st))
+        return e;
+    const BackwardLayout l = backward_layout(m, n, k, dx != nullptr, want_dw);
+    const int64_t half = padded(n), tokens = padded(m);
+    const SlopeArgs s{dh,
+                      dh_stride,
+                      saved_layout(const_cast<void*>(saved), m, n),
+                      m,
+                      n,
+                      dx ? reinterpret_cast<uint16_t*>(ws + l.by_rows) : nullptr,
+                      half,
+                      want_dw ? reinterpret_cast<uint16_t*>(ws + l.turned) : nullptr,
+                      tokens};
+    const dim3 blocks(uint32_t(half / 64 * (tokens / 64)));
+    if (dh_dtype == LT_DTYPE_F32)
+        k_gated_slopes<true><<<blocks, 256, 0, st>>>(s);
+    else
+        k_gated_slopes<false><<<blocks, 256, 0, st>>>(s);
+    uint8_t* partial = l.partial < 0 ? nullptr : ws + l.partial;
+    if (dx) {
+        launch_turn(gate, n, k, gate_stride, ws + l.w, 2 * half, st);
+        launch_turn(up, n, k, up_stride, ws + l.w + half * 2, 2 * half, st);
+        ProductArgs g{};
+        g.a = ws + l.by_rows;
+        g.b = ws + l.w;
+        g.a_pitch = g.b_pitch = 4 * half;
+        g.m = m;
+        g.n = k;
+        g.count = 1;
+        g.steps = int(2 * half / kStep);
+        g.out[0] = dx;
+        g.stride[0] = dx_stride;
+        run_product(g, dx_dtype == LT_DTYPE_F32, partial, st);
+    }
+    if (want_dw) {
+        launch_turn(x, m, k, x_stride, ws + l.x, tokens, st);
+        ProductArgs g{};
+        g.a = ws + l.turned;
+        g.b = ws + l.x;
+        g.a_pitch = g.b_pitch = 2 * tokens;
+        g.m = n;
+        g.n = k;
+        g.count = 2;
+        g.steps = int(tokens / kStep);
+        g.out[0] = dgate;
+        g.out[1] = dup;
+        g.stride[0] = dgate_stride;
+        g.stride[1] = dup_stride;
+        run_product(g, grad_dtype == LT_DTYPE_F32, partial, st);
+    }
+    LT_TRY_HIP(hipGetLastError());
+    return LT_OK;
+} catch (...) {
+    return host::caught();
+}
+
+}  // extern "C"

@@ -63,6 +63,11 @@ inline bool overlaps(const void* a, size_t a_bytes, const void* b, size_t b_byte
     return a && b && a_bytes && b_bytes && x < y + b_bytes && y < x + a_bytes;
 }
 
+// ------------------------------------------------------- empty sums (gated.hip)
+
+// Zeros in m rows of n elements of `item` bytes (1, 2 or 4), `stride` elements apart.
+lt_err launch_zero(void* out, int item, int64_t m, int64_t n, int64_t stride, hipStream_t st);
+
 // ------------------------------------------------------- 8-bit momentum (momentum.hip)
 
 // One matrix of a momentum launch.

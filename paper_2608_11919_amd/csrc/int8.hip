@@ -1,0 +1,666 @@
+// int8.hip -- matrix products in 8-bit integers with a scale for each row of either operand (a
+// token's, an output channel's), the gated projections made of them, and the quantizer.
+//
+// value = code * scale with scale = most / 127, `most` the row's largest magnitude.  Products of
+// codes are summed in 32-bit integers, exactly and in any order: 127^2 * 2^17 fits them.  The
+// scales leave the sum, so a result is one integer times two scales, three roundings of fp32.
+
+#include "gated.h"
+#include "host.h"
+
+#include <algorithm>
+#include <string>
+#include <vector>
+
+namespace {
+
+using host::fail;
+using namespace tiles;
+using gated::store_row;
+
+constexpr int kPitch = 128;  // a row of codes is padded with zeros to a multiple of this
+
+int64_t code_pitch(int64_t cols) { return host::ceil_div(cols, kPitch) * kPitch; }
+
+// ------------------------------------------------------------- quantizer
+
+struct QuantizeArgs {
+    const void* x;
+    int64_t rows, cols, stride, pitch;
+    int8_t* codes;
+    float* scales;
+};
+
+// A row's factor for its codes and its scale, from its largest magnitude.  Below 2^-100 the
+// factor would leave fp32's range: such a row is quantized as if it reached that.  A NaN or an
+// infinity makes the scale NaN and the codes 0.
+struct RowScale {
+    float factor, scale;
+};
+
+__device__ inline RowScale scale_of(uint32_t top)
+{
+    if (top >= 0x7F800000u)
+        return {0.0f, __builtin_nanf("")};
+    const float most = fmaxf(__uint_as_float(top), 0x1p-100f);
+    return {127.0f / most, most / 127.0f};
+}
+
+// The integer nearest to x * factor, ties to even, as a byte: the sum with 1.5 * 2^23 rounds the
+// exact product once, at its last bit.
+__device__ inline uint32_t code_of(float x, RowScale s)
+{
+    const float v = __builtin_fmaf(x, s.factor, 12582912.0f);
+    return s.factor == 0.0f ? 0u : __float_as_uint(v) & 0xFFu;
+}
+
+template <typename T>
+__device__ inline float value_at(const T* p)
+{
+    if constexpr (sizeof(T) == 2)
+        return __uint_as_float(uint32_t(*p) << 16);
+    else
+        return *p;
+}
+
+// Eight values from column `at` on.
+template <typename T>
+__device__ inline void load_eight(const T* row, int64_t at, int64_t cols, float (&v)[8])
+{
+    if (at + 8 <= cols) {
+        if constexpr (sizeof(T) == 2) {
+            const i32x4 w = load_any(row + at);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[2 * e] = __uint_as_float(uint32_t(w[e]) << 16);
+                v[2 * e + 1] = __uint_as_float(uint32_t(w[e]) & 0xFFFF0000u);
+            }
+        } else {
+            const f32x4 a = __builtin_bit_cast(f32x4, load_any(row + at));
+            const f32x4 b = __builtin_bit_cast(f32x4, load_any(row + at + 4));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[e] = a[e];
+                v[4 + e] = b[e];
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        v[e] = at + e < cols ? value_at(row + at + e) : 0.0f;
+}
+
+__device__ inline uint2 codes_of(const float (&v)[8], RowScale s)
+{
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        w[e / 4] |= code_of(v[e], s) << (8 * (e % 4));
+    return make_uint2(w[0], w[1]);
+}
+
+// A row by WAVES waves, eight values a lane and HELD pieces of the row in registers; what is
+// longer is read a second time (out of L2).
+template <typename T, int WAVES, int HELD>
+__global__ __launch_bounds__(256) void k_int8_quantize(QuantizeArgs a)
+{
+    constexpr int kThreads = 64 * WAVES, kRows = 4 / WAVES;
+    __shared__ uint32_t tops[4];
+    const int t = int(threadIdx.x) % kThreads, wave = int(threadIdx.x) >> 6;
+    for (int64_t r0 = int64_t(blockIdx.x) * kRows; r0 < a.rows; r0 += int64_t(gridDim.x) * kRows) {
+        const int64_t row = r0 + int(threadIdx.x) / kThreads;
+        const bool there = row < a.rows;
+        const T* x = static_cast<const T*>(a.x) + (there ? row : 0) * a.stride;
+        const int64_t cols = there ? a.cols : 0;
+        float v[HELD][8];
+        uint32_t top = 0;
+        const auto look = [&](const float (&w)[8]) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                top = max(top, __float_as_uint(w[e]) & 0x7FFFFFFFu);
+        };
+#pragma unroll
+        for (int h = 0; h < HELD; ++h)
+            load_eight(x, (h * kThreads + t) * 8, cols, v[h]);
+#pragma unroll
+        for (int h = 0; h < HELD; ++h)
+            look(v[h]);
+        for (int64_t at = (HELD * kThreads + t) * 8; at < cols; at += kThreads * 8) {
+            float w[8];
+            load_eight(x, at, cols, w);
+            look(w);
+        }
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1)
+            top = max(top, uint32_t(__shfl_xor(int(top), o, 64)));
+        if constexpr (WAVES > 1) {
+            if (t % 64 == 0)
+                tops[wave] = top;
+            __syncthreads();
+            top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+            __syncthreads();
+        }
+        if (!there)
+            continue;
+        const RowScale s = scale_of(top);
+        int8_t* to = a.codes + row * a.pitch;
+        if (t == 0)
+            a.scales[row] = s.scale;
+#pragma unroll
+        for (int h = 0; h < HELD; ++h) {
+            const int64_t at = (h * kThreads + t) * 8;
+            if (at < a.pitch)
+                *reinterpret_cast<uint2*>(to + at) = codes_of(v[h], s);
+        }
+        for (int64_t at = (HELD * kThreads + t) * 8; at < a.pitch; at += kThreads * 8) {
+            float w[8];
+            load_eight(x, at, cols, w);
+            *reinterpret_cast<uint2*>(to + at) = codes_of(w, s);
+        }
+    }
+}
+
+// ------------------------------------------------------------- products
+
+struct ProductArgs {
+    const uint8_t *a, *b, *c;  // c: the second weight of a pair
+    const float *a_scales, *b_scales, *c_scales;
+    int64_t m, n, pitch;
+    int steps, slice;
+    int activation;
+    void* out;
+    int64_t stride;
+    int32_t* partial;  // several slices: [slice][m][n]
+};
+
+__device__ inline float scaled(float bits, float row, float col)
+{
+    return float(__float_as_int(bits)) * row * col;
+}
+
+template <bool F32>
+struct ProductWriter {
+    static constexpr bool kTurned = false;
+    static constexpr int kSlots = 8;
+    const ProductArgs& g;
+    int64_t r0, c0;
+    __device__ inline void fetch(int, int, int) {}
+    __device__ inline void turn(int, int, const float (&)[8]) {}
+    __device__ inline void scales_at(const float* from, int64_t col, float (&s)[8]) const
+    {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            s[e] = from[col + e < g.n ? col + e : g.n - 1];
+    }
+    __device__ inline void store(int row_, int col_, float (&v)[8], int)
+    {
+        const int64_t row = r0 + row_, col = c0 + col_;
+        if (row >= g.m || col >= g.n)
+            return;
+        if (g.partial) {  // the integers' bits
+            store_row<true>(g.partial, (int64_t(blockIdx.y) * g.m + row) * g.n + col, v,
+                            g.n - col);
+            return;
+        }
+        float s[8];
+        scales_at(g.b_scales, col, s);
+        const float x = g.a_scales[row];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            v[e] = scaled(v[e], x, s[e]);
+        store_row<F32>(g.out, row * g.stride + col, v, g.n - col);
+    }
+    // of a pair
+    __device__ inline void store(int row_, int col_, float (&u)[8], float (&v)[8])
+    {
+        const int64_t row = r0 + row_, col = c0 + col_;
+        if (row >= g.m || col >= g.n)
+            return;
+        float s[8], t[8];
+        scales_at(g.b_scales, col, s);
+        scales_at(g.c_scales, col, t);
+        const float x = g.a_scales[row];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            u[e] = gated::activate(g.activation, scaled(u[e], x, s[e])) * scaled(v[e], x, t[e]);
+        store_row<F32>(g.out, row * g.stride + col, u, g.n - col);
+    }
+};
+
+template <typename Tile, bool F32>
+__global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_int8_product(ProductArgs g)
+{
+    __shared__ __align__(1024) uint8_t lds[Tile::kLdsBytes];
+    const TilePlace at = tile_place(int(unit_of_workgroup(Tile::kRun)),
+                                    int((g.m + Tile::kRows - 1) / Tile::kRows),
+                                    int((g.n + Tile::kCols - 1) / Tile::kCols));
+    const int64_t r0 = int64_t(at.row) * Tile::kRows, c0 = int64_t(at.col) * Tile::kCols;
+    const int first = int(blockIdx.y) * g.slice, steps = min(g.slice, g.steps - first);
+    Tile tile;
+    Int8 mul;
+    const int64_t k0 = int64_t(first) * kStepBytes;
+    product(mul, tile, g.a + r0 * g.pitch + k0, g.pitch, g.m - r0, g.b + c0 * g.pitch + k0, g.pitch,
+            g.n - c0, steps, lds);
+    ProductWriter<F32> w{g, r0, c0};
+    finish(tile, lds, w);
+}
+
+template <typename Tile, bool F32>
+__global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_int8_gated(ProductArgs g)
+{
+    __shared__ __align__(1024) uint8_t lds[Tile::kLdsBytes];
+    constexpr int kCols = Tile::kCols / 2;
+    const TilePlace at = tile_place(int(unit_of_workgroup(Tile::kRun)),
+                                    int((g.m + Tile::kRows - 1) / Tile::kRows),
+                                    int((g.n + kCols - 1) / kCols));
+    const int64_t r0 = int64_t(at.row) * Tile::kRows, c0 = int64_t(at.col) * kCols;
+    Tile tile;
+    Int8 mul;
+    product_pairs(mul, tile, g.a + r0 * g.pitch, g.pitch, g.m - r0, g.b + c0 * g.pitch, g.pitch,
+                  g.c + c0 * g.pitch, g.pitch, g.n - c0, g.steps, lds);
+    ProductWriter<F32> w{g, r0, c0};
+    finish_pairs(tile, lds, w);
+}
+
+template <bool F32>
+__global__ __launch_bounds__(256) void k_int8_join(ProductArgs g, int slices)
+{
+    const int64_t all = g.m * g.n;
+    for (int64_t e = int64_t(blockIdx.x) * 256 + threadIdx.x; e < all;
+         e += int64_t(gridDim.x) * 256) {
+        int s = g.partial[e];
+        for (int i = 1; i < slices; ++i)
+            s += g.partial[i * all + e];
+        const int64_t row = e / g.n, col = e % g.n;
+        const float v = float(s) * g.a_scales[row] * g.b_scales[col];
+        if constexpr (F32)
+            static_cast<float*>(g.out)[row * g.stride + col] = v;
+        else
+            static_cast<uint16_t*>(g.out)[row * g.stride + col] = gated::bf16_bits(v);
+    }
+}
+
+// ---------------------------------------------------------------- host side
+
+constexpr int64_t kMostSummed = int64_t(1) << 17;  // 127^2 * 2^17 < 2^31
+constexpr int64_t kMostGroups = int64_t(1) << 24;  // a grid counts threads in 32 bits
+
+struct Way {
+    int tile;    // 256, 128 or 64
+    int slices;  // of the sum
+    int slice;   // steps of each
+};
+
+// As the products in 8-bit floating point: the largest tile that gives every CU a workgroup; few
+// results of a long sum are cut into slices.
+constexpr int kLongSum = 48;
+
+Way way_of(int64_t m, int64_t n, int64_t k, bool pair)
+{
+    const int steps = int(host::ceil_div(k, kPitch));
+    Way w{64, 1, steps};
+    int64_t tiles = 0;
+    for (const int t : {256, 128, 64}) {
+        w.tile = t;
+        const int64_t wide = pair && t > 64 ? t / 2 : t;
+        tiles = host::ceil_div(m, t) * host::ceil_div(n, wide);
+        if (tiles >= 256)
+            return w;
+    }
+    if (steps < kLongSum || pair)
+        return w;
+    const int want = int(std::min<int64_t>(steps / 4, host::ceil_div(512, std::max<int64_t>(tiles, 1))));
+    w.slice = int(host::ceil_div(steps, std::max(want, 1)));
+    w.slices = int(host::ceil_div(steps, w.slice));
+    return w;
+}
+
+bool valid_sizes(int64_t m, int64_t n, int64_t k)
+{
+    const int64_t most = int64_t(1) << 26;
+    return m >= 0 && n >= 0 && k >= 0 && m < most && n < most && k <= kMostSummed &&
+           host::ceil_div(m, 64) * host::ceil_div(n, 64) < kMostGroups;
+}
+
+bool valid_stride(int64_t rows, int64_t cols, int64_t stride)
+{
+    return stride >= cols && stride <= (int64_t(1) << 46) / std::max<int64_t>(rows, 1);
+}
+
+bool valid_dtype(int dtype) { return dtype == LT_DTYPE_F32 || dtype == LT_DTYPE_BF16; }
+
+size_t span_bytes(int64_t rows, int64_t cols, int64_t stride, int dtype)
+{
+    if (rows == 0 || cols == 0)
+        return 0;
+    return size_t((rows - 1) * stride + cols) * (dtype == LT_DTYPE_BF16 ? 2 : 4);
+}
+
+lt_err launch_quantize(const void* x, int dtype, int64_t rows, int64_t cols, int64_t stride,
+                       int8_t* codes, float* scales, hipStream_t st)
+{
+    const QuantizeArgs a{x, rows, cols, stride, code_pitch(cols), codes, scales};
+    const auto go = [&](auto* kernel, int64_t rows_each) {
+        const int64_t groups = std::min<int64_t>(host::ceil_div(rows, rows_each), 1 << 20);
+        kernel<<<dim3(uint32_t(groups)), 256, 0, st>>>(a);
+    };
+    const auto pick = [&](auto zero) {
+        typedef decltype(zero) T;
+        if (a.pitch <= 512)
+            go(k_int8_quantize<T, 1, 1>, 4);
+        else if (a.pitch <= 2048)
+            go(k_int8_quantize<T, 4, 1>, 1);
+        else if (a.pitch <= 4096)
+            go(k_int8_quantize<T, 4, 2>, 1);
+        else
+            go(k_int8_quantize<T, 4, 4>, 1);
+    };
+    if (dtype == LT_DTYPE_BF16)
+        pick(uint16_t());
+    else
+        pick(float());
+    LT_TRY_HIP(hipGetLastError());
+    return LT_OK;
+}
+
+void launch_product(const ProductArgs& g, const Way& w, bool f32, hipStream_t st)
+{
+    const auto go = [&](auto* kernel, auto tile) {
+        typedef decltype(tile) Tile;
+        const dim3 grid(uint32_t(host::ceil_div(g.m, Tile::kRows) * host::ceil_div(g.n, Tile::kCols)),
+                        uint32_t(w.slices));
+        kernel<<<grid, Tile::kThreads, 0, st>>>(g);
+    };
+    if (w.tile == 256)
+        go(f32 ? k_int8_product<Large, true> : k_int8_product<Large, false>, Large());
+    else if (w.tile == 128)
+        go(f32 ? k_int8_product<Small, true> : k_int8_product<Small, false>, Small());
+    else
+        go(f32 ? k_int8_product<Tiny, true> : k_int8_product<Tiny, false>, Tiny());
+}
+
+void launch_gated(const ProductArgs& g, const Way& w, bool f32, hipStream_t st)
+{
+    const auto go = [&](auto* kernel, auto tile) {
+        typedef decltype(tile) Tile;
+        kernel<<<dim3(uint32_t(host::ceil_div(g.m, Tile::kRows) *
+                               host::ceil_div(g.n, Tile::kCols / 2))),
+                 Tile::kThreads, 0, st>>>(g);
+    };
+    if (w.tile == 256)
+        go(f32 ? k_int8_gated<Large, true> : k_int8_gated<Large, false>, Large());
+    else if (w.tile == 128)
+        go(f32 ? k_int8_gated<Small, true> : k_int8_gated<Small, false>, Small());
+    else
+        go(f32 ? k_int8_gated<Pair, true> : k_int8_gated<Pair, false>, Pair());
+}
+
+lt_err zero_rows(void* out, int dtype, int64_t m, int64_t n, int64_t stride, hipStream_t st)
+{
+    return host::launch_zero(out, dtype == LT_DTYPE_F32 ? 4 : 2, m, n, stride, st);
+}
+
+// Workspace of the calls that quantize x themselves: [codes][scales][the product's].
+struct LinearLayout {
+    size_t scales, matmul, total;
+};
+
+LinearLayout linear_layout(int64_t m, int64_t n, int64_t k, bool pair)
+{
+    LinearLayout l;
+    l.scales = host::round_up(size_t(m) * size_t(code_pitch(k)), 256);
+    l.matmul = l.scales + host::round_up(size_t(m) * 4, 256);
+    l.total = l.matmul + (pair ? 0 : lt_int8_matmul_workspace_bytes(m, n, k));
+    return l;
+}
+
+// The product of codes, its arguments checked.  c: the second weight of a pair, or null.
+lt_err run_product(const ProductArgs& args, int64_t k, int out_dtype, void* workspace,
+                   hipStream_t st)
+{
+    ProductArgs g = args;
+    const bool f32 = out_dtype == LT_DTYPE_F32, pair = g.c != nullptr;
+    g.pitch = code_pitch(k);
+    g.steps = int(host::ceil_div(k, kPitch));
+    if (g.m <= gated::kFewTokens) {
+        gated::FewArgs f{};
+        f.w[0] = g.b;
+        f.w[1] = g.c;
+        f.w_pitch[0] = f.w_pitch[1] = f.x_pitch = f.bytes = g.pitch;
+        f.x = g.a;
+        f.w_scales[0] = g.b_scales;
+        f.w_scales[1] = g.c_scales;
+        f.x_scales = g.a_scales;
+        f.m = g.m;
+        f.n = g.n;
+        f.activation = g.activation;
+        f.out = g.out;
+        f.stride = g.stride;
+        if (pair)
+            gated::launch_few<gated::FewInt8, 2>(f, f32, st);
+        else
+            gated::launch_few<gated::FewInt8, 1>(f, f32, st);
+        LT_TRY_HIP(hipGetLastError());
+        return LT_OK;
+    }
+    const Way w = way_of(g.m, g.n, k, pair);
+    g.slice = w.slice;
+    if (w.slices > 1)
+        g.partial = static_cast<int32_t*>(workspace);
+    if (pair)
+        launch_gated(g, w, f32, st);
+    else
+        launch_product(g, w, f32, st);
+    if (g.partial) {
+        auto* join = f32 ? k_int8_join<true> : k_int8_join<false>;
+        join<<<dim3(uint32_t(std::min<int64_t>(4096, host::ceil_div(g.m * g.n, 256)))), 256, 0,
+               st>>>(g, w.slices);
+    }
+    LT_TRY_HIP(hipGetLastError());
+    return LT_OK;
+}
+
+// f11's and f12's answers to values: w2 is the second weight of a pair, or not given.
+lt_err answer(const void* x, int dtype, int64_t x_stride, const int8_t* w, const float* w_scales,
+              bool pair, const int8_t* w2, const float* w2_scales, int activation, int64_t m,
+              int64_t n, int64_t k, void* out, int out_dtype, int64_t out_stride, void* workspace,
+              size_t workspace_bytes, void* stream)
+{
+    if (!valid_sizes(m, n, k) || !valid_stride(m, n, out_stride) || !valid_stride(m, k, x_stride))
+        return fail(LT_ERR_INVALID_ARG, "need 0 <= m, n < 2^26, tiles of 64 x 64 < 2^24, 0 <= k <= "
+                                        "2^17, x_stride >= k and out_stride >= n");
+    if (!valid_dtype(dtype) || !valid_dtype(out_dtype))
+        return fail(LT_ERR_INVALID_ARG, "dtypes must be LT_DTYPE_F32 or LT_DTYPE_BF16");
+    if (pair && (activation < LT_ACT_SILU || activation > LT_ACT_RELU))
+        return fail(LT_ERR_INVALID_ARG, "unknown activation");
+    if (m == 0 || n == 0)
+        return LT_OK;
+    if (!out || (k > 0 && (!x || !w || !w_scales || (pair && (!w2 || !w2_scales)))))
+        return fail(LT_ERR_INVALID_ARG, "x, the weight and out must not be NULL");
+    if (!host::aligned(x, dtype == LT_DTYPE_BF16 ? 2 : 4) || !host::aligned(w, 16) ||
+        !host::aligned(w2, 16) || !host::aligned(out, 16) || !host::aligned(w_scales, 4) ||
+        !host::aligned(w2_scales, 4))
+        return fail(LT_ERR_ALIGNMENT, "x and scales must be aligned to their elements, codes and "
+                                      "out to 16 bytes");
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (k == 0)
+        return zero_rows(out, out_dtype, m, n, out_stride, st);
+    const LinearLayout l = linear_layout(m, n, k, pair);
+    if (!workspace || !host::aligned(workspace, 256) || workspace_bytes < l.total)
+        return fail(LT_ERR_WORKSPACE, "workspace must be 256-byte aligned and hold " +
+                                          std::to_string(l.total) + " bytes");
+    const size_t out_bytes = span_bytes(m, n, out_stride, out_dtype);
+    const size_t w_bytes = size_t(n) * size_t(code_pitch(k));
+    const struct {
+        const void* p;
+        size_t bytes;
+    } read[] = {{x, span_bytes(m, k, x_stride, dtype)}, {w, w_bytes}, {w_scales, size_t(n) * 4},
+                {w2, w_bytes}, {w2_scales, size_t(n) * 4}};
+    for (const auto& r : read)
+        if (host::overlaps(out, out_bytes, r.p, r.bytes) ||
+            host::overlaps(workspace, l.total, r.p, r.bytes))
+            return fail(LT_ERR_INVALID_ARG, "out or the workspace overlaps x or a weight");
+    if (host::overlaps(out, out_bytes, workspace, l.total))
+        return fail(LT_ERR_INVALID_ARG, "out overlaps the workspace");
+    auto* ws = static_cast<uint8_t*>(workspace);
+    if (lt_err e = host::workspace_written(ws, l.total, st))
+        return e;
+    auto* codes = reinterpret_cast<int8_t*>(ws);
+    auto* scales = reinterpret_cast<float*>(ws + l.scales);
+    if (lt_err e = launch_quantize(x, dtype, m, k, x_stride, codes, scales, st))
+        return e;
+    ProductArgs g{};
+    g.a = ws;
+    g.b = reinterpret_cast<const uint8_t*>(w);
+    g.c = pair ? reinterpret_cast<const uint8_t*>(w2) : nullptr;
+    g.a_scales = scales;
+    g.b_scales = w_scales;
+    g.c_scales = w2_scales;
+    g.m = m;
+    g.n = n;
+    g.activation = activation;
+    g.out = out;
+    g.stride = out_stride;
+    return run_product(g, k, out_dtype, ws + l.matmul, st);
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t lt_int8_code_pitch(int64_t cols) { return cols < 0 ? 0 : code_pitch(cols); }
+
+lt_err lt_int8_quantize(const void* x, int dtype, int64_t rows, int64_t cols, int64_t row_stride,
+                        int8_t* codes, float* scales, void* stream)
+try {
+    host::clear_error();
+    if (!valid_dtype(dtype))
+        return fail(LT_ERR_INVALID_ARG, "dtype must be LT_DTYPE_F32 or LT_DTYPE_BF16");
+    const int64_t most = int64_t(1) << 31;
+    if (rows < 0 || cols < 0 || rows >= most || cols >= most ||
+        !valid_stride(rows, cols, row_stride))
+        return fail(LT_ERR_INVALID_ARG, "need 0 <= rows, cols < 2^31 and row_stride >= cols");
+    if (rows == 0 || cols == 0)
+        return LT_OK;
+    if (!x || !codes || !scales)
+        return fail(LT_ERR_INVALID_ARG, "x, codes and scales must not be NULL");
+    if (!host::aligned(x, dtype == LT_DTYPE_BF16 ? 2 : 4) || !host::aligned(codes, 16) ||
+        !host::aligned(scales, 4))
+        return fail(LT_ERR_ALIGNMENT, "x and scales must be aligned to their elements, codes to 16 "
+                                      "bytes");
+    const size_t x_bytes = span_bytes(rows, cols, row_stride, dtype);
+    const size_t code_bytes = size_t(rows) * size_t(code_pitch(cols));
+    if (host::overlaps(codes, code_bytes, x, x_bytes) ||
+        host::overlaps(scales, size_t(rows) * 4, x, x_bytes) ||
+        host::overlaps(codes, code_bytes, scales, size_t(rows) * 4))
+        return fail(LT_ERR_INVALID_ARG, "x, codes and scales overlap");
+    return launch_quantize(x, dtype, rows, cols, row_stride, codes, scales,
+                           static_cast<hipStream_t>(stream));
+} catch (...) {
+    return host::caught();
+}
+
+size_t lt_int8_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k)
+{
+    if (!valid_sizes(m, n, k))
+        return 0;
+    const Way w = way_of(m, n, k, false);
+    if (m <= gated::kFewTokens || w.slices == 1)
+        return 256;
+    return std::max(size_t(256), size_t(w.slices) * size_t(m) * size_t(n) * 4);
+}
+
+lt_err lt_int8_matmul(const int8_t* a_codes, const float* a_scales, const int8_t* b_codes,
+                      const float* b_scales, int64_t m, int64_t n, int64_t k, void* out,
+                      int out_dtype, int64_t out_stride, void* workspace, size_t workspace_bytes,
+                      void* stream)
+try {
+    host::clear_error();
+    if (!valid_sizes(m, n, k) || !valid_stride(m, n, out_stride))
+        return fail(LT_ERR_INVALID_ARG, "need 0 <= m, n < 2^26, tiles of 64 x 64 < 2^24, 0 <= k <= "
+                                        "2^17 and out_stride >= n");
+    if (!valid_dtype(out_dtype))
+        return fail(LT_ERR_INVALID_ARG, "out_dtype must be LT_DTYPE_F32 or LT_DTYPE_BF16");
+    if (m == 0 || n == 0)
+        return LT_OK;
+    if (!out || (k > 0 && (!a_codes || !a_scales || !b_codes || !b_scales)))
+        return fail(LT_ERR_INVALID_ARG, "operands and out must not be NULL");
+    if (!host::aligned(a_codes, 16) || !host::aligned(b_codes, 16) || !host::aligned(out, 16) ||
+        !host::aligned(a_scales, 4) || !host::aligned(b_scales, 4))
+        return fail(LT_ERR_ALIGNMENT, "codes and out must be 16-byte aligned, scales 4-byte");
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (k == 0)
+        return zero_rows(out, out_dtype, m, n, out_stride, st);
+    const size_t need = lt_int8_matmul_workspace_bytes(m, n, k);
+    const bool sliced = need > 256;
+    if (sliced && (!workspace || !host::aligned(workspace, 256) || workspace_bytes < need))
+        return fail(LT_ERR_WORKSPACE, "workspace must be 256-byte aligned and hold " +
+                                          std::to_string(need) + " bytes");
+    const size_t out_bytes = span_bytes(m, n, out_stride, out_dtype);
+    const size_t pitch = size_t(code_pitch(k));
+    const struct {
+        const void* p;
+        size_t bytes;
+    } read[] = {{a_codes, size_t(m) * pitch}, {b_codes, size_t(n) * pitch},
+                {a_scales, size_t(m) * 4}, {b_scales, size_t(n) * 4}};
+    for (const auto& r : read)
+        if (host::overlaps(out, out_bytes, r.p, r.bytes) ||
+            (sliced && host::overlaps(workspace, need, r.p, r.bytes)))
+            return fail(LT_ERR_INVALID_ARG, "out or the workspace overlaps an operand");
+    if (sliced) {
+        if (host::overlaps(out, out_bytes, workspace, need))
+            return fail(LT_ERR_INVALID_ARG, "out overlaps the workspace");
+        if (lt_err e = host::workspace_written(workspace, need, st))
+            return e;
+    }
+    ProductArgs g{};
+    g.a = reinterpret_cast<const uint8_t*>(a_codes);
+    g.b = reinterpret_cast<const uint8_t*>(b_codes);
+    g.a_scales = a_scales;
+    g.b_scales = b_scales;
+    g.m = m;
+    g.n = n;
+    g.out = out;
+    g.stride = out_stride;
+    return run_product(g, k, out_dtype, workspace, st);
+} catch (...) {
+    return host::caught();
+}
+
+size_t lt_int8_linear_workspace_bytes(int64_t m, int64_t n, int64_t k)
+{
+    return valid_sizes(m, n, k) ? linear_layout(m, n, k, false).total : 0;
+}
+
+lt_err lt_int8_linear(const void* x, int dtype, int64_t x_stride, const int8_t* w_codes,
+                      const float* w_scales, int64_t m, int64_t n, int64_t k, void* out,
+                      int out_dtype, int64_t out_stride, void* workspace, size_t workspace_bytes,
+                      void* stream)
+try {
+    host::clear_error();
+    return answer(x, dtype, x_stride, w_codes, w_scales, false, nullptr, nullptr, 0, m, n, k, out,
+                  out_dtype, out_stride, workspace, workspace_bytes, stream);
+} catch (...) {
+    return host::caught();
+}
+
+size_t lt_int8_gated_workspace_bytes(int64_t m, int64_t n, int64_t k)
+{
+    return valid_sizes(m, n, k) ? linear_layout(m, n, k, true).total : 0;
+}
+
+lt_err lt_int8_gated(const void* x, int dtype, int64_t x_stride, const int8_t* gate_codes,
+                     const float* gate_scales, const int8_t* up_codes, const float* up_scales,
+                     int activation, int64_t m, int64_t n, int64_t k, void* out, int out_dtype,
+                     int64_t out_stride, void* workspace, size_t workspace_bytes, void* stream)
+try {
+    host::clear_error();
+    return answer(x, dtype, x_stride, gate_codes, gate_scales, true, up_codes, up_scales,
+                  activation, m, n, k, out, out_dtype, out_stride, workspace, workspace_bytes,
+                  stream);
+} catch (...) {
+    return host::caught();
+}
+
+}  // extern "C"

@@ -68,6 +68,39 @@ struct TileLoad {
     }
 };
 
+// The same from two matrices of one width, whose blocks of 32 rows take turns in the tile, so that
+// a wave's blocks of columns 2 j and 2 j + 1 are the same rows of either.
+template <int ROWS, int THREADS>
+struct PairLoad {
+    static constexpr int N = ROWS * 8 / THREADS;
+    static_assert(N * 32 == ROWS && N % 2 == 0, "a copy is a block of 32 rows");
+    uint32_t offset[N];
+    int64_t apart;  // from the first matrix to the second
+
+    // `limit` rows of either exist from the tile's first on
+    __device__ inline void init(int64_t pitch, int64_t second_pitch, const void* first,
+                                const void* second, int64_t limit)
+    {
+        apart = reinterpret_cast<int64_t>(second) - reinterpret_cast<int64_t>(first);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int in_block = int(threadIdx.x) >> 3;
+            int64_t r = i / 2 * 32 + in_block;
+            const int chunk = (int(threadIdx.x) & 7) ^ (in_block >> 1 & 7);
+            r = r < limit ? r : limit - 1;
+            offset[i] = uint32_t(r * (i % 2 == 0 ? pitch : second_pitch)) + uint32_t(chunk * 16);
+        }
+    }
+    __device__ inline void issue(int i, const uint8_t* src, uint8_t* lds) const
+    {
+        const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+        const int64_t from = reinterpret_cast<int64_t>(src) + (i % 2 == 0 ? 0 : apart);
+        __builtin_amdgcn_global_load_lds(
+            (const LT_GLOBAL void*)(reinterpret_cast<const uint8_t*>(from) + offset[i]),
+            (LT_LDS void*)(lds + (i * THREADS + wave * 64) * 16), 16, 0, 0);
+    }
+};
+
 // Every LDS read that the wave has under way is complete: lgkmcnt(0), in the form that the
 // compiler sees, which then waits for no read of its own again.
 __device__ inline void wait_reads()
@@ -112,6 +145,32 @@ struct Half {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, a.c[t]),
                                                       __builtin_bit_cast(half8, b.c[t]), c, 0, 0,
                                                       0);
+    }
+};
+
+// Products of bf16, likewise.
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+struct Bf16 : Half {
+    static constexpr bool kOddSteps = true;
+    __device__ inline f32x16 mul(int t, int, int, const Chunks& a, const Chunks& b, f32x16 c) const
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a.c[t]),
+                                                       __builtin_bit_cast(bf16x8, b.c[t]), c, 0, 0,
+                                                       0);
+    }
+};
+
+// Products of 8-bit integers: 128 values a step.  The accumulators hold 32-bit integers' bits.
+typedef int i32x16 __attribute__((ext_vector_type(16)));
+
+struct Int8 : Half {
+    static constexpr bool kOddSteps = true;
+    __device__ inline f32x16 mul(int t, int, int, const Chunks& a, const Chunks& b, f32x16 c) const
+    {
+        return __builtin_bit_cast(
+            f32x16, __builtin_amdgcn_mfma_i32_32x32x32_i8(a.c[t], b.c[t],
+                                                          __builtin_bit_cast(i32x16, c), 0, 0, 0));
     }
 };
 
@@ -188,6 +247,8 @@ __device__ inline TilePlace triangle_place(int t, int side)
 typedef Shape<64, 64, 32, 32> Tiny;
 typedef Shape<128, 128, 64, 64> Small;
 typedef Shape<256, 256, 128, 128> Large;
+// The smallest tile in which a wave has two blocks of columns.
+typedef Shape<64, 128, 32, 64> Pair;
 
 // Products of fp8 (e4m3) with a power-of-two scale for each row and each 128 values: a step's in
 // two instructions of 64, which apply the scales themselves.  A scale is a byte, the
@@ -263,8 +324,8 @@ struct Fp8 {
     }
 };
 
-// The main loop over `steps` >= 1 steps.  P, Q: first rows of the tile's operands, pitches in
-// bytes, of which limit_p and limit_q rows exist.
+// The main loop over `steps` >= 1 steps.  P, Q: first rows of the tile's operands, and how they are
+// copied.
 //
 // A wave's block is multiplied in four quarters: the rows' blocks of 32 in two groups a0 and a1,
 // the columns' in b0 and b1, in an order in which neighbours share a group:
@@ -281,20 +342,16 @@ struct Fp8 {
 // A body of two steps has no branches but one at its top: past the end it copies and reads the
 // last step again, unused, and a branch inside made the compiler move all products before it
 // behind it, away from the loads that they cover.
-template <typename Mul, typename S>
-__device__ inline void product(Mul& mul, S& c, const void* P, int64_t pitch_p, int64_t limit_p,
-                               const void* Q, int64_t pitch_q, int64_t limit_q, int steps,
-                               uint8_t* lds)
+template <typename Mul, typename S, typename LoadQ>
+__device__ inline void product(Mul& mul, S& c, const void* P,
+                               const TileLoad<S::kRows, S::kThreads>& load_p, const void* Q,
+                               const LoadQ& load_q, int steps, uint8_t* lds)
 {
     constexpr int I = S::I, J = S::J;
     const int lane = S::lane(), wm = S::wave_row(), wn = S::wave_col();
-    TileLoad<S::kRows, S::kThreads> load_p;
-    TileLoad<S::kCols, S::kThreads> load_q;
-    load_p.init(pitch_p, limit_p);
-    load_q.init(pitch_q, limit_q);
     const auto* p = static_cast<const uint8_t*>(P);
     const auto* q = static_cast<const uint8_t*>(Q);
-    constexpr int kLoads = load_p.N + load_q.N;
+    constexpr int kLoads = TileLoad<S::kRows, S::kThreads>::N + LoadQ::N;
     struct Groups {
         // the blocks [first, first + n) of group g of `all`
         static constexpr int n(int all, int g) { return g == 0 ? (all + 1) / 2 : all / 2; }
@@ -423,6 +480,33 @@ __device__ inline void product(Mul& mul, S& c, const void* P, int64_t pitch_p, i
     __builtin_amdgcn_s_barrier();  // nothing is on its way into LDS any more
 }
 
+// The same for operands of pitches in bytes, of which limit_p and limit_q rows exist.
+template <typename Mul, typename S>
+__device__ inline void product(Mul& mul, S& c, const void* P, int64_t pitch_p, int64_t limit_p,
+                               const void* Q, int64_t pitch_q, int64_t limit_q, int steps,
+                               uint8_t* lds)
+{
+    TileLoad<S::kRows, S::kThreads> load_p;
+    TileLoad<S::kCols, S::kThreads> load_q;
+    load_p.init(pitch_p, limit_p);
+    load_q.init(pitch_q, limit_q);
+    product(mul, c, P, load_p, Q, load_q, steps, lds);
+}
+
+// For two matrices' rows in turns (PairLoad): columns [0, kCols / 2) of both results.
+template <typename Mul, typename S>
+__device__ inline void product_pairs(Mul& mul, S& c, const void* P, int64_t pitch_p,
+                                     int64_t limit_p, const void* first, int64_t first_pitch,
+                                     const void* second, int64_t second_pitch, int64_t limit_q,
+                                     int steps, uint8_t* lds)
+{
+    TileLoad<S::kRows, S::kThreads> load_p;
+    PairLoad<S::kCols, S::kThreads> load_q;
+    load_p.init(pitch_p, limit_p);
+    load_q.init(first_pitch, second_pitch, first, second, limit_q);
+    product(mul, c, P, load_p, first, load_q, steps, lds);
+}
+
 // What follows the main loop, for one wave's block, 32 rows at a time through LDS (the loop is
 // done with it): a lane then has eight consecutive columns of a row, so that a wave reads and
 // writes whole lines, and the code is a few short loops.  From the registers as they come a lane
@@ -483,6 +567,44 @@ __device__ inline void finish(const S& c, uint8_t* lds, Writer& w)
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
+    }
+}
+
+// The same for results of two matrices' rows in turns: w.store(row, col, u, v) takes eight
+// neighbouring columns of either result, which count in [0, kCols / 2).
+template <typename S, typename Writer>
+__device__ inline void finish_pairs(const S& c, uint8_t* lds, Writer& w)
+{
+    constexpr int W = 32 * S::J, kAcross = W / 16, kDown = 64 / kAcross, kPasses = 32 / kDown;
+    constexpr int kPitch = W + 4;
+    static_assert(S::J % 2 == 0 && S::kWaves * 32 * kPitch * 4 <= S::kLdsBytes,
+                  "every wave's rows fit");
+    float* mine = reinterpret_cast<float*>(lds) + S::wave() * 32 * kPitch;
+    const int lane = S::lane(), down = lane / kAcross, across = lane % kAcross * 8;
+    const int r0 = S::wave_row(), c0 = S::wave_col() / 2;
+#pragma unroll
+    for (int i = 0; i < S::I; ++i) {
+#pragma unroll
+        for (int jg = 0; jg < 4 * S::J; ++jg) {
+            const int j = jg / 4, g = jg % 4;
+            *reinterpret_cast<f32x4*>(mine + (lane & 31) * kPitch + 32 * j + 8 * g +
+                                      4 * (lane >> 5)) =
+                f32x4{c.acc[i][j][4 * g], c.acc[i][j][4 * g + 1], c.acc[i][j][4 * g + 2],
+                      c.acc[i][j][4 * g + 3]};
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll 1
+        for (int p = 0; p < kPasses; ++p) {
+            const float* at = mine + (p * kDown + down) * kPitch + across / 32 * 64 + across % 32;
+            float u[8], v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                u[e] = at[e];
+                v[e] = at[32 + e];
+            }
+            w.store(r0 + 32 * i + p * kDown + down, c0 + across, u, v);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 }
 

@@ -1,0 +1,191 @@
+"""The gated projections of a feed-forward block in bfloat16 (f13 and f14; see include/lazytrain.h):
+act(x gate^T) * (x up^T) with the weights the optimizer keeps in bfloat16, for answering and for
+training, with the gradients of the tokens and of both weights.
+"""
+from __future__ import annotations
+
+from typing import Optional, Tuple
+
+import torch
+
+from .fp8 import _dtype_code, _laid_out, _rows, _scratch, _tokens
+from .int8 import _activation_code
+from .lazytrain import _capturing, _check, _current, _stream_handle, lib
+
+
+def _weights(gate: torch.Tensor, up: torch.Tensor, device):
+    """The weights as the library takes them, and their row strides."""
+    laid = []
+    for w, what in ((gate, "gate"), (up, "up")):
+        if w.dim() != 2 or w.shape != gate.shape:
+            raise ValueError(f"gate and up must be matrices of one shape, got "
+                             f"{tuple(gate.shape)} and {tuple(up.shape)}")
+        if w.dtype != torch.bfloat16:
+            raise TypeError(f"{what} must be bfloat16, got {w.dtype}")
+        if w.device != device:
+            raise ValueError(f"{what} is on {w.device}, not on {device}")
+        w = _laid_out(w)
+        laid += [w, _rows(w, what)]
+    return laid
+
+
+def _input(x: torch.Tensor, features: int) -> Tuple[torch.Tensor, int]:
+    if x.dtype != torch.bfloat16:
+        raise TypeError(f"x must be bfloat16, got {x.dtype}")
+    t = _tokens(x, features, "x")
+    return t, _rows(t, "x")
+
+
+def _forward(x, gate, up, activation, out_dtype, keep, workspace):
+    act = _activation_code(activation)
+    g, g_stride, u, u_stride = _weights(gate, up, x.device)
+    n, k = g.shape
+    t, x_stride = _input(x, k)
+    m, device = t.shape[0], x.device
+    h = torch.empty(m, n, dtype=out_dtype, device=device)
+    out = _dtype_code(h, "out")
+    saved = None
+    if keep:
+        saved = torch.empty(int(lib().lt_gated_saved_bytes(m, n)), dtype=torch.uint8, device=device)
+    ws, nbytes, handle = 0, 0, _stream_handle(None, device)
+    if (keep or m > 32) and (k % 64 or (x_stride | g_stride | u_stride) % 8) or \
+            workspace is not None:
+        need = int(lib().lt_gated_forward_workspace_bytes(m, n, k, x_stride, g_stride, u_stride))
+        held, ws, nbytes = _scratch(device, need, workspace, None)
+    with _current(device):
+        _check(lib().lt_gated_forward(t.data_ptr(), x_stride, g.data_ptr(), g_stride, u.data_ptr(),
+                                      u_stride, act, m, n, k, h.data_ptr(), out, n,
+                                      saved.data_ptr() if keep else 0, ws, nbytes, handle))
+    return h if x.dim() == 2 else h.view(*x.shape[:-1], n), saved
+
+
+def gated_linear(x: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, activation: str = "silu",
+                 out_dtype: torch.dtype = torch.bfloat16,
+                 workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """f13: act(x gate^T) * (x up^T) for x (..., in_features) and two weights (out_features x
+    in_features), all bfloat16; activation is "silu", "gelu", "gelu_tanh" or "relu".  For answering:
+    nothing is kept for a backward pass.  This and the functions below allocate and work on the
+    current stream."""
+    return _forward(x, gate, up, activation, out_dtype, False, workspace)[0]
+
+
+def gated_linear_forward(x: torch.Tensor, gate: torch.Tensor, up: torch.Tensor,
+                         activation: str = "silu", out_dtype: torch.dtype = torch.bfloat16):
+    """As gated_linear, and what the backward pass needs of its results: six bytes for each, in one
+    tensor of bytes."""
+    return _forward(x, gate, up, activation, out_dtype, True, None)
+
+
+def gated_linear_backward(dh: torch.Tensor, saved: torch.Tensor, x: torch.Tensor,
+                          gate: torch.Tensor, up: torch.Tensor,
+                          out_dtype: torch.dtype = torch.bfloat16,
+                          grad_dtype: torch.dtype = torch.bfloat16):
+    """(dx, dgate, dup) of gated_linear_forward: dx in out_dtype with x's shape, the weights'
+    gradients in grad_dtype.  dh is float32 or bfloat16."""
+    return _backward(dh, saved, x, gate, up, tuple(x.shape[:-1]), tuple(gate.shape), out_dtype,
+                     grad_dtype, True, True)
+
+
+def _backward(dh, saved, x, gate, up, leading, shape, out_dtype, grad_dtype, want_dx, want_dw):
+    """dx needs the weights, the weights' gradients x; what is not needed may be None."""
+    n, k = shape
+    device = dh.device
+    d = _tokens(dh, n, "dh", aligned=False)
+    m = d.shape[0]
+    d_stride, d_code = _rows(d, "dh"), _dtype_code(d, "dh")
+    if tuple(dh.shape[:-1]) != leading:
+        raise ValueError(f"dh must have shape {leading + (n,)}, got {tuple(dh.shape)}")
+    if (saved.device != device or saved.dtype != torch.uint8 or not saved.is_contiguous() or
+            saved.numel() != int(lib().lt_gated_saved_bytes(m, n))):
+        raise ValueError("saved must be what gated_linear_forward kept of these tokens")
+    x_at, x_stride, g_at, g_stride, u_at, u_stride = 0, k, 0, k, 0, k
+    dx = dgate = dup = None
+    if want_dx:
+        g, g_stride, u, u_stride = _weights(gate, up, device)
+        g_at, u_at = g.data_ptr(), u.data_ptr()
+        dx = torch.empty(m, k, dtype=out_dtype, device=device)
+        _dtype_code(dx, "dx")
+    if want_dw:
+        if x.device != device:
+            raise ValueError(f"x is on {x.device}, dh on {device}")
+        t, x_stride = _input(x, k)
+        if t.shape[0] != m:
+            raise ValueError(f"x has {t.shape[0]} tokens, dh {m}")
+        x_at = t.data_ptr()
+        dgate = torch.empty(n, k, dtype=grad_dtype, device=device)
+        dup = torch.empty(n, k, dtype=grad_dtype, device=device)
+        _dtype_code(dgate, "the weights' gradients")
+    if not want_dx and not want_dw:
+        return None, None, None
+    handle = _stream_handle(None, device)
+    need = int(lib().lt_gated_backward_workspace_bytes(m, n, k, want_dx, want_dw))
+    held, ws, nbytes = _scratch(device, need, None, None)
+    at = lambda t: 0 if t is None else t.data_ptr()
+    code = lambda t: 0 if t is None else _dtype_code(t, "a gradient")
+    with _current(device):
+        _check(lib().lt_gated_backward(d.data_ptr(), d_code, d_stride, saved.data_ptr(), x_at,
+                                       x_stride, g_at, g_stride, u_at, u_stride, m, n, k, at(dx),
+                                       code(dx), k, at(dgate), k, at(dup), k, code(dgate), ws,
+                                       nbytes, handle))
+    return None if dx is None else dx.view(*leading, k), dgate, dup
+
+
+_MADE_ON = "lazytrain_stream"
+
+
+def _accumulators(leaves):
+    """The nodes that take the leaves' gradients, made where no graph holds one, and which of them
+    are new: a note on a node that nothing else holds goes with it."""
+    for t in leaves:
+        torch.autograd.graph.get_gradient_edge(t).node.metadata[_MADE_ON + "?"] = True
+    nodes = [torch.autograd.graph.get_gradient_edge(t).node for t in leaves]
+    return [(n, n.metadata.pop(_MADE_ON + "?", None) is None) for n in nodes]
+
+
+class GatedLinear(torch.autograd.Function):
+    """``GatedLinear.apply(x, gate, up, activation)``: gated_linear with gradients for x, gate and up
+    (for instance the optimizer's bf16 copies).  The backward pass reads x and the weights again:
+    one of them changed in place meanwhile raises, like autograd's own.  First derivatives only: a
+    backward pass that is itself to be differentiated raises.
+
+    Autograd adds up a leaf's gradient on the stream that its first graph was made on, for as long
+    as a graph of the leaf lives.  Under capture that cannot be the default stream (the process would
+    end with the capture): a captured call whose leaves an earlier call's graph, made there, still
+    holds is refused."""
+
+    @classmethod
+    def apply(cls, x, gate, up, activation="silu"):
+        leaves = list({id(t): t for t in (x, gate, up)
+                       if t.is_cuda and t.is_leaf and t.requires_grad}.values())
+        if not leaves or not torch.is_grad_enabled():
+            return super().apply(x, gate, up, activation)
+        stream = torch.cuda.current_stream(x.device).cuda_stream
+        made = _accumulators(leaves)
+        for node, new in made:
+            if new:
+                node.metadata[_MADE_ON] = stream
+            elif node.metadata.get(_MADE_ON) == 0 and _capturing(None, x.device):
+                raise RuntimeError("GatedLinear is being captured while a graph made on the default "
+                                   "stream holds the same leaf: let go of that graph's results "
+                                   "first, or make it on another stream")
+        return super().apply(x, gate, up, activation)
+
+    @staticmethod
+    def forward(ctx, x, gate, up, activation="silu"):
+        want_dx, want_dw = ctx.needs_input_grad[0], any(ctx.needs_input_grad[1:3])
+        h, saved = _forward(x, gate, up, activation, torch.bfloat16, want_dx or want_dw, None)
+        ctx.save_for_backward(saved, x if want_dw else None, *((gate, up) if want_dx
+                                                               else (None, None)))
+        ctx.leading, ctx.shape = tuple(x.shape[:-1]), tuple(gate.shape)
+        return h
+
+    @staticmethod
+    def backward(ctx, dh):
+        if torch.is_grad_enabled() and (dh.requires_grad or any(ctx.needs_input_grad[:3])):
+            raise RuntimeError("GatedLinear has first derivatives only: its backward pass cannot be "
+                               "part of a graph (create_graph=True)")
+        saved, x, gate, up = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        dx, dgate, dup = _backward(dh, saved, x, gate, up, ctx.leading, ctx.shape, torch.bfloat16,
+                                   torch.bfloat16, need[0], need[1] or need[2])
+        return dx, dgate if need[1] else None, dup if need[2] else None, None

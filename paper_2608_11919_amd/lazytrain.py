@@ -28,6 +28,7 @@ LIB_PATH = os.path.join(_HERE, "liblazytrain.so")
 LT_STATUS_OK, LT_STATUS_NONFINITE, LT_STATUS_BAD_WORKSPACE = 0, 1, 2
 LT_DTYPE_F32, LT_DTYPE_BF16 = 0, 1
 LT_MAP_LINEAR, LT_MAP_DYNAMIC = 0, 1
+LT_ACT_SILU, LT_ACT_GELU, LT_ACT_GELU_TANH, LT_ACT_RELU = range(4)
 ERROR_NAMES = {1: "LT_ERR_INVALID_ARG", 2: "LT_ERR_ALIGNMENT", 3: "LT_ERR_HIP",
                4: "LT_ERR_WORKSPACE", 5: "LT_ERR_HOST"}
 
@@ -161,6 +162,28 @@ def lib() -> ctypes.CDLL:
     L.lt_fp8_linear_workspace_bytes.restype = ctypes.c_size_t
     L.lt_fp8_linear.argtypes = [vp, ctypes.c_int, i64, vp, vp, i64, i64, i64, vp, ctypes.c_int, i64,
                                 vp, ctypes.c_size_t, vp]
+    size, num = ctypes.c_size_t, ctypes.c_int
+    L.lt_int8_code_pitch.argtypes = [i64]
+    L.lt_int8_code_pitch.restype = i64
+    L.lt_int8_quantize.argtypes = [vp, num, i64, i64, i64, vp, vp, vp]
+    for name in ("lt_int8_matmul_workspace_bytes", "lt_int8_linear_workspace_bytes",
+                 "lt_int8_gated_workspace_bytes"):
+        getattr(L, name).argtypes = [i64, i64, i64]
+        getattr(L, name).restype = size
+    L.lt_int8_matmul.argtypes = [vp, vp, vp, vp, i64, i64, i64, vp, num, i64, vp, size, vp]
+    L.lt_int8_linear.argtypes = [vp, num, i64, vp, vp, i64, i64, i64, vp, num, i64, vp, size, vp]
+    L.lt_int8_gated.argtypes = [vp, num, i64, vp, vp, vp, vp, num, i64, i64, i64, vp, num, i64, vp,
+                                size, vp]
+    L.lt_gated_saved_bytes.argtypes = [i64, i64]
+    L.lt_gated_saved_bytes.restype = size
+    L.lt_gated_forward_workspace_bytes.argtypes = [i64] * 6
+    L.lt_gated_forward_workspace_bytes.restype = size
+    L.lt_gated_forward.argtypes = [vp, i64, vp, i64, vp, i64, num, i64, i64, i64, vp, num, i64, vp,
+                                   vp, size, vp]
+    L.lt_gated_backward_workspace_bytes.argtypes = [i64, i64, i64, num, num]
+    L.lt_gated_backward_workspace_bytes.restype = size
+    L.lt_gated_backward.argtypes = [vp, num, i64, vp, vp, i64, vp, i64, vp, i64, i64, i64, i64, vp,
+                                    num, i64, vp, i64, vp, i64, num, vp, size, vp]
     L.lt_read_status.argtypes = [vp, vp, ctypes.POINTER(ctypes.c_int32)]
     L.lt_set_max_workgroups.argtypes = [ctypes.c_int]
     L.lt_workspace_release.argtypes = [vp]
@@ -172,7 +195,9 @@ def lib() -> ctypes.CDLL:
                  "lt_adamw_fp32_step", "lt_select_8bit_slice", "lt_workspace_release",
                  "lt_grad_sqnorm_noalloc", "lt_step_table", "lt_step_state_init",
                  "lt_step_state_advance", "lt_orthogonalize", "lt_muon_step",
-                 "lt_fp8_quantize", "lt_fp8_matmul", "lt_fp8_linear"):
+                 "lt_fp8_quantize", "lt_fp8_matmul", "lt_fp8_linear", "lt_int8_quantize",
+                 "lt_int8_matmul", "lt_int8_linear", "lt_int8_gated", "lt_gated_forward",
+                 "lt_gated_backward"):
         getattr(L, name).restype = ctypes.c_int
     _lib = L
     return L
