@@ -219,7 +219,7 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_gated_f
                                     int((g.n + kCols - 1) / kCols));
     const int64_t r0 = int64_t(at.row) * Tile::kRows, c0 = int64_t(at.col) * kCols;
     Tile tile;
-    Bf16 mul;
+    Bf16<Tile::kPinned> mul;
     product_pairs(mul, tile, g.x + r0 * g.x_pitch, g.x_pitch, g.m - r0, g.gate + c0 * g.gate_pitch,
                   g.gate_pitch, g.up + c0 * g.up_pitch, g.up_pitch, g.n - c0, g.steps, lds);
     ForwardWriter<F32, SAVE> w{g, r0, c0};
@@ -370,7 +370,7 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_gated_p
     const int first = int(blockIdx.y) * g.slice, steps = min(g.slice, g.steps - first);
     const int64_t k0 = int64_t(first) * kStepBytes;
     Tile tile;
-    Bf16 mul;
+    Bf16<Tile::kPinned> mul;
     product(mul, tile, g.a + (which * g.m + r0) * g.a_pitch + k0, g.a_pitch, g.m - r0,
             g.b + c0 * g.b_pitch + k0, g.b_pitch, g.n - c0, steps, lds);
     if (g.partial) {
@@ -582,11 +582,11 @@ void run_product(ProductArgs g, bool f32, uint8_t* partial, hipStream_t st)
     g.slice = w.slice;
     g.partial = w.slices > 1 ? reinterpret_cast<float*>(partial) : nullptr;
     if (w.tile == 256)
-        launch_product<Large>(g, w, f32, st);
+        launch_product<Large16>(g, w, f32, st);
     else if (w.tile == 128)
-        launch_product<Small>(g, w, f32, st);
+        launch_product<Small16>(g, w, f32, st);
     else
-        launch_product<Tiny>(g, w, f32, st);
+        launch_product<Tiny16>(g, w, f32, st);
     if (g.partial) {
         auto* join = f32 ? k_gated_join<true> : k_gated_join<false>;
         join<<<dim3(groups_for(g.m * g.n * g.count)), 256, 0, st>>>(g, w.slices);
@@ -731,11 +731,11 @@ try {
     operand(up, n, up_stride, l.up, &g.up, &g.up_pitch);
     const Way w = way_of(m, n, 1, g.steps, true);
     if (w.tile == 256)
-        launch_forward<Large>(g, f32, saved != nullptr, st);
+        launch_forward<Large16>(g, f32, saved != nullptr, st);
     else if (w.tile == 128)
-        launch_forward<Small>(g, f32, saved != nullptr, st);
+        launch_forward<Small16>(g, f32, saved != nullptr, st);
     else
-        launch_forward<Pair>(g, f32, saved != nullptr, st);
+        launch_forward<Pair16>(g, f32, saved != nullptr, st);
     LT_TRY_HIP(hipGetLastError());
     return LT_OK;
 } catch (...) {

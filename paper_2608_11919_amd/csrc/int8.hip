@@ -238,7 +238,7 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_int8_pr
     const int64_t r0 = int64_t(at.row) * Tile::kRows, c0 = int64_t(at.col) * Tile::kCols;
     const int first = int(blockIdx.y) * g.slice, steps = min(g.slice, g.steps - first);
     Tile tile;
-    Int8 mul;
+    Int8<Tile::kPinned> mul;
     const int64_t k0 = int64_t(first) * kStepBytes;
     product(mul, tile, g.a + r0 * g.pitch + k0, g.pitch, g.m - r0, g.b + c0 * g.pitch + k0, g.pitch,
             g.n - c0, steps, lds);
@@ -256,7 +256,7 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_int8_ga
                                     int((g.n + kCols - 1) / kCols));
     const int64_t r0 = int64_t(at.row) * Tile::kRows, c0 = int64_t(at.col) * kCols;
     Tile tile;
-    Int8 mul;
+    Int8<Tile::kPinned> mul;
     product_pairs(mul, tile, g.a + r0 * g.pitch, g.pitch, g.m - r0, g.b + c0 * g.pitch, g.pitch,
                   g.c + c0 * g.pitch, g.pitch, g.n - c0, g.steps, lds);
     ProductWriter<F32> w{g, r0, c0};
@@ -373,11 +373,11 @@ void launch_product(const ProductArgs& g, const Way& w, bool f32, hipStream_t st
         kernel<<<grid, Tile::kThreads, 0, st>>>(g);
     };
     if (w.tile == 256)
-        go(f32 ? k_int8_product<Large, true> : k_int8_product<Large, false>, Large());
+        go(f32 ? k_int8_product<Large16, true> : k_int8_product<Large16, false>, Large16());
     else if (w.tile == 128)
-        go(f32 ? k_int8_product<Small, true> : k_int8_product<Small, false>, Small());
+        go(f32 ? k_int8_product<Small16, true> : k_int8_product<Small16, false>, Small16());
     else
-        go(f32 ? k_int8_product<Tiny, true> : k_int8_product<Tiny, false>, Tiny());
+        go(f32 ? k_int8_product<Tiny16, true> : k_int8_product<Tiny16, false>, Tiny16());
 }
 
 void launch_gated(const ProductArgs& g, const Way& w, bool f32, hipStream_t st)
@@ -389,11 +389,11 @@ void launch_gated(const ProductArgs& g, const Way& w, bool f32, hipStream_t st)
                  Tile::kThreads, 0, st>>>(g);
     };
     if (w.tile == 256)
-        go(f32 ? k_int8_gated<Large, true> : k_int8_gated<Large, false>, Large());
+        go(f32 ? k_int8_gated<Large16, true> : k_int8_gated<Large16, false>, Large16());
     else if (w.tile == 128)
-        go(f32 ? k_int8_gated<Small, true> : k_int8_gated<Small, false>, Small());
+        go(f32 ? k_int8_gated<Small16, true> : k_int8_gated<Small16, false>, Small16());
     else
-        go(f32 ? k_int8_gated<Pair, true> : k_int8_gated<Pair, false>, Pair());
+        go(f32 ? k_int8_gated<Pair16, true> : k_int8_gated<Pair16, false>, Pair16());
 }
 
 lt_err zero_rows(void* out, int dtype, int64_t m, int64_t n, int64_t stride, hipStream_t st)

@@ -132,6 +132,21 @@ __device__ inline i32x4 read_chunk(const uint8_t* tile, int row32, int c, int la
     return *reinterpret_cast<const i32x4*>(row + at);
 }
 
+// The 16 x 16 instructions: of row 16 (c % 2) + l % 16 of the block a lane holds 16-byte chunk
+// 4 (c / 2) + l / 16.
+__device__ inline i32x4 read_chunk_16(const uint8_t* tile, int row32, int c, int lane)
+{
+    const uint8_t* row = tile + (row32 + 16 * (c & 1) + (lane & 15)) * kStepBytes;
+    const int at = ((4 * (c >> 1) + (lane >> 4)) ^ (lane >> 1 & 7)) << 4;
+    return *reinterpret_cast<const i32x4*>(row + at);
+}
+
+// The accumulators of a block of 32 x 32 in instructions of 16 x 16: quarter 2 i + j is rows
+// 16 i .. + 15, columns 16 j .. + 15.
+struct Quarters {
+    f32x4 q[4];
+};
+
 // Products of fp16: 64 values a step, in four instructions; sums over multiples of 128.
 struct Half {
     static constexpr int kInstructions = 4;
@@ -148,50 +163,114 @@ struct Half {
     }
 };
 
-// Products of bf16, likewise.
+// Products of bf16: 64 values a step, in eight instructions of 16 x 16.  PINNED, for tiles whose
+// accumulators fill the accumulation registers: written out, with the operand kinds that keep them
+// there (left to itself the compiler moves a third of them to and fro, and spills).  Between those
+// instructions are no others of these registers; what follows the last waits (settle()).
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
+template <bool PINNED>
 struct Bf16 : Half {
+    static constexpr int kInstructions = 8;
     static constexpr bool kOddSteps = true;
-    __device__ inline f32x16 mul(int t, int, int, const Chunks& a, const Chunks& b, f32x16 c) const
+    __device__ inline Quarters mul(int t, int, int, const Chunks& a, const Chunks& b,
+                                   Quarters c) const
     {
-        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a.c[t]),
-                                                       __builtin_bit_cast(bf16x8, b.c[t]), c, 0, 0,
-                                                       0);
+        const i32x4 p = a.c[t / 4 * 2 + t % 2], q = b.c[t / 4 * 2 + t / 2 % 2];
+        if constexpr (PINNED)
+            asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0"
+                         : "+a"(c.q[t % 4])
+                         : "v"(p), "v"(q));
+        else
+            c.q[t % 4] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, p),
+                                                                 __builtin_bit_cast(bf16x8, q),
+                                                                 c.q[t % 4], 0, 0, 0);
+        return c;
     }
 };
 
-// Products of 8-bit integers: 128 values a step.  The accumulators hold 32-bit integers' bits.
-typedef int i32x16 __attribute__((ext_vector_type(16)));
-
+// Products of 8-bit integers, likewise: 128 values a step.  The accumulators hold 32-bit integers'
+// bits.
+template <bool PINNED>
 struct Int8 : Half {
+    static constexpr int kInstructions = 8;
     static constexpr bool kOddSteps = true;
-    __device__ inline f32x16 mul(int t, int, int, const Chunks& a, const Chunks& b, f32x16 c) const
+    __device__ inline Quarters mul(int t, int, int, const Chunks& a, const Chunks& b,
+                                   Quarters c) const
     {
-        return __builtin_bit_cast(
-            f32x16, __builtin_amdgcn_mfma_i32_32x32x32_i8(a.c[t], b.c[t],
-                                                          __builtin_bit_cast(i32x16, c), 0, 0, 0));
+        const i32x4 p = a.c[t / 4 * 2 + t % 2], q = b.c[t / 4 * 2 + t / 2 % 2];
+        if constexpr (PINNED)
+            asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0"
+                         : "+a"(c.q[t % 4])
+                         : "v"(p), "v"(q));
+        else
+            c.q[t % 4] = __builtin_bit_cast(
+                f32x4, __builtin_amdgcn_mfma_i32_16x16x64_i8(
+                           p, q, __builtin_bit_cast(i32x4, c.q[t % 4]), 0, 0, 0));
+        return c;
     }
 };
 
 // One BM x BN output tile by waves of WM x WN each; lane l of the wave at (wm, wn) ends with
 // acc[i][j][4 g + r] = C[wm + 32 i + l % 32][wn + 32 j + 8 g + 4 (l / 32) + r]
-// (the operands are swapped in the instruction, so that a lane holds consecutive columns).
-template <int BM, int BN, int WM, int WN>
+// (the operands are swapped in the instruction, so that a lane holds consecutive columns), with
+// K16, by instructions of 16 x 16, with
+// acc[i][j].q[2 g + h][r] = C[wm + 32 i + 16 g + l % 16][wn + 32 j + 16 h + 4 (l / 16) + r].
+template <int BM, int BN, int WM, int WN, bool K16 = false>
 struct Shape {
+    static constexpr bool k16 = K16;
     static constexpr int kRows = BM, kCols = BN, I = WM / 32, J = WN / 32;
     static constexpr int kWavesAcross = BN / WN, kWaves = BM / WM * kWavesAcross;
     static constexpr int kThreads = 64 * kWaves;
     static constexpr int kWavesPerSimd = WM * WN > 64 * 128 ? 1 : 2;  // at this many registers
+    static constexpr bool kPinned = K16 && kWavesPerSimd == 1;
     static constexpr int kBufferBytes = (BM + BN) * kStepBytes;
     static constexpr int kLdsBytes = 2 * kBufferBytes;
     static constexpr int kRun = 32 * (kWavesPerSimd == 2 ? 2 : 1);  // tiles an XCD's 32 CUs hold
-    f32x16 acc[I][J];
+    typename std::conditional<K16, Quarters, f32x16>::type acc[I][J];
 
     __device__ static inline int wave() { return __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6); }
     __device__ static inline int lane() { return int(threadIdx.x) & 63; }
     __device__ static inline int wave_row() { return wave() / kWavesAcross * WM; }
     __device__ static inline int wave_col() { return wave() % kWavesAcross * WN; }
+    __device__ inline f32x4 four(int i, int j, int g) const
+    {
+        if constexpr (K16)
+            return acc[i][j].q[g];
+        else
+            return f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2],
+                         acc[i][j][4 * g + 3]};
+    }
+    // before the first and after the last of the pinned instructions: what writes the accumulators
+    // is done with them before what reads them begins
+    __device__ inline void settle()
+    {
+        asm volatile("s_nop 15\n\ts_nop 15");
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    asm volatile("" : "+a"(acc[i][j].q[g]));
+    }
+    __device__ inline void clear()
+    {
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                if constexpr (K16) {
+#pragma unroll
+                    for (int g = 0; g < 4; ++g)
+                        acc[i][j].q[g] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        acc[i][j][r] = 0.0f;
+                }
+            }
+    }
     // this lane's row of block i, and the first of its four columns g of block j, in the tile
     __device__ static inline int row(int i) { return wave_row() + 32 * i + (lane() & 31); }
     __device__ static inline int col(int j, int g) { return wave_col() + 32 * j + 8 * g + 4 * (lane() >> 5); }
@@ -247,8 +326,13 @@ __device__ inline TilePlace triangle_place(int t, int side)
 typedef Shape<64, 64, 32, 32> Tiny;
 typedef Shape<128, 128, 64, 64> Small;
 typedef Shape<256, 256, 128, 128> Large;
+// The same by instructions of 16 x 16.  They take twice the operands' registers for a product and
+// half the accumulators': less power.
+typedef Shape<64, 64, 32, 32, true> Tiny16;
+typedef Shape<128, 128, 64, 64, true> Small16;
+typedef Shape<256, 256, 128, 128, true> Large16;
 // The smallest tile in which a wave has two blocks of columns.
-typedef Shape<64, 128, 32, 64> Pair;
+typedef Shape<64, 128, 32, 64, true> Pair16;
 
 // Products of fp8 (e4m3) with a power-of-two scale for each row and each 128 values: a step's in
 // two instructions of 64, which apply the scales themselves.  A scale is a byte, the
@@ -377,20 +461,23 @@ __device__ inline void product(Mul& mul, S& c, const void* P,
                          to + S::kRows * kStepBytes);
         }
     };
+    const auto read = [](const uint8_t* tile, int row32, int c, int l) {
+        return S::k16 ? read_chunk_16(tile, row32, c, l) : read_chunk(tile, row32, c, l);
+    };
     const auto read_a = [&](int odd, int g, int k) {
         const int i = Groups::first(I, g) + k / 4;
-        a[i].c[k % 4] = read_chunk(lds + odd * S::kBufferBytes, wm + 32 * i, k % 4, lane);
+        a[i].c[k % 4] = read(lds + odd * S::kBufferBytes, wm + 32 * i, k % 4, lane);
     };
     const auto read_b = [&](int odd, int g, int k) {
         const int j = Groups::first(J, g) + k / 4;
-        b[j].c[k % 4] = read_chunk(lds + odd * S::kBufferBytes + S::kRows * kStepBytes,
+        b[j].c[k % 4] = read(lds + odd * S::kBufferBytes + S::kRows * kStepBytes,
                                    wn + 32 * j, k % 4, lane);
     };
     // the products of groups ga and gb, with reads and copies issued evenly between them: reads
     // within the first three quarters, so that the last covers their latency.  Every border
     // keeps its place: left to itself the compiler issues reads right before the products that
     // wait for them, and products ahead of the barrier.
-    const auto multiply = [&](int ga, int gb, int reads, auto read, int loads, auto copy) {
+    const auto multiply = [&](int ga, int gb, int reads, auto read_next, int loads, auto copy) {
         const int ni = Groups::n(I, ga), nj = Groups::n(J, gb);
         const int muls = ni * nj * Mul::kInstructions, paced = muls * 3 / 4;
         const auto share = [](int n, int of, int k) { return k < of ? n * k / of : n; };
@@ -400,7 +487,7 @@ __device__ inline void product(Mul& mul, S& c, const void* P,
                 copy(r);
 #pragma unroll
             for (int r = 0; r < reads; ++r)
-                read(r);
+                read_next(r);
             return;
         }
 #pragma unroll
@@ -410,7 +497,7 @@ __device__ inline void product(Mul& mul, S& c, const void* P,
                 copy(r);
 #pragma unroll
             for (int r = share(reads, paced, k); r < share(reads, paced, k + 1); ++r)
-                read(r);
+                read_next(r);
             const int t = k / (ni * nj), i = Groups::first(I, ga) + k / nj % ni,
                       j = Groups::first(J, gb) + k % nj;
             c.acc[i][j] = mul.mul(t, i, j, b[j], a[i], c.acc[i][j]);
@@ -440,13 +527,9 @@ __device__ inline void product(Mul& mul, S& c, const void* P,
         wait_loads<kLoads>();  // and its late rows
         __builtin_amdgcn_s_barrier();
     };
-#pragma unroll
-    for (int i = 0; i < I; ++i)
-#pragma unroll
-        for (int j = 0; j < J; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                c.acc[i][j][r] = 0.0f;
+    c.clear();
+    if constexpr (S::kPinned)
+        c.settle();
     mul.begin();
 #pragma unroll
     for (int s = 0; s < 2; ++s)
@@ -476,6 +559,8 @@ __device__ inline void product(Mul& mul, S& c, const void* P,
     if constexpr (Mul::kOddSteps)
         if (s < steps)
             step(s, std::integral_constant<int, 0>());
+    if constexpr (S::kPinned)
+        c.settle();
     wait_loads<0>();
     __builtin_amdgcn_s_barrier();  // nothing is on its way into LDS any more
 }
@@ -534,10 +619,11 @@ __device__ inline void finish(const S& c, uint8_t* lds, Writer& w)
 #pragma unroll
         for (int jg = 0; jg < 4 * S::J; ++jg) {
             const int j = jg / 4, g = jg % 4;
-            *reinterpret_cast<f32x4*>(mine + (lane & 31) * kPitch + 32 * j + 8 * g +
-                                      4 * (lane >> 5)) =
-                f32x4{c.acc[i][j][4 * g], c.acc[i][j][4 * g + 1], c.acc[i][j][4 * g + 2],
-                      c.acc[i][j][4 * g + 3]};
+            *reinterpret_cast<f32x4*>(mine + (S::k16 ? 16 * (g >> 1) + (lane & 15) : lane & 31) *
+                                             kPitch +
+                                      32 * j + (S::k16 ? 16 * (g & 1) + 4 * (lane >> 4)
+                                                       : 8 * g + 4 * (lane >> 5))) =
+                c.four(i, j, g);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
@@ -587,10 +673,11 @@ __device__ inline void finish_pairs(const S& c, uint8_t* lds, Writer& w)
 #pragma unroll
         for (int jg = 0; jg < 4 * S::J; ++jg) {
             const int j = jg / 4, g = jg % 4;
-            *reinterpret_cast<f32x4*>(mine + (lane & 31) * kPitch + 32 * j + 8 * g +
-                                      4 * (lane >> 5)) =
-                f32x4{c.acc[i][j][4 * g], c.acc[i][j][4 * g + 1], c.acc[i][j][4 * g + 2],
-                      c.acc[i][j][4 * g + 3]};
+            *reinterpret_cast<f32x4*>(mine + (S::k16 ? 16 * (g >> 1) + (lane & 15) : lane & 31) *
+                                             kPitch +
+                                      32 * j + (S::k16 ? 16 * (g & 1) + 4 * (lane >> 4)
+                                                       : 8 * g + 4 * (lane >> 5))) =
+                c.four(i, j, g);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll 1
