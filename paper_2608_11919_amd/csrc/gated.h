@@ -31,37 +31,28 @@ __device__ inline float normal_cdf(float g) { return 0.5f * erfcf(g * -0.7071067
 constexpr float kTanhLinear = 1.59576912f;   // 2 sqrt(2 / pi)
 constexpr float kTanhCubic = 0.0713548163f;  // that times 0.044715
 
-// The activation.  `kind` is the same for a whole launch: a branch, not a kernel for each.
-__device__ inline float activate(int kind, float g)
-{
-    switch (kind) {
-    case LT_ACT_SILU:
-        return g * logistic(g);
-    case LT_ACT_GELU:
-        return g * normal_cdf(g);
-    case LT_ACT_GELU_TANH:  // 0.5 g (1 + tanh(z / 2)) = g / (1 + e^-z)
-        return g * logistic(g * __builtin_fmaf(kTanhCubic * g, g, kTanhLinear));
-    default:
-        return g <= 0.0f ? 0.0f : g;
-    }
-}
-
-// The activation and its derivative.
-__device__ inline float activate(int kind, float g, float* slope)
-{
-    switch (kind) {
-    case LT_ACT_SILU: {
+struct Silu {
+    __device__ static inline float of(float g, float* slope)
+    {
         const float s = logistic(g);
         *slope = s * __builtin_fmaf(g, 1.0f - s, 1.0f);
         return g * s;
     }
-    case LT_ACT_GELU: {
+};
+
+struct Gelu {
+    __device__ static inline float of(float g, float* slope)
+    {
         const float p = normal_cdf(g);
         *slope = __builtin_fmaf(
             g * 0.398942280f, __builtin_amdgcn_exp2f(g * g * -0.72134752f), p);  // g e^(-g^2/2)
         return g * p;
     }
-    case LT_ACT_GELU_TANH: {
+};
+
+struct GeluTanh {  // 0.5 g (1 + tanh(z / 2)) = g / (1 + e^-z)
+    __device__ static inline float of(float g, float* slope)
+    {
         const float s = logistic(g * __builtin_fmaf(kTanhCubic * g, g, kTanhLinear));
         // beyond 100 the second term is 0, and its factors might not fit
         const float c = fminf(fmaxf(g, -100.0f), 100.0f);
@@ -69,10 +60,41 @@ __device__ inline float activate(int kind, float g, float* slope)
                                 __builtin_fmaf(3.0f * kTanhCubic * c, c, kTanhLinear), s);
         return g * s;
     }
-    default:
+};
+
+struct Relu {
+    __device__ static inline float of(float g, float* slope)
+    {
         *slope = g <= 0.0f ? 0.0f : 1.0f;
         return g <= 0.0f ? 0.0f : g;
     }
+};
+
+// The activation and its derivative of N values.  `kind` is the same for a whole launch: a branch,
+// not a kernel for each, and one for all N, whose chains of instructions then overlap.
+template <int N>
+__device__ inline void activate(int kind, const float (&g)[N], float (&y)[N], float (&slope)[N])
+{
+    const auto all = [&](auto act) {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            y[e] = act.of(g[e], &slope[e]);
+    };
+    if (kind == LT_ACT_SILU)
+        all(Silu());
+    else if (kind == LT_ACT_GELU)
+        all(Gelu());
+    else if (kind == LT_ACT_GELU_TANH)
+        all(GeluTanh());
+    else
+        all(Relu());
+}
+
+template <int N>
+__device__ inline void activate(int kind, const float (&g)[N], float (&y)[N])
+{
+    float unused[N];
+    activate(kind, g, y, unused);
 }
 
 // Eight results of a row, wherever it begins; those from `left` on do not exist.
@@ -253,8 +275,12 @@ __global__ __launch_bounds__(512) void k_few(FewArgs g)
             }
         }
         float y = v[0];
-        if constexpr (B == 2)
-            y = activate(g.activation, v[0]) * v[1];
+        if constexpr (B == 2) {
+            const float u[1] = {v[0]};
+            float a[1];
+            activate(g.activation, u, a);
+            y = a[0] * v[1];
+        }
         if constexpr (F32)
             static_cast<float*>(g.out)[tok * g.stride + row] = y;
         else

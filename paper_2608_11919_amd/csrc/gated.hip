@@ -190,20 +190,20 @@ struct ForwardWriter {
         float h[8];
         if constexpr (SAVE) {
             float a[8], b[8];
+            gated::activate(g.activation, u, b, a);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                float slope;
-                b[e] = gated::activate(g.activation, u[e], &slope);
-                a[e] = v[e] * slope;
+                a[e] *= v[e];
                 h[e] = b[e] * v[e];
             }
             const int64_t at = row * g.saved.pitch + col;
             save_eight(g.saved.a_high, g.saved.a_low, at, a);
             save_eight(g.saved.b_high, g.saved.b_low, at, b);
         } else {
+            gated::activate(g.activation, u, h);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                h[e] = gated::activate(g.activation, u[e]) * v[e];
+                h[e] *= v[e];
         }
         store_row<F32>(g.out, row * g.stride + col, h, g.n - col);
     }

@@ -222,8 +222,14 @@ struct ProductWriter {
         scales_at(g.c_scales, col, t);
         const float x = g.a_scales[row];
 #pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            u[e] = scaled(u[e], x, s[e]);
+            v[e] = scaled(v[e], x, t[e]);
+        }
+        gated::activate(g.activation, u, s);
+#pragma unroll
         for (int e = 0; e < 8; ++e)
-            u[e] = gated::activate(g.activation, scaled(u[e], x, s[e])) * scaled(v[e], x, t[e]);
+            u[e] = s[e] * v[e];
         store_row<F32>(g.out, row * g.stride + col, u, g.n - col);
     }
 };
