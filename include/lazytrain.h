@@ -646,7 +646,8 @@ lt_err lt_int8_matmul(const int8_t* a_codes, const float* a_scales, const int8_t
                       int out_dtype, int64_t out_stride, void* workspace, size_t workspace_bytes,
                       void* stream);
 
-/* Bytes of device workspace lt_int8_linear needs; 0 if an argument is invalid. */
+/* Bytes of device workspace lt_int8_linear needs (256, which it does not look at, where it is one
+ * launch: m <= 16 and k <= 8192); 0 if an argument is invalid. */
 size_t lt_int8_linear_workspace_bytes(int64_t m, int64_t n, int64_t k);
 
 /*
@@ -663,7 +664,8 @@ lt_err lt_int8_linear(const void* x, int dtype, int64_t x_stride, const int8_t* 
  * function; 0.5 g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))); max(g, 0). */
 enum { LT_ACT_SILU = 0, LT_ACT_GELU = 1, LT_ACT_GELU_TANH = 2, LT_ACT_RELU = 3 };
 
-/* Bytes of device workspace lt_int8_gated needs; 0 if an argument is invalid. */
+/* Bytes of device workspace lt_int8_gated needs (see lt_int8_linear's); 0 if an argument is
+ * invalid. */
 size_t lt_int8_gated_workspace_bytes(int64_t m, int64_t n, int64_t k);
 
 /*
@@ -682,7 +684,7 @@ size_t lt_gated_saved_bytes(int64_t m, int64_t n);
 
 /* Bytes of device workspace lt_gated_forward needs: copies of operands whose rows are not whole
  * steps of 64 values, or not multiples of 8 apart, else 256, which it does not look at (nor where
- * m <= 32 and nothing is saved).  0 if an argument is invalid. */
+ * m <= 16 and nothing is saved).  0 if an argument is invalid. */
 size_t lt_gated_forward_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t x_stride,
                                         int64_t gate_stride, int64_t up_stride);
 

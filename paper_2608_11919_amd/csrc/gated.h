@@ -183,51 +183,43 @@ __device__ inline void few_load(const uint8_t* row, int64_t at, int64_t bytes, i
         }
 }
 
-// Results for up to 16 T tokens, 16 rows of each of the B weights to a workgroup, bound by
+// Results for up to 16 tokens, 16 rows of each of the B weights to a workgroup, bound by
 // reading the weights once: no LDS tiles, every lane loads its bytes of the instruction's rows
 // straight from HBM, and the waves cut the sum into runs of neighbouring steps.
-template <typename Mul, int T, int B, bool F32>
+template <typename Mul, int B, bool F32>
 __global__ __launch_bounds__(512) void k_few(FewArgs g)
 {
-    extern __shared__ f32x4 few_sums[];  // [wave][B][T][lane], of 16 bytes
+    extern __shared__ f32x4 few_sums[];  // [wave][B][lane], of 16 bytes
     constexpr bool kInt = std::is_same<Mul, FewInt8>::value;
     typedef typename Mul::Acc Acc;
     const int lane = int(threadIdx.x) & 63, r = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
     const int waves = int(blockDim.x) >> 6;
     const int64_t n0 = int64_t(blockIdx.x) * 16;
-    const uint8_t *w[B], *x[T];
+    const uint8_t* w[B];
 #pragma unroll
     for (int b = 0; b < B; ++b) {
         const int64_t row = n0 + r < g.n ? n0 + r : g.n - 1;
         w[b] = g.w[b] + row * g.w_pitch[b];
     }
-#pragma unroll
-    for (int t = 0; t < T; ++t) {
-        const int64_t token = 16 * t + r < g.m ? 16 * t + r : g.m - 1;
-        x[t] = g.x + token * g.x_pitch;
-    }
-    Acc acc[B][T] = {};
+    const uint8_t* x = g.x + (r < g.m ? r : g.m - 1) * g.x_pitch;
+    Acc acc[B] = {};
     struct Loaded {
-        i32x4 w[B][2], x[T][2];
+        i32x4 w[B][2], x[2];
     };
     const auto load = [&](int s, Loaded& in) {
         const int64_t at = int64_t(s) * kFewStep + 32 * q;
 #pragma unroll
         for (int b = 0; b < B; ++b)
             few_load<kInt>(w[b], at, g.bytes, in.w[b]);
-#pragma unroll
-        for (int t = 0; t < T; ++t)
-            few_load<kInt>(x[t], at, g.bytes, in.x[t]);
+        few_load<kInt>(x, at, g.bytes, in.x);
     };
     const auto multiply = [&](const Loaded& in) {
 #pragma unroll
         for (int c = 0; c < 2; ++c)
 #pragma unroll
             for (int b = 0; b < B; ++b)
-#pragma unroll
-                for (int t = 0; t < T; ++t)
-                    acc[b][t] = Mul::mul(in.w[b][c], in.x[t][c], acc[b][t]);
+                acc[b] = Mul::mul(in.w[b][c], in.x[c], acc[b]);
     };
     const int steps = int((g.bytes + kFewStep - 1) / kFewStep);
     const int first = steps * wave / waves, last = steps * (wave + 1) / waves;
@@ -247,62 +239,54 @@ __global__ __launch_bounds__(512) void k_few(FewArgs g)
     }
 #pragma unroll
     for (int b = 0; b < B; ++b)
-#pragma unroll
-        for (int t = 0; t < T; ++t)
-            few_sums[((wave * B + b) * T + t) * 64 + lane] = __builtin_bit_cast(f32x4, acc[b][t]);
+        few_sums[(wave * B + b) * 64 + lane] = __builtin_bit_cast(f32x4, acc[b]);
     __syncthreads();
     // the waves' sums, added in their order
     const float* sums = reinterpret_cast<const float*>(few_sums);
-    for (int e = threadIdx.x; e < T * 256; e += int(blockDim.x)) {
-        const int t = e / 256, l = e / 4 % 64;
-        const int64_t row = n0 + 4 * (l >> 4) + e % 4, tok = 16 * t + (l & 15);
-        if (row >= g.n || tok >= g.m)
-            continue;
-        float v[B];
+    const int e = int(threadIdx.x), l = e / 4;
+    const int64_t row = n0 + 4 * (l >> 4) + e % 4, tok = l & 15;
+    if (e >= 256 || row >= g.n || tok >= g.m)
+        return;
+    float v[B];
 #pragma unroll
-        for (int b = 0; b < B; ++b) {
-            const float* from = sums + b * T * 256 + e;
-            if constexpr (kInt) {
-                int s = 0;
-                for (int i = 0; i < waves; ++i)
-                    s += __float_as_int(from[i * B * T * 256]);
-                v[b] = float(s) * g.x_scales[tok] * g.w_scales[b][row];
-            } else {
-                float s = from[0];
-                for (int i = 1; i < waves; ++i)
-                    s += from[i * B * T * 256];
-                v[b] = s;
-            }
+    for (int b = 0; b < B; ++b) {
+        const float* from = sums + b * 256 + e;
+        if constexpr (kInt) {
+            int s = 0;
+            for (int i = 0; i < waves; ++i)
+                s += __float_as_int(from[i * B * 256]);
+            v[b] = float(s) * g.x_scales[tok] * g.w_scales[b][row];
+        } else {
+            float s = from[0];
+            for (int i = 1; i < waves; ++i)
+                s += from[i * B * 256];
+            v[b] = s;
         }
-        float y = v[0];
-        if constexpr (B == 2) {
-            const float u[1] = {v[0]};
-            float a[1];
-            activate(g.activation, u, a);
-            y = a[0] * v[1];
-        }
-        if constexpr (F32)
-            static_cast<float*>(g.out)[tok * g.stride + row] = y;
-        else
-            static_cast<uint16_t*>(g.out)[tok * g.stride + row] = bf16_bits(y);
     }
+    float y = v[0];
+    if constexpr (B == 2) {
+        const float u[1] = {v[0]};
+        float a[1];
+        activate(g.activation, u, a);
+        y = a[0] * v[1];
+    }
+    if constexpr (F32)
+        static_cast<float*>(g.out)[tok * g.stride + row] = y;
+    else
+        static_cast<uint16_t*>(g.out)[tok * g.stride + row] = bf16_bits(y);
 }
 
-constexpr int64_t kFewTokens = 32;
+// Above these, tiles: 32 tokens in two passes of the instruction took 30 us through 2048 x 11008
+// (bf16, gated), 48 by tiles 19; in integers 14 and 11.
+constexpr int64_t kFewTokens = 16;
 
 template <typename Mul, int B>
 void launch_few(const FewArgs& g, bool f32, hipStream_t st)
 {
     const int64_t steps = (g.bytes + kFewStep - 1) / kFewStep;
     const int waves = steps >= 8 ? 8 : 4;
-    const dim3 grid(uint32_t((g.n + 15) / 16));
-    const auto launch = [&](auto* kernel, int t) {
-        kernel<<<grid, 64 * waves, size_t(waves) * B * t * 1024, st>>>(g);
-    };
-    if (g.m <= 16)
-        launch(f32 ? k_few<Mul, 1, B, true> : k_few<Mul, 1, B, false>, 1);
-    else
-        launch(f32 ? k_few<Mul, 2, B, true> : k_few<Mul, 2, B, false>, 2);
+    auto* kernel = f32 ? k_few<Mul, B, true> : k_few<Mul, B, false>;
+    kernel<<<dim3(uint32_t((g.n + 15) / 16)), 64 * waves, size_t(waves) * B * 1024, st>>>(g);
 }
 
 }  // namespace gated

@@ -287,6 +287,223 @@ __global__ __launch_bounds__(256) void k_int8_join(ProductArgs g, int slices)
     }
 }
 
+// ------------------------------------------------------------- few tokens
+
+// Results for up to 16 tokens where a wave can hold its share of them: eight waves cut the sum,
+// each with up to STEPS steps of 128 values of every token as codes in its registers, and go
+// through blocks of 16 weight rows together, the next block's codes under way while one is
+// multiplied.  x is read once for a workgroup, and where it comes as values (X) it is quantized
+// there, with the tokens' largest magnitudes from all eight waves: an answer is one launch.
+enum { kCodes, kF32, kBf16 };
+
+struct HeldArgs {
+    const uint8_t* w[2];         // one or two weights
+    const float* w_scales[2];
+    const void* x;
+    int64_t x_stride;            // of values
+    const float* x_scales;       // of codes
+    int64_t m, n, k, pitch;
+    int steps;
+    int activation, f32;
+    void* out;
+    int64_t stride;
+};
+
+constexpr int kHeldWaves = 8;
+
+struct Codes32 {
+    i32x4 w[2];
+};
+
+template <typename T>
+struct Values32 {
+    i32x4 w[2 * sizeof(T)];
+};
+
+// The 32 values of a row from column `at` on, zeros behind its end.
+template <typename T>
+__device__ inline Values32<T> load_values(const T* row, int64_t at, int64_t cols)
+{
+    Values32<T> v;
+    constexpr int kLines = int(2 * sizeof(T)), kEach = int(16 / sizeof(T));
+    if (at + 32 <= cols) {
+#pragma unroll
+        for (int c = 0; c < kLines; ++c)
+            v.w[c] = load_any(row + at + c * kEach);
+        return v;
+    }
+#pragma unroll
+    for (int c = 0; c < kLines; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (sizeof(T) == 2) {
+                const int64_t i = at + 8 * c + 2 * e;
+                const uint32_t lo = i < cols ? row[i] : 0u, hi = i + 1 < cols ? row[i + 1] : 0u;
+                v.w[c][e] = int(lo | hi << 16);
+            } else {
+                const int64_t i = at + 4 * c + e;
+                v.w[c][e] = i < cols ? __float_as_int(row[i]) : 0;
+            }
+        }
+    return v;
+}
+
+template <typename T>
+__device__ inline float value_of(const Values32<T>& v, int i)
+{
+    if constexpr (sizeof(T) == 2) {
+        const auto w = uint32_t(v.w[i / 8][i % 8 / 2]);
+        return __uint_as_float(i % 2 == 0 ? w << 16 : w & 0xFFFF0000u);
+    } else {
+        return __int_as_float(v.w[i / 4][i % 4]);
+    }
+}
+
+template <int STEPS, int B, int X>
+__global__ __launch_bounds__(64 * kHeldWaves) void k_int8_held(HeldArgs g)
+{
+    typedef typename std::conditional<X == kF32, float, uint16_t>::type Value;
+    __shared__ int sums[2][B][kHeldWaves][256];
+    __shared__ uint32_t tops[kHeldWaves][16];
+    __shared__ float x_scale[16];
+    const int lane = int(threadIdx.x) & 63, r = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+    const int first = g.steps * wave / kHeldWaves;
+    const int count = g.steps * (wave + 1) / kHeldWaves - first;
+    const int64_t blocks = (g.n + 15) / 16;
+
+    struct Rows {
+        Codes32 codes[STEPS];
+    } even, odd;
+    const auto load = [&](int b, int64_t block, Rows& w) {
+        int64_t row = block * 16 + r;
+        row = row < g.n ? row : g.n - 1;
+        const uint8_t* p = g.w[b] + row * g.pitch + int64_t(first) * 128 + 32 * q;
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i)
+            if (i < count) {
+                w.codes[i].w[0] = load_any(p + i * 128);
+                w.codes[i].w[1] = load_any(p + i * 128 + 16);
+            }
+    };
+    load(0, blockIdx.x, even);
+
+    Codes32 x[STEPS];
+    const int64_t token = r < g.m ? r : g.m - 1;
+    if constexpr (X == kCodes) {
+        const uint8_t* p = static_cast<const uint8_t*>(g.x) + token * g.pitch +
+                           int64_t(first) * 128 + 32 * q;
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i)
+            if (i < count) {
+                x[i].w[0] = load_any(p + i * 128);
+                x[i].w[1] = load_any(p + i * 128 + 16);
+            }
+        if (threadIdx.x < 16)
+            x_scale[threadIdx.x] = g.x_scales[token];
+    } else {
+        const Value* row = static_cast<const Value*>(g.x) + token * g.x_stride;
+        const auto values = [&](int i) {
+            return load_values(row, int64_t(first + i) * 128 + 32 * q, g.k);
+        };
+        // a short share stays in registers, a longer one is read a second time
+        constexpr int kKept = STEPS * int(sizeof(Value)) <= 8 ? STEPS : 1;
+        Values32<Value> kept[kKept];
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i)
+            if (i < count) {
+                kept[i % kKept] = values(i);
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                    top = max(top, __float_as_uint(value_of(kept[i % kKept], e)) & 0x7FFFFFFFu);
+            }
+        top = max(top, uint32_t(__shfl_xor(int(top), 16, 64)));
+        top = max(top, uint32_t(__shfl_xor(int(top), 32, 64)));
+        if (lane < 16)
+            tops[wave][lane] = top;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kHeldWaves; ++i)
+            top = max(top, tops[i][r]);
+        const RowScale scale = scale_of(top);
+        if (threadIdx.x < 16)
+            x_scale[threadIdx.x] = scale.scale;
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i)
+            if (i < count) {
+                if constexpr (kKept != STEPS)
+                    kept[0] = values(i);
+                const Values32<Value>& v = kept[i % kKept];
+#pragma unroll
+                for (int word = 0; word < 8; ++word) {
+                    uint32_t c = 0;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        c |= code_of(value_of(v, 4 * word + e), scale) << (8 * e);
+                    x[i].w[word / 4][word % 4] = int(c);
+                }
+            }
+    }
+
+    const auto multiply = [&](const Rows& w, int (&to)[kHeldWaves][256]) {
+        i32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i)
+            if (i < count)
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+                    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(w.codes[i].w[c], x[i].w[c], acc, 0,
+                                                                0, 0);
+        *reinterpret_cast<i32x4*>(&to[wave][lane * 4]) = acc;  // rows 4 q + e of token r
+    };
+    const auto finish = [&](int64_t block, int turn) {
+        __syncthreads();  // and the other buffer's sums have been read
+        const int e = int(threadIdx.x);
+        const int64_t row = block * 16 + 4 * (e >> 6) + e % 4, tok = e / 4 % 16;
+        if (e >= 256 || row >= g.n || tok >= g.m)
+            return;
+        float v[B];
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+            int s = 0;
+#pragma unroll
+            for (int i = 0; i < kHeldWaves; ++i)
+                s += sums[turn][b][i][e];
+            v[b] = float(s) * x_scale[tok] * g.w_scales[b][row];
+        }
+        float y = v[0];
+        if constexpr (B == 2) {
+            const float u[1] = {v[0]};
+            float a[1];
+            gated::activate(g.activation, u, a);
+            y = a[0] * v[1];
+        }
+        if (g.f32)
+            static_cast<float*>(g.out)[tok * g.stride + row] = y;
+        else
+            static_cast<uint16_t*>(g.out)[tok * g.stride + row] = gated::bf16_bits(y);
+    };
+    int turn = 0;
+    for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x, turn ^= 1) {
+        const int64_t next = b + gridDim.x;
+        if constexpr (B == 2) {
+            load(1, b, odd);
+            multiply(even, sums[turn][0]);
+            if (next < blocks)
+                load(0, next, even);
+            multiply(odd, sums[turn][1]);
+            finish(b, turn);
+        } else {
+            if (next < blocks)
+                load(0, next, odd);
+            multiply(even, sums[turn][0]);
+            finish(b, turn);
+            even = odd;
+        }
+    }
+}
+
 // ---------------------------------------------------------------- host side
 
 constexpr int64_t kMostSummed = int64_t(1) << 17;  // 127^2 * 2^17 < 2^31
@@ -407,6 +624,12 @@ lt_err zero_rows(void* out, int dtype, int64_t m, int64_t n, int64_t stride, hip
     return host::launch_zero(out, dtype == LT_DTYPE_F32 ? 4 : 2, m, n, stride, st);
 }
 
+// Whether few tokens' codes fit the registers of a workgroup.
+bool held(int64_t m, int64_t k)
+{
+    return m <= gated::kFewTokens && k <= kHeldWaves * 8 * 128;
+}
+
 // Workspace of the calls that quantize x themselves: [codes][scales][the product's].
 struct LinearLayout {
     size_t scales, matmul, total;
@@ -414,11 +637,62 @@ struct LinearLayout {
 
 LinearLayout linear_layout(int64_t m, int64_t n, int64_t k, bool pair)
 {
-    LinearLayout l;
+    LinearLayout l{0, 0, 256};
+    if (held(m, k))
+        return l;
     l.scales = host::round_up(size_t(m) * size_t(code_pitch(k)), 256);
     l.matmul = l.scales + host::round_up(size_t(m) * 4, 256);
     l.total = l.matmul + (pair ? 0 : lt_int8_matmul_workspace_bytes(m, n, k));
     return l;
+}
+
+// For sums that held() allows.
+template <int B, int X>
+void launch_held(const HeldArgs& g, int cus, hipStream_t st)
+{
+    const int each = int(host::ceil_div(g.steps, kHeldWaves));
+    const auto go = [&](auto* kernel, int a_cu) {
+        const int64_t groups = std::min<int64_t>(host::ceil_div(g.n, 16), int64_t(a_cu) * cus);
+        kernel<<<dim3(uint32_t(groups)), 64 * kHeldWaves, 0, st>>>(g);
+    };
+    if (each <= 2)
+        go(k_int8_held<2, B, X>, 2);
+    else if (each <= 5)
+        go(k_int8_held<5, B, X>, 1);
+    else
+        go(k_int8_held<8, B, X>, 1);
+}
+
+template <int X>
+lt_err run_held(const ProductArgs& g, const void* x, int64_t x_stride, int64_t k, int out_dtype,
+                hipStream_t st)
+{
+    HeldArgs h{};
+    h.w[0] = g.b;
+    h.w[1] = g.c;
+    h.w_scales[0] = g.b_scales;
+    h.w_scales[1] = g.c_scales;
+    h.x = x;
+    h.x_stride = x_stride;
+    h.x_scales = g.a_scales;
+    h.m = g.m;
+    h.n = g.n;
+    h.k = k;
+    h.pitch = code_pitch(k);
+    h.steps = int(host::ceil_div(k, kPitch));
+    h.activation = g.activation;
+    h.f32 = out_dtype == LT_DTYPE_F32;
+    h.out = g.out;
+    h.stride = g.stride;
+    int cus;
+    if (lt_err e = host::compute_units(&cus))
+        return e;
+    if (g.c)
+        launch_held<2, X>(h, cus, st);
+    else
+        launch_held<1, X>(h, cus, st);
+    LT_TRY_HIP(hipGetLastError());
+    return LT_OK;
 }
 
 // The product of codes, its arguments checked.  c: the second weight of a pair, or null.
@@ -429,6 +703,8 @@ lt_err run_product(const ProductArgs& args, int64_t k, int out_dtype, void* work
     const bool f32 = out_dtype == LT_DTYPE_F32, pair = g.c != nullptr;
     g.pitch = code_pitch(k);
     g.steps = int(host::ceil_div(k, kPitch));
+    if (held(g.m, k))
+        return run_held<kCodes>(g, g.a, 0, k, out_dtype, st);
     if (g.m <= gated::kFewTokens) {
         gated::FewArgs f{};
         f.w[0] = g.b;
@@ -492,10 +768,12 @@ lt_err answer(const void* x, int dtype, int64_t x_stride, const int8_t* w, const
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (k == 0)
         return zero_rows(out, out_dtype, m, n, out_stride, st);
+    const bool one = held(m, k);  // one launch without a workspace
     const LinearLayout l = linear_layout(m, n, k, pair);
-    if (!workspace || !host::aligned(workspace, 256) || workspace_bytes < l.total)
+    if (!one && (!workspace || !host::aligned(workspace, 256) || workspace_bytes < l.total))
         return fail(LT_ERR_WORKSPACE, "workspace must be 256-byte aligned and hold " +
                                           std::to_string(l.total) + " bytes");
+    const size_t ws_bytes = one ? 0 : l.total;
     const size_t out_bytes = span_bytes(m, n, out_stride, out_dtype);
     const size_t w_bytes = size_t(n) * size_t(code_pitch(k));
     const struct {
@@ -505,22 +783,13 @@ lt_err answer(const void* x, int dtype, int64_t x_stride, const int8_t* w, const
                 {w2, w_bytes}, {w2_scales, size_t(n) * 4}};
     for (const auto& r : read)
         if (host::overlaps(out, out_bytes, r.p, r.bytes) ||
-            host::overlaps(workspace, l.total, r.p, r.bytes))
+            host::overlaps(workspace, ws_bytes, r.p, r.bytes))
             return fail(LT_ERR_INVALID_ARG, "out or the workspace overlaps x or a weight");
-    if (host::overlaps(out, out_bytes, workspace, l.total))
+    if (host::overlaps(out, out_bytes, workspace, ws_bytes))
         return fail(LT_ERR_INVALID_ARG, "out overlaps the workspace");
-    auto* ws = static_cast<uint8_t*>(workspace);
-    if (lt_err e = host::workspace_written(ws, l.total, st))
-        return e;
-    auto* codes = reinterpret_cast<int8_t*>(ws);
-    auto* scales = reinterpret_cast<float*>(ws + l.scales);
-    if (lt_err e = launch_quantize(x, dtype, m, k, x_stride, codes, scales, st))
-        return e;
     ProductArgs g{};
-    g.a = ws;
     g.b = reinterpret_cast<const uint8_t*>(w);
     g.c = pair ? reinterpret_cast<const uint8_t*>(w2) : nullptr;
-    g.a_scales = scales;
     g.b_scales = w_scales;
     g.c_scales = w2_scales;
     g.m = m;
@@ -528,6 +797,18 @@ lt_err answer(const void* x, int dtype, int64_t x_stride, const int8_t* w, const
     g.activation = activation;
     g.out = out;
     g.stride = out_stride;
+    if (one)
+        return dtype == LT_DTYPE_F32 ? run_held<kF32>(g, x, x_stride, k, out_dtype, st)
+                                     : run_held<kBf16>(g, x, x_stride, k, out_dtype, st);
+    auto* ws = static_cast<uint8_t*>(workspace);
+    if (lt_err e = host::workspace_written(ws, l.total, st))
+        return e;
+    auto* codes = reinterpret_cast<int8_t*>(ws);
+    auto* scales = reinterpret_cast<float*>(ws + l.scales);
+    if (lt_err e = launch_quantize(x, dtype, m, k, x_stride, codes, scales, st))
+        return e;
+    g.a = ws;
+    g.a_scales = scales;
     return run_product(g, k, out_dtype, ws + l.matmul, st);
 }
 

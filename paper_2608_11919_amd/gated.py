@@ -48,7 +48,7 @@ def _forward(x, gate, up, activation, out_dtype, keep, workspace):
     if keep:
         saved = torch.empty(int(lib().lt_gated_saved_bytes(m, n)), dtype=torch.uint8, device=device)
     ws, nbytes, handle = 0, 0, _stream_handle(None, device)
-    if (keep or m > 32) and (k % 64 or (x_stride | g_stride | u_stride) % 8) or \
+    if (keep or m > 16) and (k % 64 or (x_stride | g_stride | u_stride) % 8) or \
             workspace is not None:
         need = int(lib().lt_gated_forward_workspace_bytes(m, n, k, x_stride, g_stride, u_stride))
         held, ws, nbytes = _scratch(device, need, workspace, None)

@@ -114,6 +114,13 @@ class Int8Weight:
             lt_int8_quantize(_laid_out(w, aligned=False), self.codes, self.scales)
 
 
+def _call_workspace(device, need, m: int, k: int, workspace):
+    """What a call works in: nothing where it is one launch (see lt_int8_linear_workspace_bytes)."""
+    if m <= 16 and k <= 8192 and workspace is None:
+        return None, 0, 0
+    return _scratch(device, int(need()), workspace, None)
+
+
 def _input(x: torch.Tensor, weight: Int8Weight):
     t = _tokens(x, weight.cols, "x", aligned=False)
     if weight.codes.device != x.device:
@@ -131,8 +138,8 @@ def int8_linear(x: torch.Tensor, weight: Int8Weight, out_dtype: torch.dtype = to
     y = torch.empty(m, n, dtype=out_dtype, device=device)
     out = _dtype_code(y, "y")
     handle = _stream_handle(None, device)
-    held, ws, nbytes = _scratch(device, int(lib().lt_int8_linear_workspace_bytes(m, n, k)),
-                                workspace, None)
+    held, ws, nbytes = _call_workspace(
+        device, lambda: lib().lt_int8_linear_workspace_bytes(m, n, k), m, k, workspace)
     with _current(device):
         _check(lib().lt_int8_linear(t.data_ptr(), code, stride, weight.codes.data_ptr(),
                                     weight.scales.data_ptr(), m, n, k, y.data_ptr(), out, n, ws,
@@ -156,8 +163,8 @@ def int8_gated_linear(x: torch.Tensor, gate: Int8Weight, up: Int8Weight,
     y = torch.empty(m, n, dtype=out_dtype, device=device)
     out = _dtype_code(y, "y")
     handle = _stream_handle(None, device)
-    held, ws, nbytes = _scratch(device, int(lib().lt_int8_gated_workspace_bytes(m, n, k)),
-                                workspace, None)
+    held, ws, nbytes = _call_workspace(
+        device, lambda: lib().lt_int8_gated_workspace_bytes(m, n, k), m, k, workspace)
     with _current(device):
         _check(lib().lt_int8_gated(t.data_ptr(), code, stride, gate.codes.data_ptr(),
                                    gate.scales.data_ptr(), up.codes.data_ptr(),

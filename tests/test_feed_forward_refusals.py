@@ -65,11 +65,11 @@ def backward(dh=BASE, dh_dtype=lt.LT_DTYPE_BF16, dhs=48, saved=2 * BASE, x=3 * B
     lambda: linear(out=BASE + ((3 * 130 + 130) * 4 - 1) // 16 * 16),
     lambda: linear(out=2 * BASE),
     lambda: linear(w_scales=4 * BASE),
-    lambda: linear(ws=2 * BASE),
-    lambda: linear(out=WS),
+    lambda: linear(m=40, ws=2 * BASE),
+    lambda: linear(m=40, out=WS),
     lambda: int8_gated(out=4 * BASE),
     lambda: int8_gated(us=6 * BASE),
-    lambda: int8_gated(ws=4 * BASE),
+    lambda: int8_gated(m=40, ws=4 * BASE),
     lambda: forward(out=BASE),
     lambda: forward(out=3 * BASE + 47 * 130 * 2 // 16 * 16),
     lambda: forward(saved=2 * BASE + 64),
@@ -171,9 +171,9 @@ def test_alignment(call):
 @pytest.mark.parametrize("call", [
     lambda: matmul(k=12800, ws=0),
     lambda: matmul(k=12800, ws_bytes=256),
-    lambda: linear(ws=0),
-    lambda: linear(ws=WS + 64),
-    lambda: int8_gated(ws_bytes=100),
+    lambda: linear(m=40, ws=0),
+    lambda: linear(m=40, ws=WS + 64),
+    lambda: int8_gated(m=40, ws_bytes=100),
     lambda: forward(ws=0),
     lambda: forward(ws_bytes=1000),
     lambda: backward(ws=0),
@@ -201,6 +201,8 @@ def test_sizes_of_memory():
     assert L.lt_int8_matmul_workspace_bytes(4, 4, 4) == 256
     assert L.lt_int8_matmul_workspace_bytes(40, 48, 1 << 18) == 0
     assert L.lt_int8_linear_workspace_bytes(100, 4, 300) >= 100 * 384 + 400
+    assert L.lt_int8_linear_workspace_bytes(16, 4, 8192) == 256
+    assert L.lt_int8_linear_workspace_bytes(16, 4, 8193) > 16 * 8193
     assert L.lt_int8_gated_workspace_bytes(-1, 4, 300) == 0
     assert L.lt_gated_saved_bytes(3, 9) == 6 * 3 * 16
     assert L.lt_gated_saved_bytes(3, 1 << 21) == 0

@@ -93,6 +93,7 @@ def same(got, want):
 
 
 SIZES = [(1, 1, 1), (1, 520, 300), (2, 17, 129), (16, 33, 1000), (17, 300, 128), (32, 64, 2048),
+         (5, 9000, 2048), (16, 8300, 2049), (3, 4200, 5121), (16, 70, 8192), (2, 70, 8193),
          (33, 65, 127), (64, 64, 6400), (65, 200, 9001), (100, 1, 12800), (300, 257, 257),
          (129, 4096, 640), (520, 2050, 96), (1030, 16390, 130)]
 
@@ -180,6 +181,7 @@ def activation(name, g):
 
 
 @pytest.mark.parametrize("m,n,k", [(1, 1, 1), (1, 520, 300), (16, 33, 1000), (17, 300, 128),
+                                   (16, 9000, 700), (5, 4200, 2100), (3, 300, 8000), (2, 40, 8300),
                                    (33, 65, 127), (65, 200, 3001), (300, 257, 257),
                                    (129, 4096, 640), (520, 2050, 96), (1030, 8200, 130)])
 @pytest.mark.parametrize("act", list(ROOM))
