@@ -647,7 +647,7 @@ lt_err lt_int8_matmul(const int8_t* a_codes, const float* a_scales, const int8_t
                       void* stream);
 
 /* Bytes of device workspace lt_int8_linear needs (256, which it does not look at, where it is one
- * launch: m <= 16 and k <= 8192); 0 if an argument is invalid. */
+ * launch: m <= 16, k <= 8192 and m * k <= 2^15); 0 if an argument is invalid. */
 size_t lt_int8_linear_workspace_bytes(int64_t m, int64_t n, int64_t k);
 
 /*

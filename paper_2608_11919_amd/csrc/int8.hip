@@ -315,56 +315,14 @@ struct Codes32 {
     i32x4 w[2];
 };
 
-template <typename T>
-struct Values32 {
-    i32x4 w[2 * sizeof(T)];
-};
-
-// The 32 values of a row from column `at` on, zeros behind its end.
-template <typename T>
-__device__ inline Values32<T> load_values(const T* row, int64_t at, int64_t cols)
-{
-    Values32<T> v;
-    constexpr int kLines = int(2 * sizeof(T)), kEach = int(16 / sizeof(T));
-    if (at + 32 <= cols) {
-#pragma unroll
-        for (int c = 0; c < kLines; ++c)
-            v.w[c] = load_any(row + at + c * kEach);
-        return v;
-    }
-#pragma unroll
-    for (int c = 0; c < kLines; ++c)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if constexpr (sizeof(T) == 2) {
-                const int64_t i = at + 8 * c + 2 * e;
-                const uint32_t lo = i < cols ? row[i] : 0u, hi = i + 1 < cols ? row[i + 1] : 0u;
-                v.w[c][e] = int(lo | hi << 16);
-            } else {
-                const int64_t i = at + 4 * c + e;
-                v.w[c][e] = i < cols ? __float_as_int(row[i]) : 0;
-            }
-        }
-    return v;
-}
-
-template <typename T>
-__device__ inline float value_of(const Values32<T>& v, int i)
-{
-    if constexpr (sizeof(T) == 2) {
-        const auto w = uint32_t(v.w[i / 8][i % 8 / 2]);
-        return __uint_as_float(i % 2 == 0 ? w << 16 : w & 0xFFFF0000u);
-    } else {
-        return __int_as_float(v.w[i / 4][i % 4]);
-    }
-}
-
 template <int STEPS, int B, int X>
 __global__ __launch_bounds__(64 * kHeldWaves) void k_int8_held(HeldArgs g)
 {
     typedef typename std::conditional<X == kF32, float, uint16_t>::type Value;
-    __shared__ int sums[2][B][kHeldWaves][256];
-    __shared__ uint32_t tops[kHeldWaves][16];
+    extern __shared__ i32x4 held_lds[];  // x's codes, m rows of pitch + 16 bytes, before the sums
+    typedef int Sums[B][kHeldWaves][256];
+    auto* sums = reinterpret_cast<Sums*>(held_lds);  // [2]
+    __shared__ uint32_t tops[kHeldWaves];
     __shared__ float x_scale[16];
     const int lane = int(threadIdx.x) & 63, r = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
@@ -386,11 +344,11 @@ __global__ __launch_bounds__(64 * kHeldWaves) void k_int8_held(HeldArgs g)
                 w.codes[i].w[1] = load_any(p + i * 128 + 16);
             }
     };
-    load(0, blockIdx.x, even);
 
     Codes32 x[STEPS];
     const int64_t token = r < g.m ? r : g.m - 1;
     if constexpr (X == kCodes) {
+        load(0, blockIdx.x, even);
         const uint8_t* p = static_cast<const uint8_t*>(g.x) + token * g.pitch +
                            int64_t(first) * 128 + 32 * q;
 #pragma unroll
@@ -402,48 +360,74 @@ __global__ __launch_bounds__(64 * kHeldWaves) void k_int8_held(HeldArgs g)
         if (threadIdx.x < 16)
             x_scale[threadIdx.x] = g.x_scales[token];
     } else {
-        const Value* row = static_cast<const Value*>(g.x) + token * g.x_stride;
-        const auto values = [&](int i) {
-            return load_values(row, int64_t(first + i) * 128 + 32 * q, g.k);
-        };
-        // a short share stays in registers, a longer one is read a second time
-        constexpr int kKept = STEPS * int(sizeof(Value)) <= 8 ? STEPS : 1;
-        Values32<Value> kept[kKept];
-        uint32_t top = 0;
+        // each value once: a token by one wave, or few tokens by several each; the first part is
+        // under way before the weights are
+        const int share = g.m == 1 ? 8 : g.m == 2 ? 4 : g.m <= 4 ? 2 : 1;
+        const int part = wave % share, at_once = kHeldWaves / share;
+        constexpr int kKept = 4;
+        const int64_t step = int64_t(share) * 64 * 8, from = (part * 64 + lane) * 8;
+        const int64_t code_row = g.pitch + 16;
+        auto* codes = reinterpret_cast<uint8_t*>(held_lds);
+        for (int t0 = 0; t0 < g.m; t0 += at_once) {
+            const int t = t0 + wave / share;
+            const bool there = t < g.m;
+            const Value* row = static_cast<const Value*>(g.x) + (there ? t : 0) * g.x_stride;
+            const int64_t cols = there ? g.k : 0;
+            float v[kKept][8];
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i)
-            if (i < count) {
-                kept[i % kKept] = values(i);
+            for (int h = 0; h < kKept; ++h)
+                load_eight(row, from + h * step, cols, v[h]);
+            if (t0 == 0)
+                load(0, blockIdx.x, even);
+            uint32_t top = 0;
+            const auto look = [&](const float (&u)[8]) {
 #pragma unroll
-                for (int e = 0; e < 32; ++e)
-                    top = max(top, __float_as_uint(value_of(kept[i % kKept], e)) & 0x7FFFFFFFu);
+                for (int e = 0; e < 8; ++e)
+                    top = max(top, __float_as_uint(u[e]) & 0x7FFFFFFFu);
+            };
+#pragma unroll
+            for (int h = 0; h < kKept; ++h)
+                look(v[h]);
+            for (int64_t at = from + kKept * step; at < cols; at += step) {
+                float u[8];
+                load_eight(row, at, cols, u);
+                look(u);
             }
-        top = max(top, uint32_t(__shfl_xor(int(top), 16, 64)));
-        top = max(top, uint32_t(__shfl_xor(int(top), 32, 64)));
-        if (lane < 16)
-            tops[wave][lane] = top;
+#pragma unroll
+            for (int o = 32; o >= 1; o >>= 1)
+                top = max(top, uint32_t(__shfl_xor(int(top), o, 64)));
+            if (share > 1) {  // all tokens at once
+                if (lane == 0)
+                    tops[wave] = top;
+                __syncthreads();
+                for (int i = 0; i < share; ++i)
+                    top = max(top, tops[wave / share * share + i]);
+            }
+            if (!there)
+                continue;
+            const RowScale scale = scale_of(top);
+            if (lane == 0)
+                x_scale[t] = scale.scale;
+#pragma unroll
+            for (int h = 0; h < kKept; ++h)
+                if (from + h * step < g.pitch)
+                    *reinterpret_cast<uint2*>(codes + t * code_row + from + h * step) =
+                        codes_of(v[h], scale);
+            for (int64_t at = from + kKept * step; at < g.pitch; at += step) {
+                float u[8];
+                load_eight(row, at, cols, u);
+                *reinterpret_cast<uint2*>(codes + t * code_row + at) = codes_of(u, scale);
+            }
+        }
         __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kHeldWaves; ++i)
-            top = max(top, tops[i][r]);
-        const RowScale scale = scale_of(top);
-        if (threadIdx.x < 16)
-            x_scale[threadIdx.x] = scale.scale;
+        const uint8_t* p = codes + token * code_row + int64_t(first) * 128 + 32 * q;
 #pragma unroll
         for (int i = 0; i < STEPS; ++i)
             if (i < count) {
-                if constexpr (kKept != STEPS)
-                    kept[0] = values(i);
-                const Values32<Value>& v = kept[i % kKept];
-#pragma unroll
-                for (int word = 0; word < 8; ++word) {
-                    uint32_t c = 0;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        c |= code_of(value_of(v, 4 * word + e), scale) << (8 * e);
-                    x[i].w[word / 4][word % 4] = int(c);
-                }
+                x[i].w[0] = *reinterpret_cast<const i32x4*>(p + i * 128);
+                x[i].w[1] = *reinterpret_cast<const i32x4*>(p + i * 128 + 16);
             }
+        __syncthreads();
     }
 
     const auto multiply = [&](const Rows& w, int (&to)[kHeldWaves][256]) {
@@ -630,6 +614,10 @@ bool held(int64_t m, int64_t k)
     return m <= gated::kFewTokens && k <= kHeldWaves * 8 * 128;
 }
 
+// Whether every workgroup quantizes x itself: 4 tokens through 5120 x 17408 23.1 us, with a launch
+// of the quantizer before 23.6; 8 tokens 25.5 and 24.1; 8 through 2048 x 11008 9.0 and 9.6.
+bool one_launch(int64_t m, int64_t k) { return held(m, k) && m * k <= 32768; }
+
 // Workspace of the calls that quantize x themselves: [codes][scales][the product's].
 struct LinearLayout {
     size_t scales, matmul, total;
@@ -638,7 +626,7 @@ struct LinearLayout {
 LinearLayout linear_layout(int64_t m, int64_t n, int64_t k, bool pair)
 {
     LinearLayout l{0, 0, 256};
-    if (held(m, k))
+    if (one_launch(m, k))
         return l;
     l.scales = host::round_up(size_t(m) * size_t(code_pitch(k)), 256);
     l.matmul = l.scales + host::round_up(size_t(m) * 4, 256);
@@ -653,10 +641,15 @@ void launch_held(const HeldArgs& g, int cus, hipStream_t st)
     const int each = int(host::ceil_div(g.steps, kHeldWaves));
     const auto go = [&](auto* kernel, int a_cu) {
         const int64_t groups = std::min<int64_t>(host::ceil_div(g.n, 16), int64_t(a_cu) * cus);
-        kernel<<<dim3(uint32_t(groups)), 64 * kHeldWaves, 0, st>>>(g);
+        const size_t codes = X == kCodes ? 0 : size_t(g.m) * size_t(g.pitch + 16);
+        kernel<<<dim3(uint32_t(groups)), 64 * kHeldWaves,
+                 std::max(codes, size_t(2 * B * kHeldWaves * 1024)), st>>>(g);
     };
+    // one workgroup to a CU (a token through 5120 x 17408 21 us, with two 23, with one for every
+    // block 26), two where they are small and find their codes made (16 tokens through
+    // 2048 x 11008, codes given, 7.7 us, with one 8.2)
     if (each <= 2)
-        go(k_int8_held<2, B, X>, 2);
+        go(k_int8_held<2, B, X>, X == kCodes ? 2 : 1);
     else if (each <= 5)
         go(k_int8_held<5, B, X>, 1);
     else
@@ -768,7 +761,7 @@ lt_err answer(const void* x, int dtype, int64_t x_stride, const int8_t* w, const
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (k == 0)
         return zero_rows(out, out_dtype, m, n, out_stride, st);
-    const bool one = held(m, k);  // one launch without a workspace
+    const bool one = one_launch(m, k);  // without a workspace
     const LinearLayout l = linear_layout(m, n, k, pair);
     if (!one && (!workspace || !host::aligned(workspace, 256) || workspace_bytes < l.total))
         return fail(LT_ERR_WORKSPACE, "workspace must be 256-byte aligned and hold " +

@@ -71,10 +71,9 @@ def lt_int8_matmul(a_codes: torch.Tensor, a_scales: torch.Tensor, b_codes: torch
     device = out.device
     a, sa = _layout(a_codes, a_scales, m, k, device, "a_codes")
     b, sb = _layout(b_codes, b_scales, n, k, device, "b_codes")
-    ws, nbytes, handle = 0, 0, _stream_handle(stream, device)
-    need = int(lib().lt_int8_matmul_workspace_bytes(m, n, k))
-    if need > 256 or workspace is not None:
-        held, ws, nbytes = _scratch(device, need, workspace, stream)
+    handle = _stream_handle(stream, device)
+    held, ws, nbytes = _call_workspace(device, lib().lt_int8_matmul_workspace_bytes(m, n, k),
+                                       workspace, stream)
     with _current(device):
         _check(lib().lt_int8_matmul(a, sa, b, sb, m, n, k, out.data_ptr(), code, stride, ws,
                                     nbytes, handle))
@@ -114,11 +113,11 @@ class Int8Weight:
             lt_int8_quantize(_laid_out(w, aligned=False), self.codes, self.scales)
 
 
-def _call_workspace(device, need, m: int, k: int, workspace):
-    """What a call works in: nothing where it is one launch (see lt_int8_linear_workspace_bytes)."""
-    if m <= 16 and k <= 8192 and workspace is None:
+def _call_workspace(device, need: int, workspace, stream=None):
+    """What a call works in; 256 bytes are what it does not look at."""
+    if need <= 256 and workspace is None:
         return None, 0, 0
-    return _scratch(device, int(need()), workspace, None)
+    return _scratch(device, need, workspace, stream)
 
 
 def _input(x: torch.Tensor, weight: Int8Weight):
@@ -138,8 +137,8 @@ def int8_linear(x: torch.Tensor, weight: Int8Weight, out_dtype: torch.dtype = to
     y = torch.empty(m, n, dtype=out_dtype, device=device)
     out = _dtype_code(y, "y")
     handle = _stream_handle(None, device)
-    held, ws, nbytes = _call_workspace(
-        device, lambda: lib().lt_int8_linear_workspace_bytes(m, n, k), m, k, workspace)
+    held, ws, nbytes = _call_workspace(device, lib().lt_int8_linear_workspace_bytes(m, n, k),
+                                       workspace)
     with _current(device):
         _check(lib().lt_int8_linear(t.data_ptr(), code, stride, weight.codes.data_ptr(),
                                     weight.scales.data_ptr(), m, n, k, y.data_ptr(), out, n, ws,
@@ -163,8 +162,8 @@ def int8_gated_linear(x: torch.Tensor, gate: Int8Weight, up: Int8Weight,
     y = torch.empty(m, n, dtype=out_dtype, device=device)
     out = _dtype_code(y, "y")
     handle = _stream_handle(None, device)
-    held, ws, nbytes = _call_workspace(
-        device, lambda: lib().lt_int8_gated_workspace_bytes(m, n, k), m, k, workspace)
+    held, ws, nbytes = _call_workspace(device, lib().lt_int8_gated_workspace_bytes(m, n, k),
+                                       workspace)
     with _current(device):
         _check(lib().lt_int8_gated(t.data_ptr(), code, stride, gate.codes.data_ptr(),
                                    gate.scales.data_ptr(), up.codes.data_ptr(),

@@ -201,8 +201,10 @@ def test_sizes_of_memory():
     assert L.lt_int8_matmul_workspace_bytes(4, 4, 4) == 256
     assert L.lt_int8_matmul_workspace_bytes(40, 48, 1 << 18) == 0
     assert L.lt_int8_linear_workspace_bytes(100, 4, 300) >= 100 * 384 + 400
-    assert L.lt_int8_linear_workspace_bytes(16, 4, 8192) == 256
-    assert L.lt_int8_linear_workspace_bytes(16, 4, 8193) > 16 * 8193
+    assert L.lt_int8_linear_workspace_bytes(4, 4, 8192) == 256
+    assert L.lt_int8_linear_workspace_bytes(16, 4, 2048) == 256
+    assert L.lt_int8_linear_workspace_bytes(16, 4, 2049) > 16 * 2049
+    assert L.lt_int8_linear_workspace_bytes(1, 4, 8193) > 8193
     assert L.lt_int8_gated_workspace_bytes(-1, 4, 300) == 0
     assert L.lt_gated_saved_bytes(3, 9) == 6 * 3 * 16
     assert L.lt_gated_saved_bytes(3, 1 << 21) == 0
