@@ -3,6 +3,8 @@
 #ifndef LAZYTRAIN_GATED_H
 #define LAZYTRAIN_GATED_H
 
+#include <algorithm>
+
 #include "lazytrain.h"
 #include "tiles.h"
 
@@ -287,6 +289,55 @@ void launch_few(const FewArgs& g, bool f32, hipStream_t st)
     const int waves = steps >= 8 ? 8 : 4;
     auto* kernel = f32 ? k_few<Mul, B, true> : k_few<Mul, B, false>;
     kernel<<<dim3(uint32_t((g.n + 15) / 16)), 64 * waves, size_t(waves) * B * 1024, st>>>(g);
+}
+
+// ------------------------------------------------------------- tiles
+
+struct Way {
+    int tile;    // 256, 128 or 64
+    int slices;  // of the sum
+    int slice;   // steps of each
+};
+
+// The tile and the slices of the sum that a launch is expected to end first with.  The CU with the
+// most tiles sets its time; a tile costs so many microseconds a step and beside its steps, and
+// slices another launch and their sums' way to memory and back (4 TB/s).  Fitted to products of 16
+// to 8192 rows, 1024 to 5120 summed values and 1024 to 17408 columns in both types, where the
+// choice is within 10% of the best tile but for a few (23% at most); the largest tile wherever it
+// gives every CU one was up to twice as slow (1536 x 2048 x 11008 in integers 61 us, by tiles of
+// 128 45; 768 x 2048 x 11008 gated in bf16 92 and 75; 3500 x 4096 x 1024 28 and 20).
+// `pair`: a tile's columns are two weights'; such sums are not cut.
+inline Way way_of(int64_t m, int64_t n, int64_t count, int steps, bool pair)
+{
+    struct Cost {
+        int tile;
+        double step, rest;
+    };
+    const Cost costs[] = {{256, 1.33, 14.0},
+                          {128, 0.5, 2.0},
+                          {64, pair ? 0.29 : 0.18, pair ? 1.0 : 0.6}};
+    Way best{64, 1, steps};
+    if (steps <= 0)
+        return best;
+    double least = 1e300;
+    for (const Cost& c : costs) {
+        const int64_t wide = pair && c.tile > 64 ? c.tile / 2 : c.tile;
+        const int64_t tiles = (m + c.tile - 1) / c.tile * ((n + wide - 1) / wide) * count;
+        for (int z = 1; z <= 64; ++z) {
+            const int slice = (steps + z - 1) / z, slices = (steps + slice - 1) / slice;
+            const double sums = double(slices) * double(m) * double(n) * double(count) * 4;
+            if (z > 1 && (pair || slice < 8 || slices != z || sums > 2.7e8))
+                continue;
+            const double most = double((tiles * slices + 255) / 256);
+            const double us =
+                most * (c.step * slice + c.rest) + (z > 1 ? 5.0 + 2.0 * sums / 4e6 : 0.0);
+            if (us < least) {
+                least = us;
+                best = Way{c.tile, slices, slice};
+            }
+        }
+    }
+    return best;
 }
 
 }  // namespace gated

@@ -182,7 +182,8 @@ template <bool F32, bool SAVE>
 struct ForwardWriter {
     const ForwardArgs& g;
     int64_t r0, c0;
-    __device__ inline void store(int row_, int col_, float (&u)[8], float (&v)[8])
+    __device__ inline int fetch(int) const { return 0; }
+    __device__ inline void store(int row_, int col_, float (&u)[8], float (&v)[8], int)
     {
         const int64_t row = r0 + row_, col = c0 + col_;
         if (row >= g.m || col >= g.n)
@@ -418,34 +419,9 @@ __global__ __launch_bounds__(256) void k_gated_join(ProductArgs g, int slices)
 // Dimensions and strides stay within the 32-bit offsets of a tile's loads: 256 rows of 2^23 bytes.
 constexpr int64_t kMost = int64_t(1) << 21;
 constexpr int64_t kMostGroups = int64_t(1) << 24;  // a grid counts threads in 32 bits
-constexpr int kLongSum = 96;  // steps: shorter sums are not cut
 
-struct Way {
-    int tile;    // 256, 128 or 64
-    int slices;  // of the sum
-    int slice;   // steps of each
-};
-
-// The largest tile that gives every CU a workgroup; few results of a long sum are cut into
-// slices.  `pair`: a tile's columns are two weights'.
-Way way_of(int64_t m, int64_t n, int count, int steps, bool pair)
-{
-    Way w{64, 1, steps};
-    int64_t tiles = 0;
-    for (const int t : {256, 128, 64}) {
-        w.tile = t;
-        const int64_t wide = pair && t > 64 ? t / 2 : t;
-        tiles = host::ceil_div(m, t) * host::ceil_div(n, wide) * count;
-        if (tiles >= 256)
-            return w;
-    }
-    if (pair || steps < kLongSum)
-        return w;
-    const int want = int(std::min<int64_t>(steps / 8, host::ceil_div(512, std::max<int64_t>(tiles, 1))));
-    w.slice = int(host::ceil_div(steps, std::max(want, 1)));
-    w.slices = int(host::ceil_div(steps, w.slice));
-    return w;
-}
+using gated::Way;
+using gated::way_of;
 
 bool valid_sizes(int64_t m, int64_t n, int64_t k)
 {

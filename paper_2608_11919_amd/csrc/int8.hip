@@ -185,15 +185,26 @@ struct ProductWriter {
     static constexpr int kSlots = 8;
     const ProductArgs& g;
     int64_t r0, c0;
-    __device__ inline void fetch(int, int, int) {}
-    __device__ inline void turn(int, int, const float (&)[8]) {}
-    __device__ inline void scales_at(const float* from, int64_t col, float (&s)[8]) const
+    float s[8], t[8];  // the lane's columns' scales, of either weight
+    float x[kSlots];   // rows'
+    __device__ inline void columns(int col_)
     {
+        const int64_t col = c0 + col_;
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            s[e] = from[col + e < g.n ? col + e : g.n - 1];
+        for (int e = 0; e < 8; ++e) {
+            const int64_t at = col + e < g.n ? col + e : g.n - 1;
+            s[e] = g.b_scales[at];
+            t[e] = g.c_scales ? g.c_scales[at] : 0.0f;
+        }
     }
-    __device__ inline void store(int row_, int col_, float (&v)[8], int)
+    __device__ inline float fetch(int row_) const
+    {
+        const int64_t row = r0 + row_;
+        return g.a_scales[row < g.m ? row : g.m - 1];
+    }
+    __device__ inline void fetch(int row, int, int p) { x[p] = fetch(row); }
+    __device__ inline void turn(int, int, const float (&)[8]) {}
+    __device__ inline void store(int row_, int col_, float (&v)[8], int p)
     {
         const int64_t row = r0 + row_, col = c0 + col_;
         if (row >= g.m || col >= g.n)
@@ -203,33 +214,27 @@ struct ProductWriter {
                             g.n - col);
             return;
         }
-        float s[8];
-        scales_at(g.b_scales, col, s);
-        const float x = g.a_scales[row];
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            v[e] = scaled(v[e], x, s[e]);
+            v[e] = scaled(v[e], x[p], s[e]);
         store_row<F32>(g.out, row * g.stride + col, v, g.n - col);
     }
     // of a pair
-    __device__ inline void store(int row_, int col_, float (&u)[8], float (&v)[8])
+    __device__ inline void store(int row_, int col_, float (&u)[8], float (&v)[8], float scale)
     {
         const int64_t row = r0 + row_, col = c0 + col_;
         if (row >= g.m || col >= g.n)
             return;
-        float s[8], t[8];
-        scales_at(g.b_scales, col, s);
-        scales_at(g.c_scales, col, t);
-        const float x = g.a_scales[row];
+        float a[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            u[e] = scaled(u[e], x, s[e]);
-            v[e] = scaled(v[e], x, t[e]);
+            u[e] = scaled(u[e], scale, s[e]);
+            v[e] = scaled(v[e], scale, t[e]);
         }
-        gated::activate(g.activation, u, s);
+        gated::activate(g.activation, u, a);
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            u[e] = s[e] * v[e];
+            u[e] = a[e] * v[e];
         store_row<F32>(g.out, row * g.stride + col, u, g.n - col);
     }
 };
@@ -493,34 +498,11 @@ __global__ __launch_bounds__(64 * kHeldWaves) void k_int8_held(HeldArgs g)
 constexpr int64_t kMostSummed = int64_t(1) << 17;  // 127^2 * 2^17 < 2^31
 constexpr int64_t kMostGroups = int64_t(1) << 24;  // a grid counts threads in 32 bits
 
-struct Way {
-    int tile;    // 256, 128 or 64
-    int slices;  // of the sum
-    int slice;   // steps of each
-};
-
-// As the products in 8-bit floating point: the largest tile that gives every CU a workgroup; few
-// results of a long sum are cut into slices.
-constexpr int kLongSum = 48;
+using gated::Way;
 
 Way way_of(int64_t m, int64_t n, int64_t k, bool pair)
 {
-    const int steps = int(host::ceil_div(k, kPitch));
-    Way w{64, 1, steps};
-    int64_t tiles = 0;
-    for (const int t : {256, 128, 64}) {
-        w.tile = t;
-        const int64_t wide = pair && t > 64 ? t / 2 : t;
-        tiles = host::ceil_div(m, t) * host::ceil_div(n, wide);
-        if (tiles >= 256)
-            return w;
-    }
-    if (steps < kLongSum || pair)
-        return w;
-    const int want = int(std::min<int64_t>(steps / 4, host::ceil_div(512, std::max<int64_t>(tiles, 1))));
-    w.slice = int(host::ceil_div(steps, std::max(want, 1)));
-    w.slices = int(host::ceil_div(steps, w.slice));
-    return w;
+    return gated::way_of(m, n, 1, int(host::ceil_div(k, kPitch)), pair);
 }
 
 bool valid_sizes(int64_t m, int64_t n, int64_t k)

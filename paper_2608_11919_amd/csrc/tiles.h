@@ -600,7 +600,18 @@ __device__ inline void product_pairs(Mul& mul, S& c, const void* P, int64_t pitc
 //   w.fetch(row, col, p)     requests what results [row][col .. col + 8) need, into slot p;
 //   w.store(row, col, v, p)  takes the sums v, leaves the results there and stores them;
 //   w.turn(col, row, v)      with kTurned: stores results [row .. row + 8)[col] of the transpose;
+//   w.columns(col)           where it has it: before all, the lane's columns [col .. col + 8).
 // Rows and columns count from the tile's origin.
+template <typename Writer>
+__device__ inline auto tell_columns(Writer& w, int col, int) -> decltype(w.columns(col))
+{
+    w.columns(col);
+}
+template <typename Writer>
+__device__ inline void tell_columns(Writer&, int, long)
+{
+}
+
 template <typename S, typename Writer>
 __device__ inline void finish(const S& c, uint8_t* lds, Writer& w)
 {
@@ -611,6 +622,7 @@ __device__ inline void finish(const S& c, uint8_t* lds, Writer& w)
     float* mine = reinterpret_cast<float*>(lds) + S::wave() * 32 * kPitch;
     const int lane = S::lane(), down = lane / kAcross, across = lane % kAcross * 8;
     const int r0 = S::wave_row(), c0 = S::wave_col();
+    tell_columns(w, c0 + across, 0);
 #pragma unroll
     for (int i = 0; i < S::I; ++i) {
 #pragma unroll
@@ -656,8 +668,10 @@ __device__ inline void finish(const S& c, uint8_t* lds, Writer& w)
     }
 }
 
-// The same for results of two matrices' rows in turns: w.store(row, col, u, v) takes eight
-// neighbouring columns of either result, which count in [0, kCols / 2).
+// The same for results of two matrices' rows in turns:
+//   w.fetch(row)               requests what a row's results need;
+//   w.store(row, col, u, v, f) takes eight neighbouring columns of either result, which count in
+//                              [0, kCols / 2), and what fetch gave.
 template <typename S, typename Writer>
 __device__ inline void finish_pairs(const S& c, uint8_t* lds, Writer& w)
 {
@@ -668,6 +682,8 @@ __device__ inline void finish_pairs(const S& c, uint8_t* lds, Writer& w)
     float* mine = reinterpret_cast<float*>(lds) + S::wave() * 32 * kPitch;
     const int lane = S::lane(), down = lane / kAcross, across = lane % kAcross * 8;
     const int r0 = S::wave_row(), c0 = S::wave_col() / 2;
+    tell_columns(w, c0 + across, 0);
+    auto next = w.fetch(r0 + down);
 #pragma unroll
     for (int i = 0; i < S::I; ++i) {
 #pragma unroll
@@ -689,7 +705,10 @@ __device__ inline void finish_pairs(const S& c, uint8_t* lds, Writer& w)
                 u[e] = at[e];
                 v[e] = at[32 + e];
             }
-            w.store(r0 + 32 * i + p * kDown + down, c0 + across, u, v);
+            const auto now = next;  // rows follow each other, also from block to block
+            const int row = r0 + 32 * i + p * kDown + down;
+            next = w.fetch(row + kDown);
+            w.store(row, c0 + across, u, v, now);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }

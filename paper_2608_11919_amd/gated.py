@@ -15,23 +15,28 @@ from .lazytrain import _capturing, _check, _current, _stream_handle, lib
 
 def _weights(gate: torch.Tensor, up: torch.Tensor, device):
     """The weights as the library takes them, and their row strides."""
-    laid = []
-    for w, what in ((gate, "gate"), (up, "up")):
-        if w.dim() != 2 or w.shape != gate.shape:
-            raise ValueError(f"gate and up must be matrices of one shape, got "
-                             f"{tuple(gate.shape)} and {tuple(up.shape)}")
-        if w.dtype != torch.bfloat16:
-            raise TypeError(f"{what} must be bfloat16, got {w.dtype}")
-        if w.device != device:
-            raise ValueError(f"{what} is on {w.device}, not on {device}")
-        w = _laid_out(w)
-        laid += [w, _rows(w, what)]
-    return laid
+    if gate.dim() != 2 or up.shape != gate.shape:
+        raise ValueError(f"gate and up must be matrices of one shape, got {tuple(gate.shape)} and "
+                         f"{tuple(up.shape)}")
+    return (*_weight(gate, "gate", device), *_weight(up, "up", device))
+
+
+def _weight(w: torch.Tensor, what: str, device):
+    if w.dtype != torch.bfloat16:
+        raise TypeError(f"{what} must be bfloat16, got {w.dtype}")
+    if w.device != device:
+        raise ValueError(f"{what} is on {w.device}, not on {device}")
+    if w.is_contiguous() and not w.data_ptr() % 16:
+        return w, w.shape[1]
+    w = _laid_out(w)
+    return w, _rows(w, what)
 
 
 def _input(x: torch.Tensor, features: int) -> Tuple[torch.Tensor, int]:
     if x.dtype != torch.bfloat16:
         raise TypeError(f"x must be bfloat16, got {x.dtype}")
+    if x.dim() == 2 and x.shape[1] == features and x.is_contiguous() and not x.data_ptr() % 16:
+        return x, features
     t = _tokens(x, features, "x")
     return t, _rows(t, "x")
 

@@ -206,6 +206,12 @@ def test_sizes_of_memory():
     assert L.lt_int8_linear_workspace_bytes(16, 4, 2049) > 16 * 2049
     assert L.lt_int8_linear_workspace_bytes(1, 4, 8193) > 8193
     assert L.lt_int8_gated_workspace_bytes(-1, 4, 300) == 0
+    for m, n, k in ((40, 0, 500), (0, 40, 500), (40, 40, 0), (0, 0, 0)):
+        assert L.lt_int8_matmul_workspace_bytes(m, n, k) == 256
+        assert L.lt_int8_linear_workspace_bytes(m, n, k) >= 256
+        assert L.lt_int8_gated_workspace_bytes(m, n, k) >= 256
+        assert L.lt_gated_forward_workspace_bytes(m, n, k, 9, 9, 9) >= 256
+        assert L.lt_gated_backward_workspace_bytes(m, n, k, 1, 1) >= 256
     assert L.lt_gated_saved_bytes(3, 9) == 6 * 3 * 16
     assert L.lt_gated_saved_bytes(3, 1 << 21) == 0
     assert L.lt_gated_forward_workspace_bytes(64, 64, 64, 64, 64, 64) == 256
