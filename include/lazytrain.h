@@ -695,7 +695,7 @@ size_t lt_gated_forward_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t
  * activation are fp32, out is rounded once to out_dtype.
  *   saved   NULL, or lt_gated_saved_bytes(m, n) bytes for lt_gated_backward: u act'(g) and act(g),
  *           24 bits each (a relative 2^-17).
- * k = 0 gives zeros.  m, n, k < 2^21, fewer than 2^23 tiles of 64 x 64 in each matrix.  x, the
+ * k = 0 gives zeros.  m, n, k < 2^21, fewer than 2^22 tiles of 64 x 64 in each matrix.  x, the
  * weights, out and saved 16-byte aligned; what is written overlaps nothing else.
  */
 lt_err lt_gated_forward(const void* x, int64_t x_stride, const void* gate, int64_t gate_stride,

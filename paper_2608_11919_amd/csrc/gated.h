@@ -323,10 +323,11 @@ inline Way way_of(int64_t m, int64_t n, int64_t count, int steps, bool pair)
     for (const Cost& c : costs) {
         const int64_t wide = pair && c.tile > 64 ? c.tile / 2 : c.tile;
         const int64_t tiles = (m + c.tile - 1) / c.tile * ((n + wide - 1) / wide) * count;
-        for (int z = 1; z <= 64; ++z) {
+        const int most_slices = pair ? 1 : std::min(64, std::max(1, steps / 8));
+        for (int z = 1; z <= most_slices; ++z) {
             const int slice = (steps + z - 1) / z, slices = (steps + slice - 1) / slice;
             const double sums = double(slices) * double(m) * double(n) * double(count) * 4;
-            if (z > 1 && (pair || slice < 8 || slices != z || sums > 2.7e8))
+            if (z > 1 && (slice < 8 || slices != z || sums > 2.7e8))
                 continue;
             const double most = double((tiles * slices + 255) / 256);
             const double us =

@@ -28,20 +28,39 @@ int64_t padded(int64_t values) { return host::ceil_div(values, kStep) * kStep; }
 
 // ------------------------------------------------------------- layouts
 
-// A matrix of bf16 with rows of whole steps, zeros behind their ends: what the products read
-// where a row as it is has another length or place.
-struct PackArgs {
+// Up to three matrices of bf16 as the products read them, in one launch: rows of whole steps, zeros
+// behind their ends, where a row as it is has another length or place.
+struct Layout {
     const uint16_t* x;
     int64_t rows, cols, stride;
     uint16_t* out;
     int64_t pitch;
+    uint32_t first;  // workgroup of the launch
 };
 
-__global__ __launch_bounds__(256) void k_gated_pack(PackArgs a)
+struct Layouts {
+    Layout of[3];
+    int count;
+    // the one that workgroup `group` works at, the last whose first it has reached
+    __device__ inline const Layout& at(uint32_t group) const
+    {
+        const int i = count > 2 && group >= of[2].first ? 2
+                                                        : count > 1 && group >= of[1].first ? 1 : 0;
+        return of[i];
+    }
+};
+
+constexpr int64_t kPackLines = 256 * 4;  // of 16 bytes, to a workgroup
+
+__global__ __launch_bounds__(256) void k_gated_pack(Layouts g)
 {
+    const Layout& a = g.at(blockIdx.x);
     const int64_t lines = a.pitch / 8, all = a.rows * lines;
-    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < all;
-         i += int64_t(gridDim.x) * 256) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int64_t i = (int64_t(blockIdx.x) - a.first) * kPackLines + j * 256 + threadIdx.x;
+        if (i >= all)
+            return;
         const int64_t row = i / lines, col = i % lines * 8;
         const uint16_t* p = a.x + row * a.stride + col;
         i32x4 v;
@@ -58,14 +77,14 @@ __global__ __launch_bounds__(256) void k_gated_pack(PackArgs a)
     }
 }
 
+constexpr int kTurnPitch = 64 + 2;
+
 // The transpose: out[c][r] = x[r][c], zeros for r from rows up to whole steps.  64 x 64 a
 // workgroup, through LDS.
-__global__ __launch_bounds__(256) void k_gated_turn(PackArgs a)
+__device__ inline void turn(const Layout& a, int64_t group, uint16_t* block)
 {
-    constexpr int kTurnPitch = 64 + 2;
-    __shared__ uint16_t block[64 * kTurnPitch];
     const int64_t down = (a.rows + 63) / 64;
-    const int64_t r0 = int64_t(blockIdx.x) % down * 64, c0 = int64_t(blockIdx.x) / down * 64;
+    const int64_t r0 = group % down * 64, c0 = group / down * 64;
     const int line = int(threadIdx.x) / 8, at = int(threadIdx.x) % 8 * 8;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -241,14 +260,19 @@ struct SlopeArgs {
     int64_t half;
     uint16_t* turned;   // [2 n][turned_pitch], or null
     int64_t turned_pitch;
+    Layouts turn;       // what the products need turned besides, by the workgroups behind
 };
 
 // 64 tokens x 64 channels to a workgroup.  Bound by HBM: 8 bytes read and 4 to 8 written a value.
 template <bool F32>
 __global__ __launch_bounds__(256) void k_gated_slopes(SlopeArgs g)
 {
-    constexpr int kTurnPitch = 64 + 2;
     __shared__ uint16_t block[2][64 * kTurnPitch];
+    if (g.turn.count > 0 && blockIdx.x >= g.turn.of[0].first) {
+        const Layout& a = g.turn.at(blockIdx.x);
+        turn(a, int64_t(blockIdx.x) - a.first, block[0]);
+        return;
+    }
     const int64_t across = g.half / 64;
     const int64_t r0 = int64_t(blockIdx.x) / across * 64, c0 = int64_t(blockIdx.x) % across * 64;
     const int line = int(threadIdx.x) / 8, at = int(threadIdx.x) % 8 * 8;
@@ -426,7 +450,7 @@ using gated::way_of;
 bool valid_sizes(int64_t m, int64_t n, int64_t k)
 {
     const auto tiles = [](int64_t a, int64_t b) {
-        return host::ceil_div(a, 64) * host::ceil_div(b, 64) * 2 < kMostGroups;
+        return host::ceil_div(a, 64) * host::ceil_div(b, 64) < kMostGroups / 4;
     };
     return m >= 0 && n >= 0 && k >= 0 && m < kMost && n < kMost && k < kMost && tiles(m, n) &&
            tiles(m, k) && tiles(n, k);
@@ -511,21 +535,18 @@ BackwardLayout backward_layout(int64_t m, int64_t n, int64_t k, bool dx, bool dw
 
 uint32_t groups_for(int64_t work) { return uint32_t(std::min<int64_t>(host::ceil_div(work, 256), 8192)); }
 
-void launch_pack(const void* x, int64_t rows, int64_t cols, int64_t stride, uint8_t* out,
-                 hipStream_t st)
+// Adds a matrix to a launch of `groups` workgroups so far.
+void add(Layouts& to, int64_t& groups, const void* x, int64_t rows, int64_t cols, int64_t stride,
+         uint8_t* out, int64_t pitch, int64_t its_groups)
 {
-    const PackArgs a{static_cast<const uint16_t*>(x), rows, cols, stride,
-                     reinterpret_cast<uint16_t*>(out), padded(cols)};
-    k_gated_pack<<<dim3(groups_for(rows * a.pitch / 8)), 256, 0, st>>>(a);
-}
-
-void launch_turn(const void* x, int64_t rows, int64_t cols, int64_t stride, uint8_t* out,
-                 int64_t pitch, hipStream_t st)
-{
-    const PackArgs a{static_cast<const uint16_t*>(x), rows, cols, stride,
-                     reinterpret_cast<uint16_t*>(out), pitch};
-    k_gated_turn<<<dim3(uint32_t(host::ceil_div(rows, 64) * host::ceil_div(cols, 64))), 256, 0,
-                   st>>>(a);
+    to.of[to.count++] = Layout{static_cast<const uint16_t*>(x),
+                               rows,
+                               cols,
+                               stride,
+                               reinterpret_cast<uint16_t*>(out),
+                               pitch,
+                               uint32_t(groups)};
+    groups += its_groups;
 }
 
 template <typename Tile>
@@ -618,7 +639,7 @@ try {
     host::clear_error();
     if (!valid_sizes(m, n, k) || !valid_stride(m, n, out_stride) || !valid_stride(m, k, x_stride) ||
         !valid_stride(n, k, gate_stride) || !valid_stride(n, k, up_stride))
-        return fail(LT_ERR_INVALID_ARG, "need 0 <= m, n, k < 2^21, fewer than 2^23 tiles of 64 x 64 "
+        return fail(LT_ERR_INVALID_ARG, "need 0 <= m, n, k < 2^21, fewer than 2^22 tiles of 64 x 64 "
                                         "in each matrix, and strides of a row's length or more");
     if (!valid_dtype(out_dtype))
         return fail(LT_ERR_INVALID_ARG, "out_dtype must be LT_DTYPE_F32 or LT_DTYPE_BF16");
@@ -692,19 +713,24 @@ try {
     g.stride = out_stride;
     if (saved)
         g.saved = saved_layout(saved, m, n);
+    Layouts pack{};
+    int64_t groups = 0;
     const auto operand = [&](const void* p, int64_t rows, int64_t stride, int64_t at,
                              const uint8_t** from, int64_t* pitch) {
         *from = static_cast<const uint8_t*>(p);
         *pitch = stride * 2;
         if (at < 0)
             return;
-        launch_pack(p, rows, k, stride, ws + at, st);
+        add(pack, groups, p, rows, k, stride, ws + at, padded(k),
+            host::ceil_div(rows * (padded(k) / 8), kPackLines));
         *from = ws + at;
         *pitch = padded(k) * 2;
     };
     operand(x, m, x_stride, l.x, &g.x, &g.x_pitch);
     operand(gate, n, gate_stride, l.gate, &g.gate, &g.gate_pitch);
     operand(up, n, up_stride, l.up, &g.up, &g.up_pitch);
+    if (pack.count > 0)
+        k_gated_pack<<<dim3(uint32_t(groups)), 256, 0, st>>>(pack);
     const Way w = way_of(m, n, 1, g.steps, true);
     if (w.tile == 256)
         launch_forward<Large16>(g, f32, saved != nullptr, st);
@@ -739,7 +765,7 @@ try {
                      !valid_stride(n, k, dup_stride))) ||
         (dx && (!valid_stride(n, k, gate_stride) || !valid_stride(n, k, up_stride) ||
                 !valid_stride(m, k, dx_stride))))
-        return fail(LT_ERR_INVALID_ARG, "need 0 <= m, n, k < 2^21, fewer than 2^23 tiles of 64 x 64 "
+        return fail(LT_ERR_INVALID_ARG, "need 0 <= m, n, k < 2^21, fewer than 2^22 tiles of 64 x 64 "
                                         "in each matrix, and strides of a row's length or more");
     if (!valid_dtype(dh_dtype) || !valid_dtype(dx_dtype) || !valid_dtype(grad_dtype))
         return fail(LT_ERR_INVALID_ARG, "dtypes must be LT_DTYPE_F32 or LT_DTYPE_BF16");
@@ -799,6 +825,19 @@ try {
         return e;
     const BackwardLayout l = backward_layout(m, n, k, dx != nullptr, want_dw);
     const int64_t half = padded(n), tokens = padded(m);
+    Layouts turn{};
+    int64_t groups = half / 64 * (tokens / 64);
+    const auto turned = [&](const void* p, int64_t rows, int64_t stride, int64_t at,
+                            int64_t pitch) {
+        add(turn, groups, p, rows, k, stride, ws + at, pitch,
+            host::ceil_div(rows, 64) * host::ceil_div(k, 64));
+    };
+    if (dx) {
+        turned(gate, n, gate_stride, l.w, 2 * half);
+        turned(up, n, up_stride, l.w + half * 2, 2 * half);
+    }
+    if (want_dw)
+        turned(x, m, x_stride, l.x, tokens);
     const SlopeArgs s{dh,
                       dh_stride,
                       saved_layout(const_cast<void*>(saved), m, n),
@@ -807,16 +846,15 @@ try {
                       dx ? reinterpret_cast<uint16_t*>(ws + l.by_rows) : nullptr,
                       half,
                       want_dw ? reinterpret_cast<uint16_t*>(ws + l.turned) : nullptr,
-                      tokens};
-    const dim3 blocks(uint32_t(half / 64 * (tokens / 64)));
+                      tokens,
+                      turn};
+    const dim3 blocks{uint32_t(groups)};
     if (dh_dtype == LT_DTYPE_F32)
         k_gated_slopes<true><<<blocks, 256, 0, st>>>(s);
     else
         k_gated_slopes<false><<<blocks, 256, 0, st>>>(s);
     uint8_t* partial = l.partial < 0 ? nullptr : ws + l.partial;
     if (dx) {
-        launch_turn(gate, n, k, gate_stride, ws + l.w, 2 * half, st);
-        launch_turn(up, n, k, up_stride, ws + l.w + half * 2, 2 * half, st);
         ProductArgs g{};
         g.a = ws + l.by_rows;
         g.b = ws + l.w;
@@ -830,7 +868,6 @@ try {
         run_product(g, dx_dtype == LT_DTYPE_F32, partial, st);
     }
     if (want_dw) {
-        launch_turn(x, m, k, x_stride, ws + l.x, tokens, st);
         ProductArgs g{};
         g.a = ws + l.turned;
         g.b = ws + l.x;

@@ -51,7 +51,7 @@ def _forward(x, gate, up, activation, out_dtype, keep, workspace):
     out = _dtype_code(h, "out")
     saved = None
     if keep:
-        saved = torch.empty(int(lib().lt_gated_saved_bytes(m, n)), dtype=torch.uint8, device=device)
+        saved = torch.empty(6 * m * (-(-n // 8) * 8), dtype=torch.uint8, device=device)
     ws, nbytes, handle = 0, 0, _stream_handle(None, device)
     if (keep or m > 16) and (k % 64 or (x_stride | g_stride | u_stride) % 8) or \
             workspace is not None:
@@ -95,44 +95,49 @@ def _backward(dh, saved, x, gate, up, leading, shape, out_dtype, grad_dtype, wan
     """dx needs the weights, the weights' gradients x; what is not needed may be None."""
     n, k = shape
     device = dh.device
-    d = _tokens(dh, n, "dh", aligned=False)
+    d_code = _dtype_code(dh, "dh")
+    if dh.dim() == 2 and dh.shape[1] == n and dh.is_contiguous():
+        d, d_stride = dh, n
+    else:
+        d = _tokens(dh, n, "dh", aligned=False)
+        d_stride = _rows(d, "dh")
     m = d.shape[0]
-    d_stride, d_code = _rows(d, "dh"), _dtype_code(d, "dh")
     if tuple(dh.shape[:-1]) != leading:
         raise ValueError(f"dh must have shape {leading + (n,)}, got {tuple(dh.shape)}")
     if (saved.device != device or saved.dtype != torch.uint8 or not saved.is_contiguous() or
-            saved.numel() != int(lib().lt_gated_saved_bytes(m, n))):
+            saved.numel() != 6 * m * (-(-n // 8) * 8)):
         raise ValueError("saved must be what gated_linear_forward kept of these tokens")
-    x_at, x_stride, g_at, g_stride, u_at, u_stride = 0, k, 0, k, 0, k
+    x_at = g_at = u_at = dx_at = dgate_at = dup_at = dx_code = grad_code = 0
+    x_stride = g_stride = u_stride = k
     dx = dgate = dup = None
     if want_dx:
         g, g_stride, u, u_stride = _weights(gate, up, device)
-        g_at, u_at = g.data_ptr(), u.data_ptr()
         dx = torch.empty(m, k, dtype=out_dtype, device=device)
-        _dtype_code(dx, "dx")
+        dx_code = _dtype_code(dx, "dx")
+        g_at, u_at, dx_at = g.data_ptr(), u.data_ptr(), dx.data_ptr()
     if want_dw:
         if x.device != device:
             raise ValueError(f"x is on {x.device}, dh on {device}")
         t, x_stride = _input(x, k)
         if t.shape[0] != m:
             raise ValueError(f"x has {t.shape[0]} tokens, dh {m}")
-        x_at = t.data_ptr()
         dgate = torch.empty(n, k, dtype=grad_dtype, device=device)
         dup = torch.empty(n, k, dtype=grad_dtype, device=device)
-        _dtype_code(dgate, "the weights' gradients")
+        grad_code = _dtype_code(dgate, "the weights' gradients")
+        x_at, dgate_at, dup_at = t.data_ptr(), dgate.data_ptr(), dup.data_ptr()
     if not want_dx and not want_dw:
         return None, None, None
     handle = _stream_handle(None, device)
-    need = int(lib().lt_gated_backward_workspace_bytes(m, n, k, want_dx, want_dw))
+    need = lib().lt_gated_backward_workspace_bytes(m, n, k, want_dx, want_dw)
     held, ws, nbytes = _scratch(device, need, None, None)
-    at = lambda t: 0 if t is None else t.data_ptr()
-    code = lambda t: 0 if t is None else _dtype_code(t, "a gradient")
     with _current(device):
         _check(lib().lt_gated_backward(d.data_ptr(), d_code, d_stride, saved.data_ptr(), x_at,
-                                       x_stride, g_at, g_stride, u_at, u_stride, m, n, k, at(dx),
-                                       code(dx), k, at(dgate), k, at(dup), k, code(dgate), ws,
-                                       nbytes, handle))
-    return None if dx is None else dx.view(*leading, k), dgate, dup
+                                       x_stride, g_at, g_stride, u_at, u_stride, m, n, k, dx_at,
+                                       dx_code, k, dgate_at, k, dup_at, k, grad_code, ws, nbytes,
+                                       handle))
+    if dx is not None and len(leading) != 1:
+        dx = dx.view(*leading, k)
+    return dx, dgate, dup
 
 
 _MADE_ON = "lazytrain_stream"
