@@ -703,9 +703,11 @@ lt_err lt_gated_forward(const void* x, int64_t x_stride, const void* gate, int64
                         int64_t k, void* out, int out_dtype, int64_t out_stride, void* saved,
                         void* workspace, size_t workspace_bytes, void* stream);
 
-/* Bytes of device workspace lt_gated_backward needs for the gradients that are asked for; 0 if an
- * argument is invalid. */
-size_t lt_gated_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int dx, int dw);
+/* Bytes of device workspace lt_gated_backward needs for the gradients that are asked for: dg and
+ * du, and copies of what is not whole steps of 64 rows (the last rows; x or the weights where k or
+ * a stride is no multiple of 8).  0 if an argument is invalid. */
+size_t lt_gated_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t x_stride,
+                                         int64_t gate_stride, int64_t up_stride, int dx, int dw);
 
 /*
  * f14: the gradients of f13 from dh, out's (m x n, dh_dtype):
@@ -714,8 +716,8 @@ size_t lt_gated_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int dx
  * dg and du are rounded to bf16 for the products, whose sums are fp32's; dx is rounded to dx_dtype,
  * the weights' gradients to grad_dtype.  dx may be NULL, and so may dgate and dup together: what only
  * they need (the weights; x) is not looked at then.  saved is lt_gated_forward's.  Empty sums give
- * zeros.  saved and the gradients 16-byte aligned, the rest to its elements; what is written overlaps
- * nothing else.
+ * zeros.  x, the weights, saved and the gradients 16-byte aligned, dh to its elements; what is
+ * written overlaps nothing else.
  */
 lt_err lt_gated_backward(const void* dh, int dh_dtype, int64_t dh_stride, const void* saved,
                          const void* x, int64_t x_stride, const void* gate, int64_t gate_stride,

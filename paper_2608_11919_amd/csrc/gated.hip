@@ -28,67 +28,36 @@ int64_t padded(int64_t values) { return host::ceil_div(values, kStep) * kStep; }
 
 // ------------------------------------------------------------- layouts
 
-// Up to three matrices of bf16 as the products read them, in one launch: rows of whole steps, zeros
-// behind their ends, where a row as it is has another length or place.
+// Up to three matrices of bf16 as the products read them, in one launch: rows of whole steps, or
+// whole steps of rows, with zeros behind, where a matrix as it is has other sizes or places.
 struct Layout {
     const uint16_t* x;
     int64_t rows, cols, stride;
     uint16_t* out;
-    int64_t pitch;
+    int64_t out_rows, pitch;
     uint32_t first;  // workgroup of the launch
 };
 
 struct Layouts {
     Layout of[3];
     int count;
-    // the one that workgroup `group` works at, the last whose first it has reached
-    __device__ inline const Layout& at(uint32_t group) const
-    {
-        const int i = count > 2 && group >= of[2].first ? 2
-                                                        : count > 1 && group >= of[1].first ? 1 : 0;
-        return of[i];
-    }
 };
 
 constexpr int64_t kPackLines = 256 * 4;  // of 16 bytes, to a workgroup
 
 __global__ __launch_bounds__(256) void k_gated_pack(Layouts g)
 {
-    const Layout& a = g.at(blockIdx.x);
-    const int64_t lines = a.pitch / 8, all = a.rows * lines;
+    const uint32_t group = blockIdx.x;
+    const Layout& a = g.of[g.count > 2 && group >= g.of[2].first
+                               ? 2
+                               : g.count > 1 && group >= g.of[1].first ? 1 : 0];
+    const int64_t lines = a.pitch / 8, all = a.out_rows * lines;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const int64_t i = (int64_t(blockIdx.x) - a.first) * kPackLines + j * 256 + threadIdx.x;
+        const int64_t i = (int64_t(group) - a.first) * kPackLines + j * 256 + threadIdx.x;
         if (i >= all)
             return;
         const int64_t row = i / lines, col = i % lines * 8;
-        const uint16_t* p = a.x + row * a.stride + col;
-        i32x4 v;
-        if (col + 8 <= a.cols) {
-            v = load_any(p);
-        } else {
-            u16x8 b;
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                b[e] = col + e < a.cols ? p[e] : uint16_t(0);
-            v = __builtin_bit_cast(i32x4, b);
-        }
-        *reinterpret_cast<i32x4*>(a.out + row * a.pitch + col) = v;
-    }
-}
-
-constexpr int kTurnPitch = 64 + 2;
-
-// The transpose: out[c][r] = x[r][c], zeros for r from rows up to whole steps.  64 x 64 a
-// workgroup, through LDS.
-__device__ inline void turn(const Layout& a, int64_t group, uint16_t* block)
-{
-    const int64_t down = (a.rows + 63) / 64;
-    const int64_t r0 = group % down * 64, c0 = group / down * 64;
-    const int line = int(threadIdx.x) / 8, at = int(threadIdx.x) % 8 * 8;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int64_t row = r0 + line + 32 * h, col = c0 + at;
         const uint16_t* p = a.x + row * a.stride + col;
         u16x8 v = {};
         if (row < a.rows && col + 8 <= a.cols) {
@@ -98,21 +67,7 @@ __device__ inline void turn(const Layout& a, int64_t group, uint16_t* block)
             for (int e = 0; e < 8; ++e)
                 v[e] = col + e < a.cols ? p[e] : uint16_t(0);
         }
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            block[(at + e) * kTurnPitch + line + 32 * h] = v[e];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int64_t col = c0 + line + 32 * h;
-        if (col >= a.cols)
-            continue;
-        u16x8 v;
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            v[e] = block[(line + 32 * h) * kTurnPitch + at + e];
-        *reinterpret_cast<i32x4*>(a.out + col * a.pitch + r0 + at) = __builtin_bit_cast(i32x4, v);
+        *reinterpret_cast<i32x4*>(a.out + row * a.pitch + col) = __builtin_bit_cast(i32x4, v);
     }
 }
 
@@ -248,119 +203,84 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_gated_f
 
 // ------------------------------------------------------------- the backward pass
 
-// dg and du as the products read them: by rows next to each other, dg in the first
-// padded(n) columns (their sum with both weights is one product), and of the transpose, dg's n
-// rows before du's.
+// dg and du as the products read them, next to each other in rows of 2 * half values: zeros in
+// columns from n up to half, and in rows from m up to whole steps.
 struct SlopeArgs {
     const void* dh;
     int64_t stride;
     Saved saved;
     int64_t m, n;
-    uint16_t* by_rows;  // [m][2 * half], or null
-    int64_t half;
-    uint16_t* turned;   // [2 n][turned_pitch], or null
-    int64_t turned_pitch;
-    Layouts turn;       // what the products need turned besides, by the workgroups behind
+    uint16_t* out;
+    int64_t half, rows;
 };
 
-// 64 tokens x 64 channels to a workgroup.  Bound by HBM: 8 bytes read and 4 to 8 written a value.
+// Eight channels of a token to a lane.  Bound by HBM: 8 bytes read and 4 written a value.
 template <bool F32>
 __global__ __launch_bounds__(256) void k_gated_slopes(SlopeArgs g)
 {
-    __shared__ uint16_t block[2][64 * kTurnPitch];
-    if (g.turn.count > 0 && blockIdx.x >= g.turn.of[0].first) {
-        const Layout& a = g.turn.at(blockIdx.x);
-        turn(a, int64_t(blockIdx.x) - a.first, block[0]);
+    const int64_t lines = g.half / 8, all = g.rows * lines;
+    const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
+    if (i >= all)
         return;
-    }
-    const int64_t across = g.half / 64;
-    const int64_t r0 = int64_t(blockIdx.x) / across * 64, c0 = int64_t(blockIdx.x) % across * 64;
-    const int line = int(threadIdx.x) / 8, at = int(threadIdx.x) % 8 * 8;
+    const int64_t row = i / lines, col = i % lines * 8;
+    u16x8 dg = {}, du = {};
+    if (row < g.m && col < g.n) {
+        float a[8], b[8], d[8];
+        load_eight(g.saved.a_high, g.saved.a_low, row * g.saved.pitch + col, a);
+        load_eight(g.saved.b_high, g.saved.b_low, row * g.saved.pitch + col, b);
+        const int64_t from = row * g.stride + col;
+        if (col + 8 <= g.n) {
+            if constexpr (F32) {
+                const auto* p = static_cast<const float*>(g.dh) + from;
+                const f32x4 lo = __builtin_bit_cast(f32x4, load_any(p));
+                const f32x4 hi = __builtin_bit_cast(f32x4, load_any(p + 4));
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int64_t row = r0 + line + 32 * h, col = c0 + at;
-        u16x8 dg = {}, du = {};
-        if (row < g.m && col < g.n) {
-            float a[8], b[8], d[8];
-            load_eight(g.saved.a_high, g.saved.a_low, row * g.saved.pitch + col, a);
-            load_eight(g.saved.b_high, g.saved.b_low, row * g.saved.pitch + col, b);
-            const int64_t from = row * g.stride + col;
-            if (col + 8 <= g.n) {
-                if constexpr (F32) {
-                    const auto* p = static_cast<const float*>(g.dh) + from;
-                    const f32x4 lo = __builtin_bit_cast(f32x4, load_any(p));
-                    const f32x4 hi = __builtin_bit_cast(f32x4, load_any(p + 4));
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        d[e] = lo[e];
-                        d[4 + e] = hi[e];
-                    }
-                } else {
-                    const i32x4 w = load_any(static_cast<const uint16_t*>(g.dh) + from);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        d[2 * e] = __uint_as_float(uint32_t(w[e]) << 16);
-                        d[2 * e + 1] = __uint_as_float(uint32_t(w[e]) & 0xFFFF0000u);
-                    }
+                for (int e = 0; e < 4; ++e) {
+                    d[e] = lo[e];
+                    d[4 + e] = hi[e];
                 }
             } else {
+                const i32x4 w = load_any(static_cast<const uint16_t*>(g.dh) + from);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    d[e] = 0.0f;
-                    if (col + e < g.n) {
-                        if constexpr (F32)
-                            d[e] = static_cast<const float*>(g.dh)[from + e];
-                        else
-                            d[e] = __uint_as_float(
-                                uint32_t(static_cast<const uint16_t*>(g.dh)[from + e]) << 16);
-                    }
+                for (int e = 0; e < 4; ++e) {
+                    d[2 * e] = __uint_as_float(uint32_t(w[e]) << 16);
+                    d[2 * e + 1] = __uint_as_float(uint32_t(w[e]) & 0xFFFF0000u);
                 }
             }
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (col + e < g.n) {  // what is kept behind a row's end is anything
-                    dg[e] = gated::bf16_bits(d[e] * a[e]);
-                    du[e] = gated::bf16_bits(d[e] * b[e]);
-                }
-        }
-        if (g.by_rows && row < g.m) {
-            uint16_t* to = g.by_rows + row * 2 * g.half + col;
-            *reinterpret_cast<i32x4*>(to) = __builtin_bit_cast(i32x4, dg);
-            *reinterpret_cast<i32x4*>(to + g.half) = __builtin_bit_cast(i32x4, du);
-        }
-        if (g.turned) {
+        } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                block[0][(at + e) * kTurnPitch + line + 32 * h] = dg[e];
-                block[1][(at + e) * kTurnPitch + line + 32 * h] = du[e];
+                d[e] = 0.0f;
+                if (col + e < g.n) {
+                    if constexpr (F32)
+                        d[e] = static_cast<const float*>(g.dh)[from + e];
+                    else
+                        d[e] = __uint_as_float(
+                            uint32_t(static_cast<const uint16_t*>(g.dh)[from + e]) << 16);
+                }
             }
         }
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (col + e < g.n) {  // what is kept behind a row's end is anything
+                dg[e] = gated::bf16_bits(d[e] * a[e]);
+                du[e] = gated::bf16_bits(d[e] * b[e]);
+            }
     }
-    if (!g.turned)
-        return;
-    __syncthreads();
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int64_t col = c0 + line + 32 * h;
-            if (col >= g.n)
-                continue;
-            u16x8 v;
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                v[e] = block[b][(line + 32 * h) * kTurnPitch + at + e];
-            *reinterpret_cast<i32x4*>(g.turned + (b * g.n + col) * g.turned_pitch + r0 + at) =
-                __builtin_bit_cast(i32x4, v);
-        }
+    uint16_t* to = g.out + row * 2 * g.half + col;
+    *reinterpret_cast<i32x4*>(to) = __builtin_bit_cast(i32x4, dg);
+    *reinterpret_cast<i32x4*>(to + g.half) = __builtin_bit_cast(i32x4, du);
 }
 
-// out[i] = A_i B^T for one or two matrices A_i of m rows each, one behind the other.
+// dx = [dg | du] [gate; up], or (DW) dgate = dg^T x and dup = du^T x.  No operand is turned in
+// memory: what has the summed index as rows is turned on its way out of LDS.
 struct ProductArgs {
-    const uint8_t *a, *b;
-    int64_t a_pitch, b_pitch;  // bytes
-    int64_t m, n;
-    int count;
+    const uint8_t* a;    // dg and du by rows
+    int64_t a_pitch;     // bytes
+    TurnedSource b;      // the weights, or x
+    int64_t b_cols;      // a multiple of 8
+    int64_t m, n;        // of one result
+    int count;           // results
     int steps, slice;
     void* out[2];
     int64_t stride[2];
@@ -382,7 +302,7 @@ struct ProductWriter {
     }
 };
 
-template <typename Tile, bool F32>
+template <typename Tile, bool F32, bool DW>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_gated_product(ProductArgs g)
 {
     __shared__ __align__(1024) uint8_t lds[Tile::kLdsBytes];
@@ -393,11 +313,36 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_gated_p
     const TilePlace at = tile_place(int(unit - int64_t(which) * down * across), down, across);
     const int64_t r0 = int64_t(at.row) * Tile::kRows, c0 = int64_t(at.col) * Tile::kCols;
     const int first = int(blockIdx.y) * g.slice, steps = min(g.slice, g.steps - first);
-    const int64_t k0 = int64_t(first) * kStepBytes;
     Tile tile;
     Bf16<Tile::kPinned> mul;
-    product(mul, tile, g.a + (which * g.m + r0) * g.a_pitch + k0, g.a_pitch, g.m - r0,
-            g.b + c0 * g.b_pitch + k0, g.b_pitch, g.n - c0, steps, lds);
+    TurnedOperand<Tile, Tile::kCols, Tile::J> q;
+    q.src = g.b;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        q.src.base[i] += c0 * 2;
+        q.src.tail[i] += c0 * 2;
+    }
+    q.first = first;
+    q.steps = steps;
+    q.init(g.b_cols - c0);
+    if constexpr (DW) {
+        const int64_t half = g.a_pitch / 4;  // columns of either
+        TurnedOperand<Tile, Tile::kRows, Tile::I> p;
+        p.src.base[0] = p.src.base[1] = g.a + (which * half + r0) * 2;
+        p.src.tail[0] = p.src.tail[1] = p.src.base[0];
+        p.src.pitch = g.a_pitch;
+        p.src.each = p.src.full = g.steps;
+        p.first = first;
+        p.steps = steps;
+        p.init(half - r0);
+        product(mul, tile, p, q, steps, lds);
+    } else {
+        RowOperand<Tile, Tile::kRows, Tile::I, TileLoad<Tile::kRows, Tile::kThreads, true>> p;
+        p.src = g.a + r0 * g.a_pitch + int64_t(first) * kStepBytes;
+        p.steps = steps;
+        p.load.init(g.a_pitch, g.m - r0);
+        product(mul, tile, p, q, steps, lds);
+    }
     if (g.partial) {
         ProductWriter<true> p;
         p.rows = g.m - r0;
@@ -500,29 +445,58 @@ ForwardLayout forward_layout(int64_t m, int64_t n, int64_t k, int64_t x_stride,
     return l;
 }
 
+// Whether the tiles can turn a matrix with rows of k values as it is: whole lines of 16 bytes, and
+// rows near enough that a copy of the last ones at that distance is small.
+bool turnable(int64_t k, int64_t stride)
+{
+    return k % 8 == 0 && stride % 8 == 0 && stride <= 4 * k + 64 && stride < 2 * kMost;
+}
+
+// A matrix that the backward products turn: as it is, with the rows behind the last whole step
+// copied at the same distance, or copied as a whole.
+struct TurnedPlace {
+    int64_t at = -1;  // of the copy, none if negative
+    int64_t rows = 0, from = 0;  // that are copied, and the first of them
+    int64_t out_rows = 0, pitch = 0;
+    bool whole = false;
+};
+
+TurnedPlace turned_place(int64_t& total, int64_t rows, int64_t k, int64_t stride, bool as_it_is)
+{
+    TurnedPlace p;
+    if (as_it_is && rows % kStep == 0)
+        return p;
+    p.whole = !as_it_is;
+    p.from = as_it_is ? rows / kStep * kStep : 0;
+    p.rows = rows - p.from;
+    p.out_rows = padded(p.rows);
+    p.pitch = as_it_is ? stride : padded(k);
+    p.at = take(total, p.out_rows * p.pitch * 2);
+    return p;
+}
+
 struct BackwardLayout {
-    int64_t by_rows = -1, turned = -1, w = -1, x = -1, partial = -1;
+    int64_t slopes = -1, partial = -1;
+    TurnedPlace gate, up, x;
     int64_t total = 0;
 };
 
-BackwardLayout backward_layout(int64_t m, int64_t n, int64_t k, bool dx, bool dw)
+BackwardLayout backward_layout(int64_t m, int64_t n, int64_t k, int64_t x_stride,
+                               int64_t gate_stride, int64_t up_stride, bool dx, bool dw)
 {
     BackwardLayout l;
-    if (dx) {
-        l.by_rows = take(l.total, m * 2 * padded(n) * 2);
-        l.w = take(l.total, k * 2 * padded(n) * 2);
-    }
-    if (dw) {
-        l.turned = take(l.total, 2 * n * padded(m) * 2);
-        l.x = take(l.total, k * padded(m) * 2);
-    }
+    l.slopes = take(l.total, padded(m) * 2 * padded(n) * 2);
     int64_t partial = 0;
     if (dx) {
+        const bool as_it_is = turnable(k, gate_stride) && gate_stride == up_stride;
+        l.gate = turned_place(l.total, n, k, gate_stride, as_it_is);
+        l.up = turned_place(l.total, n, k, up_stride, as_it_is);
         const Way w = way_of(m, k, 1, int(2 * padded(n) / kStep), false);
         if (w.slices > 1)
             partial = w.slices * m * k * 4;
     }
     if (dw) {
+        l.x = turned_place(l.total, m, k, x_stride, turnable(k, x_stride));
         const Way w = way_of(n, k, 2, int(padded(m) / kStep), false);
         if (w.slices > 1)
             partial = std::max(partial, w.slices * 2 * n * k * 4);
@@ -535,18 +509,44 @@ BackwardLayout backward_layout(int64_t m, int64_t n, int64_t k, bool dx, bool dw
 
 uint32_t groups_for(int64_t work) { return uint32_t(std::min<int64_t>(host::ceil_div(work, 256), 8192)); }
 
-// Adds a matrix to a launch of `groups` workgroups so far.
-void add(Layouts& to, int64_t& groups, const void* x, int64_t rows, int64_t cols, int64_t stride,
-         uint8_t* out, int64_t pitch, int64_t its_groups)
+// The copies of one launch.
+struct Copies {
+    Layouts of{};
+    int64_t groups = 0;
+
+    void add(const void* x, int64_t rows, int64_t cols, int64_t stride, uint8_t* out,
+             int64_t out_rows, int64_t pitch)
+    {
+        of.of[of.count++] = Layout{static_cast<const uint16_t*>(x),
+                                   rows,
+                                   cols,
+                                   stride,
+                                   reinterpret_cast<uint16_t*>(out),
+                                   out_rows,
+                                   pitch,
+                                   uint32_t(groups)};
+        groups += host::ceil_div(out_rows * (pitch / 8), kPackLines);
+    }
+    void launch(hipStream_t st) const
+    {
+        if (of.count > 0)
+            k_gated_pack<<<dim3(uint32_t(groups)), 256, 0, st>>>(of);
+    }
+};
+
+// Where the products find a matrix that they turn, its copy added to the launch; k columns.
+void turned_operand(const TurnedPlace& p, const void* x, int64_t rows, int64_t k, int64_t stride,
+                    uint8_t* ws, Copies& copies, TurnedSource* to, int which)
 {
-    to.of[to.count++] = Layout{static_cast<const uint16_t*>(x),
-                               rows,
-                               cols,
-                               stride,
-                               reinterpret_cast<uint16_t*>(out),
-                               pitch,
-                               uint32_t(groups)};
-    groups += its_groups;
+    const auto* base = static_cast<const uint8_t*>(x);
+    const uint8_t* copy = p.at < 0 ? base : ws + p.at;
+    if (p.at >= 0)
+        copies.add(base + p.from * stride * 2, p.rows, k, stride, ws + p.at, p.out_rows, p.pitch);
+    to->base[which] = p.whole ? copy : base;
+    to->tail[which] = copy;
+    to->pitch = (p.whole ? p.pitch : stride) * 2;
+    to->each = int(padded(rows) / kStep);
+    to->full = p.whole ? to->each : int(rows / kStep);
 }
 
 template <typename Tile>
@@ -562,28 +562,28 @@ void launch_forward(const ForwardArgs& g, bool f32, bool save, hipStream_t st)
 }
 
 template <typename Tile>
-void launch_product(const ProductArgs& g, const Way& w, bool f32, hipStream_t st)
+void launch_product(const ProductArgs& g, const Way& w, bool f32, bool dw, hipStream_t st)
 {
     const dim3 grid(uint32_t(host::ceil_div(g.m, Tile::kRows) * host::ceil_div(g.n, Tile::kCols) *
                              g.count),
                     uint32_t(w.slices));
-    if (f32)
-        k_gated_product<Tile, true><<<grid, Tile::kThreads, 0, st>>>(g);
-    else
-        k_gated_product<Tile, false><<<grid, Tile::kThreads, 0, st>>>(g);
+    auto* kernel = dw ? (f32 ? k_gated_product<Tile, true, true> : k_gated_product<Tile, false, true>)
+                      : (f32 ? k_gated_product<Tile, true, false>
+                             : k_gated_product<Tile, false, false>);
+    kernel<<<grid, Tile::kThreads, 0, st>>>(g);
 }
 
-void run_product(ProductArgs g, bool f32, uint8_t* partial, hipStream_t st)
+void run_product(ProductArgs g, bool f32, bool dw, uint8_t* partial, hipStream_t st)
 {
     const Way w = way_of(g.m, g.n, g.count, g.steps, false);
     g.slice = w.slice;
     g.partial = w.slices > 1 ? reinterpret_cast<float*>(partial) : nullptr;
     if (w.tile == 256)
-        launch_product<Large16>(g, w, f32, st);
+        launch_product<Large16>(g, w, f32, dw, st);
     else if (w.tile == 128)
-        launch_product<Small16>(g, w, f32, st);
+        launch_product<Small16>(g, w, f32, dw, st);
     else
-        launch_product<Tiny16>(g, w, f32, st);
+        launch_product<Tiny16>(g, w, f32, dw, st);
     if (g.partial) {
         auto* join = f32 ? k_gated_join<true> : k_gated_join<false>;
         join<<<dim3(groups_for(g.m * g.n * g.count)), 256, 0, st>>>(g, w.slices);
@@ -713,24 +713,21 @@ try {
     g.stride = out_stride;
     if (saved)
         g.saved = saved_layout(saved, m, n);
-    Layouts pack{};
-    int64_t groups = 0;
+    Copies copies;
     const auto operand = [&](const void* p, int64_t rows, int64_t stride, int64_t at,
                              const uint8_t** from, int64_t* pitch) {
         *from = static_cast<const uint8_t*>(p);
         *pitch = stride * 2;
         if (at < 0)
             return;
-        add(pack, groups, p, rows, k, stride, ws + at, padded(k),
-            host::ceil_div(rows * (padded(k) / 8), kPackLines));
+        copies.add(p, rows, k, stride, ws + at, rows, padded(k));
         *from = ws + at;
         *pitch = padded(k) * 2;
     };
     operand(x, m, x_stride, l.x, &g.x, &g.x_pitch);
     operand(gate, n, gate_stride, l.gate, &g.gate, &g.gate_pitch);
     operand(up, n, up_stride, l.up, &g.up, &g.up_pitch);
-    if (pack.count > 0)
-        k_gated_pack<<<dim3(uint32_t(groups)), 256, 0, st>>>(pack);
+    copies.launch(st);
     const Way w = way_of(m, n, 1, g.steps, true);
     if (w.tile == 256)
         launch_forward<Large16>(g, f32, saved != nullptr, st);
@@ -744,11 +741,13 @@ try {
     return host::caught();
 }
 
-size_t lt_gated_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int dx, int dw)
+size_t lt_gated_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t x_stride,
+                                         int64_t gate_stride, int64_t up_stride, int dx, int dw)
 {
     if (!valid_sizes(m, n, k))
         return 0;
-    return size_t(backward_layout(m, n, k, dx != 0, dw != 0).total);
+    return size_t(
+        backward_layout(m, n, k, x_stride, gate_stride, up_stride, dx != 0, dw != 0).total);
 }
 
 lt_err lt_gated_backward(const void* dh, int dh_dtype, int64_t dh_stride, const void* saved,
@@ -777,12 +776,14 @@ try {
     if (!empty && (!dh || !saved || (dx && (!gate || !up)) || (want_dw && !x)))
         return fail(LT_ERR_INVALID_ARG, "dh, saved and the operands must not be NULL");
     if (!host::aligned(dh, dh_dtype == LT_DTYPE_BF16 ? 2 : 4) || !host::aligned(saved, 16) ||
-        !host::aligned(x, 2) || !host::aligned(gate, 2) || !host::aligned(up, 2) ||
+        !host::aligned(x, 16) || !host::aligned(gate, 16) || !host::aligned(up, 16) ||
         !host::aligned(dx, 16) || !host::aligned(dgate, 16) || !host::aligned(dup, 16))
-        return fail(LT_ERR_ALIGNMENT, "operands must be aligned to their elements, saved and the "
-                                      "gradients to 16 bytes");
+        return fail(LT_ERR_ALIGNMENT, "dh must be aligned to its elements, x, the weights, saved and "
+                                      "the gradients to 16 bytes");
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    const size_t need = lt_gated_backward_workspace_bytes(m, n, k, dx != nullptr, want_dw);
+    const BackwardLayout l = backward_layout(m, n, k, x_stride, gate_stride, up_stride,
+                                             dx != nullptr, want_dw);
+    const auto need = size_t(l.total);
     if (!empty && (!workspace || !host::aligned(workspace, 256) || workspace_bytes < need))
         return fail(LT_ERR_WORKSPACE, "workspace must be 256-byte aligned and hold " +
                                           std::to_string(need) + " bytes");
@@ -823,64 +824,52 @@ try {
     auto* ws = static_cast<uint8_t*>(workspace);
     if (lt_err e = host::workspace_written(ws, need, st))
         return e;
-    const BackwardLayout l = backward_layout(m, n, k, dx != nullptr, want_dw);
     const int64_t half = padded(n), tokens = padded(m);
-    Layouts turn{};
-    int64_t groups = half / 64 * (tokens / 64);
-    const auto turned = [&](const void* p, int64_t rows, int64_t stride, int64_t at,
-                            int64_t pitch) {
-        add(turn, groups, p, rows, k, stride, ws + at, pitch,
-            host::ceil_div(rows, 64) * host::ceil_div(k, 64));
-    };
-    if (dx) {
-        turned(gate, n, gate_stride, l.w, 2 * half);
-        turned(up, n, up_stride, l.w + half * 2, 2 * half);
-    }
-    if (want_dw)
-        turned(x, m, x_stride, l.x, tokens);
-    const SlopeArgs s{dh,
-                      dh_stride,
-                      saved_layout(const_cast<void*>(saved), m, n),
-                      m,
-                      n,
-                      dx ? reinterpret_cast<uint16_t*>(ws + l.by_rows) : nullptr,
-                      half,
-                      want_dw ? reinterpret_cast<uint16_t*>(ws + l.turned) : nullptr,
-                      tokens,
-                      turn};
-    const dim3 blocks{uint32_t(groups)};
+    auto* slopes = reinterpret_cast<uint16_t*>(ws + l.slopes);
+    const SlopeArgs s{dh, dh_stride, saved_layout(const_cast<void*>(saved), m, n), m, n, slopes,
+                      half, tokens};
+    const dim3 blocks(uint32_t(host::ceil_div(tokens * (half / 8), 256)));
     if (dh_dtype == LT_DTYPE_F32)
         k_gated_slopes<true><<<blocks, 256, 0, st>>>(s);
     else
         k_gated_slopes<false><<<blocks, 256, 0, st>>>(s);
     uint8_t* partial = l.partial < 0 ? nullptr : ws + l.partial;
+    ProductArgs g{};
+    g.a = ws + l.slopes;
+    g.a_pitch = 4 * half;
+    ProductArgs to_x = g, to_w = g;
+    Copies copies;
     if (dx) {
-        ProductArgs g{};
-        g.a = ws + l.by_rows;
-        g.b = ws + l.w;
-        g.a_pitch = g.b_pitch = 4 * half;
-        g.m = m;
-        g.n = k;
-        g.count = 1;
-        g.steps = int(2 * half / kStep);
-        g.out[0] = dx;
-        g.stride[0] = dx_stride;
-        run_product(g, dx_dtype == LT_DTYPE_F32, partial, st);
+        turned_operand(l.gate, gate, n, k, gate_stride, ws, copies, &to_x.b, 0);
+        turned_operand(l.up, up, n, k, up_stride, ws, copies, &to_x.b, 1);
     }
     if (want_dw) {
-        ProductArgs g{};
-        g.a = ws + l.turned;
-        g.b = ws + l.x;
-        g.a_pitch = g.b_pitch = 2 * tokens;
-        g.m = n;
-        g.n = k;
-        g.count = 2;
-        g.steps = int(tokens / kStep);
-        g.out[0] = dgate;
-        g.out[1] = dup;
-        g.stride[0] = dgate_stride;
-        g.stride[1] = dup_stride;
-        run_product(g, grad_dtype == LT_DTYPE_F32, partial, st);
+        turned_operand(l.x, x, m, k, x_stride, ws, copies, &to_w.b, 0);
+        to_w.b.base[1] = to_w.b.base[0];
+        to_w.b.tail[1] = to_w.b.tail[0];
+    }
+    copies.launch(st);
+    if (dx) {
+        to_x.b_cols = l.gate.whole ? padded(k) : k;
+        to_x.m = m;
+        to_x.n = k;
+        to_x.count = 1;
+        to_x.steps = int(2 * half / kStep);
+        to_x.out[0] = dx;
+        to_x.stride[0] = dx_stride;
+        run_product(to_x, dx_dtype == LT_DTYPE_F32, false, partial, st);
+    }
+    if (want_dw) {
+        to_w.b_cols = l.x.whole ? padded(k) : k;
+        to_w.m = n;
+        to_w.n = k;
+        to_w.count = 2;
+        to_w.steps = int(tokens / kStep);
+        to_w.out[0] = dgate;
+        to_w.out[1] = dup;
+        to_w.stride[0] = dgate_stride;
+        to_w.stride[1] = dup_stride;
+        run_product(to_w, grad_dtype == LT_DTYPE_F32, true, partial, st);
     }
     LT_TRY_HIP(hipGetLastError());
     return LT_OK;

@@ -39,10 +39,29 @@ constexpr int kStepBytes = 128;  // of every row, per step of the main loop
 #define LT_GLOBAL __attribute__((address_space(1)))
 #define LT_LDS __attribute__((address_space(3)))
 
+// 16 bytes a lane from `from` + offset into LDS, in lane order from `to` on.  With UNSEEN the
+// compiler does not know of the copy: it waits for all that it knows of before it reads LDS other
+// than by plain loads.  Waits (wait_loads) are written out either way.
+template <bool UNSEEN>
+__device__ inline void copy_to_lds(const uint8_t* from, uint32_t offset, uint8_t* to)
+{
+    if constexpr (UNSEEN) {
+        const uint32_t at = uint32_t(reinterpret_cast<uintptr_t>((LT_LDS void*)(to)));
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                     :
+                     : "s"(at), "v"(offset), "s"(from)
+                     : "memory");  // and m0, which nothing else uses in a kernel of such copies
+    } else {
+        __builtin_amdgcn_global_load_lds((const LT_GLOBAL void*)(from + offset), (LT_LDS void*)(to),
+                                         16, 0, 0);
+    }
+}
+
 // ROWS rows of 128 bytes from `src` (row pitch in bytes; rows from `limit` on read the last
 // row that exists) into LDS.  offset[] holds what does not change between steps.
-template <int ROWS, int THREADS>
+template <int ROWS, int THREADS, bool UNSEEN = false>
 struct TileLoad {
+    static constexpr bool kUnseen = UNSEEN;
     static constexpr int N = ROWS * 8 / THREADS;
     static_assert(N * 32 == ROWS, "a copy is a block of 32 rows");
     uint32_t offset[N];
@@ -62,9 +81,7 @@ struct TileLoad {
     __device__ inline void issue(int i, const uint8_t* src, uint8_t* lds) const
     {
         const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
-        __builtin_amdgcn_global_load_lds((const LT_GLOBAL void*)(src + offset[i]),
-                                         (LT_LDS void*)(lds + (i * THREADS + wave * 64) * 16), 16,
-                                         0, 0);
+        copy_to_lds<UNSEEN>(src, offset[i], lds + (i * THREADS + wave * 64) * 16);
     }
 };
 
@@ -72,6 +89,7 @@ struct TileLoad {
 // a wave's blocks of columns 2 j and 2 j + 1 are the same rows of either.
 template <int ROWS, int THREADS>
 struct PairLoad {
+    static constexpr bool kUnseen = false;
     static constexpr int N = ROWS * 8 / THREADS;
     static_assert(N * 32 == ROWS && N % 2 == 0, "a copy is a block of 32 rows");
     uint32_t offset[N];
@@ -408,8 +426,141 @@ struct Fp8 {
     }
 };
 
-// The main loop over `steps` >= 1 steps.  P, Q: first rows of the tile's operands, and how they are
-// copied.
+// A wave's blocks of rows in two groups, see below: the blocks [first, first + n) of group g of
+// `all`.
+struct Groups {
+    static constexpr int n(int all, int g) { return g == 0 ? (all + 1) / 2 : all / 2; }
+    static constexpr int first(int all, int g) { return g == 0 ? 0 : (all + 1) / 2; }
+};
+
+// An address that is the same in all lanes, in scalar registers, for written-out copies: a vector
+// instruction's result there may be an address five instructions later.
+__device__ inline const uint8_t* uniform(const uint8_t* p)
+{
+    const auto v = reinterpret_cast<uint64_t>(p);
+    const uint64_t low = uint32_t(__builtin_amdgcn_readfirstlane(int(uint32_t(v))));
+    const uint64_t high = uint32_t(__builtin_amdgcn_readfirstlane(int(uint32_t(v >> 32))));
+    uint64_t same = high << 32 | low;
+    asm volatile("s_nop 4" : "+s"(same));
+    return reinterpret_cast<const uint8_t*>(same);
+}
+
+// What the main loop does with an operand of ROWS rows in the tile, BLOCKS blocks of 32 to a wave:
+//   copies(g)             copies of group g's rows, of all waves, in a step;
+//   aim(s)                the next copies are step s's;
+//   issue(g, k, to)       the k-th of group g's into the operand's place in a buffer;
+//   read(from, at, block, c, lane)  a lane's c-th chunk of a block of the wave whose first row is at.
+// This one has rows with k contiguous.
+template <typename S, int ROWS, int BLOCKS, typename Load>
+struct RowOperand {
+    const uint8_t* src;
+    int steps;
+    const uint8_t* now;
+    Load load;
+
+    static constexpr int copies(int g) { return ROWS / 32 / BLOCKS * Groups::n(BLOCKS, g); }
+    __device__ inline void aim(int s)
+    {
+        now = src + int64_t(s < steps ? s : steps - 1) * kStepBytes;
+        if constexpr (Load::kUnseen)
+            now = uniform(now);
+    }
+    __device__ inline void issue(int g, int k, uint8_t* to) const
+    {
+        const int n = Groups::n(BLOCKS, g);
+        load.issue(k / n * BLOCKS + Groups::first(BLOCKS, g) + k % n, now, to);
+    }
+    __device__ static inline i32x4 read(const uint8_t* from, int at, int block, int c, int lane)
+    {
+        return S::k16 ? read_chunk_16(from, at + 32 * block, c, lane)
+                      : read_chunk(from, at + 32 * block, c, lane);
+    }
+};
+
+// Where a step of a turned operand lies: in the first matrix, then in the second, each with `each`
+// steps of 64 rows; rows from the full ones on are in copies of their own, zeros behind the last.
+struct TurnedSource {
+    const uint8_t* base[2];
+    const uint8_t* tail[2];
+    int64_t pitch;  // bytes, of either
+    int each, full;
+    __device__ inline const uint8_t* at(int s) const
+    {
+        const int which = s >= each ? 1 : 0, t = s - which * each;
+        return t < full ? (which ? base[1] : base[0]) + int64_t(t) * 64 * pitch
+                        : (which ? tail[1] : tail[0]);
+    }
+};
+
+// This one, of 16-bit values, has the summed index as rows: its tile is 64 rows of the operand's
+// columns, read out of LDS four rows of a column at a time (ds_read_b64_tr_b16: of sixteen lanes,
+// lanes 4 j .. 4 j + 3 read 16 neighbouring columns of row j, and lane i gets the four rows of
+// column i).  A group's columns, of all waves, are an image of their own, so that it is copied and
+// free as the group is; rows of 256 bytes (two blocks to a group) or 128.  A cycle serves eight rows
+// {0 .. 3, 8 .. 11} of 32 bytes: 16-byte chunk c of row k is at position c ^ f(k), which puts them
+// next to each other.  The other operand's copies have to be UNSEEN as this one's are.
+template <typename S, int ROWS, int BLOCKS>
+struct TurnedOperand {
+    static constexpr int kAlong = ROWS / 32 / BLOCKS;  // waves
+    TurnedSource src;
+    int first, steps;  // of the sum's slice
+    const uint8_t* now;
+    uint32_t offset[2];
+
+    static constexpr int copies(int g) { return kAlong * Groups::n(BLOCKS, g); }
+    static constexpr int pitch(int g) { return 2 * 32 * kAlong * Groups::n(BLOCKS, g); }
+    static constexpr int image(int g) { return g == 0 ? 0 : 64 * pitch(0); }
+    __device__ static inline int place(int g, int chunk, int row)
+    {
+        return pitch(g) == 256 ? chunk ^ 2 * ((row & 3) + 4 * (row >> 3 & 1))
+                               : chunk ^ 2 * ((row >> 1 & 1) + 2 * (row >> 3 & 1));
+    }
+    // `limit` columns, a multiple of 8, exist from the tile's first on
+    __device__ inline void init(int64_t limit)
+    {
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const int n = Groups::n(BLOCKS, g);
+            if (n == 0)
+                continue;
+            const int byte = int(threadIdx.x) * 16, row = byte / pitch(g);
+            const int col = place(g, byte % pitch(g) / 16, row) * 8;  // its own inverse
+            int64_t at = col / (32 * n) * (32 * BLOCKS) + 32 * Groups::first(BLOCKS, g) +
+                         col % (32 * n);
+            at = at < limit ? at : limit - 8;
+            offset[g] = uint32_t(row * src.pitch) + uint32_t(at * 2);
+        }
+    }
+    __device__ inline void aim(int s)
+    {
+        now = uniform(src.at(first + (s < steps ? s : steps - 1)));
+    }
+    __device__ inline void issue(int g, int k, uint8_t* to) const
+    {
+        const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+        copy_to_lds<true>(now + int64_t(k) * (4096 / pitch(g)) * src.pitch, offset[g],
+                          to + image(g) + k * 4096 + wave * 1024);
+    }
+    __device__ static inline i32x4 read(const uint8_t* from, int at, int block, int c, int lane)
+    {
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef int i32x2 __attribute__((ext_vector_type(2)));
+        const int g = block < Groups::n(BLOCKS, 0) ? 0 : 1, n = Groups::n(BLOCKS, g);
+        const int col = at / (32 * BLOCKS) * 32 * n + 32 * (block - Groups::first(BLOCKS, g)) +
+                        16 * (c & 1);
+        const int row = 32 * (c >> 1) + 8 * (lane >> 4) + (lane >> 2 & 3);
+        const uint8_t* p = from + image(g) + row * pitch(g) +
+                           place(g, col / 8 + (lane >> 1 & 1), row) * 16 + (lane & 1) * 8;
+        const auto four = [](const uint8_t* q) {
+            return __builtin_bit_cast(
+                i32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LT_LDS s16x4*)(q)));
+        };
+        const i32x2 u = four(p), v = four(p + 4 * pitch(g));  // four rows on: the same place
+        return i32x4{u[0], u[1], v[0], v[1]};
+    }
+};
+
+// The main loop over `steps` >= 1 steps of the operands p and q.
 //
 // A wave's block is multiplied in four quarters: the rows' blocks of 32 in two groups a0 and a1,
 // the columns' in b0 and b1, in an order in which neighbours share a group:
@@ -426,52 +577,33 @@ struct Fp8 {
 // A body of two steps has no branches but one at its top: past the end it copies and reads the
 // last step again, unused, and a branch inside made the compiler move all products before it
 // behind it, away from the loads that they cover.
-template <typename Mul, typename S, typename LoadQ>
-__device__ inline void product(Mul& mul, S& c, const void* P,
-                               const TileLoad<S::kRows, S::kThreads>& load_p, const void* Q,
-                               const LoadQ& load_q, int steps, uint8_t* lds)
+template <typename Mul, typename S, typename OpP, typename OpQ>
+__device__ inline void product(Mul& mul, S& c, OpP& p, OpQ& q, int steps, uint8_t* lds)
 {
     constexpr int I = S::I, J = S::J;
     const int lane = S::lane(), wm = S::wave_row(), wn = S::wave_col();
-    const auto* p = static_cast<const uint8_t*>(P);
-    const auto* q = static_cast<const uint8_t*>(Q);
-    constexpr int kLoads = TileLoad<S::kRows, S::kThreads>::N + LoadQ::N;
-    struct Groups {
-        // the blocks [first, first + n) of group g of `all`
-        static constexpr int n(int all, int g) { return g == 0 ? (all + 1) / 2 : all / 2; }
-        static constexpr int first(int all, int g) { return g == 0 ? 0 : (all + 1) / 2; }
-        // copies of the early or late rows of an even (0) or odd (1) step
-        static constexpr int loads(int odd, int late)
-        {
-            return S::kRows / 32 / I * n(I, late) + S::kCols / 32 / J * n(J, odd ^ late);
-        }
+    constexpr int kLoads = (S::kRows + S::kCols) * 8 / S::kThreads;
+    // copies of the early or late rows of an even (0) or odd (1) step
+    constexpr auto copies = [](int odd, int late) {
+        return OpP::copies(late) + OpQ::copies(odd ^ late);
     };
     Chunks a[I], b[J];
-    // the k-th copy of step s's early or late rows
-    const auto load = [&](int s, int odd, int late, int k) {
+    // the k-th copy of the early or late rows of the step that is aimed at
+    const auto load = [&](int odd, int late, int k) {
         uint8_t* to = lds + odd * S::kBufferBytes;
-        const int64_t at = int64_t(s < steps ? s : steps - 1) * kStepBytes;
-        const int np = Groups::n(I, late), nq = Groups::n(J, odd ^ late);
-        const int all_p = S::kRows / 32 / I * np;
-        if (k < all_p) {
-            load_p.issue(k / np * I + Groups::first(I, late) + k % np, p + at, to);
-        } else {
-            const int l = k - all_p;
-            load_q.issue(l / nq * J + Groups::first(J, odd ^ late) + l % nq, q + at,
-                         to + S::kRows * kStepBytes);
-        }
-    };
-    const auto read = [](const uint8_t* tile, int row32, int c, int l) {
-        return S::k16 ? read_chunk_16(tile, row32, c, l) : read_chunk(tile, row32, c, l);
+        if (k < OpP::copies(late))
+            p.issue(late, k, to);
+        else
+            q.issue(odd ^ late, k - OpP::copies(late), to + S::kRows * kStepBytes);
     };
     const auto read_a = [&](int odd, int g, int k) {
         const int i = Groups::first(I, g) + k / 4;
-        a[i].c[k % 4] = read(lds + odd * S::kBufferBytes, wm + 32 * i, k % 4, lane);
+        a[i].c[k % 4] = p.read(lds + odd * S::kBufferBytes, wm, i, k % 4, lane);
     };
     const auto read_b = [&](int odd, int g, int k) {
         const int j = Groups::first(J, g) + k / 4;
-        b[j].c[k % 4] = read(lds + odd * S::kBufferBytes + S::kRows * kStepBytes,
-                                   wn + 32 * j, k % 4, lane);
+        b[j].c[k % 4] =
+            q.read(lds + odd * S::kBufferBytes + S::kRows * kStepBytes, wn, j, k % 4, lane);
     };
     // the products of groups ga and gb, with reads and copies issued evenly between them: reads
     // within the first three quarters, so that the last covers their latency.  Every border
@@ -507,22 +639,24 @@ __device__ inline void product(Mul& mul, S& c, const void* P,
     // step s, odd or even
     const auto step = [&](int s, auto parity) {
         constexpr int odd = decltype(parity)::value;
-        constexpr int early = Groups::loads(odd, 0), late = Groups::loads(odd, 1);
+        constexpr int early = copies(odd, 0), late = copies(odd, 1);
         constexpr int b_first = odd, b_second = 1 - odd;
         mul.next(s);
+        p.aim(s + 2);
+        q.aim(s + 2);
         multiply(0, b_first, 4 * Groups::n(J, b_second), [&](int k) { read_b(odd, b_second, k); },
-                 early / 2, [&](int k) { load(s + 2, odd, 0, k); });
+                 early / 2, [&](int k) { load(odd, 0, k); });
         multiply(0, b_second, 4 * Groups::n(I, 1), [&](int k) { read_a(odd, 1, k); },
-                 early - early / 2, [&](int k) { load(s + 2, odd, 0, early / 2 + k); });
+                 early - early / 2, [&](int k) { load(odd, 0, early / 2 + k); });
         wait_reads();
-        wait_loads<early + Groups::loads(1 - odd, 1)>();  // the next step's early rows are there
+        wait_loads<early + copies(1 - odd, 1)>();  // the next step's early rows are there
         __builtin_amdgcn_s_barrier();
         mul.read(s + 1);
         multiply(1, b_second, 4 * Groups::n(I, 0), [&](int k) { read_a(1 - odd, 0, k); },
-                 late / 2, [&](int k) { load(s + 2, odd, 1, k); });
+                 late / 2, [&](int k) { load(odd, 1, k); });
         multiply(1, b_first, 4 * Groups::n(J, b_second),
                  [&](int k) { read_b(1 - odd, b_second, k); }, late - late / 2,
-                 [&](int k) { load(s + 2, odd, 1, late / 2 + k); });
+                 [&](int k) { load(odd, 1, late / 2 + k); });
         wait_reads();
         wait_loads<kLoads>();  // and its late rows
         __builtin_amdgcn_s_barrier();
@@ -532,12 +666,15 @@ __device__ inline void product(Mul& mul, S& c, const void* P,
         c.settle();
     mul.begin();
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+    for (int s = 0; s < 2; ++s) {
+        p.aim(s);
+        q.aim(s);
 #pragma unroll
         for (int k = 0; k < kLoads; ++k) {
-            const int early = Groups::loads(s, 0);
-            load(s, s, k >= early, k < early ? k : k - early);
+            const int early = copies(s, 0);
+            load(s, k >= early, k < early ? k : k - early);
         }
+    }
     wait_loads<kLoads>();
     __builtin_amdgcn_s_barrier();
     mul.read(0);
@@ -571,11 +708,14 @@ __device__ inline void product(Mul& mul, S& c, const void* P, int64_t pitch_p, i
                                const void* Q, int64_t pitch_q, int64_t limit_q, int steps,
                                uint8_t* lds)
 {
-    TileLoad<S::kRows, S::kThreads> load_p;
-    TileLoad<S::kCols, S::kThreads> load_q;
-    load_p.init(pitch_p, limit_p);
-    load_q.init(pitch_q, limit_q);
-    product(mul, c, P, load_p, Q, load_q, steps, lds);
+    RowOperand<S, S::kRows, S::I, TileLoad<S::kRows, S::kThreads>> p;
+    RowOperand<S, S::kCols, S::J, TileLoad<S::kCols, S::kThreads>> q;
+    p.src = static_cast<const uint8_t*>(P);
+    q.src = static_cast<const uint8_t*>(Q);
+    p.steps = q.steps = steps;
+    p.load.init(pitch_p, limit_p);
+    q.load.init(pitch_q, limit_q);
+    product(mul, c, p, q, steps, lds);
 }
 
 // For two matrices' rows in turns (PairLoad): columns [0, kCols / 2) of both results.
@@ -585,11 +725,14 @@ __device__ inline void product_pairs(Mul& mul, S& c, const void* P, int64_t pitc
                                      const void* second, int64_t second_pitch, int64_t limit_q,
                                      int steps, uint8_t* lds)
 {
-    TileLoad<S::kRows, S::kThreads> load_p;
-    PairLoad<S::kCols, S::kThreads> load_q;
-    load_p.init(pitch_p, limit_p);
-    load_q.init(first_pitch, second_pitch, first, second, limit_q);
-    product(mul, c, P, load_p, first, load_q, steps, lds);
+    RowOperand<S, S::kRows, S::I, TileLoad<S::kRows, S::kThreads>> p;
+    RowOperand<S, S::kCols, S::J, PairLoad<S::kCols, S::kThreads>> q;
+    p.src = static_cast<const uint8_t*>(P);
+    q.src = static_cast<const uint8_t*>(first);
+    p.steps = q.steps = steps;
+    p.load.init(pitch_p, limit_p);
+    q.load.init(first_pitch, second_pitch, first, second, limit_q);
+    product(mul, c, p, q, steps, lds);
 }
 
 // What follows the main loop, for one wave's block, 32 rows at a time through LDS (the loop is

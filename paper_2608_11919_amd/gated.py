@@ -128,7 +128,8 @@ def _backward(dh, saved, x, gate, up, leading, shape, out_dtype, grad_dtype, wan
     if not want_dx and not want_dw:
         return None, None, None
     handle = _stream_handle(None, device)
-    need = lib().lt_gated_backward_workspace_bytes(m, n, k, want_dx, want_dw)
+    need = lib().lt_gated_backward_workspace_bytes(m, n, k, x_stride, g_stride, u_stride, want_dx,
+                                                   want_dw)
     held, ws, nbytes = _scratch(device, need, None, None)
     with _current(device):
         _check(lib().lt_gated_backward(d.data_ptr(), d_code, d_stride, saved.data_ptr(), x_at,

@@ -180,7 +180,7 @@ def lib() -> ctypes.CDLL:
     L.lt_gated_forward_workspace_bytes.restype = size
     L.lt_gated_forward.argtypes = [vp, i64, vp, i64, vp, i64, num, i64, i64, i64, vp, num, i64, vp,
                                    vp, size, vp]
-    L.lt_gated_backward_workspace_bytes.argtypes = [i64, i64, i64, num, num]
+    L.lt_gated_backward_workspace_bytes.argtypes = [i64] * 6 + [num, num]
     L.lt_gated_backward_workspace_bytes.restype = size
     L.lt_gated_backward.argtypes = [vp, num, i64, vp, vp, i64, vp, i64, vp, i64, i64, i64, i64, vp,
                                     num, i64, vp, i64, vp, i64, num, vp, size, vp]

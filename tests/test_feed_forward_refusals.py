@@ -163,6 +163,8 @@ def test_arguments(call):
     lambda: backward(dh=BASE + 1),
     lambda: backward(saved=2 * BASE + 8),
     lambda: backward(dx=6 * BASE + 2),
+    lambda: backward(x=3 * BASE + 2),
+    lambda: backward(up=5 * BASE + 8),
 ])
 def test_alignment(call):
     assert call() == lt.LT_ERR_ALIGNMENT
@@ -211,15 +213,18 @@ def test_sizes_of_memory():
         assert L.lt_int8_linear_workspace_bytes(m, n, k) >= 256
         assert L.lt_int8_gated_workspace_bytes(m, n, k) >= 256
         assert L.lt_gated_forward_workspace_bytes(m, n, k, 9, 9, 9) >= 256
-        assert L.lt_gated_backward_workspace_bytes(m, n, k, 1, 1) >= 256
+        assert L.lt_gated_backward_workspace_bytes(m, n, k, k, k, k, 1, 1) >= 256
     assert L.lt_gated_saved_bytes(3, 9) == 6 * 3 * 16
     assert L.lt_gated_saved_bytes(3, 1 << 21) == 0
     assert L.lt_gated_forward_workspace_bytes(64, 64, 64, 64, 64, 64) == 256
     assert L.lt_gated_forward_workspace_bytes(64, 32, 64, 65, 64, 64) == 64 * 128
-    assert L.lt_gated_backward_workspace_bytes(-1, 1, 1, 1, 1) == 0
-    some = [L.lt_gated_backward_workspace_bytes(100, 200, 300, *w) for w in
-            ((0, 0), (1, 0), (0, 1), (1, 1))]
-    assert some[0] == 256 and some[3] == some[1] + some[2]
+    assert L.lt_gated_backward_workspace_bytes(-1, 1, 1, 1, 1, 1, 1, 1) == 0
+    slopes, tail = 128 * 512 * 2, 64 * 304 * 2
+    for want, bytes_ in (((0, 0), slopes), ((1, 0), slopes + 2 * tail), ((0, 1), slopes + tail)):
+        assert L.lt_gated_backward_workspace_bytes(100, 200, 304, 304, 304, 304, *want) == bytes_
+    # columns that are no multiple of 8: whole copies
+    assert L.lt_gated_backward_workspace_bytes(100, 200, 300, 300, 300, 300, 1, 1) == \
+        slopes + 2 * 256 * 320 * 2 + 128 * 320 * 2
 
 
 def test_tensors():
