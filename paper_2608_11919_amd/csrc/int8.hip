@@ -54,83 +54,90 @@ __device__ inline uint32_t code_of(float x, RowScale s)
     return s.factor == 0.0f ? 0u : __float_as_uint(v) & 0xFFu;
 }
 
+// Eight values of a row, as they are stored.
 template <typename T>
-__device__ inline float value_at(const T* p)
-{
-    if constexpr (sizeof(T) == 2)
-        return __uint_as_float(uint32_t(*p) << 16);
-    else
-        return *p;
-}
-
-// Eight values from column `at` on.
-template <typename T>
-__device__ inline void load_eight(const T* row, int64_t at, int64_t cols, float (&v)[8])
-{
-    if (at + 8 <= cols) {
+struct Eight {
+    i32x4 w[sizeof(T) / 2];
+    __device__ inline float at(int e) const
+    {
         if constexpr (sizeof(T) == 2) {
-            const i32x4 w = load_any(row + at);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                v[2 * e] = __uint_as_float(uint32_t(w[e]) << 16);
-                v[2 * e + 1] = __uint_as_float(uint32_t(w[e]) & 0xFFFF0000u);
-            }
+            const auto v = uint32_t(w[0][e / 2]);
+            return __uint_as_float(e % 2 == 0 ? v << 16 : v & 0xFFFF0000u);
         } else {
-            const f32x4 a = __builtin_bit_cast(f32x4, load_any(row + at));
-            const f32x4 b = __builtin_bit_cast(f32x4, load_any(row + at + 4));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                v[e] = a[e];
-                v[4 + e] = b[e];
-            }
+            return __int_as_float(w[e / 4][e % 4]);
         }
-        return;
+    }
+    __device__ inline uint32_t largest(uint32_t top) const
+    {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            top = max(top, __float_as_uint(at(e)) & 0x7FFFFFFFu);
+        return top;
+    }
+    __device__ inline uint2 codes(RowScale s) const
+    {
+        uint32_t c[2] = {0, 0};
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            c[e / 4] |= code_of(at(e), s) << (8 * (e % 4));
+        return make_uint2(c[0], c[1]);
+    }
+};
+
+// From column `at` on; zeros behind the row's end.
+template <typename T>
+__device__ inline Eight<T> load_eight(const T* row, int64_t at, int64_t cols)
+{
+    constexpr int kLines = sizeof(T) / 2, kEach = 8 / kLines;
+    Eight<T> v;
+    if (at + 8 <= cols) {
+#pragma unroll
+        for (int c = 0; c < kLines; ++c)
+            v.w[c] = load_any(row + at + c * kEach);
+        return v;
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        v[e] = at + e < cols ? value_at(row + at + e) : 0.0f;
-}
-
-__device__ inline uint2 codes_of(const float (&v)[8], RowScale s)
-{
-    uint32_t w[2] = {0, 0};
+    for (int c = 0; c < kLines; ++c)
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        w[e / 4] |= code_of(v[e], s) << (8 * (e % 4));
-    return make_uint2(w[0], w[1]);
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (sizeof(T) == 2) {
+                const int64_t i = at + 2 * e;
+                const uint32_t lo = i < cols ? row[i] : 0u, hi = i + 1 < cols ? row[i + 1] : 0u;
+                v.w[c][e] = int(lo | hi << 16);
+            } else {
+                const int64_t i = at + 4 * c + e;
+                v.w[c][e] = i < cols ? __float_as_int(row[i]) : 0;
+            }
+        }
+    return v;
 }
 
 // A row by WAVES waves, eight values a lane and HELD pieces of the row in registers; what is
-// longer is read a second time (out of L2).
+// longer is read a second time (out of L2).  More registers mean fewer waves and cost more than
+// that: rows of 17408 by sixteen waves with one piece 88 us (8192 rows of bf16, 4.8 TB/s), with
+// three 101, by four with four 105; rows of 5120 by four waves with two pieces 46 (17408 rows,
+// 5.8 TB/s), with four 59; rows of 1024 by one wave with one 34 (65536 rows), by four 60.
 template <typename T, int WAVES, int HELD>
-__global__ __launch_bounds__(256) void k_int8_quantize(QuantizeArgs a)
+__global__ __launch_bounds__(WAVES < 4 ? 256 : 64 * WAVES) void k_int8_quantize(QuantizeArgs a)
 {
-    constexpr int kThreads = 64 * WAVES, kRows = 4 / WAVES;
-    __shared__ uint32_t tops[4];
+    constexpr int kThreads = 64 * WAVES, kRows = WAVES < 4 ? 4 / WAVES : 1;
+    __shared__ uint32_t tops[WAVES];
     const int t = int(threadIdx.x) % kThreads, wave = int(threadIdx.x) >> 6;
     for (int64_t r0 = int64_t(blockIdx.x) * kRows; r0 < a.rows; r0 += int64_t(gridDim.x) * kRows) {
         const int64_t row = r0 + int(threadIdx.x) / kThreads;
         const bool there = row < a.rows;
         const T* x = static_cast<const T*>(a.x) + (there ? row : 0) * a.stride;
         const int64_t cols = there ? a.cols : 0;
-        float v[HELD][8];
+        Eight<T> v[HELD];
         uint32_t top = 0;
-        const auto look = [&](const float (&w)[8]) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                top = max(top, __float_as_uint(w[e]) & 0x7FFFFFFFu);
-        };
 #pragma unroll
         for (int h = 0; h < HELD; ++h)
-            load_eight(x, (h * kThreads + t) * 8, cols, v[h]);
+            v[h] = load_eight(x, (h * kThreads + t) * 8, cols);
 #pragma unroll
         for (int h = 0; h < HELD; ++h)
-            look(v[h]);
-        for (int64_t at = (HELD * kThreads + t) * 8; at < cols; at += kThreads * 8) {
-            float w[8];
-            load_eight(x, at, cols, w);
-            look(w);
-        }
+            top = v[h].largest(top);
+        for (int64_t at = (HELD * kThreads + t) * 8; at < cols; at += kThreads * 8)
+            top = load_eight(x, at, cols).largest(top);
 #pragma unroll
         for (int o = 32; o >= 1; o >>= 1)
             top = max(top, uint32_t(__shfl_xor(int(top), o, 64)));
@@ -138,7 +145,9 @@ __global__ __launch_bounds__(256) void k_int8_quantize(QuantizeArgs a)
             if (t % 64 == 0)
                 tops[wave] = top;
             __syncthreads();
-            top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+#pragma unroll
+            for (int i = 0; i < WAVES; ++i)
+                top = max(top, tops[i]);
             __syncthreads();
         }
         if (!there)
@@ -151,13 +160,10 @@ __global__ __launch_bounds__(256) void k_int8_quantize(QuantizeArgs a)
         for (int h = 0; h < HELD; ++h) {
             const int64_t at = (h * kThreads + t) * 8;
             if (at < a.pitch)
-                *reinterpret_cast<uint2*>(to + at) = codes_of(v[h], s);
+                *reinterpret_cast<uint2*>(to + at) = v[h].codes(s);
         }
-        for (int64_t at = (HELD * kThreads + t) * 8; at < a.pitch; at += kThreads * 8) {
-            float w[8];
-            load_eight(x, at, cols, w);
-            *reinterpret_cast<uint2*>(to + at) = codes_of(w, s);
-        }
+        for (int64_t at = (HELD * kThreads + t) * 8; at < a.pitch; at += kThreads * 8)
+            *reinterpret_cast<uint2*>(to + at) = load_eight(x, at, cols).codes(s);
     }
 }
 
@@ -378,26 +384,18 @@ __global__ __launch_bounds__(64 * kHeldWaves) void k_int8_held(HeldArgs g)
             const bool there = t < g.m;
             const Value* row = static_cast<const Value*>(g.x) + (there ? t : 0) * g.x_stride;
             const int64_t cols = there ? g.k : 0;
-            float v[kKept][8];
+            Eight<Value> v[kKept];
 #pragma unroll
             for (int h = 0; h < kKept; ++h)
-                load_eight(row, from + h * step, cols, v[h]);
+                v[h] = load_eight(row, from + h * step, cols);
             if (t0 == 0)
                 load(0, blockIdx.x, even);
             uint32_t top = 0;
-            const auto look = [&](const float (&u)[8]) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    top = max(top, __float_as_uint(u[e]) & 0x7FFFFFFFu);
-            };
 #pragma unroll
             for (int h = 0; h < kKept; ++h)
-                look(v[h]);
-            for (int64_t at = from + kKept * step; at < cols; at += step) {
-                float u[8];
-                load_eight(row, at, cols, u);
-                look(u);
-            }
+                top = v[h].largest(top);
+            for (int64_t at = from + kKept * step; at < cols; at += step)
+                top = load_eight(row, at, cols).largest(top);
 #pragma unroll
             for (int o = 32; o >= 1; o >>= 1)
                 top = max(top, uint32_t(__shfl_xor(int(top), o, 64)));
@@ -417,12 +415,10 @@ __global__ __launch_bounds__(64 * kHeldWaves) void k_int8_held(HeldArgs g)
             for (int h = 0; h < kKept; ++h)
                 if (from + h * step < g.pitch)
                     *reinterpret_cast<uint2*>(codes + t * code_row + from + h * step) =
-                        codes_of(v[h], scale);
-            for (int64_t at = from + kKept * step; at < g.pitch; at += step) {
-                float u[8];
-                load_eight(row, at, cols, u);
-                *reinterpret_cast<uint2*>(codes + t * code_row + at) = codes_of(u, scale);
-            }
+                        v[h].codes(scale);
+            for (int64_t at = from + kKept * step; at < g.pitch; at += step)
+                *reinterpret_cast<uint2*>(codes + t * code_row + at) =
+                    load_eight(row, at, cols).codes(scale);
         }
         __syncthreads();
         const uint8_t* p = codes + token * code_row + int64_t(first) * 128 + 32 * q;
@@ -530,20 +526,23 @@ lt_err launch_quantize(const void* x, int dtype, int64_t rows, int64_t cols, int
                        int8_t* codes, float* scales, hipStream_t st)
 {
     const QuantizeArgs a{x, rows, cols, stride, code_pitch(cols), codes, scales};
-    const auto go = [&](auto* kernel, int64_t rows_each) {
+    // by what measured fastest, see the kernel
+    const auto go = [&](auto* kernel, int64_t rows_each, int threads) {
         const int64_t groups = std::min<int64_t>(host::ceil_div(rows, rows_each), 1 << 20);
-        kernel<<<dim3(uint32_t(groups)), 256, 0, st>>>(a);
+        kernel<<<dim3(uint32_t(groups)), threads, 0, st>>>(a);
     };
     const auto pick = [&](auto zero) {
         typedef decltype(zero) T;
-        if (a.pitch <= 512)
-            go(k_int8_quantize<T, 1, 1>, 4);
+        if (a.pitch <= 1024)
+            go(k_int8_quantize<T, 1, 1>, 4, 256);
         else if (a.pitch <= 2048)
-            go(k_int8_quantize<T, 4, 1>, 1);
-        else if (a.pitch <= 4096)
-            go(k_int8_quantize<T, 4, 2>, 1);
+            go(k_int8_quantize<T, 4, 1>, 1, 256);
+        else if (a.pitch <= 6144)
+            go(k_int8_quantize<T, 4, 2>, 1, 256);
+        else if (a.pitch <= 8192)
+            go(k_int8_quantize<T, 4, 4>, 1, 256);
         else
-            go(k_int8_quantize<T, 4, 4>, 1);
+            go(k_int8_quantize<T, 16, 1>, 1, 1024);
     };
     if (dtype == LT_DTYPE_BF16)
         pick(uint16_t());

@@ -103,7 +103,7 @@ class Int8Weight:
         if w.dim() != 2:
             raise ValueError(f"w must be a matrix (two dimensions, got {w.dim()})")
         weight = cls.empty(w.shape[0], w.shape[1], w.device)
-        weight.update(w)
+        lt_int8_quantize(_laid_out(w, aligned=False), weight.codes, weight.scales)
         return weight
 
     def update(self, w: torch.Tensor, stream=None) -> None:
