@@ -299,6 +299,15 @@ struct Way {
     int slice;   // steps of each
 };
 
+// What a tile costs a CU, in microseconds: each step, and beside its steps.
+struct Cost {
+    int tile;
+    double step, rest;
+};
+
+constexpr Cost kCosts[] = {{256, 1.33, 14.0}, {128, 0.5, 2.0}, {64, 0.18, 0.6}};
+constexpr Cost kPairCosts[] = {{256, 1.33, 14.0}, {128, 0.5, 2.0}, {64, 0.29, 1.0}};
+
 // The tile and the slices of the sum that a launch is expected to end first with.  The CU with the
 // most tiles sets its time; a tile costs so many microseconds a step and beside its steps, and
 // slices another launch and their sums' way to memory and back (4 TB/s).  Fitted to products of 16
@@ -309,18 +318,11 @@ struct Way {
 // `pair`: a tile's columns are two weights'; such sums are not cut.
 inline Way way_of(int64_t m, int64_t n, int64_t count, int steps, bool pair)
 {
-    struct Cost {
-        int tile;
-        double step, rest;
-    };
-    const Cost costs[] = {{256, 1.33, 14.0},
-                          {128, 0.5, 2.0},
-                          {64, pair ? 0.29 : 0.18, pair ? 1.0 : 0.6}};
     Way best{64, 1, steps};
     if (steps <= 0)
         return best;
     double least = 1e300;
-    for (const Cost& c : costs) {
+    for (const Cost& c : pair ? kPairCosts : kCosts) {
         const int64_t wide = pair && c.tile > 64 ? c.tile / 2 : c.tile;
         const int64_t tiles = (m + c.tile - 1) / c.tile * ((n + wide - 1) / wide) * count;
         const int most_slices = pair ? 1 : std::min(64, std::max(1, steps / 8));

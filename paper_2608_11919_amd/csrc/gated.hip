@@ -272,8 +272,8 @@ __global__ __launch_bounds__(256) void k_gated_slopes(SlopeArgs g)
     *reinterpret_cast<i32x4*>(to + g.half) = __builtin_bit_cast(i32x4, du);
 }
 
-// dx = [dg | du] [gate; up], or (DW) dgate = dg^T x and dup = du^T x.  No operand is turned in
-// memory: what has the summed index as rows is turned on its way out of LDS.
+// dx = [dg | du] [gate; up], or dgate = dg^T x and dup = du^T x.  No operand is turned in memory:
+// what has the summed index as rows is turned on its way out of LDS.
 struct ProductArgs {
     const uint8_t* a;    // dg and du by rows
     int64_t a_pitch;     // bytes
@@ -281,38 +281,51 @@ struct ProductArgs {
     int64_t b_cols;      // a multiple of 8
     int64_t m, n;        // of one result
     int count;           // results
-    int steps, slice;
+    int steps, slice, slices;
     void* out[2];
     int64_t stride[2];
-    float* partial;  // several slices: [slice][count][m][n]
+    int f32;
+    float* partial;      // several slices: [slice][count][m][n]
+    uint32_t tiles;      // of a slice
 };
 
-template <bool F32>
+// Both in one launch: neither needs the other, and the workgroups of one fill the CUs that the
+// other leaves.
+struct ProductsArgs {
+    ProductArgs dx, dw;
+    uint32_t dx_first, dw_first, dx_end, dw_end;  // workgroups
+};
+
 struct ProductWriter {
     static constexpr bool kTurned = false;
     static constexpr int kSlots = 8;
     void* out;
     int64_t stride, rows, cols;  // from the tile's origin on
+    bool f32;
     __device__ inline void fetch(int, int, int) {}
     __device__ inline void turn(int, int, const float (&)[8]) {}
     __device__ inline void store(int row, int col, float (&v)[8], int)
     {
-        if (row < rows && col < cols)
-            store_row<F32>(out, row * stride + col, v, cols - col);
+        if (row >= rows || col >= cols)
+            return;
+        if (f32)
+            store_row<true>(out, row * stride + col, v, cols - col);
+        else
+            store_row<false>(out, row * stride + col, v, cols - col);
     }
 };
 
-template <typename Tile, bool F32, bool DW>
-__global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_gated_product(ProductArgs g)
+template <typename Tile, bool DW>
+__device__ inline void gated_product(const ProductArgs& g, uint32_t group, uint8_t* lds)
 {
-    __shared__ __align__(1024) uint8_t lds[Tile::kLdsBytes];
     const int down = int((g.m + Tile::kRows - 1) / Tile::kRows);
     const int across = int((g.n + Tile::kCols - 1) / Tile::kCols);
-    const int64_t unit = unit_of_workgroup(Tile::kRun);
+    const int part = int(group / g.tiles);
+    const int64_t unit = unit_of_workgroup(group % g.tiles, g.tiles, Tile::kRun);
     const int which = unit >= int64_t(down) * across ? 1 : 0;
     const TilePlace at = tile_place(int(unit - int64_t(which) * down * across), down, across);
     const int64_t r0 = int64_t(at.row) * Tile::kRows, c0 = int64_t(at.col) * Tile::kCols;
-    const int first = int(blockIdx.y) * g.slice, steps = min(g.slice, g.steps - first);
+    const int first = part * g.slice, steps = min(g.slice, g.steps - first);
     Tile tile;
     Bf16<Tile::kPinned> mul;
     TurnedOperand<Tile, Tile::kCols, Tile::J> q;
@@ -343,40 +356,44 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_gated_p
         p.load.init(g.a_pitch, g.m - r0);
         product(mul, tile, p, q, steps, lds);
     }
-    if (g.partial) {
-        ProductWriter<true> p;
-        p.rows = g.m - r0;
-        p.cols = g.n - c0;
-        p.stride = g.n;
-        p.out = g.partial + ((int64_t(blockIdx.y) * g.count + which) * g.m + r0) * g.n + c0;
-        finish(tile, lds, p);
-        return;
-    }
-    ProductWriter<F32> w;
+    ProductWriter w;
     w.rows = g.m - r0;
     w.cols = g.n - c0;
-    w.stride = which ? g.stride[1] : g.stride[0];
-    void* out = which ? g.out[1] : g.out[0];
-    w.out = F32 ? static_cast<void*>(static_cast<float*>(out) + r0 * w.stride + c0)
-                : static_cast<void*>(static_cast<uint16_t*>(out) + r0 * w.stride + c0);
+    w.stride = g.partial ? g.n : which ? g.stride[1] : g.stride[0];
+    w.f32 = g.partial || g.f32;
+    const int64_t to = r0 * w.stride + c0;
+    if (g.partial)
+        w.out = g.partial + (int64_t(part) * g.count + which) * g.m * g.n + to;
+    else
+        w.out = static_cast<uint8_t*>(which ? g.out[1] : g.out[0]) + to * (g.f32 ? 4 : 2);
     finish(tile, lds, w);
 }
 
+template <typename Tile>
+__global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_gated_products(
+    ProductsArgs g)
+{
+    __shared__ __align__(1024) uint8_t lds[Tile::kLdsBytes];
+    if (blockIdx.x >= g.dx_first && blockIdx.x < g.dx_end)
+        gated_product<Tile, false>(g.dx, blockIdx.x - g.dx_first, lds);
+    else
+        gated_product<Tile, true>(g.dw, blockIdx.x - g.dw_first, lds);
+}
+
 // out = the slices' sums, added in their order.
-template <bool F32>
-__global__ __launch_bounds__(256) void k_gated_join(ProductArgs g, int slices)
+__global__ __launch_bounds__(256) void k_gated_join(ProductArgs g)
 {
     const int64_t one = g.m * g.n, all = one * g.count;
     for (int64_t e = int64_t(blockIdx.x) * 256 + threadIdx.x; e < all;
          e += int64_t(gridDim.x) * 256) {
         float s = g.partial[e];
-        for (int i = 1; i < slices; ++i)
+        for (int i = 1; i < g.slices; ++i)
             s += g.partial[i * all + e];
         const int which = e >= one ? 1 : 0;
         const int64_t i = e - which * one;
         const int64_t to = i / g.n * (which ? g.stride[1] : g.stride[0]) + i % g.n;
         void* out = which ? g.out[1] : g.out[0];
-        if constexpr (F32)
+        if (g.f32)
             static_cast<float*>(out)[to] = s;
         else
             static_cast<uint16_t*>(out)[to] = gated::bf16_bits(s);
@@ -475,10 +492,74 @@ TurnedPlace turned_place(int64_t& total, int64_t rows, int64_t k, int64_t stride
     return p;
 }
 
+// A matrix product of the backward pass, as its launch is planned: `count` results of m x n.
+struct Plan {
+    int64_t m = 0, n = 0, count = 0;
+    int steps = 0, slice = 0, slices = 1;
+    double us(const gated::Cost& c) const { return c.step * slice + c.rest; }
+    int64_t tiles(const gated::Cost& c) const
+    {
+        return host::ceil_div(m, c.tile) * host::ceil_div(n, c.tile) * count;
+    }
+    int64_t partial() const { return slices > 1 ? slices * count * m * n * 4 : 0; }
+    bool cut(int z)  // into z slices, if they are that many and long enough
+    {
+        slice = int(host::ceil_div(steps, z));
+        slices = z;
+        return z == 1 || (slice >= 8 && host::ceil_div(steps, slice) == z && partial() < 270000000);
+    }
+};
+
+// The tile of a launch with one or both, and their slices, by expected time: see gated::way_of.
+// The CUs share all tiles; the last of them leave some idle for half the time of the shorter.
+int plan(Plan* dx, Plan* dw)
+{
+    int best = 64;
+    double least = 1e300;
+    Plan one, other;
+    const int cuts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+    for (const gated::Cost& c : gated::kCosts) {
+        for (const int zx : cuts) {
+            Plan x = dx ? *dx : Plan();
+            if (dx ? !x.cut(zx) : zx > 1)
+                continue;
+            for (const int zw : cuts) {
+                Plan w = dw ? *dw : Plan();
+                if (dw ? !w.cut(zw) : zw > 1)
+                    continue;
+                const double tx = dx ? x.us(c) : 0.0, tw = dw ? w.us(c) : 0.0;
+                const int64_t nx = dx ? x.tiles(c) * x.slices : 0;
+                const int64_t nw = dw ? w.tiles(c) * w.slices : 0;
+                double us = std::max(tx, tw);
+                if (nx + nw > 256) {
+                    const double last = dx && dw ? std::min(tx, tw) : us;
+                    us = std::max(us, (nx * tx + nw * tw) / 256 + 0.5 * last);
+                }
+                for (const Plan* p : {&x, &w})
+                    if (p->slices > 1)
+                        us += 5.0 + 2.0 * double(p->partial()) / 4e6;
+                if (us < least) {
+                    least = us;
+                    best = c.tile;
+                    one = x;
+                    other = w;
+                }
+            }
+        }
+    }
+    if (dx)
+        *dx = one;
+    if (dw)
+        *dw = other;
+    return best;
+}
+
 struct BackwardLayout {
-    int64_t slopes = -1, partial = -1;
+    int64_t slopes = -1, dx_sums = -1, dw_sums = -1;
     TurnedPlace gate, up, x;
     int64_t total = 0;
+    Plan dx, dw;
+    int tile = 0;
 };
 
 BackwardLayout backward_layout(int64_t m, int64_t n, int64_t k, int64_t x_stride,
@@ -486,23 +567,21 @@ BackwardLayout backward_layout(int64_t m, int64_t n, int64_t k, int64_t x_stride
 {
     BackwardLayout l;
     l.slopes = take(l.total, padded(m) * 2 * padded(n) * 2);
-    int64_t partial = 0;
     if (dx) {
         const bool as_it_is = turnable(k, gate_stride) && gate_stride == up_stride;
         l.gate = turned_place(l.total, n, k, gate_stride, as_it_is);
         l.up = turned_place(l.total, n, k, up_stride, as_it_is);
-        const Way w = way_of(m, k, 1, int(2 * padded(n) / kStep), false);
-        if (w.slices > 1)
-            partial = w.slices * m * k * 4;
+        l.dx = Plan{m, k, 1, int(2 * padded(n) / kStep)};
     }
     if (dw) {
         l.x = turned_place(l.total, m, k, x_stride, turnable(k, x_stride));
-        const Way w = way_of(n, k, 2, int(padded(m) / kStep), false);
-        if (w.slices > 1)
-            partial = std::max(partial, w.slices * 2 * n * k * 4);
+        l.dw = Plan{n, k, 2, int(padded(m) / kStep)};
     }
-    if (partial)
-        l.partial = take(l.total, partial);
+    l.tile = plan(dx ? &l.dx : nullptr, dw ? &l.dw : nullptr);
+    if (l.dx.partial())
+        l.dx_sums = take(l.total, l.dx.partial());
+    if (l.dw.partial())
+        l.dw_sums = take(l.total, l.dw.partial());
     l.total = std::max<int64_t>(l.total, 256);
     return l;
 }
@@ -561,33 +640,39 @@ void launch_forward(const ForwardArgs& g, bool f32, bool save, hipStream_t st)
              Tile::kThreads, 0, st>>>(g);
 }
 
+// The products that are planned, the one with the longer tiles first.
 template <typename Tile>
-void launch_product(const ProductArgs& g, const Way& w, bool f32, bool dw, hipStream_t st)
+void launch_products(ProductsArgs g, bool dx, bool dw, hipStream_t st)
 {
-    const dim3 grid(uint32_t(host::ceil_div(g.m, Tile::kRows) * host::ceil_div(g.n, Tile::kCols) *
-                             g.count),
-                    uint32_t(w.slices));
-    auto* kernel = dw ? (f32 ? k_gated_product<Tile, true, true> : k_gated_product<Tile, false, true>)
-                      : (f32 ? k_gated_product<Tile, true, false>
-                             : k_gated_product<Tile, false, false>);
-    kernel<<<grid, Tile::kThreads, 0, st>>>(g);
+    const auto groups = [](ProductArgs& p) {
+        p.tiles = uint32_t(host::ceil_div(p.m, Tile::kRows) * host::ceil_div(p.n, Tile::kCols) *
+                           p.count);
+        return p.tiles * uint32_t(p.slices);
+    };
+    const uint32_t nx = dx ? groups(g.dx) : 0, nw = dw ? groups(g.dw) : 0;
+    const bool dx_first = !dw || (dx && g.dx.slice >= g.dw.slice);
+    g.dx_first = dx_first ? 0 : nw;
+    g.dw_first = dx_first ? nx : 0;
+    g.dx_end = g.dx_first + nx;
+    g.dw_end = g.dw_first + nw;
+    k_gated_products<Tile><<<dim3(nx + nw), Tile::kThreads, 0, st>>>(g);
+    for (const ProductArgs* p : {&g.dx, &g.dw})
+        if (p->partial)
+            k_gated_join<<<dim3(groups_for(p->m * p->n * p->count)), 256, 0, st>>>(*p);
 }
 
-void run_product(ProductArgs g, bool f32, bool dw, uint8_t* partial, hipStream_t st)
+// The planned part of a product's arguments.
+ProductArgs planned(const Plan& p, uint8_t* partial)
 {
-    const Way w = way_of(g.m, g.n, g.count, g.steps, false);
-    g.slice = w.slice;
-    g.partial = w.slices > 1 ? reinterpret_cast<float*>(partial) : nullptr;
-    if (w.tile == 256)
-        launch_product<Large16>(g, w, f32, dw, st);
-    else if (w.tile == 128)
-        launch_product<Small16>(g, w, f32, dw, st);
-    else
-        launch_product<Tiny16>(g, w, f32, dw, st);
-    if (g.partial) {
-        auto* join = f32 ? k_gated_join<true> : k_gated_join<false>;
-        join<<<dim3(groups_for(g.m * g.n * g.count)), 256, 0, st>>>(g, w.slices);
-    }
+    ProductArgs g{};
+    g.m = p.m;
+    g.n = p.n;
+    g.count = int(p.count);
+    g.steps = p.steps;
+    g.slice = p.slice;
+    g.slices = p.slices;
+    g.partial = reinterpret_cast<float*>(partial);
+    return g;
 }
 
 struct Read {
@@ -833,44 +918,38 @@ try {
         k_gated_slopes<true><<<blocks, 256, 0, st>>>(s);
     else
         k_gated_slopes<false><<<blocks, 256, 0, st>>>(s);
-    uint8_t* partial = l.partial < 0 ? nullptr : ws + l.partial;
-    ProductArgs g{};
-    g.a = ws + l.slopes;
-    g.a_pitch = 4 * half;
-    ProductArgs to_x = g, to_w = g;
+    ProductsArgs g{};
+    g.dx = planned(l.dx, l.dx_sums < 0 ? nullptr : ws + l.dx_sums);
+    g.dw = planned(l.dw, l.dw_sums < 0 ? nullptr : ws + l.dw_sums);
     Copies copies;
     if (dx) {
-        turned_operand(l.gate, gate, n, k, gate_stride, ws, copies, &to_x.b, 0);
-        turned_operand(l.up, up, n, k, up_stride, ws, copies, &to_x.b, 1);
+        turned_operand(l.gate, gate, n, k, gate_stride, ws, copies, &g.dx.b, 0);
+        turned_operand(l.up, up, n, k, up_stride, ws, copies, &g.dx.b, 1);
+        g.dx.b_cols = l.gate.whole ? padded(k) : k;
+        g.dx.out[0] = dx;
+        g.dx.stride[0] = dx_stride;
+        g.dx.f32 = dx_dtype == LT_DTYPE_F32;
     }
     if (want_dw) {
-        turned_operand(l.x, x, m, k, x_stride, ws, copies, &to_w.b, 0);
-        to_w.b.base[1] = to_w.b.base[0];
-        to_w.b.tail[1] = to_w.b.tail[0];
+        turned_operand(l.x, x, m, k, x_stride, ws, copies, &g.dw.b, 0);
+        g.dw.b.base[1] = g.dw.b.base[0];
+        g.dw.b.tail[1] = g.dw.b.tail[0];
+        g.dw.b_cols = l.x.whole ? padded(k) : k;
+        g.dw.out[0] = dgate;
+        g.dw.out[1] = dup;
+        g.dw.stride[0] = dgate_stride;
+        g.dw.stride[1] = dup_stride;
+        g.dw.f32 = grad_dtype == LT_DTYPE_F32;
     }
+    g.dx.a = g.dw.a = ws + l.slopes;
+    g.dx.a_pitch = g.dw.a_pitch = 4 * half;
     copies.launch(st);
-    if (dx) {
-        to_x.b_cols = l.gate.whole ? padded(k) : k;
-        to_x.m = m;
-        to_x.n = k;
-        to_x.count = 1;
-        to_x.steps = int(2 * half / kStep);
-        to_x.out[0] = dx;
-        to_x.stride[0] = dx_stride;
-        run_product(to_x, dx_dtype == LT_DTYPE_F32, false, partial, st);
-    }
-    if (want_dw) {
-        to_w.b_cols = l.x.whole ? padded(k) : k;
-        to_w.m = n;
-        to_w.n = k;
-        to_w.count = 2;
-        to_w.steps = int(tokens / kStep);
-        to_w.out[0] = dgate;
-        to_w.out[1] = dup;
-        to_w.stride[0] = dgate_stride;
-        to_w.stride[1] = dup_stride;
-        run_product(to_w, grad_dtype == LT_DTYPE_F32, true, partial, st);
-    }
+    if (l.tile == 256)
+        launch_products<Large16>(g, dx != nullptr, want_dw, st);
+    else if (l.tile == 128)
+        launch_products<Small16>(g, dx != nullptr, want_dw, st);
+    else
+        launch_products<Tiny16>(g, dx != nullptr, want_dw, st);
     LT_TRY_HIP(hipGetLastError());
     return LT_OK;
 } catch (...) {

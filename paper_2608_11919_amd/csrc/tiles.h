@@ -297,12 +297,16 @@ struct Shape {
 // The work unit of this workgroup.  Workgroups go to the eight XCDs in turn, each with an L2 of
 // its own; units are dealt out so that an XCD works on `run` consecutive units at a time (as
 // many as it holds workgroups), which tile_place makes neighbours that share operands.
-__device__ inline int64_t unit_of_workgroup(int run)
+__device__ inline int64_t unit_of_workgroup(uint32_t b, uint32_t n, int run)
 {
-    const uint32_t n = gridDim.x, b = blockIdx.x, round = 8u * uint32_t(run);
+    const uint32_t round = 8u * uint32_t(run);
     const uint32_t base = b / round * round, here = min(round, n - base);
     const uint32_t x = b % 8u, i = (b - base) / 8u;
     return int64_t(base + x * (here / 8u) + min(x, here % 8u) + i);
+}
+__device__ inline int64_t unit_of_workgroup(int run)
+{
+    return unit_of_workgroup(blockIdx.x, gridDim.x, run);
 }
 
 // Row and column of the t-th tile of `down` x `across`: strips of eight rows, column by column.
