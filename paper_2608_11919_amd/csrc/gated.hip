@@ -45,9 +45,8 @@ struct Layouts {
 
 constexpr int64_t kPackLines = 256 * 4;  // of 16 bytes, to a workgroup
 
-__global__ __launch_bounds__(256) void k_gated_pack(Layouts g)
+__device__ inline void pack(const Layouts& g, uint32_t group)
 {
-    const uint32_t group = blockIdx.x;
     const Layout& a = g.of[g.count > 2 && group >= g.of[2].first
                                ? 2
                                : g.count > 1 && group >= g.of[1].first ? 1 : 0];
@@ -70,6 +69,8 @@ __global__ __launch_bounds__(256) void k_gated_pack(Layouts g)
         *reinterpret_cast<i32x4*>(a.out + row * a.pitch + col) = __builtin_bit_cast(i32x4, v);
     }
 }
+
+__global__ __launch_bounds__(256) void k_gated_pack(Layouts g) { pack(g, blockIdx.x); }
 
 struct ZeroArgs {
     void* out;
@@ -212,12 +213,18 @@ struct SlopeArgs {
     int64_t m, n;
     uint16_t* out;
     int64_t half, rows;
+    Layouts copies;      // what the products read besides, by the workgroups behind
+    uint32_t own;        // workgroups before those
 };
 
 // Eight channels of a token to a lane.  Bound by HBM: 8 bytes read and 4 written a value.
 template <bool F32>
 __global__ __launch_bounds__(256) void k_gated_slopes(SlopeArgs g)
 {
+    if (blockIdx.x >= g.own) {
+        pack(g.copies, blockIdx.x - g.own);
+        return;
+    }
     const int64_t lines = g.half / 8, all = g.rows * lines;
     const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
     if (i >= all)
@@ -911,13 +918,6 @@ try {
         return e;
     const int64_t half = padded(n), tokens = padded(m);
     auto* slopes = reinterpret_cast<uint16_t*>(ws + l.slopes);
-    const SlopeArgs s{dh, dh_stride, saved_layout(const_cast<void*>(saved), m, n), m, n, slopes,
-                      half, tokens};
-    const dim3 blocks(uint32_t(host::ceil_div(tokens * (half / 8), 256)));
-    if (dh_dtype == LT_DTYPE_F32)
-        k_gated_slopes<true><<<blocks, 256, 0, st>>>(s);
-    else
-        k_gated_slopes<false><<<blocks, 256, 0, st>>>(s);
     ProductsArgs g{};
     g.dx = planned(l.dx, l.dx_sums < 0 ? nullptr : ws + l.dx_sums);
     g.dw = planned(l.dw, l.dw_sums < 0 ? nullptr : ws + l.dw_sums);
@@ -943,7 +943,14 @@ try {
     }
     g.dx.a = g.dw.a = ws + l.slopes;
     g.dx.a_pitch = g.dw.a_pitch = 4 * half;
-    copies.launch(st);
+    const auto own = uint32_t(host::ceil_div(tokens * (half / 8), 256));
+    const SlopeArgs s{dh,   dh_stride, saved_layout(const_cast<void*>(saved), m, n), m, n, slopes,
+                      half, tokens,    copies.of, own};
+    const dim3 blocks(own + uint32_t(copies.groups));
+    if (dh_dtype == LT_DTYPE_F32)
+        k_gated_slopes<true><<<blocks, 256, 0, st>>>(s);
+    else
+        k_gated_slopes<false><<<blocks, 256, 0, st>>>(s);
     if (l.tile == 256)
         launch_products<Large16>(g, dx != nullptr, want_dw, st);
     else if (l.tile == 128)
