@@ -499,14 +499,32 @@ TurnedPlace turned_place(int64_t& total, int64_t rows, int64_t k, int64_t stride
     return p;
 }
 
+// What a tile of these products costs, in microseconds: a step where every CU is busy and where
+// it has the CU to itself (the smaller tiles wait for their operands then), and beside its steps.
+struct TurnedCost {
+    int tile;
+    double step, alone, rest;
+};
+
+constexpr TurnedCost kTurnedCosts[] = {
+    {256, 1.45, 1.45, 14.0}, {128, 0.65, 0.6, 2.0}, {64, 0.25, 0.4, 0.8}};
+
 // A matrix product of the backward pass, as its launch is planned: `count` results of m x n.
 struct Plan {
     int64_t m = 0, n = 0, count = 0;
     int steps = 0, slice = 0, slices = 1;
-    double us(const gated::Cost& c) const { return c.step * slice + c.rest; }
-    int64_t tiles(const gated::Cost& c) const
+    double alone(const TurnedCost& c) const { return c.alone * slice + c.rest; }
+    double busy(const TurnedCost& c) const { return c.step * slice + c.rest; }
+    int64_t tiles(const TurnedCost& c) const
     {
         return host::ceil_div(m, c.tile) * host::ceil_div(n, c.tile) * count;
+    }
+    // what the tiles read
+    double bytes(const TurnedCost& c) const
+    {
+        return double(count) * steps * kStepBytes *
+               (double(m) * double(host::ceil_div(n, c.tile)) +
+                double(n) * double(host::ceil_div(m, c.tile)));
     }
     int64_t partial() const { return slices > 1 ? slices * count * m * n * 4 : 0; }
     bool cut(int z)  // into z slices, if they are that many and long enough
@@ -517,42 +535,59 @@ struct Plan {
     }
 };
 
-// The tile of a launch with one or both, and their slices, by expected time: see gated::way_of.
-// The CUs share all tiles; the last of them leave some idle for half the time of the shorter.
+// The tile of a launch with one or both, and their slices, by expected time: the longest tile, or
+// all tiles' work shared by the CUs and half of the last tiles, which leave some idle; what they
+// read, at 12 TB/s out of L2 and behind it; another launch for the sums of slices, and those to
+// memory and back (4 TB/s).  Fitted to 64 to 10000 tokens through 128 x 2048 to 5120 x 17408.
 int plan(Plan* dx, Plan* dw)
 {
+    struct Choice {
+        Plan plan;
+        double alone, busy, work, sums;
+        int64_t tiles;
+    };
+    const int cuts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+    constexpr int kCuts = sizeof(cuts) / sizeof(cuts[0]);
+    const auto choices = [&](const Plan* of, const TurnedCost& c, Choice (&to)[kCuts]) {
+        if (!of) {
+            to[0] = Choice{};
+            return 1;
+        }
+        int n = 0;
+        for (const int z : cuts) {
+            Plan p = *of;
+            if (!p.cut(z))
+                continue;
+            const int64_t tiles = p.tiles(c) * p.slices;
+            to[n++] = {p, p.alone(c), p.busy(c), tiles * p.busy(c) / 256,
+                       p.slices > 1 ? 5.0 + 2.0 * double(p.partial()) / 4e6 : 0.0, tiles};
+        }
+        return n;
+    };
     int best = 64;
     double least = 1e300;
     Plan one, other;
-    const int cuts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
-    for (const gated::Cost& c : gated::kCosts) {
-        for (const int zx : cuts) {
-            Plan x = dx ? *dx : Plan();
-            if (dx ? !x.cut(zx) : zx > 1)
-                continue;
-            for (const int zw : cuts) {
-                Plan w = dw ? *dw : Plan();
-                if (dw ? !w.cut(zw) : zw > 1)
-                    continue;
-                const double tx = dx ? x.us(c) : 0.0, tw = dw ? w.us(c) : 0.0;
-                const int64_t nx = dx ? x.tiles(c) * x.slices : 0;
-                const int64_t nw = dw ? w.tiles(c) * w.slices : 0;
-                double us = std::max(tx, tw);
-                if (nx + nw > 256) {
-                    const double last = dx && dw ? std::min(tx, tw) : us;
-                    us = std::max(us, (nx * tx + nw * tw) / 256 + 0.5 * last);
+    Choice xs[kCuts], ws[kCuts];
+    for (const TurnedCost& c : kTurnedCosts) {
+        const double read = (dx ? dx->bytes(c) : 0.0) + (dw ? dw->bytes(c) : 0.0);
+        const int nx = choices(dx, c, xs), nw = choices(dw, c, ws);
+        for (int i = 0; i < nx; ++i)
+            for (int j = 0; j < nw; ++j) {
+                const Choice &x = xs[i], &w = ws[j];
+                double us = std::max(x.alone, w.alone);
+                if (x.tiles + w.tiles > 256) {
+                    const double last = dx && dw ? std::min(x.busy, w.busy)
+                                                 : std::max(x.busy, w.busy);
+                    us = std::max(us, x.work + w.work + 0.5 * last);
                 }
-                for (const Plan* p : {&x, &w})
-                    if (p->slices > 1)
-                        us += 5.0 + 2.0 * double(p->partial()) / 4e6;
+                us += read / 12e6 + x.sums + w.sums;
                 if (us < least) {
                     least = us;
                     best = c.tile;
-                    one = x;
-                    other = w;
+                    one = x.plan;
+                    other = w.plan;
                 }
             }
-        }
     }
     if (dx)
         *dx = one;
