@@ -695,9 +695,20 @@ void launch_products(ProductsArgs g, bool dx, bool dw, hipStream_t st)
     const bool dx_first = !dw || (dx && g.dx.slice >= g.dw.slice);
     g.dx_first = dx_first ? 0 : nw;
     g.dw_first = dx_first ? nx : 0;
-    g.dx_end = g.dx_first + nx;
-    g.dw_end = g.dw_first + nw;
-    k_gated_products<Tile><<<dim3(nx + nw), Tile::kThreads, 0, st>>>(g);
+    const auto launch = [&](uint32_t x, uint32_t w) {
+        g.dx_end = g.dx_first + x;
+        g.dw_end = g.dw_first + w;
+        k_gated_products<Tile><<<dim3(x + w), Tile::kThreads, 0, st>>>(g);
+    };
+    if (nx >= 1024 && nw >= 1024) {
+        // rounds enough to fill the chip alone, where the two would share its L2 for a while: 16384
+        // tokens through 5120 x 17408 8.78 ms, in one launch 8.86
+        g.dx_first = g.dw_first = 0;
+        launch(nx, 0);
+        launch(0, nw);
+    } else {
+        launch(nx, nw);
+    }
     for (const ProductArgs* p : {&g.dx, &g.dw})
         if (p->partial)
             k_gated_join<<<dim3(groups_for(p->m * p->n * p->count)), 256, 0, st>>>(*p);
