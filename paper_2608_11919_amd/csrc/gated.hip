@@ -108,25 +108,23 @@ Saved saved_layout(void* saved, int64_t m, int64_t n)
     return s;
 }
 
-__device__ inline uint32_t round_24(float x)
-{
-    const uint32_t b = __float_as_uint(x);
-    // to nearest; an infinity or a NaN keeps its bits (a NaN that has its all in the last byte
-    // becomes one that has not)
-    return (b & 0x7F800000u) == 0x7F800000u ? b | ((b & 0xFFu) != 0u ? 0x400000u : 0u) : b + 0x80u;
-}
-
+// Eight values in 24 bits, rounded to nearest (halves away from zero) by a sum: an infinity stays
+// one, and so does a NaN, whose payload comes from bf16 operands or the hardware and leaves the
+// last byte clear.
 __device__ inline void save_eight(uint16_t* high, uint8_t* low, int64_t at, const float (&v)[8])
 {
-    uint32_t h[4], l[2] = {0, 0};
+    uint32_t r[8], h[4], l[4];
 #pragma unroll
-    for (int e = 0; e < 8; e += 2) {
-        const uint32_t x = round_24(v[e]), y = round_24(v[e + 1]);
-        h[e / 2] = x >> 16 | (y & 0xFFFF0000u);
-        l[e / 4] |= (x >> 8 & 0xFFu) << (8 * (e % 4)) | (y >> 8 & 0xFFu) << (8 * (e % 4) + 8);
+    for (int e = 0; e < 8; ++e)
+        r[e] = __float_as_uint(v[e]) + 0x80u;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {  // bytes 3 and 2 of either, and byte 1
+        h[e] = __builtin_amdgcn_perm(r[2 * e + 1], r[2 * e], 0x07060302u);
+        l[e] = __builtin_amdgcn_perm(r[2 * e + 1], r[2 * e], 0x0C0C0501u);
     }
     *reinterpret_cast<uint4*>(high + at) = make_uint4(h[0], h[1], h[2], h[3]);
-    *reinterpret_cast<uint2*>(low + at) = make_uint2(l[0], l[1]);
+    *reinterpret_cast<uint2*>(low + at) =
+        make_uint2(l[0] | l[1] << 16, l[2] | l[3] << 16);
 }
 
 __device__ inline void load_eight(const uint16_t* high, const uint8_t* low, int64_t at,
