@@ -89,13 +89,15 @@ template <typename T>
 __device__ inline Eight<T> load_eight(const T* row, int64_t at, int64_t cols)
 {
     constexpr int kLines = sizeof(T) / 2, kEach = 8 / kLines;
-    Eight<T> v;
+    Eight<T> v = {};
     if (at + 8 <= cols) {
 #pragma unroll
         for (int c = 0; c < kLines; ++c)
             v.w[c] = load_any(row + at + c * kEach);
         return v;
     }
+    if (at >= cols)
+        return v;
 #pragma unroll
     for (int c = 0; c < kLines; ++c)
 #pragma unroll
@@ -356,10 +358,20 @@ __global__ __launch_bounds__(64 * kHeldWaves) void k_int8_held(HeldArgs g)
             }
     };
 
+    // of a pair's rows both are under way as soon as there is room (16 tokens' codes through
+    // 5120 x 17408 41.8 to 40.7 us; blocks of one weight gained nothing, and the longest shares
+    // of values have no registers left)
+    constexpr bool kBoth = B == 2 && (X == kCodes || STEPS < 8);
+    const auto load_first = [&] {
+        load(0, blockIdx.x, even);
+        if constexpr (kBoth)
+            load(1, blockIdx.x, odd);
+    };
+
     Codes32 x[STEPS];
     const int64_t token = r < g.m ? r : g.m - 1;
     if constexpr (X == kCodes) {
-        load(0, blockIdx.x, even);
+        load_first();
         const uint8_t* p = static_cast<const uint8_t*>(g.x) + token * g.pitch +
                            int64_t(first) * 128 + 32 * q;
 #pragma unroll
@@ -389,7 +401,7 @@ __global__ __launch_bounds__(64 * kHeldWaves) void k_int8_held(HeldArgs g)
             for (int h = 0; h < kKept; ++h)
                 v[h] = load_eight(row, from + h * step, cols);
             if (t0 == 0)
-                load(0, blockIdx.x, even);
+                load_first();
             uint32_t top = 0;
 #pragma unroll
             for (int h = 0; h < kKept; ++h)
@@ -473,11 +485,15 @@ __global__ __launch_bounds__(64 * kHeldWaves) void k_int8_held(HeldArgs g)
     for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x, turn ^= 1) {
         const int64_t next = b + gridDim.x;
         if constexpr (B == 2) {
-            load(1, b, odd);
+            if constexpr (!kBoth)
+                load(1, b, odd);
             multiply(even, sums[turn][0]);
             if (next < blocks)
                 load(0, next, even);
             multiply(odd, sums[turn][1]);
+            if constexpr (kBoth)
+                if (next < blocks)
+                    load(1, next, odd);
             finish(b, turn);
         } else {
             if (next < blocks)

@@ -4,6 +4,7 @@ training, with the gradients of the tokens and of both weights.
 """
 from __future__ import annotations
 
+import weakref
 from typing import Optional, Tuple
 
 import torch
@@ -141,16 +142,8 @@ def _backward(dh, saved, x, gate, up, leading, shape, out_dtype, grad_dtype, wan
     return dx, dgate, dup
 
 
-_MADE_ON = "lazytrain_stream"
-
-
-def _accumulators(leaves):
-    """The nodes that take the leaves' gradients, made where no graph holds one, and which of them
-    are new: a note on a node that nothing else holds goes with it."""
-    for t in leaves:
-        torch.autograd.graph.get_gradient_edge(t).node.metadata[_MADE_ON + "?"] = True
-    nodes = [torch.autograd.graph.get_gradient_edge(t).node for t in leaves]
-    return [(n, n.metadata.pop(_MADE_ON + "?", None) is None) for n in nodes]
+# Graphs of GatedLinear that live and were made on the default stream, and the leaves they hold.
+_on_default = weakref.WeakSet()
 
 
 class GatedLinear(torch.autograd.Function):
@@ -161,29 +154,23 @@ class GatedLinear(torch.autograd.Function):
 
     Autograd adds up a leaf's gradient on the stream that its first graph was made on, for as long
     as a graph of the leaf lives.  Under capture that cannot be the default stream (the process would
-    end with the capture): a captured call whose leaves an earlier call's graph, made there, still
-    holds is refused."""
-
-    @classmethod
-    def apply(cls, x, gate, up, activation="silu"):
-        leaves = list({id(t): t for t in (x, gate, up)
-                       if t.is_cuda and t.is_leaf and t.requires_grad}.values())
-        if not leaves or not torch.is_grad_enabled():
-            return super().apply(x, gate, up, activation)
-        stream = torch.cuda.current_stream(x.device).cuda_stream
-        made = _accumulators(leaves)
-        for node, new in made:
-            if new:
-                node.metadata[_MADE_ON] = stream
-            elif node.metadata.get(_MADE_ON) == 0 and _capturing(None, x.device):
-                raise RuntimeError("GatedLinear is being captured while a graph made on the default "
-                                   "stream holds the same leaf: let go of that graph's results "
-                                   "first, or make it on another stream")
-        return super().apply(x, gate, up, activation)
+    end with the capture): a captured call is refused while the graph of an earlier call, made there,
+    holds one of its leaves."""
 
     @staticmethod
     def forward(ctx, x, gate, up, activation="silu"):
         want_dx, want_dw = ctx.needs_input_grad[0], any(ctx.needs_input_grad[1:3])
+        if x.is_cuda and (want_dx or want_dw):
+            # a graph holds its leaves: their ids stay theirs as long as it lives
+            leaves = {id(t) for t in (x, gate, up) if t.requires_grad and t.is_leaf}
+            if _stream_handle(None, x.device) == 0:
+                ctx.leaves = leaves
+                _on_default.add(ctx)
+            elif _capturing(None, x.device) and any(not leaves.isdisjoint(c.leaves)
+                                                    for c in list(_on_default)):
+                raise RuntimeError("GatedLinear is being captured while a graph made on the default "
+                                   "stream holds the same leaf: let go of that graph's results "
+                                   "first, or make it on another stream")
         h, saved = _forward(x, gate, up, activation, torch.bfloat16, want_dx or want_dw, None)
         ctx.save_for_backward(saved, x if want_dw else None, *((gate, up) if want_dx
                                                                else (None, None)))
