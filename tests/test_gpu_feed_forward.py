@@ -179,3 +179,29 @@ def test_results_do_not_change():
             want = call()
             for _ in range(3):
                 assert all(torch.equal(a, b) for a, b in zip(call(), want)), name
+
+
+def test_two_threads_at_once():
+    """Each with a stream of its own, over shared weights."""
+    import threading
+    gen = torch.Generator(DEV).manual_seed(7)
+    made = {tokens: calls(tokens, gen) for tokens in (3, 300)}
+    want = {t: {name: call() for name, (_, call) in m.items()} for t, m in made.items()}
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(tokens):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(20):
+                for name, (_, call) in made[tokens].items():
+                    got = call()
+                    torch.cuda.current_stream().synchronize()
+                    if not all(torch.equal(a, b) for a, b in zip(got, want[tokens][name])):
+                        wrong.append((tokens, name))
+
+    threads = [threading.Thread(target=work, args=(t,)) for t in (3, 300, 300)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(60)
+    assert not any(t.is_alive() for t in threads) and not wrong, wrong
