@@ -683,8 +683,9 @@ lt_err lt_int8_gated(const void* x, int dtype, int64_t x_stride, const int8_t* g
 size_t lt_gated_saved_bytes(int64_t m, int64_t n);
 
 /* Bytes of device workspace lt_gated_forward needs: copies of operands whose rows are not whole
- * steps of 64 values, or not multiples of 8 apart, else 256, which it does not look at (nor where
- * m <= 16 and nothing is saved).  0 if an argument is invalid. */
+ * steps of 64 values, not multiples of 8 or 2^22 and more apart, and partial sums where few results
+ * share a long sum; else 256, which it does not look at.  Nothing is copied or looked at where m <=
+ * 16, nothing is saved and k <= 4096 or an operand is such a one.  0 if an argument is invalid. */
 size_t lt_gated_forward_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t x_stride,
                                         int64_t gate_stride, int64_t up_stride);
 

@@ -149,6 +149,8 @@ struct ForwardArgs {
     void* out;
     int64_t stride;
     Saved saved;
+    int slice;       // steps of each slice of the sum
+    float* partial;  // several slices: [slice][weight][m][n]
 };
 
 template <bool F32, bool SAVE>
@@ -174,6 +176,12 @@ struct ForwardWriter {
             save_eight(g.saved.a_high, g.saved.a_low, at, a);
             save_eight(g.saved.b_high, g.saved.b_low, at, b);
         } else {
+            if (g.partial) {
+                const int64_t at = (int64_t(blockIdx.y) * 2 * g.m + row) * g.n + col;
+                store_row<true>(g.partial, at, u, g.n - col);
+                store_row<true>(g.partial, at + g.m * g.n, v, g.n - col);
+                return;
+            }
             gated::activate(g.activation, u, h);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -192,12 +200,162 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_gated_f
                                     int((g.m + Tile::kRows - 1) / Tile::kRows),
                                     int((g.n + kCols - 1) / kCols));
     const int64_t r0 = int64_t(at.row) * Tile::kRows, c0 = int64_t(at.col) * kCols;
+    const int first = int(blockIdx.y) * g.slice, steps = min(g.slice, g.steps - first);
     Tile tile;
     Bf16<Tile::kPinned> mul;
-    product_pairs(mul, tile, g.x + r0 * g.x_pitch, g.x_pitch, g.m - r0, g.gate + c0 * g.gate_pitch,
-                  g.gate_pitch, g.up + c0 * g.up_pitch, g.up_pitch, g.n - c0, g.steps, lds);
+    const int64_t k0 = int64_t(first) * kStepBytes;
+    product_pairs(mul, tile, g.x + r0 * g.x_pitch + k0, g.x_pitch, g.m - r0,
+                  g.gate + c0 * g.gate_pitch + k0, g.gate_pitch, g.up + c0 * g.up_pitch + k0,
+                  g.up_pitch, g.n - c0, steps, lds);
     ForwardWriter<F32, SAVE> w{g, r0, c0};
     finish_pairs(tile, lds, w);
+}
+
+// Results of the slices' sums, added in their order.
+template <bool F32>
+__global__ __launch_bounds__(256) void k_gated_answer(ForwardArgs g, int slices)
+{
+    const int64_t all = g.m * g.n;
+    for (int64_t e = int64_t(blockIdx.x) * 256 + threadIdx.x; e < all;
+         e += int64_t(gridDim.x) * 256) {
+        float u[1] = {g.partial[e]}, v = g.partial[all + e];
+        for (int i = 1; i < slices; ++i) {
+            u[0] += g.partial[2 * i * all + e];
+            v += g.partial[(2 * i + 1) * all + e];
+        }
+        float h[1];
+        gated::activate(g.activation, u, h);
+        const int64_t to = e / g.n * g.stride + e % g.n;
+        if constexpr (F32)
+            static_cast<float*>(g.out)[to] = h[0] * v;
+        else
+            static_cast<uint16_t*>(g.out)[to] = gated::bf16_bits(h[0] * v);
+    }
+}
+
+// ------------------------------------------------------------- few tokens
+
+struct FewArgs {
+    const uint8_t* w[2];    // rows of k values
+    int64_t w_pitch[2];     // bytes
+    const uint8_t* x;
+    int64_t x_pitch;
+    int64_t m, n;
+    int64_t bytes;          // of a row's values
+    int activation;
+    void* out;
+    int64_t stride;
+};
+
+// 32 bytes of a row from byte `at` on; what lies behind its end is 0.
+__device__ inline void few_load(const uint8_t* row, int64_t at, int64_t bytes, i32x4 (&v)[2])
+{
+    if (at + 32 <= bytes) {
+        v[0] = load_any(row + at);
+        v[1] = load_any(row + at + 16);
+        return;
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int64_t i = at + 16 * c + 4 * e;
+            const auto* p = reinterpret_cast<const uint16_t*>(row + i);
+            const uint32_t lo = i < bytes ? p[0] : 0u, hi = i + 2 < bytes ? p[1] : 0u;
+            v[c][e] = int(lo | hi << 16);
+        }
+}
+
+// Results for up to 16 tokens, 16 rows of both weights to a workgroup, bound by reading the weights
+// once: no LDS tiles, every lane loads its bytes of the instruction's rows straight from HBM, and
+// the waves cut the sum into runs of neighbouring steps.  An instruction is 16 rows x 16 tokens: a
+// lane holds 16 bytes of row and token l % 16, and ends with rows 4 (l / 16) + e of token l % 16.  One token through 2048 x 11008 16.9 us, 5.4 TB/s; 16 tokens 23.
+template <bool F32>
+__global__ __launch_bounds__(512) void k_few(FewArgs g)
+{
+    extern __shared__ f32x4 few_sums[];  // [wave][B][lane], of 16 bytes
+    constexpr int B = 2;
+    const int lane = int(threadIdx.x) & 63, r = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+    const int waves = int(blockDim.x) >> 6;
+    const int64_t n0 = int64_t(blockIdx.x) * 16;
+    const uint8_t* w[B];
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+        const int64_t row = n0 + r < g.n ? n0 + r : g.n - 1;
+        w[b] = g.w[b] + row * g.w_pitch[b];
+    }
+    const uint8_t* x = g.x + (r < g.m ? r : g.m - 1) * g.x_pitch;
+    f32x4 acc[B] = {};
+    struct Loaded {
+        i32x4 w[B][2], x[2];
+    };
+    const auto load = [&](int s, Loaded& in) {
+        const int64_t at = int64_t(s) * kStepBytes + 32 * q;
+#pragma unroll
+        for (int b = 0; b < B; ++b)
+            few_load(w[b], at, g.bytes, in.w[b]);
+        few_load(x, at, g.bytes, in.x);
+    };
+    const auto multiply = [&](const Loaded& in) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int b = 0; b < B; ++b)
+                acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                    __builtin_bit_cast(bf16x8, in.w[b][c]),
+                    __builtin_bit_cast(bf16x8, in.x[c]), acc[b], 0, 0, 0);
+    };
+    const int steps = int((g.bytes + kStepBytes - 1) / kStepBytes);
+    const int first = steps * wave / waves, last = steps * (wave + 1) / waves;
+    if (first < last) {
+        Loaded even, odd;
+        load(first, even);
+        int s = first;
+        for (; s + 1 < last; s += 2) {
+            load(s + 1, odd);
+            multiply(even);
+            if (s + 2 < last)
+                load(s + 2, even);
+            multiply(odd);
+        }
+        if (s < last)
+            multiply(even);
+    }
+#pragma unroll
+    for (int b = 0; b < B; ++b)
+        few_sums[(wave * B + b) * 64 + lane] = acc[b];
+    __syncthreads();
+    // the waves' sums, added in their order
+    const float* sums = reinterpret_cast<const float*>(few_sums);
+    const int e = int(threadIdx.x), l = e / 4;
+    const int64_t row = n0 + 4 * (l >> 4) + e % 4, tok = l & 15;
+    if (e >= 256 || row >= g.n || tok >= g.m)
+        return;
+    float v[B];
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+        const float* from = sums + b * 256 + e;
+        v[b] = from[0];
+        for (int i = 1; i < waves; ++i)
+            v[b] += from[i * B * 256];
+    }
+    const float u[1] = {v[0]};
+    float a[1];
+    gated::activate(g.activation, u, a);
+    const float y = a[0] * v[1];
+    if constexpr (F32)
+        static_cast<float*>(g.out)[tok * g.stride + row] = y;
+    else
+        static_cast<uint16_t*>(g.out)[tok * g.stride + row] = gated::bf16_bits(y);
+}
+
+void launch_few(const FewArgs& g, bool f32, hipStream_t st)
+{
+    const int64_t steps = (g.bytes + kStepBytes - 1) / kStepBytes;
+    const int waves = steps >= 8 ? 8 : 4;
+    auto* kernel = f32 ? k_few<true> : k_few<false>;
+    kernel<<<dim3(uint32_t((g.n + 15) / 16)), 64 * waves, size_t(waves) * 2 * 1024, st>>>(g);
 }
 
 // ------------------------------------------------------------- the backward pass
@@ -449,20 +607,35 @@ int64_t take(int64_t& at, int64_t bytes)
 
 struct ForwardLayout {
     int64_t x = -1, gate = -1, up = -1;  // of packed copies
+    int64_t partial = -1;                // of the slices' sums
+    Way way;
+    bool few = false;  // no tiles, and no workspace
     int64_t total = 0;
 };
 
 ForwardLayout forward_layout(int64_t m, int64_t n, int64_t k, int64_t x_stride,
-                             int64_t gate_stride, int64_t up_stride)
+                             int64_t gate_stride, int64_t up_stride, bool save)
 {
     ForwardLayout l;
     const int64_t pitch = padded(k) * 2;
-    if (!readable(k, x_stride))
+    const bool copy_x = !readable(k, x_stride), copy_gate = !readable(k, gate_stride),
+               copy_up = !readable(k, up_stride);
+    // tiles read a long sum faster, in slices (a token through 5120 x 2048 32 us and 26, through
+    // 11008 x 2048 29 and 23; through 2048 x 11008 21 and 27), but not what has to be copied first
+    l.few = !save && m <= gated::kFewTokens && (k <= 4096 || copy_x || copy_gate || copy_up);
+    if (l.few) {
+        l.total = 256;
+        return l;
+    }
+    if (copy_x)
         l.x = take(l.total, m * pitch);
-    if (!readable(k, gate_stride))
+    if (copy_gate)
         l.gate = take(l.total, n * pitch);
-    if (!readable(k, up_stride))
+    if (copy_up)
         l.up = take(l.total, n * pitch);
+    l.way = way_of(m, n, int(padded(k) / kStep), true, !save);
+    if (l.way.slices > 1)
+        l.partial = take(l.total, l.way.slices * m * n * 8);
     l.total = std::max<int64_t>(l.total, 256);
     return l;
 }
@@ -669,15 +842,16 @@ void turned_operand(const TurnedPlace& p, const void* x, int64_t rows, int64_t k
 }
 
 template <typename Tile>
-void launch_forward(const ForwardArgs& g, bool f32, bool save, hipStream_t st)
+void launch_forward(const ForwardArgs& g, int slices, bool f32, bool save, hipStream_t st)
 {
     auto* kernel = save ? (f32 ? k_gated_forward<Tile, true, true>
                                : k_gated_forward<Tile, false, true>)
                         : (f32 ? k_gated_forward<Tile, true, false>
                                : k_gated_forward<Tile, false, false>);
-    kernel<<<dim3(uint32_t(host::ceil_div(g.m, Tile::kRows) *
-                           host::ceil_div(g.n, Tile::kCols / 2))),
-             Tile::kThreads, 0, st>>>(g);
+    const dim3 grid(uint32_t(host::ceil_div(g.m, Tile::kRows) *
+                             host::ceil_div(g.n, Tile::kCols / 2)),
+                    uint32_t(slices));
+    kernel<<<grid, Tile::kThreads, 0, st>>>(g);
 }
 
 // The products that are planned, the one with the longer tiles first.
@@ -764,7 +938,10 @@ size_t lt_gated_forward_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t
 {
     if (!valid_sizes(m, n, k))
         return 0;
-    return size_t(forward_layout(m, n, k, x_stride, gate_stride, up_stride).total);
+    const auto total = [&](bool save) {
+        return forward_layout(m, n, k, x_stride, gate_stride, up_stride, save).total;
+    };
+    return size_t(std::max(total(false), total(true)));
 }
 
 lt_err lt_gated_forward(const void* x, int64_t x_stride, const void* gate, int64_t gate_stride,
@@ -791,9 +968,10 @@ try {
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const size_t out_bytes = span_bytes(m, n, out_stride, out_dtype);
     const size_t saved_bytes = saved ? lt_gated_saved_bytes(m, n) : 0;
-    const bool few = m <= gated::kFewTokens && !saved;
-    const ForwardLayout l = forward_layout(m, n, k, x_stride, gate_stride, up_stride);
-    const bool works = !few && k > 0 && (l.x >= 0 || l.gate >= 0 || l.up >= 0);
+    const ForwardLayout l =
+        forward_layout(m, n, k, x_stride, gate_stride, up_stride, saved != nullptr);
+    const bool works =
+        k > 0 && (l.x >= 0 || l.gate >= 0 || l.up >= 0 || l.partial >= 0);
     if (works && (!workspace || !host::aligned(workspace, 256) || workspace_bytes < size_t(l.total)))
         return fail(LT_ERR_WORKSPACE, "workspace must be 256-byte aligned and hold " +
                                           std::to_string(l.total) + " bytes");
@@ -818,8 +996,8 @@ try {
         return host::launch_zero(out, out_dtype == LT_DTYPE_F32 ? 4 : 2, m, n, out_stride, st);
     }
     const bool f32 = out_dtype == LT_DTYPE_F32;
-    if (few) {
-        gated::FewArgs f{};
+    if (l.few) {
+        FewArgs f{};
         f.w[0] = static_cast<const uint8_t*>(gate);
         f.w[1] = static_cast<const uint8_t*>(up);
         f.w_pitch[0] = gate_stride * 2;
@@ -832,7 +1010,7 @@ try {
         f.activation = activation;
         f.out = out;
         f.stride = out_stride;
-        gated::launch_few<gated::FewBf16, 2>(f, f32, st);
+        launch_few(f, f32, st);
         LT_TRY_HIP(hipGetLastError());
         return LT_OK;
     }
@@ -864,13 +1042,20 @@ try {
     operand(gate, n, gate_stride, l.gate, &g.gate, &g.gate_pitch);
     operand(up, n, up_stride, l.up, &g.up, &g.up_pitch);
     copies.launch(st);
-    const Way w = way_of(m, n, 1, g.steps, true);
-    if (w.tile == 256)
-        launch_forward<Large16>(g, f32, saved != nullptr, st);
-    else if (w.tile == 128)
-        launch_forward<Small16>(g, f32, saved != nullptr, st);
+    g.slice = l.way.slice;
+    if (l.partial >= 0)
+        g.partial = reinterpret_cast<float*>(ws + l.partial);
+    if (l.way.tile == 256)
+        launch_forward<Large16>(g, l.way.slices, f32, saved != nullptr, st);
+    else if (l.way.tile == 128)
+        launch_forward<Small16>(g, l.way.slices, f32, saved != nullptr, st);
     else
-        launch_forward<Pair16>(g, f32, saved != nullptr, st);
+        launch_forward<Pair16>(g, l.way.slices, f32, saved != nullptr, st);
+    if (g.partial) {
+        auto* answer = f32 ? k_gated_answer<true> : k_gated_answer<false>;
+        answer<<<dim3(uint32_t(std::min<int64_t>(4096, host::ceil_div(m * n, 256)))), 256, 0, st>>>(
+            g, l.way.slices);
+    }
     LT_TRY_HIP(hipGetLastError());
     return LT_OK;
 } catch (...) {

@@ -179,7 +179,7 @@ struct ProductArgs {
     int activation;
     void* out;
     int64_t stride;
-    int32_t* partial;  // several slices: [slice][m][n]
+    int32_t* partial;  // several slices: [slice][weight][m][n]
 };
 
 __device__ inline float scaled(float bits, float row, float col)
@@ -233,6 +233,12 @@ struct ProductWriter {
         const int64_t row = r0 + row_, col = c0 + col_;
         if (row >= g.m || col >= g.n)
             return;
+        if (g.partial) {
+            const int64_t at = (int64_t(blockIdx.y) * 2 * g.m + row) * g.n + col;
+            store_row<true>(g.partial, at, u, g.n - col);
+            store_row<true>(g.partial, at + g.m * g.n, v, g.n - col);
+            return;
+        }
         float a[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -274,25 +280,39 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_int8_ga
                                     int((g.m + Tile::kRows - 1) / Tile::kRows),
                                     int((g.n + kCols - 1) / kCols));
     const int64_t r0 = int64_t(at.row) * Tile::kRows, c0 = int64_t(at.col) * kCols;
+    const int first = int(blockIdx.y) * g.slice, steps = min(g.slice, g.steps - first);
     Tile tile;
     Int8<Tile::kPinned> mul;
-    product_pairs(mul, tile, g.a + r0 * g.pitch, g.pitch, g.m - r0, g.b + c0 * g.pitch, g.pitch,
-                  g.c + c0 * g.pitch, g.pitch, g.n - c0, g.steps, lds);
+    const int64_t k0 = int64_t(first) * kStepBytes;
+    product_pairs(mul, tile, g.a + r0 * g.pitch + k0, g.pitch, g.m - r0, g.b + c0 * g.pitch + k0,
+                  g.pitch, g.c + c0 * g.pitch + k0, g.pitch, g.n - c0, steps, lds);
     ProductWriter<F32> w{g, r0, c0};
     finish_pairs(tile, lds, w);
 }
 
-template <bool F32>
+// Results of the slices' sums.
+template <int B, bool F32>
 __global__ __launch_bounds__(256) void k_int8_join(ProductArgs g, int slices)
 {
     const int64_t all = g.m * g.n;
     for (int64_t e = int64_t(blockIdx.x) * 256 + threadIdx.x; e < all;
          e += int64_t(gridDim.x) * 256) {
-        int s = g.partial[e];
+        int s[B];
+#pragma unroll
+        for (int b = 0; b < B; ++b)
+            s[b] = g.partial[b * all + e];
         for (int i = 1; i < slices; ++i)
-            s += g.partial[i * all + e];
+#pragma unroll
+            for (int b = 0; b < B; ++b)
+                s[b] += g.partial[(i * B + b) * all + e];
         const int64_t row = e / g.n, col = e % g.n;
-        const float v = float(s) * g.a_scales[row] * g.b_scales[col];
+        float v = float(s[0]) * g.a_scales[row] * g.b_scales[col];
+        if constexpr (B == 2) {
+            const float u[1] = {v};
+            float a[1];
+            gated::activate(g.activation, u, a);
+            v = a[0] * (float(s[1]) * g.a_scales[row] * g.c_scales[col]);
+        }
         if constexpr (F32)
             static_cast<float*>(g.out)[row * g.stride + col] = v;
         else
@@ -514,7 +534,7 @@ using gated::Way;
 
 Way way_of(int64_t m, int64_t n, int64_t k, bool pair)
 {
-    return gated::way_of(m, n, 1, int(host::ceil_div(k, kPitch)), pair);
+    return gated::way_of(m, n, int(host::ceil_div(k, kPitch)), pair);
 }
 
 bool valid_sizes(int64_t m, int64_t n, int64_t k)
@@ -588,9 +608,10 @@ void launch_gated(const ProductArgs& g, const Way& w, bool f32, hipStream_t st)
 {
     const auto go = [&](auto* kernel, auto tile) {
         typedef decltype(tile) Tile;
-        kernel<<<dim3(uint32_t(host::ceil_div(g.m, Tile::kRows) *
-                               host::ceil_div(g.n, Tile::kCols / 2))),
-                 Tile::kThreads, 0, st>>>(g);
+        const dim3 grid(uint32_t(host::ceil_div(g.m, Tile::kRows) *
+                                 host::ceil_div(g.n, Tile::kCols / 2)),
+                        uint32_t(w.slices));
+        kernel<<<grid, Tile::kThreads, 0, st>>>(g);
     };
     if (w.tile == 256)
         go(f32 ? k_int8_gated<Large16, true> : k_int8_gated<Large16, false>, Large16());
@@ -615,6 +636,15 @@ bool held(int64_t m, int64_t k)
 // of the quantizer before 23.6; 8 tokens 25.5 and 24.1; 8 through 2048 x 11008 9.0 and 9.6.
 bool one_launch(int64_t m, int64_t k) { return held(m, k) && m * k <= 32768; }
 
+// Of a product whose sums are cut.
+size_t partial_bytes(int64_t m, int64_t n, int64_t k, bool pair)
+{
+    if (held(m, k))
+        return 0;
+    const Way w = way_of(m, n, k, pair);
+    return w.slices == 1 ? 0 : size_t(w.slices) * size_t(m) * size_t(n) * (pair ? 8 : 4);
+}
+
 // Workspace of the calls that quantize x themselves: [codes][scales][the product's].
 struct LinearLayout {
     size_t scales, matmul, total;
@@ -627,7 +657,7 @@ LinearLayout linear_layout(int64_t m, int64_t n, int64_t k, bool pair)
         return l;
     l.scales = host::round_up(size_t(m) * size_t(code_pitch(k)), 256);
     l.matmul = l.scales + host::round_up(size_t(m) * 4, 256);
-    l.total = l.matmul + (pair ? 0 : lt_int8_matmul_workspace_bytes(m, n, k));
+    l.total = l.matmul + partial_bytes(m, n, k, pair);
     return l;
 }
 
@@ -695,27 +725,6 @@ lt_err run_product(const ProductArgs& args, int64_t k, int out_dtype, void* work
     g.steps = int(host::ceil_div(k, kPitch));
     if (held(g.m, k))
         return run_held<kCodes>(g, g.a, 0, k, out_dtype, st);
-    if (g.m <= gated::kFewTokens) {
-        gated::FewArgs f{};
-        f.w[0] = g.b;
-        f.w[1] = g.c;
-        f.w_pitch[0] = f.w_pitch[1] = f.x_pitch = f.bytes = g.pitch;
-        f.x = g.a;
-        f.w_scales[0] = g.b_scales;
-        f.w_scales[1] = g.c_scales;
-        f.x_scales = g.a_scales;
-        f.m = g.m;
-        f.n = g.n;
-        f.activation = g.activation;
-        f.out = g.out;
-        f.stride = g.stride;
-        if (pair)
-            gated::launch_few<gated::FewInt8, 2>(f, f32, st);
-        else
-            gated::launch_few<gated::FewInt8, 1>(f, f32, st);
-        LT_TRY_HIP(hipGetLastError());
-        return LT_OK;
-    }
     const Way w = way_of(g.m, g.n, k, pair);
     g.slice = w.slice;
     if (w.slices > 1)
@@ -725,7 +734,8 @@ lt_err run_product(const ProductArgs& args, int64_t k, int out_dtype, void* work
     else
         launch_product(g, w, f32, st);
     if (g.partial) {
-        auto* join = f32 ? k_int8_join<true> : k_int8_join<false>;
+        auto* join = pair ? f32 ? k_int8_join<2, true> : k_int8_join<2, false>
+                     : f32 ? k_int8_join<1, true> : k_int8_join<1, false>;
         join<<<dim3(uint32_t(std::min<int64_t>(4096, host::ceil_div(g.m * g.n, 256)))), 256, 0,
                st>>>(g, w.slices);
     }
@@ -842,10 +852,7 @@ size_t lt_int8_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k)
 {
     if (!valid_sizes(m, n, k))
         return 0;
-    const Way w = way_of(m, n, k, false);
-    if (m <= gated::kFewTokens || w.slices == 1)
-        return 256;
-    return std::max(size_t(256), size_t(w.slices) * size_t(m) * size_t(n) * 4);
+    return std::max(size_t(256), partial_bytes(m, n, k, false));
 }
 
 lt_err lt_int8_matmul(const int8_t* a_codes, const float* a_scales, const int8_t* b_codes,
@@ -870,7 +877,7 @@ try {
     if (k == 0)
         return zero_rows(out, out_dtype, m, n, out_stride, st);
     const size_t need = lt_int8_matmul_workspace_bytes(m, n, k);
-    const bool sliced = need > 256;
+    const bool sliced = partial_bytes(m, n, k, false) > 0;
     if (sliced && (!workspace || !host::aligned(workspace, 256) || workspace_bytes < need))
         return fail(LT_ERR_WORKSPACE, "workspace must be 256-byte aligned and hold " +
                                           std::to_string(need) + " bytes");

@@ -10,7 +10,7 @@ from typing import Optional, Tuple
 import torch
 
 from .fp8 import _dtype_code, _laid_out, _rows, _scratch, _tokens
-from .int8 import _activation_code
+from .int8 import _activation_code, _call_workspace
 from .lazytrain import _capturing, _check, _current, _stream_handle, lib
 
 
@@ -54,10 +54,11 @@ def _forward(x, gate, up, activation, out_dtype, keep, workspace):
     if keep:
         saved = torch.empty(6 * m * (-(-n // 8) * 8), dtype=torch.uint8, device=device)
     ws, nbytes, handle = 0, 0, _stream_handle(None, device)
-    if (keep or m > 16) and (k % 64 or (x_stride | g_stride | u_stride) % 8) or \
-            workspace is not None:
+    strides = x_stride | g_stride | u_stride
+    copies = k % 64 or strides % 8 or strides >= 1 << 22
+    if workspace is not None or (copies if keep else m > 16 or k > 4096 and not copies):
         need = int(lib().lt_gated_forward_workspace_bytes(m, n, k, x_stride, g_stride, u_stride))
-        held, ws, nbytes = _scratch(device, need, workspace, None)
+        held, ws, nbytes = _call_workspace(device, need, workspace)
     with _current(device):
         _check(lib().lt_gated_forward(t.data_ptr(), x_stride, g.data_ptr(), g_stride, u.data_ptr(),
                                       u_stride, act, m, n, k, h.data_ptr(), out, n,

@@ -114,6 +114,38 @@ def test_forward(m, n, k, act):
         assert saved.numel() == 6 * m * (-(-n // 8) * 8)
 
 
+# Sums that are cut, and few tokens of long sums with rows of any place.
+@pytest.mark.parametrize("m,n,k", [(1, 70, 4160), (16, 33, 8192), (9, 33, 5001), (17, 130, 4096),
+                                   (40, 67, 5001), (90, 1, 4100), (200, 300, 2560),
+                                   (500, 257, 4096)])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_long_sums(m, n, k, act):
+    x, gate, up, _ = inputs(m, n, k)
+    e = Exact(x, gate, up, act)
+    for dtype in (torch.float32, torch.bfloat16):
+        h = lt.gated_linear(x, gate, up, act, out_dtype=dtype)
+        near(h, e.h, e.room, dtype)
+        assert torch.equal(h, lt.gated_linear(x, gate, up, act, out_dtype=dtype))
+    want = lt.gated_linear(x, gate, up, act)
+    x[0, k - 1] = float("nan")
+    got = lt.gated_linear(x, gate, up, act)
+    assert torch.isnan(got[0]).all() and torch.equal(got[1:], want[1:])
+
+
+@pytest.mark.parametrize("m", [5, 17])
+def test_rows_far_apart(m):
+    """Rows further apart than the tiles' offsets reach are copied."""
+    far = torch.zeros(m, 1 << 22, dtype=torch.bfloat16, device=DEV)
+    x, gate, up, dh = inputs(m, 40, 128)
+    far[:, :128] = x
+    assert torch.equal(lt.gated_linear(far[:, :128], gate, up), lt.gated_linear(x, gate, up))
+    got, want = (lt.gated_linear_forward(t, gate, up) for t in (far[:, :128], x))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    for a, b in zip(lt.gated_linear_backward(dh, got[1], far[:, :128], gate, up),
+                    lt.gated_linear_backward(dh, want[1], x, gate, up)):
+        assert torch.equal(a, b)
+
+
 BACKWARD = [(1, 1, 1), (1, 40, 70), (70, 33, 100), (64, 64, 64), (65, 130, 63), (301, 200, 515),
             (129, 1030, 128), (1100, 64, 64), (7000, 30, 40)]
 

@@ -95,7 +95,7 @@ def same(got, want):
 SIZES = [(1, 1, 1), (1, 520, 300), (2, 17, 129), (16, 33, 1000), (17, 300, 128), (32, 64, 2048),
          (5, 9000, 2048), (16, 8300, 2049), (3, 4200, 5121), (16, 70, 8192), (2, 70, 8193),
          (33, 65, 127), (64, 64, 6400), (65, 200, 9001), (100, 1, 12800), (300, 257, 257),
-         (129, 4096, 640), (520, 2050, 96), (1030, 16390, 130)]
+         (129, 4096, 640), (520, 2050, 96), (1030, 16390, 130), (1, 300, 17000), (16, 1, 20001)]
 
 
 @pytest.mark.parametrize("m,n,k", SIZES)
@@ -135,6 +135,18 @@ def test_a_bad_token_stays_alone(m):
     assert same(y, product(expected(x), expected(w), torch.bfloat16))
     bad = torch.isnan(y)
     assert bad[1].all() and bad[:, 7].all() and int(bad.sum()) == m + 200 - 1
+
+
+@pytest.mark.parametrize("m", [3, 90])
+def test_a_bad_token_of_a_long_sum_stays_alone(m):
+    x = matrix(m, 9000, 1, torch.bfloat16)
+    ws = [lt.Int8Weight.from_master(matrix(70, 9000, s, torch.float32)) for s in (2, 3)]
+    want = lt.int8_gated_linear(x, *ws)
+    assert torch.isfinite(want).all()
+    x[2, 8999] = float("inf")
+    got = lt.int8_gated_linear(x, *ws)
+    assert torch.isnan(got[2]).all()
+    assert torch.equal(got[:2], want[:2]) and torch.equal(got[3:], want[3:])
 
 
 def test_layouts_and_empties():
@@ -183,7 +195,8 @@ def activation(name, g):
 @pytest.mark.parametrize("m,n,k", [(1, 1, 1), (1, 520, 300), (16, 33, 1000), (17, 300, 128),
                                    (16, 9000, 700), (5, 4200, 2100), (3, 300, 8000), (2, 40, 8300),
                                    (33, 65, 127), (65, 200, 3001), (300, 257, 257),
-                                   (129, 4096, 640), (520, 2050, 96), (1030, 8200, 130)])
+                                   (129, 4096, 640), (520, 2050, 96), (1030, 8200, 130),
+                                   (1, 70, 17000), (40, 70, 4096), (300, 130, 9001)])
 @pytest.mark.parametrize("act", list(ROOM))
 def test_gated(m, n, k, act):
     x = matrix(m, k, 1, torch.bfloat16, spread=False)
