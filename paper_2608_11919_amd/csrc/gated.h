@@ -127,8 +127,8 @@ __device__ inline void store_row(void* out, int64_t at, const float (&v)[8], int
         }
 }
 
-// Tokens of an instruction.  Above these, tiles: 32 tokens in two passes of the instruction took 30 us
-// through 2048 x 11008 (bf16, gated), by tiles 19; in integers 14 and 11.
+// Tokens of an instruction.  Above these, tiles: 32 tokens in two passes of the instruction took 30
+// us through 2048 x 11008 (bf16, gated), by tiles 19; in integers 14 and 11.
 constexpr int64_t kFewTokens = 16;
 
 // ------------------------------------------------------------- tiles
@@ -139,8 +139,8 @@ struct Way {
     int slice;   // steps of each
 };
 
-// What a tile costs, in microseconds: a step of one that has a CU to itself, of one among as many as
-// a CU takes, and what is beside the steps.  `places`: how many that is.
+// What a tile costs, in microseconds: a step of one that has a CU to itself, of one among as many
+// as a CU takes, and what is beside the steps.  `places`: how many that is.
 struct Cost {
     int tile, places;
     double alone, full, rest;
