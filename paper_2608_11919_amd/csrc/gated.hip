@@ -449,7 +449,7 @@ __global__ __launch_bounds__(256) void k_gated_slopes(SlopeArgs g)
 
 // dx = [dg | du] [gate; up], or dgate = dg^T x and dup = du^T x.  No operand is turned in memory:
 // what has the summed index as rows is turned on its way out of LDS.  Bound by the matrix cores'
-// power (they work 74% of the cycles for dx at 1.85 GHz, 72% at 1.83 for the weights) and by what
+// power (they work 73% of the cycles for dx at 1.83 GHz, 71% at 1.82 for the weights) and by what
 // L2 feeds a CU, 23.5 of some 26 bytes a cycle.  16384 x 5120 x 17408: dx 4.03 to 4.22 ms, the
 // weights' 4.15 to 4.41 (1.32 to 1.45 PFLOP/s, by the card); 8192 x 2048 x 11008, all in one
 // launch, 1.07 to 1.27.
