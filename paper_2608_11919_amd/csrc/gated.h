@@ -1,5 +1,5 @@
 // gated.h -- what the gated projections in bf16 (gated.hip) and in 8-bit integers (int8.hip)
-// share: the activations, and products of few tokens with one or two weights.
+// share: the activations, stores, and how a product is cut into tiles and slices.
 #ifndef LAZYTRAIN_GATED_H
 #define LAZYTRAIN_GATED_H
 
@@ -27,8 +27,25 @@ __device__ inline float logistic(float z)
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f));
 }
 
-// g Phi(g) through the complementary error function: 1 + erf(g / sqrt 2) cancels for negative g.
-__device__ inline float normal_cdf(float g) { return 0.5f * erfcf(g * -0.70710678f); }
+// Phi(-s) = e^(-s^2/2) t P(t) for s >= 0 with t = 1 / (1 + 0.35 s): the function beside the power
+// falls slowly and smoothly, and P, of degree 8, is its fit with the least largest relative error on
+// 0 <= s <= 14.5, 3.2e-8 (least squares, reweighted by the errors).  In fp32 within (s^2 + 15) *
+// 2^-24, mostly the power's argument; 0 from 13.2 on, where s Phi(-s) is below 2e-38.  4096
+// x 2048 x 11008 in integers 228 us, with the library's erfc 279; kept in bf16 346 and 386.
+__device__ inline float tail(float s, float power)
+{
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.35f, s, 1.0f));
+    float p = -0.0291580297f;
+    p = __builtin_fmaf(p, t, 0.144031614f);
+    p = __builtin_fmaf(p, t, -0.255840391f);
+    p = __builtin_fmaf(p, t, 0.159321249f);
+    p = __builtin_fmaf(p, t, -0.0232133921f);
+    p = __builtin_fmaf(p, t, 0.105552927f);
+    p = __builtin_fmaf(p, t, 0.119821183f);
+    p = __builtin_fmaf(p, t, 0.139863536f);
+    p = __builtin_fmaf(p, t, 0.139621302f);
+    return p * t * power;
+}
 
 constexpr float kTanhLinear = 1.59576912f;   // 2 sqrt(2 / pi)
 constexpr float kTanhCubic = 0.0713548163f;  // that times 0.044715
@@ -45,9 +62,10 @@ struct Silu {
 struct Gelu {
     __device__ static inline float of(float g, float* slope)
     {
-        const float p = normal_cdf(g);
-        *slope = __builtin_fmaf(
-            g * 0.398942280f, __builtin_amdgcn_exp2f(g * g * -0.72134752f), p);  // g e^(-g^2/2)
+        const float power = __builtin_amdgcn_exp2f(g * g * -0.72134752f);  // e^(-g^2/2)
+        const float below = tail(fabsf(g), power);
+        const float p = g < 0.0f ? below : 1.0f - below;  // no difference where it would cancel
+        *slope = __builtin_fmaf(g * 0.398942280f, power, p);
         return g * p;
     }
 };

@@ -175,8 +175,9 @@ def test_layouts_and_empties():
 # roundings off the exact ones, 3 * 2^-24.  e^-z comes from a product with log2(e) (1.5 * 2^-24 |z|
 # of the result), a power of two (2^-23), a sum (2^-24) and a reciprocal (2^-23); act(g) moves by
 # |g act'(g) / act(g)| as much, relatively, as g does: at most 1 + |g| for silu, 1 + 3 |z| for
-# gelu_tanh with z = g (c + d g^2), itself three roundings off, and 1 + g^2 for gelu, whose erfc is
-# given an argument 1.5 * 2^-24 off, too, and is some 4 units in the last place off itself.
+# gelu_tanh with z = g (c + d g^2), itself three roundings off, and 1 + g^2 for gelu, whose
+# e^(-g^2/2) has an argument 2.5 * 2^-24 off, too (1.25 g^2 of the result), and whose polynomial is
+# some 15 * 2^-24 off itself.
 ROOM = {"silu": lambda g: 5 * abs(g) + 20, "relu": lambda g: 12 + 0 * g,
         "gelu_tanh": lambda g: 15 * abs(g * (1.6 + 0.072 * g * g)) + 24,
         "gelu": lambda g: 8 * g * g + 40}
