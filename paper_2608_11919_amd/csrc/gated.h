@@ -164,20 +164,20 @@ struct Cost {
     double alone, full, rest;
 };
 
-constexpr Cost kCosts[] = {{256, 1, 1.26, 1.26, 15.0}, {128, 2, 0.64, 0.56, 1.6},
-                           {64, 4, 0.39, 0.27, 0.8}};
-constexpr Cost kPairCosts[] = {{256, 1, 1.26, 1.26, 15.0}, {128, 2, 0.64, 0.56, 1.6},
-                               {64, 3, 0.50, 0.41, 1.1}};
+constexpr Cost kCosts[] = {{256, 1, 1.27, 1.27, 18.5}, {128, 2, 0.59, 0.52, 2.4},
+                           {64, 4, 0.44, 0.28, 0.8}};
+constexpr Cost kPairCosts[] = {{256, 1, 1.37, 1.37, 14.5}, {128, 2, 0.62, 0.57, 1.3},
+                               {64, 3, 0.51, 0.42, 0.5}};
 
 // The tile and the slices of the sum that a launch is expected to end first with.  The CU with the
-// most tiles sets the time of the steps; the weights come at 6.3 TB/s (those that the last cache
+// most tiles sets the time of the steps; the weights come at 6.2 TB/s (those that the last cache
 // holds count in) where all CUs have as much to read, and later the more that differs; slices cost
-// another launch and their sums' way to memory and back (5 TB/s).  Fitted to 490 products of 1 to
+// another launch and their sums' way to memory and back (5.8 TB/s).  Fitted to 628 products of 32 to
 // 8192 rows, 768 to 17408 columns and 1024 to 17408 summed values in both types, each by all tiles
-// and up to 24 slices: the choice is 0.8% from the best on average and 17% at most.  Without the
-// reading and the rounds that share a CU it was 5% and up to twice as long: 512 x 5120 x 5120 gated
-// in bf16 103 us for 67, 128 x 17408 x 5120 in integers 64 for 38; without slices of a pair's sums
-// 64 x 11008 x 2048 gated in bf16 53 for 23.
+// and up to 24 slices: the choice is 0.6% from the best on average, 7% or more for 20 of them and 23%
+// at most.  Without the reading and the rounds that share a CU it was 5% and up to twice as long: 512
+// x 5120 x 5120 gated in bf16 103 us for 67, 128 x 17408 x 5120 in integers 64 for 38; without slices
+// of a pair's sums 64 x 11008 x 2048 gated in bf16 53 for 23.
 // `pair`: a tile's columns are two weights'.  `cut`: whether sums may be.
 inline Way way_of(int64_t m, int64_t n, int steps, bool pair, bool cut = true)
 {
@@ -185,7 +185,7 @@ inline Way way_of(int64_t m, int64_t n, int steps, bool pair, bool cut = true)
     if (steps <= 0)
         return best;
     const int weights = pair ? 2 : 1, most_slices = cut ? std::min(24, std::max(1, steps / 8)) : 1;
-    const double reading = double(n) * steps * tiles::kStepBytes * weights / 6.3e6;
+    const double reading = double(n) * steps * tiles::kStepBytes * weights / 6.2e6;
     double least = 1e300;
     for (const Cost& c : pair ? kPairCosts : kCosts) {
         const int64_t wide = pair && c.tile > 64 ? c.tile / 2 : c.tile;
@@ -200,8 +200,8 @@ inline Way way_of(int64_t m, int64_t n, int steps, bool pair, bool cut = true)
                 std::max(c.alone * double((each + c.places - 1) / c.places), c.full * double(each));
             const double apart = double(each * 256) / double(groups) - 1.0;
             const double us = std::max(step * slice + c.rest * double(each),
-                                       reading * (1.0 + 0.72 * apart)) +
-                              (z > 1 ? 3.7 + 2.0 * sums / 5e6 : 0.0);
+                                       reading * (1.0 + 0.68 * apart)) +
+                              (z > 1 ? 6.7 + 2.0 * sums / 5.8e6 : 0.0);
             if (us < least) {
                 least = us;
                 best = Way{c.tile, slices, slice};
