@@ -694,7 +694,7 @@ struct TurnedCost {
 };
 
 constexpr TurnedCost kTurnedCosts[] = {
-    {256, 1.45, 1.45, 14.0}, {128, 0.65, 0.6, 2.0}, {64, 0.25, 0.4, 0.8}};
+    {256, 1.83, 1.83, 7.8}, {128, 0.67, 0.95, 2.0}, {64, 0.25, 0.53, 0.83}};
 
 // A matrix product of the backward pass, as its launch is planned: `count` results of m x n.
 struct Plan {
@@ -723,9 +723,10 @@ struct Plan {
 };
 
 // The tile of a launch with one or both, and their slices, by expected time: the longest tile, or
-// all tiles' work shared by the CUs and half of the last tiles, which leave some idle; what they
-// read, at 12 TB/s out of L2 and behind it; another launch for the sums of slices, and those to
-// memory and back (4 TB/s).  Fitted to 64 to 10000 tokens through 128 x 2048 to 5120 x 17408.
+// all tiles' work shared by the CUs and the last tiles, which leave some idle; what they read, at
+// 26 TB/s out of L2 and behind it; another launch for the sums of slices, and those to memory and
+// back (2.5 TB/s).  Fitted to 190 passes of 64 to 12288 tokens through 64 x 64 to 5120 x 17408, each
+// by all tiles and up to 32 slices: 0.7% from the best on average and 17% at most.
 int plan(Plan* dx, Plan* dw)
 {
     struct Choice {
@@ -747,7 +748,7 @@ int plan(Plan* dx, Plan* dw)
                 continue;
             const int64_t tiles = p.tiles(c) * p.slices;
             to[n++] = {p, p.alone(c), p.busy(c), tiles * p.busy(c) / 256,
-                       p.slices > 1 ? 5.0 + 2.0 * double(p.partial()) / 4e6 : 0.0, tiles};
+                       p.slices > 1 ? 3.8 + 2.0 * double(p.partial()) / 2.5e6 : 0.0, tiles};
         }
         return n;
     };
@@ -765,9 +766,9 @@ int plan(Plan* dx, Plan* dw)
                 if (x.tiles + w.tiles > 256) {
                     const double last = dx && dw ? std::min(x.busy, w.busy)
                                                  : std::max(x.busy, w.busy);
-                    us = std::max(us, x.work + w.work + 0.5 * last);
+                    us = std::max(us, x.work + w.work + 0.97 * last);
                 }
-                us += read / 12e6 + x.sums + w.sums;
+                us += read / 26e6 + x.sums + w.sums;
                 if (us < least) {
                     least = us;
                     best = c.tile;
