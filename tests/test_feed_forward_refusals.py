@@ -258,3 +258,24 @@ def test_tensors():
         lt.int8_gated_linear(f(4, 8), w, w, "tanh")
     with pytest.raises(ValueError, match="w must have shape"):
         w.update(f(6, 9))
+
+
+def test_sums_that_are_cut_need_their_memory():
+    """m x n fp32 sums of either weight for every slice; none where something is kept, or for few
+    tokens of a sum up to 4096 or of rows that tiles cannot read."""
+    L = lib()
+    need = L.lt_gated_forward_workspace_bytes(40, 64, 4096, 4096, 4096, 4096)
+    assert need > 256 and need % (2 * 40 * 64 * 4) == 0
+    assert L.lt_gated_forward_workspace_bytes(1, 64, 4160, 4160, 4160, 4160) > 256
+    assert L.lt_gated_forward_workspace_bytes(16, 64, 4096, 4096, 4096, 4096) == 256
+    kw = dict(m=40, n=64, k=4096, xs=4096, gs=4096, us=4096, stride=64)
+    assert forward(**kw, saved=0, ws_bytes=need - 1) == lt.LT_ERR_WORKSPACE
+    assert forward(**kw, saved=0, ws=0) == lt.LT_ERR_WORKSPACE
+    assert forward(**kw, saved=0, ws=WS + 16) == lt.LT_ERR_WORKSPACE
+    assert forward(**kw, saved=0, ws=4 * BASE) == lt.LT_ERR_INVALID_ARG  # out's
+    need = L.lt_int8_matmul_workspace_bytes(40, 64, 9000)
+    assert need > 256 and need % (40 * 64 * 4) == 0
+    assert L.lt_int8_matmul_workspace_bytes(16, 64, 8192) == 256
+    assert L.lt_int8_matmul_workspace_bytes(16, 64, 9000) > 256
+    codes = 40 * 9088 + 256
+    assert L.lt_int8_gated_workspace_bytes(40, 64, 9000) > codes + 2 * 40 * 64 * 4
