@@ -151,12 +151,19 @@ class GatedLinear(torch.autograd.Function):
     """``GatedLinear.apply(x, gate, up, activation)``: gated_linear with gradients for x, gate and up
     (for instance the optimizer's bf16 copies).  The backward pass reads x and the weights again:
     one of them changed in place meanwhile raises, like autograd's own.  First derivatives only: a
-    backward pass that is itself to be differentiated raises.
+    backward pass that is itself to be differentiated raises.  Where gradients are off it is
+    gated_linear and keeps nothing.
 
     Autograd adds up a leaf's gradient on the stream that its first graph was made on, for as long
     as a graph of the leaf lives.  Under capture that cannot be the default stream (the process would
     end with the capture): a captured call is refused while the graph of an earlier call, made there,
     holds one of its leaves."""
+
+    @classmethod
+    def apply(cls, x, gate, up, activation="silu"):
+        if not torch.is_grad_enabled():  # which forward below cannot see: it would keep its results
+            return gated_linear(x, gate, up, activation)
+        return super().apply(x, gate, up, activation)
 
     @staticmethod
     def forward(ctx, x, gate, up, activation="silu"):

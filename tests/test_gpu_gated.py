@@ -276,6 +276,29 @@ def test_autograd_refusals():
         y.sum().backward()
 
 
+@pytest.mark.parametrize("mode", [torch.no_grad, torch.inference_mode])
+def test_where_gradients_are_off_nothing_is_kept(mode):
+    x, gate, up, _ = inputs(2048, 1024, 256)
+    ts = [t.requires_grad_() for t in (x, gate, up)]
+    eager = lt.GatedLinear.apply(*ts)  # a graph of the leaves, on the default stream
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with mode():
+        want = lt.gated_linear(*ts, "gelu")
+        torch.cuda.synchronize()
+        torch.cuda.reset_peak_memory_stats()
+        before = torch.cuda.memory_allocated()
+        y = lt.GatedLinear.apply(*ts, "gelu")
+        assert torch.cuda.max_memory_allocated() - before < 6 * 2048 * 1024
+        assert torch.equal(y, want) and not y.requires_grad
+        with torch.cuda.stream(side):
+            with torch.cuda.graph(graph, stream=side):
+                y = lt.GatedLinear.apply(*ts, "gelu")
+            graph.replay()
+        side.synchronize()
+        assert torch.equal(y, want)
+    assert eager.requires_grad
+
+
 def test_layouts_and_empties():
     x, gate, up, dh = inputs(48, 130, 70)
     h, saved = lt.gated_linear_forward(x, gate, up)
