@@ -628,8 +628,8 @@ int64_t lt_int8_code_pitch(int64_t cols);
 lt_err lt_int8_quantize(const void* x, int dtype, int64_t rows, int64_t cols, int64_t row_stride,
                         int8_t* codes, float* scales, void* stream);
 
-/* Bytes of device workspace lt_int8_matmul needs (partial sums where few results share a long
- * sum, else 256, which it does not look at); 0 if an argument is invalid. */
+/* Bytes of device workspace lt_int8_matmul needs: more than 256 for partial sums where few results
+ * share a long sum, else 256, which it does not look at; 0 if an argument is invalid. */
 size_t lt_int8_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k);
 
 /*
@@ -646,8 +646,8 @@ lt_err lt_int8_matmul(const int8_t* a_codes, const float* a_scales, const int8_t
                       int out_dtype, int64_t out_stride, void* workspace, size_t workspace_bytes,
                       void* stream);
 
-/* Bytes of device workspace lt_int8_linear needs (256, which it does not look at, where it is one
- * launch: m <= 16, k <= 8192 and m * k <= 2^15); 0 if an argument is invalid. */
+/* Bytes of device workspace lt_int8_linear needs: 256, which it does not look at, where it is one
+ * launch (m <= 16, k <= 8192 and m * k <= 2^15), else more; 0 if an argument is invalid. */
 size_t lt_int8_linear_workspace_bytes(int64_t m, int64_t n, int64_t k);
 
 /*
@@ -684,7 +684,7 @@ size_t lt_gated_saved_bytes(int64_t m, int64_t n);
 
 /* Bytes of device workspace lt_gated_forward needs: copies of operands whose rows are not whole
  * steps of 64 values, not multiples of 8 or 2^22 and more apart, and partial sums where few results
- * share a long sum; else 256, which it does not look at.  Nothing is copied or looked at where m <=
+ * share a long sum, more than 256 in all; else 256, which it does not look at.  Nothing is copied or looked at where m <=
  * 16, nothing is saved and k <= 4096 or an operand is such a one.  0 if an argument is invalid. */
 size_t lt_gated_forward_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t x_stride,
                                         int64_t gate_stride, int64_t up_stride);

@@ -640,7 +640,7 @@ ForwardLayout forward_layout(int64_t m, int64_t n, int64_t k, int64_t x_stride,
     // 11008 x 2048 29 and 23; through 2048 x 11008 21 and 27), but not what has to be copied first
     l.few = !save && m <= gated::kFewTokens && (k <= 4096 || copy_x || copy_gate || copy_up);
     if (l.few) {
-        l.total = 256;
+        l.total = host::kNoWorkspace;
         return l;
     }
     if (copy_x)
@@ -652,7 +652,7 @@ ForwardLayout forward_layout(int64_t m, int64_t n, int64_t k, int64_t x_stride,
     l.way = way_of(m, n, int(padded(k) / kStep), true, !save);
     if (l.way.slices > 1)
         l.partial = take(l.total, l.way.slices * m * n * 8);
-    l.total = std::max<int64_t>(l.total, 256);
+    l.total = host::workspace_for(l.total);
     return l;
 }
 

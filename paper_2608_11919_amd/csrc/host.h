@@ -6,6 +6,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstddef>
 #include <cstdint>
 #include <string>
@@ -61,6 +62,15 @@ inline bool overlaps(const void* a, size_t a_bytes, const void* b, size_t b_byte
 {
     const auto x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return a && b && a_bytes && b_bytes && x < y + b_bytes && y < x + a_bytes;
+}
+
+// What a workspace query of f11 to f13 answers for a call that works in `used` bytes: 256 stands
+// for none, and whatever is looked at is more, so that a caller who passes no memory for 256 is
+// never refused.
+constexpr int64_t kNoWorkspace = 256;
+inline int64_t workspace_for(int64_t used)
+{
+    return used == 0 ? kNoWorkspace : std::max(used, 2 * kNoWorkspace);
 }
 
 // ------------------------------------------------------- empty sums (gated.hip)

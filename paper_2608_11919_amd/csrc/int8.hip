@@ -660,7 +660,7 @@ struct LinearLayout {
 
 LinearLayout linear_layout(int64_t m, int64_t n, int64_t k, bool pair)
 {
-    LinearLayout l{0, 0, 256};
+    LinearLayout l{0, 0, host::kNoWorkspace};
     if (one_launch(m, k))
         return l;
     l.scales = host::round_up(size_t(m) * size_t(code_pitch(k)), 256);
@@ -860,7 +860,7 @@ size_t lt_int8_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k)
 {
     if (!valid_sizes(m, n, k))
         return 0;
-    return std::max(size_t(256), partial_bytes(m, n, k, false));
+    return size_t(host::workspace_for(int64_t(partial_bytes(m, n, k, false))));
 }
 
 lt_err lt_int8_matmul(const int8_t* a_codes, const float* a_scales, const int8_t* b_codes,

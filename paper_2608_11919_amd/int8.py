@@ -114,7 +114,7 @@ class Int8Weight:
 
 
 def _call_workspace(device, need: int, workspace, stream=None):
-    """What a call works in; 256 bytes are what it does not look at."""
+    """What a call works in; an answer of 256 bytes stands for none."""
     if need <= 256 and workspace is None:
         return None, 0, 0
     return _scratch(device, need, workspace, stream)
