@@ -8,6 +8,7 @@ import weakref
 from typing import Optional, Tuple
 
 import torch
+from torch.autograd import forward_ad
 
 from .fp8 import _dtype_code, _laid_out, _rows, _scratch, _tokens
 from .int8 import _activation_code, _call_workspace
@@ -151,8 +152,8 @@ class GatedLinear(torch.autograd.Function):
     """``GatedLinear.apply(x, gate, up, activation)``: gated_linear with gradients for x, gate and up
     (for instance the optimizer's bf16 copies).  The backward pass reads x and the weights again:
     one of them changed in place meanwhile raises, like autograd's own.  First derivatives only: a
-    backward pass that is itself to be differentiated raises.  Where gradients are off it is
-    gated_linear and keeps nothing.
+    backward pass that is itself to be differentiated raises, and so does a tangent of forward mode.
+    Where gradients are off it is gated_linear and keeps nothing.
 
     Autograd adds up a leaf's gradient on the stream that its first graph was made on, for as long
     as a graph of the leaf lives.  Under capture that cannot be the default stream (the process would
@@ -161,7 +162,10 @@ class GatedLinear(torch.autograd.Function):
 
     @classmethod
     def apply(cls, x, gate, up, activation="silu"):
-        if not torch.is_grad_enabled():  # which forward below cannot see: it would keep its results
+        # gradients off, which forward below cannot see: it would keep its results.  A tangent of
+        # forward mode would get lost; autograd refuses it
+        if not torch.is_grad_enabled() and not any(
+                forward_ad.unpack_dual(t).tangent is not None for t in (x, gate, up)):
             return gated_linear(x, gate, up, activation)
         return super().apply(x, gate, up, activation)
 
