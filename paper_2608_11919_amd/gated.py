@@ -4,6 +4,7 @@ training, with the gradients of the tokens and of both weights.
 """
 from __future__ import annotations
 
+import threading
 import weakref
 from typing import Optional, Tuple
 
@@ -144,8 +145,27 @@ def _backward(dh, saved, x, gate, up, leading, shape, out_dtype, grad_dtype, wan
     return dx, dgate, dup
 
 
-# Graphs of GatedLinear that live and were made on the default stream, and the leaves they hold.
-_on_default = weakref.WeakSet()
+# Graphs of GatedLinear that were made on the default stream, as weak references without callbacks:
+# threads add to them while another looks, which a WeakSet's iteration does not bear.
+_on_default = []
+_on_default_lock = threading.Lock()
+_on_default_most = 256  # from here on those that are gone are dropped
+
+
+def _made_on_default(ctx) -> None:
+    global _on_default, _on_default_most
+    with _on_default_lock:
+        if len(_on_default) >= _on_default_most:
+            _on_default = [r for r in _on_default if r() is not None]
+            _on_default_most = 2 * len(_on_default) + 256
+        _on_default.append(weakref.ref(ctx))
+
+
+def _held_on_default(leaves) -> bool:
+    """Whether one of these graphs lives and holds a leaf of `leaves`, a set of ids."""
+    with _on_default_lock:
+        graphs = list(_on_default)
+    return any(c is not None and not leaves.isdisjoint(c.leaves) for c in (r() for r in graphs))
 
 
 class GatedLinear(torch.autograd.Function):
@@ -177,9 +197,8 @@ class GatedLinear(torch.autograd.Function):
             leaves = {id(t) for t in (x, gate, up) if t.requires_grad and t.is_leaf}
             if _stream_handle(None, x.device) == 0:
                 ctx.leaves = leaves
-                _on_default.add(ctx)
-            elif _capturing(None, x.device) and any(not leaves.isdisjoint(c.leaves)
-                                                    for c in list(_on_default)):
+                _made_on_default(ctx)
+            elif _capturing(None, x.device) and _held_on_default(leaves):
                 raise RuntimeError("GatedLinear is being captured while a graph made on the default "
                                    "stream holds the same leaf: let go of that graph's results "
                                    "first, or make it on another stream")

@@ -1,5 +1,8 @@
 """What GatedLinear decides before the library is called, on the CPU with the library's work left
 out: which calls keep their results, and which are refused."""
+import sys
+import threading
+
 import pytest
 import torch
 from torch.autograd import forward_ad
@@ -50,3 +53,76 @@ def test_plain_tensors_beside_duals_keep_nothing(kept):
         lt.GatedLinear.apply(*tensors(True), activation="gelu")
     assert kept == [False] * 4
     assert lt.GatedLinear.apply(*tensors(True)).requires_grad and kept[-1]
+
+
+class Context:
+    """What autograd hands to forward."""
+    needs_input_grad = (True, True, True, False)
+
+    def save_for_backward(self, *tensors):
+        self.held = tensors  # a leaf's id is its own as long as a graph holds it
+
+
+class OnGpu:
+    """A leaf as forward looks at it."""
+    is_cuda = requires_grad = is_leaf = True
+    device, shape = torch.device("cuda", 0), (6, 8)
+
+
+@pytest.fixture
+def streams(monkeypatch):
+    """A thread says which stream it works on; all but the default one are being captured."""
+    at = threading.local()
+    monkeypatch.setattr(gated, "_stream_handle", lambda stream, device: at.handle)
+    monkeypatch.setattr(gated, "_capturing", lambda stream, device: at.handle != 0)
+    monkeypatch.setattr(gated, "_forward", lambda *a: (None, None))
+    return at
+
+
+def test_a_capture_beside_eager_threads(streams):
+    """Threads make and drop graphs on the default stream while another captures."""
+    wrong, stop, held = [], threading.Event(), OnGpu()
+
+    def eager():
+        streams.handle = 0
+        try:
+            while not stop.is_set():
+                alive = []
+                for _ in range(50):
+                    alive.append(Context())
+                    gated.GatedLinear.forward(alive[-1], *(OnGpu() for _ in range(3)))
+        except Exception as e:  # the thread's, which nobody else sees
+            wrong.append(e)
+
+    interval = sys.getswitchinterval()
+    sys.setswitchinterval(1e-6)
+    threads = [threading.Thread(target=eager) for _ in range(3)]
+    try:
+        for t in threads:
+            t.start()
+        streams.handle = 0
+        graph = Context()
+        gated.GatedLinear.forward(graph, OnGpu(), held, OnGpu())
+        streams.handle = 1
+        for _ in range(1500):
+            gated.GatedLinear.forward(Context(), *(OnGpu() for _ in range(3)))
+            with pytest.raises(RuntimeError, match="holds the same leaf"):
+                gated.GatedLinear.forward(Context(), OnGpu(), OnGpu(), held)
+        del graph
+        gated.GatedLinear.forward(Context(), OnGpu(), OnGpu(), held)
+    finally:
+        stop.set()
+        for t in threads:
+            t.join(60)
+        sys.setswitchinterval(interval)
+    assert not wrong and not any(t.is_alive() for t in threads)
+
+
+def test_graphs_that_are_gone_take_no_memory(streams):
+    streams.handle = 0
+    alive = [Context() for _ in range(200)]
+    for graph in alive:
+        gated.GatedLinear.forward(graph, OnGpu(), OnGpu(), OnGpu())
+    for _ in range(5000):
+        gated.GatedLinear.forward(Context(), OnGpu(), OnGpu(), OnGpu())
+    assert 200 <= len(gated._on_default) <= 1000
