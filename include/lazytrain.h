@@ -685,7 +685,7 @@ size_t lt_gated_saved_bytes(int64_t m, int64_t n);
 /* Bytes of device workspace lt_gated_forward needs: copies of operands whose rows are not whole
  * steps of 64 values, not multiples of 8 or 2^22 and more apart, and partial sums where few results
  * share a long sum, more than 256 in all; else 256, which it does not look at.  Nothing is copied or looked at where m <=
- * 16, nothing is saved and k <= 4096 or an operand is such a one.  0 if an argument is invalid. */
+ * 16 and k <= 4096 or an operand is such a one.  0 if an argument is invalid. */
 size_t lt_gated_forward_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t x_stride,
                                         int64_t gate_stride, int64_t up_stride);
 
@@ -695,7 +695,7 @@ size_t lt_gated_forward_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t
  * for x (m x k) and two weights (n x k) of bf16, strides in elements from row to row.  Sums and the
  * activation are fp32, out is rounded once to out_dtype.
  *   saved   NULL, or lt_gated_saved_bytes(m, n) bytes for lt_gated_backward: u act'(g) and act(g),
- *           24 bits each (a relative 2^-17).
+ *           24 bits each (a relative 2^-17); out has the same bits either way.
  * k = 0 gives zeros.  m, n, k < 2^21, fewer than 2^22 tiles of 64 x 64 in each matrix.  x, the
  * weights, out and saved 16-byte aligned; what is written overlaps nothing else.
  */

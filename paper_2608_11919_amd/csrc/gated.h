@@ -178,13 +178,13 @@ constexpr Cost kPairCosts[] = {{256, 1, 1.37, 1.37, 14.5}, {128, 2, 0.62, 0.57, 
 // at most.  Without the reading and the rounds that share a CU it was 5% and up to twice as long: 512
 // x 5120 x 5120 gated in bf16 103 us for 67, 128 x 17408 x 5120 in integers 64 for 38; without slices
 // of a pair's sums 64 x 11008 x 2048 gated in bf16 53 for 23.
-// `pair`: a tile's columns are two weights'.  `cut`: whether sums may be.
-inline Way way_of(int64_t m, int64_t n, int steps, bool pair, bool cut = true)
+// `pair`: a tile's columns are two weights'.
+inline Way way_of(int64_t m, int64_t n, int steps, bool pair)
 {
     Way best{64, 1, steps};
     if (steps <= 0)
         return best;
-    const int weights = pair ? 2 : 1, most_slices = cut ? std::min(24, std::max(1, steps / 8)) : 1;
+    const int weights = pair ? 2 : 1, most_slices = std::min(24, std::max(1, steps / 8));
     const double reading = double(n) * steps * tiles::kStepBytes * weights / 6.2e6;
     double least = 1e300;
     for (const Cost& c : pair ? kPairCosts : kCosts) {

@@ -129,6 +129,32 @@ __device__ inline void save_eight(uint16_t* high, uint8_t* low, int64_t at, cons
         make_uint2(l[0] | l[1] << 16, l[2] | l[3] << 16);
 }
 
+// One of them.
+__device__ inline void save_one(uint16_t* high, uint8_t* low, int64_t at, float v)
+{
+    const uint32_t r = __float_as_uint(v) + 0x80u;
+    high[at] = uint16_t(r >> 16);
+    low[at] = uint8_t(r >> 8);
+}
+
+// A result from its sums; with SAVE what the backward pass needs of it is kept.
+template <bool SAVE>
+__device__ inline float answer_one(const Saved& saved, int activation, int64_t row, int64_t col,
+                                   float u, float v)
+{
+    const float g[1] = {u};
+    float b[1], a[1];
+    if constexpr (SAVE) {
+        gated::activate(activation, g, b, a);
+        const int64_t at = row * saved.pitch + col;
+        save_one(saved.a_high, saved.a_low, at, a[0] * v);
+        save_one(saved.b_high, saved.b_low, at, b[0]);
+    } else {
+        gated::activate(activation, g, b);
+    }
+    return b[0] * v;
+}
+
 __device__ inline void load_eight(const uint16_t* high, const uint8_t* low, int64_t at,
                                   float (&v)[8])
 {
@@ -218,28 +244,28 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void k_gated_f
     finish_pairs(tile, lds, w);
 }
 
-// Results of the slices' sums, added in their order, four loads under way at once.  Bound by
+// Results of the slices' sums, added in their order, four loads under way at once; with SAVE what the
+// backward pass needs of them is kept here (the tiles of a cut sum keep nothing).  Bound by
 // latency: 64 x 2048 from eight slices 4.0 us, a token's 5120 from sixteen 5.1 (one after the other
 // 7.4).
-template <bool F32>
+template <bool F32, bool SAVE>
 __global__ __launch_bounds__(256) void k_gated_answer(ForwardArgs g, int slices)
 {
     const int64_t all = g.m * g.n;
     for (int64_t e = int64_t(blockIdx.x) * 256 + threadIdx.x; e < all;
          e += int64_t(gridDim.x) * 256) {
-        float u[1] = {g.partial[e]}, v = g.partial[all + e];
+        float u = g.partial[e], v = g.partial[all + e];
 #pragma unroll 4
         for (int i = 1; i < slices; ++i) {
-            u[0] += g.partial[2 * i * all + e];
+            u += g.partial[2 * i * all + e];
             v += g.partial[(2 * i + 1) * all + e];
         }
-        float h[1];
-        gated::activate(g.activation, u, h);
-        const int64_t to = e / g.n * g.stride + e % g.n;
+        const int64_t row = e / g.n, col = e % g.n, to = row * g.stride + col;
+        const float h = answer_one<SAVE>(g.saved, g.activation, row, col, u, v);
         if constexpr (F32)
-            static_cast<float*>(g.out)[to] = h[0] * v;
+            static_cast<float*>(g.out)[to] = h;
         else
-            static_cast<uint16_t*>(g.out)[to] = gated::bf16_bits(h[0] * v);
+            static_cast<uint16_t*>(g.out)[to] = gated::bf16_bits(h);
     }
 }
 
@@ -255,6 +281,7 @@ struct FewArgs {
     int activation;
     void* out;
     int64_t stride;
+    Saved saved;
 };
 
 // 32 bytes of a row from byte `at` on; what lies behind its end is 0.
@@ -281,7 +308,7 @@ __device__ inline void few_load(const uint8_t* row, int64_t at, int64_t bytes, i
 // the waves cut the sum into runs of neighbouring steps.  An instruction is 16 rows x 16 tokens: a
 // lane holds 16 bytes of row and token l % 16, and ends with rows 4 (l / 16) + e of token l % 16.
 // One token through 2048 x 11008 16.9 us, 5.4 TB/s; 16 tokens 23.
-template <bool F32>
+template <bool F32, bool SAVE>
 __global__ __launch_bounds__(512) void k_few(FewArgs g)
 {
     extern __shared__ f32x4 few_sums[];  // [wave][B][lane], of 16 bytes
@@ -351,21 +378,19 @@ __global__ __launch_bounds__(512) void k_few(FewArgs g)
         for (int i = 1; i < waves; ++i)
             v[b] += from[i * B * 256];
     }
-    const float u[1] = {v[0]};
-    float a[1];
-    gated::activate(g.activation, u, a);
-    const float y = a[0] * v[1];
+    const float y = answer_one<SAVE>(g.saved, g.activation, tok, row, v[0], v[1]);
     if constexpr (F32)
         static_cast<float*>(g.out)[tok * g.stride + row] = y;
     else
         static_cast<uint16_t*>(g.out)[tok * g.stride + row] = gated::bf16_bits(y);
 }
 
-void launch_few(const FewArgs& g, bool f32, hipStream_t st)
+void launch_few(const FewArgs& g, bool f32, bool save, hipStream_t st)
 {
     const int64_t steps = (g.bytes + kStepBytes - 1) / kStepBytes;
     const int waves = steps >= 8 ? 8 : 4;
-    auto* kernel = f32 ? k_few<true> : k_few<false>;
+    auto* kernel = save ? (f32 ? k_few<true, true> : k_few<false, true>)
+                        : (f32 ? k_few<true, false> : k_few<false, false>);
     kernel<<<dim3(uint32_t((g.n + 15) / 16)), 64 * waves, size_t(waves) * 2 * 1024, st>>>(g);
 }
 
@@ -630,15 +655,16 @@ struct ForwardLayout {
 };
 
 ForwardLayout forward_layout(int64_t m, int64_t n, int64_t k, int64_t x_stride,
-                             int64_t gate_stride, int64_t up_stride, bool save)
+                             int64_t gate_stride, int64_t up_stride)
 {
     ForwardLayout l;
     const int64_t pitch = padded(k) * 2;
     const bool copy_x = !readable(k, x_stride), copy_gate = !readable(k, gate_stride),
                copy_up = !readable(k, up_stride);
     // tiles read a long sum faster, in slices (a token through 5120 x 2048 32 us and 26, through
-    // 11008 x 2048 29 and 23; through 2048 x 11008 21 and 27), but not what has to be copied first
-    l.few = !save && m <= gated::kFewTokens && (k <= 4096 || copy_x || copy_gate || copy_up);
+    // 11008 x 2048 29 and 23; through 2048 x 11008 21 and 27), but not what has to be copied first.
+    // Whether results are kept makes no difference here: h has the same bits either way
+    l.few = m <= gated::kFewTokens && (k <= 4096 || copy_x || copy_gate || copy_up);
     if (l.few) {
         l.total = host::kNoWorkspace;
         return l;
@@ -649,7 +675,7 @@ ForwardLayout forward_layout(int64_t m, int64_t n, int64_t k, int64_t x_stride,
         l.gate = take(l.total, n * pitch);
     if (copy_up)
         l.up = take(l.total, n * pitch);
-    l.way = way_of(m, n, int(padded(k) / kStep), true, !save);
+    l.way = way_of(m, n, int(padded(k) / kStep), true);
     if (l.way.slices > 1)
         l.partial = take(l.total, l.way.slices * m * n * 8);
     l.total = host::workspace_for(l.total);
@@ -955,10 +981,7 @@ size_t lt_gated_forward_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t
 {
     if (!valid_sizes(m, n, k))
         return 0;
-    const auto total = [&](bool save) {
-        return forward_layout(m, n, k, x_stride, gate_stride, up_stride, save).total;
-    };
-    return size_t(std::max(total(false), total(true)));
+    return size_t(forward_layout(m, n, k, x_stride, gate_stride, up_stride).total);
 }
 
 lt_err lt_gated_forward(const void* x, int64_t x_stride, const void* gate, int64_t gate_stride,
@@ -985,8 +1008,7 @@ try {
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const size_t out_bytes = span_bytes(m, n, out_stride, out_dtype);
     const size_t saved_bytes = saved ? lt_gated_saved_bytes(m, n) : 0;
-    const ForwardLayout l =
-        forward_layout(m, n, k, x_stride, gate_stride, up_stride, saved != nullptr);
+    const ForwardLayout l = forward_layout(m, n, k, x_stride, gate_stride, up_stride);
     const bool works =
         k > 0 && (l.x >= 0 || l.gate >= 0 || l.up >= 0 || l.partial >= 0);
     if (works && (!workspace || !host::aligned(workspace, 256) || workspace_bytes < size_t(l.total)))
@@ -1027,7 +1049,9 @@ try {
         f.activation = activation;
         f.out = out;
         f.stride = out_stride;
-        launch_few(f, f32, st);
+        if (saved)
+            f.saved = saved_layout(saved, m, n);
+        launch_few(f, f32, saved != nullptr, st);
         LT_TRY_HIP(hipGetLastError());
         return LT_OK;
     }
@@ -1062,14 +1086,16 @@ try {
     g.slice = l.way.slice;
     if (l.partial >= 0)
         g.partial = reinterpret_cast<float*>(ws + l.partial);
+    const bool keeps = saved && !g.partial;  // a cut sum's results are the last launch's
     if (l.way.tile == 256)
-        launch_forward<Large16>(g, l.way.slices, f32, saved != nullptr, st);
+        launch_forward<Large16>(g, l.way.slices, f32, keeps, st);
     else if (l.way.tile == 128)
-        launch_forward<Small16>(g, l.way.slices, f32, saved != nullptr, st);
+        launch_forward<Small16>(g, l.way.slices, f32, keeps, st);
     else
-        launch_forward<Pair16>(g, l.way.slices, f32, saved != nullptr, st);
+        launch_forward<Pair16>(g, l.way.slices, f32, keeps, st);
     if (g.partial) {
-        auto* answer = f32 ? k_gated_answer<true> : k_gated_answer<false>;
+        auto* answer = saved ? (f32 ? k_gated_answer<true, true> : k_gated_answer<false, true>)
+                             : (f32 ? k_gated_answer<true, false> : k_gated_answer<false, false>);
         answer<<<dim3(uint32_t(std::min<int64_t>(4096, host::ceil_div(m * n, 256)))), 256, 0, st>>>(
             g, l.way.slices);
     }

@@ -58,7 +58,7 @@ def _forward(x, gate, up, activation, out_dtype, keep, workspace):
     ws, nbytes, handle = 0, 0, _stream_handle(None, device)
     strides = x_stride | g_stride | u_stride
     copies = k % 64 or strides % 8 or strides >= 1 << 22
-    if workspace is not None or (copies if keep else m > 16 or k > 4096 and not copies):
+    if workspace is not None or m > 16 or (k > 4096 and not copies):
         need = int(lib().lt_gated_forward_workspace_bytes(m, n, k, x_stride, g_stride, u_stride))
         held, ws, nbytes = _call_workspace(device, need, workspace)
     with _current(device):
@@ -173,7 +173,7 @@ class GatedLinear(torch.autograd.Function):
     (for instance the optimizer's bf16 copies).  The backward pass reads x and the weights again:
     one of them changed in place meanwhile raises, like autograd's own.  First derivatives only: a
     backward pass that is itself to be differentiated raises, and so does a tangent of forward mode.
-    Where gradients are off it is gated_linear and keeps nothing.
+    Where gradients are off it is gated_linear and keeps nothing; the result has the same bits.
 
     Autograd adds up a leaf's gradient on the stream that its first graph was made on, for as long
     as a graph of the leaf lives.  Under capture that cannot be the default stream (the process would
