@@ -47,10 +47,12 @@ __device__ inline void copy_to_lds(const uint8_t* from, uint32_t offset, uint8_t
 {
     if constexpr (UNSEEN) {
         const uint32_t at = uint32_t(reinterpret_cast<uintptr_t>((LT_LDS void*)(to)));
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+        // the compiler sets m0, and knows what is there for copies that it makes itself; one state
+        // lies between
+        asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                      :
-                     : "s"(at), "v"(offset), "s"(from)
-                     : "memory");  // and m0, which nothing else uses in a kernel of such copies
+                     : "{m0}"(at), "v"(offset), "s"(from)
+                     : "memory");
     } else {
         __builtin_amdgcn_global_load_lds((const LT_GLOBAL void*)(from + offset), (LT_LDS void*)(to),
                                          16, 0, 0);
