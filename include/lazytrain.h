@@ -679,7 +679,9 @@ lt_err lt_int8_gated(const void* x, int dtype, int64_t x_stride, const int8_t* g
                      int activation, int64_t m, int64_t n, int64_t k, void* out, int out_dtype,
                      int64_t out_stride, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Bytes that lt_gated_forward keeps for the backward pass; 0 if an argument is invalid. */
+/* Bytes that lt_gated_forward keeps for the backward pass: six a result, whatever k is (below a k of
+ * some 1000 they take longer to write and read than the sums would to make again); 0 if an argument
+ * is invalid. */
 size_t lt_gated_saved_bytes(int64_t m, int64_t n);
 
 /* Bytes of device workspace lt_gated_forward needs: copies of operands whose rows are not whole
@@ -715,7 +717,7 @@ size_t lt_gated_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_
  *   dg = dh * u act'(g),  du = dh * act(g),
  *   dx = dg gate + du up,  dgate = dg^T x,  dup = du^T x.
  * dg and du are rounded to bf16 for the products, whose sums are fp32's; dx is rounded to dx_dtype,
- * the weights' gradients to grad_dtype.  dx may be NULL, and so may dgate and dup together: what only
+ * the weights' gradients to grad_dtype (fp32 leaves that last rounding out, not dg's and du's).  dx may be NULL, and so may dgate and dup together: what only
  * they need (the weights; x) is not looked at then.  saved is lt_gated_forward's.  Empty sums give
  * zeros.  x, the weights, saved and the gradients 16-byte aligned, dh to its elements; what is
  * written overlaps nothing else.

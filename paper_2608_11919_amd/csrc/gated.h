@@ -21,7 +21,8 @@ __device__ inline uint16_t bf16_bits(float x)
 }
 
 // 1 / (1 + e^-z), from the hardware's power of two and reciprocal, one unit in the last place each:
-// z * log2(e) is rounded before, which makes it |z| * 2^-24 relative.
+// z * log2(e) is rounded before, and log2(e) is a float 0.23 * 2^-24 off, which makes it 1.23 |z| *
+// 2^-24 relative.
 __device__ inline float logistic(float z)
 {
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f));
@@ -29,8 +30,10 @@ __device__ inline float logistic(float z)
 
 // Phi(-s) = e^(-s^2/2) t P(t) for s >= 0 with t = 1 / (1 + 0.35 s): the function beside the power
 // falls slowly and smoothly, and P, of degree 8, is its fit with the least largest relative error on
-// 0 <= s <= 14.5, 3.2e-8 (least squares, reweighted by the errors).  In fp32 within (s^2 + 15) *
-// 2^-24, mostly the power's argument; 0 from 13.2 on, where s Phi(-s) is below 2e-38.  4096
+// 0 <= s <= 14.5 (least squares, reweighted by the errors): 5.8e-8 with these coefficients, which
+// are floats, 3.2e-8 before.  In fp32 within (1.12 s^2 + 15) * 2^-24, mostly the power's argument
+// (a square, a constant 0.23 * 2^-24 off and a product); 0 from 13.2 on, where s Phi(-s) is below
+// 2e-38.  4096
 // x 2048 x 11008 in integers 228 us, with the library's erfc 279; kept in bf16 346 and 386.
 __device__ inline float tail(float s, float power)
 {

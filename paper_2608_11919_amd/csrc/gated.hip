@@ -397,7 +397,11 @@ void launch_few(const FewArgs& g, bool f32, bool save, hipStream_t st)
 // ------------------------------------------------------------- the backward pass
 
 // dg and du as the products read them, next to each other in rows of 2 * half values: zeros in
-// columns from n up to half, and in rows from m up to whole steps.
+// columns from n up to half, and in rows from m up to whole steps.  In bf16, the matrix cores'
+// operands: this rounding, half a step of each, is as large as that of a gradient in bf16.  The
+// gradients of 8192 x 2048 x 11008 lie 0.0023 from 64 bits (2-norm, relative), without it 0.0017.  A
+// second operand with what it leaves would double the products, four fifths of the backward pass's
+// time and more.
 struct SlopeArgs {
     const void* dh;
     int64_t stride;

@@ -90,7 +90,8 @@ def gated_linear_backward(dh: torch.Tensor, saved: torch.Tensor, x: torch.Tensor
                           out_dtype: torch.dtype = torch.bfloat16,
                           grad_dtype: torch.dtype = torch.bfloat16):
     """(dx, dgate, dup) of gated_linear_forward: dx in out_dtype with x's shape, the weights'
-    gradients in grad_dtype.  dh is float32 or bfloat16."""
+    gradients in grad_dtype (float32 leaves out their last rounding; the products' operands are
+    bfloat16 all the same).  dh is float32 or bfloat16."""
     return _backward(dh, saved, x, gate, up, tuple(x.shape[:-1]), tuple(gate.shape), out_dtype,
                      grad_dtype, True, True)
 
