@@ -686,8 +686,9 @@ size_t lt_gated_saved_bytes(int64_t m, int64_t n);
 
 /* Bytes of device workspace lt_gated_forward needs: copies of operands whose rows are not whole
  * steps of 64 values, not multiples of 8 or 2^22 and more apart, and partial sums where few results
- * share a long sum, more than 256 in all; else 256, which it does not look at.  Nothing is copied or looked at where m <=
- * 16 and k <= 4096 or an operand is such a one.  0 if an argument is invalid. */
+ * share a long sum, more than 256 in all; else 256, which it does not look at.  Nothing is copied
+ * or looked at where m <= 16 and k <= 4096 or an operand is such a one.  0 if an argument is
+ * invalid. */
 size_t lt_gated_forward_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t x_stride,
                                         int64_t gate_stride, int64_t up_stride);
 
@@ -716,11 +717,12 @@ size_t lt_gated_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_
  * f14: the gradients of f13 from dh, out's (m x n, dh_dtype):
  *   dg = dh * u act'(g),  du = dh * act(g),
  *   dx = dg gate + du up,  dgate = dg^T x,  dup = du^T x.
- * dg and du are rounded to bf16 for the products, whose sums are fp32's; dx is rounded to dx_dtype,
- * the weights' gradients to grad_dtype (fp32 leaves that last rounding out, not dg's and du's).  dx may be NULL, and so may dgate and dup together: what only
- * they need (the weights; x) is not looked at then.  saved is lt_gated_forward's.  Empty sums give
- * zeros.  x, the weights, saved and the gradients 16-byte aligned, dh to its elements; what is
- * written overlaps nothing else.
+ * dg and du are rounded to bf16 for the products, whose sums are fp32's; dx is rounded to
+ * dx_dtype, the weights' gradients to grad_dtype (fp32 leaves that last rounding out, not dg's
+ * and du's).  dx may be NULL, and so may dgate and dup together: what only they need (the
+ * weights; x) is not looked at then.  saved is lt_gated_forward's.  Empty sums give zeros.  x,
+ * the weights, saved and the gradients 16-byte aligned, dh to its elements; what is written
+ * overlaps nothing else.
  */
 lt_err lt_gated_backward(const void* dh, int dh_dtype, int64_t dh_stride, const void* saved,
                          const void* x, int64_t x_stride, const void* gate, int64_t gate_stride,
